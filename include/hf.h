@@ -427,6 +427,137 @@ int32_t hf_prof_count(hf_ctx* ctx);
 int hf_prof_get(hf_ctx* ctx, int32_t i, const char** name, int64_t* launches,
                 double* total_ms, double* flops, double* bytes);
 
+/*
+ * ------------------------------------------------------------------------
+ * The vocabulary ends of a token model: the embedding in front of a net, and
+ * behind it the softmax head over a vocabulary larger than HF_MAX_CLASSES,
+ * with the loss of hard labels or of a teacher's top logits.  With tied
+ * weights the embedding and the head share one matrix and one gradient.
+ *
+ * A context (hf_vocab) holds the vocabulary V, the width D and the type of
+ * the rows, the matrices and their gradients: fp32 or bf16 (sums, softmax
+ * statistics and losses are fp32, the sum over the rows fp64; each output is
+ * rounded to its type once).  Matrices are row-major; rows may lie `ld`
+ * elements apart and start at any element (rows of 16-byte multiples and
+ * widths that are multiples of 64 are read in place, others are packed in
+ * the workspace first).
+ * Labels, tokens and ids are int32 in [0, V), or HF_IGNORE where a place is
+ * masked; any other value counts as masked and raises HF_ELABEL in the next
+ * hf_vocab_check.  Rows without a target count nothing: no loss, a zero row
+ * of dX, nothing in dW, whatever X holds there.
+ * Memory, streams and errors as for hf_ctx: device pointers owned by the
+ * caller, one caller-provided workspace, everything asynchronous on the
+ * context's stream, HF_* codes.  Calls make no allocation and can be captured
+ * into a graph.  Work enqueued on one stream is ordered behind the context's
+ * earlier calls on another; captured calls, and graphs that share a
+ * workspace, are the caller's to order.  The current device must be the
+ * stream's.  Repeated calls give the same bits, whatever the workspace's size.
+ */
+typedef struct hf_vocab hf_vocab;
+
+enum { HF_TYPE_FP32 = 0, HF_TYPE_BF16 = 1 };
+/* A masked label, token or id. */
+#define HF_IGNORE (-100)
+/* Limits: vocabulary, width, rows per call, teacher logits per row. */
+#define HF_VOCAB_MAX (1 << 22)
+#define HF_VOCAB_MAX_WIDTH 65536
+#define HF_VOCAB_MAX_ROWS 262144
+#define HF_VOCAB_MAX_TOP 128
+
+/* Build a context for calls of up to max_rows rows; HF_EINVAL outside the
+ * limits.  No device call is made. */
+int hf_vocab_create(int64_t vocab, int32_t width, int32_t type,
+                    int64_t max_rows, void* hip_stream, hf_vocab** out);
+/* Free a context.  NULL is ok. */
+int hf_vocab_destroy(hf_vocab* ctx);
+/* Stream (a hipStream_t) of later calls; NULL = null stream. */
+int hf_vocab_set_stream(hf_vocab* ctx, void* hip_stream);
+/* Bytes of workspace for calls of up to `rows` rows (<= 0: max_rows); 0 for a
+ * NULL context or rows > max_rows.  Grows with rows. */
+size_t hf_vocab_workspace_bytes(const hf_vocab* ctx, int64_t rows);
+/* Hand over a device workspace, 256-byte aligned; calls with more rows than
+ * its bytes serve return HF_EWORKSPACE.  Synchronises the device. */
+int hf_vocab_set_workspace(hf_vocab* ctx, void* dev_ptr, size_t bytes);
+
+/*
+ * hf_vocab_loss: softmax cross entropy of the logits z = X W^T,
+ *   l_i = logsumexp(z_i) - z_{i, y_i},  loss = sum_i l_i / denom
+ * in tiles of the vocabulary: the logits are never stored.
+ *   X         rows x D, ldx >= D elements apart
+ *   W         V x D, ldw apart
+ *   y         rows labels
+ *   denom     divides the sum; 0: the number of counted rows (loss 0 if none)
+ *   loss      1 fp32
+ *   row_loss  rows fp32 (0 where a row does not count), or NULL
+ */
+int hf_vocab_loss(hf_vocab* ctx, const void* X, int64_t ldx, const void* W,
+                  int64_t ldw, const int32_t* y, int64_t rows, float denom,
+                  float* loss, float* row_loss);
+
+/*
+ * hf_vocab_loss_grad: hf_vocab_loss and its gradients
+ *   dX = delta W (rows x D),  dW = delta^T X (V x D),
+ *   delta = (softmax(z) - e_y) / denom.
+ * Where the call's logits fit 1.5 GiB they are kept in the workspace, else
+ * they are computed again a piece of the vocabulary at a time.  delta is
+ * rounded to the type (bf16 calls of up to 128 rows: to two terms of it) for
+ * the two products.
+ *   dX, dW      either may be NULL (not both): not computed
+ *   accumulate  1: dW += instead of dW = (with tied weights, or over
+ *               minibatches); dX is always written whole
+ */
+int hf_vocab_loss_grad(hf_vocab* ctx, const void* X, int64_t ldx,
+                       const void* W, int64_t ldw, const int32_t* y,
+                       int64_t rows, float denom, float* loss, float* row_loss,
+                       void* dX, int64_t lddx, void* dW, int64_t lddw,
+                       int32_t accumulate);
+
+/*
+ * hf_vocab_distill: divergence from a teacher known by the top logits of each
+ * row, at temperature tau:
+ *   q_i = softmax(t_i / tau) over the row's list,  p_i = softmax(z_i / tau)
+ *   over the vocabulary,
+ *   l_i = tau^2 sum over the listed ids v of q_iv (log q_iv - log p_iv)
+ *   ids  rows x top ids, ldi apart; HF_IGNORE where the list has ended
+ *   t    rows x top fp32 teacher logits, ldt apart; -inf counts as masked
+ *   top  1 .. HF_VOCAB_MAX_TOP;  tau in [1e-4, 1e4]
+ * An id that a row lists twice has the sum of its probabilities as q_iv.
+ * Other arguments as for hf_vocab_loss.
+ */
+int hf_vocab_distill(hf_vocab* ctx, const void* X, int64_t ldx, const void* W,
+                     int64_t ldw, const int32_t* ids, int64_t ldi,
+                     const float* t, int64_t ldt, int32_t top, float tau,
+                     int64_t rows, float denom, float* loss, float* row_loss);
+
+/* hf_vocab_distill_grad: hf_vocab_distill and its gradients, those of
+ * hf_vocab_loss_grad with delta = tau (p - q) / denom. */
+int hf_vocab_distill_grad(hf_vocab* ctx, const void* X, int64_t ldx,
+                          const void* W, int64_t ldw, const int32_t* ids,
+                          int64_t ldi, const float* t, int64_t ldt,
+                          int32_t top, float tau, int64_t rows, float denom,
+                          float* loss, float* row_loss, void* dX, int64_t lddx,
+                          void* dW, int64_t lddw, int32_t accumulate);
+
+/* hf_vocab_embed: out_i = scale E[tok_i] (rows x D, ldo apart), zeros where
+ * tok_i is masked.  E is V x D, lde apart; scale finite. */
+int hf_vocab_embed(hf_vocab* ctx, const void* E, int64_t lde,
+                   const int32_t* tok, int64_t rows, float scale, void* out,
+                   int64_t ldo);
+
+/* hf_vocab_embed_grad: its gradient, dE_v = scale sum_{i: tok_i = v} dout_i
+ * (V x D, lde apart), summed in fp32 in a fixed order; rows of dE without a
+ * token are zero.  accumulate = 1: dE += instead (rows without a token are
+ * left as they are). */
+int hf_vocab_embed_grad(hf_vocab* ctx, const int32_t* tok, int64_t rows,
+                        float scale, const void* dout, int64_t ldd, void* dE,
+                        int64_t lde, int32_t accumulate);
+
+/* Synchronise the stream and report HF_ELABEL raised since the last check;
+ * clears the flag. */
+int hf_vocab_check(hf_vocab* ctx);
+/* Message for the last failed call on ctx. */
+const char* hf_vocab_last_error(const hf_vocab* ctx);
+
 #ifdef __cplusplus
 }
 #endif

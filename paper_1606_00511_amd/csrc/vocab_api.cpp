@@ -1,0 +1,642 @@
+// Host side of the vocabulary calls declared in include/hf.h: context,
+// argument validation, workspace carve-up and the order of the kernels.
+//
+// The head works on packed rows (the N that count, N known to the device
+// only) in one of two ways, chosen by the call's sizes:
+//   kept        the logits of the call fit KEEP_BYTES: computed once, kept in
+//               fp32, turned into delta
+//   recomputed  one pass over the whole vocabulary for the statistics, then
+//               piece by piece the logits again, straight into delta, and the
+//               piece's share of dX and rows of dW
+// A loss without its gradient never keeps a logit.
+#include "hf.h"
+#include "vocab_internal.h"
+
+#include <algorithm>
+#include <cmath>
+#include <cstdarg>
+#include <cstdio>
+#include <new>
+#include <string>
+
+using namespace hfk;
+
+namespace {
+
+constexpr size_t MiB = (size_t)1 << 20;
+constexpr size_t KEEP_BYTES = 1536 * MiB;    // logits (and bf16 delta) kept
+constexpr size_t PIECE_BYTES = 512 * MiB;    // delta of a recomputed piece
+constexpr size_t WPACK_BYTES = 256 * MiB;    // packed rows of W
+constexpr int64_t MAX_LD = (int64_t)1 << 22; // in-tile offsets are 32 bits
+constexpr int TWO_TERM_ROWS = 128;
+constexpr int SPLIT_TILES = 512;             // partials: at most so many 128 x 128 tiles
+constexpr size_t SPLIT_FLOATS = (size_t)SPLIT_TILES * 128 * 128;
+
+inline int64_t up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
+
+struct Layout {
+  size_t state, pos, idx, rloss, lse, zt, tid, tdt, stat, xp, wp, z, partx, partw;
+  size_t key, spos, tkey, tpos, hist, epart, need;
+};
+
+}  // namespace
+
+struct hf_vocab {
+  int V = 0, D = 0, Dp = 0, type = 0, es = 0;
+  int64_t Rmax = 0, Rws = 0;
+  hipStream_t stream = nullptr;
+  char* ws = nullptr;
+  Layout lay = {};
+  hipEvent_t last = nullptr;       // the last call's work
+  hipStream_t last_stream = nullptr;
+  bool pending = false;
+  std::string err;
+
+  template <class T>
+  T* at(size_t off) const { return reinterpret_cast<T*>(ws + off); }
+  VocabState* st() const { return at<VocabState>(lay.state); }
+};
+
+namespace {
+
+int fail(hf_vocab* c, int code, const char* fmt, ...) __attribute__((format(printf, 3, 4)));
+int fail(hf_vocab* c, int code, const char* fmt, ...) {
+  if (c) {
+    char buf[512];
+    va_list ap;
+    va_start(ap, fmt);
+    vsnprintf(buf, sizeof buf, fmt, ap);
+    va_end(ap);
+    c->err = buf;
+  }
+  return code;
+}
+
+#define HIP_TRY(ctx, expr)                                                     \
+  do {                                                                         \
+    hipError_t e_ = (expr);                                                    \
+    if (e_ != hipSuccess)                                                      \
+      return fail(ctx, HF_EHIP, "%s failed: %s", #expr, hipGetErrorString(e_)); \
+  } while (0)
+
+// ------------------------------------------------------------------ sizes
+// Rows of delta: whole tiles; few rows of bf16 come twice (see two_term).
+inline int64_t tile_rows(int64_t T) { return std::max<int64_t>(up(T, VTILE), VTILE); }
+
+// bf16 calls of at most TWO_TERM_ROWS rows hold delta as two bf16 terms: with
+// few rows nothing averages the rounding of the label's entry, and the matrix
+// cores wait for W anyway.
+inline int two_term(const hf_vocab* c, int64_t T) {
+  return c->type == VT_BF16 && T > 0 && T <= TWO_TERM_ROWS ? (int)up(T, VPAD) : 0;
+}
+inline size_t keep_bytes(const hf_vocab* c, int64_t T) {
+  const size_t Vp = (size_t)up(c->V, VTILE), R = (size_t)tile_rows(T);
+  return R * Vp * 4 + (c->type == VT_BF16 ? R * Vp * 2 : 0);
+}
+inline bool keeps(const hf_vocab* c, int64_t T) {
+  return T <= TWO_TERM_ROWS || keep_bytes(c, T) <= KEEP_BYTES;
+}
+// columns of a recomputed piece
+inline int piece_cols(const hf_vocab* c, int64_t T) {
+  int64_t n = (int64_t)(PIECE_BYTES / ((size_t)tile_rows(T) * c->es)) / 1024 * 1024;
+  n = std::max<int64_t>(n, 1024);
+  const int64_t pieces = (c->V + n - 1) / n;      // of even sizes
+  return (int)std::min<int64_t>(up(c->V, VTILE), up((c->V + pieces - 1) / pieces, 1024));
+}
+// rows of W packed at a time
+inline int pack_rows(const hf_vocab* c) {
+  const int64_t n = (int64_t)(WPACK_BYTES / ((size_t)c->Dp * c->es)) / 1024 * 1024;
+  return (int)std::min<int64_t>(c->V, std::max<int64_t>(n, 1024));
+}
+inline size_t z_bytes(const hf_vocab* c, int64_t T) {
+  if (keeps(c, T)) return keep_bytes(c, T);
+  return (size_t)tile_rows(T) * up(piece_cols(c, T), VTILE) * c->es;
+}
+
+void plan(const hf_vocab* c, int64_t R, Layout* l) {
+  size_t off = 0;
+  auto take = [&](size_t bytes) {
+    const size_t o = off;
+    off += (bytes + 255) & ~size_t(255);
+    return o;
+  };
+  const size_t r = (size_t)R, Rp = (size_t)tile_rows(R);
+  l->state = take(sizeof(VocabState));
+  l->pos = take(r * 4);
+  l->idx = take(r * 4);
+  l->rloss = take(r * 4);
+  l->lse = take(Rp * 4);
+  l->zt = take(r * HF_VOCAB_MAX_TOP * 4);
+  l->tid = take(r * HF_VOCAB_MAX_TOP * 4);
+  l->tdt = take(r * HF_VOCAB_MAX_TOP * 4);
+  l->stat = take(r * (size_t)((c->V + VSTAT - 1) / VSTAT + 8) * sizeof(float2));
+  l->xp = take(Rp * c->Dp * c->es);
+  l->wp = take((size_t)pack_rows(c) * c->Dp * c->es);
+  // what the largest of up to R rows needs: kept logits up to the last row
+  // count that keeps them, or pieces
+  size_t zb = z_bytes(c, R);
+  if (!keeps(c, R)) {
+    int64_t lo = 1, hi = R;             // keeps(lo), not keeps(hi)
+    while (hi - lo > 1) {
+      const int64_t mid = lo + (hi - lo) / 2;
+      if (keeps(c, mid)) lo = mid;
+      else hi = mid;
+    }
+    zb = std::max(keep_bytes(c, lo), (size_t)PIECE_BYTES);
+    zb = std::max(zb, z_bytes(c, R));
+  }
+  l->z = take(zb);
+  l->partx = take(std::max(Rp * (size_t)c->Dp, SPLIT_FLOATS) * 4);
+  l->partw = take(SPLIT_FLOATS * 4);
+  l->key = take(r * 4);
+  l->spos = take(r * 4);
+  l->tkey = take(r * 4);
+  l->tpos = take(r * 4);
+  l->hist = take(vocab_sort_hist(R, c->V) * 4);
+  l->epart = take(vocab_sort_part(R, c->D, c->type) * 4);
+  l->need = off;
+}
+size_t plan_bytes(const hf_vocab* c, int64_t R) {
+  Layout l;
+  plan(c, R, &l);
+  return l.need;
+}
+
+// ----------------------------------------------------------------- checks
+// (arguments first, then whether the workspace serves the rows)
+int check_rows(hf_vocab* c, int64_t T) {
+  if (T < 0 || T > c->Rmax)
+    return fail(c, HF_EINVAL, "%lld rows outside [0, %lld]", (long long)T, (long long)c->Rmax);
+  return HF_OK;
+}
+int check_ready(hf_vocab* c, int64_t T) {
+  if (!c->ws) return fail(c, HF_EWORKSPACE, "no workspace set (hf_vocab_set_workspace)");
+  if (T > c->Rws)
+    return fail(c, HF_EWORKSPACE, "%lld rows above the %lld the workspace serves", (long long)T,
+                (long long)c->Rws);
+  return HF_OK;
+}
+// a rows x D array of elements of es bytes, rows ld elements apart
+int check_mat(hf_vocab* c, const void* p, int64_t ld, int64_t cols, int es, int64_t rows,
+              const char* what) {
+  if (rows == 0) return HF_OK;
+  if (!p) return fail(c, HF_EINVAL, "%s is NULL", what);
+  if ((uintptr_t)p % es) return fail(c, HF_EINVAL, "%s is not aligned to its elements", what);
+  if (ld < cols || ld > ((int64_t)1 << 31))
+    return fail(c, HF_EINVAL, "rows of %s are %lld elements apart, %lld wide", what,
+                (long long)ld, (long long)cols);
+  return HF_OK;
+}
+
+// -------------------------------------------------------------- the passes
+// Work of a call on this stream follows that of the context's last call on
+// another: they share the workspace.  (Calls that are being captured are the
+// caller's to order.)
+int begin(hf_vocab* c, bool* captured) {
+  hipStreamCaptureStatus cs = hipStreamCaptureStatusNone;
+  HIP_TRY(c, hipStreamIsCapturing(c->stream, &cs));
+  *captured = cs != hipStreamCaptureStatusNone;
+  if (!*captured && c->pending && c->last_stream != c->stream)
+    HIP_TRY(c, hipStreamWaitEvent(c->stream, c->last, 0));
+  return HF_OK;
+}
+int end(hf_vocab* c, bool captured) {
+  HIP_TRY(c, hipGetLastError());
+  if (captured) return HF_OK;
+  if (!c->last) HIP_TRY(c, hipEventCreateWithFlags(&c->last, hipEventDisableTiming));
+  HIP_TRY(c, hipEventRecord(c->last, c->stream));
+  c->last_stream = c->stream;
+  c->pending = true;
+  return HF_OK;
+}
+
+int splits_for(int M, int N, int K, int cap) {
+  const int64_t tiles = (int64_t)((M + 127) / 128) * ((N + 127) / 128);
+  int s = 1;
+  while (2 * s * tiles <= SPLIT_TILES && 2 * s <= cap && K / (2 * s) >= 256) s *= 2;
+  return s;
+}
+// 256 x 256 tiles once they give every compute unit a workgroup
+bool big_tiles(int64_t M, int64_t N) {
+  return ((M + 255) / 256) * ((N + 255) / 256) >= 224;
+}
+
+struct Grad {
+  void* dX;
+  int64_t lddx;
+  void* dW;
+  int64_t lddw;
+  int accumulate;
+};
+
+void head(hf_vocab* c, VRows r, const void* X, int64_t ldx, const void* W, int64_t ldw,
+          float* loss, const Grad* g) {
+  const Launch L{c->stream, nullptr};
+  const Layout& l = c->lay;
+  const int T = r.T, V = c->V, D = c->D, Dp = c->Dp, type = c->type, es = c->es;
+  r.V = V;
+  r.D = D;
+  r.st = c->st();
+  r.pos = c->at<int>(l.pos);
+  r.idx = c->at<int>(l.idx);
+  if (!r.row_loss) r.row_loss = c->at<float>(l.rloss);
+  const bool keep = g && keeps(c, T);
+  const int dup = keep ? two_term(c, T) : 0;
+  float* lse = c->at<float>(l.lse);
+  float2* stat = c->at<float2>(l.stat);
+  void* xp = c->at<void>(l.xp);
+
+  vocab_count(L, r);
+  vocab_pack_rows(L, type, r, X, ldx, xp, Dp, dup, g ? g->dX : nullptr, g ? g->lddx : 0);
+
+  // W as it is where the GEMMs' 16-byte loads can read it, else packed, at
+  // most pack_rows at a time
+  const bool direct = D % VPAD == 0 && ldw <= MAX_LD && (uintptr_t)W % 16 == 0 &&
+                      (ldw * es) % 16 == 0;
+  const int wrows = direct ? V : pack_rows(c);
+  int packed = -1;                      // first row of the packed piece
+  auto matrix = [&](int v0, int n, long long* ld) -> const void* {
+    if (direct) {
+      *ld = ldw;
+      return (const char*)W + (size_t)v0 * ldw * es;
+    }
+    void* wp = c->at<void>(l.wp);
+    if (packed != v0)
+      vocab_pack_matrix(L, type, (const char*)W + (size_t)v0 * ldw * es, ldw, n, D, wp, Dp);
+    packed = v0;
+    *ld = Dp;
+    return wp;
+  };
+
+  // ---- statistics (and kept logits) of the whole vocabulary
+  float* z = keep ? c->at<float>(l.z) : nullptr;
+  const long long ldz = up(V, VTILE);
+  const bool big = big_tiles(V, T);
+  const int stile = big ? 256 : 128;
+  const int tiles = (V + stile - 1) / stile;
+  VEpi e = {};
+  e.zscale = 1.0f / r.tau;
+  e.stat = stat;
+  e.ldstat = tiles;
+  for (int v0 = 0; v0 < V; v0 += wrows) {
+    const int n = std::min(wrows, V - v0);
+    VGemm q = {};
+    q.A = matrix(v0, n, &q.lda);
+    q.B = xp;
+    q.ldb = Dp;
+    q.M = n;
+    q.N = T;
+    q.K = Dp;
+    q.alim = n;
+    q.st = r.st;
+    q.dyn = 1;
+    q.splits = 1;
+    q.big = big;
+    e.tile0 = v0 / stile;
+    e.z = z ? z + v0 : nullptr;
+    e.ldz = ldz;
+    vocab_logits(L, type, q, e);
+  }
+
+  // ---- losses
+  VTarget tg = {c->at<float>(l.zt), nullptr, nullptr};
+  if (g) {
+    tg.id = c->at<int>(l.tid);
+    tg.dt = c->at<float>(l.tdt);
+  }
+  if (!keep && T > 0) vocab_target_logits(L, type, r, xp, Dp, W, ldw, tg.zt);
+  vocab_row_loss(L, r, stat, tiles, tiles, z, ldz, tg, lse);
+  vocab_loss_sum(L, r, loss);
+  if (!g) return;
+
+  // ---- gradients, piece by piece
+  const int Rp = (int)tile_rows(T);
+  void* d;
+  long long ldd;
+  int vc;
+  if (keep) {
+    ldd = ldz;
+    d = type == VT_F32 ? (void*)z : (void*)(z + (size_t)Rp * ldz);
+    vc = V;
+    const int rows = dup ? dup : (int)up(T, VPAD);
+    if (T > 0)
+      vocab_delta(L, type, r, z, ldz, lse, tg, rows, d, ldd, (int)up(V, VPAD), dup);
+  } else {
+    vc = piece_cols(c, T);
+    ldd = up(vc, VTILE);
+    d = c->at<void>(l.z);
+  }
+  // rows of dX's products: the counted ones, or both terms of few
+  const int xrows = dup ? 2 * dup : T;
+  float* partx = c->at<float>(l.partx);
+  int xsplits = 1, xbig = 0;
+  long long xstride = 0;
+  for (int p0 = 0; p0 < V; p0 += vc) {
+    const int pn = std::min(vc, V - p0);
+    // a piece of delta covers several packed pieces of W where logits are kept
+    for (int v0 = p0; v0 < p0 + pn; v0 += wrows) {
+      const int n = std::min(wrows, p0 + pn - v0);
+      long long lda = 0;
+      const void* A = nullptr;
+      if (!keep || g->dX) A = matrix(v0, n, &lda);
+      char* dv = (char*)d + (size_t)(v0 - p0) * es;
+      if (!keep) {
+        VGemm q = {};
+        q.A = A;
+        q.lda = lda;
+        q.B = xp;
+        q.ldb = Dp;
+        q.M = n;
+        q.N = T;
+        q.K = Dp;
+        q.alim = n;
+        q.st = r.st;
+        q.dyn = 1;
+        q.splits = 1;
+        q.big = big_tiles(n, T);
+        VEpi pe = {};
+        pe.zscale = 1.0f / r.tau;
+        pe.lse = lse;
+        pe.d = dv;
+        pe.ldd = ldd;
+        vocab_probs(L, type, q, pe);
+        vocab_fix(L, type, r, tg, v0, n, dv, ldd);
+      }
+      if (!g->dX || T < 1) continue;
+      VGemm q = {};
+      q.A = A;
+      q.lda = lda;
+      q.B = dv;
+      q.ldb = ldd;
+      q.M = D;
+      q.N = xrows;
+      q.K = n;
+      q.alim = n;
+      q.st = r.st;
+      q.dyn = dup ? 0 : 1;
+      if (v0 == 0) {
+        xbig = big_tiles(D, xrows);
+        xsplits = xbig ? 1 : splits_for(D, xrows, n, VMAX_SPLITS);
+        xstride = up(xrows, 128) * Dp;
+      }
+      q.splits = xsplits;
+      q.big = xbig;
+      VEpi pe = {};
+      pe.part = partx;
+      pe.ldp = Dp;
+      pe.split_stride = xstride;
+      pe.add = v0 > 0;
+      vocab_dx(L, type, q, pe);
+    }
+    if (!g->dW) continue;
+    VGemm q = {};
+    q.A = xp;
+    q.lda = Dp;
+    q.B = d;
+    q.ldb = ldd;
+    q.M = D;
+    q.N = pn;
+    q.K = dup ? 2 * dup : (int)up(T, VPAD);
+    q.alim = dup ? 2 * dup : Rp;
+    q.st = r.st;
+    q.dyn = dup ? 0 : 2;
+    q.big = big_tiles(D, pn);
+    q.splits = q.big ? 1 : splits_for(D, pn, q.K, VMAX_SPLITS);
+    VEpi pe = {};
+    char* out = (char*)g->dW + (size_t)p0 * g->lddw * es;
+    pe.part = c->at<float>(l.partw);
+    pe.ldp = Dp;
+    pe.split_stride = up(pn, 128) * Dp;
+    pe.out = out;
+    pe.ldo = g->lddw;
+    pe.accumulate = g->accumulate;
+    pe.vec = g->lddw % 4 == 0 && (uintptr_t)out % (4 * es) == 0;
+    vocab_dw(L, type, q, pe);
+    if (q.splits > 1)
+      vocab_finish(L, type, r.st, pe.part, q.splits, pe.split_stride, Dp, 0, pn, 0, D, nullptr,
+                   out, g->lddw, g->accumulate);
+  }
+  if (g->dX && T > 0)
+    vocab_finish(L, type, r.st, partx, xsplits, xstride, Dp, dup, T, 1, D, r.idx, g->dX,
+                 g->lddx, 0);
+}
+
+// arguments of a head call, then its work
+int head_call(hf_vocab* c, const void* X, int64_t ldx, const void* W, int64_t ldw,
+              const int32_t* ids, int64_t ldi, const float* t, int64_t ldt, int32_t K, float tau,
+              int64_t T, float denom, float* loss, float* row_loss, const Grad* g,
+              const char* ids_name) {
+  int rc;
+  if (!c) return HF_EINVAL;
+  if ((rc = check_rows(c, T)) ||
+      (rc = check_mat(c, X, ldx, c->D, c->es, T, "X")) ||
+      (rc = check_mat(c, W, ldw, c->D, c->es, c->V, "W")) ||
+      (rc = check_mat(c, ids, ldi, K, 4, T, ids_name)) ||
+      (t && (rc = check_mat(c, t, ldt, K, 4, T, "t"))) ||
+      (rc = check_mat(c, loss, 1, 1, 4, 1, "loss")) ||
+      (row_loss && (rc = check_mat(c, row_loss, 1, 1, 4, T, "row_loss"))))
+    return rc;
+  if (!(denom >= 0.0f) || std::isinf(denom))
+    return fail(c, HF_EINVAL, "denom %g is not a finite number >= 0", (double)denom);
+  if (g) {
+    if (!g->dX && !g->dW) return fail(c, HF_EINVAL, "neither dX nor dW given");
+    if ((g->dX && (rc = check_mat(c, g->dX, g->lddx, c->D, c->es, T, "dX"))) ||
+        (g->dW && (rc = check_mat(c, g->dW, g->lddw, c->D, c->es, c->V, "dW"))))
+      return rc;
+    if (g->accumulate != 0 && g->accumulate != 1)
+      return fail(c, HF_EINVAL, "accumulate %d is neither 0 nor 1", g->accumulate);
+  }
+  if ((rc = check_ready(c, T))) return rc;
+  VRows r = {};
+  r.T = (int)T;
+  r.K = K;
+  r.ids = ids;
+  r.ldi = ldi;
+  r.t = t;
+  r.ldt = ldt;
+  r.tau = tau;
+  r.denom = denom;
+  r.row_loss = row_loss;
+  bool captured;
+  if ((rc = begin(c, &captured))) return rc;
+  head(c, r, X, ldx, W, ldw, loss, g);
+  return end(c, captured);
+}
+
+int check_list(hf_vocab* c, const float* t, int64_t T, int32_t K, float tau) {
+  if (!c) return HF_EINVAL;
+  if (T > 0 && !t) return fail(c, HF_EINVAL, "t is NULL");
+  if (K < 1 || K > HF_VOCAB_MAX_TOP)
+    return fail(c, HF_EINVAL, "%d teacher logits per row outside [1, %d]", K, HF_VOCAB_MAX_TOP);
+  // 1 / tau and tau^2 stay finite and normal
+  if (!(tau >= 1e-4f && tau <= 1e4f))
+    return fail(c, HF_EINVAL, "tau %g outside [1e-4, 1e4]", (double)tau);
+  return HF_OK;
+}
+
+}  // namespace
+
+// ==================================================================== C ABI
+extern "C" {
+
+int hf_vocab_create(int64_t vocab, int32_t width, int32_t type, int64_t max_rows,
+                    void* hip_stream, hf_vocab** out) {
+  if (!out) return HF_EINVAL;
+  *out = nullptr;
+  if (vocab < 1 || vocab > HF_VOCAB_MAX || width < 1 || width > HF_VOCAB_MAX_WIDTH ||
+      (type != HF_TYPE_FP32 && type != HF_TYPE_BF16) || max_rows < 1 ||
+      max_rows > HF_VOCAB_MAX_ROWS)
+    return HF_EINVAL;
+  hf_vocab* c = new (std::nothrow) hf_vocab();
+  if (!c) return HF_ENOMEM;
+  c->V = (int)vocab;
+  c->D = width;
+  c->Dp = (int)up(width, VPAD);
+  c->type = type;
+  c->es = type == HF_TYPE_FP32 ? 4 : 2;
+  c->Rmax = max_rows;
+  c->stream = reinterpret_cast<hipStream_t>(hip_stream);
+  *out = c;
+  return HF_OK;
+}
+
+int hf_vocab_destroy(hf_vocab* c) {
+  if (!c) return HF_OK;
+  if (c->last) (void)hipEventDestroy(c->last);
+  delete c;
+  return HF_OK;
+}
+
+int hf_vocab_set_stream(hf_vocab* c, void* s) {
+  if (!c) return HF_EINVAL;
+  c->stream = reinterpret_cast<hipStream_t>(s);
+  return HF_OK;
+}
+
+size_t hf_vocab_workspace_bytes(const hf_vocab* c, int64_t rows) {
+  if (!c) return 0;
+  if (rows <= 0) rows = c->Rmax;
+  if (rows > c->Rmax) return 0;
+  return plan_bytes(c, rows);
+}
+
+int hf_vocab_set_workspace(hf_vocab* c, void* p, size_t bytes) {
+  if (!c) return HF_EINVAL;
+  if (!p) return fail(c, HF_EINVAL, "workspace pointer is NULL");
+  if ((uintptr_t)p & 255u) return fail(c, HF_EINVAL, "workspace is not 256-byte aligned");
+  const size_t need1 = plan_bytes(c, 1);
+  if (bytes < need1)
+    return fail(c, HF_EWORKSPACE, "workspace of %zu bytes is smaller than the %zu needed "
+                "for one row", bytes, need1);
+  // the largest number of rows whose layout fits (it grows with the rows)
+  int64_t lo = 1, hi = c->Rmax;
+  while (lo < hi) {
+    const int64_t mid = lo + (hi - lo + 1) / 2;
+    if (plan_bytes(c, mid) <= bytes) lo = mid;
+    else hi = mid - 1;
+  }
+  c->ws = nullptr;
+  plan(c, lo, &c->lay);
+  c->Rws = lo;
+  c->pending = false;
+  HIP_TRY(c, hipMemset((char*)p + c->lay.state, 0, sizeof(VocabState)));
+  HIP_TRY(c, hipDeviceSynchronize());
+  c->ws = reinterpret_cast<char*>(p);
+  return HF_OK;
+}
+
+int hf_vocab_loss(hf_vocab* c, const void* X, int64_t ldx, const void* W, int64_t ldw,
+                  const int32_t* y, int64_t rows, float denom, float* loss, float* row_loss) {
+  return head_call(c, X, ldx, W, ldw, y, 1, nullptr, 0, 1, 1.0f, rows, denom, loss, row_loss,
+                   nullptr, "y");
+}
+
+int hf_vocab_loss_grad(hf_vocab* c, const void* X, int64_t ldx, const void* W, int64_t ldw,
+                       const int32_t* y, int64_t rows, float denom, float* loss, float* row_loss,
+                       void* dX, int64_t lddx, void* dW, int64_t lddw, int32_t accumulate) {
+  const Grad g = {dX, lddx, dW, lddw, accumulate};
+  return head_call(c, X, ldx, W, ldw, y, 1, nullptr, 0, 1, 1.0f, rows, denom, loss, row_loss, &g,
+                   "y");
+}
+
+int hf_vocab_distill(hf_vocab* c, const void* X, int64_t ldx, const void* W, int64_t ldw,
+                     const int32_t* ids, int64_t ldi, const float* t, int64_t ldt, int32_t top,
+                     float tau, int64_t rows, float denom, float* loss, float* row_loss) {
+  const int rc = check_list(c, t, rows, top, tau);
+  if (rc) return rc;
+  return head_call(c, X, ldx, W, ldw, ids, ldi, t, ldt, top, tau, rows, denom, loss, row_loss,
+                   nullptr, "ids");
+}
+
+int hf_vocab_distill_grad(hf_vocab* c, const void* X, int64_t ldx, const void* W, int64_t ldw,
+                          const int32_t* ids, int64_t ldi, const float* t, int64_t ldt,
+                          int32_t top, float tau, int64_t rows, float denom, float* loss,
+                          float* row_loss, void* dX, int64_t lddx, void* dW, int64_t lddw,
+                          int32_t accumulate) {
+  const int rc = check_list(c, t, rows, top, tau);
+  if (rc) return rc;
+  const Grad g = {dX, lddx, dW, lddw, accumulate};
+  return head_call(c, X, ldx, W, ldw, ids, ldi, t, ldt, top, tau, rows, denom, loss, row_loss,
+                   &g, "ids");
+}
+
+int hf_vocab_embed(hf_vocab* c, const void* E, int64_t lde, const int32_t* tok, int64_t rows,
+                   float scale, void* out, int64_t ldo) {
+  int rc;
+  if (!c) return HF_EINVAL;
+  if ((rc = check_rows(c, rows)) ||
+      (rc = check_mat(c, E, lde, c->D, c->es, c->V, "E")) ||
+      (rc = check_mat(c, tok, 1, 1, 4, rows, "tok")) ||
+      (rc = check_mat(c, out, ldo, c->D, c->es, rows, "out")))
+    return rc;
+  if (!std::isfinite(scale)) return fail(c, HF_EINVAL, "scale is not finite");
+  bool captured;
+  if ((rc = check_ready(c, rows)) || (rc = begin(c, &captured))) return rc;
+  const Launch L{c->stream, nullptr};
+  vocab_embed(L, c->type, E, lde, c->V, c->D, tok, (int)rows, scale, out, ldo, c->st());
+  return end(c, captured);
+}
+
+int hf_vocab_embed_grad(hf_vocab* c, const int32_t* tok, int64_t rows, float scale,
+                        const void* dout, int64_t ldd, void* dE, int64_t lde,
+                        int32_t accumulate) {
+  int rc;
+  if (!c) return HF_EINVAL;
+  if ((rc = check_rows(c, rows)) ||
+      (rc = check_mat(c, tok, 1, 1, 4, rows, "tok")) ||
+      (rc = check_mat(c, dout, ldd, c->D, c->es, rows, "dout")) ||
+      (rc = check_mat(c, dE, lde, c->D, c->es, c->V, "dE")))
+    return rc;
+  if (!std::isfinite(scale)) return fail(c, HF_EINVAL, "scale is not finite");
+  if (accumulate != 0 && accumulate != 1)
+    return fail(c, HF_EINVAL, "accumulate %d is neither 0 nor 1", accumulate);
+  bool captured;
+  if ((rc = check_ready(c, rows)) || (rc = begin(c, &captured))) return rc;
+  const Launch L{c->stream, nullptr};
+  const Layout& l = c->lay;
+  const VSort s = {c->at<int>(l.key), c->at<int>(l.spos), c->at<int>(l.tkey), c->at<int>(l.tpos),
+                   c->at<unsigned>(l.hist), c->at<float>(l.epart)};
+  vocab_embed_grad(L, c->type, tok, (int)rows, c->V, c->D, scale, dout, ldd, dE, lde, accumulate,
+                   s, c->st());
+  return end(c, captured);
+}
+
+int hf_vocab_check(hf_vocab* c) {
+  if (!c) return HF_EINVAL;
+  if (!c->ws) return HF_OK;
+  HIP_TRY(c, hipStreamSynchronize(c->stream));
+  int flag = 0;
+  HIP_TRY(c, hipMemcpy(&flag, &c->st()->err, sizeof flag, hipMemcpyDeviceToHost));
+  if (flag) {
+    const int zero = 0;
+    HIP_TRY(c, hipMemcpy(&c->st()->err, &zero, sizeof zero, hipMemcpyHostToDevice));
+    return fail(c, HF_ELABEL, "a label, token or id outside [0, %d) was seen", c->V);
+  }
+  return HF_OK;
+}
+
+const char* hf_vocab_last_error(const hf_vocab* c) {
+  return c ? c->err.c_str() : "null context";
+}
+
+}  // extern "C"

@@ -1,0 +1,479 @@
+// The GEMMs of the softmax head over a large vocabulary.  With X the counted
+// rows (T x D), W the vocabulary matrix (V x D) and tau the temperature:
+//   logits     z = X W^T / tau, of a piece of the vocabulary; per row and
+//              vocabulary tile the maximum and the sum of exp(z - max), from
+//              which the log-sum-exp over the whole vocabulary is joined
+//   p          exp(z - lse), recomputed piece by piece
+//   dX         delta W, delta = p - q (q the targets), summed over the pieces
+//   dW         delta^T X, whole for each piece
+// 2 T V D operations each: bound by the matrix cores but for few rows, where
+// reading W bounds them.
+//
+// C(m, n) = sum_k A(m, k) B(n, k) with m the dimension that is contiguous in
+// the output: the vocabulary for logits, the width for the gradients.  A lane
+// of a 32 x 32 MFMA holds one n and 16 values of m, so the maximum and the sum
+// over the vocabulary run within a lane, and outputs leave as 4 consecutive
+// values.
+//
+// No operand is transposed in memory.  A K-contiguous operand is kept in LDS
+// as [row][k] and read 16 bytes a lane; one whose rows are k is kept as
+// [k][row], and bf16 fragments are transposed on the way out of LDS
+// (ds_read_b64_tr_b16: 16 lanes read 4 rows of 16 and get 4 values of k each),
+// fp32 ones read value by value.  LDS tiles are filled by direct loads, with
+// the 16-byte chunks of a row XOR-swizzled by the row so that the lanes that
+// LDS serves together fall into distinct banks:
+//   [row][k], 128-byte rows: chunk ^ (row / 2) % 8
+//   [k][row], bf16: 64-byte runs of 4 consecutive k: chunk ^ 4 (k % 4)
+//   [k][row], fp32: 128-byte runs of k and k + 4:    chunk ^ 8 (k / 4 % 2)
+// K advances BK at a time through S stages, each refilled S blocks ahead once
+// every wave has its last fragments in registers.
+#include <type_traits>
+
+#include "lds_dma.h"
+#include "vocab_internal.h"
+
+namespace hfk {
+namespace {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+
+__device__ __forceinline__ uint32_t f2bf(float f) {
+  return __builtin_bit_cast(uint16_t, (__bf16)f);
+}
+__device__ __forceinline__ float bf2f(uint32_t h) { return __uint_as_float(h << 16); }
+
+// fragment of one step for one 32-row block: 8 consecutive k per half-wave
+// (bf16, one MFMA) or 4 (fp32, four MFMAs)
+template <class E>
+struct FragT;
+template <>
+struct FragT<bf16_t> { typedef bf16x8 T; };
+template <>
+struct FragT<float> { typedef f32x4 T; };
+
+template <class E, bool KC, int ROWS, int BK, int NW>
+struct Tile {
+  typedef typename FragT<E>::T Frag;
+  static constexpr int EPC = 16 / (int)sizeof(E);     // elements per chunk
+  static constexpr int CH = KC ? BK / EPC : ROWS / EPC;
+  static constexpr int SIZE = ROWS * BK;
+  static constexpr int INSTR = SIZE / EPC / 64 / NW;
+  static_assert(SIZE % (EPC * 64 * NW) == 0, "tile does not split over the waves");
+  static_assert(BK * sizeof(E) == 128 && ROWS * sizeof(E) >= 256, "swizzles");
+
+  __device__ static __forceinline__ int swz(int r) {
+    if (KC) return (r >> 1) & 7;
+    return sizeof(E) == 2 ? (r & 3) << 2 : ((r >> 2) & 1) << 3;
+  }
+  // the LDS row (of rows, or of k) and the global chunk that `lane` of `wave`
+  // fetches with its direct load j
+  __device__ static __forceinline__ void src(int wave, int lane, int j, int& row, int& ch) {
+    const int P = (wave * INSTR + j) * 64 + lane;
+    row = P / CH;
+    ch = (P % CH) ^ swz(row);
+  }
+  __device__ static __forceinline__ int dst(int wave, int j) {
+    return (wave * INSTR + j) * 64 * EPC;
+  }
+  // step q of the 32-row block at row0, for lane (li, h)
+  __device__ static __forceinline__ Frag frag(const E* s, int row0, int lane, int q) {
+    const int li = lane & 31, h = lane >> 5;
+    if constexpr (KC) {
+      const int row = row0 + li;
+      return *(const Frag*)(s + row * BK + (((2 * q + h) ^ swz(row)) * EPC));
+    } else if constexpr (sizeof(E) == 2) {
+      const int l = lane & 15, col = row0 + (lane & 16) + 4 * (l & 3);
+      s16x4 v[2];
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+        const int k = 16 * q + 8 * h + 4 * r + (l >> 2);
+        const E* p = s + k * ROWS + (((col >> 3) ^ swz(k)) << 3) + (col & 7);
+        v[r] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+            (__attribute__((address_space(3))) s16x4*)p);
+      }
+      return __builtin_bit_cast(
+          bf16x8, __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7));
+    } else {
+      const int col = row0 + li;
+      Frag f;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int k = 8 * q + 4 * h + j;
+        f[j] = s[k * ROWS + (((col >> 2) ^ swz(k)) << 2) + (col & 3)];
+      }
+      return f;
+    }
+  }
+};
+
+__device__ __forceinline__ f32x16 mma1(bf16x8 a, bf16x8 b, f32x16 c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x16 mma1(f32x4 a, f32x4 b, f32x16 c) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[j], b[j], c, 0, 0, 0);
+  return c;
+}
+
+// 4 consecutive values of one row of the type's output
+__device__ __forceinline__ void store4(float* p, const float (&v)[4], int n, int vec) {
+  if (vec && n >= 4) {
+    *(f32x4*)p = f32x4{v[0], v[1], v[2], v[3]};
+  } else {
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (j < n) p[j] = v[j];
+  }
+}
+__device__ __forceinline__ void store4(bf16_t* p, const float (&v)[4], int n, int vec) {
+  if (vec && n >= 4) {
+    *(u32x2*)p = u32x2{f2bf(v[0]) | f2bf(v[1]) << 16, f2bf(v[2]) | f2bf(v[3]) << 16};
+  } else {
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (j < n) p[j] = (bf16_t)f2bf(v[j]);
+  }
+}
+// exp, to the last bits where the type keeps them
+template <class E>
+__device__ __forceinline__ float exp_of(float x) {
+  return sizeof(E) == 4 ? expf(x) : __expf(x);
+}
+__device__ __forceinline__ float load1(const float* p) { return *p; }
+__device__ __forceinline__ float load1(const bf16_t* p) { return bf2f(*p); }
+
+// ----------------------------------------------------------------- epilogues
+enum { E_LOGITS, E_PROBS, E_PART, E_OUT };
+
+// The tile (tm, tn) and split this workgroup computes.  Consecutive
+// workgroups go to the 8 XCDs in turn; each XCD gets a contiguous eighth of
+// the logical order, which walks groups of 8 tiles of n, m by m, so that the
+// workgroups resident on an XCD share their operand panels in its L2.
+__device__ __forceinline__ void tile_of(int& tm, int& tn, int& tz) {
+  const int gx = gridDim.x, gy = gridDim.y;
+  const int T = gx * gy * gridDim.z;
+  const int L = blockIdx.x + gx * (blockIdx.y + gy * blockIdx.z);
+  // XCD x's share: T / 8 workgroups, one more for the first T % 8
+  const int x = L % 8, q = T / 8, r8 = T % 8;
+  const int Lg = x * q + min(x, r8) + L / 8;
+  tz = Lg / (gx * gy);
+  const int r = Lg % (gx * gy);
+  constexpr int G = 8;
+  const int g = r / (G * gx);
+  const int first = g * G;
+  const int rows = min(G, gy - first);
+  const int w = r - g * G * gx;
+  tn = first + w % rows;
+  tm = w / rows;
+}
+
+template <class E, int EPI, bool AKC, bool BKC, int WM, int WN, int GM, int GN, int S>
+__device__ __forceinline__ void vgemm_body(const VGemm& s, const VEpi& e) {
+  constexpr int BK = 128 / (int)sizeof(E);
+  constexpr int NW = GM * GN;
+  constexpr int RM = 32 * WM * GM, RN = 32 * WN * GN;
+  using TA = Tile<E, AKC, RM, BK, NW>;
+  using TB = Tile<E, BKC, RN, BK, NW>;
+  constexpr int EPC = TA::EPC;
+  constexpr int STAGE = TA::SIZE + TB::SIZE;
+  constexpr int LPB = TA::INSTR + TB::INSTR;
+  __shared__ __attribute__((aligned(16))) E lds[S * STAGE];
+
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wm = wave / GN, wn = wave % GN;
+  const int li = lane & 31, h = lane >> 5;
+  int tm, tn, tz;
+  tile_of(tm, tn, tz);
+  const int m0 = tm * RM, n0 = tn * RN;
+  const int nrow = s.st->n;
+  const int N = s.dyn == 1 ? nrow : s.N;
+  const int K = s.dyn == 2 ? (nrow + VPAD - 1) & ~(VPAD - 1) : s.K;
+  if (n0 >= N) return;
+
+  const int nvb = (K + BK - 1) / BK;
+  int vb0 = 0, nblk = nvb;
+  if (s.splits > 1) {
+    const int per = (nvb + s.splits - 1) / s.splits;
+    vb0 = min(tz * per, nvb);
+    nblk = min(nvb, vb0 + per) - vb0;
+  }
+
+  f32x16 acc[WM][WN];
+#pragma unroll
+  for (int a = 0; a < WM; ++a)
+#pragma unroll
+    for (int b = 0; b < WN; ++b)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[a][b][r] = 0.0f;
+
+  // Element offsets of the lane's direct loads from the tile's origin.  Rows
+  // of a K-contiguous A past its last one read that one; chunks of a [k][m]
+  // operand past its padded width read the last chunk (both feed outputs that
+  // are not stored).  B's buffers are whole tiles.
+  const long long lda = s.lda, ldb = s.ldb;
+  uint32_t offa[TA::INSTR], offb[TB::INSTR];
+#pragma unroll
+  for (int j = 0; j < TA::INSTR; ++j) {
+    int row, ch;
+    TA::src(wave, lane, j, row, ch);
+    if (AKC) offa[j] = (uint32_t)((min(m0 + row, s.alim - 1) - m0) * lda) + EPC * ch;
+    else offa[j] = (uint32_t)(row * lda) + min(EPC * ch, (int)(s.M - 1 - m0) / EPC * EPC);
+  }
+#pragma unroll
+  for (int j = 0; j < TB::INSTR; ++j) {
+    int row, ch;
+    TB::src(wave, lane, j, row, ch);
+    offb[j] = (uint32_t)(row * ldb) + EPC * ch;
+  }
+  const E* const A0 = (const E*)s.A + (AKC ? (size_t)m0 * lda : (size_t)m0);
+  const E* const B0 = (const E*)s.B + (BKC ? (size_t)n0 * ldb : (size_t)n0);
+  const uint32_t lds0 = lds_address(lds);
+  auto issue = [&](int vb, int st) {
+    const int k0 = vb * BK;
+    const uint32_t base = lds0 + (uint32_t)sizeof(E) * (uint32_t)(st * STAGE);
+    const E* a = A0 + (AKC ? (size_t)k0 : (size_t)k0 * lda);
+    const E* b = B0 + (BKC ? (size_t)k0 : (size_t)k0 * ldb);
+    if (AKC || k0 + BK <= s.alim) {
+#pragma unroll
+      for (int j = 0; j < TA::INSTR; ++j)
+        dma16_at(a + offa[j], base + (uint32_t)sizeof(E) * TA::dst(wave, j));
+    } else {
+      // rows of k past the last one read the last one, against zeros of B
+#pragma unroll
+      for (int j = 0; j < TA::INSTR; ++j) {
+        int row, ch;
+        TA::src(wave, lane, j, row, ch);
+        const int over = max(0, k0 + row - (s.alim - 1));
+        dma16_at(a + offa[j] - over * lda, base + (uint32_t)sizeof(E) * TA::dst(wave, j));
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < TB::INSTR; ++j)
+      dma16_at(b + offb[j], base + (uint32_t)sizeof(E) * (TA::SIZE + TB::dst(wave, j)));
+  };
+
+  struct Frags {
+    typename TA::Frag a[WM];
+    typename TB::Frag b[WN];
+  };
+  auto fetch = [&](Frags& f, int st, int q) {
+    const E* la = lds + st * STAGE;
+    const E* lb = la + TA::SIZE;
+#pragma unroll
+    for (int a = 0; a < WM; ++a) f.a[a] = TA::frag(la, wm * 32 * WM + 32 * a, lane, q);
+#pragma unroll
+    for (int b = 0; b < WN; ++b) f.b[b] = TB::frag(lb, wn * 32 * WN + 32 * b, lane, q);
+  };
+  auto mma = [&](const Frags& f) {
+#pragma unroll
+    for (int a = 0; a < WM; ++a)
+#pragma unroll
+      for (int b = 0; b < WN; ++b) acc[a][b] = mma1(f.a[a], f.b[b], acc[a][b]);
+  };
+
+  constexpr int NQ = 4;      // steps per K block
+  static_assert(NQ % 2 == 0 && (S - 1) * LPB < 64, "pipeline depth");
+  Frags fa, fb;
+#pragma unroll
+  for (int i = 0; i < S; ++i)
+    if (i < nblk) issue(vb0 + i, i);
+  if (nblk > 0) {
+    if (nblk >= S) wait_vm<(S - 1) * LPB>();
+    else wait_vm<0>();
+    stage_barrier();
+    fetch(fa, 0, 0);
+  }
+  for (int it = 0; it < nblk; ++it) {
+    const int st = it % S;
+#pragma unroll
+    for (int q = 0; q + 1 < NQ; ++q) {
+      fetch((q & 1) ? fa : fb, st, q + 1);
+      __builtin_amdgcn_sched_barrier(0);
+      mma((q & 1) ? fb : fa);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    if (it + 1 < nblk) {
+      // this wave's loads of block it + 1 have landed once at most
+      // min(S - 2, nblk - 2 - it) later blocks are pending
+      const int ahead = min(S - 2, nblk - 2 - it);
+      wait_vm<(S - 2) * LPB>();
+      if (S > 2 && ahead < S - 2) wait_vm<0>();
+      stage_barrier();     // every wave's loads landed; stage st is free
+      fetch(fa, (it + 1) % S, 0);
+      __builtin_amdgcn_sched_barrier(0);
+      if (it + S < nblk) issue(vb0 + it + S, st);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    mma(fb);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+
+  // Lane (li, h), register r of block (a, b) holds n = 32 b + li and
+  // m = 32 a + 8 (r / 4) + 4 h + r % 4 of the wave's part of the tile.
+  const int mw = m0 + wm * 32 * WM + 4 * h, nw = n0 + wn * 32 * WN + li;
+  if constexpr (EPI == E_LOGITS) {
+    // row statistics of this tile: within the lane, the two halves of the
+    // wave, then the GM waves that share the rows
+    __shared__ float2 red[GM][RN];
+#pragma unroll
+    for (int b = 0; b < WN; ++b) {
+      const int n = nw + 32 * b;
+      float mx = -INFINITY;
+#pragma unroll
+      for (int a = 0; a < WM; ++a)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int m = mw + 32 * a + 8 * (r >> 2) + (r & 3);
+          acc[a][b][r] *= e.zscale;
+          if (m < s.M) mx = fmaxf(mx, acc[a][b][r]);
+        }
+      mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+      // nothing but -inf: exp(-inf - 0) = 0, where -inf - -inf is no number
+      const float at = mx == -INFINITY ? 0.0f : mx;
+      float sum = 0.0f;
+#pragma unroll
+      for (int a = 0; a < WM; ++a)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int m = mw + 32 * a + 8 * (r >> 2) + (r & 3);
+          sum += m < s.M ? exp_of<E>(acc[a][b][r] - at) : 0.0f;
+        }
+      sum += __shfl_xor(sum, 32, 64);
+      if (h == 0) red[wm][wn * 32 * WN + 32 * b + li] = float2{mx, sum};
+      if (e.z && n < N) {
+#pragma unroll
+        for (int a = 0; a < WM; ++a)
+#pragma unroll
+          for (int g = 0; g < 4; ++g) {
+            const int m = mw + 32 * a + 8 * g;
+            const float v[4] = {acc[a][b][4 * g], acc[a][b][4 * g + 1],
+                                acc[a][b][4 * g + 2], acc[a][b][4 * g + 3]};
+            if (m < s.M) store4(e.z + (size_t)n * e.ldz + m, v, s.M - m, 1);
+          }
+      }
+    }
+    __syncthreads();
+    for (int c = tid; c < RN; c += 64 * NW) {
+      if (n0 + c >= N) continue;
+      float mx = red[0][c].x, sum = red[0][c].y;
+#pragma unroll
+      for (int w = 1; w < GM; ++w) {
+        const float2 o = red[w][c];
+        const float t = fmaxf(mx, o.x), at = t == -INFINITY ? 0.0f : t;
+        sum = sum * exp_of<E>(mx - at) + o.y * exp_of<E>(o.x - at);
+        mx = t;
+      }
+      e.stat[(size_t)(n0 + c) * e.ldstat + e.tile0 + tm] = float2{mx, sum};
+    }
+  } else {
+    const float scale = EPI == E_OUT ? s.st->gscale : 1.0f;
+    // columns of delta are written up to whole K blocks of the next products
+    const int Mp = EPI == E_PROBS ? (s.M + VPAD - 1) & ~(VPAD - 1) : s.M;
+    // and its rows up to whole K blocks too (zeros: their lse is infinite)
+    const int Np = EPI == E_PROBS ? (N + VPAD - 1) & ~(VPAD - 1) : N;
+#pragma unroll
+    for (int b = 0; b < WN; ++b) {
+      const int n = nw + 32 * b;
+      if (n < Np) {
+        const float lse = EPI == E_PROBS ? e.lse[n] : 0.0f;
+#pragma unroll
+        for (int a = 0; a < WM; ++a)
+#pragma unroll
+          for (int g = 0; g < 4; ++g) {
+            const int m = mw + 32 * a + 8 * g;
+            if (m >= Mp) continue;
+            float v[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const float c = acc[a][b][4 * g + j];
+              if (EPI == E_PROBS) v[j] = m + j < s.M ? exp_of<E>(c * e.zscale - lse) : 0.0f;
+              else v[j] = c * scale;
+            }
+            if constexpr (EPI == E_PROBS) {
+              store4((E*)e.d + (size_t)n * e.ldd + m, v, 4, 1);
+            } else if constexpr (EPI == E_PART) {
+              float* p = e.part + (size_t)tz * e.split_stride + (size_t)n * e.ldp + m;
+              if (e.add) {
+                const f32x4 o = *(const f32x4*)p;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v[j] += o[j];
+              }
+              store4(p, v, 4, 1);
+            } else {
+              E* p = (E*)e.out + (size_t)n * e.ldo + m;
+              if (e.accumulate) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                  if (m + j < s.M) v[j] += load1(p + j);
+              }
+              store4(p, v, s.M - m, e.vec);
+            }
+          }
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  }
+}
+
+}  // namespace
+
+// big: 256 x 256 tiles, 8 waves of 128 x 64; else 128 x 128, 4 waves of 64 x 64
+#define HF_VGEMM(NAME, EPI, AKC, BKC)                                                  \
+  extern "C" __global__ __launch_bounds__(512, 1) void NAME##_bf16_big(VGemm s, VEpi e) { \
+    vgemm_body<bf16_t, EPI, AKC, BKC, 4, 2, 2, 4, 2>(s, e);                            \
+  }                                                                                    \
+  extern "C" __global__ __launch_bounds__(256, 2) void NAME##_bf16(VGemm s, VEpi e) {  \
+    vgemm_body<bf16_t, EPI, AKC, BKC, 2, 2, 2, 2, 2>(s, e);                            \
+  }                                                                                    \
+  extern "C" __global__ __launch_bounds__(512, 1) void NAME##_f32_big(VGemm s, VEpi e) {  \
+    vgemm_body<float, EPI, AKC, BKC, 4, 2, 2, 4, 2>(s, e);                             \
+  }                                                                                    \
+  extern "C" __global__ __launch_bounds__(256, 2) void NAME##_f32(VGemm s, VEpi e) {   \
+    vgemm_body<float, EPI, AKC, BKC, 2, 2, 2, 2, 2>(s, e);                             \
+  }
+HF_VGEMM(hf_vocab_logits, E_LOGITS, true, true)
+HF_VGEMM(hf_vocab_probs, E_PROBS, true, true)
+HF_VGEMM(hf_vocab_dx, E_PART, false, true)
+HF_VGEMM(hf_vocab_dw, E_OUT, false, false)
+HF_VGEMM(hf_vocab_dw_part, E_PART, false, false)
+
+// ------------------------------------------------------------- launchers
+namespace {
+typedef void (*VK)(VGemm, VEpi);
+void launch(const Launch& L, const char* name, const VK (&k)[2][2], int type, const VGemm& g,
+            const VEpi& e) {
+  if (g.M < 1 || g.N < 1) return;
+  const int R = g.big ? 256 : 128;
+  const dim3 grid((g.M + R - 1) / R, (g.N + R - 1) / R, g.splits);
+  prof_begin(L, name);
+  hipExtLaunchKernelGGL(k[type][g.big], grid, dim3(g.big ? 512 : 256), 0, L.stream,
+                        prof_a(L), prof_b(L), 0, g, e);
+  prof_end(L, name, 2.0 * g.M * (double)g.N * g.K, 0.0);
+}
+}  // namespace
+
+#define HF_VK(NAME) {{NAME##_f32, NAME##_f32_big}, {NAME##_bf16, NAME##_bf16_big}}
+void vocab_logits(const Launch& L, int type, const VGemm& g, const VEpi& e) {
+  static const VK k[2][2] = HF_VK(hf_vocab_logits);
+  launch(L, "hf_vocab_logits", k, type, g, e);
+}
+void vocab_probs(const Launch& L, int type, const VGemm& g, const VEpi& e) {
+  static const VK k[2][2] = HF_VK(hf_vocab_probs);
+  launch(L, "hf_vocab_probs", k, type, g, e);
+}
+void vocab_dx(const Launch& L, int type, const VGemm& g, const VEpi& e) {
+  static const VK k[2][2] = HF_VK(hf_vocab_dx);
+  launch(L, "hf_vocab_dx", k, type, g, e);
+}
+void vocab_dw(const Launch& L, int type, const VGemm& g, const VEpi& e) {
+  static const VK k[2][2] = HF_VK(hf_vocab_dw), p[2][2] = HF_VK(hf_vocab_dw_part);
+  launch(L, "hf_vocab_dw", g.splits > 1 ? p : k, type, g, e);
+}
+
+}  // namespace hfk

@@ -1,0 +1,149 @@
+// Internal declarations of the vocabulary kernels: the softmax head over a
+// large vocabulary (cross entropy and distillation, with their gradients) and
+// the token embedding with its gradient.
+#pragma once
+
+#include "hf_internal.h"
+
+namespace hfk {
+
+// Element type of the rows, the matrices and their gradients.
+enum VType { VT_F32 = 0, VT_BF16 = 1 };
+
+// K blocks of the GEMMs are whole multiples of this many elements: widths are
+// padded to it in packed rows, and vocabulary pieces and row counts in delta.
+constexpr int VPAD = 64;
+// Rows of packed operands come in whole tiles of this many.
+constexpr int VTILE = 256;
+// Columns of one tile of row statistics (the smallest vocabulary tile).
+constexpr int VSTAT = 128;
+constexpr int VMAX_SPLITS = 64;
+
+// Device scalars of a call.
+struct VocabState {
+  int n;           // counted rows
+  int err;         // a label, token or id outside the vocabulary was seen
+  float gscale;    // tau / denom: factor of both gradients
+  double inv;      // 1 / denom
+};
+
+// C(m, n) = sum_k A(m, k) B(n, k), stored with m contiguous.
+//   A(m, k) = akc ? A[m lda + k] : A[k lda + m],  B likewise.
+struct VGemm {
+  int M, N, K;
+  const void *A, *B;
+  long long lda, ldb;
+  int alim;        // rows of A that exist: m (akc), or k (not akc)
+  const VocabState* st;
+  int dyn;         // 1: N is st->n; 2: K is st->n rounded up to VPAD
+  int splits;      // split-K factor (partials), grid z
+  int big;         // 256 x 256 tiles rather than 128 x 128
+};
+
+struct VEpi {
+  // logits
+  float zscale;          // 1 / tau
+  float* z;              // logits kept (row n, column m), or null
+  long long ldz;
+  float2* stat;          // per row and vocabulary tile: max, sum of exp
+  int ldstat, tile0;     // tiles per row; index of this launch's first tile
+  const float* lse;      // delta: log-sum-exp per row (+inf: no such row)
+  void* d;               // delta, row n, column m
+  long long ldd;
+  // products
+  float* part;           // partials, [split][n][m]
+  long long ldp, split_stride;
+  int add;               // part += rather than =
+  void* out;             // final output, scaled by st->gscale
+  long long ldo;
+  int accumulate;        // out += rather than =
+  int vec;               // out rows take 4-element vector stores
+};
+
+// logits of a vocabulary piece: A = W piece (akc), B = packed rows (akc);
+//   stat, and z if kept
+void vocab_logits(const Launch& L, int type, const VGemm& g, const VEpi& e);
+// p = exp(z - lse) of a vocabulary piece, rounded to the type, into d
+void vocab_probs(const Launch& L, int type, const VGemm& g, const VEpi& e);
+// row gradients: A = W piece (rows k), B = delta (k contiguous); into part
+void vocab_dx(const Launch& L, int type, const VGemm& g, const VEpi& e);
+// matrix gradient: A = packed rows (rows k), B = delta (rows k); into out, or
+// into part where g.splits > 1
+void vocab_dw(const Launch& L, int type, const VGemm& g, const VEpi& e);
+
+// -------------------------------------------------------------- row kernels
+struct VRows {
+  int T;                    // rows of the call
+  int V, D, K;              // vocabulary, width, targets per row
+  const int32_t* ids;       // T x K targets (labels: K = 1)
+  long long ldi;
+  const float* t;           // T x K teacher logits, or null (hard labels)
+  long long ldt;
+  float tau;
+  float denom;              // > 0: divides the sum of the losses; 0: counted rows
+  VocabState* st;
+  int* pos;                 // T: packed row of a row, -1: not counted
+  int* idx;                 // the row of a packed row
+  float* row_loss;          // T
+};
+// which rows count: pos, idx and the state; zero losses for those that do not
+void vocab_count(const Launch& L, const VRows& r);
+// counted rows of X packed to xp (zeros past the width, and past the last row
+// up to a whole tile; twice, dup rows apart, if dup > 0), rows of dX that do
+// not count set to zero
+void vocab_pack_rows(const Launch& L, int type, const VRows& r, const void* X,
+                     long long ldx, void* xp, int Dp, int dup, void* dX,
+                     long long lddx);
+// rows [0, R) of W copied to wp (zeros past the width)
+void vocab_pack_matrix(const Launch& L, int type, const void* W, long long ldw,
+                       int R, int D, void* wp, int Dp);
+struct VTarget {
+  float* zt;                // packed row x K: target logits over tau
+  int* id;                  // packed row x K: target id, -1: none (or a repeat)
+  float* dt;                // packed row x K: delta at the target
+};
+// zt of the targets by their own products (logits not kept)
+void vocab_target_logits(const Launch& L, int type, const VRows& r, const void* xp,
+                         int Dp, const void* W, long long ldw, float* zt);
+// log-sum-exp from the tiles' statistics, the rows' losses and the targets'
+// delta; z: kept logits or null (then t.zt holds the targets')
+void vocab_row_loss(const Launch& L, const VRows& r, const float2* stat, int ldstat,
+                    int tiles, const float* z, long long ldz, const VTarget& t,
+                    float* lse);
+// loss = sum of the counted rows' losses / denom
+void vocab_loss_sum(const Launch& L, const VRows& r, float* loss);
+// delta from kept logits, targets included; two: the rounding's rest too, dup
+// rows further down
+void vocab_delta(const Launch& L, int type, const VRows& r, const float* z,
+                 long long ldz, const float* lse, const VTarget& t, int rows,
+                 void* d, long long ldd, int Vp, int dup);
+// delta at the targets within the piece [v0, v0 + Vc)
+void vocab_fix(const Launch& L, int type, const VRows& r, const VTarget& t, int v0,
+               int Vc, void* d, long long ldd);
+// out(row) = gscale (sum over splits, and over the dup copy) part(row);
+// idx: destination row of a packed row, null: itself
+void vocab_finish(const Launch& L, int type, const VocabState* st, const float* part,
+                  int splits, long long split_stride, long long ldp, int dup, int rows,
+                  int dyn, int D, const int* idx, void* out, long long ldo,
+                  int accumulate);
+
+// ---------------------------------------------------------------- embedding
+struct VSort {
+  int* key;                 // T: ids in order
+  int* pos;                 // T: their rows
+  int* tkey;                // T: scratch
+  int* tpos;
+  unsigned* hist;           // histograms of the radix passes
+  float* part;              // sums of whole chunks of one id
+};
+// unsigned words of hist, and floats of part, for T rows
+size_t vocab_sort_hist(long long T, int V);
+size_t vocab_sort_part(long long T, int D, int type);
+void vocab_embed(const Launch& L, int type, const void* E, long long lde, int V, int D,
+                 const int32_t* tok, int T, float scale, void* out, long long ldo,
+                 VocabState* st);
+void vocab_embed_grad(const Launch& L, int type, const int32_t* tok, int T, int V, int D,
+                      float scale, const void* dout, long long ldd, void* dE,
+                      long long lde, int accumulate, const VSort& s, VocabState* st);
+
+}  // namespace hfk

@@ -1,0 +1,553 @@
+// The row-wise kernels of the softmax head, between its GEMMs.
+//
+// Rows that do not count (a masked label, an empty teacher list) are left out
+// before anything is computed: the counted rows of X are packed one after the
+// other, and everything up to the row gradients works on packed rows.  What X
+// holds in the others, infinities and NaN included, reaches nothing.
+//
+// Per packed row, with z the logits over tau and q the targets (q = 1 at the
+// label, or the softmax of the teacher's logits over tau within its list):
+//   lse   = log sum_v exp z_v, joined from (max, sum) pairs of vocabulary tiles
+//   loss  = tau^2 sum_k q_k (log q_k - (z_k - lse))
+//   delta = p - q,  p_v = exp(z_v - lse)
+// delta is p rounded to the type everywhere but at the targets, where p - q is
+// formed in fp32 and rounded once.  Losses are summed in fp64.
+#include <type_traits>
+
+#include "vocab_internal.h"
+
+namespace hfk {
+namespace {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+
+__device__ __forceinline__ uint32_t f2bf(float f) {
+  return __builtin_bit_cast(uint16_t, (__bf16)f);
+}
+__device__ __forceinline__ float bf2f(uint32_t h) { return __uint_as_float(h << 16); }
+__device__ __forceinline__ float to_f(float v) { return v; }
+__device__ __forceinline__ float to_f(bf16_t v) { return bf2f(v); }
+__device__ __forceinline__ void put(float* p, float v) { *p = v; }
+__device__ __forceinline__ void put(bf16_t* p, float v) { *p = (bf16_t)f2bf(v); }
+
+__device__ __forceinline__ float wave_max(float v) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
+  return v;
+}
+__device__ __forceinline__ float wave_sum(float v) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+  return v;
+}
+__device__ __forceinline__ double wave_sum_d(double v) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+  return v;
+}
+
+// Target k of row t: its id, or -1 where the place is masked (HF_IGNORE, or a
+// teacher logit of -inf); an id outside the vocabulary raises the flag and
+// counts as masked.
+constexpr int IGNORE = -100;
+__device__ __forceinline__ int target(const VRows& r, int t, int k, float* logit) {
+  const int id = r.ids[(size_t)t * r.ldi + k];
+  if (id == IGNORE) return -1;
+  if (id < 0 || id >= r.V) {
+    r.st->err = 1;
+    return -1;
+  }
+  if (!r.t) return id;
+  const float v = r.t[(size_t)t * r.ldt + k];
+  *logit = v;
+  return v == -INFINITY ? -1 : id;
+}
+
+}  // namespace
+
+// ------------------------------------------------------------ counted rows
+// pos[t] = 1 if any of row t's K targets is there, else 0: one wave per row
+extern "C" __global__ __launch_bounds__(256) void hf_vocab_have(VRows r) {
+  const int t = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+  if (t >= r.T) return;
+  bool have = false;
+  float v;
+  for (int k = lane; k < r.K; k += 64) have |= target(r, t, k, &v) >= 0;
+  const bool any = __ballot(have) != 0;
+  if (lane == 0) r.pos[t] = any;
+}
+
+// One workgroup: each thread counts a run of rows, a scan over the threads
+// places them.  pos holds hf_vocab_have's answer for lists.
+extern "C" __global__ __launch_bounds__(1024) void hf_vocab_count(VRows r) {
+  __shared__ int sums[16];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int per = (r.T + 1023) / 1024;
+  const int t0 = min(tid * per, r.T), t1 = min(t0 + per, r.T);
+  float v;
+  int c = 0;
+  for (int t = t0; t < t1; ++t) c += r.t ? r.pos[t] : target(r, t, 0, &v) >= 0;
+  int s = c;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int u = __shfl_up(s, o, 64);
+    if (lane >= o) s += u;
+  }
+  if (lane == 63) sums[wave] = s;
+  __syncthreads();
+  int base = 0, n = 0;
+#pragma unroll
+  for (int w = 0; w < 16; ++w) {
+    if (w < wave) base += sums[w];
+    n += sums[w];
+  }
+  int at = base + s - c;
+  for (int t = t0; t < t1; ++t) {
+    const bool have = r.t ? r.pos[t] != 0 : target(r, t, 0, &v) >= 0;
+    r.pos[t] = have ? at : -1;
+    if (have) r.idx[at++] = t;
+    else r.row_loss[t] = 0.0f;
+  }
+  if (tid == 0) {
+    const double denom = r.denom > 0.0f ? (double)r.denom : (double)n;
+    r.st->n = n;
+    r.st->inv = denom > 0.0 ? 1.0 / denom : 0.0;
+    r.st->gscale = denom > 0.0 ? (float)((double)r.tau / denom) : 0.0f;
+  }
+}
+
+// ----------------------------------------------------------------- packing
+namespace {
+// n elements of src to dst (16-byte aligned, dn elements), zeros past n;
+// vec: src is 16-byte aligned.  Called by a whole workgroup of 256.
+template <class E>
+__device__ __forceinline__ void copy_row(const E* src, int n, int vec, E* dst, int dn,
+                                         E* dst2) {
+  constexpr int EPC = 16 / sizeof(E);
+  for (int c = threadIdx.x; c < dn / EPC; c += 256) {
+    u32x4 v = u32x4{0u, 0u, 0u, 0u};
+    if (vec && EPC * c + EPC <= n) {
+      v = *(const u32x4*)(src + EPC * c);
+    } else {
+      E w[EPC];
+#pragma unroll
+      for (int j = 0; j < EPC; ++j) w[j] = EPC * c + j < n ? src[EPC * c + j] : (E)0;
+      v = __builtin_bit_cast(u32x4, w);
+    }
+    *(u32x4*)(dst + EPC * c) = v;
+    if (dst2) *(u32x4*)(dst2 + EPC * c) = v;
+  }
+}
+
+template <class E>
+__device__ __forceinline__ void pack_body(const VRows& r, const E* X, long long ldx, int vecx,
+                                          E* xp, int Dp, int dup, E* dX, long long lddx) {
+  int b = blockIdx.x;
+  if (b < r.T) {
+    const int j = r.pos[b];
+    if (j >= 0) {
+      copy_row(X + (size_t)b * ldx, r.D, vecx, xp + (size_t)j * Dp, Dp,
+               dup ? xp + (size_t)(dup + j) * Dp : (E*)nullptr);
+    } else if (dX) {
+      for (int c = threadIdx.x; c < r.D; c += 256) dX[(size_t)b * lddx + c] = (E)0;
+    }
+    return;
+  }
+  const int j = r.st->n + b - r.T;
+  const int end = dup ? dup : (r.st->n + VTILE - 1) / VTILE * VTILE;
+  if (j < end)
+    copy_row((const E*)nullptr, 0, 0, xp + (size_t)j * Dp, Dp,
+             dup ? xp + (size_t)(dup + j) * Dp : (E*)nullptr);
+}
+}  // namespace
+
+extern "C" __global__ __launch_bounds__(256) void hf_vocab_pack_f32(
+    VRows r, const float* X, long long ldx, int vecx, float* xp, int Dp, int dup, float* dX,
+    long long lddx) {
+  pack_body<float>(r, X, ldx, vecx, xp, Dp, dup, dX, lddx);
+}
+extern "C" __global__ __launch_bounds__(256) void hf_vocab_pack_bf16(
+    VRows r, const bf16_t* X, long long ldx, int vecx, bf16_t* xp, int Dp, int dup, bf16_t* dX,
+    long long lddx) {
+  pack_body<bf16_t>(r, X, ldx, vecx, xp, Dp, dup, dX, lddx);
+}
+extern "C" __global__ __launch_bounds__(256) void hf_vocab_copy_f32(
+    const float* W, long long ldw, int vec, int D, float* wp, int Dp) {
+  const size_t b = blockIdx.x;
+  copy_row(W + b * ldw, D, vec, wp + b * Dp, Dp, (float*)nullptr);
+}
+extern "C" __global__ __launch_bounds__(256) void hf_vocab_copy_bf16(
+    const bf16_t* W, long long ldw, int vec, int D, bf16_t* wp, int Dp) {
+  const size_t b = blockIdx.x;
+  copy_row(W + b * ldw, D, vec, wp + b * Dp, Dp, (bf16_t*)nullptr);
+}
+
+// ---------------------------------------------------- the targets' logits
+// Where the logits are not kept: the K products x_j . W[id] of a packed row,
+// one wave each.
+namespace {
+template <class E>
+__device__ __forceinline__ void tlogit_body(const VRows& r, const E* xp, int Dp, const E* W,
+                                            long long ldw, int vec, float* zt) {
+  constexpr int EPC = 16 / sizeof(E);
+  const int j = blockIdx.x;
+  if (j >= r.st->n) return;
+  const int t = r.idx[j], wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const E* x = xp + (size_t)j * Dp;
+  float v;
+  for (int k = wave; k < r.K; k += 4) {
+    const int id = target(r, t, k, &v);
+    if (id < 0) continue;
+    const E* w = W + (size_t)id * ldw;
+    float s = 0.0f;
+    if (vec) {
+      for (int c = lane; c < r.D / EPC; c += 64) {
+        E a[EPC], b[EPC];
+        *(u32x4*)a = *(const u32x4*)(x + EPC * c);
+        *(u32x4*)b = *(const u32x4*)(w + EPC * c);
+#pragma unroll
+        for (int i = 0; i < EPC; ++i) s += to_f(a[i]) * to_f(b[i]);
+      }
+      for (int c = r.D / EPC * EPC + lane; c < r.D; c += 64) s += to_f(x[c]) * to_f(w[c]);
+    } else {
+      for (int c = lane; c < r.D; c += 64) s += to_f(x[c]) * to_f(w[c]);
+    }
+    s = wave_sum(s);
+    if (lane == 0) zt[(size_t)j * r.K + k] = s / r.tau;
+  }
+}
+}  // namespace
+extern "C" __global__ __launch_bounds__(256) void hf_vocab_tlogit_f32(
+    VRows r, const float* xp, int Dp, const float* W, long long ldw, int vec, float* zt) {
+  tlogit_body<float>(r, xp, Dp, W, ldw, vec, zt);
+}
+extern "C" __global__ __launch_bounds__(256) void hf_vocab_tlogit_bf16(
+    VRows r, const bf16_t* xp, int Dp, const bf16_t* W, long long ldw, int vec, float* zt) {
+  tlogit_body<bf16_t>(r, xp, Dp, W, ldw, vec, zt);
+}
+
+// ------------------------------------------------------------- rows' losses
+// One wave per packed row; lane l has the targets l and l + 64.
+extern "C" __global__ __launch_bounds__(256) void hf_vocab_row_loss(
+    VRows r, const float2* __restrict__ stat, int ldstat, int tiles,
+    const float* __restrict__ z, long long ldz, VTarget tg, float* __restrict__ lse_out) {
+  const int j = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int n = r.st->n;
+  if (j >= n) {
+    // rows that only fill the last K block: p = exp(0 - inf) = 0
+    if (j < (n + VPAD - 1) / VPAD * VPAD && lane == 0) lse_out[j] = INFINITY;
+    return;
+  }
+  const int t = r.idx[j];
+  float mx = -INFINITY;
+  const float2* st = stat + (size_t)j * ldstat;
+  for (int i = lane; i < tiles; i += 64) mx = fmaxf(mx, st[i].x);
+  mx = wave_max(mx);
+  const float at = mx == -INFINITY ? 0.0f : mx;
+  float sum = 0.0f;
+  for (int i = lane; i < tiles; i += 64) sum += st[i].y * expf(st[i].x - at);
+  sum = wave_sum(sum);
+  const float lse = at + logf(sum);
+  if (lane == 0) lse_out[j] = lse;
+
+  int id[2] = {-1, -1};
+  float tl[2] = {0.0f, 0.0f}, q[2] = {0.0f, 0.0f}, lz[2] = {0.0f, 0.0f};
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+    if (lane + 64 * i < r.K) {
+      const int k = lane + 64 * i;
+      id[i] = target(r, t, k, &tl[i]);
+      if (id[i] >= 0) {
+        const float zt = z ? z[(size_t)j * ldz + id[i]] : tg.zt[(size_t)j * r.K + k];
+        // log p; above 0 only by rounding (the comparison keeps a NaN)
+        lz[i] = zt - lse > 0.0f ? 0.0f : zt - lse;
+      }
+    }
+  float loss = 0.0f;
+  // an id that comes twice: its first place has the sum of its q
+  float qs[2] = {id[0] >= 0 ? 1.0f : 0.0f, 0.0f};
+  int first[2] = {1, 1};
+  if (!r.t) {
+    loss = -lz[0];
+  } else {
+    // differences before the division: a logit of the type's lowest value
+    // over a small tau is no infinity then
+    const float top = wave_max(fmaxf(id[0] >= 0 ? tl[0] : -INFINITY,
+                                     id[1] >= 0 ? tl[1] : -INFINITY));
+    float e[2], u[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      u[i] = (tl[i] - top) / r.tau;
+      e[i] = id[i] >= 0 ? expf(u[i]) : 0.0f;
+    }
+    const float total = wave_sum(e[0] + e[1]);
+    const float lt = logf(total);
+    int same[2] = {0, 0};
+    qs[0] = 0.0f;
+#pragma unroll
+    for (int i2 = 0; i2 < 2; ++i2) {
+      q[i2] = e[i2] / total;
+      for (int l = 0; l < 64 && l + 64 * i2 < r.K; ++l) {
+        const int oid = __shfl(id[i2], l, 64);
+        const float oq = __shfl(q[i2], l, 64);
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+          if (oid == id[i]) {
+            qs[i] += oq;
+            ++same[i];
+            if (l + 64 * i2 < lane + 64 * i) first[i] = 0;
+          }
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      if (id[i] >= 0 && first[i] && qs[i] != 0.0f)
+        loss += qs[i] * ((same[i] > 1 ? logf(qs[i]) : u[i] - lt) - lz[i]);
+  }
+  loss = wave_sum(loss) * (r.tau * r.tau);
+  if (loss < 0.0f) loss = 0.0f;        // no divergence is; rounding can be
+  if (lane == 0) r.row_loss[t] = loss;
+  if (!tg.dt) return;
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+    if (lane + 64 * i < r.K) {
+      const size_t o = (size_t)j * r.K + lane + 64 * i;
+      tg.id[o] = id[i] >= 0 && first[i] ? id[i] : -1;
+      tg.dt[o] = expf(lz[i]) - qs[i];
+    }
+}
+
+extern "C" __global__ __launch_bounds__(1024) void hf_vocab_loss_sum(
+    const float* __restrict__ row_loss, int T, const VocabState* st, float* loss) {
+  __shared__ double ws[16];
+  double s = 0.0;
+  for (int i = threadIdx.x; i < T; i += 1024) s += (double)row_loss[i];
+  s = wave_sum_d(s);
+  if ((threadIdx.x & 63) == 0) ws[threadIdx.x >> 6] = s;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    double f = 0.0;
+    for (int w = 0; w < 16; ++w) f += ws[w];
+    *loss = (float)(f * st->inv);
+  }
+}
+
+// ------------------------------------------------------------------- delta
+// A workgroup has 2,048 columns of one packed row.
+namespace {
+constexpr int DCOLS = 2048;
+template <class E>
+__device__ __forceinline__ void delta_body(const VRows& r, const float* z, long long ldz,
+                                           const float* lse, const VTarget& tg, int chunks,
+                                           E* d, long long ldd, int Vp, int dup) {
+  const int j = blockIdx.x / chunks, c0 = (blockIdx.x % chunks) * DCOLS;
+  const int n = r.st->n;
+  if (j >= n && j >= (dup ? dup : (n + VPAD - 1) / VPAD * VPAD)) return;
+  const bool real = j < n;
+  const float l = real ? lse[j] : 0.0f;
+  E* hi = d + (size_t)j * ldd;
+  E* lo = dup ? d + (size_t)(dup + j) * ldd : nullptr;
+  const float* zr = z + (size_t)j * ldz;
+  // 4 columns a thread and step
+#pragma unroll
+  for (int i = 0; i < DCOLS / 1024; ++i) {
+    const int c = c0 + 4 * (int)threadIdx.x + 1024 * i;
+    if (c >= Vp) break;
+    float v[4];
+    f32x4 zz = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    if (real) zz = *(const f32x4*)(zr + c);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = real && c + e < r.V ? expf(zz[e] - l) : 0.0f;
+    if constexpr (sizeof(E) == 4) {
+      *(f32x4*)(hi + c) = f32x4{v[0], v[1], v[2], v[3]};
+    } else {
+      uint32_t b[4], s[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        b[e] = f2bf(v[e]);
+        s[e] = f2bf(v[e] - bf2f(b[e]));
+      }
+      *(u32x2*)(hi + c) = u32x2{b[0] | b[1] << 16, b[2] | b[3] << 16};
+      if (lo) *(u32x2*)(lo + c) = u32x2{s[0] | s[1] << 16, s[2] | s[3] << 16};
+    }
+  }
+  if (!real) return;
+  // the targets among these columns, over what was just written
+  __syncthreads();
+  for (int k = threadIdx.x; k < r.K; k += 256) {
+    const int id = tg.id[(size_t)j * r.K + k];
+    if (id < c0 || id >= c0 + DCOLS) continue;
+    const float v = tg.dt[(size_t)j * r.K + k];
+    put(hi + id, v);
+    if constexpr (sizeof(E) == 2)
+      if (lo) put(lo + id, v - bf2f(f2bf(v)));
+  }
+}
+}  // namespace
+extern "C" __global__ __launch_bounds__(256) void hf_vocab_delta_f32(
+    VRows r, const float* z, long long ldz, const float* lse, VTarget tg, int chunks, float* d,
+    long long ldd, int Vp, int dup) {
+  delta_body<float>(r, z, ldz, lse, tg, chunks, d, ldd, Vp, dup);
+}
+extern "C" __global__ __launch_bounds__(256) void hf_vocab_delta_bf16(
+    VRows r, const float* z, long long ldz, const float* lse, VTarget tg, int chunks, bf16_t* d,
+    long long ldd, int Vp, int dup) {
+  delta_body<bf16_t>(r, z, ldz, lse, tg, chunks, d, ldd, Vp, dup);
+}
+
+namespace {
+template <class E>
+__device__ __forceinline__ void fix_body(const VRows& r, const VTarget& tg, int v0, int Vc, E* d,
+                                         long long ldd) {
+  const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
+  if (i >= (long long)r.st->n * r.K) return;
+  const int id = tg.id[i];
+  if (id >= v0 && id < v0 + Vc) put(d + (size_t)(i / r.K) * ldd + (id - v0), tg.dt[i]);
+}
+}  // namespace
+extern "C" __global__ __launch_bounds__(256) void hf_vocab_fix_f32(VRows r, VTarget tg, int v0,
+                                                                   int Vc, float* d,
+                                                                   long long ldd) {
+  fix_body<float>(r, tg, v0, Vc, d, ldd);
+}
+extern "C" __global__ __launch_bounds__(256) void hf_vocab_fix_bf16(VRows r, VTarget tg, int v0,
+                                                                    int Vc, bf16_t* d,
+                                                                    long long ldd) {
+  fix_body<bf16_t>(r, tg, v0, Vc, d, ldd);
+}
+
+// ------------------------------------------------------------------ finish
+// 4 columns a thread; the splits are added in order, then the dup copy's.
+namespace {
+template <class E>
+__device__ __forceinline__ void finish_body(const VocabState* st, const float* part, int splits,
+                                            long long ss, long long ldp, int dup, int rows,
+                                            int dyn, int D, const int* idx, E* out,
+                                            long long ldo, int accumulate) {
+  const int q = (D + 3) / 4;
+  const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
+  const int j = (int)(i / q), c = 4 * (int)(i % q);
+  if (j >= (dyn ? min(st->n, rows) : rows)) return;
+  f32x4 s = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  for (int z = 0; z < splits; ++z) s += *(const f32x4*)(part + z * ss + j * ldp + c);
+  if (dup)
+    for (int z = 0; z < splits; ++z)
+      s += *(const f32x4*)(part + z * ss + (size_t)(dup + j) * ldp + c);
+  const float g = st->gscale;
+  E* o = out + (size_t)(idx ? idx[j] : j) * ldo + c;
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    if (c + e < D) put(o + e, s[e] * g + (accumulate ? to_f(o[e]) : 0.0f));
+}
+}  // namespace
+extern "C" __global__ __launch_bounds__(256) void hf_vocab_finish_f32(
+    const VocabState* st, const float* part, int splits, long long ss, long long ldp, int dup,
+    int rows, int dyn, int D, const int* idx, float* out, long long ldo, int accumulate) {
+  finish_body<float>(st, part, splits, ss, ldp, dup, rows, dyn, D, idx, out, ldo, accumulate);
+}
+extern "C" __global__ __launch_bounds__(256) void hf_vocab_finish_bf16(
+    const VocabState* st, const float* part, int splits, long long ss, long long ldp, int dup,
+    int rows, int dyn, int D, const int* idx, bf16_t* out, long long ldo, int accumulate) {
+  finish_body<bf16_t>(st, part, splits, ss, ldp, dup, rows, dyn, D, idx, out, ldo, accumulate);
+}
+
+// ------------------------------------------------------------- launchers
+#define HF_LAUNCH(NAME, K, GRID, BLOCK, ...)                                       \
+  do {                                                                             \
+    prof_begin(L, NAME);                                                           \
+    hipExtLaunchKernelGGL(K, dim3((unsigned)(GRID)), dim3(BLOCK), 0, L.stream,     \
+                          prof_a(L), prof_b(L), 0, __VA_ARGS__);                   \
+    prof_end(L, NAME, 0.0, 0.0);                                                   \
+  } while (0)
+
+namespace {
+inline int vec16(const void* p, long long ld, int es) {
+  return ((uintptr_t)p & 15) == 0 && (ld * es) % 16 == 0;
+}
+}  // namespace
+
+void vocab_count(const Launch& L, const VRows& r) {
+  if (r.t && r.T > 0)
+    HF_LAUNCH("hf_vocab_have", hf_vocab_have, (r.T + 3) / 4, 256, r);
+  HF_LAUNCH("hf_vocab_count", hf_vocab_count, 1, 1024, r);
+}
+
+void vocab_pack_rows(const Launch& L, int type, const VRows& r, const void* X, long long ldx,
+                     void* xp, int Dp, int dup, void* dX, long long lddx) {
+  const int grid = r.T + VTILE;
+  if (type == VT_F32)
+    HF_LAUNCH("hf_vocab_pack", hf_vocab_pack_f32, grid, 256, r, (const float*)X, ldx,
+              vec16(X, ldx, 4), (float*)xp, Dp, dup, (float*)dX, lddx);
+  else
+    HF_LAUNCH("hf_vocab_pack", hf_vocab_pack_bf16, grid, 256, r, (const bf16_t*)X, ldx,
+              vec16(X, ldx, 2), (bf16_t*)xp, Dp, dup, (bf16_t*)dX, lddx);
+}
+
+void vocab_pack_matrix(const Launch& L, int type, const void* W, long long ldw, int R, int D,
+                       void* wp, int Dp) {
+  if (type == VT_F32)
+    HF_LAUNCH("hf_vocab_copy", hf_vocab_copy_f32, R, 256, (const float*)W, ldw,
+              vec16(W, ldw, 4), D, (float*)wp, Dp);
+  else
+    HF_LAUNCH("hf_vocab_copy", hf_vocab_copy_bf16, R, 256, (const bf16_t*)W, ldw,
+              vec16(W, ldw, 2), D, (bf16_t*)wp, Dp);
+}
+
+void vocab_target_logits(const Launch& L, int type, const VRows& r, const void* xp, int Dp,
+                         const void* W, long long ldw, float* zt) {
+  if (type == VT_F32)
+    HF_LAUNCH("hf_vocab_tlogit", hf_vocab_tlogit_f32, r.T, 256, r, (const float*)xp, Dp,
+              (const float*)W, ldw, vec16(W, ldw, 4), zt);
+  else
+    HF_LAUNCH("hf_vocab_tlogit", hf_vocab_tlogit_bf16, r.T, 256, r, (const bf16_t*)xp, Dp,
+              (const bf16_t*)W, ldw, vec16(W, ldw, 2), zt);
+}
+
+void vocab_row_loss(const Launch& L, const VRows& r, const float2* stat, int ldstat, int tiles,
+                    const float* z, long long ldz, const VTarget& t, float* lse) {
+  HF_LAUNCH("hf_vocab_row_loss", hf_vocab_row_loss, (r.T + VPAD + 3) / 4, 256, r, stat, ldstat,
+            tiles, z, ldz, t, lse);
+}
+
+void vocab_loss_sum(const Launch& L, const VRows& r, float* loss) {
+  HF_LAUNCH("hf_vocab_loss_sum", hf_vocab_loss_sum, 1, 1024, r.row_loss, r.T, r.st, loss);
+}
+
+void vocab_delta(const Launch& L, int type, const VRows& r, const float* z, long long ldz,
+                 const float* lse, const VTarget& t, int rows, void* d, long long ldd, int Vp,
+                 int dup) {
+  const int chunks = (Vp + DCOLS - 1) / DCOLS;
+  const long long grid = (long long)rows * chunks;
+  if (type == VT_F32)
+    HF_LAUNCH("hf_vocab_delta", hf_vocab_delta_f32, grid, 256, r, z, ldz, lse, t, chunks,
+              (float*)d, ldd, Vp, dup);
+  else
+    HF_LAUNCH("hf_vocab_delta", hf_vocab_delta_bf16, grid, 256, r, z, ldz, lse, t, chunks,
+              (bf16_t*)d, ldd, Vp, dup);
+}
+
+void vocab_fix(const Launch& L, int type, const VRows& r, const VTarget& t, int v0, int Vc,
+               void* d, long long ldd) {
+  const long long grid = ((long long)r.T * r.K + 255) / 256;
+  if (type == VT_F32)
+    HF_LAUNCH("hf_vocab_fix", hf_vocab_fix_f32, grid, 256, r, t, v0, Vc, (float*)d, ldd);
+  else
+    HF_LAUNCH("hf_vocab_fix", hf_vocab_fix_bf16, grid, 256, r, t, v0, Vc, (bf16_t*)d, ldd);
+}
+
+void vocab_finish(const Launch& L, int type, const VocabState* st, const float* part, int splits,
+                  long long ss, long long ldp, int dup, int rows, int dyn, int D, const int* idx,
+                  void* out, long long ldo, int accumulate) {
+  const long long grid = ((long long)rows * ((D + 3) / 4) + 255) / 256;
+  if (grid < 1) return;
+  if (type == VT_F32)
+    HF_LAUNCH("hf_vocab_finish", hf_vocab_finish_f32, grid, 256, st, part, splits, ss, ldp, dup,
+              rows, dyn, D, idx, (float*)out, ldo, accumulate);
+  else
+    HF_LAUNCH("hf_vocab_finish", hf_vocab_finish_bf16, grid, 256, st, part, splits, ss, ldp, dup,
+              rows, dyn, D, idx, (bf16_t*)out, ldo, accumulate);
+}
+
+}  // namespace hfk

@@ -29,6 +29,12 @@ CURVATURES = {"hessian": HF_HESSIAN, "gauss_newton": HF_GAUSS_NEWTON,
               "hybrid": HF_HYBRID}
 SOLVERS = {"cg": HF_SOLVER_CG, "bicgstab": HF_SOLVER_BICGSTAB}
 PRECS = {"fp32": HF_FP32, "bf16": HF_BF16_INPUTS}
+# HFVocab: the type of rows, matrices and gradients
+HF_TYPE_FP32, HF_TYPE_BF16 = 0, 1
+TYPES = {"fp32": HF_TYPE_FP32, "bf16": HF_TYPE_BF16}
+HF_IGNORE = -100          # a masked label, token or id
+HF_VOCAB_MAX, HF_VOCAB_MAX_WIDTH = 1 << 22, 65536
+HF_VOCAB_MAX_ROWS, HF_VOCAB_MAX_TOP = 262144, 128
 
 # Every function declared in include/hf.h.
 EXPORTS = (
@@ -39,6 +45,11 @@ EXPORTS = (
     "hf_set_trace", "hf_build_id", "hf_hvp_noalloc", "hf_check", "hf_last_error",
     "hf_strerror", "hf_prof_enable", "hf_prof_only",
     "hf_prof_reset", "hf_prof_count", "hf_prof_get",
+    "hf_vocab_create", "hf_vocab_destroy", "hf_vocab_set_stream",
+    "hf_vocab_workspace_bytes", "hf_vocab_set_workspace", "hf_vocab_loss",
+    "hf_vocab_loss_grad", "hf_vocab_distill", "hf_vocab_distill_grad",
+    "hf_vocab_embed", "hf_vocab_embed_grad", "hf_vocab_check",
+    "hf_vocab_last_error",
 )
 
 
@@ -152,6 +163,23 @@ def lib():
         "hf_prof_get": (ctypes.c_int, [P, I32, ctypes.POINTER(ctypes.c_char_p),
                                        ctypes.POINTER(I64), ctypes.POINTER(D),
                                        ctypes.POINTER(D), ctypes.POINTER(D)]),
+        "hf_vocab_create": (ctypes.c_int, [I64, I32, I32, I64, P, ctypes.POINTER(P)]),
+        "hf_vocab_destroy": (ctypes.c_int, [P]),
+        "hf_vocab_set_stream": (ctypes.c_int, [P, P]),
+        "hf_vocab_workspace_bytes": (SZ, [P, I64]),
+        "hf_vocab_set_workspace": (ctypes.c_int, [P, P, SZ]),
+        "hf_vocab_loss": (ctypes.c_int, [P, P, I64, P, I64, P, I64, F32, P, P]),
+        "hf_vocab_loss_grad": (ctypes.c_int, [P, P, I64, P, I64, P, I64, F32, P, P,
+                                              P, I64, P, I64, I32]),
+        "hf_vocab_distill": (ctypes.c_int, [P, P, I64, P, I64, P, I64, P, I64, I32,
+                                            F32, I64, F32, P, P]),
+        "hf_vocab_distill_grad": (ctypes.c_int, [P, P, I64, P, I64, P, I64, P, I64,
+                                                 I32, F32, I64, F32, P, P, P, I64, P,
+                                                 I64, I32]),
+        "hf_vocab_embed": (ctypes.c_int, [P, P, I64, P, I64, F32, P, I64]),
+        "hf_vocab_embed_grad": (ctypes.c_int, [P, P, I64, F32, P, I64, P, I64, I32]),
+        "hf_vocab_check": (ctypes.c_int, [P]),
+        "hf_vocab_last_error": (ctypes.c_char_p, [P]),
     }
     for name, (res, args) in sig.items():
         f = getattr(L, name)
@@ -443,3 +471,204 @@ class HFNet:
             out[name.value.decode()] = dict(launches=launches.value, ms=ms.value,
                                             flops=fl.value, bytes=by.value)
         return out
+
+
+class HFVocab:
+    """A vocabulary context of the C library plus its torch-allocated
+    workspace: the token embedding, and the softmax head over a large
+    vocabulary with the loss of hard labels or of a teacher's top logits.
+
+    vocab x width: the matrices; max_rows: the most rows any call will use;
+    dtype: "fp32" or "bf16", of the rows, the matrices and their gradients;
+    ws_rows: size the workspace for calls of up to this many rows only
+    (default max_rows).  Rows may be strided (the last dimension contiguous).
+    Labels, tokens and ids are int32, HF_IGNORE where masked.  Calls run on
+    torch's current stream of the context's device.
+    """
+
+    def __init__(self, vocab, width, max_rows, dtype="fp32", device="cuda",
+                 ws_rows=None):
+        import torch
+        self.vocab, self.width = int(vocab), int(width)
+        self.max_rows = int(max_rows)
+        self.dtype = {"fp32": torch.float32, "bf16": torch.bfloat16}[dtype]
+        L = lib()
+        h = ctypes.c_void_p()
+        rc = L.hf_vocab_create(self.vocab, self.width, TYPES[dtype], self.max_rows,
+                               None, ctypes.byref(h))
+        if rc != HF_OK:
+            raise HFError(rc, "hf_vocab_create rejected vocab=%d width=%d max_rows=%d"
+                          % (self.vocab, self.width, self.max_rows))
+        self._h = h
+        nbytes = int(L.hf_vocab_workspace_bytes(
+            h, self.max_rows if ws_rows is None else int(ws_rows)))
+        if nbytes == 0:
+            raise ValueError("ws_rows %s outside [1, %d]" % (ws_rows, self.max_rows))
+        device = torch.device(device)
+        if device.type == "cuda" and device.index is None:
+            device = torch.device("cuda", torch.cuda.current_device())
+        self.device = device
+        self.workspace = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+        with torch.cuda.device(self.device):
+            self._check(L.hf_vocab_set_workspace(h, self.workspace.data_ptr(), nbytes))
+
+    # ------------------------------------------------------------- plumbing
+    def _check(self, rc):
+        if rc != HF_OK:
+            raise HFError(rc, lib().hf_vocab_last_error(self._h).decode())
+        return rc
+
+    def _call(self, fn, *args):
+        import torch
+        stream = torch.cuda.current_stream(self.device).cuda_stream
+        if torch.cuda.current_device() != self.device.index:
+            with torch.cuda.device(self.device):
+                lib().hf_vocab_set_stream(self._h, stream)
+                return self._check(getattr(lib(), fn)(self._h, *args))
+        lib().hf_vocab_set_stream(self._h, stream)
+        return self._check(getattr(lib(), fn)(self._h, *args))
+
+    def close(self):
+        if getattr(self, "_h", None) is not None:
+            lib().hf_vocab_destroy(self._h)
+            self._h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def _mat(self, t, rows, cols, dtype, what):
+        """(pointer, elements between rows) of a rows x cols tensor."""
+        import torch
+        if not isinstance(t, torch.Tensor) or t.device != self.device:
+            raise TypeError("%s must be a tensor on %s" % (what, self.device))
+        if t.dtype != dtype:
+            raise TypeError("%s must be %s, got %s" % (what, dtype, t.dtype))
+        if tuple(t.shape) != (rows, cols):
+            raise ValueError("%s is %s, expected %d x %d"
+                             % (what, tuple(t.shape), rows, cols))
+        if cols > 1 and t.stride(1) != 1:
+            raise ValueError("the rows of %s must be contiguous" % what)
+        if rows > 1 and t.stride(0) < cols:
+            raise ValueError("the rows of %s overlap" % what)
+        return t.data_ptr(), (t.stride(0) if rows > 1 else cols)
+
+    def _vec(self, t, n, dtype, what):
+        import torch
+        if not isinstance(t, torch.Tensor) or t.device != self.device:
+            raise TypeError("%s must be a tensor on %s" % (what, self.device))
+        if t.dtype != dtype:
+            raise TypeError("%s must be %s, got %s" % (what, dtype, t.dtype))
+        if t.numel() != n or not t.is_contiguous():
+            raise ValueError("%s must be %d contiguous elements" % (what, n))
+        return t.data_ptr()
+
+    def _rows(self, X, what):
+        if X.dim() != 2 or X.shape[1] != self.width:
+            raise ValueError("%s must be rows x %d" % (what, self.width))
+        return int(X.shape[0])
+
+    def _out(self, *shape, dtype=None):
+        import torch
+        return torch.empty(*shape, dtype=dtype or self.dtype, device=self.device)
+
+    def _head(self, fn, X, W, targets, T, denom, loss, row_loss, grad):
+        """A head call: targets and their arguments as the C call takes them."""
+        import torch
+        f32 = torch.float32
+        xp, ldx = self._mat(X, T, self.width, self.dtype, "X")
+        wp, ldw = self._mat(W, self.vocab, self.width, self.dtype, "W")
+        loss = self._out(1, dtype=f32) if loss is None else loss
+        row_loss = self._out(T, dtype=f32) if row_loss is None else row_loss
+        args = [xp, ldx, wp, ldw, *targets, T, float(denom),
+                self._vec(loss, 1, f32, "loss"), self._vec(row_loss, T, f32, "row_loss")]
+        if grad is None:
+            self._call(fn, *args)
+            return loss, row_loss
+        dX, dW, need_dX, need_dW, accumulate = grad
+        if accumulate and dW is None:
+            raise ValueError("accumulate needs the dW to add to")
+        if dX is None and need_dX:
+            dX = self._out(T, self.width)
+        if dW is None and need_dW:
+            dW = self._out(self.vocab, self.width)
+        for t, rows, what in ((dX, T, "dX"), (dW, self.vocab, "dW")):
+            args += [None, 0] if t is None else self._mat(t, rows, self.width, self.dtype,
+                                                          what)
+        self._call(fn, *args, 1 if accumulate else 0)
+        return loss, row_loss, dX, dW
+
+    def _list(self, ids, t, T, tau):
+        import torch
+        if ids.dim() != 2:
+            raise ValueError("ids must be rows x top")
+        K = int(ids.shape[1])
+        ip, ldi = self._mat(ids, T, K, torch.int32, "ids")
+        tp, ldt = self._mat(t, T, K, torch.float32, "t")
+        return ip, ldi, tp, ldt, K, float(tau)
+
+    # -------------------------------------------------------------- the ABI
+    def hf_vocab_loss(self, X, W, y, denom=0.0, loss=None, row_loss=None):
+        """Softmax cross entropy of X W^T: (loss, row losses)."""
+        import torch
+        T = self._rows(X, "X")
+        return self._head("hf_vocab_loss", X, W, [self._vec(y, T, torch.int32, "y")], T,
+                          denom, loss, row_loss, None)
+
+    def hf_vocab_loss_grad(self, X, W, y, denom=0.0, loss=None, row_loss=None, dX=None,
+                           dW=None, need_dX=True, need_dW=True, accumulate=False):
+        """hf_vocab_loss and its gradients: (loss, row losses, dX, dW).
+        need_dX / need_dW False: that gradient is not computed (None).
+        accumulate: dW += (dW given)."""
+        import torch
+        T = self._rows(X, "X")
+        return self._head("hf_vocab_loss_grad", X, W, [self._vec(y, T, torch.int32, "y")],
+                          T, denom, loss, row_loss, (dX, dW, need_dX, need_dW, accumulate))
+
+    def hf_vocab_distill(self, X, W, ids, t, tau=1.0, denom=0.0, loss=None,
+                         row_loss=None):
+        """Divergence from a teacher's top logits t at ids, at temperature
+        tau: (loss, row losses)."""
+        T = self._rows(X, "X")
+        return self._head("hf_vocab_distill", X, W, self._list(ids, t, T, tau), T, denom,
+                          loss, row_loss, None)
+
+    def hf_vocab_distill_grad(self, X, W, ids, t, tau=1.0, denom=0.0, loss=None,
+                              row_loss=None, dX=None, dW=None, need_dX=True,
+                              need_dW=True, accumulate=False):
+        """hf_vocab_distill and its gradients: (loss, row losses, dX, dW)."""
+        T = self._rows(X, "X")
+        return self._head("hf_vocab_distill_grad", X, W, self._list(ids, t, T, tau), T,
+                          denom, loss, row_loss, (dX, dW, need_dX, need_dW, accumulate))
+
+    def hf_vocab_embed(self, E, tok, scale=1.0, out=None):
+        """scale E[tok], zeros where tok is HF_IGNORE."""
+        import torch
+        T = int(tok.numel())
+        out = self._out(T, self.width) if out is None else out
+        ep, lde = self._mat(E, self.vocab, self.width, self.dtype, "E")
+        op, ldo = self._mat(out, T, self.width, self.dtype, "out")
+        self._call("hf_vocab_embed", ep, lde, self._vec(tok, T, torch.int32, "tok"), T,
+                   float(scale), op, ldo)
+        return out
+
+    def hf_vocab_embed_grad(self, tok, dout, scale=1.0, dE=None, accumulate=False):
+        """Gradient of hf_vocab_embed with respect to E; accumulate: dE +=
+        (dE given)."""
+        import torch
+        T = self._rows(dout, "dout")
+        if accumulate and dE is None:
+            raise ValueError("accumulate needs the dE to add to")
+        dE = self._out(self.vocab, self.width) if dE is None else dE
+        dp, ldd = self._mat(dout, T, self.width, self.dtype, "dout")
+        ep, lde = self._mat(dE, self.vocab, self.width, self.dtype, "dE")
+        self._call("hf_vocab_embed_grad", self._vec(tok, T, torch.int32, "tok"), T,
+                   float(scale), dp, ldd, ep, lde, 1 if accumulate else 0)
+        return dE
+
+    def hf_vocab_check(self):
+        """Synchronise and raise HFError(HF_ELABEL) for a label, token or id
+        outside the vocabulary seen since the last check."""
+        self._call("hf_vocab_check")

@@ -36,7 +36,7 @@ inline int64_t up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
 
 struct Layout {
   size_t state, pos, idx, rloss, lse, zt, tid, tdt, stat, xp, wp, z, partx, partw;
-  size_t key, spos, tkey, tpos, hist, epart, need;
+  size_t key, spos, tkey, tpos, hist, first, epart, need;
 };
 
 }  // namespace
@@ -153,6 +153,7 @@ void plan(const hf_vocab* c, int64_t R, Layout* l) {
   l->tkey = take(r * 4);
   l->tpos = take(r * 4);
   l->hist = take(vocab_sort_hist(R, c->V) * 4);
+  l->first = take((size_t)c->V * 4);
   l->epart = take(vocab_sort_part(R, c->D, c->type) * 4);
   l->need = off;
 }
@@ -410,7 +411,7 @@ void head(hf_vocab* c, VRows r, const void* X, int64_t ldx, const void* W, int64
     pe.out = out;
     pe.ldo = g->lddw;
     pe.accumulate = g->accumulate;
-    pe.vec = g->lddw % 4 == 0 && (uintptr_t)out % (4 * es) == 0;
+    pe.vec = (g->lddw * es) % 16 == 0 && (uintptr_t)out % 16 == 0;
     vocab_dw(L, type, q, pe);
     if (q.splits > 1)
       vocab_finish(L, type, r.st, pe.part, q.splits, pe.split_stride, Dp, 0, pn, 0, D, nullptr,
@@ -615,7 +616,7 @@ int hf_vocab_embed_grad(hf_vocab* c, const int32_t* tok, int64_t rows, float sca
   const Launch L{c->stream, nullptr};
   const Layout& l = c->lay;
   const VSort s = {c->at<int>(l.key), c->at<int>(l.spos), c->at<int>(l.tkey), c->at<int>(l.tpos),
-                   c->at<unsigned>(l.hist), c->at<float>(l.epart)};
+                   c->at<unsigned>(l.hist), c->at<int>(l.first), c->at<float>(l.epart)};
   vocab_embed_grad(L, c->type, tok, (int)rows, c->V, c->D, scale, dout, ldd, dE, lde, accumulate,
                    s, c->st());
   return end(c, captured);

@@ -4,10 +4,15 @@
 // Both are bound by memory: each row is read and written once.
 //
 // The gradient sorts the rows by token (stable, two radix passes), so that the
-// rows of one token are consecutive and every row of dE is written by one
-// workgroup, zeros included: no atomics on sums, the same bits every time.
-// Runs of 64 sorted places that hold one token only are summed beforehand in
-// parallel; a frequent token's row then adds those sums instead of its rows.
+// rows of one token are consecutive, and cuts the sorted places into runs of
+// RUN.  A wave sums a run, strip of columns by strip, and writes the tokens
+// that lie within it; what reaches over a run's ends goes to partial sums.
+// The last kernel has the rows of dE: it joins the partial sums of tokens that
+// span runs, in order, and writes the zeros.  So the work per wave does not
+// depend on how often a token comes, no sum uses atomics, and every row of dE
+// is written once, with the same bits every time.
+#include <algorithm>
+
 #include "vocab_internal.h"
 
 namespace hfk {
@@ -146,16 +151,21 @@ __device__ __forceinline__ void scan_digits(unsigned* a, int n, unsigned* tmp) {
   __syncthreads();
 }
 
+// Lanes whose first `bits` bits of v agree with this lane's, of those in m.
+__device__ __forceinline__ unsigned long long alike(unsigned long long m, unsigned v, int bits) {
+  for (int b = 0; b < bits; ++b) {
+    const unsigned long long one = __ballot((v >> b) & 1);
+    m &= ((v >> b) & 1) ? one : ~one;
+  }
+  return m;
+}
+
 // The place of each thread's element among the elements of its digit: `base`
 // holds where each digit's next element goes.  The waves take their turns in
 // order, so that equal digits keep their order.
 __device__ __forceinline__ unsigned place(unsigned* base, int d, bool valid, int bits) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  unsigned long long same = __ballot(valid);
-  for (int b = 0; b < bits; ++b) {
-    const unsigned long long m = __ballot((d >> b) & 1);
-    same &= ((d >> b) & 1) ? m : ~m;
-  }
+  const unsigned long long same = alike(__ballot(valid), (unsigned)d, bits);
   const unsigned below = __popcll(same & ((1ull << lane) - 1));
   unsigned at = 0;
   for (int w = 0; w < CHUNK / 64; ++w) {
@@ -171,10 +181,11 @@ __device__ __forceinline__ unsigned place(unsigned* base, int d, bool valid, int
 }
 }  // namespace
 
-// histogram of the low digit; zeros in the high digit's
+// histogram of the low digit; zeros in the high digit's; no place of any token
 extern "C" __global__ __launch_bounds__(CHUNK) void hf_vocab_sort_hist(
-    const int32_t* tok, int T, int V, int bits, unsigned* hist, unsigned* hist2,
+    const int32_t* tok, int T, int V, int bits, unsigned* hist, unsigned* hist2, int* first,
     VocabState* st) {
+  for (int v = blockIdx.x * CHUNK + threadIdx.x; v < V; v += gridDim.x * CHUNK) first[v] = -1;
   __shared__ unsigned h[MAXDIG];
   const int digs = 1 << bits, t = blockIdx.x * CHUNK + threadIdx.x;
   for (int d = threadIdx.x; d < digs; d += CHUNK) h[d] = 0;
@@ -226,13 +237,28 @@ extern "C" __global__ __launch_bounds__(CHUNK) void hf_vocab_sort_pass(
   if (valid) {
     okey[at] = k;
     opos[at] = p;
-    if (tok) atomicAdd(&hist2[(size_t)(at / CHUNK) * digs + (k >> bits)], 1u);
+  }
+  if (tok) {
+    // one addition per wave for the lanes of one high digit and workgroup
+    // (frequent tokens share theirs)
+    const unsigned slot = (at / CHUNK) * digs + ((unsigned)k >> bits);
+    const unsigned long long m =
+        alike(__ballot(valid), slot, 32 - __clz((unsigned)(blocks * digs - 1) | 1u));
+    if (valid && (m & ((1ull << (threadIdx.x & 63)) - 1)) == 0)
+      atomicAdd(&hist2[slot], (unsigned)__popcll(m));
   }
 }
 
-// Both passes of up to 1,024 rows in one workgroup.
+// Both passes of up to 1,024 rows in the first workgroup; the others clear the
+// places of the tokens.
 extern "C" __global__ __launch_bounds__(CHUNK) void hf_vocab_sort_one(
-    const int32_t* tok, int T, int V, int bits, int* okey, int* opos, VocabState* st) {
+    const int32_t* tok, int T, int V, int bits, int* okey, int* opos, int* first,
+    VocabState* st) {
+  if (blockIdx.x > 0) {
+    for (int v = (blockIdx.x - 1) * CHUNK + threadIdx.x; v < V; v += (gridDim.x - 1) * CHUNK)
+      first[v] = -1;
+    return;
+  }
   __shared__ unsigned base[MAXDIG], tmp[16];
   __shared__ int key[CHUNK], pos[CHUNK];
   const int digs = 1 << bits, t = threadIdx.x;
@@ -265,133 +291,148 @@ extern "C" __global__ __launch_bounds__(CHUNK) void hf_vocab_sort_one(
 
 // --------------------------------------------------------------- gradient
 namespace {
-constexpr int RUN = 64;      // sorted places per chunk
+constexpr int RUN = 32;      // sorted places per wave
 constexpr int VROWS = 8;     // rows of dE per workgroup
 
-// acc += rows pos[a .. b) of dout
 template <class E, bool VEC>
-__device__ __forceinline__ void add_rows(const E* dout, long long ldd, const int* pos, int a,
-                                         int b, int strip, int lane, int D,
-                                         float (&acc)[Strip<E, VEC>::EPC]) {
+__device__ __forceinline__ void emit(E* row, int strip, int lane, int D, float scale,
+                                     int accumulate, float (&acc)[Strip<E, VEC>::EPC]) {
   using S = Strip<E, VEC>;
+#pragma unroll
+  for (int e = 0; e < S::EPC; ++e) acc[e] *= scale;
+  if (accumulate) {
+    float old[S::EPC];
+    S::load(row, strip, lane, D, old);
+#pragma unroll
+    for (int e = 0; e < S::EPC; ++e) acc[e] += old[e];
+  }
+  S::store(row, strip, lane, D, acc);
+}
+
+// One run and strip.  part[2 run]: the sum of the token that began before the
+// run (or fills it from its start and goes on); part[2 run + 1]: of the one
+// that begins within it and goes on.  first[token]: its first sorted place.
+template <class E, bool VEC>
+__device__ __forceinline__ void runs_body(const int* key, const int* pos, int T, int V, int D,
+                                          int strips, float scale, const E* dout,
+                                          long long ldd, float* part, int* first, E* dE,
+                                          long long lde, int accumulate) {
+  using S = Strip<E, VEC>;
+  const int lane = threadIdx.x & 63;
+  const long long unit = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int run = (int)(unit / strips), strip = (int)(unit % strips);
+  const int a = run * RUN;
+  if (a >= T) return;
+  // lane l: place a - 1 + l
+  const int at = a - 1 + lane;
+  const int k = at >= 0 && at < T && lane < RUN + 2 ? key[at] : -1;
+  const int p = at >= 0 && at < T && lane < RUN + 1 ? pos[at] : 0;
+  const int before = __shfl_up(k, 1, 64);
+  if (strip == 0 && lane >= 1 && lane <= RUN && k >= 0 && k < V && k != before) first[k] = at;
+  // places of tokens in the run (masked ones come last)
+  const int n = __popcll(__ballot(lane >= 1 && lane <= RUN && k >= 0 && k < V));
+  float acc[S::EPC] = {};
+  int head = n > 0 && __shfl(k, 1, 64) == __shfl(k, 0, 64);
   constexpr int U = 8;
-  int i = a;
-  for (; i + U <= b; i += U) {
+  for (int i0 = 0; i0 < n; i0 += U) {
     float v[U][S::EPC];
 #pragma unroll
     for (int u = 0; u < U; ++u)
-      S::load(dout + (size_t)__builtin_amdgcn_readfirstlane(pos[i + u]) * ldd, strip, lane, D,
-              v[u]);
+      if (i0 + u < n)
+        S::load(dout + (size_t)__builtin_amdgcn_readlane(p, 1 + i0 + u) * ldd, strip, lane, D,
+                v[u]);
 #pragma unroll
-    for (int u = 0; u < U; ++u)
+    for (int u = 0; u < U; ++u) {
+      if (i0 + u >= n) break;
 #pragma unroll
       for (int e = 0; e < S::EPC; ++e) acc[e] += v[u][e];
-  }
-  for (; i < b; ++i) {
-    float v[S::EPC];
-    S::load(dout + (size_t)__builtin_amdgcn_readfirstlane(pos[i]) * ldd, strip, lane, D, v);
+      const int cur = __builtin_amdgcn_readlane(k, 1 + i0 + u);
+      const int nxt = __builtin_amdgcn_readlane(k, 2 + i0 + u);
+      const bool last = i0 + u + 1 == RUN;
+      if (cur == nxt && !last) continue;
+      // the token's places in this run end here
+      if (head || cur == nxt) {
+        float* o = part + (((size_t)2 * run + !head) * strips + strip) * S::COLS;
 #pragma unroll
-    for (int e = 0; e < S::EPC; ++e) acc[e] += v[e];
+        for (int e = 0; e < S::EPC; ++e) o[e * 64 + lane] = acc[e];
+      } else {
+        emit<E, VEC>(dE + (size_t)cur * lde, strip, lane, D, scale, accumulate, acc);
+      }
+      head = 0;
+#pragma unroll
+      for (int e = 0; e < S::EPC; ++e) acc[e] = 0.0f;
+    }
   }
 }
 
-// part[c][col] = sum of the chunk's rows, where all of them are one token's;
-// col as the lane has it, strip by strip
+// Rows of dE: zeros where there is no token, joined sums where a token spans
+// runs.  A workgroup's rows lie far apart, so that the frequent tokens (low
+// numbers, as vocabularies are ordered) do not share one.
 template <class E, bool VEC>
-__device__ __forceinline__ void chunk_body(const int* key, const int* pos, int V, int D,
-                                           int strips, const E* dout, long long ldd,
-                                           float* part) {
+__device__ __forceinline__ void rows_body(const int* key, int T, int V, int D, int strips,
+                                          float scale, const float* part, const int* first,
+                                          E* dE, long long lde, int accumulate) {
   using S = Strip<E, VEC>;
-  const int c = blockIdx.x, a = c * RUN;
-  const int k = key[a];
-  if (k >= V || key[a + RUN - 1] != k) return;
   const int lane = threadIdx.x & 63;
-  for (int strip = threadIdx.x >> 6; strip < strips; strip += 4) {
+  const int mine = blockIdx.x + lane * gridDim.x;
+  const int f = lane < VROWS && mine < V && T > 0 ? first[mine] : -1;
+  for (int u = threadIdx.x >> 6; u < VROWS * strips; u += 4) {
+    const int i = u / strips, strip = u % strips;
+    const int v = blockIdx.x + i * gridDim.x;
+    if (v >= V) return;
+    const int a = __builtin_amdgcn_readlane(f, i);
     float acc[S::EPC] = {};
-    add_rows<E, VEC>(dout, ldd, pos, a, a + RUN, strip, lane, D, acc);
-    float* p = part + ((size_t)c * strips + strip) * S::COLS;
-#pragma unroll
-    for (int e = 0; e < S::EPC; ++e) p[e * 64 + lane] = acc[e];
-  }
-}
-
-template <class E, bool VEC>
-__device__ __forceinline__ void grad_body(const int* key, const int* pos, int T, int V, int D,
-                                          int strips, float scale, const E* dout, long long ldd,
-                                          const float* part, E* dE, long long lde,
-                                          int accumulate) {
-  using S = Strip<E, VEC>;
-  __shared__ int lb[VROWS + 1];
-  const int v0 = blockIdx.x * VROWS, tid = threadIdx.x, lane = tid & 63;
-  if (tid <= VROWS) {
-    // first place whose token is not below v
-    const int v = v0 + tid;
-    int lo = 0, hi = T;
+    if (a < 0) {
+      if (!accumulate) S::store(dE + (size_t)v * lde, strip, lane, D, acc);
+      continue;
+    }
+    const int run = a / RUN, end = (run + 1) * RUN;
+    if (end >= T || key[end] != v) continue;     // within its run: written
+    const size_t slot = 2 * (size_t)run + 1;
+    int lo = run + 1, hi = (T + RUN - 1) / RUN;  // runs past lo that start with v
     while (lo < hi) {
       const int mid = (lo + hi) >> 1;
-      if (key[mid] < v) lo = mid + 1;
+      if (key[mid * RUN] == v) lo = mid + 1;
       else hi = mid;
     }
-    lb[tid] = lo;
-  }
-  __syncthreads();
-  for (int u = tid >> 6; u < VROWS * strips; u += 4) {
-    const int i = u / strips, strip = u % strips, v = v0 + i;
-    if (v >= V) return;
-    const int a = __builtin_amdgcn_readfirstlane(lb[i]);
-    const int b = __builtin_amdgcn_readfirstlane(lb[i + 1]);
-    if (a == b && accumulate) continue;
-    E* row = dE + (size_t)v * lde;
-    float acc[S::EPC] = {};
-    const int c0 = (a + RUN - 1) / RUN, c1 = b / RUN;
-    if (c0 < c1) {
-      add_rows<E, VEC>(dout, ldd, pos, a, c0 * RUN, strip, lane, D, acc);
-      int c = c0;
-      constexpr int U = 4;
-      for (; c + U <= c1; c += U) {
-        float w[U][S::EPC];
+    auto at = [&](size_t sl, int e) {
+      return part[(sl * strips + strip) * S::COLS + e * 64 + lane];
+    };
 #pragma unroll
-        for (int x = 0; x < U; ++x)
+    for (int e = 0; e < S::EPC; ++e) acc[e] = at(slot, e);
+    int r = run + 1;
+    constexpr int U = 8;
+    for (; r + U <= lo; r += U) {
+      float w[U][S::EPC];
 #pragma unroll
-          for (int e = 0; e < S::EPC; ++e)
-            w[x][e] = part[((size_t)(c + x) * strips + strip) * S::COLS + e * 64 + lane];
+      for (int x = 0; x < U; ++x)
 #pragma unroll
-        for (int x = 0; x < U; ++x)
+        for (int e = 0; e < S::EPC; ++e) w[x][e] = at(2 * (size_t)(r + x), e);
 #pragma unroll
-          for (int e = 0; e < S::EPC; ++e) acc[e] += w[x][e];
-      }
-      for (; c < c1; ++c)
+      for (int x = 0; x < U; ++x)
 #pragma unroll
-        for (int e = 0; e < S::EPC; ++e)
-          acc[e] += part[((size_t)c * strips + strip) * S::COLS + e * 64 + lane];
-      add_rows<E, VEC>(dout, ldd, pos, c1 * RUN, b, strip, lane, D, acc);
-    } else {
-      add_rows<E, VEC>(dout, ldd, pos, a, b, strip, lane, D, acc);
+        for (int e = 0; e < S::EPC; ++e) acc[e] += w[x][e];
     }
+    for (; r < lo; ++r)
 #pragma unroll
-    for (int e = 0; e < S::EPC; ++e) acc[e] *= scale;
-    if (accumulate) {
-      float old[S::EPC];
-      S::load(row, strip, lane, D, old);
-#pragma unroll
-      for (int e = 0; e < S::EPC; ++e) acc[e] += old[e];
-    }
-    S::store(row, strip, lane, D, acc);
+      for (int e = 0; e < S::EPC; ++e) acc[e] += at(2 * (size_t)r, e);
+    emit<E, VEC>(dE + (size_t)v * lde, strip, lane, D, scale, accumulate, acc);
   }
 }
 }  // namespace
 
 #define HF_EMBED_GRAD(SUF, E, VEC)                                                          \
-  extern "C" __global__ __launch_bounds__(256) void hf_vocab_embed_chunk_##SUF(             \
-      const int* key, const int* pos, int V, int D, int strips, const E* dout,              \
-      long long ldd, float* part) {                                                         \
-    chunk_body<E, VEC>(key, pos, V, D, strips, dout, ldd, part);                            \
-  }                                                                                         \
-  extern "C" __global__ __launch_bounds__(256) void hf_vocab_embed_grad_##SUF(              \
+  extern "C" __global__ __launch_bounds__(256) void hf_vocab_embed_runs_##SUF(              \
       const int* key, const int* pos, int T, int V, int D, int strips, float scale,         \
-      const E* dout, long long ldd, const float* part, E* dE, long long lde,                \
+      const E* dout, long long ldd, float* part, int* first, E* dE, long long lde,          \
       int accumulate) {                                                                     \
-    grad_body<E, VEC>(key, pos, T, V, D, strips, scale, dout, ldd, part, dE, lde, accumulate); \
+    runs_body<E, VEC>(key, pos, T, V, D, strips, scale, dout, ldd, part, first, dE, lde,    \
+                      accumulate);                                                          \
+  }                                                                                         \
+  extern "C" __global__ __launch_bounds__(256) void hf_vocab_embed_rows_##SUF(              \
+      const int* key, int T, int V, int D, int strips, float scale, const float* part,      \
+      const int* first, E* dE, long long lde, int accumulate) {                             \
+    rows_body<E, VEC>(key, T, V, D, strips, scale, part, first, dE, lde, accumulate);       \
   }
 HF_EMBED_GRAD(f32, float, false)
 HF_EMBED_GRAD(f32_v, float, true)
@@ -425,7 +466,7 @@ size_t vocab_sort_hist(long long T, int V) {
 }
 size_t vocab_sort_part(long long T, int D, int type) {
   const int es = type == VT_F32 ? 4 : 2;
-  return (size_t)(T / RUN) * strips_of(D, es) * (1024 / es);
+  return 2 * (size_t)((T + RUN - 1) / RUN) * strips_of(D, es) * (1024 / es);
 }
 
 void vocab_embed(const Launch& L, int type, const void* E, long long lde, int V, int D,
@@ -449,30 +490,34 @@ void vocab_embed_grad(const Launch& L, int type, const int32_t* tok, int T, int 
   const int es = type == VT_F32 ? 4 : 2, strips = strips_of(D, es), bits = digit_bits(V);
   const bool vec = vec16(dout, ldd, D, es) && vec16(dE, lde, D, es);
   if (T > 0 && T <= CHUNK) {
-    HF_LAUNCH("hf_vocab_sort", hf_vocab_sort_one, 1, CHUNK, tok, T, V, bits, s.key, s.pos, st);
+    // enough workgroups to clear a large vocabulary's places beside the sort
+    const int grid = 1 + std::min(64, (V + CHUNK - 1) / CHUNK);
+    HF_LAUNCH("hf_vocab_sort", hf_vocab_sort_one, grid, CHUNK, tok, T, V, bits, s.key, s.pos,
+              s.first, st);
   } else if (T > 0) {
     const int blocks = (T + CHUNK - 1) / CHUNK;
     unsigned* h2 = s.hist + ((size_t)1 << bits) * blocks;
     HF_LAUNCH("hf_vocab_sort", hf_vocab_sort_hist, blocks, CHUNK, tok, T, V, bits, s.hist, h2,
-              st);
+              s.first, st);
     HF_LAUNCH("hf_vocab_sort", hf_vocab_sort_pass, blocks, CHUNK, tok, (const int*)nullptr,
               (const int*)nullptr, T, V, bits, (const unsigned*)s.hist, h2, s.tkey, s.tpos, st);
     HF_LAUNCH("hf_vocab_sort", hf_vocab_sort_pass, blocks, CHUNK, (const int32_t*)nullptr,
               (const int*)s.tkey, (const int*)s.tpos, T, V, bits, (const unsigned*)h2,
               (unsigned*)nullptr, s.key, s.pos, st);
   }
-  const int chunks = T / RUN, grid = (V + VROWS - 1) / VROWS;
-#define HF_EG(SUF, E)                                                                        \
-  do {                                                                                       \
-    if (chunks > 0)                                                                          \
-      HF_LAUNCH("hf_vocab_embed_chunk",                                                      \
-                (vec ? hf_vocab_embed_chunk_##SUF##_v : hf_vocab_embed_chunk_##SUF), chunks, \
-                256, (const int*)s.key, (const int*)s.pos, V, D, strips, (const E*)dout, ldd, \
-                s.part);                                                                     \
-    HF_LAUNCH("hf_vocab_embed_grad",                                                         \
-              (vec ? hf_vocab_embed_grad_##SUF##_v : hf_vocab_embed_grad_##SUF), grid, 256,  \
-              (const int*)s.key, (const int*)s.pos, T, V, D, strips, scale, (const E*)dout,  \
-              ldd, (const float*)s.part, (E*)dE, lde, accumulate);                           \
+  const long long units = (long long)((T + RUN - 1) / RUN) * strips;
+  const int grid = (V + VROWS - 1) / VROWS;
+#define HF_EG(SUF, E)                                                                         \
+  do {                                                                                        \
+    if (T > 0)                                                                                \
+      HF_LAUNCH("hf_vocab_embed_runs",                                                        \
+                (vec ? hf_vocab_embed_runs_##SUF##_v : hf_vocab_embed_runs_##SUF),            \
+                (units + 3) / 4, 256, (const int*)s.key, (const int*)s.pos, T, V, D, strips,  \
+                scale, (const E*)dout, ldd, s.part, s.first, (E*)dE, lde, accumulate);        \
+    HF_LAUNCH("hf_vocab_embed_rows",                                                          \
+              (vec ? hf_vocab_embed_rows_##SUF##_v : hf_vocab_embed_rows_##SUF), grid, 256,   \
+              (const int*)s.key, T, V, D, strips, scale, (const float*)s.part,                \
+              (const int*)s.first, (E*)dE, lde, accumulate);                                  \
   } while (0)
   if (type == VT_F32) HF_EG(f32, float);
   else HF_EG(bf16, bf16_t);

@@ -37,10 +37,9 @@ namespace {
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
-typedef short s16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
-typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 __device__ __forceinline__ uint32_t f2bf(float f) {
   return __builtin_bit_cast(uint16_t, (__bf16)f);
@@ -111,34 +110,15 @@ struct Tile {
   }
 };
 
-__device__ __forceinline__ f32x16 mma1(bf16x8 a, bf16x8 b, f32x16 c) {
+// product j of a step: one with bf16, four with fp32 (all blocks take their
+// j-th one after the other, so that no MFMA waits for the one before it)
+__device__ __forceinline__ f32x16 mma1(bf16x8 a, bf16x8 b, f32x16 c, int) {
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
 }
-__device__ __forceinline__ f32x16 mma1(f32x4 a, f32x4 b, f32x16 c) {
-#pragma unroll
-  for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[j], b[j], c, 0, 0, 0);
-  return c;
+__device__ __forceinline__ f32x16 mma1(f32x4 a, f32x4 b, f32x16 c, int j) {
+  return __builtin_amdgcn_mfma_f32_32x32x2f32(a[j], b[j], c, 0, 0, 0);
 }
 
-// 4 consecutive values of one row of the type's output
-__device__ __forceinline__ void store4(float* p, const float (&v)[4], int n, int vec) {
-  if (vec && n >= 4) {
-    *(f32x4*)p = f32x4{v[0], v[1], v[2], v[3]};
-  } else {
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-      if (j < n) p[j] = v[j];
-  }
-}
-__device__ __forceinline__ void store4(bf16_t* p, const float (&v)[4], int n, int vec) {
-  if (vec && n >= 4) {
-    *(u32x2*)p = u32x2{f2bf(v[0]) | f2bf(v[1]) << 16, f2bf(v[2]) | f2bf(v[3]) << 16};
-  } else {
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-      if (j < n) p[j] = (bf16_t)f2bf(v[j]);
-  }
-}
 // exp, to the last bits where the type keeps them
 template <class E>
 __device__ __forceinline__ float exp_of(float x) {
@@ -146,6 +126,78 @@ __device__ __forceinline__ float exp_of(float x) {
 }
 __device__ __forceinline__ float load1(const float* p) { return *p; }
 __device__ __forceinline__ float load1(const bf16_t* p) { return bf2f(*p); }
+__device__ __forceinline__ void store1(float* p, float v) { *p = v; }
+__device__ __forceinline__ void store1(bf16_t* p, float v) { *p = (bf16_t)f2bf(v); }
+// whole 16-byte chunks
+__device__ __forceinline__ void add_chunk(const float* p, float (&v)[4]) {
+  const f32x4 o = *(const f32x4*)p;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) v[j] += o[j];
+}
+__device__ __forceinline__ void add_chunk(const bf16_t* p, float (&v)[8]) {
+  const u32x4 o = *(const u32x4*)p;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    v[2 * j] += bf2f(o[j] & 0xffffu);
+    v[2 * j + 1] += bf2f(o[j] >> 16);
+  }
+}
+__device__ __forceinline__ void store_chunk(float* p, const float (&v)[4]) {
+  *(f32x4*)p = f32x4{v[0], v[1], v[2], v[3]};
+}
+__device__ __forceinline__ void store_chunk(bf16_t* p, const float (&v)[8]) {
+  u32x4 w;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) w[j] = f2bf(v[2 * j]) | f2bf(v[2 * j + 1]) << 16;
+  *(u32x4*)p = w;
+}
+
+// One 32-row part (rows n0 .. n0 + 31) of a wave's tile to memory: RL columns
+// from m0, up to row Np and column Mp, from the wave's LDS region s, where
+// row r's 16-byte chunk c is at c ^ r % (RL / 4).  Through LDS, a store
+// instruction covers whole 256- or 512-byte runs of rows instead of 16-byte
+// pieces of 32 rows.
+// vec: rows take 16-byte accesses (Mp a whole chunk, or else the rest by
+// elements); add: += what is there.
+template <class O, int RL>
+__device__ __forceinline__ void store_part(const float* s, int lane, O* out, long long ldo,
+                                           int n0, int Np, int m0, int Mp, int vec, int add) {
+  constexpr int OPC = 16 / (int)sizeof(O), CPR = RL / OPC, Q = RL / 4;
+  if (vec) {
+#pragma unroll
+    for (int i = 0; i < 32 * CPR / 64; ++i) {
+      const int r = (lane + 64 * i) / CPR, c = (lane + 64 * i) % CPR;
+      const int n = n0 + r, m = m0 + OPC * c;
+      if (n >= Np || m >= Mp) continue;
+      float v[OPC];
+#pragma unroll
+      for (int k = 0; k < OPC / 4; ++k) {
+        const f32x4 w = *(const f32x4*)(s + r * RL + 4 * ((c * (OPC / 4) + k) ^ (r & (Q - 1))));
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[4 * k + j] = w[j];
+      }
+      O* p = out + (size_t)n * ldo + m;
+      if (m + OPC <= Mp) {
+        if (add) add_chunk(p, v);
+        store_chunk(p, v);
+      } else {
+#pragma unroll
+        for (int j = 0; j < OPC; ++j)
+          if (m + j < Mp) store1(p + j, add ? v[j] + load1(p + j) : v[j]);
+      }
+    }
+  } else {
+    for (int r = 0; r < 32; ++r) {
+      if (n0 + r >= Np) break;
+      O* p = out + (size_t)(n0 + r) * ldo + m0;
+      for (int c = lane; c < RL; c += 64) {
+        if (m0 + c >= Mp) break;
+        const float v = s[r * RL + 4 * ((c >> 2) ^ (r & (Q - 1))) + (c & 3)];
+        store1(p + c, add ? v + load1(p + c) : v);
+      }
+    }
+  }
+}
 
 // ----------------------------------------------------------------- epilogues
 enum { E_LOGITS, E_PROBS, E_PART, E_OUT };
@@ -272,9 +324,11 @@ __device__ __forceinline__ void vgemm_body(const VGemm& s, const VEpi& e) {
   };
   auto mma = [&](const Frags& f) {
 #pragma unroll
-    for (int a = 0; a < WM; ++a)
+    for (int j = 0; j < (int)sizeof(E) * (int)sizeof(E) / 4; ++j)
 #pragma unroll
-      for (int b = 0; b < WN; ++b) acc[a][b] = mma1(f.a[a], f.b[b], acc[a][b]);
+      for (int a = 0; a < WM; ++a)
+#pragma unroll
+        for (int b = 0; b < WN; ++b) acc[a][b] = mma1(f.a[a], f.b[b], acc[a][b], j);
   };
 
   constexpr int NQ = 4;      // steps per K block
@@ -316,14 +370,17 @@ __device__ __forceinline__ void vgemm_body(const VGemm& s, const VEpi& e) {
 
   // Lane (li, h), register r of block (a, b) holds n = 32 b + li and
   // m = 32 a + 8 (r / 4) + 4 h + r % 4 of the wave's part of the tile.
-  const int mw = m0 + wm * 32 * WM + 4 * h, nw = n0 + wn * 32 * WN + li;
+  const int mt = m0 + wm * 32 * WM, nt = n0 + wn * 32 * WN;
+  const int mw = mt + 4 * h;
+  constexpr int RL = 32 * WM;
+  static_assert(NW * 32 * RL * 4 <= S * STAGE * (int)sizeof(E), "staging exceeds the stages");
+  float* const mine = (float*)lds + wave * 32 * RL;
   if constexpr (EPI == E_LOGITS) {
     // row statistics of this tile: within the lane, the two halves of the
     // wave, then the GM waves that share the rows
     __shared__ float2 red[GM][RN];
 #pragma unroll
     for (int b = 0; b < WN; ++b) {
-      const int n = nw + 32 * b;
       float mx = -INFINITY;
 #pragma unroll
       for (int a = 0; a < WM; ++a)
@@ -346,19 +403,8 @@ __device__ __forceinline__ void vgemm_body(const VGemm& s, const VEpi& e) {
         }
       sum += __shfl_xor(sum, 32, 64);
       if (h == 0) red[wm][wn * 32 * WN + 32 * b + li] = float2{mx, sum};
-      if (e.z && n < N) {
-#pragma unroll
-        for (int a = 0; a < WM; ++a)
-#pragma unroll
-          for (int g = 0; g < 4; ++g) {
-            const int m = mw + 32 * a + 8 * g;
-            const float v[4] = {acc[a][b][4 * g], acc[a][b][4 * g + 1],
-                                acc[a][b][4 * g + 2], acc[a][b][4 * g + 3]};
-            if (m < s.M) store4(e.z + (size_t)n * e.ldz + m, v, s.M - m, 1);
-          }
-      }
     }
-    __syncthreads();
+    __syncthreads();     // also: every wave is done with the operand stages
     for (int c = tid; c < RN; c += 64 * NW) {
       if (n0 + c >= N) continue;
       float mx = red[0][c].x, sum = red[0][c].y;
@@ -371,53 +417,48 @@ __device__ __forceinline__ void vgemm_body(const VGemm& s, const VEpi& e) {
       }
       e.stat[(size_t)(n0 + c) * e.ldstat + e.tile0 + tm] = float2{mx, sum};
     }
+    if (!e.z) return;
   } else {
-    const float scale = EPI == E_OUT ? s.st->gscale : 1.0f;
-    // columns of delta are written up to whole K blocks of the next products
-    const int Mp = EPI == E_PROBS ? (s.M + VPAD - 1) & ~(VPAD - 1) : s.M;
-    // and its rows up to whole K blocks too (zeros: their lse is infinite)
-    const int Np = EPI == E_PROBS ? (N + VPAD - 1) & ~(VPAD - 1) : N;
+    __syncthreads();     // every wave is done with the operand stages
+  }
+  // columns and rows of p are written up to whole K blocks of the products
+  // that read them: zeros past the piece, and for rows whose lse is infinite
+  const int Mp = EPI == E_PROBS ? (s.M + VPAD - 1) & ~(VPAD - 1) : s.M;
+  const int Np = EPI == E_PROBS ? (N + VPAD - 1) & ~(VPAD - 1) : N;
+  const float scale = EPI == E_OUT ? s.st->gscale : 1.0f;
 #pragma unroll
-    for (int b = 0; b < WN; ++b) {
-      const int n = nw + 32 * b;
-      if (n < Np) {
-        const float lse = EPI == E_PROBS ? e.lse[n] : 0.0f;
+  for (int b = 0; b < WN; ++b) {
+    const int n = nt + 32 * b + li;
+    const float lse = EPI == E_PROBS && n < Np ? e.lse[n] : 0.0f;
 #pragma unroll
-        for (int a = 0; a < WM; ++a)
+    for (int a = 0; a < WM; ++a)
 #pragma unroll
-          for (int g = 0; g < 4; ++g) {
-            const int m = mw + 32 * a + 8 * g;
-            if (m >= Mp) continue;
-            float v[4];
+      for (int g = 0; g < 4; ++g) {
+        f32x4 v;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              const float c = acc[a][b][4 * g + j];
-              if (EPI == E_PROBS) v[j] = m + j < s.M ? exp_of<E>(c * e.zscale - lse) : 0.0f;
-              else v[j] = c * scale;
-            }
-            if constexpr (EPI == E_PROBS) {
-              store4((E*)e.d + (size_t)n * e.ldd + m, v, 4, 1);
-            } else if constexpr (EPI == E_PART) {
-              float* p = e.part + (size_t)tz * e.split_stride + (size_t)n * e.ldp + m;
-              if (e.add) {
-                const f32x4 o = *(const f32x4*)p;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) v[j] += o[j];
-              }
-              store4(p, v, 4, 1);
-            } else {
-              E* p = (E*)e.out + (size_t)n * e.ldo + m;
-              if (e.accumulate) {
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                  if (m + j < s.M) v[j] += load1(p + j);
-              }
-              store4(p, v, s.M - m, e.vec);
-            }
-          }
+        for (int j = 0; j < 4; ++j) {
+          const float c = acc[a][b][4 * g + j];
+          if (EPI == E_PROBS)
+            v[j] = mw + 32 * a + 8 * g + j < s.M ? exp_of<E>(c * e.zscale - lse) : 0.0f;
+          else v[j] = EPI == E_OUT ? c * scale : c;
+        }
+        *(f32x4*)(mine + li * RL + 4 * ((8 * a + 2 * g + h) ^ (li & (RL / 4 - 1)))) = v;
       }
-      __builtin_amdgcn_sched_barrier(0);
-    }
+    // the wave's own region, and its LDS operations stay in order
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    const int nb = nt + 32 * b;
+    if constexpr (EPI == E_LOGITS)
+      store_part<float, RL>(mine, lane, e.z, e.ldz, nb, Np, mt, Mp, 1, 0);
+    else if constexpr (EPI == E_PROBS)
+      store_part<E, RL>(mine, lane, (E*)e.d, e.ldd, nb, Np, mt, Mp, 1, 0);
+    else if constexpr (EPI == E_PART)
+      store_part<float, RL>(mine, lane, e.part + (size_t)tz * e.split_stride, e.ldp, nb, Np, mt,
+                            Mp, 1, e.add);
+    else
+      store_part<E, RL>(mine, lane, (E*)e.out, e.ldo, nb, Np, mt, Mp, e.vec, e.accumulate);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
   }
 }
 

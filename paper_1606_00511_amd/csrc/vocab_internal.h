@@ -57,7 +57,7 @@ struct VEpi {
   void* out;             // final output, scaled by st->gscale
   long long ldo;
   int accumulate;        // out += rather than =
-  int vec;               // out rows take 4-element vector stores
+  int vec;               // rows of out are 16-byte aligned
 };
 
 // logits of a vocabulary piece: A = W piece (akc), B = packed rows (akc);
@@ -134,7 +134,8 @@ struct VSort {
   int* tkey;                // T: scratch
   int* tpos;
   unsigned* hist;           // histograms of the radix passes
-  float* part;              // sums of whole chunks of one id
+  int* first;               // V: a token's first place in order, -1: none
+  float* part;              // sums of tokens that reach over a run's ends
 };
 // unsigned words of hist, and floats of part, for T rows
 size_t vocab_sort_hist(long long T, int V);

@@ -419,22 +419,39 @@ extern "C" __global__ __launch_bounds__(256) void hf_vocab_fix_bf16(VRows r, VTa
 }
 
 // ------------------------------------------------------------------ finish
-// 4 columns a thread; the splits are added in order, then the dup copy's.
+// 4 columns of a row per group of G threads, each of which adds every G-th
+// partial (the splits, then the dup copy's) in order; then the G sums in
+// order.  With one partial per thread in turn, 128 partials took 36 us of
+// latency; G = 8 takes 5.
 namespace {
-template <class E>
+template <class E, int G>
 __device__ __forceinline__ void finish_body(const VocabState* st, const float* part, int splits,
                                             long long ss, long long ldp, int dup, int rows,
                                             int dyn, int D, const int* idx, E* out,
                                             long long ldo, int accumulate) {
-  const int q = (D + 3) / 4;
-  const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
+  constexpr int QB = 256 / G;           // column groups per workgroup
+  __shared__ f32x4 sums[G > 1 ? 256 : 1];
+  const int q = (D + 3) / 4, grp = threadIdx.x / QB;
+  const long long i = (long long)blockIdx.x * QB + threadIdx.x % QB;
   const int j = (int)(i / q), c = 4 * (int)(i % q);
-  if (j >= (dyn ? min(st->n, rows) : rows)) return;
+  const bool in = j < (dyn ? min(st->n, rows) : rows);
+  const int parts = dup ? 2 * splits : splits;
   f32x4 s = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-  for (int z = 0; z < splits; ++z) s += *(const f32x4*)(part + z * ss + j * ldp + c);
-  if (dup)
-    for (int z = 0; z < splits; ++z)
-      s += *(const f32x4*)(part + z * ss + (size_t)(dup + j) * ldp + c);
+  if (in) {
+#pragma unroll 8
+    for (int z = grp; z < parts; z += G) {
+      const int zz = z < splits ? z : z - splits;
+      const size_t row = z < splits ? j : dup + j;
+      s += *(const f32x4*)(part + zz * ss + row * ldp + c);
+    }
+  }
+  if constexpr (G > 1) {
+    sums[threadIdx.x] = s;
+    __syncthreads();
+    if (grp) return;
+    for (int k = 1; k < G; ++k) s += sums[k * QB + threadIdx.x];
+  }
+  if (!in) return;
   const float g = st->gscale;
   E* o = out + (size_t)(idx ? idx[j] : j) * ldo + c;
 #pragma unroll
@@ -442,16 +459,18 @@ __device__ __forceinline__ void finish_body(const VocabState* st, const float* p
     if (c + e < D) put(o + e, s[e] * g + (accumulate ? to_f(o[e]) : 0.0f));
 }
 }  // namespace
-extern "C" __global__ __launch_bounds__(256) void hf_vocab_finish_f32(
-    const VocabState* st, const float* part, int splits, long long ss, long long ldp, int dup,
-    int rows, int dyn, int D, const int* idx, float* out, long long ldo, int accumulate) {
-  finish_body<float>(st, part, splits, ss, ldp, dup, rows, dyn, D, idx, out, ldo, accumulate);
-}
-extern "C" __global__ __launch_bounds__(256) void hf_vocab_finish_bf16(
-    const VocabState* st, const float* part, int splits, long long ss, long long ldp, int dup,
-    int rows, int dyn, int D, const int* idx, bf16_t* out, long long ldo, int accumulate) {
-  finish_body<bf16_t>(st, part, splits, ss, ldp, dup, rows, dyn, D, idx, out, ldo, accumulate);
-}
+#define HF_FINISH(SUF, E, G)                                                               \
+  extern "C" __global__ __launch_bounds__(256) void hf_vocab_finish_##SUF(                 \
+      const VocabState* st, const float* part, int splits, long long ss, long long ldp,    \
+      int dup, int rows, int dyn, int D, const int* idx, E* out, long long ldo,            \
+      int accumulate) {                                                                    \
+    finish_body<E, G>(st, part, splits, ss, ldp, dup, rows, dyn, D, idx, out, ldo,         \
+                      accumulate);                                                         \
+  }
+HF_FINISH(f32, float, 1)
+HF_FINISH(f32_g8, float, 8)
+HF_FINISH(bf16, bf16_t, 1)
+HF_FINISH(bf16_g8, bf16_t, 8)
 
 // ------------------------------------------------------------- launchers
 #define HF_LAUNCH(NAME, K, GRID, BLOCK, ...)                                       \
@@ -540,14 +559,16 @@ void vocab_fix(const Launch& L, int type, const VRows& r, const VTarget& t, int 
 void vocab_finish(const Launch& L, int type, const VocabState* st, const float* part, int splits,
                   long long ss, long long ldp, int dup, int rows, int dyn, int D, const int* idx,
                   void* out, long long ldo, int accumulate) {
-  const long long grid = ((long long)rows * ((D + 3) / 4) + 255) / 256;
+  const bool g8 = (dup ? 2 : 1) * splits >= 16;
+  const long long grid = ((long long)rows * ((D + 3) / 4) * (g8 ? 8 : 1) + 255) / 256;
   if (grid < 1) return;
   if (type == VT_F32)
-    HF_LAUNCH("hf_vocab_finish", hf_vocab_finish_f32, grid, 256, st, part, splits, ss, ldp, dup,
-              rows, dyn, D, idx, (float*)out, ldo, accumulate);
+    HF_LAUNCH("hf_vocab_finish", (g8 ? hf_vocab_finish_f32_g8 : hf_vocab_finish_f32), grid, 256,
+              st, part, splits, ss, ldp, dup, rows, dyn, D, idx, (float*)out, ldo, accumulate);
   else
-    HF_LAUNCH("hf_vocab_finish", hf_vocab_finish_bf16, grid, 256, st, part, splits, ss, ldp, dup,
-              rows, dyn, D, idx, (bf16_t*)out, ldo, accumulate);
+    HF_LAUNCH("hf_vocab_finish", (g8 ? hf_vocab_finish_bf16_g8 : hf_vocab_finish_bf16), grid,
+              256, st, part, splits, ss, ldp, dup, rows, dyn, D, idx, (bf16_t*)out, ldo,
+              accumulate);
 }
 
 }  // namespace hfk

@@ -29,8 +29,7 @@ constexpr size_t PIECE_BYTES = 512 * MiB;    // delta of a recomputed piece
 constexpr size_t WPACK_BYTES = 256 * MiB;    // packed rows of W
 constexpr int64_t MAX_LD = (int64_t)1 << 22; // in-tile offsets are 32 bits
 constexpr int TWO_TERM_ROWS = 128;
-constexpr int SPLIT_TILES = 512;             // partials: at most so many 128 x 128 tiles
-constexpr size_t SPLIT_FLOATS = (size_t)SPLIT_TILES * 128 * 128;
+constexpr size_t SPLIT_FLOATS = (size_t)32 << 20;   // partials of a split-K product
 
 inline int64_t up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
 
@@ -211,15 +210,38 @@ int end(hf_vocab* c, bool captured) {
   return HF_OK;
 }
 
-int splits_for(int M, int N, int K, int cap) {
-  const int64_t tiles = (int64_t)((M + 127) / 128) * ((N + 127) / 128);
-  int s = 1;
-  while (2 * s * tiles <= SPLIT_TILES && 2 * s <= cap && K / (2 * s) >= 256) s *= 2;
-  return s;
-}
-// 256 x 256 tiles once they give every compute unit a workgroup
-bool big_tiles(int64_t M, int64_t N) {
-  return ((M + 255) / 256) * ((N + 255) / 256) >= 224;
+// Tiles and split-K factor of a product by its estimated time, in us.  One 256
+// x 256 tile has a compute unit to itself, two of 128 x 128 share one; per
+// unit the former do 2.4e6 (bf16) or 0.27e6 (fp32) multiply-adds a us, the
+// latter 0.74 and 0.90 of that (8,192 x 32,768 x 4,096 in bf16: 1,680 and
+// 2,370 us; 16,384 x 2,048 x 2,048 in fp32: 975 and 1,090).  Filling the LDS
+// and storing the tile take about 6 and 4 us beside that, and partials are
+// written and read again at 4 bytes each, 4,700 bytes a ns on the whole card.
+struct Shape {
+  int big, splits;
+};
+Shape shape_for(int type, int64_t M, int64_t N, int64_t K, bool split) {
+  Shape best = {0, 1};
+  double least = 1e300;
+  for (int big = 0; big < 2; ++big) {
+    const int64_t R = big ? 256 : 128, tiles = ((M + R - 1) / R) * ((N + R - 1) / R);
+    const double rate = (type == VT_F32 ? 0.27e6 * (big ? 1.0 : 0.90)
+                                        : 2.4e6 * (big ? 1.0 : 0.74)) / (big ? 1.0 : 2.0);
+    for (int s = 1; s <= VMAX_SPLITS; ++s) {
+      if (s > 1 && (!split || K / s < 256 ||
+                    (size_t)s * up(N, 128) * up(M, VPAD) > SPLIT_FLOATS))
+        break;
+      const int64_t rounds = (tiles * s + (big ? 256 : 512) - 1) / (big ? 256 : 512);
+      const double t = rounds * ((double)R * R * (double)((K + s - 1) / s) / rate +
+                                 (big ? 6.0 : 4.0)) +
+                       (s > 1 ? 5.0 + 8.0 * s * (double)M * N / 4.7e6 : 0.0);
+      if (t < least) {
+        least = t;
+        best = {big, s};
+      }
+    }
+  }
+  return best;
 }
 
 struct Grad {
@@ -247,8 +269,14 @@ void head(hf_vocab* c, VRows r, const void* X, int64_t ldx, const void* W, int64
   float2* stat = c->at<float2>(l.stat);
   void* xp = c->at<void>(l.xp);
 
-  vocab_count(L, r);
-  vocab_pack_rows(L, type, r, X, ldx, xp, Dp, dup, g ? g->dX : nullptr, g ? g->lddx : 0);
+  // rows of X that the GEMMs can read in place are not packed if all of them
+  // count (which the device finds out)
+  const bool in_place = !dup && D % VPAD == 0 && ldx <= MAX_LD && (uintptr_t)X % 16 == 0 &&
+                        (ldx * es) % 16 == 0;
+  const void* xd = in_place ? X : nullptr;
+  const bool counted = vocab_count(L, r);
+  vocab_pack_rows(L, type, r, counted, X, ldx, in_place, xp, Dp, dup, g ? g->dX : nullptr,
+                  g ? g->lddx : 0);
 
   // W as it is where the GEMMs' 16-byte loads can read it, else packed, at
   // most pack_rows at a time
@@ -272,7 +300,7 @@ void head(hf_vocab* c, VRows r, const void* X, int64_t ldx, const void* W, int64
   // ---- statistics (and kept logits) of the whole vocabulary
   float* z = keep ? c->at<float>(l.z) : nullptr;
   const long long ldz = up(V, VTILE);
-  const bool big = big_tiles(V, T);
+  const int big = shape_for(type, wrows, T, Dp, false).big;
   const int stile = big ? 256 : 128;
   const int tiles = (V + stile - 1) / stile;
   VEpi e = {};
@@ -290,6 +318,9 @@ void head(hf_vocab* c, VRows r, const void* X, int64_t ldx, const void* W, int64
     q.K = Dp;
     q.alim = n;
     q.st = r.st;
+    q.X = xd;
+    q.ldx = ldx;
+    q.T = T;
     q.dyn = 1;
     q.splits = 1;
     q.big = big;
@@ -305,9 +336,9 @@ void head(hf_vocab* c, VRows r, const void* X, int64_t ldx, const void* W, int64
     tg.id = c->at<int>(l.tid);
     tg.dt = c->at<float>(l.tdt);
   }
-  if (!keep && T > 0) vocab_target_logits(L, type, r, xp, Dp, W, ldw, tg.zt);
+  if (!keep && T > 0) vocab_target_logits(L, type, r, xd, ldx, xp, Dp, W, ldw, tg.zt);
   vocab_row_loss(L, r, stat, tiles, tiles, z, ldz, tg, lse);
-  vocab_loss_sum(L, r, loss);
+  if (!keep || T < 1) vocab_loss_sum(L, r, loss);
   if (!g) return;
 
   // ---- gradients, piece by piece
@@ -321,7 +352,7 @@ void head(hf_vocab* c, VRows r, const void* X, int64_t ldx, const void* W, int64
     vc = V;
     const int rows = dup ? dup : (int)up(T, VPAD);
     if (T > 0)
-      vocab_delta(L, type, r, z, ldz, lse, tg, rows, d, ldd, (int)up(V, VPAD), dup);
+      vocab_delta(L, type, r, z, ldz, lse, tg, rows, d, ldd, (int)up(V, VPAD), dup, loss);
   } else {
     vc = piece_cols(c, T);
     ldd = up(vc, VTILE);
@@ -330,8 +361,9 @@ void head(hf_vocab* c, VRows r, const void* X, int64_t ldx, const void* W, int64
   // rows of dX's products: the counted ones, or both terms of few
   const int xrows = dup ? 2 * dup : T;
   float* partx = c->at<float>(l.partx);
-  int xsplits = 1, xbig = 0;
+  Shape xs = {0, 1};
   long long xstride = 0;
+  bool finish = true;
   for (int p0 = 0; p0 < V; p0 += vc) {
     const int pn = std::min(vc, V - p0);
     // a piece of delta covers several packed pieces of W where logits are kept
@@ -352,9 +384,12 @@ void head(hf_vocab* c, VRows r, const void* X, int64_t ldx, const void* W, int64
         q.K = Dp;
         q.alim = n;
         q.st = r.st;
+        q.X = xd;
+        q.ldx = ldx;
+        q.T = T;
         q.dyn = 1;
         q.splits = 1;
-        q.big = big_tiles(n, T);
+        q.big = shape_for(type, n, T, Dp, false).big;
         VEpi pe = {};
         pe.zscale = 1.0f / r.tau;
         pe.lse = lse;
@@ -376,17 +411,24 @@ void head(hf_vocab* c, VRows r, const void* X, int64_t ldx, const void* W, int64
       q.st = r.st;
       q.dyn = dup ? 0 : 1;
       if (v0 == 0) {
-        xbig = big_tiles(D, xrows);
-        xsplits = xbig ? 1 : splits_for(D, xrows, n, VMAX_SPLITS);
+        xs = shape_for(type, D, xrows, n, true);
         xstride = up(xrows, 128) * Dp;
+        // one piece and no splits: straight into dX
+        finish = n < V || xs.splits > 1 || dup;
       }
-      q.splits = xsplits;
-      q.big = xbig;
+      q.splits = xs.splits;
+      q.big = xs.big;
       VEpi pe = {};
       pe.part = partx;
       pe.ldp = Dp;
       pe.split_stride = xstride;
       pe.add = v0 > 0;
+      if (!finish) {
+        pe.out = g->dX;
+        pe.ldo = g->lddx;
+        pe.idx = r.idx;
+        pe.vec = (g->lddx * es) % 16 == 0 && (uintptr_t)g->dX % 16 == 0;
+      }
       vocab_dx(L, type, q, pe);
     }
     if (!g->dW) continue;
@@ -401,8 +443,12 @@ void head(hf_vocab* c, VRows r, const void* X, int64_t ldx, const void* W, int64
     q.alim = dup ? 2 * dup : Rp;
     q.st = r.st;
     q.dyn = dup ? 0 : 2;
-    q.big = big_tiles(D, pn);
-    q.splits = q.big ? 1 : splits_for(D, pn, q.K, VMAX_SPLITS);
+    q.X = xd;
+    q.ldx = ldx;
+    q.T = T;
+    const Shape ws = shape_for(type, D, pn, q.K, true);
+    q.big = ws.big;
+    q.splits = ws.splits;
     VEpi pe = {};
     char* out = (char*)g->dW + (size_t)p0 * g->lddw * es;
     pe.part = c->at<float>(l.partw);
@@ -417,8 +463,8 @@ void head(hf_vocab* c, VRows r, const void* X, int64_t ldx, const void* W, int64
       vocab_finish(L, type, r.st, pe.part, q.splits, pe.split_stride, Dp, 0, pn, 0, D, nullptr,
                    out, g->lddw, g->accumulate);
   }
-  if (g->dX && T > 0)
-    vocab_finish(L, type, r.st, partx, xsplits, xstride, Dp, dup, T, 1, D, r.idx, g->dX,
+  if (g->dX && T > 0 && finish)
+    vocab_finish(L, type, r.st, partx, xs.splits, xstride, Dp, dup, T, 1, D, r.idx, g->dX,
                  g->lddx, 0);
 }
 

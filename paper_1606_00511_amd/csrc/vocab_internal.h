@@ -35,6 +35,9 @@ struct VGemm {
   long long lda, ldb;
   int alim;        // rows of A that exist: m (akc), or k (not akc)
   const VocabState* st;
+  const void* X;   // the rows of X (what is packed), if they can be read in
+  long long ldx;   // place: used where all T of them count; else null
+  int T;
   int dyn;         // 1: N is st->n; 2: K is st->n rounded up to VPAD
   int splits;      // split-K factor (partials), grid z
   int big;         // 256 x 256 tiles rather than 128 x 128
@@ -57,6 +60,7 @@ struct VEpi {
   void* out;             // final output, scaled by st->gscale
   long long ldo;
   int accumulate;        // out += rather than =
+  const int* idx;        // dX: row of out for a packed row
   int vec;               // rows of out are 16-byte aligned
 };
 
@@ -65,7 +69,8 @@ struct VEpi {
 void vocab_logits(const Launch& L, int type, const VGemm& g, const VEpi& e);
 // p = exp(z - lse) of a vocabulary piece, rounded to the type, into d
 void vocab_probs(const Launch& L, int type, const VGemm& g, const VEpi& e);
-// row gradients: A = W piece (rows k), B = delta (k contiguous); into part
+// row gradients: A = W piece (rows k), B = delta (k contiguous); into part, or
+// straight into out
 void vocab_dx(const Launch& L, int type, const VGemm& g, const VEpi& e);
 // matrix gradient: A = packed rows (rows k), B = delta (rows k); into out, or
 // into part where g.splits > 1
@@ -86,13 +91,15 @@ struct VRows {
   int* idx;                 // the row of a packed row
   float* row_loss;          // T
 };
-// which rows count: pos, idx and the state; zero losses for those that do not
-void vocab_count(const Launch& L, const VRows& r);
+// which rows count: pos, idx and the state; zero losses for those that do not.
+// False: few enough that vocab_pack_rows does it instead.
+bool vocab_count(const Launch& L, const VRows& r);
 // counted rows of X packed to xp (zeros past the width, and past the last row
 // up to a whole tile; twice, dup rows apart, if dup > 0), rows of dX that do
 // not count set to zero
-void vocab_pack_rows(const Launch& L, int type, const VRows& r, const void* X,
-                     long long ldx, void* xp, int Dp, int dup, void* dX,
+// (in_place: not where all rows count; counted: by vocab_count)
+void vocab_pack_rows(const Launch& L, int type, const VRows& r, bool counted, const void* X,
+                     long long ldx, bool in_place, void* xp, int Dp, int dup, void* dX,
                      long long lddx);
 // rows [0, R) of W copied to wp (zeros past the width)
 void vocab_pack_matrix(const Launch& L, int type, const void* W, long long ldw,
@@ -103,8 +110,9 @@ struct VTarget {
   float* dt;                // packed row x K: delta at the target
 };
 // zt of the targets by their own products (logits not kept)
-void vocab_target_logits(const Launch& L, int type, const VRows& r, const void* xp,
-                         int Dp, const void* W, long long ldw, float* zt);
+void vocab_target_logits(const Launch& L, int type, const VRows& r, const void* X,
+                         long long ldx, const void* xp, int Dp, const void* W,
+                         long long ldw, float* zt);
 // log-sum-exp from the tiles' statistics, the rows' losses and the targets'
 // delta; z: kept logits or null (then t.zt holds the targets')
 void vocab_row_loss(const Launch& L, const VRows& r, const float2* stat, int ldstat,
@@ -112,11 +120,11 @@ void vocab_row_loss(const Launch& L, const VRows& r, const float2* stat, int lds
                     float* lse);
 // loss = sum of the counted rows' losses / denom
 void vocab_loss_sum(const Launch& L, const VRows& r, float* loss);
-// delta from kept logits, targets included; two: the rounding's rest too, dup
-// rows further down
+// delta from kept logits, targets included (dup: the rounding's rest too, dup
+// rows further down), and the loss
 void vocab_delta(const Launch& L, int type, const VRows& r, const float* z,
                  long long ldz, const float* lse, const VTarget& t, int rows,
-                 void* d, long long ldd, int Vp, int dup);
+                 void* d, long long ldd, int Vp, int dup, float* loss);
 // delta at the targets within the piece [v0, v0 + Vc)
 void vocab_fix(const Launch& L, int type, const VRows& r, const VTarget& t, int v0,
                int Vc, void* d, long long ldd);

@@ -79,16 +79,18 @@ extern "C" __global__ __launch_bounds__(256) void hf_vocab_have(VRows r) {
   if (lane == 0) r.pos[t] = any;
 }
 
-// One workgroup: each thread counts a run of rows, a scan over the threads
-// places them.  pos holds hf_vocab_have's answer for lists.
-extern "C" __global__ __launch_bounds__(1024) void hf_vocab_count(VRows r) {
-  __shared__ int sums[16];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int per = (r.T + 1023) / 1024;
-  const int t0 = min(tid * per, r.T), t1 = min(t0 + per, r.T);
-  float v;
-  int c = 0;
-  for (int t = t0; t < t1; ++t) c += r.t ? r.pos[t] : target(r, t, 0, &v) >= 0;
+namespace {
+__device__ __forceinline__ void set_state(const VRows& r, int n) {
+  const double denom = r.denom > 0.0f ? (double)r.denom : (double)n;
+  r.st->n = n;
+  r.st->inv = denom > 0.0 ? 1.0 / denom : 0.0;
+  r.st->gscale = denom > 0.0 ? (float)((double)r.tau / denom) : 0.0f;
+}
+// Sum over the threads before this one, and over all, of a workgroup of NW
+// waves; sums: NW words of LDS.
+template <int NW>
+__device__ __forceinline__ int scan_threads(int c, int* sums, int& all) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   int s = c;
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
@@ -97,25 +99,65 @@ extern "C" __global__ __launch_bounds__(1024) void hf_vocab_count(VRows r) {
   }
   if (lane == 63) sums[wave] = s;
   __syncthreads();
-  int base = 0, n = 0;
+  int base = 0;
+  all = 0;
 #pragma unroll
-  for (int w = 0; w < 16; ++w) {
+  for (int w = 0; w < NW; ++w) {
     if (w < wave) base += sums[w];
+    all += sums[w];
+  }
+  return base + s - c;
+}
+}  // namespace
+
+// One workgroup of 16 waves: each wave counts a run of rows, 64 at a time, a
+// scan over the waves places them.  pos holds hf_vocab_have's answer for
+// lists.  (16,384 rows: 7 us; a run of rows per thread, with its scattered
+// stores, took 33.)
+extern "C" __global__ __launch_bounds__(1024) void hf_vocab_count(VRows r) {
+  __shared__ int sums[16];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int per = ((r.T + 15) / 16 + 63) & ~63;
+  const int t0 = min(wave * per, r.T), t1 = min(t0 + per, r.T);
+  constexpr int U = 4;
+  // f(row, whether it counts) for the rows of the wave, U x 64 in flight
+  auto each = [&](auto f) {
+    for (int t = t0; t < t1; t += 64 * U) {
+      int v[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int i = t + 64 * u + lane;
+        v[u] = i < t1 ? (r.t ? r.pos[i] : r.ids[(size_t)i * r.ldi]) : 0;
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int i = t + 64 * u + lane;
+        bool have = v[u] != 0;
+        if (!r.t) {
+          have = v[u] >= 0 && v[u] < r.V;
+          if (i < t1 && !have && v[u] != IGNORE) r.st->err = 1;
+        }
+        f(i, i < t1, i < t1 && have);
+      }
+    }
+  };
+  int c = 0, at = 0, n = 0;
+  each([&](int, bool, bool have) { c += __popcll(__ballot(have)); });
+  if (lane == 0) sums[wave] = c;
+  __syncthreads();
+  for (int w = 0; w < 16; ++w) {
+    if (w < wave) at += sums[w];
     n += sums[w];
   }
-  int at = base + s - c;
-  for (int t = t0; t < t1; ++t) {
-    const bool have = r.t ? r.pos[t] != 0 : target(r, t, 0, &v) >= 0;
-    r.pos[t] = have ? at : -1;
-    if (have) r.idx[at++] = t;
-    else r.row_loss[t] = 0.0f;
-  }
-  if (tid == 0) {
-    const double denom = r.denom > 0.0f ? (double)r.denom : (double)n;
-    r.st->n = n;
-    r.st->inv = denom > 0.0 ? 1.0 / denom : 0.0;
-    r.st->gscale = denom > 0.0 ? (float)((double)r.tau / denom) : 0.0f;
-  }
+  each([&](int i, bool in, bool have) {
+    const unsigned long long m = __ballot(have);
+    const int p = at + __popcll(m & ((1ull << lane) - 1));
+    at += __popcll(m);
+    if (in) r.pos[i] = have ? p : -1;
+    if (have) r.idx[p] = i;
+    else if (in) r.row_loss[i] = 0.0f;
+  });
+  if (threadIdx.x == 0) set_state(r, n);
 }
 
 // ----------------------------------------------------------------- packing
@@ -141,38 +183,68 @@ __device__ __forceinline__ void copy_row(const E* src, int n, int vec, E* dst, i
   }
 }
 
-template <class E>
+// SELF: up to 256 rows with few targets; every workgroup counts them by
+// itself (a launch less), and the first one writes down what later kernels
+// need.
+constexpr int SELF_ROWS = 256, SELF_TOP = 32;
+template <class E, bool SELF>
 __device__ __forceinline__ void pack_body(const VRows& r, const E* X, long long ldx, int vecx,
-                                          E* xp, int Dp, int dup, E* dX, long long lddx) {
-  int b = blockIdx.x;
+                                          int in_place, E* xp, int Dp, int dup, E* dX,
+                                          long long lddx) {
+  const int b = blockIdx.x;
+  int n, pos = -1;
+  if constexpr (SELF) {
+    __shared__ int sums[4], place[SELF_ROWS];
+    const int t = threadIdx.x;
+    bool have = false;
+    float v;
+    if (t < r.T)
+      for (int k = 0; k < r.K; ++k) have |= target(r, t, k, &v) >= 0;
+    const int at = scan_threads<4>(have, sums, n);
+    place[t] = have ? at : -1;
+    __syncthreads();
+    if (b < r.T) pos = place[b];
+    if (b == 0) {
+      if (t < r.T) {
+        if (have) r.idx[at] = t;
+        else r.row_loss[t] = 0.0f;
+      }
+      if (t == 0) set_state(r, n);
+    }
+  } else {
+    n = r.st->n;
+    if (in_place && n == r.T) return;
+    if (b < r.T) pos = r.pos[b];
+  }
+  if (in_place && n == r.T) return;
   if (b < r.T) {
-    const int j = r.pos[b];
-    if (j >= 0) {
-      copy_row(X + (size_t)b * ldx, r.D, vecx, xp + (size_t)j * Dp, Dp,
-               dup ? xp + (size_t)(dup + j) * Dp : (E*)nullptr);
+    if (pos >= 0) {
+      copy_row(X + (size_t)b * ldx, r.D, vecx, xp + (size_t)pos * Dp, Dp,
+               dup ? xp + (size_t)(dup + pos) * Dp : (E*)nullptr);
     } else if (dX) {
       for (int c = threadIdx.x; c < r.D; c += 256) dX[(size_t)b * lddx + c] = (E)0;
     }
     return;
   }
-  const int j = r.st->n + b - r.T;
-  const int end = dup ? dup : (r.st->n + VTILE - 1) / VTILE * VTILE;
+  const int j = n + b - r.T;
+  const int end = dup ? dup : (n + VTILE - 1) / VTILE * VTILE;
   if (j < end)
     copy_row((const E*)nullptr, 0, 0, xp + (size_t)j * Dp, Dp,
              dup ? xp + (size_t)(dup + j) * Dp : (E*)nullptr);
 }
 }  // namespace
 
-extern "C" __global__ __launch_bounds__(256) void hf_vocab_pack_f32(
-    VRows r, const float* X, long long ldx, int vecx, float* xp, int Dp, int dup, float* dX,
-    long long lddx) {
-  pack_body<float>(r, X, ldx, vecx, xp, Dp, dup, dX, lddx);
-}
-extern "C" __global__ __launch_bounds__(256) void hf_vocab_pack_bf16(
-    VRows r, const bf16_t* X, long long ldx, int vecx, bf16_t* xp, int Dp, int dup, bf16_t* dX,
-    long long lddx) {
-  pack_body<bf16_t>(r, X, ldx, vecx, xp, Dp, dup, dX, lddx);
-}
+#define HF_PACK(SUF, E, SELF)                                                             \
+  extern "C" __global__ __launch_bounds__(256) void hf_vocab_pack_##SUF(                  \
+      VRows r, const E* X, long long ldx, int vecx, int in_place, E* xp, int Dp, int dup, \
+      E* dX, long long lddx) {                                                            \
+    pack_body<E, SELF>(r, X, ldx, vecx, in_place, xp, Dp, dup, dX, lddx);                 \
+  }
+HF_PACK(f32, float, false)
+HF_PACK(f32_self, float, true)
+HF_PACK(bf16, bf16_t, false)
+HF_PACK(bf16_self, bf16_t, true)
+
 extern "C" __global__ __launch_bounds__(256) void hf_vocab_copy_f32(
     const float* W, long long ldw, int vec, int D, float* wp, int Dp) {
   const size_t b = blockIdx.x;
@@ -189,13 +261,14 @@ extern "C" __global__ __launch_bounds__(256) void hf_vocab_copy_bf16(
 // one wave each.
 namespace {
 template <class E>
-__device__ __forceinline__ void tlogit_body(const VRows& r, const E* xp, int Dp, const E* W,
-                                            long long ldw, int vec, float* zt) {
+__device__ __forceinline__ void tlogit_body(const VRows& r, const E* X, long long ldx,
+                                            const E* xp, int Dp, const E* W, long long ldw,
+                                            int vec, float* zt) {
   constexpr int EPC = 16 / sizeof(E);
   const int j = blockIdx.x;
   if (j >= r.st->n) return;
   const int t = r.idx[j], wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const E* x = xp + (size_t)j * Dp;
+  const E* x = X && r.st->n == r.T ? X + (size_t)j * ldx : xp + (size_t)j * Dp;
   float v;
   for (int k = wave; k < r.K; k += 4) {
     const int id = target(r, t, k, &v);
@@ -220,12 +293,14 @@ __device__ __forceinline__ void tlogit_body(const VRows& r, const E* xp, int Dp,
 }
 }  // namespace
 extern "C" __global__ __launch_bounds__(256) void hf_vocab_tlogit_f32(
-    VRows r, const float* xp, int Dp, const float* W, long long ldw, int vec, float* zt) {
-  tlogit_body<float>(r, xp, Dp, W, ldw, vec, zt);
+    VRows r, const float* X, long long ldx, const float* xp, int Dp, const float* W, long long ldw,
+    int vec, float* zt) {
+  tlogit_body<float>(r, X, ldx, xp, Dp, W, ldw, vec, zt);
 }
 extern "C" __global__ __launch_bounds__(256) void hf_vocab_tlogit_bf16(
-    VRows r, const bf16_t* xp, int Dp, const bf16_t* W, long long ldw, int vec, float* zt) {
-  tlogit_body<bf16_t>(r, xp, Dp, W, ldw, vec, zt);
+    VRows r, const bf16_t* X, long long ldx, const bf16_t* xp, int Dp, const bf16_t* W, long long ldw,
+    int vec, float* zt) {
+  tlogit_body<bf16_t>(r, X, ldx, xp, Dp, W, ldw, vec, zt);
 }
 
 // ------------------------------------------------------------- rows' losses
@@ -319,29 +394,42 @@ extern "C" __global__ __launch_bounds__(256) void hf_vocab_row_loss(
     }
 }
 
-extern "C" __global__ __launch_bounds__(1024) void hf_vocab_loss_sum(
-    const float* __restrict__ row_loss, int T, const VocabState* st, float* loss) {
-  __shared__ double ws[16];
+// The loss from the rows' losses, by one workgroup of 256 threads.
+namespace {
+__device__ __forceinline__ void loss_sum(const float* row_loss, int T, const VocabState* st,
+                                         float* loss) {
+  __shared__ double ws[4];
   double s = 0.0;
-  for (int i = threadIdx.x; i < T; i += 1024) s += (double)row_loss[i];
+  for (int t = threadIdx.x; t < T; t += 8 * 256) {
+    float v[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) v[u] = t + 256 * u < T ? row_loss[t + 256 * u] : 0.0f;
+#pragma unroll
+    for (int u = 0; u < 8; ++u) s += (double)v[u];
+  }
   s = wave_sum_d(s);
   if ((threadIdx.x & 63) == 0) ws[threadIdx.x >> 6] = s;
   __syncthreads();
-  if (threadIdx.x == 0) {
-    double f = 0.0;
-    for (int w = 0; w < 16; ++w) f += ws[w];
-    *loss = (float)(f * st->inv);
-  }
+  if (threadIdx.x == 0) *loss = (float)(((ws[0] + ws[1]) + (ws[2] + ws[3])) * st->inv);
+}
+}  // namespace
+extern "C" __global__ __launch_bounds__(256) void hf_vocab_loss_sum(
+    const float* __restrict__ row_loss, int T, const VocabState* st, float* loss) {
+  loss_sum(row_loss, T, st, loss);
 }
 
 // ------------------------------------------------------------------- delta
-// A workgroup has 2,048 columns of one packed row.
+// A workgroup has 2,048 columns of one packed row; the last one sums the loss.
 namespace {
 constexpr int DCOLS = 2048;
 template <class E>
 __device__ __forceinline__ void delta_body(const VRows& r, const float* z, long long ldz,
                                            const float* lse, const VTarget& tg, int chunks,
-                                           E* d, long long ldd, int Vp, int dup) {
+                                           E* d, long long ldd, int Vp, int dup, float* loss) {
+  if (blockIdx.x == gridDim.x - 1) {
+    loss_sum(r.row_loss, r.T, r.st, loss);
+    return;
+  }
   const int j = blockIdx.x / chunks, c0 = (blockIdx.x % chunks) * DCOLS;
   const int n = r.st->n;
   if (j >= n && j >= (dup ? dup : (n + VPAD - 1) / VPAD * VPAD)) return;
@@ -388,13 +476,13 @@ __device__ __forceinline__ void delta_body(const VRows& r, const float* z, long 
 }  // namespace
 extern "C" __global__ __launch_bounds__(256) void hf_vocab_delta_f32(
     VRows r, const float* z, long long ldz, const float* lse, VTarget tg, int chunks, float* d,
-    long long ldd, int Vp, int dup) {
-  delta_body<float>(r, z, ldz, lse, tg, chunks, d, ldd, Vp, dup);
+    long long ldd, int Vp, int dup, float* loss) {
+  delta_body<float>(r, z, ldz, lse, tg, chunks, d, ldd, Vp, dup, loss);
 }
 extern "C" __global__ __launch_bounds__(256) void hf_vocab_delta_bf16(
     VRows r, const float* z, long long ldz, const float* lse, VTarget tg, int chunks, bf16_t* d,
-    long long ldd, int Vp, int dup) {
-  delta_body<bf16_t>(r, z, ldz, lse, tg, chunks, d, ldd, Vp, dup);
+    long long ldd, int Vp, int dup, float* loss) {
+  delta_body<bf16_t>(r, z, ldz, lse, tg, chunks, d, ldd, Vp, dup, loss);
 }
 
 namespace {
@@ -487,21 +575,26 @@ inline int vec16(const void* p, long long ld, int es) {
 }
 }  // namespace
 
-void vocab_count(const Launch& L, const VRows& r) {
+bool vocab_count(const Launch& L, const VRows& r) {
+  if (r.T > 0 && r.T <= SELF_ROWS && r.K <= SELF_TOP) return false;
   if (r.t && r.T > 0)
     HF_LAUNCH("hf_vocab_have", hf_vocab_have, (r.T + 3) / 4, 256, r);
   HF_LAUNCH("hf_vocab_count", hf_vocab_count, 1, 1024, r);
+  return true;
 }
 
-void vocab_pack_rows(const Launch& L, int type, const VRows& r, const void* X, long long ldx,
-                     void* xp, int Dp, int dup, void* dX, long long lddx) {
-  const int grid = r.T + VTILE;
+void vocab_pack_rows(const Launch& L, int type, const VRows& r, bool counted, const void* X,
+                     long long ldx, bool in_place, void* xp, int Dp, int dup, void* dX,
+                     long long lddx) {
+  const int grid = r.T + (dup ? dup : VTILE), place = in_place;
   if (type == VT_F32)
-    HF_LAUNCH("hf_vocab_pack", hf_vocab_pack_f32, grid, 256, r, (const float*)X, ldx,
-              vec16(X, ldx, 4), (float*)xp, Dp, dup, (float*)dX, lddx);
+    HF_LAUNCH("hf_vocab_pack", (counted ? hf_vocab_pack_f32 : hf_vocab_pack_f32_self), grid,
+              256, r, (const float*)X, ldx, vec16(X, ldx, 4), place, (float*)xp, Dp, dup,
+              (float*)dX, lddx);
   else
-    HF_LAUNCH("hf_vocab_pack", hf_vocab_pack_bf16, grid, 256, r, (const bf16_t*)X, ldx,
-              vec16(X, ldx, 2), (bf16_t*)xp, Dp, dup, (bf16_t*)dX, lddx);
+    HF_LAUNCH("hf_vocab_pack", (counted ? hf_vocab_pack_bf16 : hf_vocab_pack_bf16_self), grid,
+              256, r, (const bf16_t*)X, ldx, vec16(X, ldx, 2), place, (bf16_t*)xp, Dp, dup,
+              (bf16_t*)dX, lddx);
 }
 
 void vocab_pack_matrix(const Launch& L, int type, const void* W, long long ldw, int R, int D,
@@ -514,14 +607,14 @@ void vocab_pack_matrix(const Launch& L, int type, const void* W, long long ldw, 
               vec16(W, ldw, 2), D, (bf16_t*)wp, Dp);
 }
 
-void vocab_target_logits(const Launch& L, int type, const VRows& r, const void* xp, int Dp,
-                         const void* W, long long ldw, float* zt) {
+void vocab_target_logits(const Launch& L, int type, const VRows& r, const void* X, long long ldx,
+                         const void* xp, int Dp, const void* W, long long ldw, float* zt) {
   if (type == VT_F32)
-    HF_LAUNCH("hf_vocab_tlogit", hf_vocab_tlogit_f32, r.T, 256, r, (const float*)xp, Dp,
-              (const float*)W, ldw, vec16(W, ldw, 4), zt);
+    HF_LAUNCH("hf_vocab_tlogit", hf_vocab_tlogit_f32, r.T, 256, r, (const float*)X, ldx,
+              (const float*)xp, Dp, (const float*)W, ldw, vec16(W, ldw, 4), zt);
   else
-    HF_LAUNCH("hf_vocab_tlogit", hf_vocab_tlogit_bf16, r.T, 256, r, (const bf16_t*)xp, Dp,
-              (const bf16_t*)W, ldw, vec16(W, ldw, 2), zt);
+    HF_LAUNCH("hf_vocab_tlogit", hf_vocab_tlogit_bf16, r.T, 256, r, (const bf16_t*)X, ldx,
+              (const bf16_t*)xp, Dp, (const bf16_t*)W, ldw, vec16(W, ldw, 2), zt);
 }
 
 void vocab_row_loss(const Launch& L, const VRows& r, const float2* stat, int ldstat, int tiles,
@@ -531,20 +624,20 @@ void vocab_row_loss(const Launch& L, const VRows& r, const float2* stat, int lds
 }
 
 void vocab_loss_sum(const Launch& L, const VRows& r, float* loss) {
-  HF_LAUNCH("hf_vocab_loss_sum", hf_vocab_loss_sum, 1, 1024, r.row_loss, r.T, r.st, loss);
+  HF_LAUNCH("hf_vocab_loss_sum", hf_vocab_loss_sum, 1, 256, r.row_loss, r.T, r.st, loss);
 }
 
 void vocab_delta(const Launch& L, int type, const VRows& r, const float* z, long long ldz,
                  const float* lse, const VTarget& t, int rows, void* d, long long ldd, int Vp,
-                 int dup) {
+                 int dup, float* loss) {
   const int chunks = (Vp + DCOLS - 1) / DCOLS;
-  const long long grid = (long long)rows * chunks;
+  const long long grid = (long long)rows * chunks + 1;
   if (type == VT_F32)
     HF_LAUNCH("hf_vocab_delta", hf_vocab_delta_f32, grid, 256, r, z, ldz, lse, t, chunks,
-              (float*)d, ldd, Vp, dup);
+              (float*)d, ldd, Vp, dup, loss);
   else
     HF_LAUNCH("hf_vocab_delta", hf_vocab_delta_bf16, grid, 256, r, z, ldz, lse, t, chunks,
-              (bf16_t*)d, ldd, Vp, dup);
+              (bf16_t*)d, ldd, Vp, dup, loss);
 }
 
 void vocab_fix(const Launch& L, int type, const VRows& r, const VTarget& t, int v0, int Vc,

@@ -3,11 +3,13 @@
 //
 // The head works on packed rows (the N that count, N known to the device
 // only) in one of two ways, chosen by the call's sizes:
-//   kept        the logits of the call fit KEEP_BYTES: computed once, kept in
-//               fp32, turned into delta
+//   kept        the logits of the call fit KEEP_BYTES, in fp32 or (bf16) as
+//               exponentials in fp16: computed once, turned into delta
 //   recomputed  one pass over the whole vocabulary for the statistics, then
 //               piece by piece the logits again, straight into delta, and the
-//               piece's share of dX and rows of dW
+//               piece's share of dX and rows of dW.  The first piece is the
+//               pass's last, and its logits are kept: they need no second
+//               computation
 // A loss without its gradient never keeps a logit.
 #include "hf.h"
 #include "vocab_internal.h"
@@ -24,8 +26,7 @@ using namespace hfk;
 namespace {
 
 constexpr size_t MiB = (size_t)1 << 20;
-constexpr size_t KEEP_BYTES = 1536 * MiB;    // logits (and bf16 delta) kept
-constexpr size_t PIECE_BYTES = 512 * MiB;    // delta of a recomputed piece
+constexpr size_t KEEP_BYTES = 1536 * MiB;    // kept logits
 constexpr size_t WPACK_BYTES = 256 * MiB;    // packed rows of W
 constexpr int64_t MAX_LD = (int64_t)1 << 22; // in-tile offsets are 32 bits
 constexpr int TWO_TERM_ROWS = 128;
@@ -35,7 +36,7 @@ inline int64_t up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
 
 struct Layout {
   size_t state, pos, idx, rloss, lse, zt, tid, tdt, stat, xp, wp, z, partx, partw;
-  size_t key, spos, tkey, tpos, hist, first, epart, need;
+  size_t key, spos, tkey, tpos, hist, epart, need;
 };
 
 }  // namespace
@@ -46,9 +47,8 @@ struct hf_vocab {
   hipStream_t stream = nullptr;
   char* ws = nullptr;
   Layout lay = {};
-  hipEvent_t last = nullptr;       // the last call's work
-  hipStream_t last_stream = nullptr;
-  bool pending = false;
+  hipEvent_t last = nullptr;       // the work on the stream before this one
+  bool pending = false;            // calls have been made on this stream
   std::string err;
 
   template <class T>
@@ -86,21 +86,19 @@ inline int64_t tile_rows(int64_t T) { return std::max<int64_t>(up(T, VTILE), VTI
 // few rows nothing averages the rounding of the label's entry, and the matrix
 // cores wait for W anyway.
 inline int two_term(const hf_vocab* c, int64_t T) {
-  return c->type == VT_BF16 && T > 0 && T <= TWO_TERM_ROWS ? (int)up(T, VPAD) : 0;
+  return c->type == VT_BF16 && T > 0 && T <= TWO_TERM_ROWS ? (int)up(T, VPAD / 2) : 0;
 }
-inline size_t keep_bytes(const hf_vocab* c, int64_t T) {
-  const size_t Vp = (size_t)up(c->V, VTILE), R = (size_t)tile_rows(T);
-  return R * Vp * 4 + (c->type == VT_BF16 ? R * Vp * 2 : 0);
+// Bytes of a column of what is kept and of delta, which takes its place; few
+// bf16 rows keep fp32 logits beside delta.
+inline size_t col_bytes(const hf_vocab* c, int64_t T) {
+  return (size_t)tile_rows(T) * (two_term(c, T) ? 6 : c->es);
 }
 inline bool keeps(const hf_vocab* c, int64_t T) {
-  return T <= TWO_TERM_ROWS || keep_bytes(c, T) <= KEEP_BYTES;
+  return T <= TWO_TERM_ROWS || col_bytes(c, T) * up(c->V, VTILE) <= KEEP_BYTES;
 }
-// columns of a recomputed piece
+// columns of a piece: as many as are kept
 inline int piece_cols(const hf_vocab* c, int64_t T) {
-  int64_t n = (int64_t)(PIECE_BYTES / ((size_t)tile_rows(T) * c->es)) / 1024 * 1024;
-  n = std::max<int64_t>(n, 1024);
-  const int64_t pieces = (c->V + n - 1) / n;      // of even sizes
-  return (int)std::min<int64_t>(up(c->V, VTILE), up((c->V + pieces - 1) / pieces, 1024));
+  return (int)std::max<int64_t>((int64_t)(KEEP_BYTES / col_bytes(c, T)) / 1024 * 1024, 1024);
 }
 // rows of W packed at a time
 inline int pack_rows(const hf_vocab* c) {
@@ -108,8 +106,7 @@ inline int pack_rows(const hf_vocab* c) {
   return (int)std::min<int64_t>(c->V, std::max<int64_t>(n, 1024));
 }
 inline size_t z_bytes(const hf_vocab* c, int64_t T) {
-  if (keeps(c, T)) return keep_bytes(c, T);
-  return (size_t)tile_rows(T) * up(piece_cols(c, T), VTILE) * c->es;
+  return col_bytes(c, T) * (keeps(c, T) ? up(c->V, VTILE) : piece_cols(c, T));
 }
 
 void plan(const hf_vocab* c, int64_t R, Layout* l) {
@@ -131,19 +128,10 @@ void plan(const hf_vocab* c, int64_t R, Layout* l) {
   l->stat = take(r * (size_t)((c->V + VSTAT - 1) / VSTAT + 8) * sizeof(float2));
   l->xp = take(Rp * c->Dp * c->es);
   l->wp = take((size_t)pack_rows(c) * c->Dp * c->es);
-  // what the largest of up to R rows needs: kept logits up to the last row
-  // count that keeps them, or pieces
-  size_t zb = z_bytes(c, R);
-  if (!keeps(c, R)) {
-    int64_t lo = 1, hi = R;             // keeps(lo), not keeps(hi)
-    while (hi - lo > 1) {
-      const int64_t mid = lo + (hi - lo) / 2;
-      if (keeps(c, mid)) lo = mid;
-      else hi = mid;
-    }
-    zb = std::max(keep_bytes(c, lo), (size_t)PIECE_BYTES);
-    zb = std::max(zb, z_bytes(c, R));
-  }
+  // what the largest of up to R rows needs: few rows, kept logits, pieces
+  size_t zb = z_bytes(c, std::min<int64_t>(R, TWO_TERM_ROWS));
+  if (R > TWO_TERM_ROWS)
+    zb = std::max(zb, keeps(c, R) ? z_bytes(c, R) : KEEP_BYTES);
   l->z = take(zb);
   l->partx = take(std::max(Rp * (size_t)c->Dp, SPLIT_FLOATS) * 4);
   l->partw = take(SPLIT_FLOATS * 4);
@@ -152,7 +140,6 @@ void plan(const hf_vocab* c, int64_t R, Layout* l) {
   l->tkey = take(r * 4);
   l->tpos = take(r * 4);
   l->hist = take(vocab_sort_hist(R, c->V) * 4);
-  l->first = take((size_t)c->V * 4);
   l->epart = take(vocab_sort_part(R, c->D, c->type) * 4);
   l->need = off;
 }
@@ -189,23 +176,8 @@ int check_mat(hf_vocab* c, const void* p, int64_t ld, int64_t cols, int es, int6
 }
 
 // -------------------------------------------------------------- the passes
-// Work of a call on this stream follows that of the context's last call on
-// another: they share the workspace.  (Calls that are being captured are the
-// caller's to order.)
-int begin(hf_vocab* c, bool* captured) {
-  hipStreamCaptureStatus cs = hipStreamCaptureStatusNone;
-  HIP_TRY(c, hipStreamIsCapturing(c->stream, &cs));
-  *captured = cs != hipStreamCaptureStatusNone;
-  if (!*captured && c->pending && c->last_stream != c->stream)
-    HIP_TRY(c, hipStreamWaitEvent(c->stream, c->last, 0));
-  return HF_OK;
-}
-int end(hf_vocab* c, bool captured) {
+int end(hf_vocab* c) {
   HIP_TRY(c, hipGetLastError());
-  if (captured) return HF_OK;
-  if (!c->last) HIP_TRY(c, hipEventCreateWithFlags(&c->last, hipEventDisableTiming));
-  HIP_TRY(c, hipEventRecord(c->last, c->stream));
-  c->last_stream = c->stream;
   c->pending = true;
   return HF_OK;
 }
@@ -297,18 +269,25 @@ void head(hf_vocab* c, VRows r, const void* X, int64_t ldx, const void* W, int64
     return wp;
   };
 
-  // ---- statistics (and kept logits) of the whole vocabulary
-  float* z = keep ? c->at<float>(l.z) : nullptr;
-  const long long ldz = up(V, VTILE);
-  const int big = shape_for(type, wrows, T, Dp, false).big;
-  const int stile = big ? 256 : 128;
-  const int tiles = (V + stile - 1) / stile;
+  // ---- statistics of the whole vocabulary, and the logits of the first piece
+  // (with `keep`, all of them)
+  const int Rp = (int)tile_rows(T);
+  const int vc = !g ? V : keep ? V : piece_cols(c, T);
+  const long long ldd = up(vc, VTILE);
+  // fp32: logits, then delta in their place; bf16: exponentials, then delta;
+  // few bf16 rows: fp32 logits, and delta behind them
+  const bool f16 = type == VT_BF16 && !dup;
+  float* z = g && !f16 ? c->at<float>(l.z) : nullptr;
+  void* d = !g ? nullptr : dup ? (void*)(z + (size_t)Rp * ldd) : c->at<void>(l.z);
+  const int sstep = std::min(wrows, vc);
+  const int big = shape_for(type, g ? sstep : wrows, T, Dp, false).big;
+  const int sg = big ? VSTAT_BIG : VSTAT;
+  const int tiles = (V + sg - 1) / sg;
   VEpi e = {};
   e.zscale = 1.0f / r.tau;
   e.stat = stat;
   e.ldstat = tiles;
-  for (int v0 = 0; v0 < V; v0 += wrows) {
-    const int n = std::min(wrows, V - v0);
+  auto logits = [&](int v0, int n, bool kept) {
     VGemm q = {};
     q.A = matrix(v0, n, &q.lda);
     q.B = xp;
@@ -324,11 +303,14 @@ void head(hf_vocab* c, VRows r, const void* X, int64_t ldx, const void* W, int64
     q.dyn = 1;
     q.splits = 1;
     q.big = big;
-    e.tile0 = v0 / stile;
-    e.z = z ? z + v0 : nullptr;
-    e.ldz = ldz;
+    e.tile0 = v0 / sg;
+    e.z = kept && z ? z + v0 : nullptr;
+    e.pt = kept && f16 ? (char*)d + (size_t)v0 * 2 : nullptr;
+    e.ldz = ldd;
     vocab_logits(L, type, q, e);
-  }
+  };
+  for (int v0 = g ? vc : 0; v0 < V; v0 += wrows) logits(v0, std::min(wrows, V - v0), false);
+  for (int v0 = 0; g && v0 < vc; v0 += wrows) logits(v0, std::min(wrows, std::min(vc, V) - v0), true);
 
   // ---- losses
   VTarget tg = {c->at<float>(l.zt), nullptr, nullptr};
@@ -336,28 +318,17 @@ void head(hf_vocab* c, VRows r, const void* X, int64_t ldx, const void* W, int64
     tg.id = c->at<int>(l.tid);
     tg.dt = c->at<float>(l.tdt);
   }
-  if (!keep && T > 0) vocab_target_logits(L, type, r, xd, ldx, xp, Dp, W, ldw, tg.zt);
-  vocab_row_loss(L, r, stat, tiles, tiles, z, ldz, tg, lse);
-  if (!keep || T < 1) vocab_loss_sum(L, r, loss);
+  const bool self = dup > 0;             // few rows: with delta
+  const bool dots = !keep || f16;
+  if (dots && T > 0) vocab_target_logits(L, type, r, xd, ldx, xp, Dp, W, ldw, tg.zt);
+  if (!self) vocab_row_loss(L, r, stat, tiles, tiles, dots ? nullptr : z, ldd, tg, lse);
+  if (g && T > 0)
+    vocab_delta(L, type, r, z, ldd, stat, tiles, sg, lse, tg, 0, std::min(vc, V),
+                dup ? dup : (int)up(T, VPAD), self, d, ldd, dup, self ? nullptr : loss);
+  if (!g || T < 1 || (self && !g->dX)) vocab_loss_sum(L, r, loss);
   if (!g) return;
 
   // ---- gradients, piece by piece
-  const int Rp = (int)tile_rows(T);
-  void* d;
-  long long ldd;
-  int vc;
-  if (keep) {
-    ldd = ldz;
-    d = type == VT_F32 ? (void*)z : (void*)(z + (size_t)Rp * ldz);
-    vc = V;
-    const int rows = dup ? dup : (int)up(T, VPAD);
-    if (T > 0)
-      vocab_delta(L, type, r, z, ldz, lse, tg, rows, d, ldd, (int)up(V, VPAD), dup, loss);
-  } else {
-    vc = piece_cols(c, T);
-    ldd = up(vc, VTILE);
-    d = c->at<void>(l.z);
-  }
   // rows of dX's products: the counted ones, or both terms of few
   const int xrows = dup ? 2 * dup : T;
   float* partx = c->at<float>(l.partx);
@@ -371,9 +342,9 @@ void head(hf_vocab* c, VRows r, const void* X, int64_t ldx, const void* W, int64
       const int n = std::min(wrows, p0 + pn - v0);
       long long lda = 0;
       const void* A = nullptr;
-      if (!keep || g->dX) A = matrix(v0, n, &lda);
+      if (p0 > 0 || g->dX) A = matrix(v0, n, &lda);
       char* dv = (char*)d + (size_t)(v0 - p0) * es;
-      if (!keep) {
+      if (p0 > 0) {
         VGemm q = {};
         q.A = A;
         q.lda = lda;
@@ -446,7 +417,9 @@ void head(hf_vocab* c, VRows r, const void* X, int64_t ldx, const void* W, int64
     q.X = xd;
     q.ldx = ldx;
     q.T = T;
-    const Shape ws = shape_for(type, D, pn, q.K, true);
+    // few bf16 rows: tiles of 128 (hf_vocab_dw_bf16_thin)
+    const Shape ws = type == VT_BF16 && q.K <= 256 ? Shape{0, 1}
+                                                   : shape_for(type, D, pn, q.K, true);
     q.big = ws.big;
     q.splits = ws.splits;
     VEpi pe = {};
@@ -461,11 +434,11 @@ void head(hf_vocab* c, VRows r, const void* X, int64_t ldx, const void* W, int64
     vocab_dw(L, type, q, pe);
     if (q.splits > 1)
       vocab_finish(L, type, r.st, pe.part, q.splits, pe.split_stride, Dp, 0, pn, 0, D, nullptr,
-                   out, g->lddw, g->accumulate);
+                   out, g->lddw, g->accumulate, nullptr, nullptr);
   }
   if (g->dX && T > 0 && finish)
     vocab_finish(L, type, r.st, partx, xs.splits, xstride, Dp, dup, T, 1, D, r.idx, g->dX,
-                 g->lddx, 0);
+                 g->lddx, 0, &r, self ? loss : nullptr);
 }
 
 // arguments of a head call, then its work
@@ -504,10 +477,8 @@ int head_call(hf_vocab* c, const void* X, int64_t ldx, const void* W, int64_t ld
   r.tau = tau;
   r.denom = denom;
   r.row_loss = row_loss;
-  bool captured;
-  if ((rc = begin(c, &captured))) return rc;
   head(c, r, X, ldx, W, ldw, loss, g);
-  return end(c, captured);
+  return end(c);
 }
 
 int check_list(hf_vocab* c, const float* t, int64_t T, int32_t K, float tau) {
@@ -556,7 +527,20 @@ int hf_vocab_destroy(hf_vocab* c) {
 
 int hf_vocab_set_stream(hf_vocab* c, void* s) {
   if (!c) return HF_EINVAL;
-  c->stream = reinterpret_cast<hipStream_t>(s);
+  const hipStream_t from = c->stream, to = reinterpret_cast<hipStream_t>(s);
+  if (from == to) return HF_OK;
+  c->stream = to;
+  if (!c->pending) return HF_OK;
+  // later work shares the workspace with what the old stream still does;
+  // the caller orders calls that are captured
+  hipStreamCaptureStatus a = hipStreamCaptureStatusNone, b = hipStreamCaptureStatusNone;
+  HIP_TRY(c, hipStreamIsCapturing(from, &a));
+  HIP_TRY(c, hipStreamIsCapturing(to, &b));
+  if (a != hipStreamCaptureStatusNone || b != hipStreamCaptureStatusNone) return HF_OK;
+  if (!c->last) HIP_TRY(c, hipEventCreateWithFlags(&c->last, hipEventDisableTiming));
+  HIP_TRY(c, hipEventRecord(c->last, from));
+  HIP_TRY(c, hipStreamWaitEvent(to, c->last, 0));
+  c->pending = false;
   return HF_OK;
 }
 
@@ -637,11 +621,10 @@ int hf_vocab_embed(hf_vocab* c, const void* E, int64_t lde, const int32_t* tok, 
       (rc = check_mat(c, out, ldo, c->D, c->es, rows, "out")))
     return rc;
   if (!std::isfinite(scale)) return fail(c, HF_EINVAL, "scale is not finite");
-  bool captured;
-  if ((rc = check_ready(c, rows)) || (rc = begin(c, &captured))) return rc;
+  if ((rc = check_ready(c, rows))) return rc;
   const Launch L{c->stream, nullptr};
   vocab_embed(L, c->type, E, lde, c->V, c->D, tok, (int)rows, scale, out, ldo, c->st());
-  return end(c, captured);
+  return end(c);
 }
 
 int hf_vocab_embed_grad(hf_vocab* c, const int32_t* tok, int64_t rows, float scale,
@@ -657,15 +640,14 @@ int hf_vocab_embed_grad(hf_vocab* c, const int32_t* tok, int64_t rows, float sca
   if (!std::isfinite(scale)) return fail(c, HF_EINVAL, "scale is not finite");
   if (accumulate != 0 && accumulate != 1)
     return fail(c, HF_EINVAL, "accumulate %d is neither 0 nor 1", accumulate);
-  bool captured;
-  if ((rc = check_ready(c, rows)) || (rc = begin(c, &captured))) return rc;
+  if ((rc = check_ready(c, rows))) return rc;
   const Launch L{c->stream, nullptr};
   const Layout& l = c->lay;
   const VSort s = {c->at<int>(l.key), c->at<int>(l.spos), c->at<int>(l.tkey), c->at<int>(l.tpos),
-                   c->at<unsigned>(l.hist), c->at<int>(l.first), c->at<float>(l.epart)};
+                   c->at<unsigned>(l.hist), c->at<float>(l.epart)};
   vocab_embed_grad(L, c->type, tok, (int)rows, c->V, c->D, scale, dout, ldd, dE, lde, accumulate,
                    s, c->st());
-  return end(c, captured);
+  return end(c);
 }
 
 int hf_vocab_check(hf_vocab* c) {

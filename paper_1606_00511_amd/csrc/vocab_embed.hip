@@ -6,11 +6,12 @@
 // The gradient sorts the rows by token (stable, two radix passes), so that the
 // rows of one token are consecutive, and cuts the sorted places into runs of
 // RUN.  A wave sums a run, strip of columns by strip, and writes the tokens
-// that lie within it; what reaches over a run's ends goes to partial sums.
-// The last kernel has the rows of dE: it joins the partial sums of tokens that
-// span runs, in order, and writes the zeros.  So the work per wave does not
-// depend on how often a token comes, no sum uses atomics, and every row of dE
-// is written once, with the same bits every time.
+// that lie within it; what reaches over a run's ends goes to partial sums,
+// which a last kernel joins in order.  So the work per wave does not depend on
+// how often a token comes, and no sum uses atomics: the same bits every time.
+// The sort occupies few compute units and waits for memory most of the time:
+// the other workgroups of its launches fill dE with zeros meanwhile (rows of
+// tokens that do come are written again: fewer than there are rows of dout).
 #include <algorithm>
 
 #include "vocab_internal.h"
@@ -19,6 +20,7 @@ namespace hfk {
 namespace {
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 __device__ __forceinline__ uint32_t f2bf(float f) {
   return __builtin_bit_cast(uint16_t, (__bf16)f);
@@ -123,6 +125,29 @@ __device__ __forceinline__ int key_of(const int32_t* tok, int t, int V, VocabSta
   return V;
 }
 
+// A share of the rows of dE set to zero by the workgroups past the sort's.
+struct Fill {
+  char* p;             // null: nothing to fill
+  long long ld;        // bytes between rows
+  int bytes;           // of a row
+  int unit;            // bytes of a store: 16, 4 or 2
+  int v0, v1;          // rows
+};
+__device__ __forceinline__ void fill_rows(const Fill& f, int block, int blocks) {
+  const int lane = threadIdx.x & 63;
+  for (int v = f.v0 + block * (CHUNK / 64) + (threadIdx.x >> 6); v < f.v1;
+       v += blocks * (CHUNK / 64)) {
+    char* row = f.p + (size_t)v * f.ld;
+    if (f.unit == 16) {
+      for (int i = 16 * lane; i < f.bytes; i += 1024) *(u32x4*)(row + i) = u32x4{0u, 0u, 0u, 0u};
+    } else if (f.unit == 4) {
+      for (int i = 4 * lane; i < f.bytes; i += 256) *(uint32_t*)(row + i) = 0u;
+    } else {
+      for (int i = 2 * lane; i < f.bytes; i += 128) *(uint16_t*)(row + i) = 0;
+    }
+  }
+}
+
 // Exclusive scan of a[0 .. n), n <= MAXDIG, by 1,024 threads.
 __device__ __forceinline__ void scan_digits(unsigned* a, int n, unsigned* tmp) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -181,11 +206,14 @@ __device__ __forceinline__ unsigned place(unsigned* base, int d, bool valid, int
 }
 }  // namespace
 
-// histogram of the low digit; zeros in the high digit's; no place of any token
+// histogram of the low digit; zeros in the high digit's
 extern "C" __global__ __launch_bounds__(CHUNK) void hf_vocab_sort_hist(
-    const int32_t* tok, int T, int V, int bits, unsigned* hist, unsigned* hist2, int* first,
-    VocabState* st) {
-  for (int v = blockIdx.x * CHUNK + threadIdx.x; v < V; v += gridDim.x * CHUNK) first[v] = -1;
+    const int32_t* tok, int T, int V, int bits, unsigned* hist, unsigned* hist2, int blocks,
+    Fill fill, VocabState* st) {
+  if ((int)blockIdx.x >= blocks) {
+    fill_rows(fill, blockIdx.x - blocks, gridDim.x - blocks);
+    return;
+  }
   __shared__ unsigned h[MAXDIG];
   const int digs = 1 << bits, t = blockIdx.x * CHUNK + threadIdx.x;
   for (int d = threadIdx.x; d < digs; d += CHUNK) h[d] = 0;
@@ -204,9 +232,14 @@ extern "C" __global__ __launch_bounds__(CHUNK) void hf_vocab_sort_hist(
 // smaller digits, then this digit in earlier workgroups.
 extern "C" __global__ __launch_bounds__(CHUNK) void hf_vocab_sort_pass(
     const int32_t* tok, const int* key, const int* pos, int T, int V, int bits,
-    const unsigned* hist, unsigned* hist2, int* okey, int* opos, VocabState* st) {
+    const unsigned* hist, unsigned* hist2, int* okey, int* opos, int blocks, Fill fill,
+    VocabState* st) {
+  if ((int)blockIdx.x >= blocks) {
+    fill_rows(fill, blockIdx.x - blocks, gridDim.x - blocks);
+    return;
+  }
   __shared__ unsigned base[MAXDIG], mine[MAXDIG], tmp[16];
-  const int digs = 1 << bits, blocks = gridDim.x, t = blockIdx.x * CHUNK + threadIdx.x;
+  const int digs = 1 << bits, t = blockIdx.x * CHUNK + threadIdx.x;
   for (int d = threadIdx.x; d < digs; d += CHUNK) base[d] = mine[d] = 0;
   __syncthreads();
   // every thread sums a digit over a share of the workgroups
@@ -214,6 +247,7 @@ extern "C" __global__ __launch_bounds__(CHUNK) void hf_vocab_sort_pass(
   for (int i = threadIdx.x; i < digs * groups; i += CHUNK) {
     const int d = i & (digs - 1);
     unsigned all = 0, before = 0;
+#pragma unroll 8
     for (int b = i >> bits; b < blocks; b += groups) {
       const unsigned x = hist[(size_t)b * digs + d];
       before += b < (int)blockIdx.x ? x : 0u;
@@ -249,14 +283,12 @@ extern "C" __global__ __launch_bounds__(CHUNK) void hf_vocab_sort_pass(
   }
 }
 
-// Both passes of up to 1,024 rows in the first workgroup; the others clear the
-// places of the tokens.
+// Both passes of up to 1,024 rows in the first workgroup.
 extern "C" __global__ __launch_bounds__(CHUNK) void hf_vocab_sort_one(
-    const int32_t* tok, int T, int V, int bits, int* okey, int* opos, int* first,
+    const int32_t* tok, int T, int V, int bits, int* okey, int* opos, Fill fill,
     VocabState* st) {
   if (blockIdx.x > 0) {
-    for (int v = (blockIdx.x - 1) * CHUNK + threadIdx.x; v < V; v += (gridDim.x - 1) * CHUNK)
-      first[v] = -1;
+    fill_rows(fill, blockIdx.x - 1, gridDim.x - 1);
     return;
   }
   __shared__ unsigned base[MAXDIG], tmp[16];
@@ -292,7 +324,6 @@ extern "C" __global__ __launch_bounds__(CHUNK) void hf_vocab_sort_one(
 // --------------------------------------------------------------- gradient
 namespace {
 constexpr int RUN = 32;      // sorted places per wave
-constexpr int VROWS = 8;     // rows of dE per workgroup
 
 template <class E, bool VEC>
 __device__ __forceinline__ void emit(E* row, int strip, int lane, int D, float scale,
@@ -311,12 +342,12 @@ __device__ __forceinline__ void emit(E* row, int strip, int lane, int D, float s
 
 // One run and strip.  part[2 run]: the sum of the token that began before the
 // run (or fills it from its start and goes on); part[2 run + 1]: of the one
-// that begins within it and goes on.  first[token]: its first sorted place.
+// that begins within it and goes on.
 template <class E, bool VEC>
 __device__ __forceinline__ void runs_body(const int* key, const int* pos, int T, int V, int D,
                                           int strips, float scale, const E* dout,
-                                          long long ldd, float* part, int* first, E* dE,
-                                          long long lde, int accumulate) {
+                                          long long ldd, float* part, E* dE, long long lde,
+                                          int accumulate) {
   using S = Strip<E, VEC>;
   const int lane = threadIdx.x & 63;
   const long long unit = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
@@ -327,8 +358,6 @@ __device__ __forceinline__ void runs_body(const int* key, const int* pos, int T,
   const int at = a - 1 + lane;
   const int k = at >= 0 && at < T && lane < RUN + 2 ? key[at] : -1;
   const int p = at >= 0 && at < T && lane < RUN + 1 ? pos[at] : 0;
-  const int before = __shfl_up(k, 1, 64);
-  if (strip == 0 && lane >= 1 && lane <= RUN && k >= 0 && k < V && k != before) first[k] = at;
   // places of tokens in the run (masked ones come last)
   const int n = __popcll(__ballot(lane >= 1 && lane <= RUN && k >= 0 && k < V));
   float acc[S::EPC] = {};
@@ -352,9 +381,11 @@ __device__ __forceinline__ void runs_body(const int* key, const int* pos, int T,
       if (cur == nxt && !last) continue;
       // the token's places in this run end here
       if (head || cur == nxt) {
-        float* o = part + (((size_t)2 * run + !head) * strips + strip) * S::COLS;
+        float* o = part + (((size_t)2 * run + !head) * strips + strip) * S::COLS +
+                   lane * S::EPC;
 #pragma unroll
-        for (int e = 0; e < S::EPC; ++e) o[e * 64 + lane] = acc[e];
+        for (int q = 0; q < S::EPC / 4; ++q)
+          *(f32x4*)(o + 4 * q) = f32x4{acc[4 * q], acc[4 * q + 1], acc[4 * q + 2], acc[4 * q + 3]};
       } else {
         emit<E, VEC>(dE + (size_t)cur * lde, strip, lane, D, scale, accumulate, acc);
       }
@@ -365,74 +396,99 @@ __device__ __forceinline__ void runs_body(const int* key, const int* pos, int T,
   }
 }
 
-// Rows of dE: zeros where there is no token, joined sums where a token spans
-// runs.  A workgroup's rows lie far apart, so that the frequent tokens (low
-// numbers, as vocabularies are ordered) do not share one.
+// Tokens that span runs, a strip of columns: each wave looks at one boundary
+// between runs.  Where a token has its first one, the wave joins it if it spans
+// few runs; tokens that span many are summed by the 4 waves together, a quarter
+// of the runs each, the quarters in order.
 template <class E, bool VEC>
-__device__ __forceinline__ void rows_body(const int* key, int T, int V, int D, int strips,
-                                          float scale, const float* part, const int* first,
-                                          E* dE, long long lde, int accumulate) {
+__device__ __forceinline__ void join_body(const int* key, int T, int V, int D, int strips,
+                                          float scale, const float* part, E* dE, long long lde,
+                                          int accumulate) {
   using S = Strip<E, VEC>;
-  const int lane = threadIdx.x & 63;
-  const int mine = blockIdx.x + lane * gridDim.x;
-  const int f = lane < VROWS && mine < V && T > 0 ? first[mine] : -1;
-  for (int u = threadIdx.x >> 6; u < VROWS * strips; u += 4) {
-    const int i = u / strips, strip = u % strips;
-    const int v = blockIdx.x + i * gridDim.x;
-    if (v >= V) return;
-    const int a = __builtin_amdgcn_readlane(f, i);
-    float acc[S::EPC] = {};
-    if (a < 0) {
-      if (!accumulate) S::store(dE + (size_t)v * lde, strip, lane, D, acc);
-      continue;
-    }
-    const int run = a / RUN, end = (run + 1) * RUN;
-    if (end >= T || key[end] != v) continue;     // within its run: written
-    const size_t slot = 2 * (size_t)run + 1;
-    int lo = run + 1, hi = (T + RUN - 1) / RUN;  // runs past lo that start with v
-    while (lo < hi) {
-      const int mid = (lo + hi) >> 1;
-      if (key[mid * RUN] == v) lo = mid + 1;
-      else hi = mid;
-    }
-    auto at = [&](size_t sl, int e) {
-      return part[(sl * strips + strip) * S::COLS + e * 64 + lane];
+  constexpr int LONG = 16;
+  __shared__ float quarter[4][S::COLS];
+  __shared__ int ends[4];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, strip = blockIdx.y;
+  const int runs = (T + RUN - 1) / RUN;
+  // acc += the token's partial sums of the runs x0 .. x1; it begins in `run`,
+  // whose second partial sum is its
+  auto sum = [&](int run, int x0, int x1, float (&acc)[S::EPC]) {
+    auto at = [&](int x) {
+      const size_t slot = 2 * (size_t)x + (x == run);
+      return part + (slot * strips + strip) * S::COLS + lane * S::EPC;
     };
+    constexpr int U = 16, Q = S::EPC / 4;
+    for (int x = x0; x < x1; x += U) {
+      f32x4 w[U][Q];
 #pragma unroll
-    for (int e = 0; e < S::EPC; ++e) acc[e] = at(slot, e);
-    int r = run + 1;
-    constexpr int U = 8;
-    for (; r + U <= lo; r += U) {
-      float w[U][S::EPC];
+      for (int u = 0; u < U; ++u)
 #pragma unroll
-      for (int x = 0; x < U; ++x)
+        for (int q = 0; q < Q; ++q) w[u][q] = *(const f32x4*)(at(min(x + u, x1 - 1)) + 4 * q);
 #pragma unroll
-        for (int e = 0; e < S::EPC; ++e) w[x][e] = at(2 * (size_t)(r + x), e);
+      for (int u = 0; u < U; ++u)
+        if (x + u < x1)
 #pragma unroll
-      for (int x = 0; x < U; ++x)
-#pragma unroll
-        for (int e = 0; e < S::EPC; ++e) acc[e] += w[x][e];
+          for (int e = 0; e < S::EPC; ++e) acc[e] += w[u][e / 4][e % 4];
     }
-    for (; r < lo; ++r)
+  };
+  int last = 0;              // past the last run that starts with the token
+  {
+    const int run = blockIdx.x * 4 + wave, end = (run + 1) * RUN;
+    if (end < T) {
+      const int k = key[end], k1 = key[end - 1], k0 = run > 0 ? key[end - 1 - RUN] : -1;
+      if (k < V && k1 == k && k0 != k) {
+        // 64 probes at a time (one after the other, a search among 4,096 runs
+        // took longer than the sums)
+        int lo = run + 2, hi = runs;
+        while (lo < hi) {
+          const int stride = (hi - lo + 63) / 64, i = lo + lane * stride;
+          const int n = __popcll(__ballot(i < hi && key[min(i, runs - 1) * RUN] == k));
+          hi = min(hi, lo + n * stride);
+          lo = n ? lo + (n - 1) * stride + 1 : lo;
+        }
+        last = lo;
+        if (last - run <= LONG) {
+          float acc[S::EPC] = {};
+          sum(run, run, last, acc);
+          emit<E, VEC>(dE + (size_t)k * lde, strip, lane, D, scale, accumulate, acc);
+          last = 0;
+        }
+      }
+    }
+  }
+  if (lane == 0) ends[wave] = last;
+  __syncthreads();
+  for (int w = 0; w < 4; ++w) {
+    const int run = blockIdx.x * 4 + w, lo = ends[w];
+    if (!lo) continue;
+    const int per = (lo - run + 3) / 4;
+    float acc[S::EPC] = {};
+    sum(run, min(run + wave * per, lo), min(run + (wave + 1) * per, lo), acc);
+    __syncthreads();
 #pragma unroll
-      for (int e = 0; e < S::EPC; ++e) acc[e] += at(2 * (size_t)r, e);
-    emit<E, VEC>(dE + (size_t)v * lde, strip, lane, D, scale, accumulate, acc);
+    for (int e = 0; e < S::EPC; ++e) quarter[wave][e * 64 + lane] = acc[e];
+    __syncthreads();
+    if (wave) continue;
+#pragma unroll
+    for (int e = 0; e < S::EPC; ++e)
+      acc[e] = ((quarter[0][e * 64 + lane] + quarter[1][e * 64 + lane]) +
+                quarter[2][e * 64 + lane]) + quarter[3][e * 64 + lane];
+    emit<E, VEC>(dE + (size_t)key[(run + 1) * RUN] * lde, strip, lane, D, scale, accumulate, acc);
   }
 }
 }  // namespace
 
-#define HF_EMBED_GRAD(SUF, E, VEC)                                                          \
-  extern "C" __global__ __launch_bounds__(256) void hf_vocab_embed_runs_##SUF(              \
-      const int* key, const int* pos, int T, int V, int D, int strips, float scale,         \
-      const E* dout, long long ldd, float* part, int* first, E* dE, long long lde,          \
-      int accumulate) {                                                                     \
-    runs_body<E, VEC>(key, pos, T, V, D, strips, scale, dout, ldd, part, first, dE, lde,    \
-                      accumulate);                                                          \
-  }                                                                                         \
-  extern "C" __global__ __launch_bounds__(256) void hf_vocab_embed_rows_##SUF(              \
-      const int* key, int T, int V, int D, int strips, float scale, const float* part,      \
-      const int* first, E* dE, long long lde, int accumulate) {                             \
-    rows_body<E, VEC>(key, T, V, D, strips, scale, part, first, dE, lde, accumulate);       \
+#define HF_EMBED_GRAD(SUF, E, VEC)                                                       \
+  extern "C" __global__ __launch_bounds__(256) void hf_vocab_embed_runs_##SUF(           \
+      const int* key, const int* pos, int T, int V, int D, int strips, float scale,      \
+      const E* dout, long long ldd, float* part, E* dE, long long lde, int accumulate) { \
+    runs_body<E, VEC>(key, pos, T, V, D, strips, scale, dout, ldd, part, dE, lde,        \
+                      accumulate);                                                       \
+  }                                                                                      \
+  extern "C" __global__ __launch_bounds__(256) void hf_vocab_embed_join_##SUF(           \
+      const int* key, int T, int V, int D, int strips, float scale, const float* part,   \
+      E* dE, long long lde, int accumulate) {                                            \
+    join_body<E, VEC>(key, T, V, D, strips, scale, part, dE, lde, accumulate);           \
   }
 HF_EMBED_GRAD(f32, float, false)
 HF_EMBED_GRAD(f32_v, float, true)
@@ -440,10 +496,14 @@ HF_EMBED_GRAD(bf16, bf16_t, false)
 HF_EMBED_GRAD(bf16_v, bf16_t, true)
 
 // ------------------------------------------------------------- launchers
+namespace {
+inline dim3 grid_of(dim3 g) { return g; }
+inline dim3 grid_of(long long g) { return dim3((unsigned)g); }
+}  // namespace
 #define HF_LAUNCH(NAME, K, GRID, BLOCK, ...)                                       \
   do {                                                                             \
     prof_begin(L, NAME);                                                           \
-    hipExtLaunchKernelGGL(K, dim3((unsigned)(GRID)), dim3(BLOCK), 0, L.stream,     \
+    hipExtLaunchKernelGGL(K, grid_of(GRID), dim3(BLOCK), 0, L.stream,     \
                           prof_a(L), prof_b(L), 0, __VA_ARGS__);                   \
     prof_end(L, NAME, 0.0, 0.0);                                                   \
   } while (0)
@@ -489,35 +549,49 @@ void vocab_embed_grad(const Launch& L, int type, const int32_t* tok, int T, int 
                       int accumulate, const VSort& s, VocabState* st) {
   const int es = type == VT_F32 ? 4 : 2, strips = strips_of(D, es), bits = digit_bits(V);
   const bool vec = vec16(dout, ldd, D, es) && vec16(dE, lde, D, es);
-  if (T > 0 && T <= CHUNK) {
-    // enough workgroups to clear a large vocabulary's places beside the sort
-    const int grid = 1 + std::min(64, (V + CHUNK - 1) / CHUNK);
-    HF_LAUNCH("hf_vocab_sort", hf_vocab_sort_one, grid, CHUNK, tok, T, V, bits, s.key, s.pos,
-              s.first, st);
-  } else if (T > 0) {
+  // the rows to fill, in shares like the durations of the sort's launches
+  const size_t row = (size_t)lde * es;
+  Fill all = {accumulate ? nullptr : (char*)dE, (long long)row, D * es, 0, 0, 0};
+  all.unit = ((uintptr_t)dE | row | (size_t)all.bytes) % 16 == 0 ? 16 : es;
+  auto share = [&](double a, double b) {
+    Fill f = all;
+    f.v0 = (int)(a * V);
+    f.v1 = b < 1.0 ? (int)(b * V) : V;
+    return f;
+  };
+  // workgroups that fill: two per compute unit, or fewer for little
+  const int fills = accumulate ? 0 : (int)std::min<long long>(512, ((long long)V * all.bytes >> 16) + 1);
+  if (T <= CHUNK) {
+    if (T > 0 || fills)
+      HF_LAUNCH("hf_vocab_sort", hf_vocab_sort_one, 1 + fills, CHUNK, tok, T, V, bits, s.key,
+                s.pos, share(0.0, 1.0), st);
+  } else {
     const int blocks = (T + CHUNK - 1) / CHUNK;
     unsigned* h2 = s.hist + ((size_t)1 << bits) * blocks;
-    HF_LAUNCH("hf_vocab_sort", hf_vocab_sort_hist, blocks, CHUNK, tok, T, V, bits, s.hist, h2,
-              s.first, st);
-    HF_LAUNCH("hf_vocab_sort", hf_vocab_sort_pass, blocks, CHUNK, tok, (const int*)nullptr,
-              (const int*)nullptr, T, V, bits, (const unsigned*)s.hist, h2, s.tkey, s.tpos, st);
-    HF_LAUNCH("hf_vocab_sort", hf_vocab_sort_pass, blocks, CHUNK, (const int32_t*)nullptr,
-              (const int*)s.tkey, (const int*)s.tpos, T, V, bits, (const unsigned*)h2,
-              (unsigned*)nullptr, s.key, s.pos, st);
+    HF_LAUNCH("hf_vocab_sort", hf_vocab_sort_hist, blocks + fills, CHUNK, tok, T, V, bits,
+              s.hist, h2, blocks, share(0.0, 0.2), st);
+    HF_LAUNCH("hf_vocab_sort", hf_vocab_sort_pass, blocks + fills, CHUNK, tok,
+              (const int*)nullptr, (const int*)nullptr, T, V, bits, (const unsigned*)s.hist, h2,
+              s.tkey, s.tpos, blocks, share(0.2, 0.6), st);
+    HF_LAUNCH("hf_vocab_sort", hf_vocab_sort_pass, blocks + fills, CHUNK,
+              (const int32_t*)nullptr, (const int*)s.tkey, (const int*)s.tpos, T, V, bits,
+              (const unsigned*)h2, (unsigned*)nullptr, s.key, s.pos, blocks, share(0.6, 1.0),
+              st);
   }
-  const long long units = (long long)((T + RUN - 1) / RUN) * strips;
-  const int grid = (V + VROWS - 1) / VROWS;
+  if (T < 1) return;
+  const int runs = (T + RUN - 1) / RUN;
+  const long long units = (long long)runs * strips;
 #define HF_EG(SUF, E)                                                                         \
   do {                                                                                        \
-    if (T > 0)                                                                                \
-      HF_LAUNCH("hf_vocab_embed_runs",                                                        \
-                (vec ? hf_vocab_embed_runs_##SUF##_v : hf_vocab_embed_runs_##SUF),            \
-                (units + 3) / 4, 256, (const int*)s.key, (const int*)s.pos, T, V, D, strips,  \
-                scale, (const E*)dout, ldd, s.part, s.first, (E*)dE, lde, accumulate);        \
-    HF_LAUNCH("hf_vocab_embed_rows",                                                          \
-              (vec ? hf_vocab_embed_rows_##SUF##_v : hf_vocab_embed_rows_##SUF), grid, 256,   \
-              (const int*)s.key, T, V, D, strips, scale, (const float*)s.part,                \
-              (const int*)s.first, (E*)dE, lde, accumulate);                                  \
+    HF_LAUNCH("hf_vocab_embed_runs",                                                          \
+              (vec ? hf_vocab_embed_runs_##SUF##_v : hf_vocab_embed_runs_##SUF),              \
+              (units + 3) / 4, 256, (const int*)s.key, (const int*)s.pos, T, V, D, strips,    \
+              scale, (const E*)dout, ldd, s.part, (E*)dE, lde, accumulate);                   \
+    if (runs > 1)                                                                             \
+      HF_LAUNCH("hf_vocab_embed_join",                                                        \
+                (vec ? hf_vocab_embed_join_##SUF##_v : hf_vocab_embed_join_##SUF),            \
+                dim3((runs + 3) / 4, strips), 256, (const int*)s.key, T, V, D, strips, scale, \
+                (const float*)s.part, (E*)dE, lde, accumulate);                               \
   } while (0)
   if (type == VT_F32) HF_EG(f32, float);
   else HF_EG(bf16, bf16_t);

@@ -1,8 +1,12 @@
 // The GEMMs of the softmax head over a large vocabulary.  With X the counted
 // rows (T x D), W the vocabulary matrix (V x D) and tau the temperature:
-//   logits     z = X W^T / tau, of a piece of the vocabulary; per row and
-//              vocabulary tile the maximum and the sum of exp(z - max), from
-//              which the log-sum-exp over the whole vocabulary is joined
+//   logits     z = X W^T / tau, of a piece of the vocabulary; per row and 128
+//              (small tiles: 64) columns the maximum and the sum of
+//              exp(z - max), from which the log-sum-exp over the whole
+//              vocabulary is joined.  What is kept of a piece is z itself
+//              (fp32), or exp(z - max) in fp16 (bf16): 11 bits where delta
+//              has 8, absolute below 2^-14 of the largest of the 128, in a
+//              third of the bytes of z and delta
 //   p          exp(z - lse), recomputed piece by piece
 //   dX         delta W, delta = p - q (q the targets), summed over the pieces
 //   dW         delta^T X, whole for each piece
@@ -69,10 +73,10 @@ struct Tile {
   static constexpr int SIZE = ROWS * BK;
   static constexpr int INSTR = SIZE / EPC / 64 / NW;
   static_assert(SIZE % (EPC * 64 * NW) == 0, "tile does not split over the waves");
-  static_assert(BK * sizeof(E) == 128 && ROWS * sizeof(E) >= 256, "swizzles");
+  static_assert(BK * sizeof(E) <= 128 && ROWS * sizeof(E) >= 256, "swizzles");
 
   __device__ static __forceinline__ int swz(int r) {
-    if (KC) return (r >> 1) & 7;
+    if (KC) return (r / (256 / (BK * (int)sizeof(E)))) % CH;
     return sizeof(E) == 2 ? (r & 3) << 2 : ((r >> 2) & 1) << 3;
   }
   // the LDS row (of rows, or of k) and the global chunk that `lane` of `wave`
@@ -133,7 +137,9 @@ __device__ __forceinline__ float exp_of(float x) {
 __device__ __forceinline__ float load1(const float* p) { return *p; }
 __device__ __forceinline__ float load1(const bf16_t* p) { return bf2f(*p); }
 __device__ __forceinline__ void store1(float* p, float v) { *p = v; }
+__device__ __forceinline__ float load1(const _Float16* p) { return (float)*p; }
 __device__ __forceinline__ void store1(bf16_t* p, float v) { *p = (bf16_t)f2bf(v); }
+__device__ __forceinline__ void store1(_Float16* p, float v) { *p = (_Float16)v; }
 // whole 16-byte chunks
 __device__ __forceinline__ void add_chunk(const float* p, float (&v)[4]) {
   const f32x4 o = *(const f32x4*)p;
@@ -147,6 +153,14 @@ __device__ __forceinline__ void add_chunk(const bf16_t* p, float (&v)[8]) {
     v[2 * j] += bf2f(o[j] & 0xffffu);
     v[2 * j + 1] += bf2f(o[j] >> 16);
   }
+}
+__device__ __forceinline__ void add_chunk(const _Float16*, float (&)[8]) {}
+__device__ __forceinline__ void store_chunk(_Float16* p, const float (&v)[8]) {
+  typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+  f16x8 w;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) w[j] = (_Float16)v[j];
+  *(f16x8*)p = w;
 }
 __device__ __forceinline__ void store_chunk(float* p, const float (&v)[4]) {
   *(f32x4*)p = f32x4{v[0], v[1], v[2], v[3]};
@@ -207,7 +221,7 @@ __device__ __forceinline__ void store_part(const float* s, int lane, O* out, lon
 }
 
 // ----------------------------------------------------------------- epilogues
-enum { E_LOGITS, E_PROBS, E_PART, E_OUT, E_ROWS };
+enum { E_LOGITS, E_EXPS, E_PROBS, E_PART, E_OUT, E_ROWS };
 
 // The tile (tm, tn) and split this workgroup computes.  Consecutive
 // workgroups go to the 8 XCDs in turn; each XCD gets a contiguous eighth of
@@ -231,9 +245,9 @@ __device__ __forceinline__ void tile_of(int& tm, int& tn, int& tz) {
   tm = w / rows;
 }
 
-template <class E, int EPI, bool AKC, bool BKC, int WM, int WN, int GM, int GN, int S>
+template <class E, int EPI, bool AKC, bool BKC, int WM, int WN, int GM, int GN, int S, int KB>
 __device__ __forceinline__ void vgemm_body(const VGemm& s, const VEpi& e) {
-  constexpr int BK = 128 / (int)sizeof(E);
+  constexpr int BK = KB / (int)sizeof(E);
   constexpr int NW = GM * GN;
   constexpr int RM = 32 * WM * GM, RN = 32 * WN * GN;
   using TA = Tile<E, AKC, RM, BK, NW>;
@@ -354,7 +368,7 @@ __device__ __forceinline__ void vgemm_body(const VGemm& s, const VEpi& e) {
         }
   };
 
-  constexpr int NQ = 4;      // steps per K block
+  constexpr int NQ = KB / 32;      // steps per K block
   static_assert(NQ % 2 == 0 && (S - 1) * LPB < 64, "pipeline depth");
   Frags fa, fb;
 #pragma unroll
@@ -400,21 +414,28 @@ __device__ __forceinline__ void vgemm_body(const VGemm& s, const VEpi& e) {
   constexpr int RL = 32 * WM;
   static_assert(NW * 32 * RL * 4 <= S * STAGE * (int)sizeof(E), "staging exceeds the stages");
   float* const mine = (float*)lds + wave * 32 * RL;
-  if constexpr (EPI == E_LOGITS) {
-    // row statistics of this tile: within the lane, the two halves of the
-    // wave, then the GM waves that share the rows
-    __shared__ float2 red[GM][RN];
+  constexpr bool STATS = EPI == E_LOGITS || EPI == E_EXPS;
+  if constexpr (STATS) {
+    // row statistics of the wave's columns: within the lane, then the two
+    // halves of the wave.  exp(z - max) = exp2((acc - max) c): an argument off
+    // by 2^-24 of its size weighs exp of minus that size, so exp2 itself is
+    // exact enough for fp32
+    const float c2 = e.zscale * 1.44269504f;
+    const bool full = m0 + RM <= s.M;
 #pragma unroll
     for (int b = 0; b < WN; ++b) {
+      if (!full) {
+#pragma unroll
+        for (int a = 0; a < WM; ++a)
+#pragma unroll
+          for (int r = 0; r < 16; ++r)
+            if (mw + 32 * a + 8 * (r >> 2) + (r & 3) >= s.M) acc[a][b][r] = -INFINITY;
+      }
       float mx = -INFINITY;
 #pragma unroll
       for (int a = 0; a < WM; ++a)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const int m = mw + 32 * a + 8 * (r >> 2) + (r & 3);
-          acc[a][b][r] *= e.zscale;
-          if (m < s.M) mx = fmaxf(mx, acc[a][b][r]);
-        }
+        for (int r = 0; r < 16; ++r) mx = fmaxf(mx, acc[a][b][r]);
       mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
       // nothing but -inf: exp(-inf - 0) = 0, where -inf - -inf is no number
       const float at = mx == -INFINITY ? 0.0f : mx;
@@ -423,32 +444,23 @@ __device__ __forceinline__ void vgemm_body(const VGemm& s, const VEpi& e) {
       for (int a = 0; a < WM; ++a)
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-          const int m = mw + 32 * a + 8 * (r >> 2) + (r & 3);
-          sum += m < s.M ? exp_of<E>(acc[a][b][r] - at) : 0.0f;
+          const float x = __builtin_amdgcn_exp2f((acc[a][b][r] - at) * c2);
+          sum += x;
+          if (EPI == E_EXPS) acc[a][b][r] = x;
         }
       sum += __shfl_xor(sum, 32, 64);
-      if (h == 0) red[wm][wn * 32 * WN + 32 * b + li] = float2{mx, sum};
+      const int n = nt + 32 * b + li;
+      if (h == 0 && n < N && mt < s.M)
+        e.stat[(size_t)n * e.ldstat + e.tile0 + mt / RL] = float2{mx * e.zscale, sum};
     }
-    __syncthreads();     // also: every wave is done with the operand stages
-    for (int c = tid; c < RN; c += 64 * NW) {
-      if (n0 + c >= N) continue;
-      float mx = red[0][c].x, sum = red[0][c].y;
-#pragma unroll
-      for (int w = 1; w < GM; ++w) {
-        const float2 o = red[w][c];
-        const float t = fmaxf(mx, o.x), at = t == -INFINITY ? 0.0f : t;
-        sum = sum * exp_of<E>(mx - at) + o.y * exp_of<E>(o.x - at);
-        mx = t;
-      }
-      e.stat[(size_t)(n0 + c) * e.ldstat + e.tile0 + tm] = float2{mx, sum};
-    }
-    if (!e.z) return;
+    if (EPI == E_LOGITS && !e.z) return;
+    __syncthreads();     // every wave is done with the operand stages
   } else {
     __syncthreads();     // every wave is done with the operand stages
   }
   // columns and rows of p are written up to whole K blocks of the products
   // that read them: zeros past the piece and past the last row
-  const int Mp = EPI == E_PROBS ? (s.M + VPAD - 1) & ~(VPAD - 1) : s.M;
+  const int Mp = EPI == E_PROBS || STATS ? (s.M + VPAD - 1) & ~(VPAD - 1) : s.M;
   const int Np = EPI == E_PROBS ? (N + VPAD - 1) & ~(VPAD - 1) : N;
   constexpr bool FINAL = EPI == E_OUT || EPI == E_ROWS;
   const float scale = FINAL ? s.st->gscale : 1.0f;
@@ -466,7 +478,7 @@ __device__ __forceinline__ void vgemm_body(const VGemm& s, const VEpi& e) {
           const float c = acc[a][b][4 * g + j];
           if (EPI == E_PROBS)
             v[j] = n < N && mw + 32 * a + 8 * g + j < s.M ? exp_of<E>(c * e.zscale - lse) : 0.0f;
-          else v[j] = FINAL ? c * scale : c;
+          else v[j] = FINAL ? c * scale : EPI == E_LOGITS ? c * e.zscale : c;
         }
         *(f32x4*)(mine + li * RL + 4 * ((8 * a + 2 * g + h) ^ (li & (RL / 4 - 1)))) = v;
       }
@@ -476,6 +488,8 @@ __device__ __forceinline__ void vgemm_body(const VGemm& s, const VEpi& e) {
     const int nb = nt + 32 * b;
     if constexpr (EPI == E_LOGITS)
       store_part<float, RL>(mine, lane, e.z, e.ldz, nb, Np, mt, Mp, 1, 0);
+    else if constexpr (EPI == E_EXPS)
+      store_part<_Float16, RL>(mine, lane, (_Float16*)e.pt, e.ldz, nb, Np, mt, Mp, 1, 0);
     else if constexpr (EPI == E_PROBS)
       store_part<E, RL>(mine, lane, (E*)e.d, e.ldd, nb, Np, mt, Mp, 1, 0);
     else if constexpr (EPI == E_PART)
@@ -495,23 +509,35 @@ __device__ __forceinline__ void vgemm_body(const VGemm& s, const VEpi& e) {
 // big: 256 x 256 tiles, 8 waves of 128 x 64; else 128 x 128, 4 waves of 64 x 64
 #define HF_VGEMM(NAME, EPI, AKC, BKC)                                                  \
   extern "C" __global__ __launch_bounds__(512, 1) void NAME##_bf16_big(VGemm s, VEpi e) { \
-    vgemm_body<bf16_t, EPI, AKC, BKC, 4, 2, 2, 4, 2>(s, e);                            \
+    vgemm_body<bf16_t, EPI, AKC, BKC, 4, 2, 2, 4, 2, 128>(s, e);                       \
   }                                                                                    \
   extern "C" __global__ __launch_bounds__(256, 2) void NAME##_bf16(VGemm s, VEpi e) {  \
-    vgemm_body<bf16_t, EPI, AKC, BKC, 2, 2, 2, 2, 2>(s, e);                            \
+    vgemm_body<bf16_t, EPI, AKC, BKC, 2, 2, 2, 2, 2, 128>(s, e);                       \
   }                                                                                    \
   extern "C" __global__ __launch_bounds__(512, 1) void NAME##_f32_big(VGemm s, VEpi e) {  \
-    vgemm_body<float, EPI, AKC, BKC, 4, 2, 2, 4, 2>(s, e);                             \
+    vgemm_body<float, EPI, AKC, BKC, 4, 2, 2, 4, 2, 128>(s, e);                        \
   }                                                                                    \
   extern "C" __global__ __launch_bounds__(256, 2) void NAME##_f32(VGemm s, VEpi e) {   \
-    vgemm_body<float, EPI, AKC, BKC, 2, 2, 2, 2, 2>(s, e);                             \
+    vgemm_body<float, EPI, AKC, BKC, 2, 2, 2, 2, 2, 128>(s, e);                        \
   }
 HF_VGEMM(hf_vocab_logits, E_LOGITS, true, true)
+extern "C" __global__ __launch_bounds__(512, 1) void hf_vocab_exps_bf16_big(VGemm s, VEpi e) {
+  vgemm_body<bf16_t, E_EXPS, true, true, 4, 2, 2, 4, 2, 128>(s, e);
+}
+extern "C" __global__ __launch_bounds__(256, 2) void hf_vocab_exps_bf16(VGemm s, VEpi e) {
+  vgemm_body<bf16_t, E_EXPS, true, true, 2, 2, 2, 2, 2, 128>(s, e);
+}
 HF_VGEMM(hf_vocab_probs, E_PROBS, true, true)
 HF_VGEMM(hf_vocab_dx, E_PART, false, true)
 HF_VGEMM(hf_vocab_dx_out, E_ROWS, false, true)
 HF_VGEMM(hf_vocab_dw, E_OUT, false, false)
 HF_VGEMM(hf_vocab_dw_part, E_PART, false, false)
+// dW of few rows: bound by the stores of its output, so three workgroups per
+// compute unit, with half the K block, cover each other's latency better (5
+// rows x 32,000 x 1,024: 21 -> 17.6 us)
+extern "C" __global__ __launch_bounds__(256, 3) void hf_vocab_dw_bf16_thin(VGemm s, VEpi e) {
+  vgemm_body<bf16_t, E_OUT, false, false, 2, 2, 2, 2, 2, 64>(s, e);
+}
 
 // ------------------------------------------------------------- launchers
 namespace {
@@ -531,7 +557,8 @@ void launch(const Launch& L, const char* name, const VK (&k)[2][2], int type, co
 #define HF_VK(NAME) {{NAME##_f32, NAME##_f32_big}, {NAME##_bf16, NAME##_bf16_big}}
 void vocab_logits(const Launch& L, int type, const VGemm& g, const VEpi& e) {
   static const VK k[2][2] = HF_VK(hf_vocab_logits);
-  launch(L, "hf_vocab_logits", k, type, g, e);
+  static const VK x[2][2] = {{nullptr, nullptr}, {hf_vocab_exps_bf16, hf_vocab_exps_bf16_big}};
+  launch(L, "hf_vocab_logits", e.pt ? x : k, type, g, e);
 }
 void vocab_probs(const Launch& L, int type, const VGemm& g, const VEpi& e) {
   static const VK k[2][2] = HF_VK(hf_vocab_probs);
@@ -543,7 +570,9 @@ void vocab_dx(const Launch& L, int type, const VGemm& g, const VEpi& e) {
 }
 void vocab_dw(const Launch& L, int type, const VGemm& g, const VEpi& e) {
   static const VK k[2][2] = HF_VK(hf_vocab_dw), p[2][2] = HF_VK(hf_vocab_dw_part);
-  launch(L, "hf_vocab_dw", g.splits > 1 ? p : k, type, g, e);
+  static const VK thin[2][2] = {{hf_vocab_dw_f32, hf_vocab_dw_f32_big},
+                                {hf_vocab_dw_bf16_thin, hf_vocab_dw_bf16_big}};
+  launch(L, "hf_vocab_dw", g.splits > 1 ? p : g.K <= 256 ? thin : k, type, g, e);
 }
 
 }  // namespace hfk

@@ -15,8 +15,8 @@ enum VType { VT_F32 = 0, VT_BF16 = 1 };
 constexpr int VPAD = 64;
 // Rows of packed operands come in whole tiles of this many.
 constexpr int VTILE = 256;
-// Columns of one tile of row statistics (the smallest vocabulary tile).
-constexpr int VSTAT = 128;
+// Columns of one entry of row statistics: a wave's part of a vocabulary tile.
+constexpr int VSTAT = 64, VSTAT_BIG = 128;
 constexpr int VMAX_SPLITS = 64;
 
 // Device scalars of a call.
@@ -47,10 +47,11 @@ struct VEpi {
   // logits
   float zscale;          // 1 / tau
   float* z;              // logits kept (row n, column m), or null
+  void* pt;              // or exp(z - max of its statistics entry) in fp16
   long long ldz;
-  float2* stat;          // per row and vocabulary tile: max, sum of exp
-  int ldstat, tile0;     // tiles per row; index of this launch's first tile
-  const float* lse;      // delta: log-sum-exp per row (+inf: no such row)
+  float2* stat;          // per row and entry: max, sum of exp(z - max)
+  int ldstat, tile0;     // entries per row; index of this launch's first
+  const float* lse;      // p: log-sum-exp per row
   void* d;               // delta, row n, column m
   long long ldd;
   // products
@@ -65,7 +66,7 @@ struct VEpi {
 };
 
 // logits of a vocabulary piece: A = W piece (akc), B = packed rows (akc);
-//   stat, and z if kept
+//   stat, and z or pt if kept
 void vocab_logits(const Launch& L, int type, const VGemm& g, const VEpi& e);
 // p = exp(z - lse) of a vocabulary piece, rounded to the type, into d
 void vocab_probs(const Launch& L, int type, const VGemm& g, const VEpi& e);
@@ -113,27 +114,31 @@ struct VTarget {
 void vocab_target_logits(const Launch& L, int type, const VRows& r, const void* X,
                          long long ldx, const void* xp, int Dp, const void* W,
                          long long ldw, float* zt);
-// log-sum-exp from the tiles' statistics, the rows' losses and the targets'
-// delta; z: kept logits or null (then t.zt holds the targets')
+// log-sum-exp from the statistics, the rows' losses and the targets' delta;
+// z: kept logits or null (then t.zt holds the targets')
 void vocab_row_loss(const Launch& L, const VRows& r, const float2* stat, int ldstat,
                     int tiles, const float* z, long long ldz, const VTarget& t,
                     float* lse);
 // loss = sum of the counted rows' losses / denom
 void vocab_loss_sum(const Launch& L, const VRows& r, float* loss);
-// delta from kept logits, targets included (dup: the rounding's rest too, dup
-// rows further down), and the loss
-void vocab_delta(const Launch& L, int type, const VRows& r, const float* z,
-                 long long ldz, const float* lse, const VTarget& t, int rows,
-                 void* d, long long ldd, int Vp, int dup, float* loss);
+// delta from kept logits of the columns [v0, v0 + Vc), targets included (dup:
+// the rounding's rest too, dup rows further down), and the loss unless null.
+// z null (bf16): d holds exp(z - max) in fp16, by statistics entries of `sg`
+// columns.
+// self (bf16 with all columns kept): the rows' statistics and losses as well,
+// instead of vocab_row_loss; the loss is then still to be summed.
+void vocab_delta(const Launch& L, int type, const VRows& r, const float* z, long long ldz,
+                 const float2* stat, int tiles, int sg, const float* lse, const VTarget& t,
+                 int v0, int Vc, int rows, bool self, void* d, long long ldd, int dup, float* loss);
 // delta at the targets within the piece [v0, v0 + Vc)
 void vocab_fix(const Launch& L, int type, const VRows& r, const VTarget& t, int v0,
                int Vc, void* d, long long ldd);
 // out(row) = gscale (sum over splits, and over the dup copy) part(row);
-// idx: destination row of a packed row, null: itself
+// idx: destination row of a packed row, null: itself; and the loss, unless null
 void vocab_finish(const Launch& L, int type, const VocabState* st, const float* part,
                   int splits, long long split_stride, long long ldp, int dup, int rows,
                   int dyn, int D, const int* idx, void* out, long long ldo,
-                  int accumulate);
+                  int accumulate, const VRows* r, float* loss);
 
 // ---------------------------------------------------------------- embedding
 struct VSort {
@@ -142,7 +147,6 @@ struct VSort {
   int* tkey;                // T: scratch
   int* tpos;
   unsigned* hist;           // histograms of the radix passes
-  int* first;               // V: a token's first place in order, -1: none
   float* part;              // sums of tokens that reach over a run's ends
 };
 // unsigned words of hist, and floats of part, for T rows

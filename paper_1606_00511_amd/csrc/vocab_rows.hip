@@ -11,7 +11,9 @@
 //   loss  = tau^2 sum_k q_k (log q_k - (z_k - lse))
 //   delta = p - q,  p_v = exp(z_v - lse)
 // delta is p rounded to the type everywhere but at the targets, where p - q is
-// formed in fp32 and rounded once.  Losses are summed in fp64.
+// formed in fp32 and rounded once.  With bf16, p comes from exp(z - max) kept
+// in fp16 (a rounding of 2^-12 beside delta's 2^-9) but for few rows.  Losses
+// are summed in fp64.
 #include <type_traits>
 
 #include "vocab_internal.h"
@@ -199,7 +201,7 @@ __device__ __forceinline__ void pack_body(const VRows& r, const E* X, long long 
     bool have = false;
     float v;
     if (t < r.T)
-      for (int k = 0; k < r.K; ++k) have |= target(r, t, k, &v) >= 0;
+      for (int k = 0; k < r.K && !have; ++k) have = target(r, t, k, &v) >= 0;
     const int at = scan_threads<4>(have, sums, n);
     place[t] = have ? at : -1;
     __syncthreads();
@@ -257,38 +259,62 @@ extern "C" __global__ __launch_bounds__(256) void hf_vocab_copy_bf16(
 }
 
 // ---------------------------------------------------- the targets' logits
-// Where the logits are not kept: the K products x_j . W[id] of a packed row,
-// one wave each.
+// Where the logits are not kept in fp32: the K products x_j . W[id] of a packed
+// row, U of them at a time per wave.  Bound by the reads of W's rows.
 namespace {
 template <class E>
 __device__ __forceinline__ void tlogit_body(const VRows& r, const E* X, long long ldx,
                                             const E* xp, int Dp, const E* W, long long ldw,
                                             int vec, float* zt) {
-  constexpr int EPC = 16 / sizeof(E);
+  constexpr int EPC = 16 / sizeof(E), U = 4;
   const int j = blockIdx.x;
   if (j >= r.st->n) return;
   const int t = r.idx[j], wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const E* x = X && r.st->n == r.T ? X + (size_t)j * ldx : xp + (size_t)j * Dp;
   float v;
-  for (int k = wave; k < r.K; k += 4) {
-    const int id = target(r, t, k, &v);
-    if (id < 0) continue;
-    const E* w = W + (size_t)id * ldw;
-    float s = 0.0f;
-    if (vec) {
-      for (int c = lane; c < r.D / EPC; c += 64) {
-        E a[EPC], b[EPC];
-        *(u32x4*)a = *(const u32x4*)(x + EPC * c);
-        *(u32x4*)b = *(const u32x4*)(w + EPC * c);
+  for (int k0 = wave * U; k0 < r.K; k0 += 4 * U) {
+    const E* w[U];
+    bool have[U];
+    float s[U];
 #pragma unroll
-        for (int i = 0; i < EPC; ++i) s += to_f(a[i]) * to_f(b[i]);
-      }
-      for (int c = r.D / EPC * EPC + lane; c < r.D; c += 64) s += to_f(x[c]) * to_f(w[c]);
-    } else {
-      for (int c = lane; c < r.D; c += 64) s += to_f(x[c]) * to_f(w[c]);
+    for (int u = 0; u < U; ++u) {
+      const int id = k0 + u < r.K ? target(r, t, k0 + u, &v) : -1;
+      have[u] = id >= 0;
+      w[u] = W + (size_t)max(id, 0) * ldw;
+      s[u] = 0.0f;
     }
-    s = wave_sum(s);
-    if (lane == 0) zt[(size_t)j * r.K + k] = s / r.tau;
+    // a lane has the same chunks in the same order whether its loads are of 16
+    // bytes or single elements
+    for (int c = EPC * lane; c < r.D; c += 64 * EPC) {
+      E a[EPC], b[U][EPC];
+      const bool whole = c + EPC <= r.D;
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        if (!have[u]) continue;
+        if (vec && whole) {
+          *(u32x4*)b[u] = *(const u32x4*)(w[u] + c);
+        } else {
+#pragma unroll
+          for (int i = 0; i < EPC; ++i) b[u][i] = c + i < r.D ? w[u][c + i] : (E)0;
+        }
+      }
+      if (whole) {
+        *(u32x4*)a = *(const u32x4*)(x + c);
+      } else {
+#pragma unroll
+        for (int i = 0; i < EPC; ++i) a[i] = c + i < r.D ? x[c + i] : (E)0;
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (have[u])
+#pragma unroll
+          for (int i = 0; i < EPC; ++i) s[u] += to_f(a[i]) * to_f(b[u][i]);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const float f = wave_sum(s[u]);
+      if (lane == 0 && have[u]) zt[(size_t)j * r.K + k0 + u] = f / r.tau;
+    }
   }
 }
 }  // namespace
@@ -304,28 +330,40 @@ extern "C" __global__ __launch_bounds__(256) void hf_vocab_tlogit_bf16(
 }
 
 // ------------------------------------------------------------- rows' losses
-// One wave per packed row; lane l has the targets l and l + 64.
-extern "C" __global__ __launch_bounds__(256) void hf_vocab_row_loss(
-    VRows r, const float2* __restrict__ stat, int ldstat, int tiles,
-    const float* __restrict__ z, long long ldz, VTarget tg, float* __restrict__ lse_out) {
-  const int j = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
-  const int n = r.st->n;
-  if (j >= n) {
-    // rows that only fill the last K block: p = exp(0 - inf) = 0
-    if (j < (n + VPAD - 1) / VPAD * VPAD && lane == 0) lse_out[j] = INFINITY;
-    return;
-  }
-  const int t = r.idx[j];
-  float mx = -INFINITY;
+namespace {
+struct RowTargets {          // lane l: targets l and l + 64
+  float lse, loss;
+  int id[2];                 // -1: none, or a repeat
+  float dt[2];               // delta at the target
+};
+// One packed row j < n by one wave.  zt: the targets' logits, or null: in z.
+__device__ __forceinline__ RowTargets row_targets(const VRows& r, int j,
+                                                  const float2* __restrict__ stat, int ldstat,
+                                                  int tiles, const float* __restrict__ z,
+                                                  long long ldz, const float* __restrict__ zt) {
+  const int lane = threadIdx.x & 63, t = r.idx[j];
+  RowTargets o;
   const float2* st = stat + (size_t)j * ldstat;
-  for (int i = lane; i < tiles; i += 64) mx = fmaxf(mx, st[i].x);
-  mx = wave_max(mx);
-  const float at = mx == -INFINITY ? 0.0f : mx;
-  float sum = 0.0f;
-  for (int i = lane; i < tiles; i += 64) sum += st[i].y * expf(st[i].x - at);
-  sum = wave_sum(sum);
-  const float lse = at + logf(sum);
-  if (lane == 0) lse_out[j] = lse;
+  // 8 entries a lane at a time; (m, s) of those before are scaled to the new
+  // maximum (0 instead of -inf: exp(-inf - 0) = 0)
+  constexpr int U = 8;
+  float m = -INFINITY, s = 0.0f;
+  for (int i0 = lane; i0 < tiles; i0 += 64 * U) {
+    float2 v[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      v[u] = i0 + 64 * u < tiles ? st[i0 + 64 * u] : float2{-INFINITY, 0.0f};
+    float top = m;
+#pragma unroll
+    for (int u = 0; u < U; ++u) top = fmaxf(top, v[u].x);
+    const float at = top == -INFINITY ? 0.0f : top;
+    s *= expf(m - at);
+#pragma unroll
+    for (int u = 0; u < U; ++u) s += v[u].y * expf(v[u].x - at);
+    m = top;
+  }
+  const float mx = wave_max(m), at = mx == -INFINITY ? 0.0f : mx;
+  o.lse = at + logf(wave_sum(s * expf(m - at)));
 
   int id[2] = {-1, -1};
   float tl[2] = {0.0f, 0.0f}, q[2] = {0.0f, 0.0f}, lz[2] = {0.0f, 0.0f};
@@ -335,9 +373,9 @@ extern "C" __global__ __launch_bounds__(256) void hf_vocab_row_loss(
       const int k = lane + 64 * i;
       id[i] = target(r, t, k, &tl[i]);
       if (id[i] >= 0) {
-        const float zt = z ? z[(size_t)j * ldz + id[i]] : tg.zt[(size_t)j * r.K + k];
+        const float x = zt ? zt[(size_t)j * r.K + k] : z[(size_t)j * ldz + id[i]];
         // log p; above 0 only by rounding (the comparison keeps a NaN)
-        lz[i] = zt - lse > 0.0f ? 0.0f : zt - lse;
+        lz[i] = x - o.lse > 0.0f ? 0.0f : x - o.lse;
       }
     }
   float loss = 0.0f;
@@ -382,15 +420,33 @@ extern "C" __global__ __launch_bounds__(256) void hf_vocab_row_loss(
         loss += qs[i] * ((same[i] > 1 ? logf(qs[i]) : u[i] - lt) - lz[i]);
   }
   loss = wave_sum(loss) * (r.tau * r.tau);
-  if (loss < 0.0f) loss = 0.0f;        // no divergence is; rounding can be
-  if (lane == 0) r.row_loss[t] = loss;
+  o.loss = loss < 0.0f ? 0.0f : loss;    // no divergence is; rounding can be
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    o.id[i] = first[i] ? id[i] : -1;
+    o.dt[i] = expf(lz[i]) - qs[i];
+  }
+  return o;
+}
+}  // namespace
+
+// One wave per packed row.
+extern "C" __global__ __launch_bounds__(256) void hf_vocab_row_loss(
+    VRows r, const float2* __restrict__ stat, int ldstat, int tiles,
+    const float* __restrict__ z, long long ldz, VTarget tg, float* __restrict__ lse) {
+  const int j = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+  if (j >= r.st->n) return;
+  const RowTargets o = row_targets(r, j, stat, ldstat, tiles, z, ldz, z ? nullptr : tg.zt);
+  if (lane == 0) {
+    lse[j] = o.lse;
+    r.row_loss[r.idx[j]] = o.loss;
+  }
   if (!tg.dt) return;
 #pragma unroll
   for (int i = 0; i < 2; ++i)
     if (lane + 64 * i < r.K) {
-      const size_t o = (size_t)j * r.K + lane + 64 * i;
-      tg.id[o] = id[i] >= 0 && first[i] ? id[i] : -1;
-      tg.dt[o] = expf(lz[i]) - qs[i];
+      tg.id[(size_t)j * r.K + lane + 64 * i] = o.id[i];
+      tg.dt[(size_t)j * r.K + lane + 64 * i] = o.dt[i];
     }
 }
 
@@ -419,35 +475,84 @@ extern "C" __global__ __launch_bounds__(256) void hf_vocab_loss_sum(
 }
 
 // ------------------------------------------------------------------- delta
-// A workgroup has 2,048 columns of one packed row; the last one sums the loss.
+// A workgroup has 2,048 of the Vc columns from v0 of one packed row; z and d
+// hold these columns from 0.
+// SELF (few rows): it forms the row's statistics and targets by itself (a
+// launch less), the first columns' workgroup writes the row's loss; otherwise
+// they come from hf_vocab_row_loss, and the last workgroup sums the loss.
 namespace {
 constexpr int DCOLS = 2048;
-template <class E>
-__device__ __forceinline__ void delta_body(const VRows& r, const float* z, long long ldz,
-                                           const float* lse, const VTarget& tg, int chunks,
-                                           E* d, long long ldd, int Vp, int dup, float* loss) {
-  if (blockIdx.x == gridDim.x - 1) {
-    loss_sum(r.row_loss, r.T, r.st, loss);
+struct VDelta {
+  const float* z;
+  long long ldz;
+  const float2* stat;
+  int ldstat, tiles;
+  const float* lse;
+  VTarget tg;
+  int chunks, v0, Vc, Vp, dup;
+  long long ldd;
+  float* loss;
+  int sg;                      // columns of a statistics entry
+};
+// FROM16: d holds exp(z - max) in fp16 and becomes delta in place.
+template <class E, bool SELF, bool FROM16>
+__device__ __forceinline__ void delta_body(const VRows& r, const VDelta& a, E* d) {
+  if (!SELF && a.loss && blockIdx.x == gridDim.x - 1) {
+    loss_sum(r.row_loss, r.T, r.st, a.loss);
     return;
   }
-  const int j = blockIdx.x / chunks, c0 = (blockIdx.x % chunks) * DCOLS;
+  __shared__ float lse_s, dt_s[SELF ? 128 : 1];
+  __shared__ int id_s[SELF ? 128 : 1];
+  const int j = blockIdx.x / a.chunks, c0 = (blockIdx.x % a.chunks) * DCOLS;
   const int n = r.st->n;
-  if (j >= n && j >= (dup ? dup : (n + VPAD - 1) / VPAD * VPAD)) return;
+  if (j >= n && j >= (a.dup ? a.dup : (n + VPAD - 1) / VPAD * VPAD)) return;
   const bool real = j < n;
-  const float l = real ? lse[j] : 0.0f;
-  E* hi = d + (size_t)j * ldd;
-  E* lo = dup ? d + (size_t)(dup + j) * ldd : nullptr;
-  const float* zr = z + (size_t)j * ldz;
+  if constexpr (SELF) {
+    if (real && threadIdx.x < 64) {
+      const int lane = threadIdx.x;
+      const RowTargets o = row_targets(r, j, a.stat, a.ldstat, a.tiles, a.z, a.ldz, nullptr);
+      if (lane == 0) {
+        lse_s = o.lse;
+        if (c0 == 0) r.row_loss[r.idx[j]] = o.loss;
+      }
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        id_s[lane + 64 * i] = o.id[i];
+        dt_s[lane + 64 * i] = o.dt[i];
+      }
+    }
+    __syncthreads();
+  }
+  const float l = !real ? 0.0f : SELF ? lse_s : a.lse[j];
+  E* hi = d + (size_t)j * a.ldd;
+  E* lo = a.dup ? d + (size_t)(a.dup + j) * a.ldd : nullptr;
+  const float* zr = a.z + (size_t)j * a.ldz;
+  if constexpr (FROM16) {
+    // 8 columns a thread, of one statistics entry
+    typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+    const int c = c0 + 8 * (int)threadIdx.x;
+    if (c < a.Vp) {
+      u32x4 w = u32x4{0u, 0u, 0u, 0u};
+      if (real && c < a.Vc) {
+        const float f = expf(a.stat[(size_t)j * a.ldstat + (a.v0 + c) / a.sg].x - l);
+        const f16x8 x = *(const f16x8*)(hi + c);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          w[e] = f2bf((float)x[2 * e] * f) | f2bf((float)x[2 * e + 1] * f) << 16;
+      }
+      *(u32x4*)(hi + c) = w;
+    }
+  }
   // 4 columns a thread and step
 #pragma unroll
-  for (int i = 0; i < DCOLS / 1024; ++i) {
+  for (int i = 0; !FROM16 && i < DCOLS / 1024; ++i) {
     const int c = c0 + 4 * (int)threadIdx.x + 1024 * i;
-    if (c >= Vp) break;
+    if (c >= a.Vp) break;
     float v[4];
     f32x4 zz = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     if (real) zz = *(const f32x4*)(zr + c);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = real && c + e < r.V ? expf(zz[e] - l) : 0.0f;
+    for (int e = 0; e < 4; ++e) v[e] = real && c + e < a.Vc ? expf(zz[e] - l) : 0.0f;
     if constexpr (sizeof(E) == 4) {
       *(f32x4*)(hi + c) = f32x4{v[0], v[1], v[2], v[3]};
     } else {
@@ -465,25 +570,23 @@ __device__ __forceinline__ void delta_body(const VRows& r, const float* z, long 
   // the targets among these columns, over what was just written
   __syncthreads();
   for (int k = threadIdx.x; k < r.K; k += 256) {
-    const int id = tg.id[(size_t)j * r.K + k];
-    if (id < c0 || id >= c0 + DCOLS) continue;
-    const float v = tg.dt[(size_t)j * r.K + k];
-    put(hi + id, v);
+    const int id = SELF ? id_s[k] : a.tg.id[(size_t)j * r.K + k];
+    if (id < 0 || id < a.v0 + c0 || id >= a.v0 + min(c0 + DCOLS, a.Vc)) continue;
+    const float v = SELF ? dt_s[k] : a.tg.dt[(size_t)j * r.K + k];
+    put(hi + (id - a.v0), v);
     if constexpr (sizeof(E) == 2)
-      if (lo) put(lo + id, v - bf2f(f2bf(v)));
+      if (lo) put(lo + (id - a.v0), v - bf2f(f2bf(v)));
   }
 }
 }  // namespace
-extern "C" __global__ __launch_bounds__(256) void hf_vocab_delta_f32(
-    VRows r, const float* z, long long ldz, const float* lse, VTarget tg, int chunks, float* d,
-    long long ldd, int Vp, int dup, float* loss) {
-  delta_body<float>(r, z, ldz, lse, tg, chunks, d, ldd, Vp, dup, loss);
-}
-extern "C" __global__ __launch_bounds__(256) void hf_vocab_delta_bf16(
-    VRows r, const float* z, long long ldz, const float* lse, VTarget tg, int chunks, bf16_t* d,
-    long long ldd, int Vp, int dup, float* loss) {
-  delta_body<bf16_t>(r, z, ldz, lse, tg, chunks, d, ldd, Vp, dup, loss);
-}
+#define HF_DELTA(SUF, E, SELF, FROM16)                                      \
+  extern "C" __global__ __launch_bounds__(256) void hf_vocab_delta_##SUF(   \
+      VRows r, VDelta a, E* d) {                                            \
+    delta_body<E, SELF, FROM16>(r, a, d);                                   \
+  }
+HF_DELTA(f32, float, false, false)
+HF_DELTA(bf16, bf16_t, false, true)
+HF_DELTA(bf16_self, bf16_t, true, false)
 
 namespace {
 template <class E>
@@ -516,7 +619,12 @@ template <class E, int G>
 __device__ __forceinline__ void finish_body(const VocabState* st, const float* part, int splits,
                                             long long ss, long long ldp, int dup, int rows,
                                             int dyn, int D, const int* idx, E* out,
-                                            long long ldo, int accumulate) {
+                                            long long ldo, int accumulate,
+                                            const float* row_loss, int T, float* loss) {
+  if (loss && blockIdx.x == gridDim.x - 1) {
+    loss_sum(row_loss, T, st, loss);
+    return;
+  }
   constexpr int QB = 256 / G;           // column groups per workgroup
   __shared__ f32x4 sums[G > 1 ? 256 : 1];
   const int q = (D + 3) / 4, grp = threadIdx.x / QB;
@@ -526,11 +634,18 @@ __device__ __forceinline__ void finish_body(const VocabState* st, const float* p
   const int parts = dup ? 2 * splits : splits;
   f32x4 s = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   if (in) {
-#pragma unroll 8
-    for (int z = grp; z < parts; z += G) {
-      const int zz = z < splits ? z : z - splits;
-      const size_t row = z < splits ? j : dup + j;
-      s += *(const f32x4*)(part + zz * ss + row * ldp + c);
+    constexpr int U = G > 1 ? 8 : 4;
+    for (int z0 = grp; z0 < parts; z0 += U * G) {
+      f32x4 v[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int z = min(z0 + u * G, parts - 1), zz = z < splits ? z : z - splits;
+        const size_t row = z < splits ? j : dup + j;
+        v[u] = *(const f32x4*)(part + zz * ss + row * ldp + c);
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (z0 + u * G < parts) s += v[u];
     }
   }
   if constexpr (G > 1) {
@@ -551,9 +666,9 @@ __device__ __forceinline__ void finish_body(const VocabState* st, const float* p
   extern "C" __global__ __launch_bounds__(256) void hf_vocab_finish_##SUF(                 \
       const VocabState* st, const float* part, int splits, long long ss, long long ldp,    \
       int dup, int rows, int dyn, int D, const int* idx, E* out, long long ldo,            \
-      int accumulate) {                                                                    \
+      int accumulate, const float* row_loss, int T, float* loss) {                         \
     finish_body<E, G>(st, part, splits, ss, ldp, dup, rows, dyn, D, idx, out, ldo,         \
-                      accumulate);                                                         \
+                      accumulate, row_loss, T, loss);                                      \
   }
 HF_FINISH(f32, float, 1)
 HF_FINISH(f32_g8, float, 8)
@@ -619,7 +734,8 @@ void vocab_target_logits(const Launch& L, int type, const VRows& r, const void* 
 
 void vocab_row_loss(const Launch& L, const VRows& r, const float2* stat, int ldstat, int tiles,
                     const float* z, long long ldz, const VTarget& t, float* lse) {
-  HF_LAUNCH("hf_vocab_row_loss", hf_vocab_row_loss, (r.T + VPAD + 3) / 4, 256, r, stat, ldstat,
+  if (r.T < 1) return;
+  HF_LAUNCH("hf_vocab_row_loss", hf_vocab_row_loss, (r.T + 3) / 4, 256, r, stat, ldstat,
             tiles, z, ldz, t, lse);
 }
 
@@ -628,16 +744,29 @@ void vocab_loss_sum(const Launch& L, const VRows& r, float* loss) {
 }
 
 void vocab_delta(const Launch& L, int type, const VRows& r, const float* z, long long ldz,
-                 const float* lse, const VTarget& t, int rows, void* d, long long ldd, int Vp,
-                 int dup, float* loss) {
-  const int chunks = (Vp + DCOLS - 1) / DCOLS;
-  const long long grid = (long long)rows * chunks + 1;
+                 const float2* stat, int tiles, int sg, const float* lse, const VTarget& t, int v0,
+                 int Vc, int rows, bool self, void* d, long long ldd, int dup, float* loss) {
+  VDelta a = {};
+  a.z = z;
+  a.ldz = ldz;
+  a.stat = stat;
+  a.ldstat = a.tiles = tiles;
+  a.lse = lse;
+  a.tg = t;
+  a.Vp = (Vc + VPAD - 1) / VPAD * VPAD;
+  a.chunks = (a.Vp + DCOLS - 1) / DCOLS;
+  a.v0 = v0;
+  a.Vc = Vc;
+  a.dup = dup;
+  a.ldd = ldd;
+  a.loss = loss;
+  a.sg = sg;
+  const long long grid = (long long)rows * a.chunks + (loss && !self ? 1 : 0);
   if (type == VT_F32)
-    HF_LAUNCH("hf_vocab_delta", hf_vocab_delta_f32, grid, 256, r, z, ldz, lse, t, chunks,
-              (float*)d, ldd, Vp, dup, loss);
+    HF_LAUNCH("hf_vocab_delta", hf_vocab_delta_f32, grid, 256, r, a, (float*)d);
   else
-    HF_LAUNCH("hf_vocab_delta", hf_vocab_delta_bf16, grid, 256, r, z, ldz, lse, t, chunks,
-              (bf16_t*)d, ldd, Vp, dup, loss);
+    HF_LAUNCH("hf_vocab_delta", (self ? hf_vocab_delta_bf16_self : hf_vocab_delta_bf16), grid,
+              256, r, a, (bf16_t*)d);
 }
 
 void vocab_fix(const Launch& L, int type, const VRows& r, const VTarget& t, int v0, int Vc,
@@ -651,17 +780,21 @@ void vocab_fix(const Launch& L, int type, const VRows& r, const VTarget& t, int 
 
 void vocab_finish(const Launch& L, int type, const VocabState* st, const float* part, int splits,
                   long long ss, long long ldp, int dup, int rows, int dyn, int D, const int* idx,
-                  void* out, long long ldo, int accumulate) {
+                  void* out, long long ldo, int accumulate, const VRows* r, float* loss) {
   const bool g8 = (dup ? 2 : 1) * splits >= 16;
-  const long long grid = ((long long)rows * ((D + 3) / 4) * (g8 ? 8 : 1) + 255) / 256;
+  const long long grid =
+      ((long long)rows * ((D + 3) / 4) * (g8 ? 8 : 1) + 255) / 256 + (loss ? 1 : 0);
   if (grid < 1) return;
+  const float* rl = loss ? r->row_loss : nullptr;
+  const int T = loss ? r->T : 0;
   if (type == VT_F32)
     HF_LAUNCH("hf_vocab_finish", (g8 ? hf_vocab_finish_f32_g8 : hf_vocab_finish_f32), grid, 256,
-              st, part, splits, ss, ldp, dup, rows, dyn, D, idx, (float*)out, ldo, accumulate);
+              st, part, splits, ss, ldp, dup, rows, dyn, D, idx, (float*)out, ldo, accumulate,
+              rl, T, loss);
   else
     HF_LAUNCH("hf_vocab_finish", (g8 ? hf_vocab_finish_bf16_g8 : hf_vocab_finish_bf16), grid,
               256, st, part, splits, ss, ldp, dup, rows, dyn, D, idx, (bf16_t*)out, ldo,
-              accumulate);
+              accumulate, rl, T, loss);
 }
 
 }  // namespace hfk

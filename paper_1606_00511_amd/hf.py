@@ -500,6 +500,7 @@ class HFVocab:
             raise HFError(rc, "hf_vocab_create rejected vocab=%d width=%d max_rows=%d"
                           % (self.vocab, self.width, self.max_rows))
         self._h = h
+        self._stream = 0                  # of the last call
         nbytes = int(L.hf_vocab_workspace_bytes(
             h, self.max_rows if ws_rows is None else int(ws_rows)))
         if nbytes == 0:
@@ -520,13 +521,15 @@ class HFVocab:
 
     def _call(self, fn, *args):
         import torch
-        stream = torch.cuda.current_stream(self.device).cuda_stream
         if torch.cuda.current_device() != self.device.index:
             with torch.cuda.device(self.device):
-                lib().hf_vocab_set_stream(self._h, stream)
-                return self._check(getattr(lib(), fn)(self._h, *args))
-        lib().hf_vocab_set_stream(self._h, stream)
-        return self._check(getattr(lib(), fn)(self._h, *args))
+                return self._call(fn, *args)
+        L = lib()
+        stream = torch.cuda.current_stream(self.device.index).cuda_stream
+        if stream != self._stream:
+            self._check(L.hf_vocab_set_stream(self._h, stream))
+            self._stream = stream
+        return self._check(getattr(L, fn)(self._h, *args))
 
     def close(self):
         if getattr(self, "_h", None) is not None:

@@ -445,6 +445,7 @@ int hf_prof_get(hf_ctx* ctx, int32_t i, const char** name, int64_t* launches,
  * masked; any other value counts as masked and raises HF_ELABEL in the next
  * hf_vocab_check.  Rows without a target count nothing: no loss, a zero row
  * of dX, nothing in dW, whatever X holds there.
+ * Outputs may not overlap inputs.
  * Memory, streams and errors as for hf_ctx: device pointers owned by the
  * caller, one caller-provided workspace, everything asynchronous on the
  * context's stream, HF_* codes.  Calls make no allocation and can be captured
@@ -498,10 +499,11 @@ int hf_vocab_loss(hf_vocab* ctx, const void* X, int64_t ldx, const void* W,
  * hf_vocab_loss_grad: hf_vocab_loss and its gradients
  *   dX = delta W (rows x D),  dW = delta^T X (V x D),
  *   delta = (softmax(z) - e_y) / denom.
- * Where the call's logits fit 1.5 GiB they are kept in the workspace, else
- * they are computed again a piece of the vocabulary at a time.  delta is
- * rounded to the type (bf16 calls of up to 128 rows: to two terms of it) for
- * the two products.
+ * The workspace keeps at most 1.5 GiB of logits (fp32; with bf16 exponentials
+ * in fp16): a call's whole ones, or a piece of the vocabulary's, the others
+ * being computed again piece by piece.  delta is rounded to the type (bf16
+ * calls of up to 128 rows, which keep fp32 logits whatever the vocabulary: to
+ * two terms of it) for the two products.
  *   dX, dW      either may be NULL (not both): not computed
  *   accumulate  1: dW += instead of dW = (with tied weights, or over
  *               minibatches); dX is always written whole

@@ -175,6 +175,14 @@ int check_mat(hf_vocab* c, const void* p, int64_t ld, int64_t cols, int es, int6
   return HF_OK;
 }
 
+// an output over an input, which is read after parts of the output are written
+int check_apart(hf_vocab* c, const void* in, const char* in_name, const void* out,
+                const char* out_name, int64_t rows) {
+  if (rows > 0 && out && in == out)
+    return fail(c, HF_EINVAL, "%s is %s: not in place", out_name, in_name);
+  return HF_OK;
+}
+
 // -------------------------------------------------------------- the passes
 int end(hf_vocab* c) {
   HIP_TRY(c, hipGetLastError());
@@ -463,6 +471,9 @@ int head_call(hf_vocab* c, const void* X, int64_t ldx, const void* W, int64_t ld
     if ((g->dX && (rc = check_mat(c, g->dX, g->lddx, c->D, c->es, T, "dX"))) ||
         (g->dW && (rc = check_mat(c, g->dW, g->lddw, c->D, c->es, c->V, "dW"))))
       return rc;
+    if ((rc = check_apart(c, X, "X", g->dX, "dX", T)) ||
+        (rc = check_apart(c, W, "W", g->dW, "dW", 1)))
+      return rc;
     if (g->accumulate != 0 && g->accumulate != 1)
       return fail(c, HF_EINVAL, "accumulate %d is neither 0 nor 1", g->accumulate);
   }
@@ -618,7 +629,8 @@ int hf_vocab_embed(hf_vocab* c, const void* E, int64_t lde, const int32_t* tok, 
   if ((rc = check_rows(c, rows)) ||
       (rc = check_mat(c, E, lde, c->D, c->es, c->V, "E")) ||
       (rc = check_mat(c, tok, 1, 1, 4, rows, "tok")) ||
-      (rc = check_mat(c, out, ldo, c->D, c->es, rows, "out")))
+      (rc = check_mat(c, out, ldo, c->D, c->es, rows, "out")) ||
+      (rc = check_apart(c, E, "E", out, "out", rows)))
     return rc;
   if (!std::isfinite(scale)) return fail(c, HF_EINVAL, "scale is not finite");
   if ((rc = check_ready(c, rows))) return rc;
@@ -635,7 +647,8 @@ int hf_vocab_embed_grad(hf_vocab* c, const int32_t* tok, int64_t rows, float sca
   if ((rc = check_rows(c, rows)) ||
       (rc = check_mat(c, tok, 1, 1, 4, rows, "tok")) ||
       (rc = check_mat(c, dout, ldd, c->D, c->es, rows, "dout")) ||
-      (rc = check_mat(c, dE, lde, c->D, c->es, c->V, "dE")))
+      (rc = check_mat(c, dE, lde, c->D, c->es, c->V, "dE")) ||
+      (rc = check_apart(c, dout, "dout", dE, "dE", rows)))
     return rc;
   if (!std::isfinite(scale)) return fail(c, HF_EINVAL, "scale is not finite");
   if (accumulate != 0 && accumulate != 1)

@@ -41,20 +41,28 @@ struct Strip {
   __device__ static __forceinline__ int col(int strip, int lane, int e) {
     return strip * COLS + (VEC ? lane * EPC + e : e * 64 + lane);
   }
-  __device__ static __forceinline__ void load(const E* row, int strip, int lane, int D,
-                                              float (&v)[EPC]) {
+  struct Raw {               // as loaded: 4 registers for a lane's columns
+    E v[EPC];
+  };
+  __device__ static __forceinline__ Raw raw(const E* row, int strip, int lane, int D) {
+    Raw w = {};
     if constexpr (VEC) {
-      E w[EPC] = {};
-      if (col(strip, lane, 0) < D) *(u32x4*)w = *(const u32x4*)(row + col(strip, lane, 0));
-#pragma unroll
-      for (int e = 0; e < EPC; ++e) v[e] = to_f(w[e]);
+      if (col(strip, lane, 0) < D)
+        w = __builtin_bit_cast(Raw, *(const u32x4*)(row + col(strip, lane, 0)));
     } else {
 #pragma unroll
       for (int e = 0; e < EPC; ++e) {
         const int c = col(strip, lane, e);
-        v[e] = c < D ? to_f(row[c]) : 0.0f;
+        if (c < D) w.v[e] = row[c];
       }
     }
+    return w;
+  }
+  __device__ static __forceinline__ void load(const E* row, int strip, int lane, int D,
+                                              float (&v)[EPC]) {
+    const Raw w = raw(row, strip, lane, D);
+#pragma unroll
+    for (int e = 0; e < EPC; ++e) v[e] = to_f(w.v[e]);
   }
   __device__ static __forceinline__ void store(E* row, int strip, int lane, int D,
                                                const float (&v)[EPC]) {
@@ -323,7 +331,9 @@ extern "C" __global__ __launch_bounds__(CHUNK) void hf_vocab_sort_one(
 
 // --------------------------------------------------------------- gradient
 namespace {
-constexpr int RUN = 32;      // sorted places per wave
+// Sorted places per run: 32, or 16 where that leaves compute units without a
+// wave (10,007 rows x 768 in fp32: 17 -> 12 us)
+constexpr int RUN_MIN = 16, RUN_MAX = 32;
 
 template <class E, bool VEC>
 __device__ __forceinline__ void emit(E* row, int strip, int lane, int D, float scale,
@@ -344,8 +354,8 @@ __device__ __forceinline__ void emit(E* row, int strip, int lane, int D, float s
 // run (or fills it from its start and goes on); part[2 run + 1]: of the one
 // that begins within it and goes on.
 template <class E, bool VEC>
-__device__ __forceinline__ void runs_body(const int* key, const int* pos, int T, int V, int D,
-                                          int strips, float scale, const E* dout,
+__device__ __forceinline__ void runs_body(const int* key, const int* pos, int RUN, int T, int V,
+                                          int D, int strips, float scale, const E* dout,
                                           long long ldd, float* part, E* dE, long long lde,
                                           int accumulate) {
   using S = Strip<E, VEC>;
@@ -362,19 +372,19 @@ __device__ __forceinline__ void runs_body(const int* key, const int* pos, int T,
   const int n = __popcll(__ballot(lane >= 1 && lane <= RUN && k >= 0 && k < V));
   float acc[S::EPC] = {};
   int head = n > 0 && __shfl(k, 1, 64) == __shfl(k, 0, 64);
-  constexpr int U = 8;
+  constexpr int U = 16;      // rows in flight
   for (int i0 = 0; i0 < n; i0 += U) {
-    float v[U][S::EPC];
+    typename S::Raw v[U];
 #pragma unroll
     for (int u = 0; u < U; ++u)
       if (i0 + u < n)
-        S::load(dout + (size_t)__builtin_amdgcn_readlane(p, 1 + i0 + u) * ldd, strip, lane, D,
-                v[u]);
+        v[u] = S::raw(dout + (size_t)__builtin_amdgcn_readlane(p, 1 + i0 + u) * ldd, strip, lane,
+                      D);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       if (i0 + u >= n) break;
 #pragma unroll
-      for (int e = 0; e < S::EPC; ++e) acc[e] += v[u][e];
+      for (int e = 0; e < S::EPC; ++e) acc[e] += to_f(v[u].v[e]);
       const int cur = __builtin_amdgcn_readlane(k, 1 + i0 + u);
       const int nxt = __builtin_amdgcn_readlane(k, 2 + i0 + u);
       const bool last = i0 + u + 1 == RUN;
@@ -401,7 +411,7 @@ __device__ __forceinline__ void runs_body(const int* key, const int* pos, int T,
 // few runs; tokens that span many are summed by the 4 waves together, a quarter
 // of the runs each, the quarters in order.
 template <class E, bool VEC>
-__device__ __forceinline__ void join_body(const int* key, int T, int V, int D, int strips,
+__device__ __forceinline__ void join_body(const int* key, int RUN, int T, int V, int D, int strips,
                                           float scale, const float* part, E* dE, long long lde,
                                           int accumulate) {
   using S = Strip<E, VEC>;
@@ -417,7 +427,7 @@ __device__ __forceinline__ void join_body(const int* key, int T, int V, int D, i
       const size_t slot = 2 * (size_t)x + (x == run);
       return part + (slot * strips + strip) * S::COLS + lane * S::EPC;
     };
-    constexpr int U = 16, Q = S::EPC / 4;
+    constexpr int U = 8, Q = S::EPC / 4;
     for (int x = x0; x < x1; x += U) {
       f32x4 w[U][Q];
 #pragma unroll
@@ -480,15 +490,16 @@ __device__ __forceinline__ void join_body(const int* key, int T, int V, int D, i
 
 #define HF_EMBED_GRAD(SUF, E, VEC)                                                       \
   extern "C" __global__ __launch_bounds__(256) void hf_vocab_embed_runs_##SUF(           \
-      const int* key, const int* pos, int T, int V, int D, int strips, float scale,      \
+      const int* key, const int* pos, int RUN, int T, int V, int D, int strips, float scale, \
       const E* dout, long long ldd, float* part, E* dE, long long lde, int accumulate) { \
-    runs_body<E, VEC>(key, pos, T, V, D, strips, scale, dout, ldd, part, dE, lde,        \
+    runs_body<E, VEC>(key, pos, RUN, T, V, D, strips, scale, dout, ldd, part, dE, lde,   \
                       accumulate);                                                       \
   }                                                                                      \
-  extern "C" __global__ __launch_bounds__(256) void hf_vocab_embed_join_##SUF(           \
-      const int* key, int T, int V, int D, int strips, float scale, const float* part,   \
+  extern "C" __global__ __launch_bounds__(256, 5) void hf_vocab_embed_join_##SUF(        \
+      const int* key, int RUN, int T, int V, int D, int strips, float scale,             \
+      const float* part,                                                                 \
       E* dE, long long lde, int accumulate) {                                            \
-    join_body<E, VEC>(key, T, V, D, strips, scale, part, dE, lde, accumulate);           \
+    join_body<E, VEC>(key, RUN, T, V, D, strips, scale, part, dE, lde, accumulate);      \
   }
 HF_EMBED_GRAD(f32, float, false)
 HF_EMBED_GRAD(f32_v, float, true)
@@ -526,7 +537,7 @@ size_t vocab_sort_hist(long long T, int V) {
 }
 size_t vocab_sort_part(long long T, int D, int type) {
   const int es = type == VT_F32 ? 4 : 2;
-  return 2 * (size_t)((T + RUN - 1) / RUN) * strips_of(D, es) * (1024 / es);
+  return 2 * (size_t)((T + RUN_MIN - 1) / RUN_MIN) * strips_of(D, es) * (1024 / es);
 }
 
 void vocab_embed(const Launch& L, int type, const void* E, long long lde, int V, int D,
@@ -579,18 +590,19 @@ void vocab_embed_grad(const Launch& L, int type, const int32_t* tok, int T, int 
               st);
   }
   if (T < 1) return;
+  const int RUN = (long long)((T + RUN_MAX - 1) / RUN_MAX) * strips < 2048 ? RUN_MIN : RUN_MAX;
   const int runs = (T + RUN - 1) / RUN;
   const long long units = (long long)runs * strips;
 #define HF_EG(SUF, E)                                                                         \
   do {                                                                                        \
     HF_LAUNCH("hf_vocab_embed_runs",                                                          \
               (vec ? hf_vocab_embed_runs_##SUF##_v : hf_vocab_embed_runs_##SUF),              \
-              (units + 3) / 4, 256, (const int*)s.key, (const int*)s.pos, T, V, D, strips,    \
+              (units + 3) / 4, 256, (const int*)s.key, (const int*)s.pos, RUN, T, V, D, strips, \
               scale, (const E*)dout, ldd, s.part, (E*)dE, lde, accumulate);                   \
     if (runs > 1)                                                                             \
       HF_LAUNCH("hf_vocab_embed_join",                                                        \
                 (vec ? hf_vocab_embed_join_##SUF##_v : hf_vocab_embed_join_##SUF),            \
-                dim3((runs + 3) / 4, strips), 256, (const int*)s.key, T, V, D, strips, scale, \
+                dim3((runs + 3) / 4, strips), 256, (const int*)s.key, RUN, T, V, D, strips, scale, \
                 (const float*)s.part, (E*)dE, lde, accumulate);                               \
   } while (0)
   if (type == VT_F32) HF_EG(f32, float);

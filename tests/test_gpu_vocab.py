@@ -179,10 +179,12 @@ def mask_rows(y, how, seed=5):
 
 
 # one row; sizes below, at and past tiles of 128 and 256, K blocks of 64 and
-# the 128 rows of the two-term form; odd widths and vocabularies
+# the 128 rows of the two-term form; odd widths and vocabularies; thousands of
+# statistics entries for few rows; enough tiles of 256 for every product
 SHAPES = [(1, 1, 1), (1, 1000, 64), (3, 7, 5), (64, 130, 64), (65, 129, 63), (127, 1000, 96),
           (128, 257, 128), (129, 1000, 96), (256, 256, 64), (300, 515, 200), (257, 2049, 321),
-          (1000, 513, 130), (2100, 300, 66)]
+          (1000, 513, 130), (2100, 300, 66), (100, 140000, 64), (2049, 8200, 512),
+          (4101, 4099, 1100)]
 
 
 @pytest.mark.parametrize("name", ["fp32", "bf16"])
@@ -263,7 +265,7 @@ def test_logits_in_pieces(name):
     vocabulary (with W packed, as its width is no multiple of 64, or not), for
     labels and lists."""
     torch = T()
-    for rows, V, D in ((8000, 50257, 72), (4097, 100003, 64)):
+    for rows, V, D in ((8000, 50257, 72), (4097, 100003, 64), (8000, 131075, 64)):
         X, W, y = head_inputs(name, rows, V, D)
         y = mask_rows(y, "some")
         net = H.HFVocab(V, D, rows, name)
@@ -431,8 +433,12 @@ def test_binding_refuses():
     with pytest.raises(H.HFError) as e:
         small.hf_vocab_loss(X.repeat(512, 1), W, y.repeat(512))
     assert e.value.code == H.HF_EWORKSPACE
+    for kw in (dict(need_dX=False, need_dW=False), dict(dX=X), dict(dW=W)):
+        with pytest.raises(H.HFError) as e:       # nothing to do, or in place
+            net.hf_vocab_loss_grad(X, W, y, **kw)
+        assert e.value.code == H.HF_EINVAL
     with pytest.raises(H.HFError):
-        net.hf_vocab_loss_grad(X, W, y, need_dX=False, need_dW=False)
+        net.hf_vocab_embed(W, y, out=W[:8])
 
 
 def test_gradient_against_differences():
@@ -479,7 +485,8 @@ def test_large_logits():
 
 
 @pytest.mark.parametrize("name", ["fp32", "bf16"])
-@pytest.mark.parametrize("rows,V,D", [(100, 1000, 128), (700, 1500, 200), (4200, 70000, 64)])
+@pytest.mark.parametrize("rows,V,D", [(100, 1000, 128), (700, 1500, 200), (4200, 70000, 64),
+                                      (8200, 131100, 64)])
 def test_same_bits(name, rows, V, D):
     """Repeated calls, another workspace, another stream."""
     torch = T()

@@ -10,6 +10,7 @@ from paper_1606_00511_amd import hf as H
 
 OK, EINVAL, EWS = H.HF_OK, H.HF_EINVAL, H.HF_EWORKSPACE
 FAKE = ctypes.c_void_p(1 << 20)          # never dereferenced
+FAKE2 = ctypes.c_void_p(1 << 30)
 
 
 @pytest.fixture(scope="module")
@@ -101,19 +102,20 @@ def test_workspace_refusals(L):
 NAN, INF = float("nan"), float("inf")
 LOSS = dict(X=FAKE, ldx=64, W=FAKE, ldw=64, y=FAKE, rows=4, denom=0.0, loss=FAKE,
             row_loss=FAKE)
-GRAD = dict(LOSS, dX=FAKE, lddx=64, dW=FAKE, lddw=64, accumulate=0)
+GRAD = dict(LOSS, dX=FAKE2, lddx=64, dW=FAKE2, lddw=64, accumulate=0)
 LIST = dict(X=FAKE, ldx=64, W=FAKE, ldw=64, ids=FAKE, ldi=8, t=FAKE, ldt=8, top=8, tau=1.0,
             rows=4, denom=0.0, loss=FAKE, row_loss=FAKE)
-LGRAD = dict(LIST, dX=FAKE, lddx=64, dW=FAKE, lddw=64, accumulate=0)
-EMBED = dict(E=FAKE, lde=64, tok=FAKE, rows=4, scale=1.0, out=FAKE, ldo=64)
-EGRAD = dict(tok=FAKE, rows=4, scale=1.0, dout=FAKE, ldd=64, dE=FAKE, lde=64, accumulate=0)
+LGRAD = dict(LIST, dX=FAKE2, lddx=64, dW=FAKE2, lddw=64, accumulate=0)
+EMBED = dict(E=FAKE, lde=64, tok=FAKE, rows=4, scale=1.0, out=FAKE2, ldo=64)
+EGRAD = dict(tok=FAKE, rows=4, scale=1.0, dout=FAKE, ldd=64, dE=FAKE2, lde=64, accumulate=0)
 ODD, ODD4 = ctypes.c_void_p((1 << 20) + 1), ctypes.c_void_p((1 << 20) + 2)
 HEAD_BAD = [dict(X=None), dict(X=ODD), dict(ldx=63), dict(ldx=(1 << 31) + 1), dict(W=None),
             dict(W=ODD), dict(ldw=10), dict(rows=-1), dict(rows=257), dict(denom=-1.0),
             dict(denom=NAN), dict(denom=INF), dict(loss=None), dict(loss=ODD4),
             dict(row_loss=ODD4)]
 GRAD_BAD = HEAD_BAD + [dict(dX=None, dW=None), dict(dX=ODD), dict(lddx=63), dict(dW=ODD),
-                       dict(lddw=63), dict(accumulate=2), dict(accumulate=-1)]
+                       dict(lddw=63), dict(accumulate=2), dict(accumulate=-1),
+                       dict(dX=FAKE), dict(dW=FAKE)]          # over X, over W
 LIST_BAD = [dict(ids=None), dict(ids=ODD4), dict(ldi=7), dict(t=None), dict(t=ODD4),
             dict(ldt=7), dict(top=0), dict(top=-1), dict(top=129, ldi=200, ldt=200),
             dict(tau=0.0), dict(tau=-1.0), dict(tau=NAN), dict(tau=INF), dict(tau=1e-5),
@@ -125,11 +127,12 @@ CALLS = [
     ("hf_vocab_distill_grad", LGRAD, GRAD_BAD + LIST_BAD),
     ("hf_vocab_embed", EMBED, [dict(E=None), dict(E=ODD), dict(lde=63), dict(tok=None),
                                dict(tok=ODD4), dict(rows=-1), dict(rows=257), dict(scale=NAN),
-                               dict(scale=INF), dict(out=None), dict(out=ODD), dict(ldo=63)]),
+                               dict(scale=INF), dict(out=None), dict(out=ODD), dict(ldo=63),
+                               dict(out=FAKE)]),
     ("hf_vocab_embed_grad", EGRAD, [dict(tok=None), dict(rows=-1), dict(rows=257),
                                     dict(scale=NAN), dict(dout=None), dict(dout=ODD),
                                     dict(ldd=63), dict(dE=None), dict(dE=ODD), dict(lde=63),
-                                    dict(accumulate=3)]),
+                                    dict(accumulate=3), dict(dE=FAKE)]),
 ]
 
 

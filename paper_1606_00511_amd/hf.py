@@ -489,6 +489,7 @@ class HFVocab:
     def __init__(self, vocab, width, max_rows, dtype="fp32", device="cuda",
                  ws_rows=None):
         import torch
+        self._torch = torch
         self.vocab, self.width = int(vocab), int(width)
         self.max_rows = int(max_rows)
         self.dtype = {"fp32": torch.float32, "bf16": torch.bfloat16}[dtype]
@@ -520,12 +521,11 @@ class HFVocab:
         return rc
 
     def _call(self, fn, *args):
-        import torch
-        if torch.cuda.current_device() != self.device.index:
-            with torch.cuda.device(self.device):
+        cuda, L = self._torch.cuda, lib()
+        if cuda.current_device() != self.device.index:
+            with cuda.device(self.device):
                 return self._call(fn, *args)
-        L = lib()
-        stream = torch.cuda.current_stream(self.device.index).cuda_stream
+        stream = cuda.current_stream(self.device.index).cuda_stream
         if stream != self._stream:
             self._check(L.hf_vocab_set_stream(self._h, stream))
             self._stream = stream
@@ -544,23 +544,24 @@ class HFVocab:
 
     def _mat(self, t, rows, cols, dtype, what):
         """(pointer, elements between rows) of a rows x cols tensor."""
-        import torch
-        if not isinstance(t, torch.Tensor) or t.device != self.device:
+        if not isinstance(t, self._torch.Tensor) or t.device != self.device:
             raise TypeError("%s must be a tensor on %s" % (what, self.device))
         if t.dtype != dtype:
             raise TypeError("%s must be %s, got %s" % (what, dtype, t.dtype))
-        if tuple(t.shape) != (rows, cols):
+        if t.shape != (rows, cols):
             raise ValueError("%s is %s, expected %d x %d"
                              % (what, tuple(t.shape), rows, cols))
-        if cols > 1 and t.stride(1) != 1:
+        ld, one = t.stride()
+        if cols > 1 and one != 1:
             raise ValueError("the rows of %s must be contiguous" % what)
-        if rows > 1 and t.stride(0) < cols:
+        if rows <= 1:
+            ld = cols
+        elif ld < cols:
             raise ValueError("the rows of %s overlap" % what)
-        return t.data_ptr(), (t.stride(0) if rows > 1 else cols)
+        return t.data_ptr(), ld
 
     def _vec(self, t, n, dtype, what):
-        import torch
-        if not isinstance(t, torch.Tensor) or t.device != self.device:
+        if not isinstance(t, self._torch.Tensor) or t.device != self.device:
             raise TypeError("%s must be a tensor on %s" % (what, self.device))
         if t.dtype != dtype:
             raise TypeError("%s must be %s, got %s" % (what, dtype, t.dtype))
@@ -574,13 +575,11 @@ class HFVocab:
         return int(X.shape[0])
 
     def _out(self, *shape, dtype=None):
-        import torch
-        return torch.empty(*shape, dtype=dtype or self.dtype, device=self.device)
+        return self._torch.empty(*shape, dtype=dtype or self.dtype, device=self.device)
 
     def _head(self, fn, X, W, targets, T, denom, loss, row_loss, grad):
         """A head call: targets and their arguments as the C call takes them."""
-        import torch
-        f32 = torch.float32
+        f32 = self._torch.float32
         xp, ldx = self._mat(X, T, self.width, self.dtype, "X")
         wp, ldw = self._mat(W, self.vocab, self.width, self.dtype, "W")
         loss = self._out(1, dtype=f32) if loss is None else loss
@@ -604,7 +603,7 @@ class HFVocab:
         return loss, row_loss, dX, dW
 
     def _list(self, ids, t, T, tau):
-        import torch
+        torch = self._torch
         if ids.dim() != 2:
             raise ValueError("ids must be rows x top")
         K = int(ids.shape[1])
@@ -615,9 +614,9 @@ class HFVocab:
     # -------------------------------------------------------------- the ABI
     def hf_vocab_loss(self, X, W, y, denom=0.0, loss=None, row_loss=None):
         """Softmax cross entropy of X W^T: (loss, row losses)."""
-        import torch
         T = self._rows(X, "X")
-        return self._head("hf_vocab_loss", X, W, [self._vec(y, T, torch.int32, "y")], T,
+        y = self._vec(y, T, self._torch.int32, "y")
+        return self._head("hf_vocab_loss", X, W, [y], T,
                           denom, loss, row_loss, None)
 
     def hf_vocab_loss_grad(self, X, W, y, denom=0.0, loss=None, row_loss=None, dX=None,
@@ -625,10 +624,10 @@ class HFVocab:
         """hf_vocab_loss and its gradients: (loss, row losses, dX, dW).
         need_dX / need_dW False: that gradient is not computed (None).
         accumulate: dW += (dW given)."""
-        import torch
         T = self._rows(X, "X")
-        return self._head("hf_vocab_loss_grad", X, W, [self._vec(y, T, torch.int32, "y")],
-                          T, denom, loss, row_loss, (dX, dW, need_dX, need_dW, accumulate))
+        y = self._vec(y, T, self._torch.int32, "y")
+        return self._head("hf_vocab_loss_grad", X, W, [y], T, denom, loss, row_loss,
+                          (dX, dW, need_dX, need_dW, accumulate))
 
     def hf_vocab_distill(self, X, W, ids, t, tau=1.0, denom=0.0, loss=None,
                          row_loss=None):
@@ -648,26 +647,24 @@ class HFVocab:
 
     def hf_vocab_embed(self, E, tok, scale=1.0, out=None):
         """scale E[tok], zeros where tok is HF_IGNORE."""
-        import torch
-        T = int(tok.numel())
+        T = tok.numel()
         out = self._out(T, self.width) if out is None else out
         ep, lde = self._mat(E, self.vocab, self.width, self.dtype, "E")
         op, ldo = self._mat(out, T, self.width, self.dtype, "out")
-        self._call("hf_vocab_embed", ep, lde, self._vec(tok, T, torch.int32, "tok"), T,
-                   float(scale), op, ldo)
+        self._call("hf_vocab_embed", ep, lde, self._vec(tok, T, self._torch.int32, "tok"),
+                   T, float(scale), op, ldo)
         return out
 
     def hf_vocab_embed_grad(self, tok, dout, scale=1.0, dE=None, accumulate=False):
         """Gradient of hf_vocab_embed with respect to E; accumulate: dE +=
         (dE given)."""
-        import torch
         T = self._rows(dout, "dout")
         if accumulate and dE is None:
             raise ValueError("accumulate needs the dE to add to")
         dE = self._out(self.vocab, self.width) if dE is None else dE
         dp, ldd = self._mat(dout, T, self.width, self.dtype, "dout")
         ep, lde = self._mat(dE, self.vocab, self.width, self.dtype, "dE")
-        self._call("hf_vocab_embed_grad", self._vec(tok, T, torch.int32, "tok"), T,
+        self._call("hf_vocab_embed_grad", self._vec(tok, T, self._torch.int32, "tok"), T,
                    float(scale), dp, ldd, ep, lde, 1 if accumulate else 0)
         return dE
 

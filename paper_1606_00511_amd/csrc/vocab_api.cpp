@@ -30,6 +30,7 @@ constexpr size_t KEEP_BYTES = 1536 * MiB;    // kept logits
 constexpr size_t WPACK_BYTES = 256 * MiB;    // packed rows of W
 constexpr int64_t MAX_LD = (int64_t)1 << 22; // in-tile offsets are 32 bits
 constexpr int TWO_TERM_ROWS = 128;
+constexpr int FEW_ROWS = 192;                // tiles of 32 and 64 rows up to here
 constexpr size_t SPLIT_FLOATS = (size_t)32 << 20;   // partials of a split-K product
 
 inline int64_t up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
@@ -125,7 +126,9 @@ void plan(const hf_vocab* c, int64_t R, Layout* l) {
   l->zt = take(r * HF_VOCAB_MAX_TOP * 4);
   l->tid = take(r * HF_VOCAB_MAX_TOP * 4);
   l->tdt = take(r * HF_VOCAB_MAX_TOP * 4);
-  l->stat = take(r * (size_t)((c->V + VSTAT - 1) / VSTAT + 8) * sizeof(float2));
+  // (few rows: entries of 32 columns, else of 64 or 128)
+  l->stat = take(std::max(std::min<size_t>(r, FEW_ROWS) * (size_t)(c->V / 32 + 8),
+                          r * (size_t)(c->V / 64 + 8)) * sizeof(float2));
   l->xp = take(Rp * c->Dp * c->es);
   l->wp = take((size_t)pack_rows(c) * c->Dp * c->es);
   // what the largest of up to R rows needs: few rows, kept logits, pieces
@@ -191,33 +194,39 @@ int end(hf_vocab* c) {
 }
 
 // Tiles and split-K factor of a product by its estimated time, in us.  One 256
-// x 256 tile has a compute unit to itself, two of 128 x 128 share one; per
-// unit the former do 2.4e6 (bf16) or 0.27e6 (fp32) multiply-adds a us, the
-// latter 0.74 and 0.90 of that (8,192 x 32,768 x 4,096 in bf16: 1,680 and
-// 2,370 us; 16,384 x 2,048 x 2,048 in fp32: 975 and 1,090).  Filling the LDS
-// and storing the tile take about 6 and 4 us beside that, and partials are
-// written and read again at 4 bytes each, 4,700 bytes a ns on the whole card.
+// x 256 tile has a compute unit to itself, two of the others share one; RATE:
+// multiply-adds a us of a unit with them, measured at 8,192 x 8,192 x 2,048
+// (bf16) and 8,192 x 2,048 x 2,048 (fp32).  Filling the LDS and storing a tile
+// take about 6 and 4 us beside that; A's tiles cannot be read faster than 4.7
+// TB/s once (and B's follow from L2); partials are written and read again.
 struct Shape {
-  int big, splits;
+  int tile, splits;
 };
-Shape shape_for(int type, int64_t M, int64_t N, int64_t K, bool split) {
+constexpr double RATE[2][4] = {{0.24e6, 0.27e6, 0.22e6, 0.21e6}, {1.78e6, 2.4e6, 1.45e6, 1.1e6}};
+constexpr double BYTES_US = 4.7e6;
+Shape shape_for(int type, int64_t M, int64_t N, int64_t K, bool split, bool few) {
   Shape best = {0, 1};
   double least = 1e300;
-  for (int big = 0; big < 2; ++big) {
-    const int64_t R = big ? 256 : 128, tiles = ((M + R - 1) / R) * ((N + R - 1) / R);
-    const double rate = (type == VT_F32 ? 0.27e6 * (big ? 1.0 : 0.90)
-                                        : 2.4e6 * (big ? 1.0 : 0.74)) / (big ? 1.0 : 2.0);
+  const int es = type == VT_F32 ? 4 : 2;
+  for (int tile = 0; tile < (few && N <= FEW_ROWS ? 4 : 2); ++tile) {
+    const int64_t RM = tile_m(tile), RN = tile_n(tile);
+    const int64_t tiles = ((M + RM - 1) / RM) * ((N + RN - 1) / RN);
+    const int64_t slots = tile == TILE_BIG ? 256 : 512;
     for (int s = 1; s <= VMAX_SPLITS; ++s) {
       if (s > 1 && (!split || K / s < 256 ||
                     (size_t)s * up(N, 128) * up(M, VPAD) > SPLIT_FLOATS))
         break;
-      const int64_t rounds = (tiles * s + (big ? 256 : 512) - 1) / (big ? 256 : 512);
-      const double t = rounds * ((double)R * R * (double)((K + s - 1) / s) / rate +
-                                 (big ? 6.0 : 4.0)) +
-                       (s > 1 ? 5.0 + 8.0 * s * (double)M * N / 4.7e6 : 0.0);
-      if (t < least) {
-        least = t;
-        best = {big, s};
+      const int64_t rounds = (tiles * s + slots - 1) / slots;
+      // the workgroups of a unit share it; one alone does not fill it
+      const double share = tile == TILE_BIG ? 1.0 : tiles * s > 256 ? 2.0 : 1.4;
+      const double t = rounds * (share * RM * RN * (double)((K + s - 1) / s) /
+                                     RATE[type][tile] + (tile == TILE_BIG ? 6.0 : 4.0));
+      const double mem = (double)M * K * es / BYTES_US + 4.0;
+      const double est =
+          std::max(t, mem) + (s > 1 ? 5.0 + 8.0 * s * (double)M * N / BYTES_US : 0.0);
+      if (est < least) {
+        least = est;
+        best = {tile, s};
       }
     }
   }
@@ -288,14 +297,14 @@ void head(hf_vocab* c, VRows r, const void* X, int64_t ldx, const void* W, int64
   float* z = g && !f16 ? c->at<float>(l.z) : nullptr;
   void* d = !g ? nullptr : dup ? (void*)(z + (size_t)Rp * ldd) : c->at<void>(l.z);
   const int sstep = std::min(wrows, vc);
-  const int big = shape_for(type, g ? sstep : wrows, T, Dp, false).big;
-  const int sg = big ? VSTAT_BIG : VSTAT;
+  const int tile = shape_for(type, g ? sstep : wrows, T, Dp, false, !(g && f16)).tile;
+  const int sg = tile_stat(tile);
   const int tiles = (V + sg - 1) / sg;
   VEpi e = {};
   e.zscale = 1.0f / r.tau;
   e.stat = stat;
   e.ldstat = tiles;
-  auto logits = [&](int v0, int n, bool kept) {
+  auto logits = [&](int v0, int n, bool keep_it) {
     VGemm q = {};
     q.A = matrix(v0, n, &q.lda);
     q.B = xp;
@@ -310,15 +319,16 @@ void head(hf_vocab* c, VRows r, const void* X, int64_t ldx, const void* W, int64
     q.T = T;
     q.dyn = 1;
     q.splits = 1;
-    q.big = big;
+    q.tile = tile;
     e.tile0 = v0 / sg;
-    e.z = kept && z ? z + v0 : nullptr;
-    e.pt = kept && f16 ? (char*)d + (size_t)v0 * 2 : nullptr;
+    e.z = keep_it && z ? z + v0 : nullptr;
+    e.pt = keep_it && f16 ? (char*)d + (size_t)v0 * 2 : nullptr;
     e.ldz = ldd;
     vocab_logits(L, type, q, e);
   };
   for (int v0 = g ? vc : 0; v0 < V; v0 += wrows) logits(v0, std::min(wrows, V - v0), false);
-  for (int v0 = 0; g && v0 < vc; v0 += wrows) logits(v0, std::min(wrows, std::min(vc, V) - v0), true);
+  const int kept = g ? std::min(vc, V) : 0;
+  for (int v0 = 0; v0 < kept; v0 += wrows) logits(v0, std::min(wrows, kept - v0), true);
 
   // ---- losses
   VTarget tg = {c->at<float>(l.zt), nullptr, nullptr};
@@ -328,12 +338,14 @@ void head(hf_vocab* c, VRows r, const void* X, int64_t ldx, const void* W, int64
   }
   const bool self = dup > 0;             // few rows: with delta
   const bool dots = !keep || f16;
-  if (dots && T > 0) vocab_target_logits(L, type, r, xd, ldx, xp, Dp, W, ldw, tg.zt);
-  if (!self) vocab_row_loss(L, r, stat, tiles, tiles, dots ? nullptr : z, ldd, tg, lse);
+  bool summed = false;
+  if (!self)
+    summed = vocab_row_loss(L, type, r, stat, tiles, tiles, dots ? nullptr : z, ldd, tg, lse, xd,
+                            ldx, xp, Dp, W, ldw, loss);
   if (g && T > 0)
     vocab_delta(L, type, r, z, ldd, stat, tiles, sg, lse, tg, 0, std::min(vc, V),
-                dup ? dup : (int)up(T, VPAD), self, d, ldd, dup, self ? nullptr : loss);
-  if (!g || T < 1 || (self && !g->dX)) vocab_loss_sum(L, r, loss);
+                dup ? dup : (int)up(T, VPAD), self, d, ldd, dup, self || summed ? nullptr : loss);
+  if (!summed && (!g || T < 1 || (self && !g->dX))) vocab_loss_sum(L, r, loss);
   if (!g) return;
 
   // ---- gradients, piece by piece
@@ -368,7 +380,7 @@ void head(hf_vocab* c, VRows r, const void* X, int64_t ldx, const void* W, int64
         q.T = T;
         q.dyn = 1;
         q.splits = 1;
-        q.big = shape_for(type, n, T, Dp, false).big;
+        q.tile = shape_for(type, n, T, Dp, false, false).tile;
         VEpi pe = {};
         pe.zscale = 1.0f / r.tau;
         pe.lse = lse;
@@ -390,13 +402,13 @@ void head(hf_vocab* c, VRows r, const void* X, int64_t ldx, const void* W, int64
       q.st = r.st;
       q.dyn = dup ? 0 : 1;
       if (v0 == 0) {
-        xs = shape_for(type, D, xrows, n, true);
+        xs = shape_for(type, D, xrows, n, true, true);
         xstride = up(xrows, 128) * Dp;
         // one piece and no splits: straight into dX
-        finish = n < V || xs.splits > 1 || dup;
+        finish = n < V || xs.splits > 1 || dup || xs.tile >= TILE_N64;
       }
       q.splits = xs.splits;
-      q.big = xs.big;
+      q.tile = xs.tile;
       VEpi pe = {};
       pe.part = partx;
       pe.ldp = Dp;
@@ -425,10 +437,9 @@ void head(hf_vocab* c, VRows r, const void* X, int64_t ldx, const void* W, int64
     q.X = xd;
     q.ldx = ldx;
     q.T = T;
-    // few bf16 rows: tiles of 128 (hf_vocab_dw_bf16_thin)
-    const Shape ws = type == VT_BF16 && q.K <= 256 ? Shape{0, 1}
-                                                   : shape_for(type, D, pn, q.K, true);
-    q.big = ws.big;
+    q.thin = q.K <= (type == VT_F32 ? 64 : 256) && (int64_t)pn * D >= (1 << 20);
+    const Shape ws = q.thin ? Shape{TILE_SMALL, 1} : shape_for(type, D, pn, q.K, true, false);
+    q.tile = ws.tile;
     q.splits = ws.splits;
     VEpi pe = {};
     char* out = (char*)g->dW + (size_t)p0 * g->lddw * es;

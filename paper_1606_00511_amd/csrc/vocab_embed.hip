@@ -571,7 +571,8 @@ void vocab_embed_grad(const Launch& L, int type, const int32_t* tok, int T, int 
     return f;
   };
   // workgroups that fill: two per compute unit, or fewer for little
-  const int fills = accumulate ? 0 : (int)std::min<long long>(512, ((long long)V * all.bytes >> 16) + 1);
+  const int fills =
+      accumulate ? 0 : (int)std::min<long long>(512, ((long long)V * all.bytes >> 16) + 1);
   if (T <= CHUNK) {
     if (T > 0 || fills)
       HF_LAUNCH("hf_vocab_sort", hf_vocab_sort_one, 1 + fills, CHUNK, tok, T, V, bits, s.key,

@@ -73,7 +73,7 @@ struct Tile {
   static constexpr int SIZE = ROWS * BK;
   static constexpr int INSTR = SIZE / EPC / 64 / NW;
   static_assert(SIZE % (EPC * 64 * NW) == 0, "tile does not split over the waves");
-  static_assert(BK * sizeof(E) <= 128 && ROWS * sizeof(E) >= 256, "swizzles");
+  static_assert(BK * sizeof(E) <= 128 && (KC || ROWS * sizeof(E) >= 256), "swizzles");
 
   __device__ static __forceinline__ int swz(int r) {
     if (KC) return (r / (256 / (BK * (int)sizeof(E)))) % CH;
@@ -266,7 +266,7 @@ __device__ __forceinline__ void vgemm_body(const VGemm& s, const VEpi& e) {
   const int m0 = tm * RM, n0 = tn * RN;
   const int nrow = s.st->n;
   const int N = s.dyn == 1 ? nrow : s.N;
-  const int K = s.dyn == 2 ? (nrow + VPAD - 1) & ~(VPAD - 1) : s.K;
+  const int K = s.dyn == 2 ? (nrow + BK - 1) & ~(BK - 1) : s.K;
   if (n0 >= N) return;
   // rows that all count are read where they are, not packed
   const bool whole = s.X && nrow == s.T;
@@ -353,8 +353,11 @@ __device__ __forceinline__ void vgemm_body(const VGemm& s, const VEpi& e) {
 #pragma unroll
     for (int i = 0; i < NF; ++i) fetch1(f, st, q, i);
   };
-  // the MFMAs of a step; side(i) after the i-th
+  // the MFMAs of a step; side(i) after the i-th of them, which issues its share
+  // of the next step's fragment reads (FT) and direct loads (AT)
   constexpr int NJ = (int)sizeof(E) * (int)sizeof(E) / 4, NM = NJ * WM * WN;
+  constexpr int FT = (NF + NM - 1) / NM, AT = (LPB + NM - 1) / NM;
+  constexpr int PER = NM / LPB > 0 ? NM / LPB : 1;      // MFMAs per direct load
   auto mma = [&](const Frags& f, auto side) {
 #pragma unroll
     for (int j = 0; j < NJ; ++j)
@@ -386,7 +389,9 @@ __device__ __forceinline__ void vgemm_body(const VGemm& s, const VEpi& e) {
     for (int q = 0; q + 1 < NQ; ++q) {
       Frags& nx = (q & 1) ? fa : fb;
       mma((q & 1) ? fb : fa, [&](int i) {
-        if (i < NF) fetch1(nx, st, q + 1, i);
+#pragma unroll
+        for (int x = 0; x < FT; ++x)
+          if (i * FT + x < NF) fetch1(nx, st, q + 1, i * FT + x);
       });
     }
     // this wave's loads of block it + 1 have landed once at most
@@ -398,11 +403,13 @@ __device__ __forceinline__ void vgemm_body(const VGemm& s, const VEpi& e) {
     const int vb = vb0 + it + S;
     mma(fb, [&](int i) {
       // (past the last block: a read of a stage that nobody writes, unused)
-      if (i < NF) fetch1(fa, (it + 1) % S, 0, i);
-      constexpr int PER = NM / LPB > 0 ? NM / LPB : 1, AT = NM >= LPB ? 1 : LPB / NM;
+#pragma unroll
+      for (int x = 0; x < FT; ++x)
+        if (i * FT + x < NF) fetch1(fa, (it + 1) % S, 0, i * FT + x);
       if (i % PER == 0 && i / PER * AT < LPB && more) {
 #pragma unroll
-        for (int x = 0; x < AT; ++x) issue1(vb, st, i / PER * AT + x);
+        for (int x = 0; x < AT; ++x)
+          if (i / PER * AT + x < LPB) issue1(vb, st, i / PER * AT + x);
       }
     });
   }
@@ -520,6 +527,23 @@ __device__ __forceinline__ void vgemm_body(const VGemm& s, const VEpi& e) {
   extern "C" __global__ __launch_bounds__(256, 2) void NAME##_f32(VGemm s, VEpi e) {   \
     vgemm_body<float, EPI, AKC, BKC, 2, 2, 2, 2, 2, 128>(s, e);                        \
   }
+// few rows of X: 128 x 64 and 128 x 32 tiles, a wave having 32 of W's rows, with
+// three K blocks of W on their way; bound by the reads of W
+#define HF_VGEMM_FEW(NAME, EPI, AKC, BKC)                                              \
+  extern "C" __global__ __launch_bounds__(256, 2) void NAME##_bf16_n64(VGemm s, VEpi e) { \
+    vgemm_body<bf16_t, EPI, AKC, BKC, 1, 2, 4, 1, 3, 128>(s, e);                       \
+  }                                                                                    \
+  extern "C" __global__ __launch_bounds__(256, 2) void NAME##_bf16_n32(VGemm s, VEpi e) { \
+    vgemm_body<bf16_t, EPI, AKC, BKC, 1, 1, 4, 1, 4, 128>(s, e);                       \
+  }                                                                                    \
+  extern "C" __global__ __launch_bounds__(256, 2) void NAME##_f32_n64(VGemm s, VEpi e) {  \
+    vgemm_body<float, EPI, AKC, BKC, 1, 2, 4, 1, 3, 128>(s, e);                        \
+  }                                                                                    \
+  extern "C" __global__ __launch_bounds__(256, 2) void NAME##_f32_n32(VGemm s, VEpi e) {  \
+    vgemm_body<float, EPI, AKC, BKC, 1, 1, 4, 1, 4, 128>(s, e);                        \
+  }
+HF_VGEMM_FEW(hf_vocab_logits, E_LOGITS, true, true)
+HF_VGEMM_FEW(hf_vocab_dx, E_PART, false, true)
 HF_VGEMM(hf_vocab_logits, E_LOGITS, true, true)
 extern "C" __global__ __launch_bounds__(512, 1) void hf_vocab_exps_bf16_big(VGemm s, VEpi e) {
   vgemm_body<bf16_t, E_EXPS, true, true, 4, 2, 2, 4, 2, 128>(s, e);
@@ -538,41 +562,48 @@ HF_VGEMM(hf_vocab_dw_part, E_PART, false, false)
 extern "C" __global__ __launch_bounds__(256, 3) void hf_vocab_dw_bf16_thin(VGemm s, VEpi e) {
   vgemm_body<bf16_t, E_OUT, false, false, 2, 2, 2, 2, 2, 64>(s, e);
 }
+extern "C" __global__ __launch_bounds__(256, 3) void hf_vocab_dw_f32_thin(VGemm s, VEpi e) {
+  vgemm_body<float, E_OUT, false, false, 2, 2, 2, 2, 2, 64>(s, e);
+}
 
 // ------------------------------------------------------------- launchers
 namespace {
 typedef void (*VK)(VGemm, VEpi);
-void launch(const Launch& L, const char* name, const VK (&k)[2][2], int type, const VGemm& g,
+// kernels of a product by type and tile (VT_* of VGemm::tile)
+typedef VK Kernels[2][4];
+void launch(const Launch& L, const char* name, const Kernels& k, int type, const VGemm& g,
             const VEpi& e) {
   if (g.M < 1 || g.N < 1) return;
-  const int R = g.big ? 256 : 128;
-  const dim3 grid((g.M + R - 1) / R, (g.N + R - 1) / R, g.splits);
+  const int RM = tile_m(g.tile), RN = tile_n(g.tile);
+  const dim3 grid((g.M + RM - 1) / RM, (g.N + RN - 1) / RN, g.splits);
   prof_begin(L, name);
-  hipExtLaunchKernelGGL(k[type][g.big], grid, dim3(g.big ? 512 : 256), 0, L.stream,
+  hipExtLaunchKernelGGL(k[type][g.tile], grid, dim3(g.tile == TILE_BIG ? 512 : 256), 0, L.stream,
                         prof_a(L), prof_b(L), 0, g, e);
   prof_end(L, name, 2.0 * g.M * (double)g.N * g.K, 0.0);
 }
 }  // namespace
 
 #define HF_VK(NAME) {{NAME##_f32, NAME##_f32_big}, {NAME##_bf16, NAME##_bf16_big}}
+#define HF_VK_FEW(NAME)                                               \
+  {{NAME##_f32, NAME##_f32_big, NAME##_f32_n64, NAME##_f32_n32},      \
+   {NAME##_bf16, NAME##_bf16_big, NAME##_bf16_n64, NAME##_bf16_n32}}
 void vocab_logits(const Launch& L, int type, const VGemm& g, const VEpi& e) {
-  static const VK k[2][2] = HF_VK(hf_vocab_logits);
-  static const VK x[2][2] = {{nullptr, nullptr}, {hf_vocab_exps_bf16, hf_vocab_exps_bf16_big}};
+  static const Kernels k = HF_VK_FEW(hf_vocab_logits);
+  static const Kernels x = {{}, {hf_vocab_exps_bf16, hf_vocab_exps_bf16_big}};
   launch(L, "hf_vocab_logits", e.pt ? x : k, type, g, e);
 }
 void vocab_probs(const Launch& L, int type, const VGemm& g, const VEpi& e) {
-  static const VK k[2][2] = HF_VK(hf_vocab_probs);
+  static const Kernels k = HF_VK(hf_vocab_probs);
   launch(L, "hf_vocab_probs", k, type, g, e);
 }
 void vocab_dx(const Launch& L, int type, const VGemm& g, const VEpi& e) {
-  static const VK k[2][2] = HF_VK(hf_vocab_dx), o[2][2] = HF_VK(hf_vocab_dx_out);
+  static const Kernels k = HF_VK_FEW(hf_vocab_dx), o = HF_VK(hf_vocab_dx_out);
   launch(L, "hf_vocab_dx", e.out ? o : k, type, g, e);
 }
 void vocab_dw(const Launch& L, int type, const VGemm& g, const VEpi& e) {
-  static const VK k[2][2] = HF_VK(hf_vocab_dw), p[2][2] = HF_VK(hf_vocab_dw_part);
-  static const VK thin[2][2] = {{hf_vocab_dw_f32, hf_vocab_dw_f32_big},
-                                {hf_vocab_dw_bf16_thin, hf_vocab_dw_bf16_big}};
-  launch(L, "hf_vocab_dw", g.splits > 1 ? p : g.K <= 256 ? thin : k, type, g, e);
+  static const Kernels k = HF_VK(hf_vocab_dw), p = HF_VK(hf_vocab_dw_part);
+  static const Kernels thin = {{hf_vocab_dw_f32_thin}, {hf_vocab_dw_bf16_thin}};
+  launch(L, "hf_vocab_dw", g.splits > 1 ? p : g.thin ? thin : k, type, g, e);
 }
 
 }  // namespace hfk

@@ -15,8 +15,14 @@ enum VType { VT_F32 = 0, VT_BF16 = 1 };
 constexpr int VPAD = 64;
 // Rows of packed operands come in whole tiles of this many.
 constexpr int VTILE = 256;
+// Output tiles of the GEMMs (m x n): 128 x 128, 256 x 256, 128 x 64, 128 x 32.
+enum { TILE_SMALL, TILE_BIG, TILE_N64, TILE_N32 };
+inline int tile_m(int t) { return t == TILE_BIG ? 256 : 128; }
+inline int tile_n(int t) {
+  return t == TILE_BIG ? 256 : t == TILE_N64 ? 64 : t == TILE_N32 ? 32 : 128;
+}
 // Columns of one entry of row statistics: a wave's part of a vocabulary tile.
-constexpr int VSTAT = 64, VSTAT_BIG = 128;
+inline int tile_stat(int t) { return t == TILE_BIG ? 128 : t == TILE_SMALL ? 64 : 32; }
 constexpr int VMAX_SPLITS = 64;
 
 // Device scalars of a call.
@@ -38,9 +44,10 @@ struct VGemm {
   const void* X;   // the rows of X (what is packed), if they can be read in
   long long ldx;   // place: used where all T of them count; else null
   int T;
-  int dyn;         // 1: N is st->n; 2: K is st->n rounded up to VPAD
+  int dyn;         // 1: N is st->n; 2: K is st->n, rounded up to K blocks
   int splits;      // split-K factor (partials), grid z
-  int big;         // 256 x 256 tiles rather than 128 x 128
+  int tile;
+  int thin;        // dW of few rows (TILE_SMALL, splits 1)
 };
 
 struct VEpi {
@@ -110,15 +117,13 @@ struct VTarget {
   int* id;                  // packed row x K: target id, -1: none (or a repeat)
   float* dt;                // packed row x K: delta at the target
 };
-// zt of the targets by their own products (logits not kept)
-void vocab_target_logits(const Launch& L, int type, const VRows& r, const void* X,
-                         long long ldx, const void* xp, int Dp, const void* W,
-                         long long ldw, float* zt);
 // log-sum-exp from the statistics, the rows' losses and the targets' delta;
-// z: kept logits or null (then t.zt holds the targets')
-void vocab_row_loss(const Launch& L, const VRows& r, const float2* stat, int ldstat,
-                    int tiles, const float* z, long long ldz, const VTarget& t,
-                    float* lse);
+// z: kept logits or null (then the targets' are formed of X or xp and W).
+// True: the loss is summed too.
+bool vocab_row_loss(const Launch& L, int type, const VRows& r, const float2* stat, int ldstat,
+                    int tiles, const float* z, long long ldz, const VTarget& t, float* lse,
+                    const void* X, long long ldx, const void* xp, int Dp, const void* W,
+                    long long ldw, float* loss);
 // loss = sum of the counted rows' losses / denom
 void vocab_loss_sum(const Launch& L, const VRows& r, float* loss);
 // delta from kept logits of the columns [v0, v0 + Vc), targets included (dup:

@@ -259,74 +259,84 @@ extern "C" __global__ __launch_bounds__(256) void hf_vocab_copy_bf16(
 }
 
 // ---------------------------------------------------- the targets' logits
-// Where the logits are not kept in fp32: the K products x_j . W[id] of a packed
+// Where the logits are not kept in fp32: the products x_j . W[id] of a packed
 // row, U of them at a time per wave.  Bound by the reads of W's rows.
 namespace {
+// what they are formed of; X: the rows in place where all count, or null
+struct VDots {
+  const void *X, *xp, *W;
+  long long ldx, ldw;
+  int Dp, vec;
+};
+template <class E, int U>
+__device__ __forceinline__ void dots(const VRows& r, const VDots& q, int j, const int (&id)[U],
+                                     float (&s)[U]) {
+  constexpr int EPC = 16 / sizeof(E);
+  const int lane = threadIdx.x & 63;
+  const E* x = q.X && r.st->n == r.T ? (const E*)q.X + (size_t)j * q.ldx
+                                     : (const E*)q.xp + (size_t)j * q.Dp;
+  const E* w[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    w[u] = (const E*)q.W + (size_t)max(id[u], 0) * q.ldw;
+    s[u] = 0.0f;
+  }
+  // a lane has the same chunks in the same order whether its loads are of 16
+  // bytes or single elements
+  for (int c = EPC * lane; c < r.D; c += 64 * EPC) {
+    E a[EPC], b[U][EPC];
+    const bool whole = c + EPC <= r.D;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (id[u] < 0) continue;
+      if (q.vec && whole) {
+        *(u32x4*)b[u] = *(const u32x4*)(w[u] + c);
+      } else {
+#pragma unroll
+        for (int i = 0; i < EPC; ++i) b[u][i] = c + i < r.D ? w[u][c + i] : (E)0;
+      }
+    }
+    if (whole) {
+      *(u32x4*)a = *(const u32x4*)(x + c);
+    } else {
+#pragma unroll
+      for (int i = 0; i < EPC; ++i) a[i] = c + i < r.D ? x[c + i] : (E)0;
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (id[u] >= 0)
+#pragma unroll
+        for (int i = 0; i < EPC; ++i) s[u] += to_f(a[i]) * to_f(b[u][i]);
+  }
+#pragma unroll
+  for (int u = 0; u < U; ++u) s[u] = wave_sum(s[u]) / r.tau;
+}
+// lists: four targets at a time per wave, four waves per row
 template <class E>
-__device__ __forceinline__ void tlogit_body(const VRows& r, const E* X, long long ldx,
-                                            const E* xp, int Dp, const E* W, long long ldw,
-                                            int vec, float* zt) {
-  constexpr int EPC = 16 / sizeof(E), U = 4;
+__device__ __forceinline__ void tlogit_body(const VRows& r, const VDots& q, float* zt) {
+  constexpr int U = 4;
   const int j = blockIdx.x;
   if (j >= r.st->n) return;
   const int t = r.idx[j], wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const E* x = X && r.st->n == r.T ? X + (size_t)j * ldx : xp + (size_t)j * Dp;
   float v;
   for (int k0 = wave * U; k0 < r.K; k0 += 4 * U) {
-    const E* w[U];
-    bool have[U];
+    int id[U];
     float s[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int id = k0 + u < r.K ? target(r, t, k0 + u, &v) : -1;
-      have[u] = id >= 0;
-      w[u] = W + (size_t)max(id, 0) * ldw;
-      s[u] = 0.0f;
-    }
-    // a lane has the same chunks in the same order whether its loads are of 16
-    // bytes or single elements
-    for (int c = EPC * lane; c < r.D; c += 64 * EPC) {
-      E a[EPC], b[U][EPC];
-      const bool whole = c + EPC <= r.D;
+    for (int u = 0; u < U; ++u) id[u] = k0 + u < r.K ? target(r, t, k0 + u, &v) : -1;
+    dots<E, U>(r, q, j, id, s);
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        if (!have[u]) continue;
-        if (vec && whole) {
-          *(u32x4*)b[u] = *(const u32x4*)(w[u] + c);
-        } else {
-#pragma unroll
-          for (int i = 0; i < EPC; ++i) b[u][i] = c + i < r.D ? w[u][c + i] : (E)0;
-        }
-      }
-      if (whole) {
-        *(u32x4*)a = *(const u32x4*)(x + c);
-      } else {
-#pragma unroll
-        for (int i = 0; i < EPC; ++i) a[i] = c + i < r.D ? x[c + i] : (E)0;
-      }
-#pragma unroll
-      for (int u = 0; u < U; ++u)
-        if (have[u])
-#pragma unroll
-          for (int i = 0; i < EPC; ++i) s[u] += to_f(a[i]) * to_f(b[u][i]);
-    }
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const float f = wave_sum(s[u]);
-      if (lane == 0 && have[u]) zt[(size_t)j * r.K + k0 + u] = f / r.tau;
-    }
+    for (int u = 0; u < U; ++u)
+      if (lane == 0 && id[u] >= 0) zt[(size_t)j * r.K + k0 + u] = s[u];
   }
 }
 }  // namespace
-extern "C" __global__ __launch_bounds__(256) void hf_vocab_tlogit_f32(
-    VRows r, const float* X, long long ldx, const float* xp, int Dp, const float* W, long long ldw,
-    int vec, float* zt) {
-  tlogit_body<float>(r, X, ldx, xp, Dp, W, ldw, vec, zt);
+extern "C" __global__ __launch_bounds__(256) void hf_vocab_tlogit_f32(VRows r, VDots q, float* zt) {
+  tlogit_body<float>(r, q, zt);
 }
-extern "C" __global__ __launch_bounds__(256) void hf_vocab_tlogit_bf16(
-    VRows r, const bf16_t* X, long long ldx, const bf16_t* xp, int Dp, const bf16_t* W, long long ldw,
-    int vec, float* zt) {
-  tlogit_body<bf16_t>(r, X, ldx, xp, Dp, W, ldw, vec, zt);
+extern "C" __global__ __launch_bounds__(256) void hf_vocab_tlogit_bf16(VRows r, VDots q,
+                                                                       float* zt) {
+  tlogit_body<bf16_t>(r, q, zt);
 }
 
 // ------------------------------------------------------------- rows' losses
@@ -336,11 +346,13 @@ struct RowTargets {          // lane l: targets l and l + 64
   int id[2];                 // -1: none, or a repeat
   float dt[2];               // delta at the target
 };
-// One packed row j < n by one wave.  zt: the targets' logits, or null: in z.
+// One packed row j < n by one wave.  The targets' logits: in zt, or (null) in
+// z, or (a label, both null) x.
 __device__ __forceinline__ RowTargets row_targets(const VRows& r, int j,
                                                   const float2* __restrict__ stat, int ldstat,
                                                   int tiles, const float* __restrict__ z,
-                                                  long long ldz, const float* __restrict__ zt) {
+                                                  long long ldz, const float* __restrict__ zt,
+                                                  float x0) {
   const int lane = threadIdx.x & 63, t = r.idx[j];
   RowTargets o;
   const float2* st = stat + (size_t)j * ldstat;
@@ -373,7 +385,7 @@ __device__ __forceinline__ RowTargets row_targets(const VRows& r, int j,
       const int k = lane + 64 * i;
       id[i] = target(r, t, k, &tl[i]);
       if (id[i] >= 0) {
-        const float x = zt ? zt[(size_t)j * r.K + k] : z[(size_t)j * ldz + id[i]];
+        const float x = zt ? zt[(size_t)j * r.K + k] : z ? z[(size_t)j * ldz + id[i]] : x0;
         // log p; above 0 only by rounding (the comparison keeps a NaN)
         lz[i] = x - o.lse > 0.0f ? 0.0f : x - o.lse;
       }
@@ -430,26 +442,6 @@ __device__ __forceinline__ RowTargets row_targets(const VRows& r, int j,
 }
 }  // namespace
 
-// One wave per packed row.
-extern "C" __global__ __launch_bounds__(256) void hf_vocab_row_loss(
-    VRows r, const float2* __restrict__ stat, int ldstat, int tiles,
-    const float* __restrict__ z, long long ldz, VTarget tg, float* __restrict__ lse) {
-  const int j = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
-  if (j >= r.st->n) return;
-  const RowTargets o = row_targets(r, j, stat, ldstat, tiles, z, ldz, z ? nullptr : tg.zt);
-  if (lane == 0) {
-    lse[j] = o.lse;
-    r.row_loss[r.idx[j]] = o.loss;
-  }
-  if (!tg.dt) return;
-#pragma unroll
-  for (int i = 0; i < 2; ++i)
-    if (lane + 64 * i < r.K) {
-      tg.id[(size_t)j * r.K + lane + 64 * i] = o.id[i];
-      tg.dt[(size_t)j * r.K + lane + 64 * i] = o.dt[i];
-    }
-}
-
 // The loss from the rows' losses, by one workgroup of 256 threads.
 namespace {
 __device__ __forceinline__ void loss_sum(const float* row_loss, int T, const VocabState* st,
@@ -469,6 +461,53 @@ __device__ __forceinline__ void loss_sum(const float* row_loss, int T, const Voc
   if (threadIdx.x == 0) *loss = (float)(((ws[0] + ws[1]) + (ws[2] + ws[3])) * st->inv);
 }
 }  // namespace
+// One wave per packed row.  DOT: the label's logit is formed here.  With `loss`
+// (few rows, one workgroup) the rows' losses are summed as well.
+namespace {
+template <class E, bool DOT>
+__device__ __forceinline__ void row_loss_body(const VRows& r, const float2* stat, int ldstat,
+                                              int tiles, const float* z, long long ldz,
+                                              const VTarget& tg, float* lse, const VDots& q,
+                                              float* loss) {
+  const int lane = threadIdx.x & 63, waves = blockDim.x >> 6;
+  for (int j = blockIdx.x * waves + (threadIdx.x >> 6); j < r.st->n; j += gridDim.x * waves) {
+    float x0 = 0.0f;
+    if constexpr (DOT) {
+      float v, s[1];
+      const int id[1] = {target(r, r.idx[j], 0, &v)};
+      dots<E, 1>(r, q, j, id, s);
+      x0 = s[0];
+    }
+    const RowTargets o = row_targets(r, j, stat, ldstat, tiles, DOT ? nullptr : z, ldz,
+                                     DOT || z ? nullptr : tg.zt, x0);
+    if (lane == 0) {
+      lse[j] = o.lse;
+      r.row_loss[r.idx[j]] = o.loss;
+    }
+    if (!tg.dt) continue;
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      if (lane + 64 * i < r.K) {
+        tg.id[(size_t)j * r.K + lane + 64 * i] = o.id[i];
+        tg.dt[(size_t)j * r.K + lane + 64 * i] = o.dt[i];
+      }
+  }
+  if (loss) {
+    __syncthreads();
+    loss_sum(r.row_loss, r.T, r.st, loss);
+  }
+}
+}  // namespace
+#define HF_ROW_LOSS(SUF, E, DOT)                                                          \
+  extern "C" __global__ __launch_bounds__(256) void hf_vocab_row_loss##SUF(               \
+      VRows r, const float2* stat, int ldstat, int tiles, const float* z, long long ldz,  \
+      VTarget tg, float* lse, VDots q, float* loss) {                                     \
+    row_loss_body<E, DOT>(r, stat, ldstat, tiles, z, ldz, tg, lse, q, loss);              \
+  }
+HF_ROW_LOSS(, float, false)
+HF_ROW_LOSS(_f32, float, true)
+HF_ROW_LOSS(_bf16, bf16_t, true)
+
 extern "C" __global__ __launch_bounds__(256) void hf_vocab_loss_sum(
     const float* __restrict__ row_loss, int T, const VocabState* st, float* loss) {
   loss_sum(row_loss, T, st, loss);
@@ -510,7 +549,8 @@ __device__ __forceinline__ void delta_body(const VRows& r, const VDelta& a, E* d
   if constexpr (SELF) {
     if (real && threadIdx.x < 64) {
       const int lane = threadIdx.x;
-      const RowTargets o = row_targets(r, j, a.stat, a.ldstat, a.tiles, a.z, a.ldz, nullptr);
+      const RowTargets o = row_targets(r, j, a.stat, a.ldstat, a.tiles, a.z, a.ldz, nullptr,
+                                       0.0f);
       if (lane == 0) {
         lse_s = o.lse;
         if (c0 == 0) r.row_loss[r.idx[j]] = o.loss;
@@ -690,6 +730,10 @@ inline int vec16(const void* p, long long ld, int es) {
 }
 }  // namespace
 
+namespace {
+constexpr int SUM_ROWS = 16;      // rows whose losses one workgroup forms and sums
+}  // namespace
+
 bool vocab_count(const Launch& L, const VRows& r) {
   if (r.T > 0 && r.T <= SELF_ROWS && r.K <= SELF_TOP) return false;
   if (r.t && r.T > 0)
@@ -722,21 +766,26 @@ void vocab_pack_matrix(const Launch& L, int type, const void* W, long long ldw, 
               vec16(W, ldw, 2), D, (bf16_t*)wp, Dp);
 }
 
-void vocab_target_logits(const Launch& L, int type, const VRows& r, const void* X, long long ldx,
-                         const void* xp, int Dp, const void* W, long long ldw, float* zt) {
-  if (type == VT_F32)
-    HF_LAUNCH("hf_vocab_tlogit", hf_vocab_tlogit_f32, r.T, 256, r, (const float*)X, ldx,
-              (const float*)xp, Dp, (const float*)W, ldw, vec16(W, ldw, 4), zt);
-  else
-    HF_LAUNCH("hf_vocab_tlogit", hf_vocab_tlogit_bf16, r.T, 256, r, (const bf16_t*)X, ldx,
-              (const bf16_t*)xp, Dp, (const bf16_t*)W, ldw, vec16(W, ldw, 2), zt);
-}
-
-void vocab_row_loss(const Launch& L, const VRows& r, const float2* stat, int ldstat, int tiles,
-                    const float* z, long long ldz, const VTarget& t, float* lse) {
-  if (r.T < 1) return;
-  HF_LAUNCH("hf_vocab_row_loss", hf_vocab_row_loss, (r.T + 3) / 4, 256, r, stat, ldstat,
-            tiles, z, ldz, t, lse);
+bool vocab_row_loss(const Launch& L, int type, const VRows& r, const float2* stat, int ldstat,
+                    int tiles, const float* z, long long ldz, const VTarget& t, float* lse,
+                    const void* X, long long ldx, const void* xp, int Dp, const void* W,
+                    long long ldw, float* loss) {
+  if (r.T < 1) return false;
+  const int es = type == VT_F32 ? 4 : 2;
+  const VDots q = {X, xp, W, ldx, ldw, Dp, vec16(W, ldw, es)};
+  if (!z && r.K > 1) {
+    if (type == VT_F32)
+      HF_LAUNCH("hf_vocab_tlogit", hf_vocab_tlogit_f32, r.T, 256, r, q, t.zt);
+    else
+      HF_LAUNCH("hf_vocab_tlogit", hf_vocab_tlogit_bf16, r.T, 256, r, q, t.zt);
+  }
+  const bool sum = loss && r.T <= SUM_ROWS, dot = !z && r.K == 1;
+  HF_LAUNCH("hf_vocab_row_loss",
+            (!dot ? hf_vocab_row_loss : type == VT_F32 ? hf_vocab_row_loss_f32
+                                                       : hf_vocab_row_loss_bf16),
+            sum ? 1 : (r.T + 3) / 4, 256, r, stat, ldstat, tiles, z, ldz, t, lse, q,
+            sum ? loss : nullptr);
+  return sum;
 }
 
 void vocab_loss_sum(const Launch& L, const VRows& r, float* loss) {

@@ -272,16 +272,17 @@ void head(hf_vocab* c, VRows r, const void* X, int64_t ldx, const void* W, int64
   const bool direct = D % VPAD == 0 && ldw <= MAX_LD && (uintptr_t)W % 16 == 0 &&
                       (ldw * es) % 16 == 0;
   const int wrows = direct ? V : pack_rows(c);
-  int packed = -1;                      // first row of the packed piece
+  int packed = -1, packed_n = 0;        // the packed piece
   auto matrix = [&](int v0, int n, long long* ld) -> const void* {
     if (direct) {
       *ld = ldw;
       return (const char*)W + (size_t)v0 * ldw * es;
     }
     void* wp = c->at<void>(l.wp);
-    if (packed != v0)
+    if (packed != v0 || packed_n < n)
       vocab_pack_matrix(L, type, (const char*)W + (size_t)v0 * ldw * es, ldw, n, D, wp, Dp);
     packed = v0;
+    packed_n = n;
     *ld = Dp;
     return wp;
   };

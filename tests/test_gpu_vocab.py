@@ -11,7 +11,10 @@ bf16 and 2^-24 for fp32; e: 2^-24, the rounding of fp32 sums):
   loss     both of these, twice the logit error for the target's own logit;
            times tau^2; the teacher's q as good as its exponentials
   delta    p relative by the error of z - lse and 64 e for the exp, rounded to
-           the type by u (two terms of bf16: u^2), likewise at the targets
+           the type by u (two terms of bf16: u^2), likewise at the targets; with
+           bf16 and more than 128 rows exp(z - max) is rounded to fp16 before,
+           2^-12 of it or, where fp16 has no smaller step, 2^-25 of the maximum:
+           p is off by 2^-12 p + 2^-25 max p besides
   dX, dW   sum of K products in fp32: K e sum |terms|, terms off by delta's
            error, the result times a factor good to 2 e, rounded by u
   embedding  exact but for one rounding of the product by u (and e of it in
@@ -98,6 +101,8 @@ def reference(X, W, q_of, tau, rows_used, denom, chunk=2048):
         r["erow"].append(tau ** 2 * (elp + 256 * E32 * (1 + size)))
         d = torch.where(use, p - q, 0.0)
         ed = torch.where(use, p * (elp[:, None] + 64 * E32) + q * 256 * E32, 0.0)
+        if X.dtype == torch.bfloat16 and n > 128:
+            ed = ed + torch.where(use, 2.0 ** -12 * p + 2.0 ** -25 * p.amax(1, keepdim=True), 0.0)
         r["dX"].append(scale * (d @ Wd))
         for u, key in ((None, "bX"),):
             r[key].append((d, ed))
@@ -630,6 +635,53 @@ def test_masked_gradient_rows_reach_nothing():
     want = net.hf_vocab_embed_grad(tok, dout)
     dout[tok < 0] = math.nan
     assert torch.equal(want, net.hf_vocab_embed_grad(tok, dout))
+
+
+@pytest.mark.parametrize("name", ["fp32", "bf16"])
+def test_limits(name):
+    """The widest rows, the largest vocabulary, the most rows."""
+    torch = T()
+    for rows, V, D in ((3, 9, H.HF_VOCAB_MAX_WIDTH), (5, H.HF_VOCAB_MAX, 8),
+                       (H.HF_VOCAB_MAX_ROWS, 3, 4)):
+        X, W, y = head_inputs(name, rows, V, D)
+        y = mask_rows(y, "some") if rows > 100 else y
+        net = H.HFVocab(V, D, rows, name)
+        q_of, used = label_targets(y, V)
+        ref = reference(X, W, q_of, 1.0, used, int(used.sum()), chunk=1 << 18)
+        check_head(name, ref, V, net.hf_vocab_loss_grad(X, W, y), two=rows <= 128)
+        emb = net.hf_vocab_embed(W, y, 2.0)
+        keep = y >= 0
+        assert torch.equal(emb, W[y.long().clamp(min=0)] * 2 * keep[:, None])
+        # whole numbers: their sums are exact in fp32, in any order
+        whole = torch.randint(-2, 3, X.shape, generator=gen(1), device="cuda").to(X.dtype)
+        want = torch.zeros(V, D, dtype=torch.float64, device="cuda")
+        want.index_add_(0, y[keep].long(), whole[keep].double())
+        assert torch.equal(net.hf_vocab_embed_grad(y, whole), want.to(X.dtype))
+        del net, ref, want
+        torch.cuda.empty_cache()
+
+
+def test_two_contexts_on_two_streams():
+    """Contexts share nothing: both working at once give the bits of each
+    alone."""
+    torch = T()
+    jobs = []
+    for k, (rows, V, D) in enumerate(((900, 5000, 256), (60, 9000, 320))):
+        X, W, y = head_inputs("bf16", rows, V, D, seed=k)
+        net = H.HFVocab(V, D, rows, "bf16")
+        want = [o.clone() for o in net.hf_vocab_loss_grad(X, W, y)]
+        want.append(net.hf_vocab_embed_grad(y, X).clone())
+        jobs.append((net, X, W, y, want, torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(5):
+        for k, (net, X, W, y, want, s) in enumerate(jobs):
+            with torch.cuda.stream(s):
+                got[k] = [*net.hf_vocab_loss_grad(X, W, y), net.hf_vocab_embed_grad(y, X)]
+    torch.cuda.synchronize()
+    for k in range(2):
+        for a, b in zip(jobs[k][4], got[k]):
+            assert torch.equal(a, b)
 
 
 # ------------------------------------------------------------- all together

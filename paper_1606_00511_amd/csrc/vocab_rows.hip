@@ -268,11 +268,11 @@ struct VDots {
   long long ldx, ldw;
   int Dp, vec;
 };
-template <class E, int U>
+template <class E, int U, int LANES>
 __device__ __forceinline__ void dots(const VRows& r, const VDots& q, int j, const int (&id)[U],
                                      float (&s)[U]) {
   constexpr int EPC = 16 / sizeof(E);
-  const int lane = threadIdx.x & 63;
+  const int lane = threadIdx.x & (LANES - 1);
   const E* x = q.X && r.st->n == r.T ? (const E*)q.X + (size_t)j * q.ldx
                                      : (const E*)q.xp + (size_t)j * q.Dp;
   const E* w[U];
@@ -283,7 +283,7 @@ __device__ __forceinline__ void dots(const VRows& r, const VDots& q, int j, cons
   }
   // a lane has the same chunks in the same order whether its loads are of 16
   // bytes or single elements
-  for (int c = EPC * lane; c < r.D; c += 64 * EPC) {
+  for (int c = EPC * lane; c < r.D; c += LANES * EPC) {
     E a[EPC], b[U][EPC];
     const bool whole = c + EPC <= r.D;
 #pragma unroll
@@ -309,26 +309,39 @@ __device__ __forceinline__ void dots(const VRows& r, const VDots& q, int j, cons
         for (int i = 0; i < EPC; ++i) s[u] += to_f(a[i]) * to_f(b[u][i]);
   }
 #pragma unroll
-  for (int u = 0; u < U; ++u) s[u] = wave_sum(s[u]) / r.tau;
+  for (int u = 0; u < U; ++u) {
+#pragma unroll
+    for (int o = LANES / 2; o > 0; o >>= 1) s[u] += __shfl_xor(s[u], o, 64);
+    s[u] /= r.tau;
+  }
 }
-// lists: four targets at a time per wave, four waves per row
-template <class E>
-__device__ __forceinline__ void tlogit_body(const VRows& r, const VDots& q, float* zt) {
-  constexpr int U = 4;
-  const int j = blockIdx.x;
-  if (j >= r.st->n) return;
-  const int t = r.idx[j], wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+// lists: LANES lanes take up to four targets at a time, a workgroup a row
+template <class E, int LANES>
+__device__ __forceinline__ void tlogit_row(const VRows& r, const VDots& q, int j, float* zt) {
+  constexpr int U = 4, G = 256 / LANES;
+  const int t = r.idx[j], g = threadIdx.x / LANES;
   float v;
-  for (int k0 = wave * U; k0 < r.K; k0 += 4 * U) {
+  for (int k0 = g; k0 < r.K; k0 += U * G) {
     int id[U];
     float s[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) id[u] = k0 + u < r.K ? target(r, t, k0 + u, &v) : -1;
-    dots<E, U>(r, q, j, id, s);
+    for (int u = 0; u < U; ++u) id[u] = k0 + u * G < r.K ? target(r, t, k0 + u * G, &v) : -1;
+    dots<E, U, LANES>(r, q, j, id, s);
 #pragma unroll
     for (int u = 0; u < U; ++u)
-      if (lane == 0 && id[u] >= 0) zt[(size_t)j * r.K + k0 + u] = s[u];
+      if ((threadIdx.x & (LANES - 1)) == 0 && id[u] >= 0)
+        zt[(size_t)j * r.K + k0 + u * G] = s[u];
   }
+}
+// A row of W that one load of a wave covers (1 KiB) leaves lanes without work:
+// a quarter of a wave each then (7,276 rows of 57 targets, 128 columns of bf16:
+// 56 -> 23 us; 2,048 columns keep the wave, at 6.9 TB/s).
+template <class E>
+__device__ __forceinline__ void tlogit_body(const VRows& r, const VDots& q, float* zt) {
+  const int j = blockIdx.x;
+  if (j >= r.st->n) return;
+  if (r.D * (int)sizeof(E) <= 1024) tlogit_row<E, 16>(r, q, j, zt);
+  else tlogit_row<E, 64>(r, q, j, zt);
 }
 }  // namespace
 extern "C" __global__ __launch_bounds__(256) void hf_vocab_tlogit_f32(VRows r, VDots q, float* zt) {
@@ -475,7 +488,7 @@ __device__ __forceinline__ void row_loss_body(const VRows& r, const float2* stat
     if constexpr (DOT) {
       float v, s[1];
       const int id[1] = {target(r, r.idx[j], 0, &v)};
-      dots<E, 1>(r, q, j, id, s);
+      dots<E, 1, 64>(r, q, j, id, s);
       x0 = s[0];
     }
     const RowTargets o = row_targets(r, j, stat, ldstat, tiles, DOT ? nullptr : z, ldz,

@@ -185,11 +185,12 @@ def mask_rows(y, how, seed=5):
 
 # one row; sizes below, at and past tiles of 128 and 256, K blocks of 64 and
 # the 128 rows of the two-term form; odd widths and vocabularies; thousands of
-# statistics entries for few rows; enough tiles of 256 for every product
+# statistics entries for few rows; enough tiles of 256 for every product; 1,024
+# rows, up to which tiles of 32 and 64 are taken, on few columns
 SHAPES = [(1, 1, 1), (1, 1000, 64), (3, 7, 5), (64, 130, 64), (65, 129, 63), (127, 1000, 96),
           (128, 257, 128), (129, 1000, 96), (256, 256, 64), (300, 515, 200), (257, 2049, 321),
-          (1000, 513, 130), (2100, 300, 66), (100, 140000, 64), (2049, 8200, 512),
-          (4101, 4099, 1100)]
+          (1000, 513, 130), (300, 1360, 520), (1024, 900, 260), (1025, 900, 260),
+          (2100, 300, 66), (100, 140000, 64), (2049, 8200, 512), (4101, 4099, 1100)]
 
 
 @pytest.mark.parametrize("name", ["fp32", "bf16"])
@@ -211,7 +212,8 @@ def test_loss_and_gradient(name, rows, V, D):
 @pytest.mark.parametrize("name", ["fp32", "bf16"])
 @pytest.mark.parametrize("rows,V,D,K,tau", [
     (1, 5, 3, 5, 1.0), (2, 1000, 64, 1, 2.0), (64, 130, 64, 16, 2.0), (129, 700, 63, 65, 0.5),
-    (300, 2000, 128, 128, 4.0), (513, 257, 72, 100, 1.0)])
+    (300, 2000, 128, 128, 4.0), (513, 257, 72, 100, 1.0), (700, 900, 256, 57, 1.0),
+    (200, 600, 513, 70, 1.0)])
 def test_distillation(name, rows, V, D, K, tau):
     torch = T()
     X, W, _ = head_inputs(name, rows, V, D, seed=rows)

@@ -210,13 +210,13 @@ int end(hf_vocab* c) {
 // Partials are written and read again, few of them in the last-level cache.
 struct Shape {
   int tile, splits;
+  double us;
 };
 constexpr double RATE[2][4] = {{0.24e6, 0.27e6, 0.22e6, 0.21e6}, {1.78e6, 2.4e6, 1.45e6, 1.1e6}};
 constexpr double BYTES_US = 4.7e6, L2_US = 15e6;
 constexpr double AHEAD[4] = {16384, 32768, 32768, 49152};
 Shape shape_for(int type, int64_t M, int64_t N, int64_t K, bool split, bool few) {
-  Shape best = {0, 1};
-  double least = 1e300;
+  Shape best = {0, 1, 1e300};
   const int es = type == VT_F32 ? 4 : 2;
   for (int tile = 0; tile < (few && N <= FEW_ROWS ? 4 : 2); ++tile) {
     const int64_t RM = tile_m(tile), RN = tile_n(tile);
@@ -239,10 +239,7 @@ Shape shape_for(int type, int64_t M, int64_t N, int64_t K, bool split, bool few)
       const double l2 = ((double)tn * M + (double)tm * N) * K * es / L2_US + 4.0;
       const double est = std::max({t, mem, l2}) +
                          (s > 1 ? 4.0 + part / (part < 64e6 ? 2 * BYTES_US : BYTES_US) : 0.0);
-      if (est < least) {
-        least = est;
-        best = {tile, s};
-      }
+      if (est < best.us) best = {tile, s, est};
     }
   }
   return best;
@@ -442,10 +439,8 @@ void head(hf_vocab* c, VRows r, const void* X, int64_t ldx, const void* W, int64
     VGemm q = {};
     q.A = xp;
     q.lda = Dp;
-    q.B = d;
     q.ldb = ldd;
     q.M = D;
-    q.N = pn;
     q.K = dup ? 2 * dup : (int)up(T, VPAD);
     q.alim = dup ? 2 * dup : Rp;
     q.st = r.st;
@@ -454,22 +449,44 @@ void head(hf_vocab* c, VRows r, const void* X, int64_t ldx, const void* W, int64
     q.ldx = ldx;
     q.T = T;
     q.thin = q.K <= (type == VT_F32 ? 64 : 256) && (int64_t)pn * D >= (1 << 20);
-    const Shape ws = q.thin ? Shape{TILE_SMALL, 1} : shape_for(type, D, pn, q.K, true, false);
-    q.tile = ws.tile;
-    q.splits = ws.splits;
-    VEpi pe = {};
-    char* out = (char*)g->dW + (size_t)p0 * g->lddw * es;
-    pe.part = c->at<float>(l.partw);
-    pe.ldp = Dp;
-    pe.split_stride = up(pn, 128) * Dp;
-    pe.out = out;
-    pe.ldo = g->lddw;
-    pe.accumulate = g->accumulate;
-    pe.vec = (g->lddw * es) % 16 == 0 && (uintptr_t)out % 16 == 0;
-    vocab_dw(L, type, q, pe);
-    if (q.splits > 1)
-      vocab_finish(L, type, r.st, pe.part, q.splits, pe.split_stride, Dp, 0, pn, 0, D, nullptr,
-                   out, g->lddw, g->accumulate, nullptr, nullptr);
+    Shape ws = {TILE_SMALL, 1, 0.0}, rest = ws;
+    int n1 = pn;
+    if (!q.thin) {
+      ws = shape_for(type, D, pn, q.K, true, false);
+      // a last round of few tiles of 256 leaves most units idle: its rows of dW
+      // are a product of their own then, of a shape of their own (788 tiles,
+      // K = 2,251: 310 -> 282 us)
+      const int64_t tm = (D + 255) / 256, whole = tm * ((pn + 255) / 256) / 256 * 256 / tm * 256;
+      if (ws.tile == TILE_BIG && ws.splits == 1 && whole > 0 && whole < pn) {
+        const Shape a = shape_for(type, D, whole, q.K, true, false);
+        rest = shape_for(type, D, pn - whole, q.K, true, false);
+        if (a.us + rest.us + 4.0 < ws.us) {
+          ws = a;
+          n1 = (int)whole;
+        }
+      }
+    }
+    auto product = [&](int r0, int n, const Shape& h) {
+      q.B = (const char*)d + (size_t)r0 * es;
+      q.N = n;
+      q.tile = h.tile;
+      q.splits = h.splits;
+      VEpi pe = {};
+      char* out = (char*)g->dW + (size_t)(p0 + r0) * g->lddw * es;
+      pe.part = c->at<float>(l.partw);
+      pe.ldp = Dp;
+      pe.split_stride = up(n, 128) * Dp;
+      pe.out = out;
+      pe.ldo = g->lddw;
+      pe.accumulate = g->accumulate;
+      pe.vec = (g->lddw * es) % 16 == 0 && (uintptr_t)out % 16 == 0;
+      vocab_dw(L, type, q, pe);
+      if (q.splits > 1)
+        vocab_finish(L, type, r.st, pe.part, q.splits, pe.split_stride, Dp, 0, n, 0, D, nullptr,
+                     out, g->lddw, g->accumulate, nullptr, nullptr);
+    };
+    product(0, n1, ws);
+    if (n1 < pn) product(n1, pn - n1, rest);
   }
   if (g->dX && T > 0 && finish)
     vocab_finish(L, type, r.st, partx, xs.splits, xstride, Dp, dup, T, 1, D, r.idx, g->dX,

@@ -223,14 +223,17 @@ __device__ __forceinline__ void store_part(const float* s, int lane, O* out, lon
 // ----------------------------------------------------------------- epilogues
 enum { E_LOGITS, E_EXPS, E_PROBS, E_PART, E_OUT, E_ROWS };
 
-// The tile (tm, tn) and split this workgroup computes.  Consecutive
-// workgroups go to the 8 XCDs in turn; each XCD gets a contiguous eighth of
-// the logical order, which walks groups of 8 tiles of n, m by m, so that the
-// workgroups resident on an XCD share their operand panels in its L2.
-__device__ __forceinline__ void tile_of(int& tm, int& tn, int& tz) {
-  const int gx = gridDim.x, gy = gridDim.y;
+// The tile (tm, tn) and split this workgroup computes, of gy tiles of n that
+// have rows; false: none.  Consecutive workgroups go to the 8 XCDs in turn;
+// each XCD gets a contiguous eighth of the logical order, which walks groups
+// of 8 tiles of n, m by m, so that the workgroups resident on an XCD share
+// their operand panels in its L2.  Tiles without rows take no place in the
+// order (2,251 of 3,001 rows counted, 50,257 x 1,024: 301 -> 222 us).
+__device__ __forceinline__ bool tile_of(int gy, int& tm, int& tn, int& tz) {
+  const int gx = gridDim.x;
   const int T = gx * gy * gridDim.z;
-  const int L = blockIdx.x + gx * (blockIdx.y + gy * blockIdx.z);
+  const int L = blockIdx.x + gx * (blockIdx.y + gridDim.y * blockIdx.z);
+  if (L >= T) return false;
   // XCD x's share: T / 8 workgroups, one more for the first T % 8
   const int x = L % 8, q = T / 8, r8 = T % 8;
   const int Lg = x * q + min(x, r8) + L / 8;
@@ -243,6 +246,7 @@ __device__ __forceinline__ void tile_of(int& tm, int& tn, int& tz) {
   const int w = r - g * G * gx;
   tn = first + w % rows;
   tm = w / rows;
+  return true;
 }
 
 template <class E, int EPI, bool AKC, bool BKC, int WM, int WN, int GM, int GN, int S, int KB>
@@ -261,13 +265,12 @@ __device__ __forceinline__ void vgemm_body(const VGemm& s, const VEpi& e) {
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wave / GN, wn = wave % GN;
   const int li = lane & 31, h = lane >> 5;
-  int tm, tn, tz;
-  tile_of(tm, tn, tz);
-  const int m0 = tm * RM, n0 = tn * RN;
   const int nrow = s.st->n;
   const int N = s.dyn == 1 ? nrow : s.N;
   const int K = s.dyn == 2 ? (nrow + BK - 1) & ~(BK - 1) : s.K;
-  if (n0 >= N) return;
+  int tm, tn, tz;
+  if (!tile_of((N + RN - 1) / RN, tm, tn, tz)) return;
+  const int m0 = tm * RM, n0 = tn * RN;
   // rows that all count are read where they are, not packed
   const bool whole = s.X && nrow == s.T;
   constexpr bool XA = !BKC;              // dW: X is A; logits: X is B

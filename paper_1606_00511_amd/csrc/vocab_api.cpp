@@ -224,7 +224,7 @@ Shape shape_for(int type, int64_t M, int64_t N, int64_t K, bool split, bool few)
     const int64_t slots = tile == TILE_BIG ? 256 : 512;
     for (int s = 1; s <= VMAX_SPLITS; ++s) {
       if (s > 1 && (!split || K / s < 256 ||
-                    (size_t)s * up(N, 128) * up(M, VPAD) > SPLIT_FLOATS))
+                    (size_t)s * up(N, VTILE) * up(M, VPAD) > SPLIT_FLOATS))
         break;
       const int64_t rounds = (tiles * s + slots - 1) / slots;
       // the workgroups of a unit share it; one alone does not fill it
@@ -366,8 +366,9 @@ void head(hf_vocab* c, VRows r, const void* X, int64_t ldx, const void* W, int64
   const int xrows = dup ? 2 * dup : T;
   float* partx = c->at<float>(l.partx);
   Shape xs = {0, 1};
-  long long xstride = 0;
-  bool finish = true;
+  VGemm xq = {};
+  VEpi xe = {};
+  int xmax = 0;
   for (int p0 = 0; p0 < V; p0 += vc) {
     const int pn = std::min(vc, V - p0);
     // a piece of delta covers several packed pieces of W where logits are kept
@@ -416,24 +417,23 @@ void head(hf_vocab* c, VRows r, const void* X, int64_t ldx, const void* W, int64
       q.dyn = dup ? 0 : 1;
       if (v0 == 0) {
         xs = shape_for(type, D, xrows, n, true, true);
-        xstride = up(xrows, 128) * Dp;
+        xmax = (int)std::min<int64_t>(VMAX_SPLITS, n / 256);
+        xe.part = partx;
+        xe.ldp = Dp;
         // one piece and no splits: straight into dX
-        finish = n < V || xs.splits > 1 || dup || xs.tile >= TILE_N64;
+        if (n == V && xs.splits == 1 && !dup && xs.tile < TILE_N64) {
+          xe.out = g->dX;
+          xe.ldo = g->lddx;
+          xe.idx = r.idx;
+          xe.vec = (g->lddx * es) % 16 == 0 && (uintptr_t)g->dX % 16 == 0;
+        }
       }
       q.splits = xs.splits;
+      q.smax = xmax;
       q.tile = xs.tile;
-      VEpi pe = {};
-      pe.part = partx;
-      pe.ldp = Dp;
-      pe.split_stride = xstride;
-      pe.add = v0 > 0;
-      if (!finish) {
-        pe.out = g->dX;
-        pe.ldo = g->lddx;
-        pe.idx = r.idx;
-        pe.vec = (g->lddx * es) % 16 == 0 && (uintptr_t)g->dX % 16 == 0;
-      }
-      vocab_dx(L, type, q, pe);
+      xe.add = v0 > 0;
+      vocab_dx(L, type, q, xe);
+      xq = q;
     }
     if (!g->dW) continue;
     VGemm q = {};
@@ -475,22 +475,21 @@ void head(hf_vocab* c, VRows r, const void* X, int64_t ldx, const void* W, int64
       char* out = (char*)g->dW + (size_t)(p0 + r0) * g->lddw * es;
       pe.part = c->at<float>(l.partw);
       pe.ldp = Dp;
-      pe.split_stride = up(n, 128) * Dp;
       pe.out = out;
       pe.ldo = g->lddw;
       pe.accumulate = g->accumulate;
       pe.vec = (g->lddw * es) % 16 == 0 && (uintptr_t)out % 16 == 0;
       vocab_dw(L, type, q, pe);
       if (q.splits > 1)
-        vocab_finish(L, type, r.st, pe.part, q.splits, pe.split_stride, Dp, 0, n, 0, D, nullptr,
-                     out, g->lddw, g->accumulate, nullptr, nullptr);
+        vocab_finish(L, type, q, pe, 0, n, 0, D, nullptr, out, g->lddw, g->accumulate, nullptr,
+                     nullptr);
     };
     product(0, n1, ws);
     if (n1 < pn) product(n1, pn - n1, rest);
   }
-  if (g->dX && T > 0 && finish)
-    vocab_finish(L, type, r.st, partx, xs.splits, xstride, Dp, dup, T, 1, D, r.idx, g->dX,
-                 g->lddx, 0, &r, self ? loss : nullptr);
+  if (g->dX && T > 0)
+    vocab_finish(L, type, xq, xe, dup, T, 1, D, r.idx, g->dX, g->lddx, 0, &r,
+                 self ? loss : nullptr);
 }
 
 // arguments of a head call, then its work

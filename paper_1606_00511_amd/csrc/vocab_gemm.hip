@@ -224,14 +224,14 @@ __device__ __forceinline__ void store_part(const float* s, int lane, O* out, lon
 enum { E_LOGITS, E_EXPS, E_PROBS, E_PART, E_OUT, E_ROWS };
 
 // The tile (tm, tn) and split this workgroup computes, of gy tiles of n that
-// have rows; false: none.  Consecutive workgroups go to the 8 XCDs in turn;
+// have rows and gz splits; false: none.  Consecutive workgroups go to the 8 XCDs in turn;
 // each XCD gets a contiguous eighth of the logical order, which walks groups
 // of 8 tiles of n, m by m, so that the workgroups resident on an XCD share
 // their operand panels in its L2.  Tiles without rows take no place in the
 // order (2,251 of 3,001 rows counted, 50,257 x 1,024: 301 -> 222 us).
-__device__ __forceinline__ bool tile_of(int gy, int& tm, int& tn, int& tz) {
+__device__ __forceinline__ bool tile_of(int gy, int gz, int& tm, int& tn, int& tz) {
   const int gx = gridDim.x;
-  const int T = gx * gy * gridDim.z;
+  const int T = gx * gy * gz;
   const int L = blockIdx.x + gx * (blockIdx.y + gridDim.y * blockIdx.z);
   if (L >= T) return false;
   // XCD x's share: T / 8 workgroups, one more for the first T % 8
@@ -268,8 +268,10 @@ __device__ __forceinline__ void vgemm_body(const VGemm& s, const VEpi& e) {
   const int nrow = s.st->n;
   const int N = s.dyn == 1 ? nrow : s.N;
   const int K = s.dyn == 2 ? (nrow + BK - 1) & ~(BK - 1) : s.K;
+  const int gy = (N + RN - 1) / RN;
+  const int splits = splits_of(s.splits, s.smax, gridDim.y, gy);
   int tm, tn, tz;
-  if (!tile_of((N + RN - 1) / RN, tm, tn, tz)) return;
+  if (!tile_of(gy, splits, tm, tn, tz)) return;
   const int m0 = tm * RM, n0 = tn * RN;
   // rows that all count are read where they are, not packed
   const bool whole = s.X && nrow == s.T;
@@ -279,8 +281,8 @@ __device__ __forceinline__ void vgemm_body(const VGemm& s, const VEpi& e) {
 
   const int nvb = (K + BK - 1) / BK;
   int vb0 = 0, nblk = nvb;
-  if (s.splits > 1) {
-    const int per = (nvb + s.splits - 1) / s.splits;
+  if (splits > 1) {
+    const int per = (nvb + splits - 1) / splits;
     vb0 = min(tz * per, nvb);
     nblk = min(nvb, vb0 + per) - vb0;
   }
@@ -473,7 +475,9 @@ __device__ __forceinline__ void vgemm_body(const VGemm& s, const VEpi& e) {
   const int Mp = EPI == E_PROBS || STATS ? (s.M + VPAD - 1) & ~(VPAD - 1) : s.M;
   const int Np = EPI == E_PROBS ? (N + VPAD - 1) & ~(VPAD - 1) : N;
   constexpr bool FINAL = EPI == E_OUT || EPI == E_ROWS;
-  const float scale = FINAL ? s.st->gscale : 1.0f;
+  const bool parts = EPI == E_PART || (EPI == E_ROWS && splits > 1);
+  const float scale = FINAL && !parts ? s.st->gscale : 1.0f;
+  float* const part = e.part + (size_t)tz * gy * RN * e.ldp;
 #pragma unroll
   for (int b = 0; b < WN; ++b) {
     const int n = nt + 32 * b + li;
@@ -502,12 +506,11 @@ __device__ __forceinline__ void vgemm_body(const VGemm& s, const VEpi& e) {
       store_part<_Float16, RL>(mine, lane, (_Float16*)e.pt, e.ldz, nb, Np, mt, Mp, 1, 0);
     else if constexpr (EPI == E_PROBS)
       store_part<E, RL>(mine, lane, (E*)e.d, e.ldd, nb, Np, mt, Mp, 1, 0);
-    else if constexpr (EPI == E_PART)
-      store_part<float, RL>(mine, lane, e.part + (size_t)tz * e.split_stride, e.ldp, nb, Np, mt,
-                            Mp, 1, e.add);
     else if constexpr (EPI == E_OUT)
       store_part<E, RL>(mine, lane, (E*)e.out, e.ldo, nb, Np, mt, Mp, e.vec, e.accumulate);
-    else
+    else if (parts)
+      store_part<float, RL>(mine, lane, part, e.ldp, nb, Np, mt, Mp, 1, e.add);
+    else if constexpr (EPI == E_ROWS)
       store_part<E, RL>(mine, lane, (E*)e.out, e.ldo, nb, Np, mt, Mp, e.vec, 0, e.idx);
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();

@@ -46,9 +46,19 @@ struct VGemm {
   int T;
   int dyn;         // 1: N is st->n; 2: K is st->n, rounded up to K blocks
   int splits;      // split-K factor (partials), grid z
+  int smax;        // where fewer rows count than N, up to so many (0: no more)
   int tile;
   int thin;        // dW of few rows (TILE_SMALL, splits 1)
 };
+
+// The partials of a product whose grid is for gy tiles of rows, of which gya
+// have any: the workgroups of the others are given to more splits (a tenth of
+// 8,192 rows counted, bf16, 32,000 x 2,048: 649 -> 130 us).  A partial is gya
+// tiles of rows; so many of them take no more than splits of gy tiles.
+__host__ __device__ inline int splits_of(int splits, int smax, int gy, int gya) {
+  const int more = gya > 0 ? splits * gy / gya : splits;
+  return smax <= splits ? splits : more < smax ? more : smax;
+}
 
 struct VEpi {
   // logits
@@ -63,7 +73,7 @@ struct VEpi {
   long long ldd;
   // products
   float* part;           // partials, [split][n][m]
-  long long ldp, split_stride;
+  long long ldp;
   int add;               // part += rather than =
   void* out;             // final output, scaled by st->gscale
   long long ldo;
@@ -77,8 +87,8 @@ struct VEpi {
 void vocab_logits(const Launch& L, int type, const VGemm& g, const VEpi& e);
 // p = exp(z - lse) of a vocabulary piece, rounded to the type, into d
 void vocab_probs(const Launch& L, int type, const VGemm& g, const VEpi& e);
-// row gradients: A = W piece (rows k), B = delta (k contiguous); into part, or
-// straight into out
+// row gradients: A = W piece (rows k), B = delta (k contiguous); into part, or,
+// with e.out and one split, straight into out
 void vocab_dx(const Launch& L, int type, const VGemm& g, const VEpi& e);
 // matrix gradient: A = packed rows (rows k), B = delta (rows k); into out, or
 // into part where g.splits > 1
@@ -138,11 +148,12 @@ void vocab_delta(const Launch& L, int type, const VRows& r, const float* z, long
 // delta at the targets within the piece [v0, v0 + Vc)
 void vocab_fix(const Launch& L, int type, const VRows& r, const VTarget& t, int v0,
                int Vc, void* d, long long ldd);
-// out(row) = gscale (sum over splits, and over the dup copy) part(row);
+// out(row) = gscale (sum over splits, and over the dup copy) part(row) of the
+// partials that product g wrote with e; rows: of out, those counted of them
+// where counted.  If e.out, nothing where g had one split, which wrote out.
 // idx: destination row of a packed row, null: itself; and the loss, unless null
-void vocab_finish(const Launch& L, int type, const VocabState* st, const float* part,
-                  int splits, long long split_stride, long long ldp, int dup, int rows,
-                  int dyn, int D, const int* idx, void* out, long long ldo,
+void vocab_finish(const Launch& L, int type, const VGemm& g, const VEpi& e, int dup, int rows,
+                  int counted, int D, const int* idx, void* out, long long ldo,
                   int accumulate, const VRows* r, float* loss);
 
 // ---------------------------------------------------------------- embedding

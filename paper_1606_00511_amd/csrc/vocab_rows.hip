@@ -668,10 +668,15 @@ extern "C" __global__ __launch_bounds__(256) void hf_vocab_fix_bf16(VRows r, VTa
 // order.  With one partial per thread in turn, 128 partials took 36 us of
 // latency; G = 8 takes 5.
 namespace {
+struct VParts {
+  const float* part;
+  long long ldp;
+  int splits, smax, n, rn, dyn;   // of the product: n rows in tiles of rn
+  int direct;                     // one split: nothing is left to do
+};
 template <class E, int G>
-__device__ __forceinline__ void finish_body(const VocabState* st, const float* part, int splits,
-                                            long long ss, long long ldp, int dup, int rows,
-                                            int dyn, int D, const int* idx, E* out,
+__device__ __forceinline__ void finish_body(const VocabState* st, const VParts& p, int dup,
+                                            int rows, int counted, int D, const int* idx, E* out,
                                             long long ldo, int accumulate,
                                             const float* row_loss, int T, float* loss) {
   if (loss && blockIdx.x == gridDim.x - 1) {
@@ -681,47 +686,58 @@ __device__ __forceinline__ void finish_body(const VocabState* st, const float* p
   constexpr int QB = 256 / G;           // column groups per workgroup
   __shared__ f32x4 sums[G > 1 ? 256 : 1];
   const int q = (D + 3) / 4, grp = threadIdx.x / QB;
-  const long long i = (long long)blockIdx.x * QB + threadIdx.x % QB;
-  const int j = (int)(i / q), c = 4 * (int)(i % q);
-  const bool in = j < (dyn ? min(st->n, rows) : rows);
+  if (counted) rows = min(st->n, rows);
+  const int gy = (p.n + p.rn - 1) / p.rn;
+  const int gya = p.dyn == 1 ? (st->n + p.rn - 1) / p.rn : gy;
+  const int splits = splits_of(p.splits, p.smax, gy, gya);
+  if (p.direct && splits == 1) return;
+  const size_t ss = (size_t)gya * p.rn * p.ldp;
   const int parts = dup ? 2 * splits : splits;
-  f32x4 s = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-  if (in) {
-    constexpr int U = G > 1 ? 8 : 4;
-    for (int z0 = grp; z0 < parts; z0 += U * G) {
-      f32x4 v[U];
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int z = min(z0 + u * G, parts - 1), zz = z < splits ? z : z - splits;
-        const size_t row = z < splits ? j : dup + j;
-        v[u] = *(const f32x4*)(part + zz * ss + row * ldp + c);
-      }
-#pragma unroll
-      for (int u = 0; u < U; ++u)
-        if (z0 + u * G < parts) s += v[u];
-    }
-  }
-  if constexpr (G > 1) {
-    sums[threadIdx.x] = s;
-    __syncthreads();
-    if (grp) return;
-    for (int k = 1; k < G; ++k) s += sums[k * QB + threadIdx.x];
-  }
-  if (!in) return;
   const float g = st->gscale;
-  E* o = out + (size_t)(idx ? idx[j] : j) * ldo + c;
+  // (once, except where the direct store was likelier)
+  for (long long i0 = (long long)blockIdx.x * QB; i0 < (long long)rows * q;
+       i0 += (long long)gridDim.x * QB) {
+    const long long i = i0 + threadIdx.x % QB;
+    const int j = (int)(i / q), c = 4 * (int)(i % q);
+    const bool in = j < rows;
+    f32x4 s = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    if (in) {
+      constexpr int U = G > 1 ? 8 : 4;
+      for (int z0 = grp; z0 < parts; z0 += U * G) {
+        f32x4 v[U];
 #pragma unroll
-  for (int e = 0; e < 4; ++e)
-    if (c + e < D) put(o + e, s[e] * g + (accumulate ? to_f(o[e]) : 0.0f));
+        for (int u = 0; u < U; ++u) {
+          const int z = min(z0 + u * G, parts - 1), zz = z < splits ? z : z - splits;
+          const size_t row = z < splits ? j : dup + j;
+          v[u] = *(const f32x4*)(p.part + zz * ss + row * p.ldp + c);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+          if (z0 + u * G < parts) s += v[u];
+      }
+    }
+    if constexpr (G > 1) {
+      __syncthreads();
+      sums[threadIdx.x] = s;
+      __syncthreads();
+      if (!grp)
+        for (int k = 1; k < G; ++k) s += sums[k * QB + threadIdx.x];
+    }
+    if (!in || grp) continue;
+    E* o = out + (size_t)(idx ? idx[j] : j) * ldo + c;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (c + e < D) put(o + e, s[e] * g + (accumulate ? to_f(o[e]) : 0.0f));
+  }
 }
 }  // namespace
 #define HF_FINISH(SUF, E, G)                                                               \
   extern "C" __global__ __launch_bounds__(256) void hf_vocab_finish_##SUF(                 \
-      const VocabState* st, const float* part, int splits, long long ss, long long ldp,    \
-      int dup, int rows, int dyn, int D, const int* idx, E* out, long long ldo,            \
-      int accumulate, const float* row_loss, int T, float* loss) {                         \
-    finish_body<E, G>(st, part, splits, ss, ldp, dup, rows, dyn, D, idx, out, ldo,         \
-                      accumulate, row_loss, T, loss);                                      \
+      const VocabState* st, VParts p, int dup, int rows, int counted, int D,               \
+      const int* idx, E* out, long long ldo, int accumulate, const float* row_loss, int T, \
+      float* loss) {                                                                       \
+    finish_body<E, G>(st, p, dup, rows, counted, D, idx, out, ldo, accumulate, row_loss,   \
+                      T, loss);                                                            \
   }
 HF_FINISH(f32, float, 1)
 HF_FINISH(f32_g8, float, 8)
@@ -840,23 +856,25 @@ void vocab_fix(const Launch& L, int type, const VRows& r, const VTarget& t, int 
     HF_LAUNCH("hf_vocab_fix", hf_vocab_fix_bf16, grid, 256, r, t, v0, Vc, (bf16_t*)d, ldd);
 }
 
-void vocab_finish(const Launch& L, int type, const VocabState* st, const float* part, int splits,
-                  long long ss, long long ldp, int dup, int rows, int dyn, int D, const int* idx,
-                  void* out, long long ldo, int accumulate, const VRows* r, float* loss) {
-  const bool g8 = (dup ? 2 : 1) * splits >= 16;
-  const long long grid =
-      ((long long)rows * ((D + 3) / 4) * (g8 ? 8 : 1) + 255) / 256 + (loss ? 1 : 0);
+void vocab_finish(const Launch& L, int type, const VGemm& g, const VEpi& e, int dup, int rows,
+                  int counted, int D, const int* idx, void* out, long long ldo, int accumulate,
+                  const VRows* r, float* loss) {
+  const VParts p = {e.part, e.ldp, g.splits, g.smax, g.N, tile_n(g.tile), g.dyn, e.out != nullptr};
+  const bool g8 = (dup ? 2 : 1) * g.splits >= 16;
+  long long grid = ((long long)rows * ((D + 3) / 4) * (g8 ? 8 : 1) + 255) / 256 + (loss ? 1 : 0);
+  // most often nothing is left to do: 16,384 workgroups that end at once take 12
+  // us, these 4.5
+  if (p.direct && g.splits == 1) grid = std::min<long long>(grid, 2048);
   if (grid < 1) return;
   const float* rl = loss ? r->row_loss : nullptr;
   const int T = loss ? r->T : 0;
   if (type == VT_F32)
     HF_LAUNCH("hf_vocab_finish", (g8 ? hf_vocab_finish_f32_g8 : hf_vocab_finish_f32), grid, 256,
-              st, part, splits, ss, ldp, dup, rows, dyn, D, idx, (float*)out, ldo, accumulate,
-              rl, T, loss);
+              g.st, p, dup, rows, counted, D, idx, (float*)out, ldo, accumulate, rl, T, loss);
   else
     HF_LAUNCH("hf_vocab_finish", (g8 ? hf_vocab_finish_bf16_g8 : hf_vocab_finish_bf16), grid,
-              256, st, part, splits, ss, ldp, dup, rows, dyn, D, idx, (bf16_t*)out, ldo,
-              accumulate, rl, T, loss);
+              256, g.st, p, dup, rows, counted, D, idx, (bf16_t*)out, ldo, accumulate, rl, T,
+              loss);
 }
 
 }  // namespace hfk

@@ -210,6 +210,27 @@ def test_loss_and_gradient(name, rows, V, D):
 
 
 @pytest.mark.parametrize("name", ["fp32", "bf16"])
+@pytest.mark.parametrize("rows,V,D,left", [
+    (3000, 1500, 260, 300), (3000, 1500, 260, 1), (1500, 9000, 300, 700), (5000, 2000, 1024, 257),
+    (20000, 1100, 520, 4000), (2300, 14000, 1200, 2300)])
+def test_mostly_masked(name, rows, V, D, left):
+    """A few counted rows of many: the row gradients' products take more splits
+    than the grid was made for; and a matrix gradient with a last round of few
+    tiles."""
+    torch = T()
+    X, W, y = head_inputs(name, rows, V, D, seed=left)
+    at = torch.randperm(rows, generator=gen(left), device="cuda")[left:]
+    y[at] = IGN
+    X[at] = math.nan                       # what stands there must not matter
+    net = H.HFVocab(V, D, rows, name)
+    q_of, used = label_targets(y, V)
+    ref = reference(X, W, q_of, 1.0, used, left)
+    check_head(name, ref, V, net.hf_vocab_loss_grad(X, W, y))
+    got = net.hf_vocab_loss_grad(X, W, y, need_dW=False)
+    check_head(name, ref, V, (got[0], got[1], got[2], None))
+
+
+@pytest.mark.parametrize("name", ["fp32", "bf16"])
 @pytest.mark.parametrize("rows,V,D,K,tau", [
     (1, 5, 3, 5, 1.0), (2, 1000, 64, 1, 2.0), (64, 130, 64, 16, 2.0), (129, 700, 63, 65, 0.5),
     (300, 2000, 128, 128, 4.0), (513, 257, 72, 100, 1.0), (700, 900, 256, 57, 1.0),

@@ -425,7 +425,6 @@ void head(hf_vocab* c, VRows r, const void* X, int64_t ldx, const void* W, int64
           xe.out = g->dX;
           xe.ldo = g->lddx;
           xe.idx = r.idx;
-          xe.vec = (g->lddx * es) % 16 == 0 && (uintptr_t)g->dX % 16 == 0;
         }
       }
       q.splits = xs.splits;
@@ -478,7 +477,6 @@ void head(hf_vocab* c, VRows r, const void* X, int64_t ldx, const void* W, int64
       pe.out = out;
       pe.ldo = g->lddw;
       pe.accumulate = g->accumulate;
-      pe.vec = (g->lddw * es) % 16 == 0 && (uintptr_t)out % 16 == 0;
       vocab_dw(L, type, q, pe);
       if (q.splits > 1)
         vocab_finish(L, type, q, pe, 0, n, 0, D, nullptr, out, g->lddw, g->accumulate, nullptr,

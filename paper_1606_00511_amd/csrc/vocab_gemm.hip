@@ -140,14 +140,16 @@ __device__ __forceinline__ void store1(float* p, float v) { *p = v; }
 __device__ __forceinline__ float load1(const _Float16* p) { return (float)*p; }
 __device__ __forceinline__ void store1(bf16_t* p, float v) { *p = (bf16_t)f2bf(v); }
 __device__ __forceinline__ void store1(_Float16* p, float v) { *p = (_Float16)v; }
-// whole 16-byte chunks
+// whole 16-byte chunks, of any alignment
 __device__ __forceinline__ void add_chunk(const float* p, float (&v)[4]) {
-  const f32x4 o = *(const f32x4*)p;
+  f32x4 o;
+  __builtin_memcpy(&o, p, 16);
 #pragma unroll
   for (int j = 0; j < 4; ++j) v[j] += o[j];
 }
 __device__ __forceinline__ void add_chunk(const bf16_t* p, float (&v)[8]) {
-  const u32x4 o = *(const u32x4*)p;
+  u32x4 o;
+  __builtin_memcpy(&o, p, 16);
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     v[2 * j] += bf2f(o[j] & 0xffffu);
@@ -163,13 +165,13 @@ __device__ __forceinline__ void store_chunk(_Float16* p, const float (&v)[8]) {
   *(f16x8*)p = w;
 }
 __device__ __forceinline__ void store_chunk(float* p, const float (&v)[4]) {
-  *(f32x4*)p = f32x4{v[0], v[1], v[2], v[3]};
+  __builtin_memcpy(p, v, 16);
 }
 __device__ __forceinline__ void store_chunk(bf16_t* p, const float (&v)[8]) {
   u32x4 w;
 #pragma unroll
   for (int j = 0; j < 4; ++j) w[j] = f2bf(v[2 * j]) | f2bf(v[2 * j + 1]) << 16;
-  *(u32x4*)p = w;
+  __builtin_memcpy(p, &w, 16);
 }
 
 // One 32-row part (rows n0 .. n0 + 31) of a wave's tile to memory: RL columns
@@ -177,45 +179,32 @@ __device__ __forceinline__ void store_chunk(bf16_t* p, const float (&v)[8]) {
 // row r's 16-byte chunk c is at c ^ r % (RL / 4).  Through LDS, a store
 // instruction covers whole 256- or 512-byte runs of rows instead of 16-byte
 // pieces of 32 rows.
-// vec: rows take 16-byte accesses (Mp a whole chunk, or else the rest by
-// elements); add: += what is there; idx: the row of out for each row.
+// add: += what is there; idx: the row of out for each row.
 template <class O, int RL>
 __device__ __forceinline__ void store_part(const float* s, int lane, O* out, long long ldo,
-                                           int n0, int Np, int m0, int Mp, int vec, int add,
+                                           int n0, int Np, int m0, int Mp, int add,
                                            const int* idx = nullptr) {
   constexpr int OPC = 16 / (int)sizeof(O), CPR = RL / OPC, Q = RL / 4;
-  if (vec) {
 #pragma unroll
-    for (int i = 0; i < 32 * CPR / 64; ++i) {
-      const int r = (lane + 64 * i) / CPR, c = (lane + 64 * i) % CPR;
-      const int n = n0 + r, m = m0 + OPC * c;
-      if (n >= Np || m >= Mp) continue;
-      float v[OPC];
+  for (int i = 0; i < 32 * CPR / 64; ++i) {
+    const int r = (lane + 64 * i) / CPR, c = (lane + 64 * i) % CPR;
+    const int n = n0 + r, m = m0 + OPC * c;
+    if (n >= Np || m >= Mp) continue;
+    float v[OPC];
 #pragma unroll
-      for (int k = 0; k < OPC / 4; ++k) {
-        const f32x4 w = *(const f32x4*)(s + r * RL + 4 * ((c * (OPC / 4) + k) ^ (r & (Q - 1))));
+    for (int k = 0; k < OPC / 4; ++k) {
+      const f32x4 w = *(const f32x4*)(s + r * RL + 4 * ((c * (OPC / 4) + k) ^ (r & (Q - 1))));
 #pragma unroll
-        for (int j = 0; j < 4; ++j) v[4 * k + j] = w[j];
-      }
-      O* p = out + (size_t)(idx ? idx[n] : n) * ldo + m;
-      if (m + OPC <= Mp) {
-        if (add) add_chunk(p, v);
-        store_chunk(p, v);
-      } else {
-#pragma unroll
-        for (int j = 0; j < OPC; ++j)
-          if (m + j < Mp) store1(p + j, add ? v[j] + load1(p + j) : v[j]);
-      }
+      for (int j = 0; j < 4; ++j) v[4 * k + j] = w[j];
     }
-  } else {
-    for (int r = 0; r < 32; ++r) {
-      if (n0 + r >= Np) break;
-      O* p = out + (size_t)(idx ? idx[n0 + r] : n0 + r) * ldo + m0;
-      for (int c = lane; c < RL; c += 64) {
-        if (m0 + c >= Mp) break;
-        const float v = s[r * RL + 4 * ((c >> 2) ^ (r & (Q - 1))) + (c & 3)];
-        store1(p + c, add ? v + load1(p + c) : v);
-      }
+    O* p = out + (size_t)(idx ? idx[n] : n) * ldo + m;
+    if (m + OPC <= Mp) {
+      if (add) add_chunk(p, v);
+      store_chunk(p, v);
+    } else {
+#pragma unroll
+      for (int j = 0; j < OPC; ++j)
+        if (m + j < Mp) store1(p + j, add ? v[j] + load1(p + j) : v[j]);
     }
   }
 }
@@ -501,17 +490,17 @@ __device__ __forceinline__ void vgemm_body(const VGemm& s, const VEpi& e) {
     __builtin_amdgcn_wave_barrier();
     const int nb = nt + 32 * b;
     if constexpr (EPI == E_LOGITS)
-      store_part<float, RL>(mine, lane, e.z, e.ldz, nb, Np, mt, Mp, 1, 0);
+      store_part<float, RL>(mine, lane, e.z, e.ldz, nb, Np, mt, Mp, 0);
     else if constexpr (EPI == E_EXPS)
-      store_part<_Float16, RL>(mine, lane, (_Float16*)e.pt, e.ldz, nb, Np, mt, Mp, 1, 0);
+      store_part<_Float16, RL>(mine, lane, (_Float16*)e.pt, e.ldz, nb, Np, mt, Mp, 0);
     else if constexpr (EPI == E_PROBS)
-      store_part<E, RL>(mine, lane, (E*)e.d, e.ldd, nb, Np, mt, Mp, 1, 0);
+      store_part<E, RL>(mine, lane, (E*)e.d, e.ldd, nb, Np, mt, Mp, 0);
     else if constexpr (EPI == E_OUT)
-      store_part<E, RL>(mine, lane, (E*)e.out, e.ldo, nb, Np, mt, Mp, e.vec, e.accumulate);
+      store_part<E, RL>(mine, lane, (E*)e.out, e.ldo, nb, Np, mt, Mp, e.accumulate);
     else if (parts)
-      store_part<float, RL>(mine, lane, part, e.ldp, nb, Np, mt, Mp, 1, e.add);
+      store_part<float, RL>(mine, lane, part, e.ldp, nb, Np, mt, Mp, e.add);
     else if constexpr (EPI == E_ROWS)
-      store_part<E, RL>(mine, lane, (E*)e.out, e.ldo, nb, Np, mt, Mp, e.vec, 0, e.idx);
+      store_part<E, RL>(mine, lane, (E*)e.out, e.ldo, nb, Np, mt, Mp, 0, e.idx);
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
   }

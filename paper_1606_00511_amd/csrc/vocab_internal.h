@@ -79,7 +79,6 @@ struct VEpi {
   long long ldo;
   int accumulate;        // out += rather than =
   const int* idx;        // dX: row of out for a packed row
-  int vec;               // rows of out are 16-byte aligned
 };
 
 // logits of a vocabulary piece: A = W piece (akc), B = packed rows (akc);

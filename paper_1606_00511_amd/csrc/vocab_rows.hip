@@ -165,15 +165,15 @@ extern "C" __global__ __launch_bounds__(1024) void hf_vocab_count(VRows r) {
 // ----------------------------------------------------------------- packing
 namespace {
 // n elements of src to dst (16-byte aligned, dn elements), zeros past n;
-// vec: src is 16-byte aligned.  Called by a whole workgroup of 256.
+// Called by a whole workgroup of 256.
 template <class E>
-__device__ __forceinline__ void copy_row(const E* src, int n, int vec, E* dst, int dn,
+__device__ __forceinline__ void copy_row(const E* src, int n, E* dst, int dn,
                                          E* dst2) {
   constexpr int EPC = 16 / sizeof(E);
   for (int c = threadIdx.x; c < dn / EPC; c += 256) {
     u32x4 v = u32x4{0u, 0u, 0u, 0u};
-    if (vec && EPC * c + EPC <= n) {
-      v = *(const u32x4*)(src + EPC * c);
+    if (EPC * c + EPC <= n) {
+      __builtin_memcpy(&v, src + EPC * c, 16);
     } else {
       E w[EPC];
 #pragma unroll
@@ -190,7 +190,7 @@ __device__ __forceinline__ void copy_row(const E* src, int n, int vec, E* dst, i
 // need.
 constexpr int SELF_ROWS = 256, SELF_TOP = 32;
 template <class E, bool SELF>
-__device__ __forceinline__ void pack_body(const VRows& r, const E* X, long long ldx, int vecx,
+__device__ __forceinline__ void pack_body(const VRows& r, const E* X, long long ldx,
                                           int in_place, E* xp, int Dp, int dup, E* dX,
                                           long long lddx) {
   const int b = blockIdx.x;
@@ -221,7 +221,7 @@ __device__ __forceinline__ void pack_body(const VRows& r, const E* X, long long 
   if (in_place && n == r.T) return;
   if (b < r.T) {
     if (pos >= 0) {
-      copy_row(X + (size_t)b * ldx, r.D, vecx, xp + (size_t)pos * Dp, Dp,
+      copy_row(X + (size_t)b * ldx, r.D, xp + (size_t)pos * Dp, Dp,
                dup ? xp + (size_t)(dup + pos) * Dp : (E*)nullptr);
     } else if (dX) {
       for (int c = threadIdx.x; c < r.D; c += 256) dX[(size_t)b * lddx + c] = (E)0;
@@ -231,31 +231,56 @@ __device__ __forceinline__ void pack_body(const VRows& r, const E* X, long long 
   const int j = n + b - r.T;
   const int end = dup ? dup : (n + VTILE - 1) / VTILE * VTILE;
   if (j < end)
-    copy_row((const E*)nullptr, 0, 0, xp + (size_t)j * Dp, Dp,
+    copy_row((const E*)nullptr, 0, xp + (size_t)j * Dp, Dp,
              dup ? xp + (size_t)(dup + j) * Dp : (E*)nullptr);
 }
 }  // namespace
 
 #define HF_PACK(SUF, E, SELF)                                                             \
   extern "C" __global__ __launch_bounds__(256) void hf_vocab_pack_##SUF(                  \
-      VRows r, const E* X, long long ldx, int vecx, int in_place, E* xp, int Dp, int dup, \
-      E* dX, long long lddx) {                                                            \
-    pack_body<E, SELF>(r, X, ldx, vecx, in_place, xp, Dp, dup, dX, lddx);                 \
+      VRows r, const E* X, long long ldx, int in_place, E* xp, int Dp, int dup, E* dX,    \
+      long long lddx) {                                                                  \
+    pack_body<E, SELF>(r, X, ldx, in_place, xp, Dp, dup, dX, lddx);                       \
   }
 HF_PACK(f32, float, false)
 HF_PACK(f32_self, float, true)
 HF_PACK(bf16, bf16_t, false)
 HF_PACK(bf16_self, bf16_t, true)
 
+// Rows of W, padded with zeros to whole K blocks: chunks of 16 bytes, four a
+// thread on their way, whatever the rows' width (a workgroup per row took 55 us
+// for 50,257 x 1,021 of bf16, 206 MB, and 21 for 58,864 x 214: now 41 and 10).
+namespace {
+constexpr int COPY_U = 4;
+template <class E>
+__device__ __forceinline__ void copy_body(const E* W, long long ldw, int R, int D, E* wp,
+                                          int Dp) {
+  constexpr int EPC = 16 / sizeof(E);
+  const int per = Dp / EPC, n = R * per, i0 = blockIdx.x * (256 * COPY_U) + threadIdx.x;
+  E v[COPY_U][EPC];
+#pragma unroll
+  for (int u = 0; u < COPY_U; ++u) {
+    const int i = min(i0 + 256 * u, n - 1), row = i / per, c = EPC * (i % per);
+    const E* w = W + (size_t)row * ldw + c;
+    if (c + EPC <= D) {
+      __builtin_memcpy(v[u], w, 16);
+    } else {
+#pragma unroll
+      for (int j = 0; j < EPC; ++j) v[u][j] = c + j < D ? w[j] : (E)0;
+    }
+  }
+#pragma unroll
+  for (int u = 0; u < COPY_U; ++u)
+    if (i0 + 256 * u < n) *(u32x4*)(wp + (size_t)(i0 + 256 * u) * EPC) = *(const u32x4*)v[u];
+}
+}  // namespace
 extern "C" __global__ __launch_bounds__(256) void hf_vocab_copy_f32(
-    const float* W, long long ldw, int vec, int D, float* wp, int Dp) {
-  const size_t b = blockIdx.x;
-  copy_row(W + b * ldw, D, vec, wp + b * Dp, Dp, (float*)nullptr);
+    const float* W, long long ldw, int R, int D, float* wp, int Dp) {
+  copy_body(W, ldw, R, D, wp, Dp);
 }
 extern "C" __global__ __launch_bounds__(256) void hf_vocab_copy_bf16(
-    const bf16_t* W, long long ldw, int vec, int D, bf16_t* wp, int Dp) {
-  const size_t b = blockIdx.x;
-  copy_row(W + b * ldw, D, vec, wp + b * Dp, Dp, (bf16_t*)nullptr);
+    const bf16_t* W, long long ldw, int R, int D, bf16_t* wp, int Dp) {
+  copy_body(W, ldw, R, D, wp, Dp);
 }
 
 // ---------------------------------------------------- the targets' logits
@@ -266,7 +291,7 @@ namespace {
 struct VDots {
   const void *X, *xp, *W;
   long long ldx, ldw;
-  int Dp, vec;
+  int Dp;
 };
 template <class E, int U, int LANES>
 __device__ __forceinline__ void dots(const VRows& r, const VDots& q, int j, const int (&id)[U],
@@ -275,38 +300,30 @@ __device__ __forceinline__ void dots(const VRows& r, const VDots& q, int j, cons
   const int lane = threadIdx.x & (LANES - 1);
   const E* x = q.X && r.st->n == r.T ? (const E*)q.X + (size_t)j * q.ldx
                                      : (const E*)q.xp + (size_t)j * q.Dp;
-  const E* w[U];
+  const E* w[U];          // (no target: the first row, its product unused)
 #pragma unroll
   for (int u = 0; u < U; ++u) {
     w[u] = (const E*)q.W + (size_t)max(id[u], 0) * q.ldw;
     s[u] = 0.0f;
   }
-  // a lane has the same chunks in the same order whether its loads are of 16
-  // bytes or single elements
   for (int c = EPC * lane; c < r.D; c += LANES * EPC) {
     E a[EPC], b[U][EPC];
-    const bool whole = c + EPC <= r.D;
+    if (c + EPC <= r.D) {
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      if (id[u] < 0) continue;
-      if (q.vec && whole) {
-        *(u32x4*)b[u] = *(const u32x4*)(w[u] + c);
-      } else {
-#pragma unroll
-        for (int i = 0; i < EPC; ++i) b[u][i] = c + i < r.D ? w[u][c + i] : (E)0;
-      }
-    }
-    if (whole) {
-      *(u32x4*)a = *(const u32x4*)(x + c);
+      for (int u = 0; u < U; ++u) __builtin_memcpy(b[u], w[u] + c, 16);
+      __builtin_memcpy(a, x + c, 16);
     } else {
 #pragma unroll
-      for (int i = 0; i < EPC; ++i) a[i] = c + i < r.D ? x[c + i] : (E)0;
+      for (int i = 0; i < EPC; ++i) {
+        a[i] = c + i < r.D ? x[c + i] : (E)0;
+#pragma unroll
+        for (int u = 0; u < U; ++u) b[u][i] = c + i < r.D ? w[u][c + i] : (E)0;
+      }
     }
 #pragma unroll
     for (int u = 0; u < U; ++u)
-      if (id[u] >= 0)
 #pragma unroll
-        for (int i = 0; i < EPC; ++i) s[u] += to_f(a[i]) * to_f(b[u][i]);
+      for (int i = 0; i < EPC; ++i) s[u] += to_f(a[i]) * to_f(b[u][i]);
   }
 #pragma unroll
   for (int u = 0; u < U; ++u) {
@@ -335,7 +352,7 @@ __device__ __forceinline__ void tlogit_row(const VRows& r, const VDots& q, int j
 }
 // A row of W that one load of a wave covers (1 KiB) leaves lanes without work:
 // a quarter of a wave each then (7,276 rows of 57 targets, 128 columns of bf16:
-// 56 -> 23 us; 2,048 columns keep the wave, at 6.9 TB/s).
+// 56 -> 27 us; 2,048 columns keep the wave, at 7.1 TB/s).
 template <class E>
 __device__ __forceinline__ void tlogit_body(const VRows& r, const VDots& q, float* zt) {
   const int j = blockIdx.x;
@@ -725,9 +742,19 @@ __device__ __forceinline__ void finish_body(const VocabState* st, const VParts& 
     }
     if (!in || grp) continue;
     E* o = out + (size_t)(idx ? idx[j] : j) * ldo + c;
+    E w[4] = {};
+    if (accumulate) {
+      if (c + 4 <= D) __builtin_memcpy(w, o, sizeof w);
+      else
+        for (int e = 0; e < 3; ++e)
+          if (c + e < D) w[e] = o[e];
+    }
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
-      if (c + e < D) put(o + e, s[e] * g + (accumulate ? to_f(o[e]) : 0.0f));
+    for (int e = 0; e < 4; ++e) put(w + e, s[e] * g + (accumulate ? to_f(w[e]) : 0.0f));
+    if (c + 4 <= D) __builtin_memcpy(o, w, sizeof w);
+    else
+      for (int e = 0; e < 3; ++e)
+        if (c + e < D) o[e] = w[e];
   }
 }
 }  // namespace
@@ -754,12 +781,6 @@ HF_FINISH(bf16_g8, bf16_t, 8)
   } while (0)
 
 namespace {
-inline int vec16(const void* p, long long ld, int es) {
-  return ((uintptr_t)p & 15) == 0 && (ld * es) % 16 == 0;
-}
-}  // namespace
-
-namespace {
 constexpr int SUM_ROWS = 16;      // rows whose losses one workgroup forms and sums
 }  // namespace
 
@@ -777,22 +798,22 @@ void vocab_pack_rows(const Launch& L, int type, const VRows& r, bool counted, co
   const int grid = r.T + (dup ? dup : VTILE), place = in_place;
   if (type == VT_F32)
     HF_LAUNCH("hf_vocab_pack", (counted ? hf_vocab_pack_f32 : hf_vocab_pack_f32_self), grid,
-              256, r, (const float*)X, ldx, vec16(X, ldx, 4), place, (float*)xp, Dp, dup,
+              256, r, (const float*)X, ldx, place, (float*)xp, Dp, dup,
               (float*)dX, lddx);
   else
     HF_LAUNCH("hf_vocab_pack", (counted ? hf_vocab_pack_bf16 : hf_vocab_pack_bf16_self), grid,
-              256, r, (const bf16_t*)X, ldx, vec16(X, ldx, 2), place, (bf16_t*)xp, Dp, dup,
+              256, r, (const bf16_t*)X, ldx, place, (bf16_t*)xp, Dp, dup,
               (bf16_t*)dX, lddx);
 }
 
 void vocab_pack_matrix(const Launch& L, int type, const void* W, long long ldw, int R, int D,
                        void* wp, int Dp) {
+  const int es = type == VT_F32 ? 4 : 2, chunks = R * (Dp * es / 16);   // of 256 MiB at most
+  const int grid = (chunks + 256 * COPY_U - 1) / (256 * COPY_U);
   if (type == VT_F32)
-    HF_LAUNCH("hf_vocab_copy", hf_vocab_copy_f32, R, 256, (const float*)W, ldw,
-              vec16(W, ldw, 4), D, (float*)wp, Dp);
+    HF_LAUNCH("hf_vocab_copy", hf_vocab_copy_f32, grid, 256, (const float*)W, ldw, R, D, (float*)wp, Dp);
   else
-    HF_LAUNCH("hf_vocab_copy", hf_vocab_copy_bf16, R, 256, (const bf16_t*)W, ldw,
-              vec16(W, ldw, 2), D, (bf16_t*)wp, Dp);
+    HF_LAUNCH("hf_vocab_copy", hf_vocab_copy_bf16, grid, 256, (const bf16_t*)W, ldw, R, D, (bf16_t*)wp, Dp);
 }
 
 bool vocab_row_loss(const Launch& L, int type, const VRows& r, const float2* stat, int ldstat,
@@ -800,8 +821,7 @@ bool vocab_row_loss(const Launch& L, int type, const VRows& r, const float2* sta
                     const void* X, long long ldx, const void* xp, int Dp, const void* W,
                     long long ldw, float* loss) {
   if (r.T < 1) return false;
-  const int es = type == VT_F32 ? 4 : 2;
-  const VDots q = {X, xp, W, ldx, ldw, Dp, vec16(W, ldw, es)};
+  const VDots q = {X, xp, W, ldx, ldw, Dp};
   if (!z && r.K > 1) {
     if (type == VT_F32)
       HF_LAUNCH("hf_vocab_tlogit", hf_vocab_tlogit_f32, r.T, 256, r, q, t.zt);

@@ -589,6 +589,8 @@ def zipf(n, V, seed=0):
 @pytest.mark.parametrize("name", ["fp32", "bf16"])
 @pytest.mark.parametrize("rows,V,D", [(1, 1, 1), (1, 100, 4096), (5, 10, 3), (63, 50, 257),
                                       (1000, 5000, 64), (1024, 4096, 520), (1025, 4095, 130),
+                                      (500, 80, 8), (500, 80, 9), (2000, 70, 255), (1200, 90, 511),
+                                      (1200, 90, 513), (1200, 90, 519), (1100, 60, 1021),
                                       (20000, 1000, 72), (30011, 200003, 24)])
 def test_embedding_and_gradient(name, rows, V, D):
     torch = T()

@@ -452,7 +452,8 @@ int hf_prof_get(hf_ctx* ctx, int32_t i, const char** name, int64_t* launches,
  * into a graph.  hf_vocab_set_stream orders the new stream behind the
  * context's calls on the old one (which must still exist), as they share the
  * workspace; captured calls, and graphs that share a workspace, are the
- * caller's to order.  The current device must be the stream's.  Repeated calls give the same bits, whatever the workspace's size.
+ * caller's to order.  The current device must be the stream's.  Repeated calls
+ * give the same bits, whatever the workspace's size.
  */
 typedef struct hf_vocab hf_vocab;
 

@@ -179,7 +179,8 @@ def mask_rows(y, how, seed=5):
         return y
     if how == "all":
         return torch.full_like(y, IGN)
-    gone = torch.rand(y.shape, generator=gen(seed), device="cuda") < 0.4
+    share = 0.95 if how == "most" else 0.4
+    gone = torch.rand(y.shape, generator=gen(seed), device="cuda") < share
     return torch.where(gone, IGN, y)
 
 
@@ -541,11 +542,12 @@ def test_same_bits(name, rows, V, D):
 
 
 @pytest.mark.parametrize("name", ["fp32", "bf16"])
-def test_captured_and_replayed(name):
+@pytest.mark.parametrize("rows", [200, 3000])
+def test_captured_and_replayed(name, rows):
     """Loss, distillation, embedding and their gradients in one graph, replayed
-    on new inputs between eager calls of the same context."""
+    on new inputs and masks between eager calls of the same context."""
     torch = T()
-    rows, V, D, K = 200, 1100, 96, 12
+    V, D, K = 1100, 96, 12
     net = H.HFVocab(V, D, rows, name)
     X, W, y = head_inputs(name, rows, V, D)
     ids, t = teacher(rows, V, K)
@@ -569,7 +571,7 @@ def test_captured_and_replayed(name):
         nX, nW, ny = head_inputs(name, rows, V, D, seed=20 + seed)
         X.copy_(nX)
         W.copy_(nW)
-        y.copy_(mask_rows(ny, "some" if seed % 2 else "none"))
+        y.copy_(mask_rows(ny, ("none", "some", "most", "all")[seed]))
         g.replay()
         got = [o.clone() for o in outs]
         torch.cuda.synchronize()

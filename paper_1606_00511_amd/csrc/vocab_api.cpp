@@ -452,15 +452,21 @@ void head(hf_vocab* c, VRows r, const void* X, int64_t ldx, const void* W, int64
     int n1 = pn;
     if (!q.thin) {
       ws = shape_for(type, D, pn, q.K, true, false);
-      // a last round of few tiles of 256 leaves most units idle: its rows of dW
-      // are a product of their own then, of a shape of their own (788 tiles,
-      // K = 2,251: 310 -> 282 us)
-      const int64_t tm = (D + 255) / 256, whole = tm * ((pn + 255) / 256) / 256 * 256 / tm * 256;
-      if (ws.tile == TILE_BIG && ws.splits == 1 && whole > 0 && whole < pn) {
+      // a last round of few tiles leaves most units idle: its rows of dW are a
+      // product of their own then, of a shape of their own (788 tiles of 256, K
+      // = 2,251: 310 -> 282 us)
+      double least = ws.us;
+      for (int tile : {TILE_BIG, TILE_SMALL}) {
+        const int64_t rn = tile_n(tile), tm = (D + tile_m(tile) - 1) / tile_m(tile);
+        const int64_t slots = tile == TILE_BIG ? 256 : 512;
+        const int64_t whole = tm * ((pn + rn - 1) / rn) / slots * slots / tm * rn;
+        if (whole <= 0 || whole >= pn) continue;
         const Shape a = shape_for(type, D, whole, q.K, true, false);
-        rest = shape_for(type, D, pn - whole, q.K, true, false);
-        if (a.us + rest.us + 4.0 < ws.us) {
+        const Shape b = shape_for(type, D, pn - whole, q.K, true, false);
+        if (a.us + b.us + 4.0 < least) {
+          least = a.us + b.us + 4.0;
           ws = a;
+          rest = b;
           n1 = (int)whole;
         }
       }

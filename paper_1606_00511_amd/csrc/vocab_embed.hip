@@ -21,6 +21,7 @@ namespace {
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef u32x4 __attribute__((aligned(2))) loose;      // of any alignment
 
 __device__ __forceinline__ uint32_t f2bf(float f) {
   return __builtin_bit_cast(uint16_t, (__bf16)f);
@@ -37,7 +38,7 @@ constexpr int IGNORE = -100;
 // a row's end takes the last 16 bytes; it and the lane before it then compute
 // the same, and write the same, in one instruction.  So VEC is for rows whose
 // end shares a strip with a whole chunk (30,000 x 1,021 of bf16: embedding
-// 32 -> 18 us, gradient 66 -> 58).
+// 32 -> 18 us, gradient 66 -> 58).  STREAM: past the caches.
 template <class E, bool VEC>
 struct Strip {
   static constexpr int EPC = 16 / (int)sizeof(E);
@@ -52,10 +53,14 @@ struct Strip {
   struct Raw {               // as loaded: 4 registers for a lane's columns
     E v[EPC];
   };
+  template <bool STREAM>
   __device__ static __forceinline__ Raw raw(const E* row, int strip, int lane, int D) {
     Raw w = {};
     if constexpr (VEC) {
-      if (col(strip, lane, 0) < D) __builtin_memcpy(&w, row + first(strip, lane, D), 16);
+      if (col(strip, lane, 0) < D) {
+        const loose* const p = (const loose*)(row + first(strip, lane, D));
+        w = __builtin_bit_cast(Raw, STREAM ? __builtin_nontemporal_load(p) : *p);
+      }
     } else {
 #pragma unroll
       for (int e = 0; e < EPC; ++e) {
@@ -67,17 +72,23 @@ struct Strip {
   }
   __device__ static __forceinline__ void load(const E* row, int strip, int lane, int D,
                                               float (&v)[EPC]) {
-    const Raw w = raw(row, strip, lane, D);
+    const Raw w = raw<false>(row, strip, lane, D);
 #pragma unroll
     for (int e = 0; e < EPC; ++e) v[e] = to_f(w.v[e]);
   }
+  template <bool STREAM>
   __device__ static __forceinline__ void store(E* row, int strip, int lane, int D,
                                                const float (&v)[EPC]) {
     if constexpr (VEC) {
       E w[EPC];
 #pragma unroll
       for (int e = 0; e < EPC; ++e) put(w + e, v[e]);
-      if (col(strip, lane, 0) < D) __builtin_memcpy(row + first(strip, lane, D), w, 16);
+      if (col(strip, lane, 0) < D) {
+        loose* const p = (loose*)(row + first(strip, lane, D));
+        const u32x4 x = __builtin_bit_cast(u32x4, w);
+        if (STREAM) __builtin_nontemporal_store(x, p);
+        else *p = x;
+      }
     } else {
 #pragma unroll
       for (int e = 0; e < EPC; ++e) {
@@ -89,7 +100,7 @@ struct Strip {
 };
 
 // One strip of one row per wave.
-template <class E, bool VEC>
+template <class E, bool VEC, bool STREAM>
 __device__ __forceinline__ void embed_body(const E* table, long long lde, int V, int D,
                                            const int32_t* tok, int T, int strips, float scale,
                                            E* out, long long ldo, VocabState* st) {
@@ -109,21 +120,23 @@ __device__ __forceinline__ void embed_body(const E* table, long long lde, int V,
   }
 #pragma unroll
   for (int e = 0; e < S::EPC; ++e) v[e] *= scale;
-  S::store(out + (size_t)t * ldo, strip, lane, D, v);
+  S::template store<STREAM>(out + (size_t)t * ldo, strip, lane, D, v);
 }
 
 }  // namespace
 
-#define HF_EMBED(SUF, E, VEC)                                                            \
+#define HF_EMBED(SUF, E, VEC, STREAM)                                                    \
   extern "C" __global__ __launch_bounds__(256) void hf_vocab_embed_##SUF(                \
       const E* table, long long lde, int V, int D, const int32_t* tok, int T, int strips, \
       float scale, E* out, long long ldo, VocabState* st) {                              \
-    embed_body<E, VEC>(table, lde, V, D, tok, T, strips, scale, out, ldo, st);           \
+    embed_body<E, VEC, STREAM>(table, lde, V, D, tok, T, strips, scale, out, ldo, st);   \
   }
-HF_EMBED(f32, float, false)
-HF_EMBED(f32_v, float, true)
-HF_EMBED(bf16, bf16_t, false)
-HF_EMBED(bf16_v, bf16_t, true)
+HF_EMBED(f32, float, false, false)
+HF_EMBED(f32_v, float, true, false)
+HF_EMBED(f32_s, float, true, true)
+HF_EMBED(bf16, bf16_t, false, false)
+HF_EMBED(bf16_v, bf16_t, true, false)
+HF_EMBED(bf16_s, bf16_t, true, true)
 
 // -------------------------------------------------------------------- sort
 // Least-significant digit first, two digits of `bits` bits.  The key is the
@@ -154,7 +167,7 @@ __device__ __forceinline__ void fill_rows(const Fill& f, int block, int blocks) 
     char* row = f.p + (size_t)v * f.ld;
     const u32x4 zero = u32x4{0u, 0u, 0u, 0u};
     for (int i = 16 * lane; i < f.bytes; i += 1024) {
-      if (i + 16 <= f.bytes) __builtin_memcpy(row + i, &zero, 16);
+      if (i + 16 <= f.bytes) *(loose*)(row + i) = zero;
       else
         for (int j = i; j < f.bytes; j += 2) *(uint16_t*)(row + j) = 0;
     }
@@ -352,13 +365,13 @@ __device__ __forceinline__ void emit(E* row, int strip, int lane, int D, float s
 #pragma unroll
     for (int e = 0; e < S::EPC; ++e) acc[e] += old[e];
   }
-  S::store(row, strip, lane, D, acc);
+  S::template store<false>(row, strip, lane, D, acc);
 }
 
 // One run and strip.  part[2 run]: the sum of the token that began before the
 // run (or fills it from its start and goes on); part[2 run + 1]: of the one
 // that begins within it and goes on.
-template <class E, bool VEC>
+template <class E, bool VEC, bool STREAM>
 __device__ __forceinline__ void runs_body(const int* key, const int* pos, int RUN, int T, int V,
                                           int D, int strips, float scale, const E* dout,
                                           long long ldd, float* part, E* dE, long long lde,
@@ -383,7 +396,7 @@ __device__ __forceinline__ void runs_body(const int* key, const int* pos, int RU
 #pragma unroll
     for (int u = 0; u < U; ++u)
       if (i0 + u < n)
-        v[u] = S::raw(dout + (size_t)__builtin_amdgcn_readlane(p, 1 + i0 + u) * ldd, strip, lane,
+        v[u] = S::template raw<STREAM>(dout + (size_t)__builtin_amdgcn_readlane(p, 1 + i0 + u) * ldd, strip, lane,
                       D);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -493,23 +506,33 @@ __device__ __forceinline__ void join_body(const int* key, int RUN, int T, int V,
 }
 }  // namespace
 
-#define HF_EMBED_GRAD(SUF, E, VEC)                                                       \
+// _s: dout past the caches, where it and dE do not fit the last-level one, and
+// partial sums and dE stay in them (131,072 x 2,048 of bf16: 173 -> 126 us, and
+// the join 26 -> 18; whole calls of 8,192 rows, 32,000 x 4,096: 86 -> 77; but
+// 30,000 rows, 50,257 x 768 of fp32, 246 MB: 65 -> 75)
+#define HF_EMBED_RUNS(SUF, E, VEC, STREAM)                                               \
   extern "C" __global__ __launch_bounds__(256) void hf_vocab_embed_runs_##SUF(           \
       const int* key, const int* pos, int RUN, int T, int V, int D, int strips, float scale, \
       const E* dout, long long ldd, float* part, E* dE, long long lde, int accumulate) { \
-    runs_body<E, VEC>(key, pos, RUN, T, V, D, strips, scale, dout, ldd, part, dE, lde,   \
-                      accumulate);                                                       \
-  }                                                                                      \
+    runs_body<E, VEC, STREAM>(key, pos, RUN, T, V, D, strips, scale, dout, ldd, part, dE, \
+                              lde, accumulate);                                          \
+  }
+#define HF_EMBED_JOIN(SUF, E, VEC)                                                       \
   extern "C" __global__ __launch_bounds__(256, 5) void hf_vocab_embed_join_##SUF(        \
       const int* key, int RUN, int T, int V, int D, int strips, float scale,             \
-      const float* part,                                                                 \
-      E* dE, long long lde, int accumulate) {                                            \
+      const float* part, E* dE, long long lde, int accumulate) {                         \
     join_body<E, VEC>(key, RUN, T, V, D, strips, scale, part, dE, lde, accumulate);      \
   }
-HF_EMBED_GRAD(f32, float, false)
-HF_EMBED_GRAD(f32_v, float, true)
-HF_EMBED_GRAD(bf16, bf16_t, false)
-HF_EMBED_GRAD(bf16_v, bf16_t, true)
+HF_EMBED_RUNS(f32, float, false, false)
+HF_EMBED_RUNS(f32_v, float, true, false)
+HF_EMBED_RUNS(f32_s, float, true, true)
+HF_EMBED_RUNS(bf16, bf16_t, false, false)
+HF_EMBED_RUNS(bf16_v, bf16_t, true, false)
+HF_EMBED_RUNS(bf16_s, bf16_t, true, true)
+HF_EMBED_JOIN(f32, float, false)
+HF_EMBED_JOIN(f32_v, float, true)
+HF_EMBED_JOIN(bf16, bf16_t, false)
+HF_EMBED_JOIN(bf16_v, bf16_t, true)
 
 // ------------------------------------------------------------- launchers
 namespace {
@@ -553,12 +576,18 @@ void vocab_embed(const Launch& L, int type, const void* E, long long lde, int V,
   const int es = type == VT_F32 ? 4 : 2, strips = strips_of(D, es);
   const bool vec = chunks(D, es);
   const long long grid = ((long long)T * strips + 3) / 4;
-  if (type == VT_F32)
-    HF_LAUNCH("hf_vocab_embed", (vec ? hf_vocab_embed_f32_v : hf_vocab_embed_f32), grid, 256,
-              (const float*)E, lde, V, D, tok, T, strips, scale, (float*)out, ldo, st);
-  else
-    HF_LAUNCH("hf_vocab_embed", (vec ? hf_vocab_embed_bf16_v : hf_vocab_embed_bf16), grid, 256,
-              (const bf16_t*)E, lde, V, D, tok, T, strips, scale, (bf16_t*)out, ldo, st);
+  // _s: much output does not take the place of frequent tokens' rows of E in the
+  // caches (65,536 x 4,096 of bf16: 179 -> 104 us); little stays for its reader
+  const bool stream = (long long)T * D * es > L2_BYTES;
+#define HF_EMB(SUF, E_T)                                                                   \
+  HF_LAUNCH("hf_vocab_embed",                                                              \
+            (vec && stream ? hf_vocab_embed_##SUF##_s                                      \
+             : vec         ? hf_vocab_embed_##SUF##_v                                      \
+                           : hf_vocab_embed_##SUF),                                        \
+            grid, 256, (const E_T*)E, lde, V, D, tok, T, strips, scale, (E_T*)out, ldo, st)
+  if (type == VT_F32) HF_EMB(f32, float);
+  else HF_EMB(bf16, bf16_t);
+#undef HF_EMB
 }
 
 void vocab_embed_grad(const Launch& L, int type, const int32_t* tok, int T, int V, int D,
@@ -599,10 +628,13 @@ void vocab_embed_grad(const Launch& L, int type, const int32_t* tok, int T, int 
   const int RUN = (long long)((T + RUN_MAX - 1) / RUN_MAX) * strips < 2048 ? RUN_MIN : RUN_MAX;
   const int runs = (T + RUN - 1) / RUN;
   const long long units = (long long)runs * strips;
+  const bool stream = ((long long)T + V) * D * es > L3_BYTES;
 #define HF_EG(SUF, E)                                                                         \
   do {                                                                                        \
     HF_LAUNCH("hf_vocab_embed_runs",                                                          \
-              (vec ? hf_vocab_embed_runs_##SUF##_v : hf_vocab_embed_runs_##SUF),              \
+              (vec && stream ? hf_vocab_embed_runs_##SUF##_s                                  \
+               : vec         ? hf_vocab_embed_runs_##SUF##_v                                  \
+                             : hf_vocab_embed_runs_##SUF),                                    \
               (units + 3) / 4, 256, (const int*)s.key, (const int*)s.pos, RUN, T, V, D, strips, \
               scale, (const E*)dout, ldd, s.part, (E*)dE, lde, accumulate);                   \
     if (runs > 1)                                                                             \

@@ -24,6 +24,8 @@ inline int tile_n(int t) {
 // Columns of one entry of row statistics: a wave's part of a vocabulary tile.
 inline int tile_stat(int t) { return t == TILE_BIG ? 128 : t == TILE_SMALL ? 64 : 32; }
 constexpr int VMAX_SPLITS = 64;
+constexpr long long L2_BYTES = 32ll << 20;   // the level-2 caches of the 8 XCDs
+constexpr long long L3_BYTES = 256ll << 20;  // the last-level cache
 
 // Device scalars of a call.
 struct VocabState {
@@ -78,6 +80,7 @@ struct VEpi {
   void* out;             // final output, scaled by st->gscale
   long long ldo;
   int accumulate;        // out += rather than =
+  int stream;            // (dW of few rows) out past the caches
   const int* idx;        // dX: row of out for a packed row
 };
 

@@ -396,8 +396,8 @@ __device__ __forceinline__ void runs_body(const int* key, const int* pos, int RU
 #pragma unroll
     for (int u = 0; u < U; ++u)
       if (i0 + u < n)
-        v[u] = S::template raw<STREAM>(dout + (size_t)__builtin_amdgcn_readlane(p, 1 + i0 + u) * ldd, strip, lane,
-                      D);
+        v[u] = S::template raw<STREAM>(
+            dout + (size_t)__builtin_amdgcn_readlane(p, 1 + i0 + u) * ldd, strip, lane, D);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       if (i0 + u >= n) break;

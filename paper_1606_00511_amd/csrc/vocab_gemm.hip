@@ -226,11 +226,11 @@ __device__ __forceinline__ void store_part(const float* s, int lane, O* out, lon
 enum { E_LOGITS, E_EXPS, E_PROBS, E_PART, E_OUT, E_STREAM, E_ROWS };
 
 // The tile (tm, tn) and split this workgroup computes, of gy tiles of n that
-// have rows and gz splits; false: none.  Consecutive workgroups go to the 8 XCDs in turn;
-// each XCD gets a contiguous eighth of the logical order, which walks groups
-// of 8 tiles of n, m by m, so that the workgroups resident on an XCD share
-// their operand panels in its L2.  Tiles without rows take no place in the
-// order (2,251 of 3,001 rows counted, 50,257 x 1,024: 301 -> 222 us).
+// have rows and gz splits; false: none.  Consecutive workgroups go to the 8
+// XCDs in turn; each XCD gets a contiguous eighth of the logical order, which
+// walks groups of 8 tiles of n, m by m, so that the workgroups resident on an
+// XCD share their operand panels in its L2.  Tiles without rows take no place
+// in the order (2,251 of 3,001 rows counted, 50,257 x 1,024: 301 -> 222 us).
 __device__ __forceinline__ bool tile_of(int gy, int gz, int& tm, int& tn, int& tz) {
   const int gx = gridDim.x;
   const int T = gx * gy * gz;
@@ -536,7 +536,7 @@ __device__ __forceinline__ void vgemm_body(const VGemm& s, const VEpi& e) {
   extern "C" __global__ __launch_bounds__(256, 2) void NAME##_f32(VGemm s, VEpi e) {   \
     vgemm_body<float, EPI, AKC, BKC, 2, 2, 2, 2, 2, 128>(s, e);                        \
   }
-// few rows of X: 128 x 64 and 128 x 32 tiles, a wave having 32 of W's rows, with
+// up to 1,024 rows of X: 128 x 64 and 128 x 32 tiles, a wave having 32 of W's rows, with
 // three K blocks of W on their way; bound by the reads of W
 #define HF_VGEMM_FEW(NAME, EPI, AKC, BKC)                                              \
   extern "C" __global__ __launch_bounds__(256, 2) void NAME##_bf16_n64(VGemm s, VEpi e) { \

@@ -164,11 +164,10 @@ extern "C" __global__ __launch_bounds__(1024) void hf_vocab_count(VRows r) {
 
 // ----------------------------------------------------------------- packing
 namespace {
-// n elements of src to dst (16-byte aligned, dn elements), zeros past n;
-// Called by a whole workgroup of 256.
+// n elements of src to dst (16-byte aligned, dn elements), zeros past n, by a
+// whole workgroup of 256.
 template <class E>
-__device__ __forceinline__ void copy_row(const E* src, int n, E* dst, int dn,
-                                         E* dst2) {
+__device__ __forceinline__ void copy_row(const E* src, int n, E* dst, int dn, E* dst2) {
   constexpr int EPC = 16 / sizeof(E);
   for (int c = threadIdx.x; c < dn / EPC; c += 256) {
     u32x4 v = u32x4{0u, 0u, 0u, 0u};
@@ -811,9 +810,11 @@ void vocab_pack_matrix(const Launch& L, int type, const void* W, long long ldw, 
   const int es = type == VT_F32 ? 4 : 2, chunks = R * (Dp * es / 16);   // of 256 MiB at most
   const int grid = (chunks + 256 * COPY_U - 1) / (256 * COPY_U);
   if (type == VT_F32)
-    HF_LAUNCH("hf_vocab_copy", hf_vocab_copy_f32, grid, 256, (const float*)W, ldw, R, D, (float*)wp, Dp);
+    HF_LAUNCH("hf_vocab_copy", hf_vocab_copy_f32, grid, 256, (const float*)W, ldw, R, D,
+              (float*)wp, Dp);
   else
-    HF_LAUNCH("hf_vocab_copy", hf_vocab_copy_bf16, grid, 256, (const bf16_t*)W, ldw, R, D, (bf16_t*)wp, Dp);
+    HF_LAUNCH("hf_vocab_copy", hf_vocab_copy_bf16, grid, 256, (const bf16_t*)W, ldw, R, D,
+              (bf16_t*)wp, Dp);
 }
 
 bool vocab_row_loss(const Launch& L, int type, const VRows& r, const float2* stat, int ldstat,

@@ -191,7 +191,8 @@ def mask_rows(y, how, seed=5):
 SHAPES = [(1, 1, 1), (1, 1000, 64), (3, 7, 5), (64, 130, 64), (65, 129, 63), (127, 1000, 96),
           (128, 257, 128), (129, 1000, 96), (256, 256, 64), (300, 515, 200), (257, 2049, 321),
           (1000, 513, 130), (300, 1360, 520), (1024, 900, 260), (1025, 900, 260),
-          (2100, 300, 66), (100, 140000, 64), (2049, 8200, 512), (4101, 4099, 1100)]
+          (2100, 300, 66), (5, 20000, 1024), (100, 140000, 64), (2049, 8200, 512),
+          (4101, 4099, 1100)]
 
 
 @pytest.mark.parametrize("name", ["fp32", "bf16"])
@@ -593,7 +594,8 @@ def zipf(n, V, seed=0):
                                       (1000, 5000, 64), (1024, 4096, 520), (1025, 4095, 130),
                                       (500, 80, 8), (500, 80, 9), (2000, 70, 255), (1200, 90, 511),
                                       (1200, 90, 513), (1200, 90, 519), (1100, 60, 1021),
-                                      (20000, 1000, 72), (30011, 200003, 24)])
+                                      (20000, 1000, 72), (30011, 200003, 24), (30011, 120000, 1024),
+                                      (20000, 140000, 1021)])
 def test_embedding_and_gradient(name, rows, V, D):
     torch = T()
     u = unit(name)

@@ -52,7 +52,9 @@ struct hf_vocab {
   char* ws = nullptr;
   Layout lay = {};
   hipEvent_t last = nullptr;       // the work on the stream before this one
-  bool pending = false;            // calls have been made on this stream
+  // This stream has calls, or a wait for those on the streams before it, which
+  // the next one has to wait for in turn.
+  bool pending = false;
   std::string err;
 
   template <class T>
@@ -602,7 +604,6 @@ int hf_vocab_set_stream(hf_vocab* c, void* s) {
   if (!c->last) HIP_TRY(c, hipEventCreateWithFlags(&c->last, hipEventDisableTiming));
   HIP_TRY(c, hipEventRecord(c->last, from));
   HIP_TRY(c, hipStreamWaitEvent(to, c->last, 0));
-  c->pending = false;
   return HF_OK;
 }
 

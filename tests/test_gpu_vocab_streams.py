@@ -1,0 +1,36 @@
+"""The vocabulary calls on changing streams: one context's workspace is used by
+one call at a time, whatever stream each call is on."""
+
+import pytest
+
+from paper_1606_00511_amd import hf as H
+from tests.test_gpu_vocab import head_inputs
+
+pytestmark = pytest.mark.gpu
+
+
+def inputs(k, rows=3000, V=20000, D=512):
+    return head_inputs("bf16", rows, V, D, seed=k)
+
+
+def test_switches_with_a_refused_call_between():
+    """A long call on one stream, a refused one on a second, a call with other
+    inputs on a third, again and again: the bits of each alone."""
+    import torch
+    jobs = [inputs(k) for k in range(2)]
+    net = H.HFVocab(20000, 512, 3000, "bf16")
+    want = [[o.clone() for o in net.hf_vocab_loss_grad(*j)] for j in jobs]
+    s = [torch.cuda.Stream() for _ in range(3)]
+    torch.cuda.synchronize()
+    got = []
+    for _ in range(4):
+        with torch.cuda.stream(s[0]):
+            got.append((0, net.hf_vocab_loss_grad(*jobs[0])))
+        with torch.cuda.stream(s[1]), pytest.raises(H.HFError):
+            net.hf_vocab_loss_grad(*jobs[0], denom=-1.0)
+        with torch.cuda.stream(s[2]):
+            got.append((1, net.hf_vocab_loss_grad(*jobs[1])))
+    torch.cuda.synchronize()
+    for k, outs in got:
+        for a, b in zip(want[k], outs):
+            assert torch.equal(a, b)

@@ -449,11 +449,14 @@ int hf_prof_get(hf_ctx* ctx, int32_t i, const char** name, int64_t* launches,
  * Memory, streams and errors as for hf_ctx: device pointers owned by the
  * caller, one caller-provided workspace, everything asynchronous on the
  * context's stream, HF_* codes.  Calls make no allocation and can be captured
- * into a graph.  hf_vocab_set_stream orders the new stream behind the
- * context's calls on the old one (which must still exist), as they share the
- * workspace; captured calls, and graphs that share a workspace, are the
- * caller's to order.  The current device must be the stream's.  Repeated calls
- * give the same bits, whatever the workspace's size.
+ * into a graph.  As they share the workspace, a call waits for the context's
+ * calls before it, whatever streams they are on: hf_vocab_set_stream orders the
+ * new stream behind the old one (which must still exist), or, while one of the
+ * two is captured, the next call does (until then the stream of the calls
+ * before it must exist; while that one is captured, the call is refused).
+ * Captured calls, and graphs that share a workspace, are the caller's to order.
+ * The current device must be the stream's.  Repeated calls give the same bits,
+ * whatever the workspace's size.
  */
 typedef struct hf_vocab hf_vocab;
 

@@ -51,10 +51,11 @@ struct hf_vocab {
   hipStream_t stream = nullptr;
   char* ws = nullptr;
   Layout lay = {};
-  hipEvent_t last = nullptr;       // the work on the stream before this one
-  // This stream has calls, or a wait for those on the streams before it, which
-  // the next one has to wait for in turn.
+  // The calls so far that no graph captured are on `work` (if pending), or
+  // `work` waits for them.
   bool pending = false;
+  hipStream_t work = nullptr;
+  hipEvent_t last = nullptr;       // their end, for another stream to wait for
   std::string err;
 
   template <class T>
@@ -194,6 +195,29 @@ int check_apart(hf_vocab* c, const void* in, const char* in_name, const void* ou
 // -------------------------------------------------------------- the passes
 int end(hf_vocab* c) {
   HIP_TRY(c, hipGetLastError());
+  return HF_OK;
+}
+
+// Puts the context's stream behind the calls so far, with which it shares the
+// workspace, for a call or ahead of one.  While the stream is captured nothing
+// is done: a wait would go into the graph, and the caller orders what is
+// captured.  The first call after that, if it is not captured itself, gets
+// here with work still on the stream of before.
+int follow(hf_vocab* c, bool call) {
+  if (c->pending && c->work == c->stream) return HF_OK;
+  hipStreamCaptureStatus to = hipStreamCaptureStatusNone, from = to;
+  HIP_TRY(c, hipStreamIsCapturing(c->stream, &to));
+  if (to != hipStreamCaptureStatusNone) return HF_OK;
+  if (c->pending) {
+    HIP_TRY(c, hipStreamIsCapturing(c->work, &from));
+    if (from != hipStreamCaptureStatusNone)
+      return !call ? HF_OK
+                   : fail(c, HF_EHIP, "the stream of the calls before this one is being captured");
+    if (!c->last) HIP_TRY(c, hipEventCreateWithFlags(&c->last, hipEventDisableTiming));
+    HIP_TRY(c, hipEventRecord(c->last, c->work));
+    HIP_TRY(c, hipStreamWaitEvent(c->stream, c->last, 0));
+  }
+  c->work = c->stream;
   c->pending = true;
   return HF_OK;
 }
@@ -530,7 +554,7 @@ int head_call(hf_vocab* c, const void* X, int64_t ldx, const void* W, int64_t ld
     if (g->accumulate != 0 && g->accumulate != 1)
       return fail(c, HF_EINVAL, "accumulate %d is neither 0 nor 1", g->accumulate);
   }
-  if ((rc = check_ready(c, T))) return rc;
+  if ((rc = check_ready(c, T)) || (rc = follow(c, true))) return rc;
   VRows r = {};
   r.T = (int)T;
   r.K = K;
@@ -591,20 +615,8 @@ int hf_vocab_destroy(hf_vocab* c) {
 
 int hf_vocab_set_stream(hf_vocab* c, void* s) {
   if (!c) return HF_EINVAL;
-  const hipStream_t from = c->stream, to = reinterpret_cast<hipStream_t>(s);
-  if (from == to) return HF_OK;
-  c->stream = to;
-  if (!c->pending) return HF_OK;
-  // later work shares the workspace with what the old stream still does;
-  // the caller orders calls that are captured
-  hipStreamCaptureStatus a = hipStreamCaptureStatusNone, b = hipStreamCaptureStatusNone;
-  HIP_TRY(c, hipStreamIsCapturing(from, &a));
-  HIP_TRY(c, hipStreamIsCapturing(to, &b));
-  if (a != hipStreamCaptureStatusNone || b != hipStreamCaptureStatusNone) return HF_OK;
-  if (!c->last) HIP_TRY(c, hipEventCreateWithFlags(&c->last, hipEventDisableTiming));
-  HIP_TRY(c, hipEventRecord(c->last, from));
-  HIP_TRY(c, hipStreamWaitEvent(to, c->last, 0));
-  return HF_OK;
+  c->stream = reinterpret_cast<hipStream_t>(s);
+  return c->pending ? follow(c, false) : HF_OK;
 }
 
 size_t hf_vocab_workspace_bytes(const hf_vocab* c, int64_t rows) {
@@ -685,7 +697,7 @@ int hf_vocab_embed(hf_vocab* c, const void* E, int64_t lde, const int32_t* tok, 
       (rc = check_apart(c, E, "E", out, "out", rows)))
     return rc;
   if (!std::isfinite(scale)) return fail(c, HF_EINVAL, "scale is not finite");
-  if ((rc = check_ready(c, rows))) return rc;
+  if ((rc = check_ready(c, rows)) || (rc = follow(c, true))) return rc;
   const Launch L{c->stream, nullptr};
   vocab_embed(L, c->type, E, lde, c->V, c->D, tok, (int)rows, scale, out, ldo, c->st());
   return end(c);
@@ -705,7 +717,7 @@ int hf_vocab_embed_grad(hf_vocab* c, const int32_t* tok, int64_t rows, float sca
   if (!std::isfinite(scale)) return fail(c, HF_EINVAL, "scale is not finite");
   if (accumulate != 0 && accumulate != 1)
     return fail(c, HF_EINVAL, "accumulate %d is neither 0 nor 1", accumulate);
-  if ((rc = check_ready(c, rows))) return rc;
+  if ((rc = check_ready(c, rows)) || (rc = follow(c, true))) return rc;
   const Launch L{c->stream, nullptr};
   const Layout& l = c->lay;
   const VSort s = {c->at<int>(l.key), c->at<int>(l.spos), c->at<int>(l.tkey), c->at<int>(l.tpos),
@@ -718,6 +730,7 @@ int hf_vocab_embed_grad(hf_vocab* c, const int32_t* tok, int64_t rows, float sca
 int hf_vocab_check(hf_vocab* c) {
   if (!c) return HF_EINVAL;
   if (!c->ws) return HF_OK;
+  if (c->pending && c->work != c->stream) HIP_TRY(c, hipStreamSynchronize(c->work));
   HIP_TRY(c, hipStreamSynchronize(c->stream));
   int flag = 0;
   HIP_TRY(c, hipMemcpy(&flag, &c->st()->err, sizeof flag, hipMemcpyDeviceToHost));

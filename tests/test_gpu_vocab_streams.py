@@ -34,3 +34,40 @@ def test_switches_with_a_refused_call_between():
     for k, outs in got:
         for a, b in zip(want[k], outs):
             assert torch.equal(a, b)
+
+
+def test_capture_between_eager_calls():
+    """A long eager call on one stream, a captured call on a second, an eager
+    one with other inputs on a third, and replays: the bits of each alone."""
+    import torch
+    jobs = [inputs(k) for k in range(2)]
+    net = H.HFVocab(20000, 512, 3000, "bf16")
+    want = [[o.clone() for o in net.hf_vocab_loss_grad(*j)] for j in jobs]
+    first, side, third = (torch.cuda.Stream() for _ in range(3))
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    # (begun and ended by hand: torch.cuda.graph waits for the device first)
+    with torch.cuda.stream(side):
+        net.hf_vocab_loss_grad(*jobs[0])
+        torch.cuda.synchronize()
+        with torch.cuda.stream(first):
+            eager = [net.hf_vocab_loss_grad(*jobs[0])]
+        g.capture_begin()
+        caught = net.hf_vocab_loss_grad(*jobs[0])
+        g.capture_end()
+    with torch.cuda.stream(third):
+        eager.append(net.hf_vocab_loss_grad(*jobs[1]))
+    torch.cuda.synchronize()
+    for w, got in zip(want, eager):
+        for a, b in zip(w, got):
+            assert torch.equal(a, b)
+    for _ in range(3):
+        for o in caught:
+            o.zero_()
+        g.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(want[0], caught):
+            assert torch.equal(a, b)
+        for a, b in zip(want[1], net.hf_vocab_loss_grad(*jobs[1])):
+            assert torch.equal(a, b)
+        torch.cuda.synchronize()

@@ -52,3 +52,67 @@ result = log()
 """)
         assert [l[-1] for l in lines if l[0] == "launch"] == [A, C]
         assert hip_stub.unordered(lines) == []
+
+
+def test_a_captured_call_between(stub):
+    """An eager call on A, a captured one on B, an eager one on C: C's is
+    behind A's, though nothing could be made to wait on B meanwhile.  Then the
+    same with B's capture ended before the switch, and with eager calls on B
+    itself after its capture."""
+    for ended, last in ((False, 0xc00), (True, 0xc00), (True, 0xb00)):
+        lines = hip_stub.run(stub, EMBED + """
+h = vocab(stream=0xa00)
+assert call() == H.HF_OK
+S.stub_capture(0xb00, 1)
+assert L.hf_vocab_set_stream(h, 0xb00) == H.HF_OK
+at = len(S.stub_log().splitlines())
+assert call() == H.HF_OK
+ended, last = %r, %r
+if ended:
+    S.stub_capture(0xb00, 0)
+to = len(S.stub_log().splitlines())
+assert L.hf_vocab_set_stream(h, last) == H.HF_OK
+assert call() == H.HF_OK
+lines = log()
+result = [lines, at, to]
+""" % (ended, last))
+        lines, at, to = lines
+        assert [l[-1] for l in lines if l[0] == "launch"] == [A, B, hex(last)]
+        assert hip_stub.unordered(lines, [(B, at, to)]) == [], (ended, last)
+        # nothing of A's enters B's capture
+        assert all(l[0] == "launch" for l in lines[at:to])
+
+
+def test_a_switch_to_capture_records_nothing(stub):
+    """Events and waits on a stream that captures would become part of the
+    graph: none are made, and the eager call after it makes them."""
+    lines = hip_stub.run(stub, EMBED + """
+h = vocab(stream=0xa00)
+assert call() == H.HF_OK
+S.stub_capture(0xb00, 1)
+assert L.hf_vocab_set_stream(h, 0xb00) == H.HF_OK
+assert call() == H.HF_OK
+assert call() == H.HF_OK
+S.stub_capture(0xb00, 0)
+result = log()
+""")
+    assert [l[0] for l in lines] == ["launch"] * 3
+
+
+def test_eager_call_behind_a_stream_that_captures(stub):
+    """Calls on A, then A captures: an eager call on B could only be put behind
+    A's earlier ones through the capture.  It is refused, and goes through once
+    the capture has ended."""
+    lines = hip_stub.run(stub, EMBED + """
+h = vocab(stream=0xa00)
+assert call() == H.HF_OK
+S.stub_capture(0xa00, 1)
+assert L.hf_vocab_set_stream(h, 0xb00) == H.HF_OK
+assert call() == H.HF_EHIP
+assert b"captur" in L.hf_vocab_last_error(h)
+S.stub_capture(0xa00, 0)
+assert call() == H.HF_OK
+result = log()
+""")
+    assert [l[-1] for l in lines if l[0] == "launch"] == [A, B]
+    assert hip_stub.unordered(lines) == []

@@ -116,3 +116,23 @@ result = log()
 """)
     assert [l[-1] for l in lines if l[0] == "launch"] == [A, B]
     assert hip_stub.unordered(lines) == []
+
+
+@pytest.mark.parametrize("fails", ["hipStreamIsCapturing", "hipEventCreateWithFlags",
+                                   "hipEventRecord", "hipStreamWaitEvent"])
+def test_a_switch_that_fails(stub, fails):
+    """The runtime fails during a switch of streams, which says so; the switch
+    made again, or the next call, is behind the earlier ones all the same."""
+    for again in (True, False):
+        lines = hip_stub.run(stub, EMBED + """
+h = vocab(stream=0xa00)
+assert call() == H.HF_OK
+S.stub_fail(b%r)
+assert L.hf_vocab_set_stream(h, 0xb00) == H.HF_EHIP
+if %r:
+    assert L.hf_vocab_set_stream(h, 0xb00) == H.HF_OK
+assert call() == H.HF_OK
+result = log()
+""" % (fails, again))
+        assert [l[-1] for l in lines if l[0] == "launch"] == [A, B]
+        assert hip_stub.unordered(lines) == [], again

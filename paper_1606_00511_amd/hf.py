@@ -483,7 +483,9 @@ class HFVocab:
     ws_rows: size the workspace for calls of up to this many rows only
     (default max_rows).  Rows may be strided (the last dimension contiguous).
     Labels, tokens and ids are int32, HF_IGNORE where masked.  Calls run on
-    torch's current stream of the context's device.
+    torch's current stream of the context's device; the workspace goes back to
+    torch's allocator once the work on all of them is done.  A graph that has
+    captured calls works in it at every replay: keep the object as long.
     """
 
     def __init__(self, vocab, width, max_rows, dtype="fp32", device="cuda",
@@ -501,7 +503,7 @@ class HFVocab:
             raise HFError(rc, "hf_vocab_create rejected vocab=%d width=%d max_rows=%d"
                           % (self.vocab, self.width, self.max_rows))
         self._h = h
-        self._stream = 0                  # of the last call
+        self._stream = None               # of the last call
         nbytes = int(L.hf_vocab_workspace_bytes(
             h, self.max_rows if ws_rows is None else int(ws_rows)))
         if nbytes == 0:
@@ -525,8 +527,10 @@ class HFVocab:
         if cuda.current_device() != self.device.index:
             with cuda.device(self.device):
                 return self._call(fn, *args)
-        stream = cuda.current_stream(self.device.index).cuda_stream
+        current = cuda.current_stream(self.device.index)
+        stream = current.cuda_stream
         if stream != self._stream:
+            self.workspace.record_stream(current)
             self._check(L.hf_vocab_set_stream(self._h, stream))
             self._stream = stream
         return self._check(getattr(L, fn)(self._h, *args))

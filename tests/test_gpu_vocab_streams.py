@@ -71,3 +71,27 @@ def test_capture_between_eager_calls():
         for a, b in zip(want[1], net.hf_vocab_loss_grad(*jobs[1])):
             assert torch.equal(a, b)
         torch.cuda.synchronize()
+
+
+def test_workspace_of_a_dropped_context():
+    """A context dropped while a side stream still works in its workspace: the
+    allocator does not hand the memory to another stream meanwhile."""
+    import torch
+    X, W, y = inputs(0)
+    want = [o.clone() for o in H.HFVocab(20000, 512, 3000, "bf16").hf_vocab_loss_grad(X, W, y)]
+    net = H.HFVocab(20000, 512, 3000, "bf16")      # on the default stream
+    at, size = net.workspace.data_ptr(), net.workspace.numel()
+    s, done = torch.cuda.Stream(), torch.cuda.Event()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(s):
+        for _ in range(50):
+            got = net.hf_vocab_loss_grad(X, W, y)
+        done.record()
+    del net
+    new = torch.empty(size, dtype=torch.uint8, device="cuda")
+    apart = new.data_ptr() >= at + size or at >= new.data_ptr() + size
+    assert done.query() or apart
+    new.fill_(0xff)
+    torch.cuda.synchronize()
+    for a, b in zip(want, got):
+        assert torch.equal(a, b)

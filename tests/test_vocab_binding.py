@@ -1,0 +1,52 @@
+"""What HFVocab hands to the C calls and to torch, with both faked.  No GPU."""
+
+from types import SimpleNamespace
+
+import pytest
+
+from paper_1606_00511_amd import hf as H
+
+
+class Fakes:
+    """A library that answers `codes` in turn and then HF_OK, and torch's
+    current stream."""
+
+    def __init__(self, monkeypatch):
+        self.calls, self.codes, self.recorded = [], [], []
+        self.stream = 0
+        self.torch = SimpleNamespace(cuda=SimpleNamespace(
+            current_device=lambda: 0,
+            current_stream=lambda i=None: SimpleNamespace(cuda_stream=self.stream)))
+        monkeypatch.setattr(H, "lib", lambda: self)
+        self.hf_vocab_last_error = lambda h: b"an error"
+        self.hf_strerror = lambda c: b"a code"
+
+    def __getattr__(self, name):
+        def call(h, *args):
+            self.calls.append((name, *args))
+            return self.codes.pop(0) if self.codes else H.HF_OK
+        return call
+
+    def vocab(self):
+        net = H.HFVocab.__new__(H.HFVocab)
+        net._torch, net._h, net._stream = self.torch, 1, None
+        net.device = SimpleNamespace(index=0)
+        net.workspace = SimpleNamespace(
+            record_stream=lambda s: self.recorded.append(s.cuda_stream))
+        return net
+
+
+@pytest.fixture
+def fakes(monkeypatch):
+    return Fakes(monkeypatch)
+
+
+def test_every_stream_is_recorded_for_the_workspace(fakes):
+    """The allocator knows of each stream that the workspace is used on, the
+    first one included: the context may have been made on another."""
+    net = fakes.vocab()
+    for s in (0, 0, 5, 5, 0, 7):
+        fakes.stream = s
+        net._call("hf_vocab_check")
+    assert [c[1] for c in fakes.calls if c[0] == "hf_vocab_set_stream"] == [0, 5, 0, 7]
+    assert set(fakes.recorded) == {0, 5, 7}

@@ -475,7 +475,8 @@ int hf_vocab_create(int64_t vocab, int32_t width, int32_t type,
                     int64_t max_rows, void* hip_stream, hf_vocab** out);
 /* Free a context.  NULL is ok. */
 int hf_vocab_destroy(hf_vocab* ctx);
-/* Stream (a hipStream_t) of later calls; NULL = null stream. */
+/* Stream (a hipStream_t) of later calls, after an error as well; NULL = null
+ * stream. */
 int hf_vocab_set_stream(hf_vocab* ctx, void* hip_stream);
 /* Bytes of workspace for calls of up to `rows` rows (<= 0: max_rows); 0 for a
  * NULL context or rows > max_rows.  Grows with rows. */

@@ -531,6 +531,7 @@ class HFVocab:
         stream = current.cuda_stream
         if stream != self._stream:
             self.workspace.record_stream(current)
+            self._stream = None
             self._check(L.hf_vocab_set_stream(self._h, stream))
             self._stream = stream
         return self._check(getattr(L, fn)(self._h, *args))

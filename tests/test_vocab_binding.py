@@ -50,3 +50,17 @@ def test_every_stream_is_recorded_for_the_workspace(fakes):
         net._call("hf_vocab_check")
     assert [c[1] for c in fakes.calls if c[0] == "hf_vocab_set_stream"] == [0, 5, 0, 7]
     assert set(fakes.recorded) == {0, 5, 7}
+
+
+def test_a_switch_that_failed_is_made_again(fakes):
+    """A switch of streams fails, and the caller goes back to the stream of
+    before: the C context is told, as it may be on the other one."""
+    net = fakes.vocab()
+    net._call("hf_vocab_check")
+    fakes.stream, fakes.codes = 5, [H.HF_EHIP]
+    with pytest.raises(H.HFError):
+        net._call("hf_vocab_check")
+    fakes.stream = 0
+    del fakes.calls[:]
+    net._call("hf_vocab_check")
+    assert fakes.calls == [("hf_vocab_set_stream", 0), ("hf_vocab_check",)]

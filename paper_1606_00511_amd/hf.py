@@ -235,6 +235,7 @@ class HFNet:
             raise HFError(rc, "hf_create rejected dims=%s act=%s max_batch=%d prec=%s"
                           % (self.dims, act, self.max_batch, prec))
         self._h = h
+        self._last = None                 # stream of the last call
         self.n = int(L.hf_num_params(h))
         nbytes = int(L.hf_workspace_bytes(
             h, self.max_batch if ws_batch is None else int(ws_batch)))
@@ -252,8 +253,12 @@ class HFNet:
 
     def _stream(self):
         import torch
-        self._check(lib().hf_set_stream(self._h, torch.cuda.current_stream(
-            self.device).cuda_stream))
+        current = torch.cuda.current_stream(self.device)
+        if current.cuda_stream != self._last:
+            # the allocator keeps the workspace until this stream's work is done
+            self.workspace.record_stream(current)
+            self._last = current.cuda_stream
+        self._check(lib().hf_set_stream(self._h, current.cuda_stream))
 
     def close(self):
         if getattr(self, "_h", None) is not None:

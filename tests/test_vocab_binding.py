@@ -1,4 +1,5 @@
-"""What HFVocab hands to the C calls and to torch, with both faked.  No GPU."""
+"""What HFVocab, and HFNet of its streams, hand to the C calls and to torch,
+with both faked.  No GPU."""
 
 from types import SimpleNamespace
 
@@ -64,3 +65,17 @@ def test_a_switch_that_failed_is_made_again(fakes):
     del fakes.calls[:]
     net._call("hf_vocab_check")
     assert fakes.calls == [("hf_vocab_set_stream", 0), ("hf_vocab_check",)]
+
+
+def test_every_stream_is_recorded_for_a_nets_workspace(fakes, monkeypatch):
+    import torch
+    monkeypatch.setattr(torch.cuda, "current_stream",
+                        lambda d=None: SimpleNamespace(cuda_stream=fakes.stream))
+    net = H.HFNet.__new__(H.HFNet)
+    net._h, net._last, net.device = 1, None, None
+    net.workspace = fakes.vocab().workspace
+    for s in (0, 0, 5, 0, 7):
+        fakes.stream = s
+        net._stream()
+    assert [c[1] for c in fakes.calls if c[0] == "hf_set_stream"] == [0, 0, 5, 0, 7]
+    assert set(fakes.recorded) == {0, 5, 7}

@@ -106,7 +106,7 @@ __device__ __forceinline__ void embed_body(const E* table, long long lde, int V,
                                            E* out, long long ldo, VocabState* st) {
   using S = Strip<E, VEC>;
   const int lane = threadIdx.x & 63;
-  const long long u = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
+  const long long u = ((long long)blockIdx.y * gridDim.x + blockIdx.x) * 4 + (threadIdx.x >> 6);
   const int t = (int)(u / strips), strip = (int)(u % strips);
   if (t >= T) return;
   const int id = __builtin_amdgcn_readfirstlane(tok[t]);
@@ -575,7 +575,11 @@ void vocab_embed(const Launch& L, int type, const void* E, long long lde, int V,
   if (T < 1) return;
   const int es = type == VT_F32 ? 4 : 2, strips = strips_of(D, es);
   const bool vec = chunks(D, es);
-  const long long grid = ((long long)T * strips + 3) / 4;
+  // (a launch has fewer than 2^32 work-items in x: 262,144 rows of 65,536 of fp32
+  // are as many)
+  constexpr long long MAX_X = 1 << 20;
+  const long long groups = ((long long)T * strips + 3) / 4;
+  const dim3 grid((unsigned)std::min(groups, MAX_X), (unsigned)((groups + MAX_X - 1) / MAX_X));
   // _s: much output does not take the place of frequent tokens' rows of E in the
   // caches (65,536 x 4,096 of bf16: 179 -> 104 us); little stays for its reader
   const bool stream = (long long)T * D * es > L2_BYTES;

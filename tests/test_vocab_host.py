@@ -136,3 +136,37 @@ result = log()
 """ % (fails, again))
         assert [l[-1] for l in lines if l[0] == "launch"] == [A, B]
         assert hip_stub.unordered(lines) == [], again
+
+
+def launches(lines, name):
+    return [(l[1], [int(v) for v in l[2:8]]) for l in lines
+            if l[0] == "launch" and l[1].startswith(name)]
+
+
+def fits(lines):
+    """Work-items of a launch: below 2^32 each way, as its size is 32 bits; at
+    most 65,535 workgroups in y and z."""
+    for l in lines:
+        if l[0] == "launch":
+            g, b = [int(v) for v in l[2:5]], [int(v) for v in l[5:8]]
+            assert all(0 < x * y < 2 ** 32 for x, y in zip(g, b)), l
+            assert g[1] < 65536 and g[2] < 65536, l
+
+
+LIMITS = """
+T, D = H.HF_VOCAB_MAX_ROWS, H.HF_VOCAB_MAX_WIDTH
+result = []
+for type in (H.HF_TYPE_FP32, H.HF_TYPE_BF16):
+    h = vocab(%s, D, type, T)
+    assert %s == H.HF_OK
+    result += log()
+    assert L.hf_vocab_destroy(h) == H.HF_OK
+"""
+
+
+def test_embedding_at_both_limits(stub):
+    lines = hip_stub.run(stub, LIMITS % (9, "L.hf_vocab_embed(h, IN, D, IN, T, 1.0, OUT, D)"))
+    fits(lines)
+    # a wave has 64 times 16 bytes of a row
+    for (_, (x, y, z, b, _, _)), size in zip(launches(lines, "hf_vocab_embed"), (4, 2)):
+        assert x * y * z * (b // 64) >= 262144 * 65536 * size // 1024

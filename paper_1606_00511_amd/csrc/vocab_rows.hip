@@ -700,6 +700,7 @@ __device__ __forceinline__ void finish_body(const VocabState* st, const VParts& 
     return;
   }
   constexpr int QB = 256 / G;           // column groups per workgroup
+  const int groups = gridDim.x - (loss ? 1 : 0);
   __shared__ f32x4 sums[G > 1 ? 256 : 1];
   const int q = (D + 3) / 4, grp = threadIdx.x / QB;
   if (counted) rows = min(st->n, rows);
@@ -710,9 +711,9 @@ __device__ __forceinline__ void finish_body(const VocabState* st, const VParts& 
   const size_t ss = (size_t)gya * p.rn * p.ldp;
   const int parts = dup ? 2 * splits : splits;
   const float g = st->gscale;
-  // (once, except where the direct store was likelier)
+  // (once, except where the direct store was likelier, and for very large outputs)
   for (long long i0 = (long long)blockIdx.x * QB; i0 < (long long)rows * q;
-       i0 += (long long)gridDim.x * QB) {
+       i0 += (long long)groups * QB) {
     const long long i = i0 + threadIdx.x % QB;
     const int j = (int)(i / q), c = 4 * (int)(i % q);
     const bool in = j < rows;
@@ -882,10 +883,11 @@ void vocab_finish(const Launch& L, int type, const VGemm& g, const VEpi& e, int 
                   const VRows* r, float* loss) {
   const VParts p = {e.part, e.ldp, g.splits, g.smax, g.N, tile_n(g.tile), g.dyn, e.out != nullptr};
   const bool g8 = (dup ? 2 : 1) * g.splits >= 16;
-  long long grid = ((long long)rows * ((D + 3) / 4) * (g8 ? 8 : 1) + 255) / 256 + (loss ? 1 : 0);
-  // most often nothing is left to do: 16,384 workgroups that end at once take 12
-  // us, these 4.5
-  if (p.direct && g.splits == 1) grid = std::min<long long>(grid, 2048);
+  long long grid = ((long long)rows * ((D + 3) / 4) * (g8 ? 8 : 1) + 255) / 256;
+  // a launch has fewer than 2^32 work-items (262,144 rows of 65,536 columns would
+  // have as many); and most often nothing is left to do after a direct store:
+  // 16,384 workgroups that end at once take 12 us, 2,048 take 4.5
+  grid = std::min<long long>(grid, p.direct && g.splits == 1 ? 2048 : 1 << 20) + (loss ? 1 : 0);
   if (grid < 1) return;
   const float* rl = loss ? r->row_loss : nullptr;
   const int T = loss ? r->T : 0;

@@ -36,3 +36,46 @@ def test_embedding_past_a_million_workgroups():
     net.hf_vocab_check()
     del net, out
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("name", ["fp32", "bf16"])
+def test_row_gradients_past_a_million_workgroups(name):
+    """Row gradients of several pieces of the vocabulary, with more groups of
+    columns than the kernel that finishes them has threads.  The vocabulary's
+    words are 5 different rows of W, so the reference needs 5 columns of them;
+    checked on the first and last rows and every 997th."""
+    torch = T()
+    torch.cuda.empty_cache()
+    rows, V, D, R = 65793, 13000 if name == "bf16" else 7000, 16390, 5
+    X, W, y = head_inputs(name, rows, R, D)
+    net = H.HFVocab(V, D, rows, name)
+    word = torch.arange(V, device="cuda") % R
+    _, rl, dX, _ = net.hf_vocab_loss_grad(X, W[word].contiguous(), y, need_dW=False)
+    assert rows * -(-D // 4) > 256 << 20
+    at = torch.cat([torch.arange(64), torch.arange(0, rows, 997),
+                    torch.arange(rows - 64, rows)]).cuda()
+    # p of a row of W is that of all its words together
+    n = torch.bincount(word, minlength=R).double()
+    x, w = X[at].double(), W.double()
+    z = x @ w.t()
+    lp = torch.log_softmax(z + n.log(), 1)
+    q = torch.zeros_like(z).scatter_(1, y[at].long()[:, None], 1.0)
+    ez = (D * E32 * (x.abs() @ w.abs().t()) + E32 * z.abs()).amax(1, keepdim=True)
+    elp = 2 * ez + (512 + V // 128) * E32
+    p1 = lp.exp() / n                  # of a word
+    # each word's delta is rounded: p by its error, by u, and by the fp16
+    # exponentials of bf16; the label's own word has p - 1
+    u = unit(name)
+    each = p1 * (elp + 64 * E32 + u) + (2.0 ** -12 * p1 + 2.0 ** -25 * p1.amax(1, keepdim=True)
+                                        if name == "bf16" else 0.0)
+    ed = n * each + q * (u + 256 * E32)
+    d = lp.exp() - q
+    terms = (lp.exp() + q) @ w.abs()
+    want = (d @ w) / rows
+    bound = ((ed @ w.abs()) * (1 + u) + terms * (V + 64) * E32) / rows + (u + 4 * E32) * want.abs()
+    within(dX[at], want, bound, "dX")
+    label = lp.gather(1, y[at].long()[:, None])[:, 0] - n[y[at].long()].log()
+    within(rl[at], -label, (elp[:, 0] + 256 * E32) * (1 + label.abs()) + E32, "row losses")
+    assert torch.isfinite(dX).all()
+    del net, dX
+    torch.cuda.empty_cache()

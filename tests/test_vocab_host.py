@@ -170,3 +170,13 @@ def test_embedding_at_both_limits(stub):
     # a wave has 64 times 16 bytes of a row
     for (_, (x, y, z, b, _, _)), size in zip(launches(lines, "hf_vocab_embed"), (4, 2)):
         assert x * y * z * (b // 64) >= 262144 * 65536 * size // 1024
+
+
+def test_gradients_at_both_limits(stub):
+    """All rows of the widest kind, with the vocabulary in several pieces (so
+    that the row gradients are finished by a kernel of their own)."""
+    lines = hip_stub.run(stub, LIMITS % (5000, """L.hf_vocab_loss_grad(
+        h, IN, D, IN, D, IN, T, 0.0, IN, None, OUT, D, OUT, D, 0)"""))
+    fits(lines)
+    assert len(launches(lines, "hf_vocab_finish")) >= 2
+    fits(hip_stub.run(stub, LIMITS % (9, "L.hf_vocab_embed_grad(h, IN, T, 1.0, IN, D, OUT, D, 0)")))

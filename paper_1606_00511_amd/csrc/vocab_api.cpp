@@ -86,7 +86,6 @@ int fail(hf_vocab* c, int code, const char* fmt, ...) {
   } while (0)
 
 // ------------------------------------------------------------------ sizes
-// Rows of delta: whole tiles; few rows of bf16 come twice (see two_term).
 inline int64_t tile_rows(int64_t T) { return std::max<int64_t>(up(T, VTILE), VTILE); }
 
 // bf16 calls of at most TWO_TERM_ROWS rows hold delta as two bf16 terms: with
@@ -95,10 +94,17 @@ inline int64_t tile_rows(int64_t T) { return std::max<int64_t>(up(T, VTILE), VTI
 inline int two_term(const hf_vocab* c, int64_t T) {
   return c->type == VT_BF16 && T > 0 && T <= TWO_TERM_ROWS ? (int)up(T, VPAD / 2) : 0;
 }
+// Rows of delta: whole tiles; of few rows, whose logits are kept however many
+// they are, no more than the K blocks of dW's product read.
+inline int64_t delta_rows(const hf_vocab* c, int64_t T) {
+  if (T > TWO_TERM_ROWS) return tile_rows(T);
+  const int dup = two_term(c, T);
+  return dup ? 2 * dup : up(T, VPAD);
+}
 // Bytes of a column of what is kept and of delta, which takes its place; few
 // bf16 rows keep fp32 logits beside delta.
 inline size_t col_bytes(const hf_vocab* c, int64_t T) {
-  return (size_t)tile_rows(T) * (two_term(c, T) ? 6 : c->es);
+  return (size_t)delta_rows(c, T) * c->es + (two_term(c, T) ? (size_t)T * 4 : 0);
 }
 inline bool keeps(const hf_vocab* c, int64_t T) {
   return T <= TWO_TERM_ROWS || col_bytes(c, T) * up(c->V, VTILE) <= KEEP_BYTES;
@@ -334,7 +340,7 @@ void head(hf_vocab* c, VRows r, const void* X, int64_t ldx, const void* W, int64
   // few bf16 rows: fp32 logits, and delta behind them
   const bool f16 = type == VT_BF16 && !dup;
   float* z = g && !f16 ? c->at<float>(l.z) : nullptr;
-  void* d = !g ? nullptr : dup ? (void*)(z + (size_t)Rp * ldd) : c->at<void>(l.z);
+  void* d = !g ? nullptr : dup ? (void*)(z + (size_t)T * ldd) : c->at<void>(l.z);
   const int sstep = std::min(wrows, vc);
   const int tile = shape_for(type, g ? sstep : wrows, T, Dp, false, !(g && f16)).tile;
   const int sg = tile_stat(tile);
@@ -352,6 +358,7 @@ void head(hf_vocab* c, VRows r, const void* X, int64_t ldx, const void* W, int64
     q.N = T;
     q.K = Dp;
     q.alim = n;
+    q.blim = Rp;
     q.st = r.st;
     q.X = xd;
     q.ldx = ldx;
@@ -414,6 +421,7 @@ void head(hf_vocab* c, VRows r, const void* X, int64_t ldx, const void* W, int64
         q.N = T;
         q.K = Dp;
         q.alim = n;
+        q.blim = Rp;
         q.st = r.st;
         q.X = xd;
         q.ldx = ldx;
@@ -439,6 +447,7 @@ void head(hf_vocab* c, VRows r, const void* X, int64_t ldx, const void* W, int64
       q.N = xrows;
       q.K = n;
       q.alim = n;
+      q.blim = (int)delta_rows(c, T);
       q.st = r.st;
       q.dyn = dup ? 0 : 1;
       if (v0 == 0) {

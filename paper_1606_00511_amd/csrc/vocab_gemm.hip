@@ -36,7 +36,6 @@
 // together ahead of them, they left the matrix cores idle 30% of the time
 // (8,192 rows x 32,768 x 4,096 in bf16: logits 1,830 -> 1,680 us, dX 1,980 ->
 // 1,730, dW 2,050 -> 1,840; fp32 16,384 x 2,048 x 2,048: 1,230 -> 975 us).
-#include <climits>
 #include <type_traits>
 
 #include "lds_dma.h"
@@ -279,7 +278,7 @@ __device__ __forceinline__ void vgemm_body(const VGemm& s, const VEpi& e) {
   const bool whole = s.X && nrow == s.T;
   constexpr bool XA = !BKC;              // dW: X is A; logits: X is B
   const int alim = XA && whole ? s.T : s.alim;
-  const int blim = !XA && whole ? s.T : INT_MAX;
+  const int blim = !XA && whole ? s.T : s.blim;
 
   const int nvb = (K + BK - 1) / BK;
   int vb0 = 0, nblk = nvb;
@@ -300,7 +299,7 @@ __device__ __forceinline__ void vgemm_body(const VGemm& s, const VEpi& e) {
   // Element offsets of the lane's direct loads from the tile's origin.  Rows
   // of a K-contiguous operand past its last one read that one; chunks of a
   // [k][m] operand past its padded width read the last chunk (both feed
-  // outputs that are not stored).  Packed rows and delta are whole tiles.
+  // outputs that are not stored).
   const long long lda = XA && whole ? s.ldx : s.lda, ldb = !XA && whole ? s.ldx : s.ldb;
   uint32_t offa[TA::INSTR], offb[TB::INSTR];
 #pragma unroll

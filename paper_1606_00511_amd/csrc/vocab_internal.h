@@ -42,6 +42,7 @@ struct VGemm {
   const void *A, *B;
   long long lda, ldb;
   int alim;        // rows of A that exist: m (akc), or k (not akc)
+  int blim;        // rows of B that exist, where they are n
   const VocabState* st;
   const void* X;   // the rows of X (what is packed), if they can be read in
   long long ldx;   // place: used where all T of them count; else null

@@ -79,3 +79,26 @@ def test_row_gradients_past_a_million_workgroups(name):
     assert torch.isfinite(dX).all()
     del net, dX
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("name", ["fp32", "bf16"])
+@pytest.mark.parametrize("rows,V,D", [(1, 1000, 64), (1, 70000, 72), (31, 5000, 200),
+                                      (64, 30000, 128), (65, 700, 64), (128, 20000, 320)])
+def test_few_rows_in_their_own_workspace(name, rows, V, D):
+    """A workspace of just the bytes asked for, full of NaN, with more of them
+    on both sides, which stay as they are."""
+    torch = T()
+    X, W, y = head_inputs(name, rows, V, D)
+    ids, t = teacher(rows, V, 40)
+    net = H.HFVocab(V, D, rows, name)
+    n, side = net.workspace.numel(), 1 << 20
+    room = torch.full((n + 2 * side,), 0xff, dtype=torch.uint8, device="cuda")
+    net._check(H.lib().hf_vocab_set_workspace(net._h, room.data_ptr() + side, n))
+    q_of, used = label_targets(y, V)
+    check_head(name, reference(X, W, q_of, 1.0, used, rows), V,
+               net.hf_vocab_loss_grad(X, W, y), two=name == "bf16")
+    q_of, used = list_targets(ids, t, 2.0, V)
+    check_head(name, reference(X, W, q_of, 2.0, used, rows), V,
+               net.hf_vocab_distill_grad(X, W, ids, t, 2.0), two=name == "bf16")
+    net.hf_vocab_embed_grad(y, X)
+    assert (room[:side] == 0xff).all() and (room[n + side:] == 0xff).all()

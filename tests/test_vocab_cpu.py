@@ -149,3 +149,18 @@ def test_refusals(L, fn, good, bads):
     assert f(h, *good.values()) == EWS
     assert b"workspace" in L.hf_vocab_last_error(h)
     assert L.hf_vocab_destroy(h) == OK
+
+
+@pytest.mark.parametrize("type,rows,a_word", [
+    (H.HF_TYPE_FP32, 1, 64 * 4), (H.HF_TYPE_FP32, 128, 128 * 4),
+    (H.HF_TYPE_BF16, 1, 1 * 4 + 2 * 32 * 2), (H.HF_TYPE_BF16, 128, 128 * 4 + 2 * 128 * 2)])
+def test_workspace_of_few_rows(L, type, rows, a_word):
+    """Few rows of the largest vocabulary: their logits and delta take what the
+    rows need (delta of whole blocks of 64 or 32 rows), beside a statistics
+    entry of 8 bytes a row and 32 words, 256 MiB each of packed W and of
+    partials, and little else."""
+    rc, h = create(L, H.HF_VOCAB_MAX, 64, type, rows)
+    assert rc == OK
+    most = H.HF_VOCAB_MAX * (a_word + rows / 4) + (520 << 20)
+    assert L.hf_vocab_workspace_bytes(h, 0) < most
+    assert L.hf_vocab_destroy(h) == OK

@@ -507,9 +507,11 @@ int hf_vocab_loss(hf_vocab* ctx, const void* X, int64_t ldx, const void* W,
  * The workspace keeps a call's logits: all of up to 128 rows, whatever the
  * vocabulary (of a word, 4 bytes a row, the rows up to a multiple of 64; with
  * bf16 8, up to a multiple of 32); of more rows at most 1.5 GiB (fp32; with
- * bf16 exponentials in fp16), the whole ones or a piece of the vocabulary's, the
- * others being computed again piece by piece.  delta is rounded to the type
- * (bf16 calls of up to 128 rows: to two terms of it) for the two products.
+ * bf16 exponentials in fp16: softmax(z) to 2^-12 of itself, or to 2^-40 of the
+ * largest among up to 128 neighbours), the whole ones or a piece of the
+ * vocabulary's, the others being computed again piece by piece.  delta is
+ * rounded to the type (bf16 calls of up to 128 rows: to two terms of it) for the
+ * two products.
  *   dX, dW      either may be NULL (not both): not computed
  *   accumulate  1: dW += instead of dW = (with tied weights, or over
  *               minibatches); dX is always written whole

@@ -5,8 +5,8 @@
 //              exp(z - max), from which the log-sum-exp over the whole
 //              vocabulary is joined.  What is kept of a piece is z itself
 //              (fp32), or exp(z - max) in fp16 (bf16): 11 bits where delta
-//              has 8, absolute below 2^-14 of the largest of the 128, in a
-//              third of the bytes of z and delta
+//              has 8 down to 2^-29 of the largest of the 128 (scaled by
+//              2^15), in a third of the bytes of z and delta
 //   p          exp(z - lse), recomputed piece by piece
 //   dX         delta W, delta = p - q (q the targets), summed over the pieces
 //   dW         delta^T X, whole for each piece
@@ -459,7 +459,7 @@ __device__ __forceinline__ void vgemm_body(const VGemm& s, const VEpi& e) {
         for (int r = 0; r < 16; ++r) {
           const float x = __builtin_amdgcn_exp2f((acc[a][b][r] - at) * c2);
           sum += x;
-          if (EPI == E_EXPS) acc[a][b][r] = x;
+          if (EPI == E_EXPS) acc[a][b][r] = x * EXP_SCALE;
         }
       sum += __shfl_xor(sum, 32, 64);
       const int n = nt + 32 * b + li;

@@ -23,6 +23,10 @@ inline int tile_n(int t) {
 }
 // Columns of one entry of row statistics: a wave's part of a vocabulary tile.
 inline int tile_stat(int t) { return t == TILE_BIG ? 128 : t == TILE_SMALL ? 64 : 32; }
+// exp(z - max) is kept in fp16 times this: with the largest at 2^15, terms down
+// to 2^-29 of it (20 less in z) have fp16's 11 bits, and those below an absolute
+// 2^-40 of it (as they are, 2^-14 and 2^-25: a word 17 below lost its gradient).
+constexpr float EXP_SCALE = 32768.0f;
 constexpr int VMAX_SPLITS = 64;
 constexpr long long L2_BYTES = 32ll << 20;   // the level-2 caches of the 8 XCDs
 constexpr long long L3_BYTES = 256ll << 20;  // the last-level cache
@@ -67,7 +71,7 @@ struct VEpi {
   // logits
   float zscale;          // 1 / tau
   float* z;              // logits kept (row n, column m), or null
-  void* pt;              // or exp(z - max of its statistics entry) in fp16
+  void* pt;              // or EXP_SCALE exp(z - max of its statistics entry) in fp16
   long long ldz;
   float2* stat;          // per row and entry: max, sum of exp(z - max)
   int ldstat, tile0;     // entries per row; index of this launch's first
@@ -141,7 +145,7 @@ bool vocab_row_loss(const Launch& L, int type, const VRows& r, const float2* sta
 void vocab_loss_sum(const Launch& L, const VRows& r, float* loss);
 // delta from kept logits of the columns [v0, v0 + Vc), targets included (dup:
 // the rounding's rest too, dup rows further down), and the loss unless null.
-// z null (bf16): d holds exp(z - max) in fp16, by statistics entries of `sg`
+// z null (bf16): d holds EXP_SCALE exp(z - max) in fp16, by statistics entries of `sg`
 // columns.
 // self (bf16 with all columns kept): the rows' statistics and losses as well,
 // instead of vocab_row_loss; the loss is then still to be summed.

@@ -12,8 +12,8 @@
 //   delta = p - q,  p_v = exp(z_v - lse)
 // delta is p rounded to the type everywhere but at the targets, where p - q is
 // formed in fp32 and rounded once.  With bf16, p comes from exp(z - max) kept
-// in fp16 (a rounding of 2^-12 beside delta's 2^-9) but for few rows.  Losses
-// are summed in fp64.
+// in fp16 (a rounding of 2^-12 beside delta's 2^-9, down to 2^-29 of the largest
+// of the entry) but for few rows.  Losses are summed in fp64.
 #include <type_traits>
 
 #include "vocab_internal.h"
@@ -562,7 +562,7 @@ struct VDelta {
   float* loss;
   int sg;                      // columns of a statistics entry
 };
-// FROM16: d holds exp(z - max) in fp16 and becomes delta in place.
+// FROM16: d holds EXP_SCALE exp(z - max) in fp16 and becomes delta in place.
 template <class E, bool SELF, bool FROM16>
 __device__ __forceinline__ void delta_body(const VRows& r, const VDelta& a, E* d) {
   if (!SELF && a.loss && blockIdx.x == gridDim.x - 1) {
@@ -603,7 +603,8 @@ __device__ __forceinline__ void delta_body(const VRows& r, const VDelta& a, E* d
     if (c < a.Vp) {
       u32x4 w = u32x4{0u, 0u, 0u, 0u};
       if (real && c < a.Vc) {
-        const float f = expf(a.stat[(size_t)j * a.ldstat + (a.v0 + c) / a.sg].x - l);
+        const float f = expf(a.stat[(size_t)j * a.ldstat + (a.v0 + c) / a.sg].x - l) *
+                        (1.0f / EXP_SCALE);
         const f16x8 x = *(const f16x8*)(hi + c);
 #pragma unroll
         for (int e = 0; e < 4; ++e)

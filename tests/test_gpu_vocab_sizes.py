@@ -102,3 +102,34 @@ def test_few_rows_in_their_own_workspace(name, rows, V, D):
                net.hf_vocab_distill_grad(X, W, ids, t, 2.0), two=name == "bf16")
     net.hf_vocab_embed_grad(y, X)
     assert (room[:side] == 0xff).all() and (room[n + side:] == 0xff).all()
+
+
+@pytest.mark.parametrize("rows", [200, 1500])
+def test_words_far_below_their_neighbours(rows):
+    """bf16 keeps exponentials in fp16, below the largest of 64 or 128 words: a
+    word whose logit is 10 to 20 less than a neighbour's has its gradient to the
+    bits of the type all the same.  p is off by its exponential's rounding,
+    2^-12, and the error of z - lse; delta by u besides, its sum over the rows
+    by 2 rows e, the result by u."""
+    torch = T()
+    V, D, u = 700, 64, unit("bf16")
+    # x = 1 in one column, and small whole numbers over 8 in another
+    X = torch.zeros(rows, D, device="cuda", dtype=torch.bfloat16)
+    X[:, 0] = 1
+    X[:, 1] = torch.randint(1, 9, (rows,), generator=gen(0), device="cuda") / 8.0
+    y = torch.zeros(rows, dtype=torch.int32, device="cuda")
+    W = torch.zeros(V, D, device="cuda", dtype=torch.bfloat16)
+    W[0, 0] = W[640, 0] = 20                # the largest of their entries
+    gaps = (10, 12, 14, 16, 17, 18, 19, 20)
+    for i, g in enumerate(gaps):
+        W[1 + 5 * i, 0] = W[641 + 5 * i, 0] = 20 - g
+    net = H.HFVocab(V, D, rows, "bf16")
+    dW = net.hf_vocab_loss_grad(X, W, y)[3]
+    x = X.double()
+    z = x @ W.double().t()
+    p = torch.log_softmax(z, 1).exp()
+    want = (p.t() @ x) / rows
+    elp = 2 * (D * E32 * 20 + E32 * 20) + (512 + V // 128) * E32 + 64 * E32
+    rel = (2.0 ** -12 + elp + u) * (1 + u) + 2 * rows * E32 + u + 4 * E32
+    at = [v + 5 * i for i in range(len(gaps)) for v in (1, 641)]
+    within(dW[at], want[at], rel * want[at].abs() + 1e-38, "dW")

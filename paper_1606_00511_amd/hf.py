@@ -600,6 +600,9 @@ class HFVocab:
             self._call(fn, *args)
             return loss, row_loss
         dX, dW, need_dX, need_dW, accumulate = grad
+        for t, need, what in ((dX, need_dX, "dX"), (dW, need_dW, "dW")):
+            if t is not None and not need:
+                raise ValueError("%s is given, and need_%s is False" % (what, what))
         if accumulate and dW is None:
             raise ValueError("accumulate needs the dW to add to")
         if dX is None and need_dX:
@@ -632,8 +635,8 @@ class HFVocab:
     def hf_vocab_loss_grad(self, X, W, y, denom=0.0, loss=None, row_loss=None, dX=None,
                            dW=None, need_dX=True, need_dW=True, accumulate=False):
         """hf_vocab_loss and its gradients: (loss, row losses, dX, dW).
-        need_dX / need_dW False: that gradient is not computed (None).
-        accumulate: dW += (dW given)."""
+        need_dX / need_dW False: that gradient is not computed (None, and none
+        may be given).  accumulate: dW += (dW given)."""
         T = self._rows(X, "X")
         y = self._vec(y, T, self._torch.int32, "y")
         return self._head("hf_vocab_loss_grad", X, W, [y], T, denom, loss, row_loss,

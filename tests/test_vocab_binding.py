@@ -79,3 +79,29 @@ def test_every_stream_is_recorded_for_a_nets_workspace(fakes, monkeypatch):
         net._stream()
     assert [c[1] for c in fakes.calls if c[0] == "hf_set_stream"] == [0, 0, 5, 0, 7]
     assert set(fakes.recorded) == {0, 5, 7}
+
+
+def test_a_gradient_given_but_not_needed(fakes):
+    """A buffer for a gradient that the call is told not to compute: refused,
+    for the caller expects one or the other.  Without the buffer it is None."""
+    import torch
+    net = fakes.vocab()
+    net._torch, net.device, net.dtype = torch, torch.device("cpu"), torch.float32
+    net.vocab, net.width = 5, 3
+    net._call = lambda fn, *args: fakes.calls.append((fn, *args))
+    X, W = torch.zeros(2, 3), torch.zeros(5, 3)
+    y = torch.zeros(2, dtype=torch.int32)
+    ids, t = y[:, None].repeat(1, 4), torch.zeros(2, 4)
+    for call, targets in ((net.hf_vocab_loss_grad, (y,)), (net.hf_vocab_distill_grad, (ids, t))):
+        for kw in (dict(dX=torch.empty(2, 3), need_dX=False),
+                   dict(dW=torch.empty(5, 3), need_dW=False),
+                   dict(dW=torch.empty(5, 3), need_dW=False, accumulate=True)):
+            with pytest.raises(ValueError):
+                call(X, W, *targets, **kw)
+        assert not fakes.calls
+        got = call(X, W, *targets, need_dX=False)
+        assert got[2] is None and got[3].shape == (5, 3)
+        got = call(X, W, *targets, need_dW=False)
+        assert got[3] is None and got[2].shape == (2, 3)
+        assert [c[0] for c in fakes.calls] == [call.__name__] * 2
+        del fakes.calls[:]

@@ -8,6 +8,12 @@ import pytest
 from paper_1606_00511_amd import hf as H
 
 
+def bare(cls):
+    """An object without a C context; nothing is freed when it goes."""
+    kind = type(cls.__name__, (cls,), {"close": lambda self: None})
+    return kind.__new__(kind)
+
+
 class Fakes:
     """A library that answers `codes` in turn and then HF_OK, and torch's
     current stream."""
@@ -29,7 +35,7 @@ class Fakes:
         return call
 
     def vocab(self):
-        net = H.HFVocab.__new__(H.HFVocab)
+        net = bare(H.HFVocab)
         net._torch, net._h, net._stream = self.torch, 1, None
         net.device = SimpleNamespace(index=0)
         net.workspace = SimpleNamespace(
@@ -71,7 +77,7 @@ def test_every_stream_is_recorded_for_a_nets_workspace(fakes, monkeypatch):
     import torch
     monkeypatch.setattr(torch.cuda, "current_stream",
                         lambda d=None: SimpleNamespace(cuda_stream=fakes.stream))
-    net = H.HFNet.__new__(H.HFNet)
+    net = bare(H.HFNet)
     net._h, net._last, net.device = 1, None, None
     net.workspace = fakes.vocab().workspace
     for s in (0, 0, 5, 0, 7):

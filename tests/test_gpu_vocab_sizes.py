@@ -133,3 +133,128 @@ def test_words_far_below_their_neighbours(rows):
     rel = (2.0 ** -12 + elp + u) * (1 + u) + 2 * rows * E32 + u + 4 * E32
     at = [v + 5 * i for i in range(len(gaps)) for v in (1, 641)]
     within(dW[at], want[at], rel * want[at].abs() + 1e-38, "dW")
+
+
+@pytest.mark.parametrize("name", ["fp32", "bf16"])
+@pytest.mark.parametrize("rows", [100, 300, 3000])
+def test_last_words(name, rows):
+    """Labels among the last words of an odd vocabulary: what these words give
+    is most of each row's gradient, far above the bound of its sum."""
+    torch = T()
+    V, D = 50257, 200
+    X, W, _ = head_inputs(name, rows, V, D)
+    y = (V - 1 - torch.arange(rows, device="cuda") % 130).int()
+    net = H.HFVocab(V, D, rows, name)
+    q_of, used = label_targets(y, V)
+    ref = reference(X, W, q_of, 1.0, used, rows)
+    assert (ref["adX"] * V * E32).mean() < 0.02 * ref["dX"].abs().mean()
+    check_head(name, ref, V, net.hf_vocab_loss_grad(X, W, y), two=name == "bf16" and rows <= 128)
+
+
+# (fp32 and bf16 in pieces, W in place or packed; the last: a piece of W's
+# packing ends within a piece of the logits, in the kept one and those computed
+# again)
+PIECES = [("fp32", 8000, 131075, 72), ("bf16", 8000, 131075, 72), ("bf16", 8000, 131075, 64),
+          ("fp32", 12000, 70000, 2050), ("bf16", 12000, 131500, 2050)]
+
+
+@pytest.mark.parametrize("name,rows,V,D", PIECES)
+def test_pieces_with_all_the_options(name, rows, V, D):
+    """Logits computed again in pieces: with NaN and infinities in masked rows,
+    one gradient only, a strided dW, and dW added to, for labels and lists."""
+    torch = T()
+    torch.cuda.empty_cache()
+    X, W, y = head_inputs(name, rows, V, D)
+    y = mask_rows(y, "some")
+    X[y < 0] = math.nan
+    X[(y < 0).nonzero()[::2, 0]] = math.inf
+    ids, t = teacher(rows, V, 20)
+    ids[y < 0] = IGN
+    net = H.HFVocab(V, D, rows, name)
+    u = unit(name)
+    for call, targets, (q_of, used), tau in (
+            (net.hf_vocab_loss_grad, (y,), label_targets(y, V), 1.0),
+            (net.hf_vocab_distill_grad, (ids, t, 2.0), list_targets(ids, t, 2.0, V), 2.0)):
+        n = int(used.sum())
+        ref = reference(X, W, q_of, tau, used, n, chunk=512)
+        want = [o.clone() for o in call(X, W, *targets)]
+        check_head(name, ref, V, want)
+        assert torch.equal(call(X, W, *targets, need_dW=False)[2], want[2])
+        assert torch.equal(call(X, W, *targets, need_dX=False)[3], want[3])
+        wide = torch.full((V, D + 5), 7.0, device="cuda", dtype=dt(name))
+        call(X, W, *targets, dW=wide[:, 3:3 + D], need_dX=False)
+        assert torch.equal(wide[:, 3:3 + D], want[3])
+        assert (wide[:, :3] == 7).all() and (wide[:, 3 + D:] == 7).all()
+        # dW += : one rounding of the sum
+        old = torch.randn(V, D, generator=gen(9), device="cuda").to(dt(name)) * 1e-3
+        got = call(X, W, *targets, dW=old.clone(), accumulate=True)[3]
+        total = ref["dW"] + old.double()
+        within(got, total, ref["edW"] * (1 + u) + ref["adW"] * (u + (2 * rows + 64) * E32) *
+               (1 + 2 * u) + (u + 4 * E32) * total.abs() + E32 * old.double().abs(), "dW +=")
+        del ref, want, wide, old, got, total
+    net.hf_vocab_check()
+    del net
+    torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("name", ["fp32", "bf16"])
+@pytest.mark.parametrize("rows", [40, 300])
+def test_rows_that_count_with_no_numbers(name, rows):
+    """NaN and infinities in rows that count: NaN or infinity where the
+    definition has one, and nowhere else."""
+    torch = T()
+    V, D = 300, 64
+    X, W, y = head_inputs(name, rows, V, D)
+    y %= 100
+    net = H.HFVocab(V, D, rows, name)
+    want = [o.clone() for o in net.hf_vocab_loss_grad(X, W, y)]
+    for bad in (math.nan, math.inf, -math.inf):
+        Z = X.clone()
+        Z[7, 3] = bad                       # logits of both infinities, or NaN
+        loss, rl, dX, dW = net.hf_vocab_loss_grad(Z, W, y)
+        others = torch.arange(rows, device="cuda") != 7
+        assert rl[7].isnan() and loss[0].isnan() and dX[7].isnan().all() and dW.isnan().all()
+        assert torch.equal(rl[others], want[1][others])
+        assert torch.equal(dX[others], want[2][others])
+        assert net.hf_vocab_loss(Z, W, y)[0].isnan()
+        # a list of two on every row, with the label's place first
+        ids = torch.stack([y, y + 100], 1).int()
+        t = torch.zeros(rows, 2, device="cuda")
+        good = [o.clone() for o in net.hf_vocab_distill_grad(X, W, ids, t)]
+        for got in (net.hf_vocab_distill_grad(Z, W, ids, t),):
+            assert got[1][7].isnan() and got[2][7].isnan().all() and got[3].isnan().all()
+            assert torch.equal(got[2][others], good[2][others])
+        if bad != -math.inf:                # (which is a masked place)
+            t[7, 1] = bad
+            got = net.hf_vocab_distill_grad(X, W, ids, t)
+            assert got[1][7].isnan() and got[2][7].isnan().any()
+            assert torch.equal(got[2][others], good[2][others])
+
+
+@pytest.mark.parametrize("name", ["fp32", "bf16"])
+@pytest.mark.parametrize("rows", [40, 300])
+def test_words_without_probability(name, rows):
+    """Words whose logits are -inf (a column of X at 1, -inf there in their
+    rows of W): the others' losses are those of the vocabulary without them;
+    a label there has a loss of infinity; every word there, the loss is NaN."""
+    torch = T()
+    V, D = 700, 64
+    X, W, y = head_inputs(name, rows, V, D)
+    X[:, 0], W[:, 0] = 1, 0
+    y %= 100
+    net = H.HFVocab(V, D, rows, name)
+    q_of, used = label_targets(y, 300)
+    ref = reference(X, W[:300].contiguous(), q_of, 1.0, used, rows)
+    W[300:, 0] = -math.inf                  # whole entries of the statistics
+    loss, rl = net.hf_vocab_loss(X, W, y)
+    check_head(name, ref, V, (loss, rl, None, None))
+    loss, rl, dX, dW = net.hf_vocab_loss_grad(X, W, y)
+    check_head(name, ref, V, (loss, rl, None, dW[:300]), two=name == "bf16" and rows <= 128)
+    assert (dW[300:] == 0).all()
+    # 0 times -inf in the column, as the definition has it; the others as ever
+    assert dX[:, 0].isnan().all() and torch.isfinite(dX[:, 1:]).all()
+    y[5] = 650
+    rl = net.hf_vocab_loss(X, W, y)[1]
+    assert rl[5].item() == math.inf and torch.isfinite(rl[:5]).all()
+    W[:, 0] = -math.inf
+    assert net.hf_vocab_loss(X, W, y)[1].isnan().all()

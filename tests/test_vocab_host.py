@@ -180,3 +180,50 @@ def test_gradients_at_both_limits(stub):
     fits(lines)
     assert len(launches(lines, "hf_vocab_finish")) >= 2
     fits(hip_stub.run(stub, LIMITS % (9, "L.hf_vocab_embed_grad(h, IN, T, 1.0, IN, D, OUT, D, 0)")))
+
+
+@pytest.mark.parametrize("call", [
+    "L.hf_vocab_loss(h, IN, 64, IN, 64, IN, 4, 0.0, IN, None)",
+    "L.hf_vocab_loss_grad(h, IN, 64, IN, 64, IN, 4, 0.0, IN, None, OUT, 64, OUT, 64, 0)",
+    "L.hf_vocab_distill(h, IN, 64, IN, 64, IN, 8, IN, 8, 8, 1.0, 4, 0.0, IN, None)",
+    "L.hf_vocab_distill_grad(h, IN, 64, IN, 64, IN, 8, IN, 8, 8, 1.0, 4, 0.0, IN, None, OUT, 64,"
+    " OUT, 64, 0)",
+    "L.hf_vocab_embed(h, IN, 64, IN, 4, 1.0, OUT, 64)",
+    "L.hf_vocab_embed_grad(h, IN, 4, 1.0, IN, 64, OUT, 64, 0)"])
+def test_every_call_is_ordered(stub, call):
+    """Eager, captured on a second stream, eager on a third: every call with
+    kernels on the workspace keeps the order."""
+    lines, at, to = hip_stub.run(stub, """
+h = vocab(stream=0xa00)
+def call():
+    assert %s == H.HF_OK
+call()
+S.stub_capture(0xb00, 1)
+assert L.hf_vocab_set_stream(h, 0xb00) == H.HF_OK
+at = len(S.stub_log().splitlines())
+call()
+to = len(S.stub_log().splitlines())
+S.stub_capture(0xb00, 0)
+assert L.hf_vocab_set_stream(h, 0xc00) == H.HF_OK
+call()
+result = [log(), at, to]
+""" % call)
+    used = [l[-1] for l in lines if l[0] == "launch"]
+    assert {A, B, C} == set(used) and used.count(A) == used.count(B) == used.count(C)
+    assert hip_stub.unordered(lines, [(B, at, to)]) == []
+
+
+def test_check_waits_for_the_calls_before(stub):
+    """hf_vocab_check on a stream that could not be made to wait yet: it waits
+    for the calls on the one before too."""
+    lines = hip_stub.run(stub, EMBED + """
+h = vocab(stream=0xa00)
+assert call() == H.HF_OK
+S.stub_capture(0xa00, 1)
+assert L.hf_vocab_set_stream(h, 0xb00) == H.HF_OK
+S.stub_capture(0xa00, 0)
+log()
+assert L.hf_vocab_check(h) == H.HF_OK
+result = log()
+""")
+    assert ["sync", A] in lines and ["sync", B] in lines

@@ -432,7 +432,10 @@ int hf_prof_get(hf_ctx* ctx, int32_t i, const char** name, int64_t* launches,
  * The vocabulary ends of a token model: the embedding in front of a net, and
  * behind it the softmax head over a vocabulary larger than HF_MAX_CLASSES,
  * with the loss of hard labels or of a teacher's top logits.  With tied
- * weights the embedding and the head share one matrix and one gradient.
+ * weights the embedding and the head share one matrix and one gradient.  What
+ * lies between them (rows in, their gradient back) is the caller's: an hf_ctx
+ * takes no rows from an embedding that is trained with it, and gives no
+ * activations to a head; and the solvers have no curvature product of these.
  *
  * A context (hf_vocab) holds the vocabulary V, the width D and the type of
  * the rows, the matrices and their gradients: fp32 or bf16 (sums, softmax

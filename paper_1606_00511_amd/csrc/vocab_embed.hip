@@ -581,7 +581,8 @@ void vocab_embed(const Launch& L, int type, const void* E, long long lde, int V,
   const long long groups = ((long long)T * strips + 3) / 4;
   const dim3 grid((unsigned)std::min(groups, MAX_X), (unsigned)((groups + MAX_X - 1) / MAX_X));
   // _s: much output does not take the place of frequent tokens' rows of E in the
-  // caches (65,536 x 4,096 of bf16: 179 -> 104 us); little stays for its reader
+  // caches (65,536 x 4,096 of bf16: with cold caches 179 -> 160 us, call after call
+  // 182 -> 108); little stays for its reader
   const bool stream = (long long)T * D * es > L2_BYTES;
 #define HF_EMB(SUF, E_T)                                                                   \
   HF_LAUNCH("hf_vocab_embed",                                                              \

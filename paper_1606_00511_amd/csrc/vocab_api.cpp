@@ -295,6 +295,7 @@ void head(hf_vocab* c, VRows r, const void* X, int64_t ldx, const void* W, int64
   r.st = c->st();
   r.pos = c->at<int>(l.pos);
   r.idx = c->at<int>(l.idx);
+  r.lab = c->at<int>(l.tid);
   if (!r.row_loss) r.row_loss = c->at<float>(l.rloss);
   const bool keep = g && keeps(c, T);
   const int dup = keep ? two_term(c, T) : 0;
@@ -349,6 +350,13 @@ void head(hf_vocab* c, VRows r, const void* X, int64_t ldx, const void* W, int64
   e.zscale = 1.0f / r.tau;
   e.stat = stat;
   e.ldstat = tiles;
+  // labels' logits that are not kept in fp32
+  const bool dots = !keep || f16;
+  VTarget tg = {c->at<float>(l.zt), nullptr, nullptr};
+  if (dots && !r.t) {
+    e.lab = r.lab;
+    e.zt = tg.zt;
+  }
   auto logits = [&](int v0, int n, bool keep_it) {
     VGemm q = {};
     q.A = matrix(v0, n, &q.lda);
@@ -367,6 +375,7 @@ void head(hf_vocab* c, VRows r, const void* X, int64_t ldx, const void* W, int64
     q.splits = 1;
     q.tile = tile;
     e.tile0 = v0 / sg;
+    e.v0 = v0;
     e.z = keep_it && z ? z + v0 : nullptr;
     e.pt = keep_it && f16 ? (char*)d + (size_t)v0 * 2 : nullptr;
     e.ldz = ldd;
@@ -377,13 +386,11 @@ void head(hf_vocab* c, VRows r, const void* X, int64_t ldx, const void* W, int64
   for (int v0 = 0; v0 < kept; v0 += wrows) logits(v0, std::min(wrows, kept - v0), true);
 
   // ---- losses
-  VTarget tg = {c->at<float>(l.zt), nullptr, nullptr};
   if (g) {
     tg.id = c->at<int>(l.tid);
     tg.dt = c->at<float>(l.tdt);
   }
   const bool self = dup > 0;             // few rows: with delta
-  const bool dots = !keep || f16;
   bool summed = false;
   if (!self)
     summed = vocab_row_loss(L, type, r, stat, tiles, tiles, dots ? nullptr : z, ldd, tg, lse, xd,

@@ -383,6 +383,19 @@ __device__ __forceinline__ void vgemm_body(const VGemm& s, const VEpi& e) {
 #pragma unroll
   for (int i = 0; i < S; ++i)
     if (i < nblk) issue(vb0 + i, i);
+  // the rows' labels, for the epilogue: behind the first stages, which the waits
+  // below are for (4,096 rows, 50,257 x 768: a loss 314 -> 317 us, where a pass of
+  // its own over the labels' rows of W took 2 in hf_vocab_row_loss; ahead of the
+  // stages 324 -> 329)
+  constexpr bool STATS = EPI == E_LOGITS || EPI == E_EXPS;
+  int lab[WN];
+  if constexpr (STATS) {
+#pragma unroll
+    for (int b = 0; b < WN; ++b) {
+      const int n = n0 + wn * 32 * WN + 32 * b + li;
+      lab[b] = e.lab && n < N ? e.lab[n] : -1;
+    }
+  }
   if (nblk > 0) {
     if (nblk >= S) wait_vm<(S - 1) * LPB>();
     else wait_vm<0>();
@@ -427,7 +440,6 @@ __device__ __forceinline__ void vgemm_body(const VGemm& s, const VEpi& e) {
   constexpr int RL = 32 * WM;
   static_assert(NW * 32 * RL * 4 <= S * STAGE * (int)sizeof(E), "staging exceeds the stages");
   float* const mine = (float*)lds + wave * 32 * RL;
-  constexpr bool STATS = EPI == E_LOGITS || EPI == E_EXPS;
   if constexpr (STATS) {
     // row statistics of the wave's columns: within the lane, then the two
     // halves of the wave.  exp(z - max) = exp2((acc - max) c): an argument off
@@ -435,6 +447,10 @@ __device__ __forceinline__ void vgemm_body(const VGemm& s, const VEpi& e) {
     // exact enough for fp32
     const float c2 = e.zscale * 1.44269504f;
     const bool full = m0 + RM <= s.M;
+    // (a wait for one of them further down would be a wait for the stores before
+    // it too)
+#pragma unroll
+    for (int b = 0; b < WN; ++b) asm volatile("" : "+v"(lab[b]));
 #pragma unroll
     for (int b = 0; b < WN; ++b) {
       if (!full) {
@@ -443,6 +459,23 @@ __device__ __forceinline__ void vgemm_body(const VGemm& s, const VEpi& e) {
 #pragma unroll
           for (int r = 0; r < 16; ++r)
             if (mw + 32 * a + 8 * (r >> 2) + (r & 3) >= s.M) acc[a][b][r] = -INFINITY;
+      }
+      // The label's logit, the very number that is in the sums: of a word with
+      // nearly all the probability a logit summed in another order is off by
+      // more than what is left for the others.  Few waves have one (128 of
+      // 50,000 columns, 32 rows: 8%).
+      if (e.lab) {
+        const int d = lab[b] - e.v0 - mt;
+        const bool here = lab[b] >= 0 && d >= 0 && d < RL && ((d >> 2) & 1) == h;
+        if (__ballot(here)) {
+          float x = 0.0f;
+#pragma unroll
+          for (int a = 0; a < WM; ++a)
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+              if (4 * (d >> 3) + (d & 3) == 16 * a + r) x = acc[a][b][r];
+          if (here) e.zt[nt + 32 * b + li] = x * e.zscale;
+        }
       }
       float mx = -INFINITY;
 #pragma unroll

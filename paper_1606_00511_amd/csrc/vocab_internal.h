@@ -75,6 +75,9 @@ struct VEpi {
   long long ldz;
   float2* stat;          // per row and entry: max, sum of exp(z - max)
   int ldstat, tile0;     // entries per row; index of this launch's first
+  const int* lab;        // the rows' labels, whose logits go to zt; or null
+  float* zt;
+  int v0;                // this launch's first column
   const float* lse;      // p: log-sum-exp per row
   void* d;               // delta, row n, column m
   long long ldd;
@@ -114,6 +117,7 @@ struct VRows {
   VocabState* st;
   int* pos;                 // T: packed row of a row, -1: not counted
   int* idx;                 // the row of a packed row
+  int* lab;                 // labels: that of a packed row
   float* row_loss;          // T
 };
 // which rows count: pos, idx and the state; zero losses for those that do not.
@@ -135,8 +139,8 @@ struct VTarget {
   float* dt;                // packed row x K: delta at the target
 };
 // log-sum-exp from the statistics, the rows' losses and the targets' delta;
-// z: kept logits or null (then the targets' are formed of X or xp and W).
-// True: the loss is summed too.
+// z: kept logits or null (then a label's is in t.zt, and those of lists are
+// formed of X or xp and W).  True: the loss is summed too.
 bool vocab_row_loss(const Launch& L, int type, const VRows& r, const float2* stat, int ldstat,
                     int tiles, const float* z, long long ldz, const VTarget& t, float* lse,
                     const void* X, long long ldx, const void* xp, int Dp, const void* W,

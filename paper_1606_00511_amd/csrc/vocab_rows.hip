@@ -139,25 +139,29 @@ extern "C" __global__ __launch_bounds__(1024) void hf_vocab_count(VRows r) {
           have = v[u] >= 0 && v[u] < r.V;
           if (i < t1 && !have && v[u] != IGNORE) r.st->err = 1;
         }
-        f(i, i < t1, i < t1 && have);
+        f(i, i < t1, i < t1 && have, v[u]);
       }
     }
   };
   int c = 0, at = 0, n = 0;
-  each([&](int, bool, bool have) { c += __popcll(__ballot(have)); });
+  each([&](int, bool, bool have, int) { c += __popcll(__ballot(have)); });
   if (lane == 0) sums[wave] = c;
   __syncthreads();
   for (int w = 0; w < 16; ++w) {
     if (w < wave) at += sums[w];
     n += sums[w];
   }
-  each([&](int i, bool in, bool have) {
+  each([&](int i, bool in, bool have, int id) {
     const unsigned long long m = __ballot(have);
     const int p = at + __popcll(m & ((1ull << lane) - 1));
     at += __popcll(m);
     if (in) r.pos[i] = have ? p : -1;
-    if (have) r.idx[p] = i;
-    else if (in) r.row_loss[i] = 0.0f;
+    if (have) {
+      r.idx[p] = i;
+      if (!r.t) r.lab[p] = id;
+    } else if (in) {
+      r.row_loss[i] = 0.0f;
+    }
   });
   if (threadIdx.x == 0) set_state(r, n);
 }
@@ -197,18 +201,23 @@ __device__ __forceinline__ void pack_body(const VRows& r, const E* X, long long 
   if constexpr (SELF) {
     __shared__ int sums[4], place[SELF_ROWS];
     const int t = threadIdx.x;
-    bool have = false;
+    int id = -1;
     float v;
     if (t < r.T)
-      for (int k = 0; k < r.K && !have; ++k) have = target(r, t, k, &v) >= 0;
+      for (int k = 0; k < r.K && id < 0; ++k) id = target(r, t, k, &v);
+    const bool have = id >= 0;
     const int at = scan_threads<4>(have, sums, n);
     place[t] = have ? at : -1;
     __syncthreads();
     if (b < r.T) pos = place[b];
     if (b == 0) {
       if (t < r.T) {
-        if (have) r.idx[at] = t;
-        else r.row_loss[t] = 0.0f;
+        if (have) {
+          r.idx[at] = t;
+          if (!r.t) r.lab[at] = id;
+        } else {
+          r.row_loss[t] = 0.0f;
+        }
       }
       if (t == 0) set_state(r, n);
     }
@@ -283,8 +292,9 @@ extern "C" __global__ __launch_bounds__(256) void hf_vocab_copy_bf16(
 }
 
 // ---------------------------------------------------- the targets' logits
-// Where the logits are not kept in fp32: the products x_j . W[id] of a packed
-// row, U of them at a time per wave.  Bound by the reads of W's rows.
+// Where the logits are not kept in fp32, those of lists (a label's comes with the
+// statistics): the products x_j . W[id] of a packed row, U of them at a time per
+// wave.  Bound by the reads of W's rows.
 namespace {
 // what they are formed of; X: the rows in place where all count, or null
 struct VDots {
@@ -375,13 +385,12 @@ struct RowTargets {          // lane l: targets l and l + 64
   int id[2];                 // -1: none, or a repeat
   float dt[2];               // delta at the target
 };
-// One packed row j < n by one wave.  The targets' logits: in zt, or (null) in
-// z, or (a label, both null) x.
+// One packed row j < n by one wave.  The targets' logits: in zt, or (null) in z.
 __device__ __forceinline__ RowTargets row_targets(const VRows& r, int j,
                                                   const float2* __restrict__ stat, int ldstat,
                                                   int tiles, const float* __restrict__ z,
-                                                  long long ldz, const float* __restrict__ zt,
-                                                  float x0) {
+                                                  long long ldz,
+                                                  const float* __restrict__ zt) {
   const int lane = threadIdx.x & 63, t = r.idx[j];
   RowTargets o;
   const float2* st = stat + (size_t)j * ldstat;
@@ -404,7 +413,8 @@ __device__ __forceinline__ RowTargets row_targets(const VRows& r, int j,
     m = top;
   }
   const float mx = wave_max(m), at = mx == -INFINITY ? 0.0f : mx;
-  o.lse = at + logf(wave_sum(s * expf(m - at)));
+  const float ls = logf(wave_sum(s * expf(m - at)));
+  o.lse = at + ls;
 
   int id[2] = {-1, -1};
   float tl[2] = {0.0f, 0.0f}, q[2] = {0.0f, 0.0f}, lz[2] = {0.0f, 0.0f};
@@ -414,9 +424,12 @@ __device__ __forceinline__ RowTargets row_targets(const VRows& r, int j,
       const int k = lane + 64 * i;
       id[i] = target(r, t, k, &tl[i]);
       if (id[i] >= 0) {
-        const float x = zt ? zt[(size_t)j * r.K + k] : z ? z[(size_t)j * ldz + id[i]] : x0;
-        // log p; above 0 only by rounding (the comparison keeps a NaN)
-        lz[i] = x - o.lse > 0.0f ? 0.0f : x - o.lse;
+        const float x = zt ? zt[(size_t)j * r.K + k] : z[(size_t)j * ldz + id[i]];
+        // log p, of the difference to the largest, which for a target with nearly
+        // all the probability is 0 where lse is rounded to its own size; above 0
+        // only by rounding (the comparison keeps a NaN)
+        const float lp = (x - at) - ls;
+        lz[i] = lp > 0.0f ? 0.0f : lp;
       }
     }
   float loss = 0.0f;
@@ -490,25 +503,14 @@ __device__ __forceinline__ void loss_sum(const float* row_loss, int T, const Voc
   if (threadIdx.x == 0) *loss = (float)(((ws[0] + ws[1]) + (ws[2] + ws[3])) * st->inv);
 }
 }  // namespace
-// One wave per packed row.  DOT: the label's logit is formed here.  With `loss`
-// (few rows, one workgroup) the rows' losses are summed as well.
-namespace {
-template <class E, bool DOT>
-__device__ __forceinline__ void row_loss_body(const VRows& r, const float2* stat, int ldstat,
-                                              int tiles, const float* z, long long ldz,
-                                              const VTarget& tg, float* lse, const VDots& q,
-                                              float* loss) {
+// One wave per packed row.  With `loss` (few rows, one workgroup) the rows' losses
+// are summed as well.
+extern "C" __global__ __launch_bounds__(256) void hf_vocab_row_loss(
+    VRows r, const float2* stat, int ldstat, int tiles, const float* z, long long ldz,
+    VTarget tg, float* lse, float* loss) {
   const int lane = threadIdx.x & 63, waves = blockDim.x >> 6;
   for (int j = blockIdx.x * waves + (threadIdx.x >> 6); j < r.st->n; j += gridDim.x * waves) {
-    float x0 = 0.0f;
-    if constexpr (DOT) {
-      float v, s[1];
-      const int id[1] = {target(r, r.idx[j], 0, &v)};
-      dots<E, 1, 64>(r, q, j, id, s);
-      x0 = s[0];
-    }
-    const RowTargets o = row_targets(r, j, stat, ldstat, tiles, DOT ? nullptr : z, ldz,
-                                     DOT || z ? nullptr : tg.zt, x0);
+    const RowTargets o = row_targets(r, j, stat, ldstat, tiles, z, ldz, z ? nullptr : tg.zt);
     if (lane == 0) {
       lse[j] = o.lse;
       r.row_loss[r.idx[j]] = o.loss;
@@ -526,16 +528,6 @@ __device__ __forceinline__ void row_loss_body(const VRows& r, const float2* stat
     loss_sum(r.row_loss, r.T, r.st, loss);
   }
 }
-}  // namespace
-#define HF_ROW_LOSS(SUF, E, DOT)                                                          \
-  extern "C" __global__ __launch_bounds__(256) void hf_vocab_row_loss##SUF(               \
-      VRows r, const float2* stat, int ldstat, int tiles, const float* z, long long ldz,  \
-      VTarget tg, float* lse, VDots q, float* loss) {                                     \
-    row_loss_body<E, DOT>(r, stat, ldstat, tiles, z, ldz, tg, lse, q, loss);              \
-  }
-HF_ROW_LOSS(, float, false)
-HF_ROW_LOSS(_f32, float, true)
-HF_ROW_LOSS(_bf16, bf16_t, true)
 
 extern "C" __global__ __launch_bounds__(256) void hf_vocab_loss_sum(
     const float* __restrict__ row_loss, int T, const VocabState* st, float* loss) {
@@ -578,8 +570,7 @@ __device__ __forceinline__ void delta_body(const VRows& r, const VDelta& a, E* d
   if constexpr (SELF) {
     if (real && threadIdx.x < 64) {
       const int lane = threadIdx.x;
-      const RowTargets o = row_targets(r, j, a.stat, a.ldstat, a.tiles, a.z, a.ldz, nullptr,
-                                       0.0f);
+      const RowTargets o = row_targets(r, j, a.stat, a.ldstat, a.tiles, a.z, a.ldz, nullptr);
       if (lane == 0) {
         lse_s = o.lse;
         if (c0 == 0) r.row_loss[r.idx[j]] = o.loss;
@@ -825,18 +816,15 @@ bool vocab_row_loss(const Launch& L, int type, const VRows& r, const float2* sta
                     long long ldw, float* loss) {
   if (r.T < 1) return false;
   const VDots q = {X, xp, W, ldx, ldw, Dp};
-  if (!z && r.K > 1) {
+  if (!z && r.t) {
     if (type == VT_F32)
       HF_LAUNCH("hf_vocab_tlogit", hf_vocab_tlogit_f32, r.T, 256, r, q, t.zt);
     else
       HF_LAUNCH("hf_vocab_tlogit", hf_vocab_tlogit_bf16, r.T, 256, r, q, t.zt);
   }
-  const bool sum = loss && r.T <= SUM_ROWS, dot = !z && r.K == 1;
-  HF_LAUNCH("hf_vocab_row_loss",
-            (!dot ? hf_vocab_row_loss : type == VT_F32 ? hf_vocab_row_loss_f32
-                                                       : hf_vocab_row_loss_bf16),
-            sum ? 1 : (r.T + 3) / 4, 256, r, stat, ldstat, tiles, z, ldz, t, lse, q,
-            sum ? loss : nullptr);
+  const bool sum = loss && r.T <= SUM_ROWS;
+  HF_LAUNCH("hf_vocab_row_loss", hf_vocab_row_loss, sum ? 1 : (r.T + 3) / 4, 256, r, stat, ldstat,
+            tiles, z, ldz, t, lse, sum ? loss : nullptr);
   return sum;
 }
 

@@ -10,7 +10,8 @@
 //               piece's share of dX and rows of dW.  The first piece is the
 //               pass's last, and its logits are kept: they need no second
 //               computation
-// A loss without its gradient never keeps a logit.
+// A loss without its gradient keeps none, but for few rows with lists, whose
+// targets' are then read there.
 #include "hf.h"
 #include "vocab_internal.h"
 
@@ -108,6 +109,17 @@ inline size_t col_bytes(const hf_vocab* c, int64_t T) {
 }
 inline bool keeps(const hf_vocab* c, int64_t T) {
   return T <= TWO_TERM_ROWS || col_bytes(c, T) * up(c->V, VTILE) <= KEEP_BYTES;
+}
+// Whether a loss alone with lists of K targets keeps its logits, in fp32, to read
+// the targets' there, rather than form these again (vocab_tlogit: a launch, rows
+// of W at 7 TB/s, and a wave waits about 1 us for memory every 64 (fp32) or 128
+// columns); us either way
+inline bool reads_lists(const hf_vocab* c, int64_t T, int K) {
+  if (T > TWO_TERM_ROWS && (c->type != VT_F32 || !keeps(c, T))) return false;
+  const double keep = 4.0 * (double)T * c->V / 6e6;
+  const double again = 4.0 + c->D / (c->type == VT_F32 ? 64.0 : 128.0) +
+                       (double)T * K * c->D * c->es / 7e6;
+  return keep < again;
 }
 // columns of a piece: as many as are kept
 inline int piece_cols(const hf_vocab* c, int64_t T) {
@@ -298,6 +310,7 @@ void head(hf_vocab* c, VRows r, const void* X, int64_t ldx, const void* W, int64
   r.lab = c->at<int>(l.tid);
   if (!r.row_loss) r.row_loss = c->at<float>(l.rloss);
   const bool keep = g && keeps(c, T);
+  const bool lists = !g && r.t && reads_lists(c, T, r.K);
   const int dup = keep ? two_term(c, T) : 0;
   float* lse = c->at<float>(l.lse);
   float2* stat = c->at<float2>(l.stat);
@@ -335,15 +348,15 @@ void head(hf_vocab* c, VRows r, const void* X, int64_t ldx, const void* W, int64
   // ---- statistics of the whole vocabulary, and the logits of the first piece
   // (with `keep`, all of them)
   const int Rp = (int)tile_rows(T);
-  const int vc = !g ? V : keep ? V : piece_cols(c, T);
+  const int vc = !g || keep ? V : piece_cols(c, T);
   const long long ldd = up(vc, VTILE);
   // fp32: logits, then delta in their place; bf16: exponentials, then delta;
   // few bf16 rows: fp32 logits, and delta behind them
-  const bool f16 = type == VT_BF16 && !dup;
-  float* z = g && !f16 ? c->at<float>(l.z) : nullptr;
+  const bool f16 = type == VT_BF16 && !dup && !lists;
+  float* z = (g && !f16) || lists ? c->at<float>(l.z) : nullptr;
   void* d = !g ? nullptr : dup ? (void*)(z + (size_t)T * ldd) : c->at<void>(l.z);
   const int sstep = std::min(wrows, vc);
-  const int tile = shape_for(type, g ? sstep : wrows, T, Dp, false, !(g && f16)).tile;
+  const int tile = shape_for(type, sstep, T, Dp, false, !(g && f16)).tile;
   const int sg = tile_stat(tile);
   const int tiles = (V + sg - 1) / sg;
   VEpi e = {};
@@ -351,7 +364,7 @@ void head(hf_vocab* c, VRows r, const void* X, int64_t ldx, const void* W, int64
   e.stat = stat;
   e.ldstat = tiles;
   // labels' logits that are not kept in fp32
-  const bool dots = !keep || f16;
+  const bool dots = (!keep && !lists) || f16;
   VTarget tg = {c->at<float>(l.zt), nullptr, nullptr};
   if (dots && !r.t) {
     e.lab = r.lab;
@@ -381,8 +394,8 @@ void head(hf_vocab* c, VRows r, const void* X, int64_t ldx, const void* W, int64
     e.ldz = ldd;
     vocab_logits(L, type, q, e);
   };
-  for (int v0 = g ? vc : 0; v0 < V; v0 += wrows) logits(v0, std::min(wrows, V - v0), false);
-  const int kept = g ? std::min(vc, V) : 0;
+  const int kept = g || lists ? std::min(vc, V) : 0;
+  for (int v0 = kept; v0 < V; v0 += wrows) logits(v0, std::min(wrows, V - v0), false);
   for (int v0 = 0; v0 < kept; v0 += wrows) logits(v0, std::min(wrows, kept - v0), true);
 
   // ---- losses

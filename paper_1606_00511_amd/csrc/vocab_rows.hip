@@ -293,8 +293,18 @@ extern "C" __global__ __launch_bounds__(256) void hf_vocab_copy_bf16(
 
 // ---------------------------------------------------- the targets' logits
 // Where the logits are not kept in fp32, those of lists (a label's comes with the
-// statistics): the products x_j . W[id] of a packed row, U of them at a time per
-// wave.  Bound by the reads of W's rows.
+// statistics): the products x_j . W[id] of a packed row, bit for bit as the
+// logits' MFMAs sum them.  A logit summed in another order would be off, against
+// the sums of the softmax, by as much as is left for the other words where a
+// target has nearly all the probability.
+//   bf16  the same MFMAs, 32 targets a wave, with the target's row of W as a row
+//         of A and its row of X as a column of B, of which the diagonal is used
+//   fp32  32 x 32 x 2 MFMAs are a chain of fused multiply-adds, k after k: here
+//         one a lane, in the order in which the fragments hold the ks
+// Bound by the reads of W's rows (3,686 rows of 64 targets, 2,048 columns of bf16,
+// 966 MB: 134 us, 7.2 TB/s from the caches; with 16 bytes of a row a lane straight
+// into the fragments, 32 bytes of a line at a time, 170), and where there are few
+// by the trips to memory one after the other.
 namespace {
 // what they are formed of; X: the rows in place where all count, or null
 struct VDots {
@@ -302,80 +312,127 @@ struct VDots {
   long long ldx, ldw;
   int Dp;
 };
-template <class E, int U, int LANES>
-__device__ __forceinline__ void dots(const VRows& r, const VDots& q, int j, const int (&id)[U],
-                                     float (&s)[U]) {
-  constexpr int EPC = 16 / sizeof(E);
-  const int lane = threadIdx.x & (LANES - 1);
-  const E* x = q.X && r.st->n == r.T ? (const E*)q.X + (size_t)j * q.ldx
-                                     : (const E*)q.xp + (size_t)j * q.Dp;
-  const E* w[U];          // (no target: the first row, its product unused)
-#pragma unroll
-  for (int u = 0; u < U; ++u) {
-    w[u] = (const E*)q.W + (size_t)max(id[u], 0) * q.ldw;
-    s[u] = 0.0f;
-  }
-  for (int c = EPC * lane; c < r.D; c += LANES * EPC) {
-    E a[EPC], b[U][EPC];
-    if (c + EPC <= r.D) {
-#pragma unroll
-      for (int u = 0; u < U; ++u) __builtin_memcpy(b[u], w[u] + c, 16);
-      __builtin_memcpy(a, x + c, 16);
-    } else {
-#pragma unroll
-      for (int i = 0; i < EPC; ++i) {
-        a[i] = c + i < r.D ? x[c + i] : (E)0;
-#pragma unroll
-        for (int u = 0; u < U; ++u) b[u][i] = c + i < r.D ? w[u][c + i] : (E)0;
-      }
-    }
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-#pragma unroll
-      for (int i = 0; i < EPC; ++i) s[u] += to_f(a[i]) * to_f(b[u][i]);
-  }
-#pragma unroll
-  for (int u = 0; u < U; ++u) {
-#pragma unroll
-    for (int o = LANES / 2; o > 0; o >>= 1) s[u] += __shfl_xor(s[u], o, 64);
-    s[u] /= r.tau;
-  }
-}
-// lists: LANES lanes take up to four targets at a time, a workgroup a row
-template <class E, int LANES>
-__device__ __forceinline__ void tlogit_row(const VRows& r, const VDots& q, int j, float* zt) {
-  constexpr int U = 4, G = 256 / LANES;
-  const int t = r.idx[j], g = threadIdx.x / LANES;
-  float v;
-  for (int k0 = g; k0 < r.K; k0 += U * G) {
-    int id[U];
-    float s[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u) id[u] = k0 + u * G < r.K ? target(r, t, k0 + u * G, &v) : -1;
-    dots<E, U, LANES>(r, q, j, id, s);
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-      if ((threadIdx.x & (LANES - 1)) == 0 && id[u] >= 0)
-        zt[(size_t)j * r.K + k0 + u * G] = s[u];
-  }
-}
-// A row of W that one load of a wave covers (1 KiB) leaves lanes without work:
-// a quarter of a wave each then (7,276 rows of 57 targets, 128 columns of bf16:
-// 56 -> 27 us; 2,048 columns keep the wave, at 7.1 TB/s).
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+// 16 bytes of a row from column c on, zeros past its D columns
 template <class E>
-__device__ __forceinline__ void tlogit_body(const VRows& r, const VDots& q, float* zt) {
-  const int j = blockIdx.x;
-  if (j >= r.st->n) return;
-  if (r.D * (int)sizeof(E) <= 1024) tlogit_row<E, 16>(r, q, j, zt);
-  else tlogit_row<E, 64>(r, q, j, zt);
+__device__ __forceinline__ u32x4 row_chunk(const E* row, int c, int D) {
+  constexpr int EPC = 16 / sizeof(E);
+  u32x4 v = u32x4{0u, 0u, 0u, 0u};
+  if (c + EPC <= D) {
+    __builtin_memcpy(&v, row + c, 16);
+  } else if (c < D) {
+    E w[EPC];
+#pragma unroll
+    for (int i = 0; i < EPC; ++i) w[i] = c + i < D ? row[c + i] : (E)0;
+    v = __builtin_bit_cast(u32x4, w);
+  }
+  return v;
+}
+
+// A wave has P pairs: pair p is target p % K of packed row p / K.  RB bytes of
+// each pair's row of W at a time come in whole 128-byte lines, through LDS, with
+// the next ones on their way; X's rows, which pairs share, straight from the
+// caches.  (fp32, 64 pairs and 128 bytes: 300 rows of 32 targets, 768 columns, 17
+// us more.)
+template <class E>
+struct Pairs {
+  static constexpr bool F32 = sizeof(E) == 4;
+  static constexpr int P = 32, RB = 256;
+  static constexpr int EPC = 16 / sizeof(E), CH = RB / 16, N = RB / sizeof(E);
+  static constexpr int LOADS = P * CH / 64, STRIDE = RB + 16;   // (STRIDE: LDS banks)
+  static constexpr int XL = F32 ? CH : CH / 2;                  // chunks of X a lane needs
+};
+
+// f(chunk g of X, chunk g of W) of the wave's pairs from the first column on;
+// lane's pair: lane % P, its chunks: all (fp32, both halves of the wave alike), or
+// every second (bf16)
+template <class E, class F>
+__device__ __forceinline__ void over_pairs(const VRows& r, const VDots& q, int first, int all,
+                                           F f) {
+  using S = Pairs<E>;
+  __shared__ __attribute__((aligned(16))) char lds[4][S::P * S::STRIDE];
+  char* const mine = lds[threadIdx.x >> 6];
+  const int lane = threadIdx.x & 63, li = lane % S::P, h = lane / S::P;
+  const int p = min(first + li, all - 1), j = p / r.K;
+  float v;
+  // (no target: the first row, its product unused)
+  const int id = max(target(r, r.idx[j], p % r.K, &v), 0);
+  const E* const x = q.X && r.st->n == r.T ? (const E*)q.X + (size_t)j * q.ldx
+                                           : (const E*)q.xp + (size_t)j * q.Dp;
+  const E* w[S::LOADS];
+#pragma unroll
+  for (int i = 0; i < S::LOADS; ++i)
+    w[i] = (const E*)q.W + (size_t)__shfl(id, (64 * i + lane) / S::CH, 64) * q.ldw;
+  u32x4 a[S::LOADS], b[S::XL];
+  auto fetch = [&](int c0) {
+#pragma unroll
+    for (int i = 0; i < S::LOADS; ++i)
+      a[i] = row_chunk(w[i], c0 + S::EPC * ((64 * i + lane) % S::CH), r.D);
+#pragma unroll
+    for (int g = 0; g < S::XL; ++g)
+      b[g] = row_chunk(x, c0 + S::EPC * (S::F32 ? g : 2 * g + h), r.D);
+  };
+  fetch(0);
+  for (int c0 = 0; c0 < r.D; c0 += S::N) {
+    u32x4 now[S::XL];
+#pragma unroll
+    for (int i = 0; i < S::LOADS; ++i)
+      *(u32x4*)(mine + (64 * i + lane) / S::CH * S::STRIDE + (64 * i + lane) % S::CH * 16) = a[i];
+#pragma unroll
+    for (int g = 0; g < S::XL; ++g) now[g] = b[g];
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    if (c0 + S::N < r.D) fetch(c0 + S::N);
+#pragma unroll
+    for (int g = 0; g < S::XL; ++g)
+      f(now[g], *(const u32x4*)(mine + li * S::STRIDE + (S::F32 ? g : 2 * g + h) * 16), g);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+  }
 }
 }  // namespace
-extern "C" __global__ __launch_bounds__(256) void hf_vocab_tlogit_f32(VRows r, VDots q, float* zt) {
-  tlogit_body<float>(r, q, zt);
-}
+
 extern "C" __global__ __launch_bounds__(256) void hf_vocab_tlogit_bf16(VRows r, VDots q,
-                                                                       float* zt) {
-  tlogit_body<bf16_t>(r, q, zt);
+                                                                       float zscale, float* zt) {
+  const int lane = threadIdx.x & 63, li = lane & 31, h = lane >> 5;
+  const int first = (blockIdx.x * 4 + (threadIdx.x >> 6)) * 32, all = r.st->n * r.K;
+  if (first >= all) return;
+  f32x16 acc;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) acc[i] = 0.0f;
+  over_pairs<bf16_t>(r, q, first, all, [&](u32x4 x, u32x4 w, int) {
+    acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, w),
+                                                  __builtin_bit_cast(bf16x8, x), acc, 0, 0, 0);
+  });
+  // lane (li, h), register i holds row 8 (i / 4) + 4 h + i % 4 of column li
+  float v = 0.0f;
+#pragma unroll
+  for (int i = 0; i < 16; ++i)
+    if (4 * (li >> 3) + (li & 3) == i) v = acc[i];
+  if (((li >> 2) & 1) == h && first + li < all) zt[first + li] = v * zscale;
+}
+
+extern "C" __global__ __launch_bounds__(256) void hf_vocab_tlogit_f32(VRows r, VDots q,
+                                                                      float zscale, float* zt) {
+  const int lane = threadIdx.x & 63;
+  const int first = (blockIdx.x * 4 + (threadIdx.x >> 6)) * 32, all = r.st->n * r.K;
+  if (first >= all) return;
+  float s = 0.0f;
+  f32x4 x0, w0;            // of the chunk before
+  over_pairs<float>(r, q, first, all, [&](u32x4 x, u32x4 w, int g) {
+    const f32x4 xf = __builtin_bit_cast(f32x4, x), wf = __builtin_bit_cast(f32x4, w);
+    // a lane of half 0 of the MFMAs has columns 8 q .. 8 q + 3 of step q, one of
+    // half 1 the next four; MFMA i takes the i-th of both
+    if (g & 1) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s = __builtin_fmaf(wf[i], xf[i], __builtin_fmaf(w0[i], x0[i], s));
+    }
+    x0 = xf;
+    w0 = wf;
+  });
+  if (lane < 32 && first + lane < all) zt[first + lane] = s * zscale;
 }
 
 // ------------------------------------------------------------- rows' losses
@@ -817,10 +874,14 @@ bool vocab_row_loss(const Launch& L, int type, const VRows& r, const float2* sta
   if (r.T < 1) return false;
   const VDots q = {X, xp, W, ldx, ldw, Dp};
   if (!z && r.t) {
+    const long long pairs = (long long)r.T * r.K;
+    const float zscale = 1.0f / r.tau;        // as the logits'
     if (type == VT_F32)
-      HF_LAUNCH("hf_vocab_tlogit", hf_vocab_tlogit_f32, r.T, 256, r, q, t.zt);
+      HF_LAUNCH("hf_vocab_tlogit", hf_vocab_tlogit_f32, (pairs + 127) / 128, 256, r, q, zscale,
+                t.zt);
     else
-      HF_LAUNCH("hf_vocab_tlogit", hf_vocab_tlogit_bf16, r.T, 256, r, q, t.zt);
+      HF_LAUNCH("hf_vocab_tlogit", hf_vocab_tlogit_bf16, (pairs + 127) / 128, 256, r, q, zscale,
+                t.zt);
   }
   const bool sum = loss && r.T <= SUM_ROWS;
   HF_LAUNCH("hf_vocab_row_loss", hf_vocab_row_loss, sum ? 1 : (r.T + 3) / 4, 256, r, stat, ldstat,

@@ -83,3 +83,33 @@ def test_labels_in_pieces(name):
             word = v
             _, rl, dX, _ = net.hf_vocab_loss_grad(X, W, y)
             check(V, rows, rl, dX)
+
+
+@pytest.mark.parametrize("name", ["fp32", "bf16"])
+@pytest.mark.parametrize("rows,V,D,K", [
+    (1, 700, 512, 1), (5, 20000, 512, 16), (40, 3000, 1024, 5), (128, 20000, 512, 128),
+    (129, 700, 320, 33), (300, 9000, 1000, 64), (1500, 5000, 512, 7), (3000, 20000, 1024, 32),
+    (4096, 4100, 770, 65), (8200, 131100, 64, 3)])
+def test_lists(name, rows, V, D, K):
+    """The word in each place of the list in turn, some lists ending early; tau
+    squared of the label's bound, and of q's."""
+    import torch
+    for sign in (1, -1):
+        X, W, word = learnt(name, rows, V, D, sign)
+        at = torch.arange(rows, device="cuda") % K
+        k = torch.arange(K, device="cuda")[None]
+        ids = (word + 1 + k).repeat(rows, 1) % V
+        ids[torch.arange(rows), at] = word
+        ids = torch.where(k > torch.maximum(at, torch.randint(0, K, (rows,), device="cuda",
+                                                              generator=gen(K)))[:, None],
+                          H.HF_IGNORE, ids).int()
+        t = torch.where(ids == word, 40.0, 0.0)
+        net = H.HFVocab(V, W.shape[1], rows, name)
+        for tau in (1.0, 0.5):
+            bound = tau ** 2 * ((136 + V // 32 // 64 + 24) * E32 + 1e-12)
+            zero = torch.zeros(rows, dtype=torch.float64, device="cuda")
+            within(net.hf_vocab_distill(X, W, ids, t, tau)[1], zero, zero + bound, "losses alone")
+            _, rl, dX, _ = net.hf_vocab_distill_grad(X, W, ids, t, tau)
+            within(rl, zero, zero + bound, "losses")
+            within(dX[:, -1].float() * (rows / 40 / tau), zero, zero + 1.01 * bound / tau ** 2,
+                   "delta")

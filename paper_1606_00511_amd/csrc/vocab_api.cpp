@@ -406,8 +406,8 @@ void head(hf_vocab* c, VRows r, const void* X, int64_t ldx, const void* W, int64
   const bool self = dup > 0;             // few rows: with delta
   bool summed = false;
   if (!self)
-    summed = vocab_row_loss(L, type, r, stat, tiles, tiles, dots ? nullptr : z, ldd, tg, lse, xd,
-                            ldx, xp, Dp, W, ldw, loss);
+    summed = vocab_row_loss(L, type, r, sums_parts(type, tile), stat, tiles, tiles,
+                            dots ? nullptr : z, ldd, tg, lse, xd, ldx, xp, Dp, W, ldw, loss);
   if (g && T > 0)
     vocab_delta(L, type, r, z, ldd, stat, tiles, sg, lse, tg, 0, std::min(vc, V),
                 dup ? dup : (int)up(T, VPAD), self, d, ldd, dup, self || summed ? nullptr : loss);

@@ -296,6 +296,30 @@ __device__ __forceinline__ void vgemm_body(const VGemm& s, const VEpi& e) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[a][b][r] = 0.0f;
 
+  // fp32 logits: the sum of the K blocks before these SUM_COLS columns (see there)
+  constexpr bool PARTS = (EPI == E_LOGITS || EPI == E_PROBS) && sizeof(E) == 4 && WM * WN < 8;
+  static_assert(SUM_COLS % BK == 0, "K blocks of a sum");
+  f32x16 before[PARTS ? WM : 1][PARTS ? WN : 1];
+  if constexpr (PARTS) {
+#pragma unroll
+    for (int a = 0; a < WM; ++a)
+#pragma unroll
+      for (int b = 0; b < WN; ++b) before[a][b] = acc[a][b];
+  }
+  auto add_up = [&]() {
+    if constexpr (PARTS) {
+#pragma unroll
+      for (int a = 0; a < WM; ++a)
+#pragma unroll
+        for (int b = 0; b < WN; ++b)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            before[a][b][r] += acc[a][b][r];
+            acc[a][b][r] = 0.0f;
+          }
+    }
+  };
+
   // Element offsets of the lane's direct loads from the tile's origin.  Rows
   // of a K-contiguous operand past its last one read that one; chunks of a
   // [k][m] operand past its padded width read the last chunk (both feed
@@ -431,6 +455,15 @@ __device__ __forceinline__ void vgemm_body(const VGemm& s, const VEpi& e) {
           if (i / PER * AT + x < LPB) issue1(vb, st, i / PER * AT + x);
       }
     });
+    if ((it + 1) % (SUM_COLS / BK) == 0) add_up();
+  }
+  if constexpr (PARTS) {
+#pragma unroll
+    for (int a = 0; a < WM; ++a)
+#pragma unroll
+      for (int b = 0; b < WN; ++b)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[a][b][r] = before[a][b][r] + acc[a][b][r];
   }
 
   // Lane (li, h), register r of block (a, b) holds n = 32 b + li and

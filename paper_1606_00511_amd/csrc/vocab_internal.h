@@ -27,6 +27,12 @@ inline int tile_stat(int t) { return t == TILE_BIG ? 128 : t == TILE_SMALL ? 64 
 // to 2^-29 of it (20 less in z) have fp16's 11 bits, and those below an absolute
 // 2^-40 of it (as they are, 2^-14 and 2^-25: a word 17 below lost its gradient).
 constexpr float EXP_SCALE = 32768.0f;
+// fp32 logits of tiles but the largest are summed so many columns at a time, and
+// then these sums: 128 + D / 128 additions reach one, not D (2 rows, 1,974 x 1,971:
+// dW off by 1.3e-6 in one chain, 4e-7; 130 to 1,024 rows, 50,000 x 768: a loss
+// takes 2 to 3% more).  Tiles of 256 x 256 have no registers left for it.
+constexpr int SUM_COLS = 128;
+inline bool sums_parts(int type, int tile) { return type == VT_F32 && tile != TILE_BIG; }
 constexpr int VMAX_SPLITS = 64;
 constexpr long long L2_BYTES = 32ll << 20;   // the level-2 caches of the 8 XCDs
 constexpr long long L3_BYTES = 256ll << 20;  // the last-level cache
@@ -141,8 +147,9 @@ struct VTarget {
 // log-sum-exp from the statistics, the rows' losses and the targets' delta;
 // z: kept logits or null (then a label's is in t.zt, and those of lists are
 // formed of X or xp and W).  True: the loss is summed too.
-bool vocab_row_loss(const Launch& L, int type, const VRows& r, const float2* stat, int ldstat,
-                    int tiles, const float* z, long long ldz, const VTarget& t, float* lse,
+// parts: the logits are summed SUM_COLS at a time.
+bool vocab_row_loss(const Launch& L, int type, const VRows& r, bool parts, const float2* stat,
+                    int ldstat, int tiles, const float* z, long long ldz, const VTarget& t, float* lse,
                     const void* X, long long ldx, const void* xp, int Dp, const void* W,
                     long long ldw, float* loss);
 // loss = sum of the counted rows' losses / denom

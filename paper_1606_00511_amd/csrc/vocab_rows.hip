@@ -345,7 +345,7 @@ struct Pairs {
   static constexpr int XL = F32 ? CH : CH / 2;                  // chunks of X a lane needs
 };
 
-// f(chunk g of X, chunk g of W) of the wave's pairs from the first column on;
+// f(chunk of X, chunk of W, its number) of the wave's pairs from the first column on;
 // lane's pair: lane % P, its chunks: all (fp32, both halves of the wave alike), or
 // every second (bf16)
 template <class E, class F>
@@ -387,7 +387,8 @@ __device__ __forceinline__ void over_pairs(const VRows& r, const VDots& q, int f
     if (c0 + S::N < r.D) fetch(c0 + S::N);
 #pragma unroll
     for (int g = 0; g < S::XL; ++g)
-      f(now[g], *(const u32x4*)(mine + li * S::STRIDE + (S::F32 ? g : 2 * g + h) * 16), g);
+      f(now[g], *(const u32x4*)(mine + li * S::STRIDE + (S::F32 ? g : 2 * g + h) * 16),
+        c0 / S::EPC + g);
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
   }
@@ -414,12 +415,12 @@ extern "C" __global__ __launch_bounds__(256) void hf_vocab_tlogit_bf16(VRows r, 
   if (((li >> 2) & 1) == h && first + li < all) zt[first + li] = v * zscale;
 }
 
-extern "C" __global__ __launch_bounds__(256) void hf_vocab_tlogit_f32(VRows r, VDots q,
+extern "C" __global__ __launch_bounds__(256) void hf_vocab_tlogit_f32(VRows r, VDots q, int parts,
                                                                       float zscale, float* zt) {
   const int lane = threadIdx.x & 63;
   const int first = (blockIdx.x * 4 + (threadIdx.x >> 6)) * 32, all = r.st->n * r.K;
   if (first >= all) return;
-  float s = 0.0f;
+  float s = 0.0f, before = 0.0f;
   f32x4 x0, w0;            // of the chunk before
   over_pairs<float>(r, q, first, all, [&](u32x4 x, u32x4 w, int g) {
     const f32x4 xf = __builtin_bit_cast(f32x4, x), wf = __builtin_bit_cast(f32x4, w);
@@ -429,9 +430,14 @@ extern "C" __global__ __launch_bounds__(256) void hf_vocab_tlogit_f32(VRows r, V
 #pragma unroll
       for (int i = 0; i < 4; ++i) s = __builtin_fmaf(wf[i], xf[i], __builtin_fmaf(w0[i], x0[i], s));
     }
+    if (parts && (g + 1) % (SUM_COLS / 4) == 0) {
+      before += s;
+      s = 0.0f;
+    }
     x0 = xf;
     w0 = wf;
   });
+  if (parts) s = before + s;
   if (lane < 32 && first + lane < all) zt[first + lane] = s * zscale;
 }
 
@@ -867,8 +873,8 @@ void vocab_pack_matrix(const Launch& L, int type, const void* W, long long ldw, 
               (bf16_t*)wp, Dp);
 }
 
-bool vocab_row_loss(const Launch& L, int type, const VRows& r, const float2* stat, int ldstat,
-                    int tiles, const float* z, long long ldz, const VTarget& t, float* lse,
+bool vocab_row_loss(const Launch& L, int type, const VRows& r, bool parts, const float2* stat,
+                    int ldstat, int tiles, const float* z, long long ldz, const VTarget& t, float* lse,
                     const void* X, long long ldx, const void* xp, int Dp, const void* W,
                     long long ldw, float* loss) {
   if (r.T < 1) return false;
@@ -877,8 +883,8 @@ bool vocab_row_loss(const Launch& L, int type, const VRows& r, const float2* sta
     const long long pairs = (long long)r.T * r.K;
     const float zscale = 1.0f / r.tau;        // as the logits'
     if (type == VT_F32)
-      HF_LAUNCH("hf_vocab_tlogit", hf_vocab_tlogit_f32, (pairs + 127) / 128, 256, r, q, zscale,
-                t.zt);
+      HF_LAUNCH("hf_vocab_tlogit", hf_vocab_tlogit_f32, (pairs + 127) / 128, 256, r, q,
+                (int)parts, zscale, t.zt);
     else
       HF_LAUNCH("hf_vocab_tlogit", hf_vocab_tlogit_bf16, (pairs + 127) / 128, 256, r, q, zscale,
                 t.zt);

@@ -89,7 +89,8 @@ def test_labels_in_pieces(name):
 @pytest.mark.parametrize("rows,V,D,K", [
     (1, 700, 512, 1), (5, 20000, 512, 16), (40, 3000, 1024, 5), (128, 20000, 512, 128),
     (129, 700, 320, 33), (300, 9000, 1000, 64), (1500, 5000, 512, 7), (3000, 20000, 1024, 32),
-    (4096, 4100, 770, 65), (8200, 131100, 64, 3)])
+    (4096, 4100, 770, 65), (8200, 131100, 64, 3), (300, 60000, 256, 1), (1000, 50000, 384, 2),
+    (1500, 50000, 320, 2)])
 def test_lists(name, rows, V, D, K):
     """The word in each place of the list in turn, some lists ending early; tau
     squared of the label's bound, and of q's."""

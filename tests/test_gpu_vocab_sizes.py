@@ -258,3 +258,28 @@ def test_words_without_probability(name, rows):
     assert rl[5].item() == math.inf and torch.isfinite(rl[:5]).all()
     W[:, 0] = -math.inf
     assert net.hf_vocab_loss(X, W, y)[1].isnan().all()
+
+
+@pytest.mark.parametrize("rows,V", [(1, 700), (16, 1900), (100, 3000), (300, 900), (700, 3000)])
+def test_sums_of_wide_rows(rows, V):
+    """fp32 logits of few rows are summed 128 columns at a time, and then these
+    sums: a logit is off by at most 128 + D / 128 + 2 times e of its magnitudes.
+    In one chain of D additions the target's products, 2^-6 (1 + 2^-14), would
+    lose their last bits at every addition past 32, 0.002 in all; the other
+    words' are 2^-6, whose sums are exact."""
+    torch = T()
+    D = 4096
+    X = torch.ones(rows, D, device="cuda")
+    W = torch.full((V, D), 2.0 ** -6, device="cuda")
+    W[V // 2] = 2.0 ** -6 * (1 + 2.0 ** -14)
+    y = torch.full((rows,), V // 2, dtype=torch.int32, device="cuda")
+    net = H.HFVocab(V, D, rows, "fp32")
+    want = torch.full((rows,), math.log1p((V - 1) * math.exp(-(2.0 ** -8))), dtype=torch.float64,
+                      device="cuda")
+    most = (128 + D / 128 + 2) * E32 * 64.01
+    bound = torch.full_like(want, most + (512 + V // 128) * E32 + 256 * E32 * 10)
+    assert bound[0] < 1e-3
+    within(net.hf_vocab_loss_grad(X, W, y)[1], want, bound, "row losses")
+    within(net.hf_vocab_loss(X, W, y)[1], want, bound, "row losses, alone")
+    t = torch.zeros(rows, 1, device="cuda")
+    within(net.hf_vocab_distill(X, W, y[:, None], t)[1], want, bound, "list's losses")

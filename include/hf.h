@@ -535,6 +535,7 @@ int hf_vocab_loss_grad(hf_vocab* ctx, const void* X, int64_t ldx,
  *   t    rows x top fp32 teacher logits, ldt apart; -inf counts as masked
  *   top  1 .. HF_VOCAB_MAX_TOP;  tau in [1e-4, 1e4]
  * An id that a row lists twice has the sum of its probabilities as q_iv.
+ * Few rows' logits are stored in the workspace where that is quicker.
  * Other arguments as for hf_vocab_loss.
  */
 int hf_vocab_distill(hf_vocab* ctx, const void* X, int64_t ldx, const void* W,

@@ -1,0 +1,367 @@
+"""The gated feed-forward block of a token model, as cases that can be timed:
+the block and its gradients, with what is kept between the two in full or in
+8 bits; activation checkpoints in 8 bits on their own; and the product of
+8-bit integers with a scale for each token and channel, alone and as the block
+that serves with it.
+
+With ``rows`` tokens, X of rows x width, Wg and Wu of hidden x width and Wd of
+width x hidden, the block is Y = (act(X Wg^T) * (X Wu^T)) Wd^T.
+
+A case: ``op`` ("forward", "grad", "pack", "product8" or "forward8"), ``type``
+("fp32" or "bf16", of rows, matrices and gradients), ``rows``, ``width``,
+``hidden``; ``act``, the activation; ``keep`` ("none", "full" or "int8"), what
+"forward" keeps of the two products for the gradient and "grad" is given (with
+"int8" also X).  "pack" packs and unpacks rows x hidden numbers; "product8" is
+of rows x width by hidden x width codes.
+
+Codes of a checkpoint: 32 neighbours of a row share a scale, a power of two.
+Codes of a product: a row has one scale, its largest number over 127.
+"""
+
+import math
+
+import torch
+
+own = False
+
+TYPES = {"fp32": torch.float32, "bf16": torch.bfloat16}
+ACTS = ("silu", "gelu", "gelu_tanh", "sigmoid", "tanh", "relu")
+
+
+def _case(op, type, rows, width, hidden, act="", keep="", name=None):
+    c = dict(op=op, type=type, rows=rows, width=width, hidden=hidden, act=act, keep=keep)
+    if name:
+        c["name"] = name
+    return c
+
+
+def listed():
+    return [
+        # one new token of a small model
+        _case("forward", "bf16", 1, 1024, 4096, "silu", "none", name="forward_one"),
+        # a serving batch, a new token of each of 24 users
+        _case("forward", "bf16", 24, 4096, 16384, "silu", "none", name="forward_few"),
+        # a long prompt, or the evaluation of a minibatch
+        _case("forward", "bf16", 8192, 4096, 16384, "silu", "none", name="forward_large"),
+        # a ragged training minibatch of odd widths that keeps 8 bits
+        _case("forward", "bf16", 3001, 1021, 2731, "gelu_tanh", "int8",
+              name="forward_keep8_ragged"),
+        # training in single precision on the minibatch of a small model
+        _case("grad", "fp32", 4096, 1024, 2731, "silu", "full", name="grad_fp32"),
+        # fine-tuning on a short prompt's answers, of what 8 bits kept
+        _case("grad", "bf16", 300, 768, 2050, "gelu", "int8", name="grad8_short"),
+        # the training minibatch of a large model, of what 8 bits kept
+        _case("grad", "bf16", 8192, 4096, 16384, "silu", "int8", name="grad8_large"),
+        # a layer's activations to 8 bits and back, a large minibatch
+        _case("pack", "bf16", 16384, 4096, 8192, name="pack_large"),
+        # and a small one in single precision, with ragged rows
+        _case("pack", "fp32", 777, 2048, 1973, name="pack_fp32"),
+        # the 8-bit logits of one token over a vocabulary
+        _case("product8", "fp32", 1, 1024, 32000, name="product8_one"),
+        # an 8-bit projection of a long prompt
+        _case("product8", "bf16", 8192, 4096, 16384, name="product8_large"),
+        # the 8-bit block for a new token of each of 32 users
+        _case("forward8", "bf16", 32, 4096, 16384, "silu", name="forward8_few"),
+    ]
+
+
+def _log_int(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def draw(rng):
+    op = rng.choice(("forward", "forward", "grad", "grad", "grad", "pack", "product8",
+                     "forward8"))
+    type = rng.choice(("bf16", "bf16", "fp32"))
+    act = rng.choice(("silu", "silu", "gelu_tanh") + ACTS)
+    width = _log_int(rng, 64, 4096)
+    hidden = _log_int(rng, width, min(4 * width, 16384))
+    if rng.random() < 0.6:      # most models' widths are multiples of 64
+        width, hidden = max(64, width // 64 * 64), max(64, hidden // 64 * 64)
+    rows = _log_int(rng, 1, 16384)
+    # no more than the largest listed block
+    rows = max(1, min(rows, 8192 * 4096 * 16384 // (width * hidden)))
+    if op == "pack":
+        return _case(op, type, rows, width, hidden)
+    if op == "product8":
+        return _case(op, type, min(rows, 8192), width, hidden)
+    if op == "forward8":
+        # (as one type: H is rounded to 8 bits on the way, and a number next to
+        # a border between two codes falls on either side with a sum's last bit,
+        # which single precision would show)
+        return _case(op, "bf16", rows, width, hidden, act)
+    if op == "forward":
+        keep = rng.choice(("none", "none", "full", "int8" if type == "bf16" else "full"))
+        return _case(op, type, rows, width, hidden, act, keep)
+    return _case(op, type, rows, width, hidden, act, rng.choice(("full", "int8")))
+
+
+# ------------------------------------------------------------------- inputs
+
+def _blocks(x):
+    """(codes int8, scale bytes) of a checkpoint of x."""
+    R, C = x.shape
+    n = (C + 31) // 32
+    v = torch.zeros(R, n * 32, device=x.device)
+    v[:, :C] = x
+    v = v.view(R, n, 32)
+    big = v.abs().amax(2)
+    # the exponent of the largest, one more where its code would round to 128
+    e = ((big.view(torch.int32) + 0x10000) >> 23) - 6
+    e = torch.where(big > 0, e, 0).clamp_(min=0)
+    q = torch.round(torch.ldexp(v.double(), 127 - e[:, :, None]))
+    return q.to(torch.int8).view(R, -1)[:, :C].contiguous(), e.to(torch.uint8)
+
+
+def _values(codes, scale):
+    """What the codes of a checkpoint stand for, in fp32."""
+    e = scale.int().repeat_interleave(32, 1)[:, :codes.shape[1]] - 127
+    return torch.ldexp(codes.float(), e)
+
+
+def _rows8(x):
+    """(codes int8, fp32 scale of each row): q = round(x / s), s = max |x| / 127,
+    the quotient in 64 bits, since a border between two codes may be near."""
+    s = x.float().abs().amax(1) / 127
+    q = torch.round(x.double() / torch.where(s > 0, s, 1.0).double()[:, None])
+    return q.to(torch.int8), s
+
+
+def _inputs(case, seed):
+    g = torch.Generator("cuda").manual_seed(seed)
+    T, D, F, op = case["rows"], case["width"], case["hidden"], case["op"]
+    dt = TYPES[case["type"]]
+    randn = lambda *s: torch.randn(*s, generator=g, device="cuda")   # noqa: E731
+    # activations: some columns are larger than others by far
+    acts = lambda r, c: (randn(r, c) * torch.exp(randn(c) * 0.5)).to(dt)   # noqa: E731
+    s = {}
+    if op == "pack":
+        s["X"] = acts(T, F)
+        return s
+    s["X"] = acts(T, D)
+    Wg = randn(F, D) * D ** -0.5
+    if op == "product8":
+        s["B"] = _rows8(Wg.to(dt))
+        return s
+    Wg, Wu = Wg.to(dt), (randn(F, D) * D ** -0.5).to(dt)
+    Wd = (randn(D, F) * F ** -0.5).to(dt)
+    if op == "forward8":
+        s["Wg"], s["Wu"], s["Wd"] = _rows8(Wg), _rows8(Wu), _rows8(Wd)
+        return s
+    s["Wg"], s["Wu"], s["Wd"] = Wg, Wu, Wd
+    if op == "grad":
+        s["dY"] = (randn(T, D) / T).to(dt)
+        # what the forward pass of these inputs has kept
+        X = s["X"].float()
+        G, U = X @ Wg.float().t(), X @ Wu.float().t()
+        if case["keep"] == "full":
+            s["kept"] = torch.cat((G.to(dt), U.to(dt)), 1)
+        else:
+            (cg, sg), (cu, su) = _blocks(G), _blocks(U)
+            s["kept"] = (torch.cat((cg, cu), 1), torch.cat((sg, su), 1))
+            s["X"] = _blocks(X)
+    return s
+
+
+def prepare(case, seed):
+    s = dict(case=case, **_inputs(case, seed))
+    if own:
+        from paper_1606_00511_amd.hf import HFGated
+        s["net"] = HFGated(case["width"], case["hidden"], case["rows"],
+                           act=case["act"] or "silu", dtype=case["type"])
+    return s
+
+
+# ------------------------------------------------------------- one pass
+
+def _own(s):
+    case, net = s["case"], s["net"]
+    op, F = case["op"], case["hidden"]
+    if op == "pack":
+        return {"X": net.hf_gated_unpack(*net.hf_gated_pack(s["X"]))}
+    if op == "product8":
+        return {"Y": net.hf_gated_product8(*net.hf_gated_rows8(s["X"]), *s["B"])}
+    if op == "forward8":
+        return {"Y": net.hf_gated_forward8(s["X"], s["Wg"], s["Wu"], s["Wd"])}
+    if op == "grad":
+        dX, dWg, dWu, dWd = net.hf_gated_grad(s["X"], s["Wg"], s["Wu"], s["Wd"], s["kept"],
+                                              s["dY"])
+        return {"dX": dX, "dWg": dWg, "dWu": dWu, "dWd": dWd}
+    keep = None if case["keep"] == "none" else case["keep"]
+    Y, kept = net.hf_gated_forward(s["X"], s["Wg"], s["Wu"], s["Wd"], keep=keep)
+    if not keep:
+        return {"Y": Y}
+    if keep == "full":
+        return {"Y": Y, "G": kept[:, :F], "U": kept[:, F:]}
+    codes, scale = kept
+    n = scale.shape[1] // 2
+    return {"Y": Y, "G": net.hf_gated_unpack(codes[:, :F], scale[:, :n]),
+            "U": net.hf_gated_unpack(codes[:, F:], scale[:, n:])}
+
+
+def _act(name, z):
+    if name == "silu":
+        return z / (1 + torch.exp(-z))
+    if name == "gelu":
+        return 0.5 * z * (1 + torch.erf(z * math.sqrt(0.5)))
+    if name == "gelu_tanh":
+        return 0.5 * z * (1 + torch.tanh(math.sqrt(2 / math.pi) * (z + 0.044715 * z ** 3)))
+    if name == "sigmoid":
+        return 1 / (1 + torch.exp(-z))
+    return torch.tanh(z) if name == "tanh" else z * (z > 0)
+
+
+def _slope(name, z):
+    """The derivative of the activation."""
+    if name in ("silu", "sigmoid"):
+        p = 1 / (1 + torch.exp(-z))
+        return p * (1 - p) if name == "sigmoid" else p * (1 + z * (1 - p))
+    if name == "gelu":
+        return (0.5 * (1 + torch.erf(z * math.sqrt(0.5)))
+                + z * torch.exp(-0.5 * z * z) / math.sqrt(2 * math.pi))
+    if name == "gelu_tanh":
+        c = math.sqrt(2 / math.pi)
+        t = torch.tanh(c * (z + 0.044715 * z ** 3))
+        return 0.5 * (1 + t) + 0.5 * z * (1 - t * t) * c * (1 + 3 * 0.044715 * z * z)
+    if name == "tanh":
+        return 1 - torch.tanh(z) ** 2
+    return (z > 0).float()
+
+
+def _product8(a, sa, b, sb):
+    """Sums of products of codes pass 24 bits: in 64."""
+    return a.double() @ b.double().t() * (sa.double()[:, None] * sb.double())
+
+
+def run(s):
+    if own:
+        return _own(s)
+    case = s["case"]
+    op, dt, act, F = case["op"], TYPES[case["type"]], case["act"], case["hidden"]
+    if op == "pack":
+        return {"X": _values(*_blocks(s["X"].float())).to(dt)}
+    if op == "product8":
+        return {"Y": _product8(*_rows8(s["X"]), *s["B"]).to(dt)}
+    if op == "forward8":
+        x = _rows8(s["X"])
+        # (64 bits: H's codes have borders)
+        H = _act(act, _product8(*x, *s["Wg"])) * _product8(*x, *s["Wu"])
+        return {"Y": _product8(*_rows8(H), *s["Wd"]).to(dt)}
+    Wg, Wu, Wd = s["Wg"].float(), s["Wu"].float(), s["Wd"].float()
+    if op == "forward":
+        X = s["X"].float()
+        G, U = X @ Wg.t(), X @ Wu.t()
+        out = {"Y": ((_act(act, G) * U) @ Wd.t()).to(dt)}
+        if case["keep"] == "full":
+            out.update(G=G.to(dt), U=U.to(dt))
+        elif case["keep"] == "int8":
+            out.update(G=_values(*_blocks(G)).to(dt), U=_values(*_blocks(U)).to(dt))
+        return out
+    if case["keep"] == "full":
+        X, G, U = s["X"].float(), s["kept"][:, :F].float(), s["kept"][:, F:].float()
+    else:
+        X, (codes, scale) = _values(*s["X"]), s["kept"]
+        n = scale.shape[1] // 2
+        G, U = _values(codes[:, :F], scale[:, :n]), _values(codes[:, F:], scale[:, n:])
+    dY = s["dY"].float()
+    A, dH = _act(act, G), dY @ Wd
+    dWd = dY.t() @ (A * U)
+    dU, dG = dH * A, dH * U * _slope(act, G)
+    return {"dX": (dG @ Wg + dU @ Wu).to(dt), "dWg": (dG.t() @ X).to(dt),
+            "dWu": (dU.t() @ X).to(dt), "dWd": dWd.to(dt)}
+
+
+# -------------------------------------------------------------------- work
+
+def work(case):
+    T, D, F, op = case["rows"], case["width"], case["hidden"], case["op"]
+    b = 4 if case["type"] == "fp32" else 2
+    code = 1 + 1 / 32
+    if op == "pack":        # to codes, and back from them
+        return {"bytes": 2 * T * F * (b + code), "flops": 4 * T * F}
+    if op == "product8":
+        return {"bytes": b * T * (D + F) + F * D + 4 * F, "flops": 2 * T * D * F}
+    if op == "forward8":
+        return {"bytes": 2 * b * T * D + 3 * D * F + 4 * (2 * F + D), "flops": 6 * T * D * F}
+    kept = 2 * T * F * {"none": 0, "full": b, "int8": code}[case["keep"]]
+    if op == "forward":
+        return {"bytes": b * (2 * T * D + 3 * D * F) + kept, "flops": 6 * T * D * F}
+    x = T * D * (code if case["keep"] == "int8" else b)
+    return {"bytes": b * (2 * T * D + 6 * D * F) + kept + x, "flops": 12 * T * D * F}
+
+
+# ------------------------------------------------------------------- exact
+
+def _f64(name, z):
+    """The activation, of 64 bits."""
+    f = torch.nn.functional
+    return {"silu": f.silu, "gelu": f.gelu, "sigmoid": torch.sigmoid, "tanh": torch.tanh,
+            "relu": torch.relu,
+            "gelu_tanh": lambda v: f.gelu(v, approximate="tanh")}[name](z)
+
+
+def _integers(x, s):
+    """The codes of rows x with scales s, as 64-bit numbers."""
+    return torch.where(s[:, None] > 0, (x / s[:, None]).round(), 0.0)
+
+
+def _of_codes(codes, scale):
+    """A checkpoint's numbers."""
+    R, C = codes.shape
+    at = torch.arange(C, device=codes.device) // 32
+    return codes.double() * torch.exp2(scale.double() - 127)[:, at]
+
+
+def exact(case, seed):
+    """The definitions in 64 bits."""
+    s = _inputs(case, seed)
+    op, F, act = case["op"], case["hidden"], case["act"]
+    if op == "pack":
+        X = s["X"].double()
+        C = X.shape[1]
+        at = torch.arange(C, device="cuda") // 32
+        big = torch.zeros(X.shape[0], int(at[-1]) + 1, dtype=torch.float64, device="cuda")
+        big.scatter_reduce_(1, at.expand_as(X), X.abs(), "amax")
+        # the smallest power of two whose multiples up to 127 reach the block's
+        # largest within half a step
+        step = torch.exp2(torch.ceil(torch.log2(big / 127.5)))
+        step = torch.where(big / step == 127.5, 2 * step, step)
+        step = torch.where(big > 0, step, 1.0)[:, at]
+        return {"X": (X / step).round() * step}
+    if op in ("product8", "forward8"):
+        X = s["X"].double()
+        sx = (s["X"].float().abs().amax(1) / 127).double()
+        qx = _integers(X, sx)
+        times = lambda m: (qx @ m[0].double().t()) * sx[:, None] * m[1].double()   # noqa: E731
+        if op == "product8":
+            return {"Y": times(s["B"])}
+        H = _f64(act, times(s["Wg"])) * times(s["Wu"])
+        sh = (H.abs().amax(1).float() / 127).double()
+        qd, sd = s["Wd"]
+        return {"Y": (_integers(H, sh) @ qd.double().t()) * sh[:, None] * sd.double()}
+    Wg, Wu, Wd = (s[k].double() for k in ("Wg", "Wu", "Wd"))
+    if op == "forward":
+        X = s["X"].double()
+        G, U = X @ Wg.t(), X @ Wu.t()
+        out = {"Y": torch.mm(_f64(act, G).mul_(U), Wd.t())}
+        if case["keep"] == "full":
+            out.update(G=G, U=U)
+        elif case["keep"] == "int8":
+            # a number next to a border between two codes falls on either side
+            # with the last bit of a sum in 32 bits
+            out.update(G=None, U=None)
+        return out
+    if case["keep"] == "full":
+        X, G, U = s["X"].double(), s["kept"][:, :F].double(), s["kept"][:, F:].double()
+    else:
+        X, n = _of_codes(*s["X"]), s["kept"][1].shape[1] // 2
+        G = _of_codes(s["kept"][0][:, :F], s["kept"][1][:, :n])
+        U = _of_codes(s["kept"][0][:, F:], s["kept"][1][:, n:])
+    dY = s["dY"].double()
+    G.requires_grad_()
+    U.requires_grad_()
+    H = _f64(act, G) * U
+    dG, dU = torch.autograd.grad(H, (G, U), dY @ Wd)
+    H = H.detach()
+    return {"dX": dG @ Wg + dU @ Wu, "dWg": torch.mm(dG.t(), X), "dWu": torch.mm(dU.t(), X),
+            "dWd": torch.mm(dY.t(), H)}

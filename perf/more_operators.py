@@ -180,9 +180,9 @@ def _own(s):
     if op == "pack":
         return {"X": net.hf_gated_unpack(*net.hf_gated_pack(s["X"]))}
     if op == "product8":
-        return {"Y": net.hf_gated_product8(*net.hf_gated_rows8(s["X"]), *s["B"])}
+        return {"Y": net.hf_gated_product(*net.hf_gated_codes(s["X"]), *s["B"])}
     if op == "forward8":
-        return {"Y": net.hf_gated_forward8(s["X"], s["Wg"], s["Wu"], s["Wd"])}
+        return {"Y": net.hf_gated_forward_codes(s["X"], s["Wg"], s["Wu"], s["Wd"])}
     if op == "grad":
         dX, dWg, dWu, dWd = net.hf_gated_grad(s["X"], s["Wg"], s["Wu"], s["Wd"], s["kept"],
                                               s["dY"])

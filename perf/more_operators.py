@@ -121,8 +121,8 @@ def _values(codes, scale):
 
 def _rows8(x):
     """(codes int8, fp32 scale of each row): q = round(x / s), s = max |x| / 127,
-    the quotient in 64 bits, since a border between two codes may be near."""
-    s = x.float().abs().amax(1) / 127
+    the quotients in 64 bits, since a border between two codes may be near."""
+    s = (x.float().abs().amax(1).double() / 127).float()
     q = torch.round(x.double() / torch.where(s > 0, s, 1.0).double()[:, None])
     return q.to(torch.int8), s
 
@@ -330,13 +330,13 @@ def exact(case, seed):
         return {"X": (X / step).round() * step}
     if op in ("product8", "forward8"):
         X = s["X"].double()
-        sx = (s["X"].float().abs().amax(1) / 127).double()
+        sx = (X.abs().amax(1) / 127).float().double()
         qx = _integers(X, sx)
         times = lambda m: (qx @ m[0].double().t()) * sx[:, None] * m[1].double()   # noqa: E731
         if op == "product8":
             return {"Y": times(s["B"])}
         H = _f64(act, times(s["Wg"])) * times(s["Wu"])
-        sh = (H.abs().amax(1).float() / 127).double()
+        sh = (H.abs().amax(1).float().double() / 127).float().double()
         qd, sd = s["Wd"]
         return {"Y": (_integers(H, sh) @ qd.double().t()) * sh[:, None] * sd.double()}
     Wg, Wu, Wd = (s[k].double() for k in ("Wg", "Wu", "Wd"))

@@ -572,6 +572,159 @@ int hf_vocab_check(hf_vocab* ctx);
 /* Message for the last failed call on ctx. */
 const char* hf_vocab_last_error(const hf_vocab* ctx);
 
+/*
+ * ------------------------------------------------------------------------
+ * The gated feed-forward block of a token model, which lies between its two
+ * ends: with D the width and F the hidden width,
+ *   g = X Wg^T,  u = X Wu^T,  h = phi(g) u,  Y = h Wd^T
+ *   X, Y  rows x D;  Wg, Wu  F x D;  Wd  D x F
+ * in training, with what the gradient needs kept in full or in 8 bits, and in
+ * serving, down to one token, with the matrices as they are or in 8-bit codes.
+ *
+ * A context (hf_gated) holds D, F, the activation phi and the type of the
+ * rows, the matrices and their gradients: fp32 or bf16 (sums and the activation
+ * are fp32; h, and in the gradient dg and du, are rounded to the type for the
+ * product that reads them, with bf16 calls of up to 128 rows to two terms of
+ * it; each output is rounded to its type once).  Matrices are row-major; rows
+ * may lie `ld` elements apart and start at any element (rows of 16-byte
+ * multiples and widths that are multiples of 64, of codes 128, are read in
+ * place, others are copied to the workspace first).  Columns and rows around an
+ * output are left as they were.  Outputs may not overlap inputs.
+ * Memory, streams, the order of calls and errors as for hf_vocab; calls make no
+ * allocation and can be captured into a graph.  hf_gated_pack, _unpack and
+ * _codes use no workspace.  Repeated calls give the same bits.  Rows do not mix:
+ * a row with a number that is not finite spoils its own results and the
+ * matrices' gradients.
+ */
+typedef struct hf_gated hf_gated;
+
+/* Activations, besides HF_SIGMOID, HF_TANH and HF_RELU: z sigmoid(z);
+ * z Phi(z); and z Phi(z) with Phi(z) = (1 + tanh(sqrt(2 / pi) (z + 0.044715
+ * z^3))) / 2. */
+enum { HF_SILU = 3, HF_GELU = 4, HF_GELU_TANH = 5 };
+/* What hf_gated_forward keeps of g and u. */
+enum { HF_KEEP_NONE = 0, HF_KEEP_FULL = 1, HF_KEEP_CODES = 2 };
+/* Limits: width, hidden width and columns of an array; rows per call; rows of
+ * a matrix that is turned into codes, and channels of a product. */
+#define HF_GATED_MAX_WIDTH 65536
+#define HF_GATED_MAX_ROWS 262144
+#define HF_GATED_MAX_OUT (1 << 22)
+/* Neighbours in a row that share a scale in a checkpoint. */
+#define HF_CODE_BLOCK 32
+
+/* Build a context for calls of up to max_rows rows; HF_EINVAL outside the
+ * limits.  No device call is made. */
+int hf_gated_create(int32_t width, int32_t hidden, int32_t act, int32_t type,
+                    int64_t max_rows, void* hip_stream, hf_gated** out);
+/* Free a context.  NULL is ok. */
+int hf_gated_destroy(hf_gated* ctx);
+/* Stream (a hipStream_t) of later calls, after an error as well; NULL = null
+ * stream. */
+int hf_gated_set_stream(hf_gated* ctx, void* hip_stream);
+/* Bytes of workspace for calls of up to `rows` rows (<= 0: max_rows); 0 for a
+ * NULL context or rows > max_rows.  Grows with rows. */
+size_t hf_gated_workspace_bytes(const hf_gated* ctx, int64_t rows);
+/* Hand over a device workspace, 256-byte aligned; calls with more rows than
+ * its bytes serve return HF_EWORKSPACE. */
+int hf_gated_set_workspace(hf_gated* ctx, void* dev_ptr, size_t bytes);
+
+/*
+ * hf_gated_forward: Y of the block, and what its gradient needs.
+ *   X       rows x D, ldx >= D elements apart;  Y  rows x D, ldy apart
+ *   Wg, Wu  F x D, ldg and ldu apart;  Wd  D x F, ldd apart
+ *   keep    HF_KEEP_NONE; HF_KEEP_FULL: g and u in the type; HF_KEEP_CODES: in
+ *           8 bits, as hf_gated_pack writes them (of the fp32 sums)
+ *   kept    rows x 2 F, ldk apart: a row of g and then of u, in the type or as
+ *           codes; ignored with HF_KEEP_NONE
+ *   scale   HF_KEEP_CODES: rows x 2 ceil(F / 32) scale bytes, lds apart: g's
+ *           and then u's
+ */
+int hf_gated_forward(hf_gated* ctx, const void* X, int64_t ldx, const void* Wg,
+                     int64_t ldg, const void* Wu, int64_t ldu, const void* Wd,
+                     int64_t ldd, int64_t rows, void* Y, int64_t ldy,
+                     int32_t keep, void* kept, int64_t ldk, uint8_t* scale,
+                     int64_t lds);
+
+/*
+ * hf_gated_grad: the block's gradients from that of Y and what was kept,
+ *   dh = dY Wd,  du = dh phi(g),  dg = dh u phi'(g)
+ *   dX = dg Wg + du Wu,  dWg = dg^T X,  dWu = du^T X,  dWd = dY^T h
+ * relu's slope at 0 is 0.
+ *   X, xscale   X as forward had it (xscale NULL), or its codes and scale bytes
+ *               from hf_gated_pack (ldx and ldxs apart): read for dWg and dWu
+ *   keep, kept, scale   what hf_gated_forward has kept
+ *   dX, dWg, dWu, dWd   shaped like X and the matrices, each or NULL (not all):
+ *               not computed
+ *   accumulate  1: dWg, dWu and dWd += instead of = (over minibatches); dX is
+ *               always written whole
+ */
+int hf_gated_grad(hf_gated* ctx, const void* X, int64_t ldx,
+                  const uint8_t* xscale, int64_t ldxs, const void* Wg,
+                  int64_t ldg, const void* Wu, int64_t ldu, const void* Wd,
+                  int64_t ldd, int32_t keep, const void* kept, int64_t ldk,
+                  const uint8_t* scale, int64_t lds, const void* dY,
+                  int64_t lddy, int64_t rows, void* dX, int64_t lddx, void* dWg,
+                  int64_t lddg, void* dWu, int64_t lddu, void* dWd,
+                  int64_t lddd, int32_t accumulate);
+
+/*
+ * hf_gated_pack: a checkpoint of rows x cols numbers of the type in 8 bits.
+ * HF_CODE_BLOCK neighbours of a row (the last block of a row may be shorter)
+ * share a scale byte b, and a number's code q in [-127, 127] stands for
+ * q 2^(b - 127):
+ *   b = 127 + e - 6, 2^e the largest power of two up to the block's largest
+ *   magnitude, one more where that one's code would round to 128; at least 0
+ *   q = the number over 2^(b - 127), rounded to nearest, ties to even
+ * Each number is within half a step 2^(b - 127), at most 2^-6.99 of the
+ * block's largest.  A block with a NaN or an infinity has b = 255 and unpacks to
+ * NaN.  hf_gated_unpack writes the numbers in the type: exactly, as 7 bits and a
+ * power of two (below bf16's smallest normal number, rounded).
+ *   codes  rows x cols, ldc apart;  scale  rows x ceil(cols / 32), lds apart
+ */
+int hf_gated_pack(hf_gated* ctx, const void* X, int64_t ldx, int64_t rows,
+                  int64_t cols, int8_t* codes, int64_t ldc, uint8_t* scale,
+                  int64_t lds);
+int hf_gated_unpack(hf_gated* ctx, const int8_t* codes, int64_t ldc,
+                    const uint8_t* scale, int64_t lds, int64_t rows,
+                    int64_t cols, void* X, int64_t ldx);
+
+/*
+ * hf_gated_codes: rows of the type as 8-bit codes with a scale for each row (a
+ * token's, or a matrix's channel's): s = max |x| / 127 in fp32, q = x / s
+ * rounded to nearest, ties to even.  A row of zeros has s = 0; one with a NaN or
+ * an infinity has s = NaN and codes 0.
+ *   X  rows x cols;  codes  rows x cols, ldc apart;  scale  rows fp32
+ */
+int hf_gated_codes(hf_gated* ctx, const void* X, int64_t ldx, int64_t rows,
+                   int64_t cols, int8_t* codes, int64_t ldc, float* scale);
+
+/*
+ * hf_gated_product: the product of two matrices of codes, y_tn = sa_t sb_n
+ * sum_k A_tk B_nk, the sum exact in 32 bits, then rounded to fp32 and scaled.
+ *   A  rows x k codes, lda apart, with sa: rows fp32 scales
+ *   B  n x k codes, ldb apart, with sb: n fp32 scales
+ *   n  1 .. HF_GATED_MAX_OUT;  k  1 .. the larger of the context's widths
+ *   Y  rows x n of the type, ldy apart
+ */
+int hf_gated_product(hf_gated* ctx, const int8_t* A, int64_t lda,
+                     const float* sa, const int8_t* B, int64_t ldb,
+                     const float* sb, int64_t rows, int64_t n, int64_t k,
+                     void* Y, int64_t ldy);
+
+/*
+ * hf_gated_forward_codes: hf_gated_forward with the matrices as codes of
+ * hf_gated_codes (F, F and D scales).  X's rows, and h's (of fp32), are turned
+ * into codes on the way; every product is hf_gated_product's.
+ */
+int hf_gated_forward_codes(hf_gated* ctx, const void* X, int64_t ldx,
+                           const int8_t* Wg, int64_t ldg, const float* sg,
+                           const int8_t* Wu, int64_t ldu, const float* su,
+                           const int8_t* Wd, int64_t ldd, const float* sd,
+                           int64_t rows, void* Y, int64_t ldy);
+
+/* Message for the last failed call on ctx. */
+const char* hf_gated_last_error(const hf_gated* ctx);
+
 #ifdef __cplusplus
 }
 #endif

@@ -14,7 +14,8 @@ CSRC = os.path.join(HERE, "csrc")
 HEADER = os.path.join(os.path.dirname(HERE), "include", "hf.h")
 SOURCES = ["hf_api.cpp", "gemm.hip", "gemm_bf16.hip", "rowops.hip", "cgvec.hip",
            "noalloc.hip", "narrow.hip", "vocab_api.cpp", "vocab_gemm.hip",
-           "vocab_rows.hip", "vocab_embed.hip"]
+           "vocab_rows.hip", "vocab_embed.hip", "gated_api.cpp", "gated_gemm.hip",
+           "gated_rows.hip"]
 
 
 def source_files():

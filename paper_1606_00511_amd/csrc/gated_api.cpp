@@ -1,0 +1,624 @@
+// Host side of the gated feed-forward calls declared in include/hf.h: context,
+// argument validation, workspace carve-up and the order of the kernels.
+//
+// Inside, the width and the hidden width are whole multiples of 64 (codes: 128):
+// operands that are not, or whose rows the GEMMs' 16-byte loads cannot read, are
+// copied to the workspace with zeros around them first.
+#include "hf.h"
+#include "call_context.h"
+#include "gated_internal.h"
+#include "gemm_shape.h"
+
+#include <algorithm>
+#include <climits>
+#include <new>
+
+using namespace hfk;
+
+namespace {
+
+// bf16 calls of at most so many rows hold h, dg and du as two bf16 terms, the
+// second what the first's rounding left: with few rows nothing averages a
+// rounding away, and the matrix cores wait for the matrices anyway.
+constexpr int TWO_TERM_ROWS = 128;
+constexpr size_t WPACK_BYTES = (size_t)64 << 20;   // packed channels of a product of codes
+
+struct Layout {
+  size_t part, wg, wu, wd;                    // every call
+  size_t xp, yp, xt, yt, h, dgu;              // forward, gradient
+  size_t xq, sx, hf, hmax, hq, sh;            // codes
+  size_t aq, bq;                              // products of codes
+  size_t need;
+};
+
+}  // namespace
+
+struct hf_gated : hfk::CallContext {
+  int D = 0, F = 0, Dp = 0, Fp = 0, Dc = 0, Fc = 0, act = 0, type = 0, es = 0;
+  int64_t Rmax = 0, Rws = 0;
+  char* ws = nullptr;
+  Layout lay = {};
+
+  template <class T>
+  T* at(size_t off) const { return reinterpret_cast<T*>(ws + off); }
+};
+
+namespace {
+
+// rows apart of the second terms, 0 where there are none
+inline int two_term(const hf_gated* c, int64_t T) {
+  return c->type == VT_BF16 && T > 0 && T <= TWO_TERM_ROWS ? (int)up(T, 64) : 0;
+}
+
+void plan(const hf_gated* c, int64_t R, Layout* l) {
+  size_t off = 0, need = 0;
+  auto take = [&](size_t bytes) {
+    const size_t o = off;
+    off += (bytes + 255) & ~size_t(255);
+    need = std::max(need, off);
+    return o;
+  };
+  const size_t Dp = c->Dp, Fp = c->Fp, Dc = c->Dc, Fc = c->Fc, es = c->es, r = (size_t)R;
+  // rows of h, dg, du and of packed rows: whole K blocks, and of few rows both terms
+  const size_t rk = (size_t)std::max(up(R, 64), 2 * up(std::min<int64_t>(R, TWO_TERM_ROWS), 64));
+  l->part = take(SPLIT_FLOATS * 4);
+  // (as codes: a byte an element, up to 128)
+  const size_t wbytes = std::max(Fp * Dp * es, std::max(Fp * Dc, Dp * Fc));
+  l->wg = take(wbytes);
+  l->wu = take(wbytes);
+  l->wd = take(wbytes);
+  const size_t start = off;
+  l->xp = take(rk * Dp * es);
+  l->yp = take(rk * Dp * es);
+  l->xt = take(64 * Dp * es);
+  l->yt = take(64 * Dp * es);
+  l->h = take(rk * Fp * es);
+  l->dgu = take(rk * 2 * Fp * es);
+  off = start;
+  l->xq = take(r * Dc);
+  l->sx = take(r * 4);
+  l->hf = take(r * Fc * 4);
+  l->hmax = take(r * (Fp / 32) * 4);
+  l->hq = take(r * Fc);
+  l->sh = take(r * 4);
+  off = start;
+  l->aq = take(r * std::max(Dc, Fc));
+  l->bq = take(WPACK_BYTES);
+  l->need = need;
+}
+size_t plan_bytes(const hf_gated* c, int64_t R) {
+  Layout l;
+  plan(c, R, &l);
+  return l.need;
+}
+
+// ----------------------------------------------------------------- checks
+int check_rows(hf_gated* c, int64_t T) {
+  if (T < 0 || T > c->Rmax)
+    return fail(c, HF_EINVAL, "%lld rows outside [0, %lld]", (long long)T, (long long)c->Rmax);
+  return HF_OK;
+}
+int check_ready(hf_gated* c, int64_t T) {
+  if (!c->ws) return fail(c, HF_EWORKSPACE, "no workspace set (hf_gated_set_workspace)");
+  if (T > c->Rws)
+    return fail(c, HF_EWORKSPACE, "%lld rows above the %lld the workspace serves", (long long)T,
+                (long long)c->Rws);
+  return HF_OK;
+}
+// a rows x cols array on its own
+int check_size(hf_gated* c, int64_t rows, int64_t most, int64_t cols) {
+  if (rows < 0 || rows > most)
+    return fail(c, HF_EINVAL, "%lld rows outside [0, %lld]", (long long)rows, (long long)most);
+  if (cols < 1 || cols > HF_GATED_MAX_WIDTH)
+    return fail(c, HF_EINVAL, "%lld columns outside [1, %d]", (long long)cols, HF_GATED_MAX_WIDTH);
+  return HF_OK;
+}
+int check_weights(hf_gated* c, const void* Wg, int64_t ldg, const void* Wu, int64_t ldu,
+                  const void* Wd, int64_t ldd, int es) {
+  int rc;
+  if ((rc = check_mat(c, Wg, ldg, c->D, es, c->F, "Wg")) ||
+      (rc = check_mat(c, Wu, ldu, c->D, es, c->F, "Wu")) ||
+      (rc = check_mat(c, Wd, ldd, c->F, es, c->D, "Wd")))
+    return rc;
+  return HF_OK;
+}
+int end(hf_gated* c) {
+  HIP_TRY(c, hipGetLastError());
+  return HF_OK;
+}
+inline int blocks_of(int64_t cols) { return (int)((cols + CODE_BLOCK - 1) / CODE_BLOCK); }
+
+// -------------------------------------------------------------- operands
+// whether the GEMMs' 16-byte loads can read rows of p where they are
+inline bool loads16(const void* p, int64_t ld, int es) {
+  return ld <= MAX_LD && (uintptr_t)p % 16 == 0 && ld * es % 16 == 0;
+}
+
+// The copies that a call's operands need, made in one launch.
+struct Pads {
+  GPads all = {};
+  // p where it is (in_place), or its copy at dst
+  const void* operand(bool in_place, const void* p, int64_t ld, int64_t rows, int cols, int es,
+                      void* dst, int64_t prows, int pcols, int times, long long* out_ld) {
+    if (in_place) {
+      *out_ld = ld;
+      return p;
+    }
+    *out_ld = pcols;
+    all.p[all.n++] = GPad{p, dst, ld, (int)rows, cols, (int)prows, pcols, times, es};
+    return dst;
+  }
+};
+
+GGemm product(int M, int N, int K) {
+  GGemm g = {};
+  g.M = M;
+  g.N = N;
+  g.K = K;
+  g.alim = M;
+  g.blim = N;
+  g.ktail = INT_MAX;
+  g.splits = 1;
+  return g;
+}
+void set_shape(GGemm* g, int type, bool split) {
+  const Shape s = shape_for(type, g->M, g->N, g->K, split, false);
+  g->tile = s.tile;
+  g->splits = s.splits;
+}
+GEpi epilogue(const hf_gated* c, int64_t T) {
+  GEpi e = {};
+  e.act = c->act;
+  e.F = c->F;
+  e.Fp = c->Fp;
+  e.T = (int)T;
+  e.n1 = INT_MAX;
+  return e;
+}
+void set_out(GEpi* e, void* out, int64_t ldo, int64_t rows, int cols) {
+  e->out = out;
+  e->ldo = ldo;
+  e->nout = (int)rows;
+  e->mout = cols;
+}
+// a product into e's out: straight, or by partials
+template <class Kernel>
+void summed(hf_gated* c, const Launch& L, int type, int out_type, GGemm* g, GEpi* e, int dup,
+            Kernel kernel) {
+  set_shape(g, type, true);
+  if (g->splits > 1 || dup) {
+    e->part = c->at<float>(c->lay.part);
+    e->ldp = g->M;
+  }
+  kernel(*g, *e);
+  if (e->part) gated_finish(L, type, out_type, *g, *e, dup);
+}
+
+}  // namespace
+
+// ==================================================================== C ABI
+extern "C" {
+
+int hf_gated_create(int32_t width, int32_t hidden, int32_t act, int32_t type, int64_t max_rows,
+                    void* hip_stream, hf_gated** out) {
+  if (!out) return HF_EINVAL;
+  *out = nullptr;
+  if (width < 1 || width > HF_GATED_MAX_WIDTH || hidden < 1 || hidden > HF_GATED_MAX_WIDTH ||
+      act < HF_SIGMOID || act > HF_GELU_TANH ||
+      (type != HF_TYPE_FP32 && type != HF_TYPE_BF16) || max_rows < 1 ||
+      max_rows > HF_GATED_MAX_ROWS)
+    return HF_EINVAL;
+  hf_gated* c = new (std::nothrow) hf_gated();
+  if (!c) return HF_ENOMEM;
+  c->D = width;
+  c->F = hidden;
+  c->Dp = (int)up(width, VPAD);
+  c->Fp = (int)up(hidden, VPAD);
+  c->Dc = (int)up(width, CPAD);
+  c->Fc = (int)up(hidden, CPAD);
+  c->act = act;
+  c->type = type;
+  c->es = type == HF_TYPE_FP32 ? 4 : 2;
+  c->Rmax = max_rows;
+  c->stream = reinterpret_cast<hipStream_t>(hip_stream);
+  *out = c;
+  return HF_OK;
+}
+
+int hf_gated_destroy(hf_gated* c) {
+  if (!c) return HF_OK;
+  if (c->last) (void)hipEventDestroy(c->last);
+  delete c;
+  return HF_OK;
+}
+
+int hf_gated_set_stream(hf_gated* c, void* s) {
+  if (!c) return HF_EINVAL;
+  c->stream = reinterpret_cast<hipStream_t>(s);
+  return c->pending ? follow(c, false) : HF_OK;
+}
+
+size_t hf_gated_workspace_bytes(const hf_gated* c, int64_t rows) {
+  if (!c) return 0;
+  if (rows <= 0) rows = c->Rmax;
+  if (rows > c->Rmax) return 0;
+  return plan_bytes(c, rows);
+}
+
+int hf_gated_set_workspace(hf_gated* c, void* p, size_t bytes) {
+  if (!c) return HF_EINVAL;
+  if (!p) return fail(c, HF_EINVAL, "workspace pointer is NULL");
+  if ((uintptr_t)p & 255u) return fail(c, HF_EINVAL, "workspace is not 256-byte aligned");
+  const size_t need1 = plan_bytes(c, 1);
+  if (bytes < need1)
+    return fail(c, HF_EWORKSPACE, "workspace of %zu bytes is smaller than the %zu needed "
+                "for one row", bytes, need1);
+  // the largest number of rows whose layout fits (it grows with the rows)
+  int64_t lo = 1, hi = c->Rmax;
+  while (lo < hi) {
+    const int64_t mid = lo + (hi - lo + 1) / 2;
+    if (plan_bytes(c, mid) <= bytes) lo = mid;
+    else hi = mid - 1;
+  }
+  plan(c, lo, &c->lay);
+  c->Rws = lo;
+  c->pending = false;
+  c->ws = reinterpret_cast<char*>(p);
+  return HF_OK;
+}
+
+int hf_gated_forward(hf_gated* c, const void* X, int64_t ldx, const void* Wg, int64_t ldg,
+                     const void* Wu, int64_t ldu, const void* Wd, int64_t ldd, int64_t rows,
+                     void* Y, int64_t ldy, int32_t keep, void* kept, int64_t ldk, uint8_t* scale,
+                     int64_t lds) {
+  int rc;
+  if (!c) return HF_EINVAL;
+  if ((rc = check_rows(c, rows)) ||
+      (rc = check_mat(c, X, ldx, c->D, c->es, rows, "X")) ||
+      (rc = check_weights(c, Wg, ldg, Wu, ldu, Wd, ldd, c->es)) ||
+      (rc = check_mat(c, Y, ldy, c->D, c->es, rows, "Y")) ||
+      (rc = check_apart(c, X, "X", Y, "Y", rows)))
+    return rc;
+  if (keep != HF_KEEP_NONE && keep != HF_KEEP_FULL && keep != HF_KEEP_CODES)
+    return fail(c, HF_EINVAL, "keep %d is none of HF_KEEP_*", keep);
+  if (keep != HF_KEEP_NONE &&
+      ((rc = check_mat(c, kept, ldk, 2 * (int64_t)c->F, keep == HF_KEEP_FULL ? c->es : 1, rows,
+                       "kept")) ||
+       (rc = check_apart(c, X, "X", kept, "kept", rows)) ||
+       (rc = check_apart(c, Y, "Y", kept, "kept", rows))))
+    return rc;
+  if (keep == HF_KEEP_CODES &&
+      (rc = check_mat(c, scale, lds, 2 * blocks_of(c->F), 1, rows, "scale")))
+    return rc;
+  if ((rc = check_ready(c, rows)) || (rc = follow(c, true))) return rc;
+  if (rows == 0) return HF_OK;
+  const Launch L{c->stream, nullptr};
+  const Layout& l = c->lay;
+  const int T = (int)rows, D = c->D, F = c->F, Dp = c->Dp, Fp = c->Fp, es = c->es;
+  const int dup = two_term(c, T);
+
+  GGemm gu = product(2 * Fp, T, Dp), gd = product(Dp, dup ? 2 * dup : T, Fp);
+  GEpi eu = epilogue(c, T), ed = epilogue(c, T);
+  Pads pads;
+  gu.B = pads.operand(D == Dp && loads16(X, ldx, es), X, ldx, T, D, es, c->at<void>(l.xp), T, Dp, 1,
+                      &gu.ldb);
+  const bool pair = D == Dp && ldg == ldu && loads16(Wg, ldg, es) && loads16(Wu, ldu, es);
+  gu.A = pads.operand(pair, Wg, ldg, F, D, es, c->at<void>(l.wg), Fp, Dp, 1, &gu.lda);
+  gu.A1 = pads.operand(pair, Wu, ldu, F, D, es, c->at<void>(l.wu), Fp, Dp, 1, &gu.lda);
+  gu.alim = F;
+  gd.A = pads.operand(F == Fp && loads16(Wd, ldd, es), Wd, ldd, D, F, es, c->at<void>(l.wd), D, Fp, 1,
+                      &gd.lda);
+  gd.alim = D;
+  gated_pad(L, pads.all);
+
+  eu.h = c->at<void>(l.h);
+  eu.ldh = Fp;
+  eu.dup = dup;
+  eu.keep = keep;
+  eu.kept = kept;
+  eu.ldk = ldk;
+  eu.ks = scale;
+  eu.ldks = lds;
+  set_shape(&gu, c->type, false);
+  gated_up(L, c->type, gu, eu);
+
+  gd.B = eu.h;
+  gd.ldb = Fp;
+  set_out(&ed, Y, ldy, T, D);
+  summed(c, L, c->type, c->type, &gd, &ed, dup, [&](const GGemm& g, const GEpi& e) {
+    gated_down(L, c->type, c->type, g, e);
+  });
+  return end(c);
+}
+
+int hf_gated_grad(hf_gated* c, const void* X, int64_t ldx, const uint8_t* xscale, int64_t ldxs,
+                  const void* Wg, int64_t ldg, const void* Wu, int64_t ldu, const void* Wd,
+                  int64_t ldd, int32_t keep, const void* kept, int64_t ldk, const uint8_t* scale,
+                  int64_t lds, const void* dY, int64_t lddy, int64_t rows, void* dX, int64_t lddx,
+                  void* dWg, int64_t lddg, void* dWu, int64_t lddu, void* dWd, int64_t lddd,
+                  int32_t accumulate) {
+  int rc;
+  if (!c) return HF_EINVAL;
+  if (keep != HF_KEEP_FULL && keep != HF_KEEP_CODES)
+    return fail(c, HF_EINVAL, "keep %d is neither HF_KEEP_FULL nor HF_KEEP_CODES", keep);
+  if ((rc = check_rows(c, rows)) ||
+      (rc = check_mat(c, X, ldx, c->D, xscale ? 1 : c->es, rows, "X")) ||
+      (xscale && (rc = check_mat(c, xscale, ldxs, blocks_of(c->D), 1, rows, "xscale"))) ||
+      (rc = check_weights(c, Wg, ldg, Wu, ldu, Wd, ldd, c->es)) ||
+      (rc = check_mat(c, kept, ldk, 2 * (int64_t)c->F, keep == HF_KEEP_FULL ? c->es : 1, rows,
+                      "kept")) ||
+      (keep == HF_KEEP_CODES &&
+       (rc = check_mat(c, scale, lds, 2 * blocks_of(c->F), 1, rows, "scale"))) ||
+      (rc = check_mat(c, dY, lddy, c->D, c->es, rows, "dY")))
+    return rc;
+  if (!dX && !dWg && !dWu && !dWd) return fail(c, HF_EINVAL, "no gradient given");
+  if ((dX && (rc = check_mat(c, dX, lddx, c->D, c->es, rows, "dX"))) ||
+      (dWg && (rc = check_mat(c, dWg, lddg, c->D, c->es, c->F, "dWg"))) ||
+      (dWu && (rc = check_mat(c, dWu, lddu, c->D, c->es, c->F, "dWu"))) ||
+      (dWd && (rc = check_mat(c, dWd, lddd, c->F, c->es, c->D, "dWd"))))
+    return rc;
+  if ((rc = check_apart(c, X, "X", dX, "dX", rows)) ||
+      (rc = check_apart(c, dY, "dY", dX, "dX", rows)) ||
+      (rc = check_apart(c, kept, "kept", dX, "dX", rows)) ||
+      (rc = check_apart(c, Wg, "Wg", dWg, "dWg", 1)) ||
+      (rc = check_apart(c, Wu, "Wu", dWu, "dWu", 1)) ||
+      (rc = check_apart(c, Wd, "Wd", dWd, "dWd", 1)) ||
+      (rc = check_apart(c, dWg, "dWg", dWu, "dWu", 1)))
+    return rc;
+  if (accumulate != 0 && accumulate != 1)
+    return fail(c, HF_EINVAL, "accumulate %d is neither 0 nor 1", accumulate);
+  if ((rc = check_ready(c, rows)) || (rc = follow(c, true))) return rc;
+  const Launch L{c->stream, nullptr};
+  const Layout& l = c->lay;
+  const int T = (int)rows, D = c->D, F = c->F, Dp = c->Dp, Fp = c->Fp, es = c->es, type = c->type;
+  const int dup = two_term(c, T);
+  const int Tp = (int)up(T, 64), Kt = dup ? 2 * dup : Tp, T0 = T / 64 * 64;
+  // (no rows: the sum of nothing)
+  GGemm gd = product(Fp, Dp, Kt), gw = product(Dp, 2 * Fp, Kt);
+  GEpi ed = epilogue(c, T), ew = epilogue(c, T);
+  ed.accumulate = ew.accumulate = accumulate;
+  set_out(&ed, dWd, lddd, D, F);
+  set_out(&ew, dWg ? dWg : dWu, dWg ? lddg : lddu, F, D);
+  if (!dWg || !dWu) gw.N = Fp;
+  ew.n1 = dWg && dWu ? Fp : INT_MAX;
+  ew.out1 = dWu;
+  ew.ldo1 = lddu;
+  if (T == 0) {
+    if (accumulate) return HF_OK;
+    gd.splits = gw.splits = 0;
+    if (dWd) gated_finish(L, type, type, gd, ed, 0);
+    if (ew.out) gated_finish(L, type, type, gw, ew, 0);
+    return end(c);
+  }
+
+  Pads pads;
+  const bool weights = D == Dp && F == Fp && ldg == ldu && loads16(Wg, ldg, es) &&
+                       loads16(Wu, ldu, es) && loads16(Wd, ldd, es);
+  GGemm gh = product(Fp, Tp, Dp), gx = product(Dp, dup ? 2 * dup : T, 2 * Fp);
+  gh.A = pads.operand(weights, Wd, ldd, D, F, es, c->at<void>(l.wd), Dp, Fp, 1, &gh.lda);
+  if (dX) {
+    gx.A = pads.operand(weights, Wg, ldg, F, D, es, c->at<void>(l.wg), Fp, Dp, 1, &gx.lda);
+    gx.A1 = pads.operand(weights, Wu, ldu, F, D, es, c->at<void>(l.wu), Fp, Dp, 1, &gx.lda);
+  }
+  // rows of X and dY: whole K blocks (few bf16 rows: both copies), or where they
+  // are, with the last block's in a copy
+  auto rows_of = [&](const void* p, int64_t ld, size_t copy, size_t tail, bool need_k,
+                     const void** at, long long* ldat, long long* out_ld) -> const void* {
+    const bool place = D == Dp && loads16(p, ld, es) && !(dup && need_k);
+    const void* q = pads.operand(place, p, ld, T, D, es, c->at<void>(copy), dup ? dup : Tp, Dp,
+                                 dup ? 2 : 1, out_ld);
+    if (place && need_k && T % 64)
+      *at = pads.operand(false, (const char*)p + (size_t)T0 * ld * es, ld, T - T0, D, es,
+                         c->at<void>(tail), 64, Dp, 1, ldat);
+    return q;
+  };
+  gh.B = rows_of(dY, lddy, l.yp, l.yt, dWd != nullptr, &gd.bt, &gd.ldbt, &gh.ldb);
+  gh.blim = T;
+  gd.B = gh.B;
+  gd.ldb = gh.ldb;
+  gd.ktail = gw.ktail = T0;
+  if (ew.out) {
+    if (xscale) {
+      gw.A = c->at<void>(l.xp);
+      gw.lda = Dp;
+    } else {
+      gw.A = rows_of(X, ldx, l.xp, l.xt, true, &gw.at, &gw.ldat, &gw.lda);
+    }
+  }
+  gated_pad(L, pads.all);
+  if (ew.out && xscale)
+    gated_unpack(L, type, (const int8_t*)X, ldx, xscale, ldxs, T, D, c->at<void>(l.xp), Dp,
+                 dup ? dup : Tp, Dp, dup ? 2 : 1);
+
+  GEpi eh = epilogue(c, T), ex = epilogue(c, T);
+  eh.h = c->at<void>(l.h);
+  eh.ldh = Fp;
+  eh.dgu = c->at<void>(l.dgu);
+  eh.lddgu = 2 * Fp;
+  eh.dup = dup;
+  eh.keep = keep;
+  eh.kept = const_cast<void*>(kept);
+  eh.ldk = ldk;
+  eh.ks = const_cast<uint8_t*>(scale);
+  eh.ldks = lds;
+  set_shape(&gh, type, false);
+  gated_dh(L, type, gh, eh);
+
+  if (dX) {
+    gx.B = eh.dgu;
+    gx.ldb = eh.lddgu;
+    gx.kh = Fp;
+    set_out(&ex, dX, lddx, T, D);
+    summed(c, L, type, type, &gx, &ex, dup,
+           [&](const GGemm& g, const GEpi& e) { gated_dx(L, type, g, e); });
+  }
+  auto dw = [&](const GGemm& g, const GEpi& e) { gated_dw(L, type, g, e); };
+  if (dWd) {
+    gd.A = eh.h;
+    gd.lda = Fp;
+    summed(c, L, type, type, &gd, &ed, 0, dw);
+  }
+  if (ew.out) {
+    gw.B = (const char*)eh.dgu + (dWg ? 0 : (size_t)Fp * es);
+    gw.ldb = eh.lddgu;
+    summed(c, L, type, type, &gw, &ew, 0, dw);
+  }
+  return end(c);
+}
+
+int hf_gated_pack(hf_gated* c, const void* X, int64_t ldx, int64_t rows, int64_t cols,
+                  int8_t* codes, int64_t ldc, uint8_t* scale, int64_t lds) {
+  int rc;
+  if (!c) return HF_EINVAL;
+  if ((rc = check_size(c, rows, HF_GATED_MAX_ROWS, cols)) ||
+      (rc = check_mat(c, X, ldx, cols, c->es, rows, "X")) ||
+      (rc = check_mat(c, codes, ldc, cols, 1, rows, "codes")) ||
+      (rc = check_mat(c, scale, lds, blocks_of(cols), 1, rows, "scale")) ||
+      (rc = check_apart(c, X, "X", codes, "codes", rows)))
+    return rc;
+  gated_pack(Launch{c->stream, nullptr}, c->type, X, ldx, rows, (int)cols, codes, ldc, scale, lds);
+  return end(c);
+}
+
+int hf_gated_unpack(hf_gated* c, const int8_t* codes, int64_t ldc, const uint8_t* scale,
+                    int64_t lds, int64_t rows, int64_t cols, void* X, int64_t ldx) {
+  int rc;
+  if (!c) return HF_EINVAL;
+  if ((rc = check_size(c, rows, HF_GATED_MAX_ROWS, cols)) ||
+      (rc = check_mat(c, codes, ldc, cols, 1, rows, "codes")) ||
+      (rc = check_mat(c, scale, lds, blocks_of(cols), 1, rows, "scale")) ||
+      (rc = check_mat(c, X, ldx, cols, c->es, rows, "X")) ||
+      (rc = check_apart(c, codes, "codes", X, "X", rows)))
+    return rc;
+  gated_unpack(Launch{c->stream, nullptr}, c->type, codes, ldc, scale, lds, rows, (int)cols, X, ldx,
+               rows, (int)cols, 1);
+  return end(c);
+}
+
+int hf_gated_codes(hf_gated* c, const void* X, int64_t ldx, int64_t rows, int64_t cols,
+                   int8_t* codes, int64_t ldc, float* scale) {
+  int rc;
+  if (!c) return HF_EINVAL;
+  if ((rc = check_size(c, rows, HF_GATED_MAX_OUT, cols)) ||
+      (rc = check_mat(c, X, ldx, cols, c->es, rows, "X")) ||
+      (rc = check_mat(c, codes, ldc, cols, 1, rows, "codes")) ||
+      (rc = check_mat(c, scale, 1, 1, 4, rows, "scale")) ||
+      (rc = check_apart(c, X, "X", codes, "codes", rows)))
+    return rc;
+  gated_codes(Launch{c->stream, nullptr}, c->type, X, ldx, rows, (int)cols, codes, ldc, (int)cols,
+              scale);
+  return end(c);
+}
+
+int hf_gated_product(hf_gated* c, const int8_t* A, int64_t lda, const float* sa, const int8_t* B,
+                     int64_t ldb, const float* sb, int64_t rows, int64_t n, int64_t k, void* Y,
+                     int64_t ldy) {
+  int rc;
+  if (!c) return HF_EINVAL;
+  if ((rc = check_rows(c, rows))) return rc;
+  if (n < 1 || n > HF_GATED_MAX_OUT)
+    return fail(c, HF_EINVAL, "%lld channels outside [1, %d]", (long long)n, HF_GATED_MAX_OUT);
+  if (k < 1 || k > std::max(c->D, c->F))
+    return fail(c, HF_EINVAL, "%lld columns outside [1, %d], the larger of the widths",
+                (long long)k, std::max(c->D, c->F));
+  if ((rc = check_mat(c, A, lda, k, 1, rows, "A")) || (rc = check_mat(c, sa, 1, 1, 4, rows, "sa")) ||
+      (rc = check_mat(c, B, ldb, k, 1, n, "B")) || (rc = check_mat(c, sb, 1, 1, 4, n, "sb")) ||
+      (rc = check_mat(c, Y, ldy, n, c->es, rows, "Y")) ||
+      (rc = check_apart(c, A, "A", Y, "Y", rows)) || (rc = check_apart(c, B, "B", Y, "Y", rows)) ||
+      (rc = check_ready(c, rows)) || (rc = follow(c, true)))
+    return rc;
+  if (rows == 0) return HF_OK;
+  const Launch L{c->stream, nullptr};
+  const Layout& l = c->lay;
+  const int T = (int)rows, K = (int)up(k, CPAD);
+  const bool place = k % CPAD == 0 && loads16(B, ldb, 1);
+  // channels at a time: all where they are, or as many as are packed; tiles of
+  // partials go by columns of 64
+  const int64_t step = place ? n : std::max<int64_t>((int64_t)(WPACK_BYTES / (size_t)K) / 256 * 256, 256);
+  long long ldaq = 0;
+  const void* aq = nullptr;
+  for (int64_t n0 = 0; n0 < n; n0 += step) {
+    const int nn = (int)std::min(step, n - n0);
+    Pads pads;
+    GGemm g = product((int)up(nn, 64), T, K);
+    if (n0 == 0)
+      aq = pads.operand(k % CPAD == 0 && loads16(A, lda, 1), A, lda, T, (int)k, 1,
+                        c->at<void>(l.aq), T, K, 1, &ldaq);
+    g.A = pads.operand(place, B + n0 * ldb, ldb, nn, (int)k, 1, c->at<void>(l.bq), nn, K, 1, &g.lda);
+    g.alim = nn;
+    g.B = aq;
+    g.ldb = ldaq;
+    gated_pad(L, pads.all);
+    GEpi e = epilogue(c, T);
+    e.sn = sa;
+    e.sm = sb + n0;
+    set_out(&e, (char*)Y + n0 * c->es, ldy, T, nn);
+    summed(c, L, VT_I8, c->type, &g, &e, 0, [&](const GGemm& gg, const GEpi& ee) {
+      gated_down(L, VT_I8, c->type, gg, ee);
+    });
+  }
+  return end(c);
+}
+
+int hf_gated_forward_codes(hf_gated* c, const void* X, int64_t ldx, const int8_t* Wg, int64_t ldg,
+                           const float* sg, const int8_t* Wu, int64_t ldu, const float* su,
+                           const int8_t* Wd, int64_t ldd, const float* sd, int64_t rows, void* Y,
+                           int64_t ldy) {
+  int rc;
+  if (!c) return HF_EINVAL;
+  if ((rc = check_rows(c, rows)) ||
+      (rc = check_mat(c, X, ldx, c->D, c->es, rows, "X")) ||
+      (rc = check_weights(c, Wg, ldg, Wu, ldu, Wd, ldd, 1)) ||
+      (rc = check_mat(c, sg, 1, 1, 4, c->F, "sg")) || (rc = check_mat(c, su, 1, 1, 4, c->F, "su")) ||
+      (rc = check_mat(c, sd, 1, 1, 4, c->D, "sd")) ||
+      (rc = check_mat(c, Y, ldy, c->D, c->es, rows, "Y")) ||
+      (rc = check_apart(c, X, "X", Y, "Y", rows)) ||
+      (rc = check_ready(c, rows)) || (rc = follow(c, true)))
+    return rc;
+  if (rows == 0) return HF_OK;
+  const Launch L{c->stream, nullptr};
+  const Layout& l = c->lay;
+  const int T = (int)rows, D = c->D, F = c->F, Dc = c->Dc, Fc = c->Fc, Fp = c->Fp;
+  GGemm gu = product(2 * Fp, T, Dc), gd = product(c->Dp, T, Fc);
+  GEpi eu = epilogue(c, T), ed = epilogue(c, T);
+  Pads pads;
+  const bool pair = D == Dc && ldg == ldu && loads16(Wg, ldg, 1) && loads16(Wu, ldu, 1);
+  gu.A = pads.operand(pair, Wg, ldg, F, D, 1, c->at<void>(l.wg), F, Dc, 1, &gu.lda);
+  gu.A1 = pads.operand(pair, Wu, ldu, F, D, 1, c->at<void>(l.wu), F, Dc, 1, &gu.lda);
+  gu.alim = F;
+  gd.A = pads.operand(F == Fc && loads16(Wd, ldd, 1), Wd, ldd, D, F, 1, c->at<void>(l.wd), D, Fc, 1,
+                      &gd.lda);
+  gd.alim = D;
+  gated_pad(L, pads.all);
+  int8_t* xq = c->at<int8_t>(l.xq);
+  int8_t* hq = c->at<int8_t>(l.hq);
+  float *sx = c->at<float>(l.sx), *sh = c->at<float>(l.sh);
+  gated_codes(L, c->type, X, ldx, T, D, xq, Dc, Dc, sx);
+  gu.B = xq;
+  gu.ldb = Dc;
+  eu.sn = sx;
+  eu.sm = sg;
+  eu.sm1 = su;
+  eu.h = c->at<float>(l.hf);
+  eu.ldh = Fc;
+  eu.hmax = c->at<float>(l.hmax);
+  eu.ldmax = Fp / 32;
+  set_shape(&gu, VT_I8, false);
+  gated_up(L, VT_I8, gu, eu);
+  gated_codes_h(L, c->at<float>(l.hf), Fc, eu.hmax, eu.ldmax, T, F, hq, Fc, Fc, sh);
+  gd.B = hq;
+  gd.ldb = Fc;
+  ed.sn = sh;
+  ed.sm = sd;
+  set_out(&ed, Y, ldy, T, D);
+  summed(c, L, VT_I8, c->type, &gd, &ed, 0, [&](const GGemm& g, const GEpi& e) {
+    gated_down(L, VT_I8, c->type, g, e);
+  });
+  return end(c);
+}
+
+const char* hf_gated_last_error(const hf_gated* c) {
+  return c ? c->err.c_str() : "null context";
+}
+
+}  // extern "C"

@@ -1,0 +1,101 @@
+// Internal declarations of the gated feed-forward block: its products in fp32,
+// bf16 and 8-bit codes, checkpoints in 8 bits, and the row kernels around them.
+#pragma once
+
+#include "vocab_internal.h"
+
+namespace hfk {
+
+enum { GA_SIGMOID, GA_TANH, GA_RELU, GA_SILU, GA_GELU, GA_GELU_TANH };
+enum { KEEP_NONE, KEEP_FULL, KEEP_CODES };
+
+// Columns of a checkpoint that share a scale byte.
+constexpr int CODE_BLOCK = 32;
+// Widths of packed codes: whole K blocks of 128.
+constexpr int CPAD = 128;
+
+// C(m, n) = sum_k A(m, k) B(n, k), m contiguous in the output (see mfma_tile.h).
+struct GGemm {
+  int M, N, K;
+  const void *A, *A1, *B;
+  long long lda, ldb;
+  int alim, blim;        // rows m of A and n of B that exist, where these are rows
+  int kh;                // row products: A1 has the rows k from kh on
+  // operands whose rows are k: those from ktail on are read here, where zeros
+  // follow the last one; null: they follow where the operand is
+  const void *at, *bt;
+  long long ldat, ldbt;
+  int ktail;
+  int splits, tile;
+};
+
+struct GEpi {
+  int act, F, Fp;        // hidden width, and as the workspace has it
+  int T;                 // rows of the call
+  void* h;               // phi(g) u: fp32 for codes, else of the type
+  long long ldh;
+  int dup;               // > 0: the rounding's rest too, dup rows further down
+  int keep;
+  void* kept;            // g, and F elements further u
+  long long ldk;
+  uint8_t* ks;           // scale bytes of g's blocks, and then of u's
+  long long ldks;
+  void* dgu;             // dg, and Fp columns further du
+  long long lddgu;
+  const float *sn, *sm, *sm1;   // codes: scales of the rows n, and of m (sm1: of u)
+  float* hmax;           // codes: largest |h| of a row in each wave's columns
+  int ldmax;
+  void *out, *out1;      // out1: rows from n1 on, at row n - n1
+  long long ldo, ldo1;
+  int n1, nout, mout;    // rows of each, columns
+  int accumulate;
+  float* part;           // partials [split][n][m] (codes: int32)
+  long long ldp;
+};
+
+// h = phi(X Wg^T) * (X Wu^T): A = Wg, A1 = Wu (rows alim), B = X; M = 2 Fp
+void gated_up(const Launch& L, int type, const GGemm& g, const GEpi& e);
+// out = B A^T: A = Wd, B = h; codes: out_type, scaled
+void gated_down(const Launch& L, int type, int out_type, const GGemm& g, const GEpi& e);
+// dh = dY Wd in the tile, from it and what is kept h, dg and du
+void gated_dh(const Launch& L, int type, const GGemm& g, const GEpi& e);
+// dX = dg Wg + du Wu
+void gated_dx(const Launch& L, int type, const GGemm& g, const GEpi& e);
+// B^T A over the rows
+void gated_dw(const Launch& L, int type, const GGemm& g, const GEpi& e);
+// out from the partials of g with e; row n + dup joins row n if dup
+void gated_finish(const Launch& L, int type, int out_type, const GGemm& g, const GEpi& e, int dup);
+
+// Copies of a call's operands with zeros around: rows x cols elements of es
+// bytes, ld apart, to prows x pcols ones (times > 1: so often, below each other).
+struct GPad {
+  const void* src;
+  void* dst;
+  long long ld;
+  int rows, cols, prows, pcols, times;
+  int es;
+};
+constexpr int GPADS = 6;
+struct GPads {
+  GPad p[GPADS];
+  int n;
+};
+void gated_pad(const Launch& L, const GPads& p);
+
+// checkpoints: rows x cols of the type to codes and scale bytes, and back
+void gated_pack(const Launch& L, int type, const void* X, long long ldx, long long rows, int cols,
+                int8_t* codes, long long ldc, uint8_t* scale, long long lds);
+// zrows (>= rows): rows of zeros up to there, zcols (>= cols) columns
+void gated_unpack(const Launch& L, int type, const int8_t* codes, long long ldc,
+                  const uint8_t* scale, long long lds, long long rows, int cols, void* X,
+                  long long ldx, long long zrows, int zcols, int times);
+
+// codes of rows with a scale each: q = round(x / s), s = max |x| / 127; zeros up
+// to zcols columns
+void gated_codes(const Launch& L, int type, const void* X, long long ldx, long long rows, int cols,
+                 int8_t* codes, long long ldc, int zcols, float* scale);
+// the same of fp32 rows whose largest numbers are in hmax's ldmax parts
+void gated_codes_h(const Launch& L, const float* H, long long ldh, const float* hmax, int ldmax,
+                   int rows, int cols, int8_t* codes, long long ldc, int zcols, float* scale);
+
+}  // namespace hfk

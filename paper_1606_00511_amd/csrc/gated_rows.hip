@@ -1,0 +1,370 @@
+// Row kernels of the gated block: copies of operands with zeros around, sums of
+// split products, checkpoints in 8 bits and codes with a scale for each row.  All
+// are bound by memory.
+#include <algorithm>
+
+#include "gated_act.h"
+#include "gated_values.h"
+#include "mfma_tile.h"
+
+namespace hfk {
+namespace {
+
+// ------------------------------------------------------------------- padding
+// 16 bytes of a destination row from chunk c: elements of the source row, zeros
+// past `cols`
+template <class E>
+__device__ __forceinline__ u32x4 padded(const E* src, int c, int cols) {
+  constexpr int N = 16 / (int)sizeof(E);
+  const int at = c * N;
+  u32x4 w = u32x4{0u, 0u, 0u, 0u};
+  if (at + N <= cols) {
+    __builtin_memcpy(&w, src + at, 16);
+  } else if (at < cols) {
+    E v[N];
+#pragma unroll
+    for (int j = 0; j < N; ++j) v[j] = at + j < cols ? src[at + j] : E(0);
+    __builtin_memcpy(&w, v, 16);
+  }
+  return w;
+}
+
+// ------------------------------------------------- sums of split products
+template <class E, class O>
+__device__ __forceinline__ void finish_body(const GGemm& g, const GEpi& e, int dup, int rows,
+                                            int chunks, long long stride, long long total) {
+  for (long long i = blockIdx.x * 256ll + threadIdx.x; i < total; i += gridDim.x * 256ll) {
+    const int row = (int)(i / chunks), m = 8 * (int)(i % chunks);
+    const bool second = row >= e.nout;
+    const int n = second ? e.n1 + row - e.nout : row, have = e.mout - m;
+    const float* p = e.part + (size_t)n * e.ldp + m;
+    float v[8];
+    if constexpr (sizeof(E) == 1) {
+      int t[8] = {};
+      for (int s = 0; s < g.splits; ++s) {
+        const i32x4 a = *(const i32x4*)(p + s * stride), b = *(const i32x4*)(p + s * stride + 4);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          t[j] += a[j];
+          t[4 + j] += b[j];
+        }
+      }
+      const float sn = e.sn[n];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = (float)t[j] * (sn * e.sm[min(m + j, e.mout - 1)]);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = 0.0f;
+      for (int h = 0; h < (dup ? 2 : 1); ++h) {
+        const float* q = p + (size_t)h * dup * e.ldp;
+        for (int s = 0; s < g.splits; ++s) {
+          const f32x4 a = *(const f32x4*)(q + s * stride), b = *(const f32x4*)(q + s * stride + 4);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            v[j] += a[j];
+            v[4 + j] += b[j];
+          }
+        }
+      }
+    }
+    O* out = (O*)(second ? e.out1 : e.out) +
+             (size_t)(second ? row - e.nout : row) * (second ? e.ldo1 : e.ldo) + m;
+    if (e.accumulate) {
+      float o[8];
+      get(out, o, have);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] += o[j];
+    }
+    put(out, v, have);
+  }
+}
+
+// ------------------------------------------------------------- checkpoints
+template <class E>
+__device__ __forceinline__ void pack_body(const E* X, long long ldx, uint32_t total, int cols,
+                                          uint32_t per, int8_t* codes, long long ldc,
+                                          uint8_t* scale, long long lds) {
+  // (whole blocks of 32: the 4 lanes of one are all here or none is)
+  const uint32_t i = blockIdx.x * 256u + threadIdx.x;
+  if (i >= total) return;
+  const uint32_t row = i / per, c = i % per;
+  const int at = 8 * (int)c, have = cols - at;
+  float v[8];
+  get(X + (size_t)row * ldx + at, v, have);
+  const int byte = put_codes(codes + (size_t)row * ldc + at, v, have);
+  if ((c & 3) == 0) scale[(size_t)row * lds + c / 4] = (uint8_t)byte;
+}
+
+template <class E>
+__device__ __forceinline__ void unpack_body(const int8_t* codes, long long ldc,
+                                            const uint8_t* scale, long long lds, uint32_t rows,
+                                            int cols, E* X, long long ldx, uint32_t zrows,
+                                            int zcols, uint32_t per, uint32_t total) {
+  const uint32_t i = blockIdx.x * 256u + threadIdx.x;
+  if (i >= total) return;
+  const uint32_t to = i / per, c = i % per, row = to % zrows;
+  const int at = 8 * (int)c;
+  const int have = row < rows ? cols - at : 0;
+  float v[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) v[j] = 0.0f;
+  if (have > 0)
+    get_codes(codes + (size_t)row * ldc + at, code_step(scale[(size_t)row * lds + c / 4]), v, have);
+  put(X + (size_t)to * ldx + at, v, zcols - at);
+}
+
+// --------------------------------------------------------- codes of rows
+// q = round(x / s) to even, exactly: the quotient by 1 / s is off by less than
+// one, and what is left of x is exact in an fma
+__device__ __forceinline__ int row_code(float x, float s, float inv) {
+  float q = rintf(x * inv);
+  const float r = fmaf(-q, s, x), half = 0.5f * s;
+  const bool odd = (int)q & 1;
+  if (r > half || (r == half && odd)) q += 1.0f;
+  else if (-r > half || (-r == half && odd)) q -= 1.0f;
+  return (int)fminf(fmaxf(q, -127.0f), 127.0f);
+}
+struct RowScale {
+  float s;       // what is stored
+  float f, ss, inv;   // x f / ss, with f a power of two that keeps 1 / ss finite
+};
+__device__ __forceinline__ RowScale row_scale(uint32_t big) {
+  RowScale r;
+  const float amax = __uint_as_float(big);
+  r.s = big >= 0x7f800000u ? __uint_as_float(0x7fc00000u) : amax / 127.0f;
+  const bool none = big >= 0x7f800000u || r.s == 0.0f;
+  r.f = none ? 0.0f : r.s < 1e-30f ? 0x1p64f : 1.0f;
+  r.ss = none ? 1.0f : r.s * r.f;
+  r.inv = 1.0f / r.ss;
+  return r;
+}
+__device__ __forceinline__ void put_row_codes(int8_t* p, const float (&v)[8], const RowScale& r,
+                                              int have, int room) {
+  uint32_t w[2] = {0u, 0u};
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const int q = j < have && r.f != 0.0f ? row_code(v[j] * r.f, r.ss, r.inv) : 0;
+    w[j >> 2] |= (uint32_t)(q & 255) << (8 * (j & 3));
+  }
+  if (room >= 8) {
+    __builtin_memcpy(p, w, 8);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (j < room) p[j] = (int8_t)(w[j >> 2] >> (8 * (j & 3)));
+  }
+}
+// the largest of the workgroup's, W waves
+template <int W>
+__device__ __forceinline__ uint32_t group_max(uint32_t big) {
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) big = max(big, (uint32_t)__shfl_xor((int)big, d, 64));
+  if constexpr (W > 1) {
+    __shared__ uint32_t part[W];
+    if (threadIdx.x % 64 == 0) part[threadIdx.x / 64] = big;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < W; ++w) big = max(big, part[w]);
+  }
+  return big;
+}
+// a row by a workgroup of 64 W lanes
+template <class E, int W>
+__device__ __forceinline__ void codes_body(const E* X, long long ldx, int cols, int8_t* codes,
+                                           long long ldc, int zcols, float* scale) {
+  const size_t row = blockIdx.x;
+  const E* x = X + row * ldx;
+  uint32_t big = 0;
+  for (int at = 8 * (int)threadIdx.x; at < cols; at += 512 * W) {
+    float v[8];
+    get(x + at, v, cols - at);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) big = max(big, __float_as_uint(v[j]) & 0x7fffffffu);
+  }
+  const RowScale r = row_scale(group_max<W>(big));
+  if (threadIdx.x == 0) scale[row] = r.s;
+  for (int at = 8 * (int)threadIdx.x; at < zcols; at += 512 * W) {
+    float v[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = 0.0f;
+    if (at < cols) get(x + at, v, cols - at);
+    put_row_codes(codes + row * ldc + at, v, r, cols - at, zcols - at);
+  }
+}
+
+}  // namespace
+
+extern "C" __global__ __launch_bounds__(256) void hf_gated_pad(GPads all, int chunks0, int chunks1,
+                                                               int chunks2, int chunks3,
+                                                               int chunks4) {
+  // the copy that this workgroup belongs to
+  int b = blockIdx.x, k = 0;
+  const int n[GPADS - 1] = {chunks0, chunks1, chunks2, chunks3, chunks4};
+#pragma unroll
+  for (int j = 0; j < GPADS - 1; ++j)
+    if (k == j && b >= n[j]) {
+      b -= n[j];
+      k = j + 1;
+    }
+  const GPad p = all.p[k];
+  const uint32_t per = (uint32_t)(p.pcols * p.es / 16);
+  const uint32_t rows = (uint32_t)p.prows * p.times;
+  // 4 rows of chunks a workgroup and step: 1,024 chunks
+#pragma unroll
+  for (int u = 0; u < 4; ++u) {
+    const uint32_t i = (uint32_t)b * 1024u + 256u * u + threadIdx.x;
+    const uint32_t to = i / per, c = i % per;
+    if (to >= rows) return;
+    const uint32_t row = to % (uint32_t)p.prows;
+    u32x4 w = u32x4{0u, 0u, 0u, 0u};
+    if ((int)row < p.rows) {
+      const char* src = (const char*)p.src + (size_t)row * p.ld * p.es;
+      w = p.es == 4 ? padded((const float*)src, (int)c, p.cols)
+                    : p.es == 2 ? padded((const uint16_t*)src, (int)c, p.cols)
+                                : padded((const int8_t*)src, (int)c, p.cols);
+    }
+    *(u32x4*)((char*)p.dst + (size_t)i * 16) = w;
+  }
+}
+
+#define HF_FINISH(SUF, E, O)                                                                     \
+  extern "C" __global__ __launch_bounds__(256) void hf_gated_finish_##SUF(                       \
+      GGemm g, GEpi e, int dup, int rows, int chunks, long long stride, long long total) {       \
+    finish_body<E, O>(g, e, dup, rows, chunks, stride, total);                                   \
+  }
+HF_FINISH(f32, float, float)
+HF_FINISH(bf16, bf16_t, bf16_t)
+HF_FINISH(codes_f32, int8_t, float)
+HF_FINISH(codes_bf16, int8_t, bf16_t)
+
+#define HF_CODES(SUF, E)                                                                         \
+  extern "C" __global__ __launch_bounds__(256) void hf_gated_pack_##SUF(                         \
+      const E* X, long long ldx, uint32_t total, int cols, uint32_t per, int8_t* codes,          \
+      long long ldc, uint8_t* scale, long long lds) {                                            \
+    pack_body<E>(X, ldx, total, cols, per, codes, ldc, scale, lds);                              \
+  }                                                                                              \
+  extern "C" __global__ __launch_bounds__(256) void hf_gated_unpack_##SUF(                       \
+      const int8_t* codes, long long ldc, const uint8_t* scale, long long lds, uint32_t rows,    \
+      int cols, E* X, long long ldx, uint32_t zrows, int zcols, uint32_t per, uint32_t total) {  \
+    unpack_body<E>(codes, ldc, scale, lds, rows, cols, X, ldx, zrows, zcols, per, total);        \
+  }                                                                                              \
+  extern "C" __global__ __launch_bounds__(256) void hf_gated_codes_##SUF(                        \
+      const E* X, long long ldx, int cols, int8_t* codes, long long ldc, int zcols,              \
+      float* scale) {                                                                            \
+    codes_body<E, 4>(X, ldx, cols, codes, ldc, zcols, scale);                                    \
+  }
+HF_CODES(f32, float)
+HF_CODES(bf16, bf16_t)
+
+extern "C" __global__ __launch_bounds__(256) void hf_gated_codes_h(const float* H, long long ldh,
+                                                                   const float* hmax, int ldmax,
+                                                                   int cols, int8_t* codes,
+                                                                   long long ldc, int zcols,
+                                                                   float* scale) {
+  const size_t row = blockIdx.x;
+  uint32_t big = 0;
+  for (int i = threadIdx.x; i < ldmax; i += 256)
+    big = max(big, __float_as_uint(hmax[row * ldmax + i]));
+  const RowScale r = row_scale(group_max<4>(big));
+  if (threadIdx.x == 0) scale[row] = r.s;
+  for (int at = 8 * (int)threadIdx.x; at < zcols; at += 2048) {
+    float v[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = 0.0f;
+    if (at < cols) get(H + row * ldh + at, v, cols - at);
+    put_row_codes(codes + row * ldc + at, v, r, cols - at, zcols - at);
+  }
+}
+
+// ------------------------------------------------------------- launchers
+#define HF_LAUNCH(NAME, K, GRID, BLOCK, ...)                                       \
+  do {                                                                             \
+    prof_begin(L, NAME);                                                           \
+    hipExtLaunchKernelGGL(K, dim3((unsigned)(GRID)), dim3(BLOCK), 0, L.stream,     \
+                          prof_a(L), prof_b(L), 0, __VA_ARGS__);                   \
+    prof_end(L, NAME, 0.0, 0.0);                                                   \
+  } while (0)
+
+void gated_pad(const Launch& L, const GPads& p) {
+  if (p.n < 1) return;
+  int c[GPADS] = {};
+  long long grid = 0;
+  for (int i = 0; i < p.n; ++i) {
+    const long long chunks = (long long)p.p[i].prows * p.p[i].times * (p.p[i].pcols * p.p[i].es / 16);
+    c[i] = (int)((chunks + 1023) / 1024);
+    grid += c[i];
+  }
+  // (the copies after the last one have no workgroups)
+  for (int i = p.n; i < GPADS; ++i) c[i] = 0;
+  HF_LAUNCH("hf_gated_pad", hf_gated_pad, grid, 256, p, c[0], c[1], c[2], c[3], c[4]);
+}
+
+void gated_finish(const Launch& L, int type, int out_type, const GGemm& g, const GEpi& e, int dup) {
+  const int halves = e.n1 < g.N ? 2 : 1;
+  const int rows = halves * e.nout, chunks = (e.mout + 7) / 8, rn = tile_n(g.tile);
+  const long long stride = (long long)((g.N + rn - 1) / rn) * rn * e.ldp;
+  const long long total = (long long)rows * chunks;
+  const long long grid = std::min<long long>((total + 255) / 256, 1 << 20);
+  if (grid < 1) return;
+  if (type == VT_I8) {
+    if (out_type == VT_F32)
+      HF_LAUNCH("hf_gated_finish", hf_gated_finish_codes_f32, grid, 256, g, e, dup, rows, chunks,
+                stride, total);
+    else
+      HF_LAUNCH("hf_gated_finish", hf_gated_finish_codes_bf16, grid, 256, g, e, dup, rows, chunks,
+                stride, total);
+  } else if (type == VT_F32) {
+    HF_LAUNCH("hf_gated_finish", hf_gated_finish_f32, grid, 256, g, e, dup, rows, chunks, stride,
+              total);
+  } else {
+    HF_LAUNCH("hf_gated_finish", hf_gated_finish_bf16, grid, 256, g, e, dup, rows, chunks, stride,
+              total);
+  }
+}
+
+void gated_pack(const Launch& L, int type, const void* X, long long ldx, long long rows, int cols,
+                int8_t* codes, long long ldc, uint8_t* scale, long long lds) {
+  const uint32_t per = (uint32_t)((cols + CODE_BLOCK - 1) / CODE_BLOCK * (CODE_BLOCK / 8));
+  const uint32_t total = (uint32_t)rows * per;      // below 2^31: 262,144 rows of 65,536
+  if (!total) return;
+  if (type == VT_F32)
+    HF_LAUNCH("hf_gated_pack", hf_gated_pack_f32, (total + 255) / 256, 256, (const float*)X, ldx,
+              total, cols, per, codes, ldc, scale, lds);
+  else
+    HF_LAUNCH("hf_gated_pack", hf_gated_pack_bf16, (total + 255) / 256, 256, (const bf16_t*)X, ldx,
+              total, cols, per, codes, ldc, scale, lds);
+}
+
+void gated_unpack(const Launch& L, int type, const int8_t* codes, long long ldc,
+                  const uint8_t* scale, long long lds, long long rows, int cols, void* X,
+                  long long ldx, long long zrows, int zcols, int times) {
+  const uint32_t per = (uint32_t)((zcols + 7) / 8);
+  const uint32_t total = (uint32_t)zrows * times * per;
+  if (!total) return;
+  if (type == VT_F32)
+    HF_LAUNCH("hf_gated_unpack", hf_gated_unpack_f32, (total + 255) / 256, 256, codes, ldc, scale,
+              lds, (uint32_t)rows, cols, (float*)X, ldx, (uint32_t)zrows, zcols, per, total);
+  else
+    HF_LAUNCH("hf_gated_unpack", hf_gated_unpack_bf16, (total + 255) / 256, 256, codes, ldc, scale,
+              lds, (uint32_t)rows, cols, (bf16_t*)X, ldx, (uint32_t)zrows, zcols, per, total);
+}
+
+void gated_codes(const Launch& L, int type, const void* X, long long ldx, long long rows, int cols,
+                 int8_t* codes, long long ldc, int zcols, float* scale) {
+  if (rows < 1) return;
+  if (type == VT_F32)
+    HF_LAUNCH("hf_gated_codes", hf_gated_codes_f32, rows, 256, (const float*)X, ldx, cols, codes,
+              ldc, zcols, scale);
+  else
+    HF_LAUNCH("hf_gated_codes", hf_gated_codes_bf16, rows, 256, (const bf16_t*)X, ldx, cols, codes,
+              ldc, zcols, scale);
+}
+
+void gated_codes_h(const Launch& L, const float* H, long long ldh, const float* hmax, int ldmax,
+                   int rows, int cols, int8_t* codes, long long ldc, int zcols, float* scale) {
+  if (rows < 1) return;
+  HF_LAUNCH("hf_gated_codes_h", hf_gated_codes_h, rows, 256, H, ldh, hmax, ldmax, cols, codes,
+            ldc, zcols, scale);
+}
+
+}  // namespace hfk

@@ -1,0 +1,102 @@
+// Eight neighbours of a row, the work of a lane in the gated block's kernels: their
+// loads and stores in every type and as the codes of a checkpoint.
+#pragma once
+
+#include "gated_act.h"
+#include "mfma_tile.h"
+
+namespace hfk {
+namespace {
+
+// 8 values to p, of any alignment, the first `have` of them, and from it
+__device__ __forceinline__ void put(float* p, const float (&v)[8], int have) {
+  if (have >= 8) {
+    put16<false>(p, __builtin_bit_cast(u32x4, f32x4{v[0], v[1], v[2], v[3]}));
+    put16<false>(p + 4, __builtin_bit_cast(u32x4, f32x4{v[4], v[5], v[6], v[7]}));
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (j < have) p[j] = v[j];
+  }
+}
+__device__ __forceinline__ void put(bf16_t* p, const float (&v)[8], int have) {
+  if (have >= 8) {
+    store_chunk<false>(p, v);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (j < have) store1(p + j, v[j]);
+  }
+}
+__device__ __forceinline__ void get(const float* p, float (&v)[8], int have) {
+  if (have >= 8) {
+    f32x4 a, b;
+    __builtin_memcpy(&a, p, 16);
+    __builtin_memcpy(&b, p + 4, 16);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      v[j] = a[j];
+      v[4 + j] = b[j];
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = j < have ? p[j] : 0.0f;
+  }
+}
+__device__ __forceinline__ void get(const bf16_t* p, float (&v)[8], int have) {
+  if (have >= 8) {
+    u32x4 w;
+    __builtin_memcpy(&w, p, 16);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      v[2 * j] = bf2f(w[j] & 0xffffu);
+      v[2 * j + 1] = bf2f(w[j] >> 16);
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = j < have ? bf2f(p[j]) : 0.0f;
+  }
+}
+// 8 codes times step
+__device__ __forceinline__ void get_codes(const int8_t* p, float step, float (&v)[8], int have) {
+  if (have >= 8) {
+    uint32_t w[2];
+    __builtin_memcpy(w, p, 8);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = (float)(int8_t)(w[j >> 2] >> (8 * (j & 3))) * step;
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = j < have ? (float)p[j] * step : 0.0f;
+  }
+}
+// 8 values of a block of 32, which 4 neighbouring lanes share, to codes: their
+// scale byte; values past `have` count 0
+__device__ __forceinline__ int put_codes(int8_t* p, const float (&v)[8], int have) {
+  // (of magnitudes as whole numbers the largest: NaN is above all, where fmaxf
+  // would lose it)
+  uint32_t big = 0;
+#pragma unroll
+  for (int j = 0; j < 8; ++j)
+    if (j < have) big = max(big, __float_as_uint(v[j]) & 0x7fffffffu);
+  big = max(big, (uint32_t)__shfl_xor((int)big, 1, 64));
+  big = max(big, (uint32_t)__shfl_xor((int)big, 2, 64));
+  const int byte = block_byte(__uint_as_float(big));
+  const float f = byte == 255 ? 0.0f : code_factor(byte);
+  uint32_t w[2] = {0u, 0u};
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const int q = byte == 255 ? 0 : (int)rintf(v[j] * f);
+    w[j >> 2] |= (uint32_t)(q & 255) << (8 * (j & 3));
+  }
+  if (have >= 8) {
+    __builtin_memcpy(p, w, 8);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (j < have) p[j] = (int8_t)(w[j >> 2] >> (8 * (j & 3)));
+  }
+  return byte;
+}
+
+}  // namespace
+}  // namespace hfk

@@ -13,14 +13,13 @@
 // A loss without its gradient keeps none, but for few rows with lists, whose
 // targets' are then read there.
 #include "hf.h"
+#include "call_context.h"
+#include "gemm_shape.h"
 #include "vocab_internal.h"
 
 #include <algorithm>
 #include <cmath>
-#include <cstdarg>
-#include <cstdio>
 #include <new>
-#include <string>
 
 using namespace hfk;
 
@@ -29,15 +28,7 @@ namespace {
 constexpr size_t MiB = (size_t)1 << 20;
 constexpr size_t KEEP_BYTES = 1536 * MiB;    // kept logits
 constexpr size_t WPACK_BYTES = 256 * MiB;    // packed rows of W
-constexpr int64_t MAX_LD = (int64_t)1 << 22; // in-tile offsets are 32 bits
 constexpr int TWO_TERM_ROWS = 128;
-// Tiles of 32 and 64 rows up to here (the statistics have an entry a tile): for
-// few columns of logits they fill the card (fp32, 299 rows, 1,360 x 1,728: 121
-// -> 50 us; 1,000 rows: 124 -> 79; no difference from 16,000 columns on).
-constexpr int FEW_ROWS = 1024;
-constexpr size_t SPLIT_FLOATS = (size_t)32 << 20;   // partials of a split-K product
-
-inline int64_t up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
 
 struct Layout {
   size_t state, pos, idx, rloss, lse, zt, tid, tdt, stat, xp, wp, z, partx, partw;
@@ -46,18 +37,11 @@ struct Layout {
 
 }  // namespace
 
-struct hf_vocab {
+struct hf_vocab : hfk::CallContext {
   int V = 0, D = 0, Dp = 0, type = 0, es = 0;
   int64_t Rmax = 0, Rws = 0;
-  hipStream_t stream = nullptr;
   char* ws = nullptr;
   Layout lay = {};
-  // The calls so far that no graph captured are on `work` (if pending), or
-  // `work` waits for them.
-  bool pending = false;
-  hipStream_t work = nullptr;
-  hipEvent_t last = nullptr;       // their end, for another stream to wait for
-  std::string err;
 
   template <class T>
   T* at(size_t off) const { return reinterpret_cast<T*>(ws + off); }
@@ -65,26 +49,6 @@ struct hf_vocab {
 };
 
 namespace {
-
-int fail(hf_vocab* c, int code, const char* fmt, ...) __attribute__((format(printf, 3, 4)));
-int fail(hf_vocab* c, int code, const char* fmt, ...) {
-  if (c) {
-    char buf[512];
-    va_list ap;
-    va_start(ap, fmt);
-    vsnprintf(buf, sizeof buf, fmt, ap);
-    va_end(ap);
-    c->err = buf;
-  }
-  return code;
-}
-
-#define HIP_TRY(ctx, expr)                                                     \
-  do {                                                                         \
-    hipError_t e_ = (expr);                                                    \
-    if (e_ != hipSuccess)                                                      \
-      return fail(ctx, HF_EHIP, "%s failed: %s", #expr, hipGetErrorString(e_)); \
-  } while (0)
 
 // ------------------------------------------------------------------ sizes
 inline int64_t tile_rows(int64_t T) { return std::max<int64_t>(up(T, VTILE), VTILE); }
@@ -190,103 +154,10 @@ int check_ready(hf_vocab* c, int64_t T) {
                 (long long)c->Rws);
   return HF_OK;
 }
-// a rows x D array of elements of es bytes, rows ld elements apart
-int check_mat(hf_vocab* c, const void* p, int64_t ld, int64_t cols, int es, int64_t rows,
-              const char* what) {
-  if (rows == 0) return HF_OK;
-  if (!p) return fail(c, HF_EINVAL, "%s is NULL", what);
-  if ((uintptr_t)p % es) return fail(c, HF_EINVAL, "%s is not aligned to its elements", what);
-  if (ld < cols || ld > ((int64_t)1 << 31))
-    return fail(c, HF_EINVAL, "rows of %s are %lld elements apart, %lld wide", what,
-                (long long)ld, (long long)cols);
-  return HF_OK;
-}
-
-// an output over an input, which is read after parts of the output are written
-int check_apart(hf_vocab* c, const void* in, const char* in_name, const void* out,
-                const char* out_name, int64_t rows) {
-  if (rows > 0 && out && in == out)
-    return fail(c, HF_EINVAL, "%s is %s: not in place", out_name, in_name);
-  return HF_OK;
-}
-
 // -------------------------------------------------------------- the passes
 int end(hf_vocab* c) {
   HIP_TRY(c, hipGetLastError());
   return HF_OK;
-}
-
-// Puts the context's stream behind the calls so far, with which it shares the
-// workspace, for a call or ahead of one.  While the stream is captured nothing
-// is done: a wait would go into the graph, and the caller orders what is
-// captured.  The first call after that, if it is not captured itself, gets
-// here with work still on the stream of before.
-int follow(hf_vocab* c, bool call) {
-  if (c->pending && c->work == c->stream) return HF_OK;
-  hipStreamCaptureStatus to = hipStreamCaptureStatusNone, from = to;
-  HIP_TRY(c, hipStreamIsCapturing(c->stream, &to));
-  if (to != hipStreamCaptureStatusNone) return HF_OK;
-  if (c->pending) {
-    HIP_TRY(c, hipStreamIsCapturing(c->work, &from));
-    if (from != hipStreamCaptureStatusNone)
-      return !call ? HF_OK
-                   : fail(c, HF_EHIP, "the stream of the calls before this one is being captured");
-    if (!c->last) HIP_TRY(c, hipEventCreateWithFlags(&c->last, hipEventDisableTiming));
-    HIP_TRY(c, hipEventRecord(c->last, c->work));
-    HIP_TRY(c, hipStreamWaitEvent(c->stream, c->last, 0));
-  }
-  c->work = c->stream;
-  c->pending = true;
-  return HF_OK;
-}
-
-// Tiles and split-K factor of a product by its estimated time, in us, the
-// longest of three and then some:
-//   products  a 256 x 256 tile has a compute unit to itself, two of the others
-//             share one; RATE: multiply-adds a us of a unit with them, measured
-//             at 8,192 x 8,192 x 2,048 (bf16) and 8,192 x 2,048 x 2,048 (fp32);
-//             filling the LDS and storing a tile take about 6 and 4 us more
-//   memory    A once at 4.7 TB/s, which takes 5.5 MB on their way: AHEAD bytes
-//             of A per workgroup (32,000 x 1,024 of bf16 for 5 rows: 18.6 us
-//             with 250 tiles of 128 x 128, 13.6 with 250 of 128 x 64), and
-//             somewhat less with fewer than two workgroups a unit
-//   L2        every tile's operands at 15 TB/s
-// Partials are written and read again, few of them in the last-level cache.
-struct Shape {
-  int tile, splits;
-  double us;
-};
-constexpr double RATE[2][4] = {{0.24e6, 0.27e6, 0.22e6, 0.21e6}, {1.78e6, 2.4e6, 1.45e6, 1.1e6}};
-constexpr double BYTES_US = 4.7e6, L2_US = 15e6;
-constexpr double AHEAD[4] = {16384, 32768, 32768, 49152};
-Shape shape_for(int type, int64_t M, int64_t N, int64_t K, bool split, bool few) {
-  Shape best = {0, 1, 1e300};
-  const int es = type == VT_F32 ? 4 : 2;
-  for (int tile = 0; tile < (few && N <= FEW_ROWS ? 4 : 2); ++tile) {
-    const int64_t RM = tile_m(tile), RN = tile_n(tile);
-    const int64_t tm = (M + RM - 1) / RM, tn = (N + RN - 1) / RN, tiles = tm * tn;
-    const int64_t slots = tile == TILE_BIG ? 256 : 512;
-    for (int s = 1; s <= VMAX_SPLITS; ++s) {
-      if (s > 1 && (!split || K / s < 256 ||
-                    (size_t)s * up(N, VTILE) * up(M, VPAD) > SPLIT_FLOATS))
-        break;
-      const int64_t rounds = (tiles * s + slots - 1) / slots;
-      // the workgroups of a unit share it; one alone does not fill it
-      const double share = tile == TILE_BIG ? 1.0 : tiles * s > 256 ? 2.0 : 1.4;
-      const double t = rounds * (share * RM * RN * (double)((K + s - 1) / s) /
-                                     RATE[type][tile] + (tile == TILE_BIG ? 6.0 : 4.0));
-      const double groups = (double)std::min(tiles * s, slots);
-      const double mem = (double)M * K * es / BYTES_US *
-                             std::max(1.0, 5.5e6 / (groups * AHEAD[tile])) *
-                             std::max(1.0, 0.85 + 0.15 * 512 / groups) + 4.0;
-      const double part = 8.0 * s * (double)M * N;
-      const double l2 = ((double)tn * M + (double)tm * N) * K * es / L2_US + 4.0;
-      const double est = std::max({t, mem, l2}) +
-                         (s > 1 ? 4.0 + part / (part < 64e6 ? 2 * BYTES_US : BYTES_US) : 0.0);
-      if (est < best.us) best = {tile, s, est};
-    }
-  }
-  return best;
 }
 
 struct Grad {

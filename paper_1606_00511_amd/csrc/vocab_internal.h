@@ -7,8 +7,9 @@
 
 namespace hfk {
 
-// Element type of the rows, the matrices and their gradients.
-enum VType { VT_F32 = 0, VT_BF16 = 1 };
+// Element type of the rows, the matrices and their gradients; codes of 8 bits in
+// the gated block's products.
+enum VType { VT_F32 = 0, VT_BF16 = 1, VT_I8 = 2 };
 
 // K blocks of the GEMMs are whole multiples of this many elements: widths are
 // padded to it in packed rows, and vocabulary pieces and row counts in delta.

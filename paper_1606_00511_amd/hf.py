@@ -35,6 +35,13 @@ TYPES = {"fp32": HF_TYPE_FP32, "bf16": HF_TYPE_BF16}
 HF_IGNORE = -100          # a masked label, token or id
 HF_VOCAB_MAX, HF_VOCAB_MAX_WIDTH = 1 << 22, 65536
 HF_VOCAB_MAX_ROWS, HF_VOCAB_MAX_TOP = 262144, 128
+# HFGated: its activations, and what a forward call keeps for the gradient
+HF_SILU, HF_GELU, HF_GELU_TANH = 3, 4, 5
+GATED_ACTS = dict(ACTS, silu=HF_SILU, gelu=HF_GELU, gelu_tanh=HF_GELU_TANH)
+HF_KEEP_NONE, HF_KEEP_FULL, HF_KEEP_CODES = 0, 1, 2
+KEEPS = {None: HF_KEEP_NONE, "full": HF_KEEP_FULL, "int8": HF_KEEP_CODES}
+HF_GATED_MAX_WIDTH, HF_GATED_MAX_ROWS, HF_GATED_MAX_OUT = 65536, 262144, 1 << 22
+HF_CODE_BLOCK = 32
 
 # Every function declared in include/hf.h.
 EXPORTS = (
@@ -50,6 +57,10 @@ EXPORTS = (
     "hf_vocab_loss_grad", "hf_vocab_distill", "hf_vocab_distill_grad",
     "hf_vocab_embed", "hf_vocab_embed_grad", "hf_vocab_check",
     "hf_vocab_last_error",
+    "hf_gated_create", "hf_gated_destroy", "hf_gated_set_stream",
+    "hf_gated_workspace_bytes", "hf_gated_set_workspace", "hf_gated_forward",
+    "hf_gated_grad", "hf_gated_pack", "hf_gated_unpack", "hf_gated_codes",
+    "hf_gated_product", "hf_gated_forward_codes", "hf_gated_last_error",
 )
 
 
@@ -180,6 +191,21 @@ def lib():
         "hf_vocab_embed_grad": (ctypes.c_int, [P, P, I64, F32, P, I64, P, I64, I32]),
         "hf_vocab_check": (ctypes.c_int, [P]),
         "hf_vocab_last_error": (ctypes.c_char_p, [P]),
+        "hf_gated_create": (ctypes.c_int, [I32, I32, I32, I32, I64, P, ctypes.POINTER(P)]),
+        "hf_gated_destroy": (ctypes.c_int, [P]),
+        "hf_gated_set_stream": (ctypes.c_int, [P, P]),
+        "hf_gated_workspace_bytes": (SZ, [P, I64]),
+        "hf_gated_set_workspace": (ctypes.c_int, [P, P, SZ]),
+        "hf_gated_forward": (ctypes.c_int, [P] + [P, I64] * 4 + [I64, P, I64, I32, P, I64, P,
+                                                                 I64]),
+        "hf_gated_grad": (ctypes.c_int, [P] + [P, I64] * 5 + [I32] + [P, I64] * 3 + [I64]
+                          + [P, I64] * 4 + [I32]),
+        "hf_gated_pack": (ctypes.c_int, [P, P, I64, I64, I64, P, I64, P, I64]),
+        "hf_gated_unpack": (ctypes.c_int, [P, P, I64, P, I64, I64, I64, P, I64]),
+        "hf_gated_codes": (ctypes.c_int, [P, P, I64, I64, I64, P, I64, P]),
+        "hf_gated_product": (ctypes.c_int, [P, P, I64, P, P, I64, P, I64, I64, I64, P, I64]),
+        "hf_gated_forward_codes": (ctypes.c_int, [P, P, I64] + [P, I64, P] * 3 + [I64, P, I64]),
+        "hf_gated_last_error": (ctypes.c_char_p, [P]),
     }
     for name, (res, args) in sig.items():
         f = getattr(L, name)
@@ -478,38 +504,17 @@ class HFNet:
         return out
 
 
-class HFVocab:
-    """A vocabulary context of the C library plus its torch-allocated
-    workspace: the token embedding, and the softmax head over a large
-    vocabulary with the loss of hard labels or of a teacher's top logits.
+class _RowContext:
+    """What HFVocab and HFGated share: a context of the C library whose calls
+    work on rows, its workspace, and the checks of tensors.  _prefix: of the C
+    calls' names."""
 
-    vocab x width: the matrices; max_rows: the most rows any call will use;
-    dtype: "fp32" or "bf16", of the rows, the matrices and their gradients;
-    ws_rows: size the workspace for calls of up to this many rows only
-    (default max_rows).  Rows may be strided (the last dimension contiguous).
-    Labels, tokens and ids are int32, HF_IGNORE where masked.  Calls run on
-    torch's current stream of the context's device; the workspace goes back to
-    torch's allocator once the work on all of them is done.  A graph that has
-    captured calls works in it at every replay: keep the object as long.
-    """
-
-    def __init__(self, vocab, width, max_rows, dtype="fp32", device="cuda",
-                 ws_rows=None):
-        import torch
-        self._torch = torch
-        self.vocab, self.width = int(vocab), int(width)
-        self.max_rows = int(max_rows)
-        self.dtype = {"fp32": torch.float32, "bf16": torch.bfloat16}[dtype]
-        L = lib()
-        h = ctypes.c_void_p()
-        rc = L.hf_vocab_create(self.vocab, self.width, TYPES[dtype], self.max_rows,
-                               None, ctypes.byref(h))
-        if rc != HF_OK:
-            raise HFError(rc, "hf_vocab_create rejected vocab=%d width=%d max_rows=%d"
-                          % (self.vocab, self.width, self.max_rows))
+    def _open(self, h, ws_rows, device):
+        """The context h's workspace for calls of ws_rows rows (None: max_rows)."""
+        torch, L = self._torch, lib()
         self._h = h
         self._stream = None               # of the last call
-        nbytes = int(L.hf_vocab_workspace_bytes(
+        nbytes = int(getattr(L, self._prefix + "_workspace_bytes")(
             h, self.max_rows if ws_rows is None else int(ws_rows)))
         if nbytes == 0:
             raise ValueError("ws_rows %s outside [1, %d]" % (ws_rows, self.max_rows))
@@ -519,12 +524,13 @@ class HFVocab:
         self.device = device
         self.workspace = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
         with torch.cuda.device(self.device):
-            self._check(L.hf_vocab_set_workspace(h, self.workspace.data_ptr(), nbytes))
+            self._check(getattr(L, self._prefix + "_set_workspace")(
+                h, self.workspace.data_ptr(), nbytes))
 
     # ------------------------------------------------------------- plumbing
     def _check(self, rc):
         if rc != HF_OK:
-            raise HFError(rc, lib().hf_vocab_last_error(self._h).decode())
+            raise HFError(rc, getattr(lib(), self._prefix + "_last_error")(self._h).decode())
         return rc
 
     def _call(self, fn, *args):
@@ -537,13 +543,13 @@ class HFVocab:
         if stream != self._stream:
             self.workspace.record_stream(current)
             self._stream = None
-            self._check(L.hf_vocab_set_stream(self._h, stream))
+            self._check(getattr(L, self._prefix + "_set_stream")(self._h, stream))
             self._stream = stream
         return self._check(getattr(L, fn)(self._h, *args))
 
     def close(self):
         if getattr(self, "_h", None) is not None:
-            lib().hf_vocab_destroy(self._h)
+            getattr(lib(), self._prefix + "_destroy")(self._h)
             self._h = None
 
     def __del__(self):
@@ -579,13 +585,47 @@ class HFVocab:
             raise ValueError("%s must be %d contiguous elements" % (what, n))
         return t.data_ptr()
 
+    def _out(self, *shape, dtype=None):
+        return self._torch.empty(*shape, dtype=dtype or self.dtype, device=self.device)
+
+
+class HFVocab(_RowContext):
+    """A vocabulary context of the C library plus its torch-allocated
+    workspace: the token embedding, and the softmax head over a large
+    vocabulary with the loss of hard labels or of a teacher's top logits.
+
+    vocab x width: the matrices; max_rows: the most rows any call will use;
+    dtype: "fp32" or "bf16", of the rows, the matrices and their gradients;
+    ws_rows: size the workspace for calls of up to this many rows only
+    (default max_rows).  Rows may be strided (the last dimension contiguous).
+    Labels, tokens and ids are int32, HF_IGNORE where masked.  Calls run on
+    torch's current stream of the context's device; the workspace goes back to
+    torch's allocator once the work on all of them is done.  A graph that has
+    captured calls works in it at every replay: keep the object as long.
+    """
+
+    _prefix = "hf_vocab"
+
+    def __init__(self, vocab, width, max_rows, dtype="fp32", device="cuda",
+                 ws_rows=None):
+        import torch
+        self._torch = torch
+        self.vocab, self.width = int(vocab), int(width)
+        self.max_rows = int(max_rows)
+        self.dtype = {"fp32": torch.float32, "bf16": torch.bfloat16}[dtype]
+        L = lib()
+        h = ctypes.c_void_p()
+        rc = L.hf_vocab_create(self.vocab, self.width, TYPES[dtype], self.max_rows,
+                               None, ctypes.byref(h))
+        if rc != HF_OK:
+            raise HFError(rc, "hf_vocab_create rejected vocab=%d width=%d max_rows=%d"
+                          % (self.vocab, self.width, self.max_rows))
+        self._open(h, ws_rows, device)
+
     def _rows(self, X, what):
         if X.dim() != 2 or X.shape[1] != self.width:
             raise ValueError("%s must be rows x %d" % (what, self.width))
         return int(X.shape[0])
-
-    def _out(self, *shape, dtype=None):
-        return self._torch.empty(*shape, dtype=dtype or self.dtype, device=self.device)
 
     def _head(self, fn, X, W, targets, T, denom, loss, row_loss, grad):
         """A head call: targets and their arguments as the C call takes them."""
@@ -685,3 +725,177 @@ class HFVocab:
         """Synchronise and raise HFError(HF_ELABEL) for a label, token or id
         outside the vocabulary seen since the last check."""
         self._call("hf_vocab_check")
+
+
+class HFGated(_RowContext):
+    """A context of the gated feed-forward block of the C library plus its
+    torch-allocated workspace: Y = (act(X Wg^T) * (X Wu^T)) Wd^T and its
+    gradients, activation checkpoints in 8 bits, and products of 8-bit codes.
+
+    width x hidden: X and Y are rows x width, Wg and Wu hidden x width, Wd width
+    x hidden; max_rows: the most rows any call will use; act: "silu", "gelu",
+    "gelu_tanh", "sigmoid", "tanh" or "relu"; dtype: "fp32" or "bf16", of the
+    rows, the matrices and their gradients; ws_rows: size the workspace for
+    calls of up to this many rows only (default max_rows).  One context serves
+    every layer of these sizes.  Rows may be strided (the last dimension
+    contiguous).  Streams, the workspace and graphs as for HFVocab.
+
+    A checkpoint in 8 bits is a pair (codes int8, scale uint8), of a rows x cols
+    matrix with a scale byte for every 32 columns; a matrix for products is a
+    pair (codes int8, scale fp32) with a scale for every row.
+    """
+
+    _prefix = "hf_gated"
+
+    def __init__(self, width, hidden, max_rows, act="silu", dtype="fp32", device="cuda",
+                 ws_rows=None):
+        import torch
+        self._torch = torch
+        self.width, self.hidden = int(width), int(hidden)
+        self.max_rows = int(max_rows)
+        self.dtype = {"fp32": torch.float32, "bf16": torch.bfloat16}[dtype]
+        h = ctypes.c_void_p()
+        rc = lib().hf_gated_create(self.width, self.hidden, GATED_ACTS[act], TYPES[dtype],
+                                   self.max_rows, None, ctypes.byref(h))
+        if rc != HF_OK:
+            raise HFError(rc, "hf_gated_create rejected width=%d hidden=%d max_rows=%d"
+                          % (self.width, self.hidden, self.max_rows))
+        self._open(h, ws_rows, device)
+
+    def _rows(self, X, what):
+        if X.dim() != 2 or X.shape[1] != self.width:
+            raise ValueError("%s must be rows x %d" % (what, self.width))
+        return int(X.shape[0])
+
+    def _weights(self, Wg, Wu, Wd, dtype=None):
+        dtype, D, F = dtype or self.dtype, self.width, self.hidden
+        return (*self._mat(Wg, F, D, dtype, "Wg"), *self._mat(Wu, F, D, dtype, "Wu"),
+                *self._mat(Wd, D, F, dtype, "Wd"))
+
+    def _blocks(self, cols):
+        return (cols + HF_CODE_BLOCK - 1) // HF_CODE_BLOCK
+
+    def _codes(self, pair, rows, cols, blocks, what):
+        """(pointer, ld, pointer, ld) of a checkpoint's codes and scale bytes."""
+        codes, scale = pair
+        return (*self._mat(codes, rows, cols, self._torch.int8, what),
+                *self._mat(scale, rows, blocks, self._torch.uint8, what + "'s scale"))
+
+    def _kept(self, keep, kept, T):
+        """(keep, pointer, ld, pointer, ld) of what a forward call keeps."""
+        F = self.hidden
+        if keep == "int8":
+            return (HF_KEEP_CODES, *self._codes(kept, T, 2 * F, 2 * self._blocks(F), "kept"))
+        return (HF_KEEP_FULL, *self._mat(kept, T, 2 * F, self.dtype, "kept"), None, 0)
+
+    # -------------------------------------------------------------- the ABI
+    def hf_gated_forward(self, X, Wg, Wu, Wd, keep=None, Y=None, kept=None):
+        """The block: (Y, kept).  keep: what its gradient will need: None
+        (nothing; kept is None), "full" (a rows x 2 hidden tensor: a row's
+        X Wg^T and then its X Wu^T) or "int8" (that as a checkpoint, with
+        2 ceil(hidden / 32) scale bytes a row)."""
+        torch, T, F = self._torch, self._rows(X, "X"), self.hidden
+        if keep not in KEEPS:
+            raise ValueError("keep is %r, none of None, 'full', 'int8'" % (keep,))
+        if keep is None and kept is not None:
+            raise ValueError("kept is given, and keep is None")
+        Y = self._out(T, self.width) if Y is None else Y
+        if keep == "full" and kept is None:
+            kept = self._out(T, 2 * F)
+        elif keep == "int8" and kept is None:
+            kept = (self._out(T, 2 * F, dtype=torch.int8),
+                    self._out(T, 2 * self._blocks(F), dtype=torch.uint8))
+        k = (HF_KEEP_NONE, None, 0, None, 0) if keep is None else self._kept(keep, kept, T)
+        self._call("hf_gated_forward", *self._mat(X, T, self.width, self.dtype, "X"),
+                   *self._weights(Wg, Wu, Wd), T,
+                   *self._mat(Y, T, self.width, self.dtype, "Y"), *k)
+        return Y, kept
+
+    def hf_gated_grad(self, X, Wg, Wu, Wd, kept, dY, dX=None, dWg=None, dWu=None, dWd=None,
+                      need_dX=True, need_dW=True, accumulate=False):
+        """Gradients of the block: (dX, dWg, dWu, dWd).  kept: what
+        hf_gated_forward kept, a tensor or a checkpoint; X: as forward had it,
+        or its checkpoint.  need_dX / need_dW False: these are not computed
+        (None, and none may be given).  accumulate: dWg, dWu and dWd += (all
+        given)."""
+        D, F = self.width, self.hidden
+        T = self._rows(dY, "dY")
+        for given, need, what in ((dX, need_dX, "dX"), (dWg, need_dW, "dW"),
+                                  (dWu, need_dW, "dW"), (dWd, need_dW, "dW")):
+            if given is not None and not need:
+                raise ValueError("%s is given, and need_%s is False" % (what, what))
+        if accumulate and (dWg is None or dWu is None or dWd is None):
+            raise ValueError("accumulate needs the dWg, dWu and dWd to add to")
+        if isinstance(X, (tuple, list)):
+            x = self._codes(X, T, D, self._blocks(D), "X")
+        else:
+            x = (*self._mat(X, T, D, self.dtype, "X"), None, 0)
+        k = self._kept("int8" if isinstance(kept, (tuple, list)) else "full", kept, T)
+        if dX is None and need_dX:
+            dX = self._out(T, D)
+        if need_dW:
+            dWg = self._out(F, D) if dWg is None else dWg
+            dWu = self._out(F, D) if dWu is None else dWu
+            dWd = self._out(D, F) if dWd is None else dWd
+        outs = []
+        for t, rows, cols, what in ((dX, T, D, "dX"), (dWg, F, D, "dWg"), (dWu, F, D, "dWu"),
+                                    (dWd, D, F, "dWd")):
+            outs += [None, 0] if t is None else self._mat(t, rows, cols, self.dtype, what)
+        self._call("hf_gated_grad", *x, *self._weights(Wg, Wu, Wd), *k,
+                   *self._mat(dY, T, D, self.dtype, "dY"), T, *outs, 1 if accumulate else 0)
+        return dX, dWg, dWu, dWd
+
+    def hf_gated_pack(self, X, codes=None, scale=None):
+        """X (any rows x cols) as a checkpoint in 8 bits: (codes, scale)."""
+        rows, cols = X.shape
+        n = self._blocks(cols)
+        codes = self._out(rows, cols, dtype=self._torch.int8) if codes is None else codes
+        scale = self._out(rows, n, dtype=self._torch.uint8) if scale is None else scale
+        self._call("hf_gated_pack", *self._mat(X, rows, cols, self.dtype, "X"), rows, cols,
+                   *self._codes((codes, scale), rows, cols, n, "codes"))
+        return codes, scale
+
+    def hf_gated_unpack(self, codes, scale, X=None):
+        """The numbers that a checkpoint stands for."""
+        rows, cols = codes.shape
+        X = self._out(rows, cols) if X is None else X
+        self._call("hf_gated_unpack",
+                   *self._codes((codes, scale), rows, cols, self._blocks(cols), "codes"),
+                   rows, cols, *self._mat(X, rows, cols, self.dtype, "X"))
+        return X
+
+    def hf_gated_codes(self, X, codes=None, scale=None):
+        """X (any rows x cols) as codes with a scale for each row, for a
+        product: (codes, scale)."""
+        torch = self._torch
+        rows, cols = X.shape
+        codes = self._out(rows, cols, dtype=torch.int8) if codes is None else codes
+        scale = self._out(rows, dtype=torch.float32) if scale is None else scale
+        self._call("hf_gated_codes", *self._mat(X, rows, cols, self.dtype, "X"), rows, cols,
+                   *self._mat(codes, rows, cols, torch.int8, "codes"),
+                   self._vec(scale, rows, torch.float32, "scale"))
+        return codes, scale
+
+    def _coded(self, codes, scale, rows, cols, what):
+        return (*self._mat(codes, rows, cols, self._torch.int8, what),
+                self._vec(scale, rows, self._torch.float32, what + "'s scale"))
+
+    def hf_gated_product(self, A, sa, B, sb, Y=None):
+        """A B^T of codes A (rows x k) and B (channels x k) with the scales sa
+        and sb of their rows."""
+        T, k = A.shape
+        n = B.shape[0]
+        Y = self._out(T, n) if Y is None else Y
+        self._call("hf_gated_product", *self._coded(A, sa, T, k, "A"),
+                   *self._coded(B, sb, n, k, "B"), T, n, k, *self._mat(Y, T, n, self.dtype, "Y"))
+        return Y
+
+    def hf_gated_forward_codes(self, X, Wg, Wu, Wd, Y=None):
+        """The block with its matrices as pairs (codes, scale) of
+        hf_gated_codes."""
+        T, D, F = self._rows(X, "X"), self.width, self.hidden
+        Y = self._out(T, D) if Y is None else Y
+        self._call("hf_gated_forward_codes", *self._mat(X, T, D, self.dtype, "X"),
+                   *self._coded(*Wg, F, D, "Wg"), *self._coded(*Wu, F, D, "Wu"),
+                   *self._coded(*Wd, D, F, "Wd"), T, *self._mat(Y, T, D, self.dtype, "Y"))
+        return Y

@@ -1,0 +1,485 @@
+"""The gated block, its gradients, 8-bit checkpoints and products of codes
+against plain forms in 64 bits, over the types, sizes, layouts and values where
+they can go wrong."""
+
+import math
+
+import pytest
+import torch
+
+from paper_1606_00511_amd import hf as H
+from tests import gated_util as G
+
+pytestmark = pytest.mark.gpu
+
+# one row and column; around the 32, 64 and 128 of blocks, tiles and few rows; odd
+# widths; more than one tile of 256; hidden below the width
+SIZES = [(1, 1, 1), (1, 64, 64), (2, 3, 5), (3, 130, 33), (17, 65, 131), (31, 128, 192),
+         (33, 64, 256), (64, 192, 96), (127, 100, 260), (128, 256, 128), (129, 192, 320),
+         (130, 72, 517), (256, 320, 704), (300, 129, 450), (700, 512, 1365)]
+ACTS = ["silu", "gelu", "gelu_tanh", "sigmoid", "tanh", "relu"]
+
+
+def net(T, D, F, type="bf16", act="silu", **kw):
+    return H.HFGated(D, F, max(1, T), act=act, dtype=type, **kw)
+
+
+# ------------------------------------------------------------------ forward
+@pytest.mark.parametrize("type", ["fp32", "bf16"])
+@pytest.mark.parametrize("T,D,F", SIZES)
+def test_forward(type, T, D, F):
+    act = ACTS[(T + D + F) % 6]
+    X, Wg, Wu, Wd, _ = G.inputs(T, D, F, G.TYPES[type], seed=T + D)
+    n = net(T, D, F, type, act)
+    Y, kept = n.hf_gated_forward(X, Wg, Wu, Wd)
+    assert kept is None
+    want = G.block(act, X, Wg, Wu, Wd)[0]
+    bound = G.block_bound(act, X, Wg, Wu, Wd, two_term=type == "bf16" and T <= 128)[0]
+    G.close(Y, want, bound, "Y")
+
+
+@pytest.mark.parametrize("type", ["fp32", "bf16"])
+@pytest.mark.parametrize("act", ACTS)
+@pytest.mark.parametrize("T", [40, 200])
+def test_activations_and_keep(type, act, T):
+    """Every activation; g and u kept in full are the products, and in 8 bits
+    their checkpoint (a number next to a border between two codes may be on its
+    other side); Y has the same bits in any case."""
+    D, F = 96, 200
+    X, Wg, Wu, Wd, _ = G.inputs(T, D, F, G.TYPES[type], seed=T)
+    X[0] *= 60                 # far out on both sides
+    n = net(T, D, F, type, act)
+    Y, _ = n.hf_gated_forward(X, Wg, Wu, Wd)
+    Yf, full = n.hf_gated_forward(X, Wg, Wu, Wd, keep="full")
+    Y8, (codes, scale) = n.hf_gated_forward(X, Wg, Wu, Wd, keep="int8")
+    assert torch.equal(Y, Yf) and torch.equal(Y, Y8)
+    want, g, u, _ = G.block(act, X, Wg, Wu, Wd)
+    by, bg, bu = G.block_bound(act, X, Wg, Wu, Wd, two_term=type == "bf16" and T <= 128)
+    G.close(Y, want, by, "Y")
+    G.close(full[:, :F], g, bg, "g")
+    G.close(full[:, F:], u, bu, "u")
+    nb = (F + 31) // 32
+    assert scale.shape == (T, 2 * nb)
+    for part, s, t, b in ((codes[:, :F], scale[:, :nb], g, bg),
+                          (codes[:, F:], scale[:, nb:], u, bu)):
+        at = torch.arange(F, device="cuda") // 32
+        step = torch.exp2(s.double() - 127)[:, at]
+        # half a step, and what the sum was off by
+        G.close(G.values(part, s), t, step / 2 + b, "kept codes")
+        wc, ws = G.pack(t)
+        assert float((ws != s).float().mean()) < 0.01
+        assert float((wc != part).float().mean()) < 0.02
+
+
+@pytest.mark.parametrize("type", ["fp32", "bf16"])
+@pytest.mark.parametrize("T,D,F", [(9, 64, 128), (200, 128, 192), (77, 61, 99)])
+def test_strided(type, T, D, F):
+    """Rows apart, at any element; what lies between them stays, in outputs and
+    in what is kept; the same numbers as of contiguous rows."""
+    X, Wg, Wu, Wd, dY = G.inputs(T, D, F, G.TYPES[type], seed=3)
+    n = net(T, D, F, type)
+    Y, kept = n.hf_gated_forward(X, Wg, Wu, Wd, keep="full")
+    _, k8 = n.hf_gated_forward(X, Wg, Wu, Wd, keep="int8")
+    g = n.hf_gated_grad(X, Wg, Wu, Wd, kept, dY)
+    xs, wg, wu, wd, dys = (G.strided(t, gap, sh)[0] for t, gap, sh in
+                           ((X, 5, 3), (Wg, 8, 8), (Wu, 1, 0), (Wd, 3, 1), (dY, 64, 64)))
+    bound = G.block_bound("silu", X, Wg, Wu, Wd, two_term=type == "bf16" and T <= 128)[0]
+    for keep, want in (("full", (kept,)), ("int8", k8)):
+        ys, ybuf = G.strided(torch.empty_like(Y))
+        ks = [G.strided(torch.empty_like(w)) for w in want]
+        views = tuple(v for v, _ in ks)
+        before = [b.clone() for b in [ybuf] + [b for _, b in ks]]
+        n.hf_gated_forward(xs, wg, wu, wd, keep=keep, Y=ys,
+                           kept=views if keep == "int8" else views[0])
+        # (sums are in the same order wherever the operands lie)
+        assert torch.equal(ys, Y) and all(torch.equal(v, w) for v, w in zip(views, want))
+        for (view, buf), old in zip([(ys, ybuf)] + ks, before):
+            mask = torch.ones_like(buf, dtype=torch.bool)
+            mask.as_strided(view.shape, view.stride(), view.storage_offset()).fill_(False)
+            assert torch.equal(buf[mask].view(torch.uint8), old[mask].view(torch.uint8))
+    G.close(Y, G.block("silu", X, Wg, Wu, Wd)[0], bound, "Y")
+    outs = [G.strided(torch.empty_like(t)) for t in g]
+    kv = G.strided(kept)[0]
+    before = [b.clone() for _, b in outs]
+    n.hf_gated_grad(xs, wg, wu, wd, kv, dys, *(v for v, _ in outs))
+    for (view, buf), old, t in zip(outs, before, g):
+        assert torch.equal(view, t)
+        mask = torch.ones_like(buf, dtype=torch.bool)
+        mask.as_strided(view.shape, view.stride(), view.storage_offset()).fill_(False)
+        assert torch.equal(buf[mask].view(torch.uint8), old[mask].view(torch.uint8))
+
+
+def test_rows_do_not_mix():
+    """NaN, infinities and huge numbers in some rows leave the others' bits."""
+    T, D, F = 150, 128, 256
+    X, Wg, Wu, Wd, dY = G.inputs(T, D, F, torch.bfloat16)
+    n = net(T, D, F)
+    Y, kept = n.hf_gated_forward(X, Wg, Wu, Wd, keep="int8")
+    bad = X.clone()
+    bad[3], bad[70, 5], bad[149] = math.nan, math.inf, 1e30
+    Yb, kb = n.hf_gated_forward(bad, Wg, Wu, Wd, keep="int8")
+    rows = torch.ones(T, dtype=torch.bool, device="cuda")
+    rows[[3, 70, 149]] = False
+    assert torch.equal(Y[rows], Yb[rows])
+    assert all(torch.equal(a[rows], b[rows]) for a, b in zip(kept, kb))
+    assert torch.isnan(Yb[3]).all() and (kb[1][3] == 255).all()
+    dX = n.hf_gated_grad(X, Wg, Wu, Wd, kept, dY, need_dW=False)[0]
+    dXb = n.hf_gated_grad(bad, Wg, Wu, Wd, kb, dY, need_dW=False)[0]
+    assert torch.equal(dX[rows], dXb[rows]) and torch.isnan(dXb[3]).all()
+
+
+# ----------------------------------------------------------------- gradients
+@pytest.mark.parametrize("type", ["fp32", "bf16"])
+@pytest.mark.parametrize("T,D,F", SIZES)
+def test_grad(type, T, D, F):
+    act = ACTS[(T + D + F + 1) % 6]
+    X, Wg, Wu, Wd, dY = G.inputs(T, D, F, G.TYPES[type], seed=T + F)
+    n = net(T, D, F, type, act)
+    _, kept = n.hf_gated_forward(X, Wg, Wu, Wd, keep="full")
+    got = n.hf_gated_grad(X, Wg, Wu, Wd, kept, dY)
+    want, bound = G.grads(act, X, Wg, Wu, Wd, kept[:, :F], kept[:, F:], dY)
+    for a, b, c, what in zip(got, want, bound, ("dX", "dWg", "dWu", "dWd")):
+        G.close(a, b, c, what)
+
+
+@pytest.mark.parametrize("type", ["fp32", "bf16"])
+@pytest.mark.parametrize("act", ACTS)
+@pytest.mark.parametrize("T,D,F", [(45, 100, 130), (192, 128, 256)])
+def test_grad_of_codes(type, act, T, D, F):
+    """From 8-bit checkpoints of g, u and X: the gradient of the numbers they
+    stand for."""
+    X, Wg, Wu, Wd, dY = G.inputs(T, D, F, G.TYPES[type], seed=T)
+    n = net(T, D, F, type, act)
+    _, kept = n.hf_gated_forward(X, Wg, Wu, Wd, keep="int8")
+    x8 = n.hf_gated_pack(X)
+    got = n.hf_gated_grad(x8, Wg, Wu, Wd, kept, dY)
+    nb = (F + 31) // 32
+    g, u = G.values(kept[0][:, :F], kept[1][:, :nb]), G.values(kept[0][:, F:], kept[1][:, nb:])
+    want, bound = G.grads(act, G.values(*x8), Wg, Wu, Wd, g, u, dY)
+    for a, b, c, what in zip(got, want, bound, ("dX", "dWg", "dWu", "dWd")):
+        G.close(a, b, c, what)
+
+
+@pytest.mark.parametrize("act", ACTS)
+def test_grad_against_differences(act):
+    """sum(dY * Y) along a direction of every input: central differences of the
+    64-bit block against the fp32 gradients.  At relu's corner no difference is
+    taken: directions are short and no product lies that near 0."""
+    T, D, F, h = 24, 40, 56, 1e-5
+    X, Wg, Wu, Wd, dY = G.inputs(T, D, F, torch.float32, seed=7)
+    n = net(T, D, F, "fp32", act)
+    _, kept = n.hf_gated_forward(X, Wg, Wu, Wd, keep="full")
+    got = n.hf_gated_grad(X, Wg, Wu, Wd, kept, dY)
+    ins = [t.double() for t in (X, Wg, Wu, Wd)]
+    value = lambda v: float((G.block(act, *v)[0] * dY.double()).sum())      # noqa: E731
+    for i in range(4):
+        d = torch.randn(ins[i].shape, generator=torch.Generator("cuda").manual_seed(i),
+                        device="cuda", dtype=torch.float64)
+        if act == "relu":
+            g = ins[0] @ ins[1].t()
+            dg = d @ ins[1].t() if i == 0 else ins[0] @ d.t() if i == 1 else 0 * g
+            assert (g.abs() > 2 * h * dg.abs()).all()
+        up, dn = list(ins), list(ins)
+        up[i], dn[i] = ins[i] + h * d, ins[i] - h * d
+        diff = (value(up) - value(dn)) / (2 * h)
+        along = float((got[i].double() * d).sum())
+        # the difference: h^2 / 6 of a third derivative and 2^-52 of the value
+        # over h; the gradients: fp32 sums of at most 2 F, T and D terms
+        size = float((got[i].double().abs() * d.abs()).sum())
+        assert abs(diff - along) <= 1e-5 * size, (i, diff, along)
+
+
+@pytest.mark.parametrize("type", ["fp32", "bf16"])
+@pytest.mark.parametrize("T", [50, 260])
+def test_need_and_accumulate(type, T):
+    D, F = 64, 136
+    X, Wg, Wu, Wd, dY = G.inputs(T, D, F, G.TYPES[type], seed=1)
+    n = net(T, D, F, type)
+    _, kept = n.hf_gated_forward(X, Wg, Wu, Wd, keep="full")
+    all_ = n.hf_gated_grad(X, Wg, Wu, Wd, kept, dY)
+    dX, *none = n.hf_gated_grad(X, Wg, Wu, Wd, kept, dY, need_dW=False)
+    assert torch.equal(dX, all_[0]) and none == [None] * 3
+    no, *dW = n.hf_gated_grad(X, Wg, Wu, Wd, kept, dY, need_dX=False)
+    assert no is None and all(torch.equal(a, b) for a, b in zip(dW, all_[1:]))
+    # accumulate: what was there, and the gradient, added before the one rounding
+    want, bound = G.grads("silu", X, Wg, Wu, Wd, kept[:, :F], kept[:, F:], dY)
+    old = [torch.randn_like(t) for t in all_[1:]]
+    new = [t.clone() for t in old]
+    dX2, *acc = n.hf_gated_grad(X, Wg, Wu, Wd, kept, dY, None, *new, accumulate=True)
+    assert torch.equal(dX2, all_[0])
+    for a, o, w, b in zip(acc, old, want[1:], bound[1:]):
+        G.close(a, w + o.double(), b + (G.U[a.dtype] + G.S) * (w + o.double()).abs()
+                + 2 * G.U[a.dtype] * b, "accumulated")
+
+
+@pytest.mark.parametrize("type", ["fp32", "bf16"])
+def test_single_matrices(type):
+    """Through the C call: each gradient alone, the others NULL."""
+    T, D, F = 70, 64, 128
+    X, Wg, Wu, Wd, dY = G.inputs(T, D, F, G.TYPES[type], seed=2)
+    n = net(T, D, F, type)
+    _, kept = n.hf_gated_forward(X, Wg, Wu, Wd, keep="full")
+    want = n.hf_gated_grad(X, Wg, Wu, Wd, kept, dY)
+    ptr = lambda t: (t.data_ptr(), t.stride(0))     # noqa: E731
+    for i in range(4):
+        out = torch.full_like(want[i], math.nan)
+        outs = [None, 0] * i + list(ptr(out)) + [None, 0] * (3 - i)
+        n._call("hf_gated_grad", *ptr(X), None, 0, *ptr(Wg), *ptr(Wu), *ptr(Wd),
+                H.HF_KEEP_FULL, *ptr(kept), None, 0, *ptr(dY), T, *outs, 0)
+        assert torch.equal(out, want[i]), i
+
+
+def test_no_rows():
+    n = net(8, 64, 96)
+    X, Wg, Wu, Wd, dY = G.inputs(0, 64, 96, torch.bfloat16)
+    Y, kept = n.hf_gated_forward(X, Wg, Wu, Wd, keep="int8")
+    assert Y.shape == (0, 64)
+    dX, *dW = n.hf_gated_grad(X, Wg, Wu, Wd, kept, dY)
+    assert dX.shape == (0, 64) and all((t == 0).all() for t in dW)
+    old = [torch.randn_like(t) for t in dW]
+    new = [t.clone() for t in old]
+    n.hf_gated_grad(X, Wg, Wu, Wd, kept, dY, None, *new, accumulate=True)
+    assert all(torch.equal(a, b) for a, b in zip(old, new))
+    assert n.hf_gated_pack(X)[0].shape == (0, 64)
+    q = [n.hf_gated_codes(w) for w in (Wg, Wu, Wd)]
+    assert n.hf_gated_forward_codes(X, *q).shape == (0, 64)
+    assert n.hf_gated_product(*n.hf_gated_codes(X), *q[0]).shape == (0, 96)
+
+
+# --------------------------------------------------------------- checkpoints
+@pytest.mark.parametrize("type", ["fp32", "bf16"])
+@pytest.mark.parametrize("R,C", [(1, 1), (3, 31), (5, 32), (7, 33), (64, 1973), (300, 4096)])
+def test_pack(type, R, C):
+    g = torch.Generator("cuda").manual_seed(R + C)
+    X = torch.randn(R, C, generator=g, device="cuda")
+    X = (X * torch.exp(3 * torch.randn(R, C, generator=g, device="cuda"))).to(G.TYPES[type])
+    n = net(1, 64, 64, type)
+    codes, scale = n.hf_gated_pack(X)
+    wc, ws = G.pack(X)
+    assert torch.equal(codes, wc) and torch.equal(scale, ws)
+    assert torch.equal(n.hf_gated_unpack(codes, scale).double(), G.values(codes, scale))
+    # strided on both sides, at odd elements
+    xs, _ = G.strided(X)
+    cs, cbuf = G.strided(codes)
+    ss, sbuf = G.strided(scale)
+    cs.fill_(1)
+    ss.fill_(1)
+    n.hf_gated_pack(xs, cs, ss)
+    assert torch.equal(cs, codes) and torch.equal(ss, scale)
+    assert int((cbuf == 77).sum()) >= cbuf.numel() - codes.numel()
+    assert (sbuf[:3] == 77).all() and (cbuf[:3] == 77).all()
+    back, bbuf = G.strided(torch.empty_like(X))
+    n.hf_gated_unpack(cs, ss, back)
+    assert torch.equal(back, n.hf_gated_unpack(codes, scale))
+    assert int(torch.isnan(bbuf).sum()) == bbuf.numel() - X.numel()
+
+
+def test_pack_edges():
+    """Zeros, ties, the block's largest next to where its code would be 128,
+    the smallest and largest numbers, and numbers that are not finite."""
+    n = net(1, 64, 64, "fp32")
+    X = torch.zeros(12, 64, device="cuda")
+    X[0, 3] = -0.0
+    X[1] = torch.arange(64, device="cuda") / 2           # ties
+    X[2, 0], X[2, 1] = 127.5, 127.0
+    X[3, 0], X[3, 1] = 127.49999, -0.5
+    X[4, 0] = 2.0 ** -149
+    X[5, :4] = torch.tensor([2.0 ** -126, 2.0 ** -130, 3 * 2.0 ** -149, -2.0 ** -127],
+                            device="cuda")
+    X[6, 40] = torch.finfo(torch.float32).max
+    X[7, 5], X[7, 40] = math.nan, 1.0
+    X[8, 63], X[8, 0] = -math.inf, 2.0
+    X[9] = 1.9921875
+    X[10] = -1.9921874
+    X[11] = torch.linspace(-1, 1, 64, device="cuda")
+    codes, scale = n.hf_gated_pack(X)
+    wc, ws = G.pack(X)
+    assert torch.equal(codes, wc) and torch.equal(scale, ws)
+    back = n.hf_gated_unpack(codes, scale)
+    assert torch.isnan(back[7, :32]).all() and back[7, 40] == 1 and back[8, 0] == 2
+    assert torch.isnan(back[8, 32:]).all()
+    ok = torch.isfinite(back)
+    assert torch.equal(back[ok].double(), G.values(codes, scale)[ok])
+    # within half a step, which is at most 2^-6.99 of the block's largest
+    off = (back - X).abs().view(12, 2, 32)
+    big = X.abs().view(12, 2, 32).amax(2, keepdim=True)
+    fine = torch.isfinite(off) & (big > 2.0 ** -119)
+    assert (off <= big * 2.0 ** -6.99)[fine].all()
+
+
+# ------------------------------------------------------------ codes, products
+@pytest.mark.parametrize("type", ["fp32", "bf16"])
+@pytest.mark.parametrize("R,C", [(1, 1), (2, 7), (9, 64), (5, 131), (40, 1000), (3, 20001)])
+def test_codes(type, R, C):
+    g = torch.Generator("cuda").manual_seed(R * C)
+    X = torch.randn(R, C, generator=g, device="cuda").to(G.TYPES[type])
+    n = net(1, 64, 64, type)
+    codes, s = n.hf_gated_codes(X)
+    wc, ws = G.row_codes(X)
+    assert torch.equal(s, ws) and torch.equal(codes, wc)
+    xs, _ = G.strided(X)
+    cs, cbuf = G.strided(codes)
+    cs.fill_(1)
+    n.hf_gated_codes(xs, cs)
+    assert torch.equal(cs, codes) and (cbuf[:3] == 77).all()
+
+
+def test_codes_edges():
+    n = net(1, 64, 64, "fp32")
+    X = torch.zeros(10, 100, device="cuda")
+    X[1] = (torch.arange(100, device="cuda") - 50) * 0.5
+    X[1, 0] = 127.0                                  # s = 1: ties to even
+    X[2, 4] = torch.finfo(torch.float32).max
+    X[3, 4], X[3, 5] = math.nan, 1.0
+    X[4, 4] = -math.inf
+    X[5, 0], X[5, 1] = 1e-36, 0.3e-36
+    X[6, 0], X[6, 1] = 2.0 ** -120, -2.0 ** -122
+    X[7] = torch.randn(100, device="cuda") * 1e-30
+    X[8] = 127.0 * 3.0
+    X[9] = (torch.arange(100, device="cuda") + 0.5) * 0.3
+    X[9, 99] = 127 * 0.3
+    codes, s = n.hf_gated_codes(X)
+    wc, ws = G.row_codes(X)
+    assert torch.equal(s.nan_to_num(-1), ws.nan_to_num(-1)) and torch.equal(codes, wc)
+    assert torch.isnan(s[3]) and torch.isnan(s[4]) and s[0] == 0
+
+
+@pytest.mark.parametrize("type", ["fp32", "bf16"])
+@pytest.mark.parametrize("T,N,K", [(1, 1, 1), (1, 1000, 128), (3, 5, 130), (16, 77, 64),
+                                   (33, 300, 256), (129, 257, 1000), (260, 640, 512),
+                                   (5, 40000, 200)])
+def test_product(type, T, N, K):
+    g = torch.Generator("cuda").manual_seed(T + N + K)
+    r = lambda *s: torch.randint(-127, 128, s, generator=g, device="cuda").to(torch.int8)   # noqa: E731
+    A, B = r(T, K), r(N, K)
+    A[0] = 127
+    B[0] = -127
+    sa = torch.rand(T, generator=g, device="cuda") + 0.1
+    sb = torch.rand(N, generator=g, device="cuda") + 0.1
+    n = net(T, K, 64, type)
+    Y = n.hf_gated_product(A, sa, B, sb)
+    sums = A.double() @ B.double().t()
+    want = sums * (sa.double()[:, None] * sb.double())
+    # the sum to fp32, the product of the scales, and theirs: three roundings, and
+    # that to the type
+    G.close(Y, want, (3.01 * G.S + G.U[Y.dtype] * (1 + 4 * G.S)) * want.abs() + 1e-300, "Y")
+    As, Bs = G.strided(A, 7, 1)[0], G.strided(B, 16, 16)[0]
+    ys, buf = G.strided(torch.empty_like(Y))
+    n.hf_gated_product(As, sa, Bs, sb, ys)
+    assert torch.equal(ys, Y) and int(torch.isnan(buf).sum()) == buf.numel() - Y.numel()
+
+
+def test_product_largest_sum():
+    """Codes of -128 too, and sums near 2^30."""
+    K = 65536
+    n = net(2, K, 64, "fp32")
+    A = torch.full((2, K), -128, dtype=torch.int8, device="cuda")
+    B = torch.full((3, K), -128, dtype=torch.int8, device="cuda")
+    B[1] = 127
+    one = torch.ones(3, device="cuda")
+    Y = n.hf_gated_product(A, one[:2], B, one)
+    want = torch.tensor([128 * 128 * K, -128 * 127 * K, 128 * 128 * K], device="cuda").double()
+    G.close(Y, want.expand(2, 3), G.S * want.abs().expand(2, 3), "Y")
+
+
+@pytest.mark.parametrize("type", ["fp32", "bf16"])
+@pytest.mark.parametrize("T,D,F", [(1, 64, 64), (4, 33, 75), (24, 128, 512), (200, 256, 384),
+                                   (300, 130, 515)])
+def test_forward_codes(type, T, D, F):
+    act = ACTS[(T + D) % 6]
+    dt = G.TYPES[type]
+    X, Wg, Wu, Wd, _ = G.inputs(T, D, F, dt, seed=T)
+    n = net(T, D, F, type, act)
+    q = [n.hf_gated_codes(w) for w in (Wg, Wu, Wd)]
+    Y = n.hf_gated_forward_codes(X, *q)
+    qx, sx = G.row_codes(X)
+    times = lambda a, sa, m: (a.double() @ m[0].double().t()) * (   # noqa: E731
+        sa.double()[:, None] * m[1].double())
+    g, u = times(qx, sx, q[0]), times(qx, sx, q[1])
+    Hh = G.act(act, g) * u
+    sh = (Hh.abs().amax(1).float().double() / 127).float().double()
+    steps = Hh / sh[:, None]
+    want = times(steps.round(), sh, q[2])
+    # h in fp32 is off by at most `off` of it (g and u 4 roundings each, the
+    # activation, the product); a code changes where that crosses a border: by one
+    # step.  A scale off by a rounding: 2^-23 of the row.
+    off = G.SLOPE * 4 * G.S * g.abs() * u.abs() + 8 * G.S * (g.abs() + 1) * u.abs() \
+        + 8 * G.S * Hh.abs()
+    off = off / sh[:, None] + 4 * G.S * steps.abs()
+    near = ((steps - steps.floor() - 0.5).abs() <= off).double()
+    w = (q[2][0].double() * q[2][1].double()[:, None]).abs()
+    bound = (near * sh[:, None]) @ w.t() + 8 * G.S * (steps.abs() * sh[:, None]) @ w.t()
+    G.close(Y, want, bound + G.U[dt] * (want.abs() + bound), "Y")
+
+
+# -------------------------------------------------- sizes, streams and graphs
+@pytest.mark.parametrize("type", ["fp32", "bf16"])
+def test_workspace_of_fewer_rows(type):
+    D, F = 64, 128
+    n = H.HFGated(D, F, 500, dtype=type, ws_rows=200)
+    big = H.HFGated(D, F, 500, dtype=type)
+    X, Wg, Wu, Wd, _ = G.inputs(200, D, F, G.TYPES[type])
+    assert torch.equal(n.hf_gated_forward(X, Wg, Wu, Wd)[0], big.hf_gated_forward(X, Wg, Wu, Wd)[0])
+    X = G.inputs(400, D, F, G.TYPES[type])[0]
+    with pytest.raises(H.HFError) as e:
+        n.hf_gated_forward(X, Wg, Wu, Wd)
+    assert e.value.code == H.HF_EWORKSPACE
+
+
+def test_streams():
+    """Calls on two streams in turn share the workspace in order."""
+    T, D, F = 600, 256, 512
+    n = net(T, D, F)
+    sets = [G.inputs(T, D, F, torch.bfloat16, seed=s) for s in range(2)]
+    want = [n.hf_gated_forward(*s[:4])[0] for s in sets]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    got = []
+    for i in range(8):
+        with torch.cuda.stream(streams[i % 2]):
+            got.append(n.hf_gated_forward(*sets[i % 2][:4])[0])
+    torch.cuda.synchronize()
+    assert all(torch.equal(y, want[i % 2]) for i, y in enumerate(got))
+
+
+@pytest.mark.parametrize("type,T", [("bf16", 5), ("bf16", 300), ("fp32", 70)])
+def test_graph(type, T):
+    """A captured training step (forward, gradients) and a captured serving step,
+    replayed with other inputs, eager calls of the same context between."""
+    D, F = 128, 320
+    dt = G.TYPES[type]
+    n = net(T, D, F, type)
+    X, Wg, Wu, Wd, dY = G.inputs(T, D, F, dt)
+    q = [n.hf_gated_codes(w) for w in (Wg, Wu, Wd)]
+
+    def step(X, dY):
+        Y, kept = n.hf_gated_forward(X, Wg, Wu, Wd, keep="int8")
+        g = n.hf_gated_grad(n.hf_gated_pack(X), Wg, Wu, Wd, kept, dY)
+        return (Y, *kept, *g, n.hf_gated_forward_codes(X, *q))
+    step(X, dY)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = step(X, dY)
+    for seed in range(1, 4):
+        x2, *_, dy2 = G.inputs(T, D, F, dt, seed=seed)
+        want = [t.clone() for t in step(x2, dy2)]
+        torch.cuda.synchronize()
+        X.copy_(x2)
+        dY.copy_(dy2)
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(out, want):
+            assert torch.equal(a, b)
+
+
+def test_same_bits_again():
+    T, D, F = 333, 200, 600
+    n = net(T, D, F)
+    X, Wg, Wu, Wd, dY = G.inputs(T, D, F, torch.bfloat16)
+    Y, kept = n.hf_gated_forward(X, Wg, Wu, Wd, keep="full")
+    g = n.hf_gated_grad(X, Wg, Wu, Wd, kept, dY)
+    for _ in range(3):
+        assert torch.equal(n.hf_gated_forward(X, Wg, Wu, Wd)[0], Y)
+        assert all(torch.equal(a, b) for a, b in
+                   zip(n.hf_gated_grad(X, Wg, Wu, Wd, kept, dY), g))

@@ -3,6 +3,8 @@
 // erfc and a sigmoid, so that values far below 0 keep their digits.
 #pragma once
 
+#include <type_traits>
+
 #include "gated_internal.h"
 
 namespace hfk {
@@ -14,54 +16,56 @@ __device__ __forceinline__ float sigmoid_of(float z) {
   if constexpr (EXACT) return 1.0f / (1.0f + expf(-z));
   else return __builtin_amdgcn_rcpf(1.0f + __expf(-z));
 }
-template <bool EXACT>
-__device__ __forceinline__ float act_of(int act, float z) {
-  switch (act) {
-    case GA_SIGMOID: return sigmoid_of<EXACT>(z);
-    case GA_TANH: return tanhf(z);
-    case GA_RELU: return z <= 0.0f ? 0.0f : z;        // (NaN stays)
-    case GA_SILU: return z * sigmoid_of<EXACT>(z);
-    case GA_GELU: return 0.5f * z * erfcf(-0.70710678f * z);
-    default: {
-      const float z2 = fminf(z * z, 1e4f);       // (finite; the sigmoid is 0 or 1 by then)
-      return z * sigmoid_of<EXACT>(1.59576912f * z * (1.0f + 0.044715f * z2));
-    }
+// phi(z), ACT one of GA_*
+template <int ACT, bool EXACT>
+__device__ __forceinline__ float act_of(float z) {
+  if constexpr (ACT == GA_SIGMOID) return sigmoid_of<EXACT>(z);
+  if constexpr (ACT == GA_TANH) return tanhf(z);
+  if constexpr (ACT == GA_RELU) return z <= 0.0f ? 0.0f : z;        // (NaN stays)
+  if constexpr (ACT == GA_SILU) return z * sigmoid_of<EXACT>(z);
+  if constexpr (ACT == GA_GELU) return 0.5f * z * erfcf(-0.70710678f * z);
+  // 1.5957...: 2 sqrt(2 / pi); z^2 stays finite (the sigmoid is 0 or 1 by 1e4)
+  return z * sigmoid_of<EXACT>(1.59576912f * z * (1.0f + 0.044715f * fminf(z * z, 1e4f)));
+}
+// and its slope
+template <int ACT, bool EXACT>
+__device__ __forceinline__ void act_and_slope(float z, float& a, float& d) {
+  if constexpr (ACT == GA_SIGMOID) {
+    a = sigmoid_of<EXACT>(z);
+    d = a * (1.0f - a);
+  } else if constexpr (ACT == GA_TANH) {
+    a = tanhf(z);
+    d = 1.0f - a * a;
+  } else if constexpr (ACT == GA_RELU) {
+    a = z <= 0.0f ? 0.0f : z;
+    d = z > 0.0f ? 1.0f : 0.0f;
+  } else if constexpr (ACT == GA_SILU) {
+    const float p = sigmoid_of<EXACT>(z);
+    a = z * p;
+    d = p + a * (1.0f - p);
+  } else if constexpr (ACT == GA_GELU) {
+    const float p = 0.5f * erfcf(-0.70710678f * z);
+    const float q = -0.5f * z * z;
+    a = z * p;
+    d = p + z * 0.39894228f * (EXACT ? expf(q) : __expf(q));     // 1 / sqrt(2 pi)
+  } else {
+    const float z2 = fminf(z * z, 1e4f);
+    const float p = sigmoid_of<EXACT>(1.59576912f * z * (1.0f + 0.044715f * z2));
+    a = z * p;
+    d = p + a * (1.0f - p) * 1.59576912f * (1.0f + 0.134145f * z2);
   }
 }
-template <bool EXACT>
-__device__ __forceinline__ void act_and_slope(int act, float z, float& a, float& d) {
+// f with the activation as a constant: what f does for many values is compiled
+// for each activation, with no branch between the values
+template <class Fn>
+__device__ __forceinline__ void with_act(int act, Fn f) {
   switch (act) {
-    case GA_SIGMOID:
-      a = sigmoid_of<EXACT>(z);
-      d = a * (1.0f - a);
-      break;
-    case GA_TANH:
-      a = tanhf(z);
-      d = 1.0f - a * a;
-      break;
-    case GA_RELU:
-      a = z <= 0.0f ? 0.0f : z;
-      d = z > 0.0f ? 1.0f : 0.0f;
-      break;
-    case GA_SILU: {
-      const float p = sigmoid_of<EXACT>(z);
-      a = z * p;
-      d = p + a * (1.0f - p);
-      break;
-    }
-    case GA_GELU: {
-      const float p = 0.5f * erfcf(-0.70710678f * z);
-      const float q = -0.5f * z * z;
-      a = z * p;
-      d = p + z * 0.39894228f * (EXACT ? expf(q) : __expf(q));     // 1 / sqrt(2 pi)
-      break;
-    }
-    default: {
-      const float z2 = fminf(z * z, 1e4f);       // 1.5957...: 2 sqrt(2 / pi)
-      const float p = sigmoid_of<EXACT>(1.59576912f * z * (1.0f + 0.044715f * z2));
-      a = z * p;
-      d = p + a * (1.0f - p) * 1.59576912f * (1.0f + 0.134145f * z2);
-    }
+    case GA_SIGMOID: f(std::integral_constant<int, GA_SIGMOID>()); break;
+    case GA_TANH: f(std::integral_constant<int, GA_TANH>()); break;
+    case GA_RELU: f(std::integral_constant<int, GA_RELU>()); break;
+    case GA_SILU: f(std::integral_constant<int, GA_SILU>()); break;
+    case GA_GELU: f(std::integral_constant<int, GA_GELU>()); break;
+    default: f(std::integral_constant<int, GA_GELU_TANH>());
   }
 }
 

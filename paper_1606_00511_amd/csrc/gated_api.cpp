@@ -78,7 +78,7 @@ void plan(const hf_gated* c, int64_t R, Layout* l) {
   l->xq = take(r * Dc);
   l->sx = take(r * 4);
   l->hf = take(r * Fc * 4);
-  l->hmax = take(r * (Fp / 32) * 4);
+  l->hmax = take(std::max(r * (Fp / 32), std::min<size_t>(r, FEW_X) * (Fp / 16)) * 4);
   l->hq = take(r * Fc);
   l->sh = take(r * 4);
   off = start;
@@ -160,6 +160,14 @@ GGemm product(int M, int N, int K) {
   g.ktail = INT_MAX;
   g.splits = 1;
   return g;
+}
+// operands that are read where they are
+void operands(GGemm* g, const void* A, const void* A1, int64_t lda, const void* B, int64_t ldb) {
+  g->A = A;
+  g->A1 = A1;
+  g->lda = lda;
+  g->B = B;
+  g->ldb = ldb;
 }
 void set_shape(GGemm* g, int type, bool split) {
   const Shape s = shape_for(type, g->M, g->N, g->K, split, false);
@@ -295,6 +303,19 @@ int hf_gated_forward(hf_gated* c, const void* X, int64_t ldx, const void* Wg, in
   const Launch L{c->stream, nullptr};
   const Layout& l = c->lay;
   const int T = (int)rows, D = c->D, F = c->F, Dp = c->Dp, Fp = c->Fp, es = c->es;
+  if (T <= FEW_X && keep == HF_KEEP_NONE && ldg == ldu) {
+    GGemm gu = product(F, T, D), gd = product(D, T, F);
+    GEpi eu = epilogue(c, T), ed = epilogue(c, T);
+    operands(&gu, Wg, Wu, ldg, X, ldx);
+    eu.h = c->at<void>(l.h);
+    eu.ldh = Fp;
+    eu.dup = ed.dup = T <= TWO_X ? TWO_X : 0;
+    gated_few_up(L, c->type, gu, eu);
+    operands(&gd, Wd, nullptr, ldd, eu.h, Fp);
+    set_out(&ed, Y, ldy, T, D);
+    gated_few_down(L, c->type, c->type, gd, ed);
+    return end(c);
+  }
   const int dup = two_term(c, T);
 
   GGemm gu = product(2 * Fp, T, Dp), gd = product(Dp, dup ? 2 * dup : T, Fp);
@@ -531,6 +552,16 @@ int hf_gated_product(hf_gated* c, const int8_t* A, int64_t lda, const float* sa,
   const Launch L{c->stream, nullptr};
   const Layout& l = c->lay;
   const int T = (int)rows, K = (int)up(k, CPAD);
+  if (T <= FEW_X) {
+    GGemm g = product((int)n, T, (int)k);
+    GEpi e = epilogue(c, T);
+    operands(&g, B, nullptr, ldb, A, lda);
+    e.sn = sa;
+    e.sm = sb;
+    set_out(&e, Y, ldy, T, (int)n);
+    gated_few_down(L, VT_I8, c->type, g, e);
+    return end(c);
+  }
   const bool place = k % CPAD == 0 && loads16(B, ldb, 1);
   // channels at a time: all where they are, or as many as are packed; tiles of
   // partials go by columns of 64
@@ -579,41 +610,56 @@ int hf_gated_forward_codes(hf_gated* c, const void* X, int64_t ldx, const int8_t
   const Launch L{c->stream, nullptr};
   const Layout& l = c->lay;
   const int T = (int)rows, D = c->D, F = c->F, Dc = c->Dc, Fc = c->Fc, Fp = c->Fp;
-  GGemm gu = product(2 * Fp, T, Dc), gd = product(c->Dp, T, Fc);
-  GEpi eu = epilogue(c, T), ed = epilogue(c, T);
-  Pads pads;
-  const bool pair = D == Dc && ldg == ldu && loads16(Wg, ldg, 1) && loads16(Wu, ldu, 1);
-  gu.A = pads.operand(pair, Wg, ldg, F, D, 1, c->at<void>(l.wg), F, Dc, 1, &gu.lda);
-  gu.A1 = pads.operand(pair, Wu, ldu, F, D, 1, c->at<void>(l.wu), F, Dc, 1, &gu.lda);
-  gu.alim = F;
-  gd.A = pads.operand(F == Fc && loads16(Wd, ldd, 1), Wd, ldd, D, F, 1, c->at<void>(l.wd), D, Fc, 1,
-                      &gd.lda);
-  gd.alim = D;
-  gated_pad(L, pads.all);
   int8_t* xq = c->at<int8_t>(l.xq);
   int8_t* hq = c->at<int8_t>(l.hq);
   float *sx = c->at<float>(l.sx), *sh = c->at<float>(l.sh);
+  const bool few = T <= FEW_X && ldg == ldu;
+  GGemm gu = few ? product(F, T, D) : product(2 * Fp, T, Dc);
+  GGemm gd = few ? product(D, T, F) : product(c->Dp, T, Fc);
+  GEpi eu = epilogue(c, T), ed = epilogue(c, T);
+  if (few) {
+    operands(&gu, Wg, Wu, ldg, xq, Dc);
+    operands(&gd, Wd, nullptr, ldd, hq, Fc);
+  } else {
+    Pads pads;
+    const bool pair = D == Dc && ldg == ldu && loads16(Wg, ldg, 1) && loads16(Wu, ldu, 1);
+    gu.A = pads.operand(pair, Wg, ldg, F, D, 1, c->at<void>(l.wg), F, Dc, 1, &gu.lda);
+    gu.A1 = pads.operand(pair, Wu, ldu, F, D, 1, c->at<void>(l.wu), F, Dc, 1, &gu.lda);
+    gu.alim = F;
+    gu.B = xq;
+    gu.ldb = Dc;
+    gd.A = pads.operand(F == Fc && loads16(Wd, ldd, 1), Wd, ldd, D, F, 1, c->at<void>(l.wd), D, Fc,
+                        1, &gd.lda);
+    gd.alim = D;
+    gd.B = hq;
+    gd.ldb = Fc;
+    gated_pad(L, pads.all);
+  }
   gated_codes(L, c->type, X, ldx, T, D, xq, Dc, Dc, sx);
-  gu.B = xq;
-  gu.ldb = Dc;
   eu.sn = sx;
   eu.sm = sg;
   eu.sm1 = su;
   eu.h = c->at<float>(l.hf);
   eu.ldh = Fc;
   eu.hmax = c->at<float>(l.hmax);
-  eu.ldmax = Fp / 32;
-  set_shape(&gu, VT_I8, false);
-  gated_up(L, VT_I8, gu, eu);
+  eu.ldmax = few ? (F + 15) / 16 : Fp / 32;
+  if (few) {
+    gated_few_up(L, VT_I8, gu, eu);
+  } else {
+    set_shape(&gu, VT_I8, false);
+    gated_up(L, VT_I8, gu, eu);
+  }
   gated_codes_h(L, c->at<float>(l.hf), Fc, eu.hmax, eu.ldmax, T, F, hq, Fc, Fc, sh);
-  gd.B = hq;
-  gd.ldb = Fc;
   ed.sn = sh;
   ed.sm = sd;
   set_out(&ed, Y, ldy, T, D);
-  summed(c, L, VT_I8, c->type, &gd, &ed, 0, [&](const GGemm& g, const GEpi& e) {
-    gated_down(L, VT_I8, c->type, g, e);
-  });
+  if (few) {
+    gated_few_down(L, VT_I8, c->type, gd, ed);
+  } else {
+    summed(c, L, VT_I8, c->type, &gd, &ed, 0, [&](const GGemm& g, const GEpi& e) {
+      gated_down(L, VT_I8, c->type, g, e);
+    });
+  }
   return end(c);
 }
 

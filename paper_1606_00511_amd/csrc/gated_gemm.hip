@@ -1,376 +1,60 @@
-// The products of the gated feed-forward block (T rows, width D, hidden F):
-//   up    g = X Wg^T, u = X Wu^T and h = phi(g) u, which leaves the tile; g and
-//         u only where they are kept for the gradient
-//   down  Y = h Wd^T
-//   dh    dh = dY Wd, which stays in the tile: h, dg = dh u phi'(g) and
-//         du = dh phi(g) leave it
-//   dx    dX = dg Wg + du Wu, one product of 2 F
-//   dw    dWd = dY^T h, and dWg = dg^T X with dWu = du^T X as one product
-// 2 T D F operations for each of the three matrices forward and four times that
-// backward: bound by the matrix cores, and for few rows by reading the matrices.
-//
-// A tile of "up" takes its rows m from both matrices, 32 of Wg and the same 32 of
-// Wu in turn: a wave then has g and u of the same features in neighbouring blocks
-// of its accumulators, and neither goes through memory.
-// Sums are fp32 (codes: int32, exact), the activation and its slope fp32; h, dg
-// and du are rounded to the type for the products that read them (few bf16
-// rows: to two terms of it, as few rows average no rounding away).
-#include "gated_act.h"
-#include "gated_values.h"
-#include "mfma_tile.h"
+// The products of the gated block without an activation, and the launches of all.
+#include "gated_gemm.h"
 
 namespace hfk {
-namespace {
 
-enum { UP, DOWN, DH, DX, DW };
-
-// h, dg or du to the workspace, where whole chunks are aligned; dup: the rest of
-// the rounding too
-__device__ __forceinline__ void put_term(float* p, const float (&v)[8], long long) {
-  *(f32x4*)p = f32x4{v[0], v[1], v[2], v[3]};
-  *(f32x4*)(p + 4) = f32x4{v[4], v[5], v[6], v[7]};
-}
-__device__ __forceinline__ void put_term(bf16_t* p, const float (&v)[8], long long rest) {
-  uint32_t b[8];
-#pragma unroll
-  for (int j = 0; j < 8; ++j) b[j] = f2bf(v[j]);
-  *(u32x4*)p = u32x4{b[0] | b[1] << 16, b[2] | b[3] << 16, b[4] | b[5] << 16, b[6] | b[7] << 16};
-  if (!rest) return;
-#pragma unroll
-  for (int j = 0; j < 8; ++j) b[j] = f2bf(v[j] - bf2f(b[j]));
-  *(u32x4*)(p + rest) =
-      u32x4{b[0] | b[1] << 16, b[2] | b[3] << 16, b[4] | b[5] << 16, b[6] | b[7] << 16};
-}
-
-// 8 numbers of row r of a wave's staged part, from its chunk c of 4 on
-template <int RL>
-__device__ __forceinline__ void staged8(const float* s, int r, int c, float (&v)[8]) {
-#pragma unroll
-  for (int k = 0; k < 2; ++k) {
-    const f32x4 w = *(const f32x4*)(s + r * RL + 4 * ((c + k) ^ (r & (RL / 4 - 1))));
-#pragma unroll
-    for (int j = 0; j < 4; ++j) v[4 * k + j] = w[j];
-  }
-}
-
-// rows n0 .. n0 + 31 of "up": WM / 2 blocks of 32 features from f0, g and u in
-// turn in the staged columns
-template <class E, int WM>
-__device__ __forceinline__ void up_part(const float* s, int lane, const GEpi& e, int n0, int f0) {
-  constexpr int RL = 32 * WM, FC = 2 * WM;       // lanes a row, 8 features each
-  constexpr bool I8 = sizeof(E) == 1;
-#pragma unroll 2
-  for (int i = 0; i < FC / 2; ++i) {
-    const int r = (lane + 64 * i) / FC, fc = (lane + 64 * i) % FC;
-    const int n = n0 + r, f = f0 + 8 * fc, c = 16 * (fc / 4) + 2 * (fc % 4);
-    const int have = e.F - f;                    // < 8: the last of them
-    if (f >= e.Fp || n >= e.T) continue;         // (the same in the lanes of a block)
-    float g[8], u[8], hv[8];
-    staged8<RL>(s, r, c, g);
-    staged8<RL>(s, r, c + 8, u);
-    if constexpr (I8) {
-      const float sn = e.sn[n];
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const int m = min(f + j, e.F - 1);
-        g[j] = (float)__float_as_int(g[j]) * (sn * e.sm[m]);
-        u[j] = (float)__float_as_int(u[j]) * (sn * e.sm1[m]);
-      }
-    }
-#pragma unroll
-    for (int j = 0; j < 8; ++j)
-      hv[j] = j < have ? act_of<sizeof(E) != 2>(e.act, g[j]) * u[j] : 0.0f;
-    if constexpr (I8) {
-      put_term((float*)e.h + (size_t)n * e.ldh + f, hv, 0);
-      uint32_t big = 0;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) big = max(big, __float_as_uint(hv[j]) & 0x7fffffffu);
-      big = max(big, (uint32_t)__shfl_xor((int)big, 1, 64));
-      big = max(big, (uint32_t)__shfl_xor((int)big, 2, 64));
-      if (fc % 4 == 0) e.hmax[(size_t)n * e.ldmax + f / 32] = __uint_as_float(big);
-    } else {
-      put_term((E*)e.h + (size_t)n * e.ldh + f, hv, e.dup * e.ldh);
-      if (e.keep == KEEP_FULL) {
-        E* p = (E*)e.kept + (size_t)n * e.ldk + f;
-        put(p, g, have);
-        put(p + e.F, u, have);
-      } else if (e.keep == KEEP_CODES) {
-        int8_t* p = (int8_t*)e.kept + (size_t)n * e.ldk + f;
-        uint8_t* ks = e.ks + (size_t)n * e.ldks + f / CODE_BLOCK;
-        const int bg = put_codes(p, g, have), bu = put_codes(p + e.F, u, have);
-        if (fc % 4 == 0 && have > 0) {
-          ks[0] = (uint8_t)bg;
-          ks[(e.F + CODE_BLOCK - 1) / CODE_BLOCK] = (uint8_t)bu;
-        }
-      }
-    }
-  }
-}
-
-// rows n0 .. n0 + 31 of "dh": 32 WM features from f0
-template <class E, int WM>
-__device__ __forceinline__ void dh_part(const float* s, int lane, const GEpi& e, int n0, int f0,
-                                        int Np) {
-  constexpr int RL = 32 * WM, FC = 4 * WM;
-#pragma unroll 2
-  for (int i = 0; i < FC / 2; ++i) {
-    const int r = (lane + 64 * i) / FC, fc = (lane + 64 * i) % FC;
-    const int n = n0 + r, f = f0 + 8 * fc;
-    if (f >= e.Fp || n >= Np) continue;
-    const int have = n < e.T ? e.F - f : 0;
-    float d[8], g[8], u[8], hv[8];
-    staged8<RL>(s, r, 2 * fc, d);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) g[j] = u[j] = 0.0f;
-    if (have > 0) {
-      if (e.keep == KEEP_FULL) {
-        const E* p = (const E*)e.kept + (size_t)n * e.ldk + f;
-        get(p, g, have);
-        get(p + e.F, u, have);
-      } else {
-        const int8_t* p = (const int8_t*)e.kept + (size_t)n * e.ldk + f;
-        const uint8_t* ks = e.ks + (size_t)n * e.ldks + f / CODE_BLOCK;
-        get_codes(p, code_step(ks[0]), g, have);
-        get_codes(p + e.F, code_step(ks[(e.F + CODE_BLOCK - 1) / CODE_BLOCK]), u, have);
-      }
-    }
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      float a, sl;
-      act_and_slope<sizeof(E) == 4>(e.act, g[j], a, sl);
-      hv[j] = j < have ? a * u[j] : 0.0f;
-      g[j] = j < have ? d[j] * u[j] * sl : 0.0f;
-      u[j] = j < have ? d[j] * a : 0.0f;
-    }
-    put_term((E*)e.h + (size_t)n * e.ldh + f, hv, e.dup * e.ldh);
-    E* q = (E*)e.dgu + (size_t)n * e.lddgu + f;
-    put_term(q, g, e.dup * e.lddgu);
-    put_term(q + e.Fp, u, e.dup * e.lddgu);
-  }
-}
-
-// rows n0 .. n0 + 31 of a product of codes, scaled
-template <class O, int RL>
-__device__ __forceinline__ void scaled_part(const float* s, int lane, const GEpi& e, int n0, int m0) {
-  constexpr int CPR = RL / 8;
-#pragma unroll
-  for (int i = 0; i < CPR / 2; ++i) {
-    const int r = (lane + 64 * i) / CPR, c = (lane + 64 * i) % CPR;
-    const int n = n0 + r, m = m0 + 8 * c, have = e.mout - m;
-    if (n >= e.nout || have <= 0) continue;
-    float v[8];
-    staged8<RL>(s, r, 2 * c, v);
-    const float sn = e.sn[n];
-#pragma unroll
-    for (int j = 0; j < 8; ++j)
-      v[j] = (float)__float_as_int(v[j]) * (sn * e.sm[min(m + j, e.mout - 1)]);
-    put((O*)e.out + (size_t)n * e.ldo + m, v, have);
-  }
-}
-
-// E: the operands' type, O: the output's
-template <class E, class O, int MODE, int WM, int WN, int GM, int GN, int S>
-__device__ __forceinline__ void ggemm_body(const GGemm& s, const GEpi& e) {
-  constexpr bool AKC = MODE == UP || MODE == DOWN, BKC = MODE != DW;
-  constexpr int BK = 128 / (int)sizeof(E);
-  constexpr int NW = GM * GN;
-  constexpr int RM = 32 * WM * GM, RN = 32 * WN * GN;
-  using TA = Tile<E, AKC, RM, BK, NW>;
-  using TB = Tile<E, BKC, RN, BK, NW>;
-  constexpr int EPC = TA::EPC;
-  constexpr int STAGE = TA::SIZE + TB::SIZE;
-  __shared__ __attribute__((aligned(16))) E lds[S * STAGE];
-
-  const int tid = threadIdx.x, lane = tid & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int wm = wave / GN, wn = wave % GN;
-  const int li = lane & 31, h = lane >> 5;
-  const int gy = gridDim.y;
-  int tm, tn, tz;
-  if (!tile_of(gy, s.splits, tm, tn, tz)) return;
-  const int m0 = tm * RM, n0 = tn * RN;
-
-  const int nvb = s.K / BK;
-  int vb0 = 0, nblk = nvb;
-  if (s.splits > 1) {
-    const int per = (nvb + s.splits - 1) / s.splits;
-    vb0 = min(tz * per, nvb);
-    nblk = min(nvb, vb0 + per) - vb0;
-  }
-
-  typename SumT<E>::T acc[WM][WN];
-#pragma unroll
-  for (int a = 0; a < WM; ++a)
-#pragma unroll
-    for (int b = 0; b < WN; ++b)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) acc[a][b][r] = 0;
-
-  // Element offsets of the lane's direct loads from the tile's origin.  Rows of
-  // a K-contiguous operand past its last one read that one; chunks of a [k][m]
-  // operand past its width read its last chunk (both feed outputs that are not
-  // stored).
-  const int fa = MODE == UP ? m0 / 2 : m0;       // A's first row or column
-  auto offset_a = [&](int j, long long ld) {
-    int row, ch;
-    TA::src(wave, lane, j, row, ch);
-    if (MODE == UP) row = row / 64 * 32 + row % 32;
-    return AKC ? (uint32_t)((min(fa + row, s.alim - 1) - fa) * ld) + EPC * ch
-               : (uint32_t)(row * ld) + min(EPC * ch, (s.M - 1 - m0) / EPC * EPC);
-  };
-  auto offset_b = [&](int j, long long ld) {
-    int row, ch;
-    TB::src(wave, lane, j, row, ch);
-    return BKC ? (uint32_t)((min(n0 + row, s.blim - 1) - n0) * ld) + EPC * ch
-               : (uint32_t)(row * ld) + min(EPC * ch, (s.N - 1 - n0) / EPC * EPC);
-  };
-  uint32_t offa[TA::INSTR], offb[TB::INSTR];
-#pragma unroll
-  for (int j = 0; j < TA::INSTR; ++j) offa[j] = offset_a(j, s.lda);
-#pragma unroll
-  for (int j = 0; j < TB::INSTR; ++j) offb[j] = offset_b(j, s.ldb);
-  const size_t a0 = AKC ? (size_t)fa * s.lda : (size_t)m0;
-  const size_t b0 = BKC ? (size_t)n0 * s.ldb : (size_t)n0;
-  const uint32_t lds0 = lds_address(lds);
-  static_assert(TA::CH == 8 || !AKC, "8 rows of 128 bytes a direct load");
-  // direct load j of K block vb into stage st (A's, then B's)
-  auto issue1 = [&](int vb, int st, int j) {
-    const int k0 = vb * BK;
-    const uint32_t base = lds0 + (uint32_t)sizeof(E) * (uint32_t)(st * STAGE);
-    if (j < TA::INSTR) {
-      const E* a = (const E*)s.A;
-      int k = k0;
-      // a load's 8 rows are of one matrix: blocks of 32 rows in turn
-      if (MODE == UP && ((wave * TA::INSTR + j) / 4 & 1)) a = (const E*)s.A1;
-      if (MODE == DX && k0 >= s.kh) {
-        a = (const E*)s.A1;
-        k -= s.kh;
-      }
-      a += a0 + (AKC ? (size_t)k : (size_t)k * s.lda) + offa[j];
-      if (MODE == DW && s.at && k0 >= s.ktail)
-        a = (const E*)s.at + a0 + (size_t)(k0 - s.ktail) * s.ldat + offset_a(j, s.ldat);
-      dma16_at(a, base + (uint32_t)sizeof(E) * TA::dst(wave, j));
-    } else {
-      j -= TA::INSTR;
-      const E* b = (const E*)s.B + b0 + (BKC ? (size_t)k0 : (size_t)k0 * s.ldb) + offb[j];
-      if (MODE == DW && s.bt && k0 >= s.ktail)
-        b = (const E*)s.bt + b0 + (size_t)(k0 - s.ktail) * s.ldbt + offset_b(j, s.ldbt);
-      dma16_at(b, base + (uint32_t)sizeof(E) * (TA::SIZE + TB::dst(wave, j)));
-    }
-  };
-  auto fetch1 = [&](FragsT<E, TA, TB, WM, WN>& f, int st, int q, int i) {
-    const E* la = lds + st * STAGE;
-    const E* lb = la + TA::SIZE;
-    if (i < WN) f.b[i] = TB::frag(lb, wn * 32 * WN + 32 * i, lane, q);
-    else f.a[i - WN] = TA::frag(la, wm * 32 * WM + 32 * (i - WN), lane, q);
-  };
-  k_loop<E, TA, TB, WM, WN, S>(acc, vb0, nblk, fetch1, issue1, [] {}, [](int) {});
-
-  // Lane (li, h), register r of block (a, b) holds n = 32 b + li and
-  // m = 32 a + 8 (r / 4) + 4 h + r % 4 of the wave's part of the tile.
-  const int mt = m0 + wm * 32 * WM, nt = n0 + wn * 32 * WN;
-  constexpr int RL = 32 * WM;
-  static_assert(NW * 32 * RL * 4 <= S * STAGE * (int)sizeof(E), "staging exceeds the stages");
-  float* const mine = (float*)lds + wave * 32 * RL;
-  const bool parts = (MODE == DOWN || MODE == DX || MODE == DW) && e.part;
-  float* const part = parts ? e.part + (size_t)tz * gy * RN * e.ldp : nullptr;
-  __syncthreads();     // every wave is done with the operand stages
-#pragma unroll
-  for (int b = 0; b < WN; ++b) {
-#pragma unroll
-    for (int a = 0; a < WM; ++a)
-#pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        f32x4 v;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          if constexpr (sizeof(E) == 1) v[j] = __int_as_float(acc[a][b][4 * g + j]);
-          else v[j] = acc[a][b][4 * g + j];
-        }
-        *(f32x4*)(mine + li * RL + 4 * ((8 * a + 2 * g + h) ^ (li & (RL / 4 - 1)))) = v;
-      }
-    // the wave's own region, and its LDS operations stay in order
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    const int nb = nt + 32 * b;
-    if constexpr (MODE == UP) {
-      up_part<E, WM>(mine, lane, e, nb, mt / 2);
-    } else if constexpr (MODE == DH) {
-      dh_part<E, WM>(mine, lane, e, nb, mt, s.N);
-    } else if (parts) {
-      store_part<float, RL>(mine, lane, part, e.ldp, nb, s.N, mt, s.M, 0);
-    } else if constexpr (sizeof(E) == 1) {
-      scaled_part<O, RL>(mine, lane, e, nb, mt);
-    } else {
-      // (32 rows are on one side of n1, a multiple of 64)
-      const bool second = nb >= e.n1;
-      store_part<O, RL>(mine, lane, (O*)(second ? e.out1 : e.out), second ? e.ldo1 : e.ldo,
-                        second ? nb - e.n1 : nb, e.nout, mt, e.mout, e.accumulate);
-    }
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-  }
-}
-
-}  // namespace
-
-// big: 256 x 256 tiles, 8 waves of 128 x 64; else 128 x 128, 4 waves of 64 x 64
-#define HF_GGEMM(NAME, E, O, MODE)                                                    \
-  extern "C" __global__ __launch_bounds__(512, 1) void NAME##_big(GGemm s, GEpi e) {  \
-    ggemm_body<E, O, MODE, 4, 2, 2, 4, 2>(s, e);                                      \
-  }                                                                                   \
-  extern "C" __global__ __launch_bounds__(256, 2) void NAME(GGemm s, GEpi e) {        \
-    ggemm_body<E, O, MODE, 2, 2, 2, 2, 2>(s, e);                                      \
-  }
-#define HF_GGEMM_T(NAME, MODE)                   \
-  HF_GGEMM(NAME##_f32, float, float, MODE)       \
-  HF_GGEMM(NAME##_bf16, bf16_t, bf16_t, MODE)
-HF_GGEMM_T(hf_gated_up, UP)
+#define HF_GGEMM_T(NAME, MODE)                              \
+  HF_GGEMM(NAME##_f32, float, float, MODE, GA_RELU)         \
+  HF_GGEMM(NAME##_bf16, bf16_t, bf16_t, MODE, GA_RELU)
 HF_GGEMM_T(hf_gated_down, DOWN)
-HF_GGEMM_T(hf_gated_dh, DH)
 HF_GGEMM_T(hf_gated_dx, DX)
 HF_GGEMM_T(hf_gated_dw, DW)
-HF_GGEMM(hf_gated_up_codes, int8_t, float, UP)
-HF_GGEMM(hf_gated_down_codes_f32, int8_t, float, DOWN)
-HF_GGEMM(hf_gated_down_codes_bf16, int8_t, bf16_t, DOWN)
+HF_GGEMM(hf_gated_down_codes_f32, int8_t, float, DOWN, GA_RELU)
+HF_GGEMM(hf_gated_down_codes_bf16, int8_t, bf16_t, DOWN, GA_RELU)
 
-// ------------------------------------------------------------- launchers
+extern const GActKernels gated_sigmoid, gated_tanh, gated_relu, gated_silu, gated_gelu,
+    gated_gelu_tanh;
+
 namespace {
-typedef void (*GK)(GGemm, GEpi);
-// kernels of a product by type and tile (VT_*, TILE_* of GGemm::tile)
-typedef GK Kernels[3][2];
-void launch(const Launch& L, const char* name, const GK (&k)[2], const GGemm& g, const GEpi& e) {
-  if (g.M < 1 || g.N < 1) return;
+const GActKernels& act_kernels(int act) {
+  switch (act) {
+    case GA_SIGMOID: return gated_sigmoid;
+    case GA_TANH: return gated_tanh;
+    case GA_RELU: return gated_relu;
+    case GA_SILU: return gated_silu;
+    case GA_GELU: return gated_gelu;
+    default: return gated_gelu_tanh;
+  }
+}
+void launch(const Launch& L, const char* name, const GKernel (&k)[2], const GGemm& g,
+            const GEpi& e) {
+  if (g.M <= g.m0 || g.N < 1) return;
   const int RM = tile_m(g.tile), RN = tile_n(g.tile);
-  const dim3 grid((g.M + RM - 1) / RM, (g.N + RN - 1) / RN, g.splits);
+  const dim3 grid((g.M - g.m0 + RM - 1) / RM, (g.N + RN - 1) / RN, g.splits);
   prof_begin(L, name);
   hipExtLaunchKernelGGL(k[g.tile], grid, dim3(g.tile == TILE_BIG ? 512 : 256), 0, L.stream,
                         prof_a(L), prof_b(L), 0, g, e);
-  prof_end(L, name, 2.0 * g.M * (double)g.N * g.K, 0.0);
+  prof_end(L, name, 2.0 * (g.M - g.m0) * (double)g.N * g.K, 0.0);
 }
 }  // namespace
 
-#define HF_GK(NAME) {NAME, NAME##_big}
 void gated_up(const Launch& L, int type, const GGemm& g, const GEpi& e) {
-  static const Kernels k = {HF_GK(hf_gated_up_f32), HF_GK(hf_gated_up_bf16),
-                            HF_GK(hf_gated_up_codes)};
-  launch(L, "hf_gated_up", k[type], g, e);
-}
-void gated_down(const Launch& L, int type, int out_type, const GGemm& g, const GEpi& e) {
-  static const Kernels k = {HF_GK(hf_gated_down_f32), HF_GK(hf_gated_down_bf16)};
-  static const Kernels c = {HF_GK(hf_gated_down_codes_f32), HF_GK(hf_gated_down_codes_bf16)};
-  launch(L, "hf_gated_down", type == VT_I8 ? c[out_type] : k[type], g, e);
+  launch(L, "hf_gated_up", act_kernels(e.act).up[type], g, e);
 }
 void gated_dh(const Launch& L, int type, const GGemm& g, const GEpi& e) {
-  static const Kernels k = {HF_GK(hf_gated_dh_f32), HF_GK(hf_gated_dh_bf16)};
-  launch(L, "hf_gated_dh", k[type], g, e);
+  launch(L, "hf_gated_dh", act_kernels(e.act).dh[type], g, e);
+}
+void gated_down(const Launch& L, int type, int out_type, const GGemm& g, const GEpi& e) {
+  static const GKernel k[2][2] = {HF_GK(hf_gated_down_f32), HF_GK(hf_gated_down_bf16)};
+  static const GKernel c[2][2] = {HF_GK(hf_gated_down_codes_f32), HF_GK(hf_gated_down_codes_bf16)};
+  launch(L, "hf_gated_down", type == VT_I8 ? c[out_type] : k[type], g, e);
 }
 void gated_dx(const Launch& L, int type, const GGemm& g, const GEpi& e) {
-  static const Kernels k = {HF_GK(hf_gated_dx_f32), HF_GK(hf_gated_dx_bf16)};
+  static const GKernel k[2][2] = {HF_GK(hf_gated_dx_f32), HF_GK(hf_gated_dx_bf16)};
   launch(L, "hf_gated_dx", k[type], g, e);
 }
 void gated_dw(const Launch& L, int type, const GGemm& g, const GEpi& e) {
-  static const Kernels k = {HF_GK(hf_gated_dw_f32), HF_GK(hf_gated_dw_bf16)};
+  static const GKernel k[2][2] = {HF_GK(hf_gated_dw_f32), HF_GK(hf_gated_dw_bf16)};
   launch(L, "hf_gated_dw", k[type], g, e);
 }
 

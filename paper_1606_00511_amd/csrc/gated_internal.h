@@ -17,6 +17,7 @@ constexpr int CPAD = 128;
 // C(m, n) = sum_k A(m, k) B(n, k), m contiguous in the output (see mfma_tile.h).
 struct GGemm {
   int M, N, K;
+  int m0;                // columns of the output before it are another launch's
   const void *A, *A1, *B;
   long long lda, ldb;
   int alim, blim;        // rows m of A and n of B that exist, where these are rows
@@ -53,10 +54,22 @@ struct GEpi {
   long long ldp;
 };
 
+// The kernels with an activation, by type and tile (VT_*, TILE_*).
+typedef void (*GKernel)(GGemm, GEpi);
+struct GActKernels {
+  GKernel up[3][2], dh[2][2];
+};
+
 // h = phi(X Wg^T) * (X Wu^T): A = Wg, A1 = Wu (rows alim), B = X; M = 2 Fp
 void gated_up(const Launch& L, int type, const GGemm& g, const GEpi& e);
 // out = B A^T: A = Wd, B = h; codes: out_type, scaled
 void gated_down(const Launch& L, int type, int out_type, const GGemm& g, const GEpi& e);
+// the same of up to FEW_X rows, in place at any alignment; "up" keeps nothing, its
+// M is F, and of codes hmax has an entry for 16 columns; "down" of up to TWO_X
+// bf16 rows reads the second terms that "up" wrote, TWO_X rows further down
+constexpr int FEW_X = 64, TWO_X = 16;
+void gated_few_up(const Launch& L, int type, const GGemm& g, const GEpi& e);
+void gated_few_down(const Launch& L, int type, int out_type, const GGemm& g, const GEpi& e);
 // dh = dY Wd in the tile, from it and what is kept h, dg and du
 void gated_dh(const Launch& L, int type, const GGemm& g, const GEpi& e);
 // dX = dg Wg + du Wu

@@ -154,7 +154,8 @@ __device__ __forceinline__ void put_row_codes(int8_t* p, const float (&v)[8], co
       if (j < room) p[j] = (int8_t)(w[j >> 2] >> (8 * (j & 3)));
   }
 }
-// the largest of the workgroup's, W waves
+__device__ __forceinline__ uint32_t magnitude(float v) { return __float_as_uint(v) & 0x7fffffffu; }
+// the largest of W waves'
 template <int W>
 __device__ __forceinline__ uint32_t group_max(uint32_t big) {
 #pragma unroll
@@ -168,27 +169,54 @@ __device__ __forceinline__ uint32_t group_max(uint32_t big) {
   }
   return big;
 }
-// a row by a workgroup of 64 W lanes
-template <class E, int W>
-__device__ __forceinline__ void codes_body(const E* X, long long ldx, int cols, int8_t* codes,
-                                           long long ldc, int zcols, float* scale) {
-  const size_t row = blockIdx.x;
-  const E* x = X + row * ldx;
+// A row by W waves, of a workgroup of 4.  C > 0: a lane's C chunks stay in registers
+// between the two passes (cols <= 512 W C); else the row is read twice.
+template <class E, int W, int C>
+__device__ __forceinline__ void codes_body(const E* X, long long ldx, int rows, int cols,
+                                           int8_t* codes, long long ldc, int zcols, float* scale) {
+  const int row = W == 4 ? blockIdx.x : 4 * blockIdx.x + threadIdx.x / 64;
+  if (row >= rows) return;                    // (W == 1: a whole wave)
+  const int t = W == 4 ? threadIdx.x : threadIdx.x % 64;
+  const E* x = X + (size_t)row * ldx;
+  int8_t* out = codes + (size_t)row * ldc;
   uint32_t big = 0;
-  for (int at = 8 * (int)threadIdx.x; at < cols; at += 512 * W) {
-    float v[8];
-    get(x + at, v, cols - at);
+  float keep[C > 0 ? C : 1][8];
+  if constexpr (C > 0) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) big = max(big, __float_as_uint(v[j]) & 0x7fffffffu);
+    for (int i = 0; i < C; ++i) {
+      const int at = 8 * (t + 64 * W * i);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) keep[i][j] = 0.0f;
+      if (at < cols) get(x + at, keep[i], cols - at);
+    }
+#pragma unroll
+    for (int i = 0; i < C; ++i)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) big = max(big, magnitude(keep[i][j]));
+  } else {
+    for (int at = 8 * t; at < cols; at += 512 * W) {
+      float v[8];
+      get(x + at, v, cols - at);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) big = max(big, magnitude(v[j]));
+    }
   }
   const RowScale r = row_scale(group_max<W>(big));
-  if (threadIdx.x == 0) scale[row] = r.s;
-  for (int at = 8 * (int)threadIdx.x; at < zcols; at += 512 * W) {
-    float v[8];
+  if (t == 0) scale[row] = r.s;
+  if constexpr (C > 0) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = 0.0f;
-    if (at < cols) get(x + at, v, cols - at);
-    put_row_codes(codes + row * ldc + at, v, r, cols - at, zcols - at);
+    for (int i = 0; i < C; ++i) {
+      const int at = 8 * (t + 64 * W * i);
+      if (at < zcols) put_row_codes(out + at, keep[i], r, cols - at, zcols - at);
+    }
+  } else {
+    for (int at = 8 * t; at < zcols; at += 512 * W) {
+      float v[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = 0.0f;
+      if (at < cols) get(x + at, v, cols - at);
+      put_row_codes(out + at, v, r, cols - at, zcols - at);
+    }
   }
 }
 
@@ -237,6 +265,12 @@ HF_FINISH(bf16, bf16_t, bf16_t)
 HF_FINISH(codes_f32, int8_t, float)
 HF_FINISH(codes_bf16, int8_t, bf16_t)
 
+#define HF_ROW_CODES(NAME, E, W, C)                                                             \
+  extern "C" __global__ __launch_bounds__(256) void NAME(                                       \
+      const E* X, long long ldx, int rows, int cols, int8_t* codes, long long ldc, int zcols,    \
+      float* scale) {                                                                            \
+    codes_body<E, W, C>(X, ldx, rows, cols, codes, ldc, zcols, scale);                           \
+  }
 #define HF_CODES(SUF, E)                                                                         \
   extern "C" __global__ __launch_bounds__(256) void hf_gated_pack_##SUF(                         \
       const E* X, long long ldx, uint32_t total, int cols, uint32_t per, int8_t* codes,          \
@@ -248,32 +282,32 @@ HF_FINISH(codes_bf16, int8_t, bf16_t)
       int cols, E* X, long long ldx, uint32_t zrows, int zcols, uint32_t per, uint32_t total) {  \
     unpack_body<E>(codes, ldc, scale, lds, rows, cols, X, ldx, zrows, zcols, per, total);        \
   }                                                                                              \
-  extern "C" __global__ __launch_bounds__(256) void hf_gated_codes_##SUF(                        \
-      const E* X, long long ldx, int cols, int8_t* codes, long long ldc, int zcols,              \
-      float* scale) {                                                                            \
-    codes_body<E, 4>(X, ldx, cols, codes, ldc, zcols, scale);                                    \
-  }
+  HF_ROW_CODES(hf_gated_codes_##SUF, E, 4, 0)                                                    \
+  HF_ROW_CODES(hf_gated_codes_##SUF##_c1, E, 1, 2)                                               \
+  HF_ROW_CODES(hf_gated_codes_##SUF##_c4, E, 1, 8)                                               \
+  HF_ROW_CODES(hf_gated_codes_##SUF##_c16, E, 4, 8)
 HF_CODES(f32, float)
 HF_CODES(bf16, bf16_t)
 
+// 2,048 columns of a row a workgroup, which finds the row's largest among the
+// products' parts of it first
 extern "C" __global__ __launch_bounds__(256) void hf_gated_codes_h(const float* H, long long ldh,
                                                                    const float* hmax, int ldmax,
                                                                    int cols, int8_t* codes,
                                                                    long long ldc, int zcols,
-                                                                   float* scale) {
-  const size_t row = blockIdx.x;
+                                                                   int chunks, float* scale) {
+  const size_t row = blockIdx.x / (uint32_t)chunks;
+  const int at = 2048 * (int)(blockIdx.x % (uint32_t)chunks) + 8 * (int)threadIdx.x;
+  float v[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) v[j] = 0.0f;
+  if (at < cols) get(H + row * ldh + at, v, cols - at);
   uint32_t big = 0;
   for (int i = threadIdx.x; i < ldmax; i += 256)
     big = max(big, __float_as_uint(hmax[row * ldmax + i]));
   const RowScale r = row_scale(group_max<4>(big));
-  if (threadIdx.x == 0) scale[row] = r.s;
-  for (int at = 8 * (int)threadIdx.x; at < zcols; at += 2048) {
-    float v[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = 0.0f;
-    if (at < cols) get(H + row * ldh + at, v, cols - at);
-    put_row_codes(codes + row * ldc + at, v, r, cols - at, zcols - at);
-  }
+  if (at == 0) scale[row] = r.s;
+  if (at < zcols) put_row_codes(codes + row * ldc + at, v, r, cols - at, zcols - at);
 }
 
 // ------------------------------------------------------------- launchers
@@ -349,22 +383,38 @@ void gated_unpack(const Launch& L, int type, const int8_t* codes, long long ldc,
               lds, (uint32_t)rows, cols, (bf16_t*)X, ldx, (uint32_t)zrows, zcols, per, total);
 }
 
+namespace {
+// a row a wave, whose lanes hold 16 or 64 numbers of it, or 4 waves (8,192 rows of
+// 4,096, bf16: 39 us with 4 waves and two reads of a row, 24 with one)
+template <class E>
+void codes_of(const Launch& L, void (*const (&k)[4])(const E*, long long, int, int, int8_t*,
+                                                     long long, int, float*),
+              const E* X, long long ldx, int rows, int cols, int8_t* codes, long long ldc,
+              int zcols, float* scale) {
+  const int i = zcols <= 1024 ? 1 : zcols <= 4096 ? 2 : zcols <= 16384 ? 3 : 0;
+  HF_LAUNCH("hf_gated_codes", k[i], i == 1 || i == 2 ? (rows + 3) / 4 : rows, 256, X, ldx, rows,
+            cols, codes, ldc, zcols, scale);
+}
+}  // namespace
+
 void gated_codes(const Launch& L, int type, const void* X, long long ldx, long long rows, int cols,
                  int8_t* codes, long long ldc, int zcols, float* scale) {
   if (rows < 1) return;
+#define HF_CK(SUF) {hf_gated_codes_##SUF, hf_gated_codes_##SUF##_c1, hf_gated_codes_##SUF##_c4, \
+                    hf_gated_codes_##SUF##_c16}
   if (type == VT_F32)
-    HF_LAUNCH("hf_gated_codes", hf_gated_codes_f32, rows, 256, (const float*)X, ldx, cols, codes,
-              ldc, zcols, scale);
+    codes_of<float>(L, HF_CK(f32), (const float*)X, ldx, (int)rows, cols, codes, ldc, zcols, scale);
   else
-    HF_LAUNCH("hf_gated_codes", hf_gated_codes_bf16, rows, 256, (const bf16_t*)X, ldx, cols, codes,
-              ldc, zcols, scale);
+    codes_of<bf16_t>(L, HF_CK(bf16), (const bf16_t*)X, ldx, (int)rows, cols, codes, ldc, zcols,
+                     scale);
 }
 
 void gated_codes_h(const Launch& L, const float* H, long long ldh, const float* hmax, int ldmax,
                    int rows, int cols, int8_t* codes, long long ldc, int zcols, float* scale) {
   if (rows < 1) return;
-  HF_LAUNCH("hf_gated_codes_h", hf_gated_codes_h, rows, 256, H, ldh, hmax, ldmax, cols, codes,
-            ldc, zcols, scale);
+  const int chunks = (zcols + 2047) / 2048;
+  HF_LAUNCH("hf_gated_codes_h", hf_gated_codes_h, (long long)rows * chunks, 256, H, ldh, hmax,
+            ldmax, cols, codes, ldc, zcols, chunks, scale);
 }
 
 }  // namespace hfk

@@ -34,8 +34,11 @@ def test_forward(type, T, D, F):
     Y, kept = n.hf_gated_forward(X, Wg, Wu, Wd)
     assert kept is None
     want = G.block(act, X, Wg, Wu, Wd)[0]
-    bound = G.block_bound(act, X, Wg, Wu, Wd, two_term=type == "bf16" and T <= 128)[0]
-    G.close(Y, want, bound, "Y")
+    two = type == "bf16" and (T <= 16 or 64 < T <= 128)
+    G.close(Y, want, G.block_bound(act, X, Wg, Wu, Wd, two_term=two)[0], "Y")
+    Y, _ = n.hf_gated_forward(X, Wg, Wu, Wd, keep="full")
+    two = type == "bf16" and T <= 128
+    G.close(Y, want, G.block_bound(act, X, Wg, Wu, Wd, two_term=two)[0], "Y with g and u kept")
 
 
 @pytest.mark.parametrize("type", ["fp32", "bf16"])
@@ -44,7 +47,8 @@ def test_forward(type, T, D, F):
 def test_activations_and_keep(type, act, T):
     """Every activation; g and u kept in full are the products, and in 8 bits
     their checkpoint (a number next to a border between two codes may be on its
-    other side); Y has the same bits in any case."""
+    other side).  Y is the same whatever is kept; of up to 64 rows that keep
+    nothing, whose sums are in another order, it is as near."""
     D, F = 96, 200
     X, Wg, Wu, Wd, _ = G.inputs(T, D, F, G.TYPES[type], seed=T)
     X[0] *= 60                 # far out on both sides
@@ -52,9 +56,12 @@ def test_activations_and_keep(type, act, T):
     Y, _ = n.hf_gated_forward(X, Wg, Wu, Wd)
     Yf, full = n.hf_gated_forward(X, Wg, Wu, Wd, keep="full")
     Y8, (codes, scale) = n.hf_gated_forward(X, Wg, Wu, Wd, keep="int8")
-    assert torch.equal(Y, Yf) and torch.equal(Y, Y8)
+    assert torch.equal(Yf, Y8) and (T <= 64 or torch.equal(Y, Yf))
     want, g, u, _ = G.block(act, X, Wg, Wu, Wd)
     by, bg, bu = G.block_bound(act, X, Wg, Wu, Wd, two_term=type == "bf16" and T <= 128)
+    G.close(Yf, want, by, "Y with g and u kept")
+    if T <= 64:
+        by = G.block_bound(act, X, Wg, Wu, Wd)[0]
     G.close(Y, want, by, "Y")
     G.close(full[:, :F], g, bg, "g")
     G.close(full[:, F:], u, bu, "u")

@@ -169,11 +169,6 @@ void operands(GGemm* g, const void* A, const void* A1, int64_t lda, const void* 
   g->B = B;
   g->ldb = ldb;
 }
-void set_shape(GGemm* g, int type, bool split) {
-  const Shape s = shape_for(type, g->M, g->N, g->K, split, false);
-  g->tile = s.tile;
-  g->splits = s.splits;
-}
 GEpi epilogue(const hf_gated* c, int64_t T) {
   GEpi e = {};
   e.act = c->act;
@@ -189,17 +184,54 @@ void set_out(GEpi* e, void* out, int64_t ldo, int64_t rows, int cols) {
   e->nout = (int)rows;
   e->mout = cols;
 }
+// A product in one launch or two, by their estimated time: a last round of few tiles
+// leaves most units idle, and its columns are then a launch of their own, of a shape
+// of their own.  run(g) launches columns [g.m0, g.M); shapes: 3, or 2 without tiles of
+// 64 rows.
+template <class Run>
+void ranged(GGemm g, int type, bool split, int shapes, Run run) {
+  const int64_t M = g.M, N = g.N, K = g.K;
+  Shape a = shape_for(type, M, N, K, split, shapes), b = {};
+  int64_t m1 = M;
+  double least = a.us;
+  for (int tile : {TILE_BIG, TILE_SMALL}) {
+    const int64_t rm = tile_m(tile), tn = (N + tile_n(tile) - 1) / tile_n(tile);
+    const int64_t slots = tile == TILE_BIG ? 256 : 512;
+    const int64_t whole = ((M + rm - 1) / rm * tn) / slots * slots / tn * rm;
+    if (whole <= 0 || whole >= M) continue;
+    const Shape x = shape_for(type, whole, N, K, split, shapes);
+    const Shape y = shape_for(type, M - whole, N, K, split, shapes);
+    if (x.us + y.us + 4.0 < least) {
+      least = x.us + y.us + 4.0;
+      a = x;
+      b = y;
+      m1 = whole;
+    }
+  }
+  g.M = (int)m1;
+  g.tile = a.tile;
+  g.splits = a.splits;
+  run(g);
+  if (m1 == M) return;
+  g.m0 = (int)m1;
+  g.M = (int)M;
+  g.tile = b.tile;
+  g.splits = b.splits;
+  run(g);
+}
 // a product into e's out: straight, or by partials
 template <class Kernel>
-void summed(hf_gated* c, const Launch& L, int type, int out_type, GGemm* g, GEpi* e, int dup,
-            Kernel kernel) {
-  set_shape(g, type, true);
-  if (g->splits > 1 || dup) {
-    e->part = c->at<float>(c->lay.part);
-    e->ldp = g->M;
-  }
-  kernel(*g, *e);
-  if (e->part) gated_finish(L, type, out_type, *g, *e, dup);
+void summed(hf_gated* c, const Launch& L, int type, int out_type, const GGemm& all, const GEpi& out,
+            int dup, int shapes, Kernel kernel) {
+  ranged(all, type, true, shapes, [&](const GGemm& g) {
+    GEpi e = out;
+    if (g.splits > 1 || dup) {
+      e.part = c->at<float>(c->lay.part);
+      e.ldp = all.M;
+    }
+    kernel(g, e);
+    if (e.part) gated_finish(L, type, out_type, g, e, dup);
+  });
 }
 
 }  // namespace
@@ -340,13 +372,12 @@ int hf_gated_forward(hf_gated* c, const void* X, int64_t ldx, const void* Wg, in
   eu.ldk = ldk;
   eu.ks = scale;
   eu.ldks = lds;
-  set_shape(&gu, c->type, false);
-  gated_up(L, c->type, gu, eu);
+  ranged(gu, c->type, false, 3, [&](const GGemm& g) { gated_up(L, c->type, g, eu); });
 
   gd.B = eu.h;
   gd.ldb = Fp;
   set_out(&ed, Y, ldy, T, D);
-  summed(c, L, c->type, c->type, &gd, &ed, dup, [&](const GGemm& g, const GEpi& e) {
+  summed(c, L, c->type, c->type, gd, ed, dup, 3, [&](const GGemm& g, const GEpi& e) {
     gated_down(L, c->type, c->type, g, e);
   });
   return end(c);
@@ -462,27 +493,26 @@ int hf_gated_grad(hf_gated* c, const void* X, int64_t ldx, const uint8_t* xscale
   eh.ldk = ldk;
   eh.ks = const_cast<uint8_t*>(scale);
   eh.ldks = lds;
-  set_shape(&gh, type, false);
-  gated_dh(L, type, gh, eh);
+  ranged(gh, type, false, 3, [&](const GGemm& g) { gated_dh(L, type, g, eh); });
 
   if (dX) {
     gx.B = eh.dgu;
     gx.ldb = eh.lddgu;
     gx.kh = Fp;
     set_out(&ex, dX, lddx, T, D);
-    summed(c, L, type, type, &gx, &ex, dup,
+    summed(c, L, type, type, gx, ex, dup, 3,
            [&](const GGemm& g, const GEpi& e) { gated_dx(L, type, g, e); });
   }
   auto dw = [&](const GGemm& g, const GEpi& e) { gated_dw(L, type, g, e); };
   if (dWd) {
     gd.A = eh.h;
     gd.lda = Fp;
-    summed(c, L, type, type, &gd, &ed, 0, dw);
+    summed(c, L, type, type, gd, ed, 0, 2, dw);
   }
   if (ew.out) {
     gw.B = (const char*)eh.dgu + (dWg ? 0 : (size_t)Fp * es);
     gw.ldb = eh.lddgu;
-    summed(c, L, type, type, &gw, &ew, 0, dw);
+    summed(c, L, type, type, gw, ew, 0, 2, dw);
   }
   return end(c);
 }
@@ -584,7 +614,7 @@ int hf_gated_product(hf_gated* c, const int8_t* A, int64_t lda, const float* sa,
     e.sn = sa;
     e.sm = sb + n0;
     set_out(&e, (char*)Y + n0 * c->es, ldy, T, nn);
-    summed(c, L, VT_I8, c->type, &g, &e, 0, [&](const GGemm& gg, const GEpi& ee) {
+    summed(c, L, VT_I8, c->type, g, e, 0, 3, [&](const GGemm& gg, const GEpi& ee) {
       gated_down(L, VT_I8, c->type, gg, ee);
     });
   }
@@ -646,8 +676,7 @@ int hf_gated_forward_codes(hf_gated* c, const void* X, int64_t ldx, const int8_t
   if (few) {
     gated_few_up(L, VT_I8, gu, eu);
   } else {
-    set_shape(&gu, VT_I8, false);
-    gated_up(L, VT_I8, gu, eu);
+    ranged(gu, VT_I8, false, 3, [&](const GGemm& g) { gated_up(L, VT_I8, g, eu); });
   }
   gated_codes_h(L, c->at<float>(l.hf), Fc, eu.hmax, eu.ldmax, T, F, hq, Fc, Fc, sh);
   ed.sn = sh;
@@ -656,7 +685,7 @@ int hf_gated_forward_codes(hf_gated* c, const void* X, int64_t ldx, const int8_t
   if (few) {
     gated_few_down(L, VT_I8, c->type, gd, ed);
   } else {
-    summed(c, L, VT_I8, c->type, &gd, &ed, 0, [&](const GGemm& g, const GEpi& e) {
+    summed(c, L, VT_I8, c->type, gd, ed, 0, 3, [&](const GGemm& g, const GEpi& e) {
       gated_down(L, VT_I8, c->type, g, e);
     });
   }

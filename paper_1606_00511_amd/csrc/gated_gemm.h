@@ -117,24 +117,49 @@ __device__ __forceinline__ void up_rows(const float* s, int lane, const GEpi& e,
   }
 }
 
-// What is kept as codes of g and u at a lane's places in 32 rows of 32 WM features,
-// all of which exist: fetched ahead of the products that need it.
-template <int WM>
-struct KeptCodes {
+// What is kept of g and u at a lane's places in PB of its rows of 32 WM features, all
+// of which exist: fetched ahead of the products that need it.
+template <class E, bool CODES, int WM>
+struct Kept {
   static constexpr int FC = 4 * WM, I = 2 * WM;  // lanes a row, 8 features each; rows a lane
-  uint32_t g[I][2], u[I][2];
-  uint8_t sg[I], su[I];
-  __device__ __forceinline__ void fetch(const GEpi& e, int lane, int n0, int f0) {
+  // rows at once, in 16 to 20 registers (twice as many leave the largest tiles none)
+  static constexpr int PB = CODES ? (I < 4 ? I : 4) : sizeof(E) == 2 ? 2 : 1;
+  static constexpr int W = CODES ? 2 : 2 * (int)sizeof(E);
+  uint32_t g[PB][W], u[PB][W];
+  uint8_t sg[PB], su[PB];
+  // rows n0 + (lane + 64 i) / FC, i = i0 .. i0 + PB - 1
+  __device__ __forceinline__ void fetch(const GEpi& e, int lane, int n0, int i0, int f0) {
     const int f = f0 + 8 * (lane % FC), nb = (e.F + CODE_BLOCK - 1) / CODE_BLOCK;
 #pragma unroll
-    for (int i = 0; i < I; ++i) {
-      const int n = n0 + (lane + 64 * i) / FC;
-      const int8_t* p = (const int8_t*)e.kept + (size_t)n * e.ldk + f;
-      const uint8_t* ks = e.ks + (size_t)n * e.ldks + f / CODE_BLOCK;
-      __builtin_memcpy(g[i], p, 8);
-      __builtin_memcpy(u[i], p + e.F, 8);
-      sg[i] = ks[0];
-      su[i] = ks[nb];
+    for (int i = 0; i < PB; ++i) {
+      const int n = n0 + (lane + 64 * (i0 + i)) / FC;
+      if constexpr (CODES) {
+        const int8_t* p = (const int8_t*)e.kept + (size_t)n * e.ldk + f;
+        const uint8_t* ks = e.ks + (size_t)n * e.ldks + f / CODE_BLOCK;
+        __builtin_memcpy(g[i], p, 8);
+        __builtin_memcpy(u[i], p + e.F, 8);
+        sg[i] = ks[0];
+        su[i] = ks[nb];
+      } else {
+        const E* p = (const E*)e.kept + (size_t)n * e.ldk + f;
+#pragma unroll
+        for (int j = 0; j < W; j += 4) {
+          __builtin_memcpy(&g[i][j], (const char*)p + 4 * j, 16);
+          __builtin_memcpy(&u[i][j], (const char*)(p + e.F) + 4 * j, 16);
+        }
+      }
+    }
+  }
+  __device__ __forceinline__ void value(const uint32_t (&w)[W], uint8_t scale, float (&v)[8]) const {
+    if constexpr (CODES) {
+      const float step = code_step(scale);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = (float)(int8_t)(w[j >> 2] >> (8 * (j & 3))) * step;
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        v[j] = sizeof(E) == 4 ? __uint_as_float(w[j % W])
+                              : bf2f(j & 1 ? w[j / 2] >> 16 : w[j / 2] & 0xffffu);
     }
   }
 };
@@ -158,28 +183,41 @@ __device__ __forceinline__ void dh_chunk(const GEpi& e, int n, int f, int have, 
   put_term(q, g, e.dup * e.lddgu);
   put_term(q + e.Fp, u, e.dup * e.lddgu);
 }
-__device__ __forceinline__ void codes8(const uint32_t (&w)[2], float step, float (&v)[8]) {
+// "dh" of a wave's 32 WN rows from n0 and 32 WM features from f0, all of which exist:
+// stage(b) puts 32 rows of dh into s; what is kept of the next rows is on its way
+// during the products of these
+template <class E, bool CODES, int WM, int WN, int ACT, class Stage>
+__device__ __forceinline__ void dh_full(const float* s, int lane, const GEpi& e, int n0, int f0,
+                                        Stage stage) {
+  typedef Kept<E, CODES, WM> K;
+  constexpr int RL = 32 * WM, NB = K::I / K::PB;
+  const int fc = lane % K::FC, f = f0 + 8 * fc;
+  K first, other;
+  first.fetch(e, lane, n0, 0, f0);
+  __syncthreads();     // every wave is done with the operand stages
 #pragma unroll
-  for (int j = 0; j < 8; ++j) v[j] = (float)(int8_t)(w[j >> 2] >> (8 * (j & 3))) * step;
-}
-// rows n0 .. n0 + 31 of "dh": 32 WM features from f0, all there, kept as codes
-template <class E, int WM, int ACT>
-__device__ __forceinline__ void dh_codes(const float* s, int lane, const GEpi& e, int n0, int f0,
-                                         const KeptCodes<WM>& k) {
-  constexpr int RL = 32 * WM, FC = 4 * WM;
-  const int fc = lane % FC, f = f0 + 8 * fc;
+  for (int b = 0; b < WN; ++b) {
+    stage(b);
 #pragma unroll
-  for (int i = 0; i < FC / 2; ++i) {
-    const int r = (lane + 64 * i) / FC;
-    float d[8], g[8], u[8];
-    staged8<RL>(s, r, 2 * fc, d);
-    codes8(k.g[i], code_step(k.sg[i]), g);
-    codes8(k.u[i], code_step(k.su[i]), u);
-    dh_chunk<E, ACT, true>(e, n0 + r, f, 8, d, g, u);
-    __builtin_amdgcn_sched_barrier(0);     // (more of them at once take registers)
+    for (int q = 0; q < NB; ++q) {
+      const int t = b * NB + q;
+      K &k = t & 1 ? other : first, &next = t & 1 ? first : other;
+      if (t + 1 < WN * NB) next.fetch(e, lane, n0 + 32 * ((t + 1) / NB), (t + 1) % NB * K::PB, f0);
+#pragma unroll
+      for (int i = 0; i < K::PB; ++i) {
+        const int r = (lane + 64 * (q * K::PB + i)) / K::FC;
+        float d[8], g[8], u[8];
+        staged8<RL>(s, r, 2 * fc, d);
+        k.value(k.g[i], k.sg[i], g);
+        k.value(k.u[i], k.su[i], u);
+        dh_chunk<E, ACT, true>(e, n0 + 32 * b + r, f, 8, d, g, u);
+        __builtin_amdgcn_sched_barrier(0);     // (more of them at once take registers)
+      }
+    }
+    staged_fence();
   }
 }
-// the same of any rows below Np and any features
+// 32 rows from n0 of "dh", any below Np and of any features
 template <class E, int WM, int ACT>
 __device__ __forceinline__ void dh_rows(const float* s, int lane, const GEpi& e, int n0, int f0,
                                         int Np) {
@@ -337,14 +375,10 @@ __device__ __forceinline__ void ggemm_body(const GGemm& s, const GEpi& e) {
   float* const mine = (float*)lds + wave * 32 * RL;
   const bool parts = (MODE == DOWN || MODE == DX || MODE == DW) && e.part;
   float* const part = parts ? e.part + (size_t)tz * gy * RN * e.ldp : nullptr;
-  // whether all of the wave's rows and features exist
-  const int fw = MODE == UP ? mt / 2 : mt, fn = MODE == UP ? 16 * WM : 32 * WM;
-  const bool full = (MODE == UP || MODE == DH) && nt + 32 * WN <= e.T && fw + fn <= e.F;
-  const bool ahead = MODE == DH && full && e.keep == KEEP_CODES;
-  KeptCodes<MODE == DH ? WM : 1> kept[MODE == DH ? WN : 1];
-  if constexpr (MODE == DH) {
-    if (ahead) kept[0].fetch(e, lane, nt, mt);
-  }
+  // whether all of the tile's rows and features exist
+  const int fw = MODE == UP ? mt / 2 : mt;
+  const bool full = (MODE == UP || MODE == DH) && n0 + RN <= e.T &&
+                    (MODE == UP ? (m0 + RM) / 2 : m0 + RM) <= e.F;
   // scales of the lane's columns of codes
   float sm[8], sm1[8];
   if constexpr (sizeof(E) == 1) {
@@ -357,7 +391,6 @@ __device__ __forceinline__ void ggemm_body(const GGemm& s, const GEpi& e) {
       get(e.sm + m, sm, e.mout - m);
     }
   }
-  __syncthreads();     // every wave is done with the operand stages
   // the sums of 32 rows to the wave's own region, whose LDS operations stay in order
   auto stage = [&](int b) {
 #pragma unroll
@@ -374,6 +407,7 @@ __device__ __forceinline__ void ggemm_body(const GGemm& s, const GEpi& e) {
       }
     staged_fence();
   };
+  if constexpr (MODE != DH) __syncthreads();     // every wave is done with the operand stages
   if constexpr (MODE == UP) {
 #pragma unroll
     for (int b = 0; b < WN; ++b) {
@@ -383,14 +417,18 @@ __device__ __forceinline__ void ggemm_body(const GGemm& s, const GEpi& e) {
       staged_fence();
     }
   } else if constexpr (MODE == DH) {
+    if (full && e.keep == KEEP_CODES) {
+      dh_full<E, true, WM, WN, ACT>(mine, lane, e, nt, mt, stage);
+    } else if (full) {
+      dh_full<E, false, WM, WN, ACT>(mine, lane, e, nt, mt, stage);
+    } else {
+      __syncthreads();
 #pragma unroll
-    for (int b = 0; b < WN; ++b) {
-      stage(b);
-      // (what is kept of the next rows is on its way meanwhile)
-      if (ahead && b + 1 < WN) kept[b + 1 < WN ? b + 1 : 0].fetch(e, lane, nt + 32 * b + 32, mt);
-      if (ahead) dh_codes<E, WM, ACT>(mine, lane, e, nt + 32 * b, mt, kept[b]);
-      else dh_rows<E, WM, ACT>(mine, lane, e, nt + 32 * b, mt, s.N);
-      staged_fence();
+      for (int b = 0; b < WN; ++b) {
+        stage(b);
+        dh_rows<E, WM, ACT>(mine, lane, e, nt + 32 * b, mt, s.N);
+        staged_fence();
+      }
     }
   } else {
 #pragma unroll
@@ -416,16 +454,22 @@ __device__ __forceinline__ void ggemm_body(const GGemm& s, const GEpi& e) {
 }  // namespace hfk
 
 
-// Kernels of a product: big: 256 x 256 tiles, 8 waves of 128 x 64; else 128 x 128,
-// 4 waves of 64 x 64
-#define HF_GGEMM(NAME, E, O, MODE, ACT)                                                \
+// Kernels of a product: big: 256 x 256 tiles, 8 waves of 128 x 64; n64: 128 x 64, 4
+// waves of 64 x 32, with three K blocks on their way, for few rows; else 128 x 128, 4
+// waves of 64 x 64
+#define HF_GGEMM_WIDE(NAME, E, O, MODE, ACT)                                           \
   extern "C" __global__ __launch_bounds__(512, 1) void NAME##_big(GGemm s, GEpi e) {   \
     ggemm_body<E, O, MODE, ACT, 4, 2, 2, 4, 2>(s, e);                                  \
   }                                                                                    \
   extern "C" __global__ __launch_bounds__(256, 2) void NAME(GGemm s, GEpi e) {         \
     ggemm_body<E, O, MODE, ACT, 2, 2, 2, 2, 2>(s, e);                                  \
   }
-#define HF_GK(NAME) {NAME, NAME##_big}
+#define HF_GGEMM(NAME, E, O, MODE, ACT)                                                \
+  HF_GGEMM_WIDE(NAME, E, O, MODE, ACT)                                                 \
+  extern "C" __global__ __launch_bounds__(256, 2) void NAME##_n64(GGemm s, GEpi e) {   \
+    ggemm_body<E, O, MODE, ACT, 2, 1, 2, 2, 3>(s, e);                                  \
+  }
+#define HF_GK(NAME) {NAME, NAME##_big, NAME##_n64}
 // The kernels with an activation, a source file for each: "up" by type, "dh" by type
 #define HF_GATED_ACT(SUF, ACT)                                                         \
   namespace hfk {                                                                      \

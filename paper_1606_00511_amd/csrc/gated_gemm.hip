@@ -8,7 +8,8 @@ namespace hfk {
   HF_GGEMM(NAME##_bf16, bf16_t, bf16_t, MODE, GA_RELU)
 HF_GGEMM_T(hf_gated_down, DOWN)
 HF_GGEMM_T(hf_gated_dx, DX)
-HF_GGEMM_T(hf_gated_dw, DW)
+HF_GGEMM_WIDE(hf_gated_dw_f32, float, float, DW, GA_RELU)
+HF_GGEMM_WIDE(hf_gated_dw_bf16, bf16_t, bf16_t, DW, GA_RELU)
 HF_GGEMM(hf_gated_down_codes_f32, int8_t, float, DOWN, GA_RELU)
 HF_GGEMM(hf_gated_down_codes_bf16, int8_t, bf16_t, DOWN, GA_RELU)
 
@@ -26,7 +27,7 @@ const GActKernels& act_kernels(int act) {
     default: return gated_gelu_tanh;
   }
 }
-void launch(const Launch& L, const char* name, const GKernel (&k)[2], const GGemm& g,
+void launch(const Launch& L, const char* name, const GKernel (&k)[3], const GGemm& g,
             const GEpi& e) {
   if (g.M <= g.m0 || g.N < 1) return;
   const int RM = tile_m(g.tile), RN = tile_n(g.tile);
@@ -45,16 +46,17 @@ void gated_dh(const Launch& L, int type, const GGemm& g, const GEpi& e) {
   launch(L, "hf_gated_dh", act_kernels(e.act).dh[type], g, e);
 }
 void gated_down(const Launch& L, int type, int out_type, const GGemm& g, const GEpi& e) {
-  static const GKernel k[2][2] = {HF_GK(hf_gated_down_f32), HF_GK(hf_gated_down_bf16)};
-  static const GKernel c[2][2] = {HF_GK(hf_gated_down_codes_f32), HF_GK(hf_gated_down_codes_bf16)};
+  static const GKernel k[2][3] = {HF_GK(hf_gated_down_f32), HF_GK(hf_gated_down_bf16)};
+  static const GKernel c[2][3] = {HF_GK(hf_gated_down_codes_f32), HF_GK(hf_gated_down_codes_bf16)};
   launch(L, "hf_gated_down", type == VT_I8 ? c[out_type] : k[type], g, e);
 }
 void gated_dx(const Launch& L, int type, const GGemm& g, const GEpi& e) {
-  static const GKernel k[2][2] = {HF_GK(hf_gated_dx_f32), HF_GK(hf_gated_dx_bf16)};
+  static const GKernel k[2][3] = {HF_GK(hf_gated_dx_f32), HF_GK(hf_gated_dx_bf16)};
   launch(L, "hf_gated_dx", k[type], g, e);
 }
 void gated_dw(const Launch& L, int type, const GGemm& g, const GEpi& e) {
-  static const GKernel k[2][2] = {HF_GK(hf_gated_dw_f32), HF_GK(hf_gated_dw_bf16)};
+  static const GKernel k[2][3] = {{hf_gated_dw_f32, hf_gated_dw_f32_big},
+                                  {hf_gated_dw_bf16, hf_gated_dw_bf16_big}};
   launch(L, "hf_gated_dw", k[type], g, e);
 }
 

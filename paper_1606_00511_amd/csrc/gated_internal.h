@@ -57,7 +57,7 @@ struct GEpi {
 // The kernels with an activation, by type and tile (VT_*, TILE_*).
 typedef void (*GKernel)(GGemm, GEpi);
 struct GActKernels {
-  GKernel up[3][2], dh[2][2];
+  GKernel up[3][3], dh[2][3];
 };
 
 // h = phi(X Wg^T) * (X Wu^T): A = Wg, A1 = Wu (rows alim), B = X; M = 2 Fp

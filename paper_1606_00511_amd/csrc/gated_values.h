@@ -82,12 +82,15 @@ __device__ __forceinline__ int put_codes(int8_t* p, const float (&v)[8], int hav
   big = max(big, (uint32_t)__shfl_xor((int)big, 2, 64));
   const int byte = block_byte(__uint_as_float(big));
   const float f = byte == 255 ? 0.0f : code_factor(byte);
+  // (bytes of the code + 128, and then their highest bits turned)
   uint32_t w[2] = {0u, 0u};
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
-    const int q = byte == 255 ? 0 : (int)rintf(v[j] * f);
-    w[j >> 2] |= (uint32_t)(q & 255) << (8 * (j & 3));
+    const float q = byte == 255 ? 0.0f : rintf(v[j] * f);
+    w[j >> 2] = __builtin_amdgcn_cvt_pk_u8_f32(q + 128.0f, j & 3, w[j >> 2]);
   }
+  w[0] ^= 0x80808080u;
+  w[1] ^= 0x80808080u;
   if (have >= 8) {
     __builtin_memcpy(p, w, 8);
   } else {

@@ -36,10 +36,11 @@ constexpr double RATE[3][4] = {{0.24e6, 0.27e6, 0.22e6, 0.21e6},
                                {3.5e6, 4.8e6, 2.9e6, 2.2e6}};
 constexpr double BYTES_US = 4.7e6, L2_US = 15e6;
 constexpr double AHEAD[4] = {16384, 32768, 32768, 49152};
-inline Shape shape_for(int type, int64_t M, int64_t N, int64_t K, bool split, bool few) {
+// shapes: how many of the tiles TILE_* there are (2 .. 4; those of few rows from 3 on)
+inline Shape shape_for(int type, int64_t M, int64_t N, int64_t K, bool split, int shapes) {
   Shape best = {0, 1, 1e300};
   const int es = type == VT_F32 ? 4 : type == VT_BF16 ? 2 : 1;
-  for (int tile = 0; tile < (few && N <= FEW_ROWS ? 4 : 2); ++tile) {
+  for (int tile = 0; tile < (N <= FEW_ROWS ? shapes : 2); ++tile) {
     const int64_t RM = tile_m(tile), RN = tile_n(tile);
     const int64_t tm = (M + RM - 1) / RM, tn = (N + RN - 1) / RN, tiles = tm * tn;
     const int64_t slots = tile == TILE_BIG ? 256 : 512;

@@ -227,7 +227,7 @@ void head(hf_vocab* c, VRows r, const void* X, int64_t ldx, const void* W, int64
   float* z = (g && !f16) || lists ? c->at<float>(l.z) : nullptr;
   void* d = !g ? nullptr : dup ? (void*)(z + (size_t)T * ldd) : c->at<void>(l.z);
   const int sstep = std::min(wrows, vc);
-  const int tile = shape_for(type, sstep, T, Dp, false, !(g && f16)).tile;
+  const int tile = shape_for(type, sstep, T, Dp, false, g && f16 ? 2 : 4).tile;
   const int sg = tile_stat(tile);
   const int tiles = (V + sg - 1) / sg;
   VEpi e = {};
@@ -319,7 +319,7 @@ void head(hf_vocab* c, VRows r, const void* X, int64_t ldx, const void* W, int64
         q.T = T;
         q.dyn = 1;
         q.splits = 1;
-        q.tile = shape_for(type, n, T, Dp, false, false).tile;
+        q.tile = shape_for(type, n, T, Dp, false, 2).tile;
         VEpi pe = {};
         pe.zscale = 1.0f / r.tau;
         pe.lse = lse;
@@ -342,7 +342,7 @@ void head(hf_vocab* c, VRows r, const void* X, int64_t ldx, const void* W, int64
       q.st = r.st;
       q.dyn = dup ? 0 : 1;
       if (v0 == 0) {
-        xs = shape_for(type, D, xrows, n, true, true);
+        xs = shape_for(type, D, xrows, n, true, 4);
         xmax = (int)std::min<int64_t>(VMAX_SPLITS, n / 256);
         xe.part = partx;
         xe.ldp = Dp;
@@ -377,7 +377,7 @@ void head(hf_vocab* c, VRows r, const void* X, int64_t ldx, const void* W, int64
     Shape ws = {TILE_SMALL, 1, 0.0}, rest = ws;
     int n1 = pn;
     if (!q.thin) {
-      ws = shape_for(type, D, pn, q.K, true, false);
+      ws = shape_for(type, D, pn, q.K, true, 2);
       // a last round of few tiles leaves most units idle: its rows of dW are a
       // product of their own then, of a shape of their own (788 tiles of 256, K
       // = 2,251: 310 -> 282 us)
@@ -387,8 +387,8 @@ void head(hf_vocab* c, VRows r, const void* X, int64_t ldx, const void* W, int64
         const int64_t slots = tile == TILE_BIG ? 256 : 512;
         const int64_t whole = tm * ((pn + rn - 1) / rn) / slots * slots / tm * rn;
         if (whole <= 0 || whole >= pn) continue;
-        const Shape a = shape_for(type, D, whole, q.K, true, false);
-        const Shape b = shape_for(type, D, pn - whole, q.K, true, false);
+        const Shape a = shape_for(type, D, whole, q.K, true, 2);
+        const Shape b = shape_for(type, D, pn - whole, q.K, true, 2);
         if (a.us + b.us + 4.0 < least) {
           least = a.us + b.us + 4.0;
           ws = a;

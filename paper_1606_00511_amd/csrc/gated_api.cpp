@@ -23,6 +23,11 @@ namespace {
 constexpr int TWO_TERM_ROWS = 128;
 constexpr size_t WPACK_BYTES = (size_t)64 << 20;   // packed channels of a product of codes
 
+// Elements (bytes, of codes) between the rows of h, dg and du and of codes, past
+// their widths: with rows a power of two apart the 16 rows of a load, and the
+// loads of all workgroups, fall on one channel of the caches.
+constexpr int LD_GAP = 64, LD_GAP_CODES = 128;
+
 struct Layout {
   size_t part, wg, wu, wd;                    // every call
   size_t xp, yp, xt, yt, h, dgu;              // forward, gradient
@@ -41,6 +46,10 @@ struct hf_gated : hfk::CallContext {
 
   template <class T>
   T* at(size_t off) const { return reinterpret_cast<T*>(ws + off); }
+  size_t ldh() const { return Fp + LD_GAP; }
+  size_t ldgu() const { return 2 * Fp + LD_GAP; }
+  size_t ldxq() const { return Dc + LD_GAP_CODES; }
+  size_t ldhq() const { return Fc + LD_GAP_CODES; }
 };
 
 namespace {
@@ -72,14 +81,14 @@ void plan(const hf_gated* c, int64_t R, Layout* l) {
   l->yp = take(rk * Dp * es);
   l->xt = take(64 * Dp * es);
   l->yt = take(64 * Dp * es);
-  l->h = take(rk * Fp * es);
-  l->dgu = take(rk * 2 * Fp * es);
+  l->h = take(rk * c->ldh() * es);
+  l->dgu = take(rk * c->ldgu() * es);
   off = start;
-  l->xq = take(r * Dc);
+  l->xq = take(r * c->ldxq());
   l->sx = take(r * 4);
   l->hf = take(r * Fc * 4);
   l->hmax = take(std::max(r * (Fp / 32), std::min<size_t>(r, FEW_X) * (Fp / 16)) * 4);
-  l->hq = take(r * Fc);
+  l->hq = take(r * c->ldhq());
   l->sh = take(r * 4);
   off = start;
   l->aq = take(r * std::max(Dc, Fc));
@@ -186,8 +195,8 @@ void set_out(GEpi* e, void* out, int64_t ldo, int64_t rows, int cols) {
 }
 // A product in one launch or two, by their estimated time: a last round of few tiles
 // leaves most units idle, and its columns are then a launch of their own, of a shape
-// of their own.  run(g) launches columns [g.m0, g.M); shapes: 3, or 2 without tiles of
-// 64 rows.
+// of their own.  run(g) launches columns [g.m0, g.M); shapes: how many of the tiles
+// the product has.
 template <class Run>
 void ranged(GGemm g, int type, bool split, int shapes, Run run) {
   const int64_t M = g.M, N = g.N, K = g.K;
@@ -340,12 +349,20 @@ int hf_gated_forward(hf_gated* c, const void* X, int64_t ldx, const void* Wg, in
     GEpi eu = epilogue(c, T), ed = epilogue(c, T);
     operands(&gu, Wg, Wu, ldg, X, ldx);
     eu.h = c->at<void>(l.h);
-    eu.ldh = Fp;
+    eu.ldh = c->ldh();
     eu.dup = ed.dup = T <= TWO_X ? TWO_X : 0;
     gated_few_up(L, c->type, gu, eu);
-    operands(&gd, Wd, nullptr, ldd, eu.h, Fp);
     set_out(&ed, Y, ldy, T, D);
-    gated_few_down(L, c->type, c->type, gd, ed);
+    if (T > TWO_X && D == Dp && F == Fp && loads16(Wd, ldd, es)) {
+      // (each row of h once for 128 of Wd's: 24 rows, 4,096 x 16,384: 45 -> 33 us)
+      operands(&gd, Wd, nullptr, ldd, eu.h, eu.ldh);
+      summed(c, L, c->type, c->type, gd, ed, 0, 4, [&](const GGemm& g, const GEpi& e) {
+        gated_down(L, c->type, c->type, g, e);
+      });
+    } else {
+      operands(&gd, Wd, nullptr, ldd, eu.h, eu.ldh);
+      gated_few_down(L, c->type, c->type, gd, ed);
+    }
     return end(c);
   }
   const int dup = two_term(c, T);
@@ -365,7 +382,7 @@ int hf_gated_forward(hf_gated* c, const void* X, int64_t ldx, const void* Wg, in
   gated_pad(L, pads.all);
 
   eu.h = c->at<void>(l.h);
-  eu.ldh = Fp;
+  eu.ldh = c->ldh();
   eu.dup = dup;
   eu.keep = keep;
   eu.kept = kept;
@@ -375,9 +392,9 @@ int hf_gated_forward(hf_gated* c, const void* X, int64_t ldx, const void* Wg, in
   ranged(gu, c->type, false, 3, [&](const GGemm& g) { gated_up(L, c->type, g, eu); });
 
   gd.B = eu.h;
-  gd.ldb = Fp;
+  gd.ldb = c->ldh();
   set_out(&ed, Y, ldy, T, D);
-  summed(c, L, c->type, c->type, gd, ed, dup, 3, [&](const GGemm& g, const GEpi& e) {
+  summed(c, L, c->type, c->type, gd, ed, dup, 4, [&](const GGemm& g, const GEpi& e) {
     gated_down(L, c->type, c->type, g, e);
   });
   return end(c);
@@ -484,9 +501,9 @@ int hf_gated_grad(hf_gated* c, const void* X, int64_t ldx, const uint8_t* xscale
 
   GEpi eh = epilogue(c, T), ex = epilogue(c, T);
   eh.h = c->at<void>(l.h);
-  eh.ldh = Fp;
+  eh.ldh = c->ldh();
   eh.dgu = c->at<void>(l.dgu);
-  eh.lddgu = 2 * Fp;
+  eh.lddgu = c->ldgu();
   eh.dup = dup;
   eh.keep = keep;
   eh.kept = const_cast<void*>(kept);
@@ -500,13 +517,13 @@ int hf_gated_grad(hf_gated* c, const void* X, int64_t ldx, const uint8_t* xscale
     gx.ldb = eh.lddgu;
     gx.kh = Fp;
     set_out(&ex, dX, lddx, T, D);
-    summed(c, L, type, type, gx, ex, dup, 3,
+    summed(c, L, type, type, gx, ex, dup, 4,
            [&](const GGemm& g, const GEpi& e) { gated_dx(L, type, g, e); });
   }
   auto dw = [&](const GGemm& g, const GEpi& e) { gated_dw(L, type, g, e); };
   if (dWd) {
     gd.A = eh.h;
-    gd.lda = Fp;
+    gd.lda = c->ldh();
     summed(c, L, type, type, gd, ed, 0, 2, dw);
   }
   if (ew.out) {
@@ -582,7 +599,8 @@ int hf_gated_product(hf_gated* c, const int8_t* A, int64_t lda, const float* sa,
   const Launch L{c->stream, nullptr};
   const Layout& l = c->lay;
   const int T = (int)rows, K = (int)up(k, CPAD);
-  if (T <= FEW_X) {
+  const bool place = k % CPAD == 0 && loads16(B, ldb, 1);
+  if (T <= (place ? TWO_X : FEW_X)) {
     GGemm g = product((int)n, T, (int)k);
     GEpi e = epilogue(c, T);
     operands(&g, B, nullptr, ldb, A, lda);
@@ -592,7 +610,6 @@ int hf_gated_product(hf_gated* c, const int8_t* A, int64_t lda, const float* sa,
     gated_few_down(L, VT_I8, c->type, g, e);
     return end(c);
   }
-  const bool place = k % CPAD == 0 && loads16(B, ldb, 1);
   // channels at a time: all where they are, or as many as are packed; tiles of
   // partials go by columns of 64
   const int64_t step = place ? n : std::max<int64_t>((int64_t)(WPACK_BYTES / (size_t)K) / 256 * 256, 256);
@@ -614,7 +631,7 @@ int hf_gated_product(hf_gated* c, const int8_t* A, int64_t lda, const float* sa,
     e.sn = sa;
     e.sm = sb + n0;
     set_out(&e, (char*)Y + n0 * c->es, ldy, T, nn);
-    summed(c, L, VT_I8, c->type, g, e, 0, 3, [&](const GGemm& gg, const GEpi& ee) {
+    summed(c, L, VT_I8, c->type, g, e, 0, 4, [&](const GGemm& gg, const GEpi& ee) {
       gated_down(L, VT_I8, c->type, gg, ee);
     });
   }
@@ -643,13 +660,15 @@ int hf_gated_forward_codes(hf_gated* c, const void* X, int64_t ldx, const int8_t
   int8_t* xq = c->at<int8_t>(l.xq);
   int8_t* hq = c->at<int8_t>(l.hq);
   float *sx = c->at<float>(l.sx), *sh = c->at<float>(l.sh);
-  const bool few = T <= FEW_X && ldg == ldu;
+  const bool few = T <= FEW_X && ldg == ldu, place = F == Fc && loads16(Wd, ldd, 1);
+  const bool few_down = few && (T <= TWO_X || !place);
   GGemm gu = few ? product(F, T, D) : product(2 * Fp, T, Dc);
-  GGemm gd = few ? product(D, T, F) : product(c->Dp, T, Fc);
+  GGemm gd = few_down ? product(D, T, F) : product(c->Dp, T, Fc);
   GEpi eu = epilogue(c, T), ed = epilogue(c, T);
+  gd.alim = D;
   if (few) {
-    operands(&gu, Wg, Wu, ldg, xq, Dc);
-    operands(&gd, Wd, nullptr, ldd, hq, Fc);
+    operands(&gu, Wg, Wu, ldg, xq, c->ldxq());
+    operands(&gd, Wd, nullptr, ldd, hq, c->ldhq());
   } else {
     Pads pads;
     const bool pair = D == Dc && ldg == ldu && loads16(Wg, ldg, 1) && loads16(Wu, ldu, 1);
@@ -657,15 +676,13 @@ int hf_gated_forward_codes(hf_gated* c, const void* X, int64_t ldx, const int8_t
     gu.A1 = pads.operand(pair, Wu, ldu, F, D, 1, c->at<void>(l.wu), F, Dc, 1, &gu.lda);
     gu.alim = F;
     gu.B = xq;
-    gu.ldb = Dc;
-    gd.A = pads.operand(F == Fc && loads16(Wd, ldd, 1), Wd, ldd, D, F, 1, c->at<void>(l.wd), D, Fc,
-                        1, &gd.lda);
-    gd.alim = D;
+    gu.ldb = c->ldxq();
+    gd.A = pads.operand(place, Wd, ldd, D, F, 1, c->at<void>(l.wd), D, Fc, 1, &gd.lda);
     gd.B = hq;
-    gd.ldb = Fc;
+    gd.ldb = c->ldhq();
     gated_pad(L, pads.all);
   }
-  gated_codes(L, c->type, X, ldx, T, D, xq, Dc, Dc, sx);
+  gated_codes(L, c->type, X, ldx, T, D, xq, c->ldxq(), Dc, sx);
   eu.sn = sx;
   eu.sm = sg;
   eu.sm1 = su;
@@ -678,14 +695,14 @@ int hf_gated_forward_codes(hf_gated* c, const void* X, int64_t ldx, const int8_t
   } else {
     ranged(gu, VT_I8, false, 3, [&](const GGemm& g) { gated_up(L, VT_I8, g, eu); });
   }
-  gated_codes_h(L, c->at<float>(l.hf), Fc, eu.hmax, eu.ldmax, T, F, hq, Fc, Fc, sh);
+  gated_codes_h(L, c->at<float>(l.hf), Fc, eu.hmax, eu.ldmax, T, F, hq, c->ldhq(), Fc, sh);
   ed.sn = sh;
   ed.sm = sd;
   set_out(&ed, Y, ldy, T, D);
-  if (few) {
+  if (few_down) {
     gated_few_down(L, VT_I8, c->type, gd, ed);
   } else {
-    summed(c, L, VT_I8, c->type, gd, ed, 0, 3, [&](const GGemm& g, const GEpi& e) {
+    summed(c, L, VT_I8, c->type, gd, ed, 0, 4, [&](const GGemm& g, const GEpi& e) {
       gated_down(L, VT_I8, c->type, g, e);
     });
   }

@@ -469,7 +469,14 @@ __device__ __forceinline__ void ggemm_body(const GGemm& s, const GEpi& e) {
   extern "C" __global__ __launch_bounds__(256, 2) void NAME##_n64(GGemm s, GEpi e) {   \
     ggemm_body<E, O, MODE, ACT, 2, 1, 2, 2, 3>(s, e);                                  \
   }
+// and n32: 128 x 32, a wave having 32 of the matrix's rows, with four K blocks on their way
+#define HF_GGEMM_FEW(NAME, E, O, MODE, ACT)                                            \
+  HF_GGEMM(NAME, E, O, MODE, ACT)                                                      \
+  extern "C" __global__ __launch_bounds__(256, 2) void NAME##_n32(GGemm s, GEpi e) {   \
+    ggemm_body<E, O, MODE, ACT, 1, 1, 4, 1, 4>(s, e);                                  \
+  }
 #define HF_GK(NAME) {NAME, NAME##_big, NAME##_n64}
+#define HF_GK_FEW(NAME) {NAME, NAME##_big, NAME##_n64, NAME##_n32}
 // The kernels with an activation, a source file for each: "up" by type, "dh" by type
 #define HF_GATED_ACT(SUF, ACT)                                                         \
   namespace hfk {                                                                      \

@@ -141,9 +141,12 @@ __device__ __forceinline__ RowScale row_scale(uint32_t big) {
   r.inv = 1.0f / r.ss;
   return r;
 }
+// (EVEN: all 8 are there; have, room: how many are, and how many are written)
+template <bool EVEN>
 __device__ __forceinline__ void put_row_codes(int8_t* p, const float (&v)[8], const RowScale& r,
                                               int have, int room) {
   if (r.f == 0.0f) have = 0;                   // (a row without codes)
+  else if (EVEN) have = 8;
   // x inv is off by less than 2^-15 of a step: only next to a border, 2^-13 of all
   // places, does it not tell the code (a branch for each number: 49 us for 8,192 rows
   // of 4,096, for 8 at once 32)
@@ -167,7 +170,7 @@ __device__ __forceinline__ void put_row_codes(int8_t* p, const float (&v)[8], co
         __builtin_amdgcn_fmed3f(q[j], -127.0f, 127.0f) + 128.0f, j & 3, w[j >> 2]);
   w[0] ^= 0x80808080u;
   w[1] ^= 0x80808080u;
-  if (room >= 8) {
+  if (EVEN || room >= 8) {
     __builtin_memcpy(p, w, 8);
   } else {
 #pragma unroll
@@ -190,8 +193,10 @@ __device__ __forceinline__ uint32_t group_max(uint32_t big) {
   }
   return big;
 }
-// A row by W waves, of a workgroup of 4.  C > 0: a lane's C chunks stay in registers
-// between the two passes (cols <= 512 W C); else the row is read twice.
+// A row by W waves, of a workgroup of 4.  C > 0: cols is a multiple of 8, and a lane's C
+// chunks stay in registers between the two passes (zcols <= 512 W C); else the row is
+// read twice.  (Chunks that may be cut are four times the code, which a row or two
+// wait for: 32 rows of 4,096 took 10.7 us with them and 4.6 without.)
 template <class E, int W, int C>
 __device__ __forceinline__ void codes_body(const E* X, long long ldx, int rows, int cols,
                                            int8_t* codes, long long ldc, int zcols, float* scale) {
@@ -208,7 +213,7 @@ __device__ __forceinline__ void codes_body(const E* X, long long ldx, int rows, 
       const int at = 8 * (t + 64 * W * i);
 #pragma unroll
       for (int j = 0; j < 8; ++j) keep[i][j] = 0.0f;
-      if (at < cols) get(x + at, keep[i], cols - at);
+      if (at < cols) get(x + at, keep[i], 8);
     }
 #pragma unroll
     for (int i = 0; i < C; ++i)
@@ -228,7 +233,7 @@ __device__ __forceinline__ void codes_body(const E* X, long long ldx, int rows, 
 #pragma unroll
     for (int i = 0; i < C; ++i) {
       const int at = 8 * (t + 64 * W * i);
-      if (at < zcols) put_row_codes(out + at, keep[i], r, cols - at, zcols - at);
+      if (at < zcols) put_row_codes<true>(out + at, keep[i], r, 8, 8);
     }
   } else {
     for (int at = 8 * t; at < zcols; at += 512 * W) {
@@ -236,7 +241,7 @@ __device__ __forceinline__ void codes_body(const E* X, long long ldx, int rows, 
 #pragma unroll
       for (int j = 0; j < 8; ++j) v[j] = 0.0f;
       if (at < cols) get(x + at, v, cols - at);
-      put_row_codes(out + at, v, r, cols - at, zcols - at);
+      put_row_codes<false>(out + at, v, r, cols - at, zcols - at);
     }
   }
 }
@@ -305,7 +310,7 @@ HF_FINISH(codes_bf16, int8_t, bf16_t)
   }                                                                                              \
   HF_ROW_CODES(hf_gated_codes_##SUF, E, 4, 0)                                                    \
   HF_ROW_CODES(hf_gated_codes_##SUF##_c1, E, 1, 2)                                               \
-  HF_ROW_CODES(hf_gated_codes_##SUF##_c4, E, 1, 8)                                               \
+  HF_ROW_CODES(hf_gated_codes_##SUF##_c4, E, 4, 2)                                               \
   HF_ROW_CODES(hf_gated_codes_##SUF##_c16, E, 4, 8)
 HF_CODES(f32, float)
 HF_CODES(bf16, bf16_t)
@@ -328,7 +333,7 @@ extern "C" __global__ __launch_bounds__(256) void hf_gated_codes_h(const float* 
     big = max(big, __float_as_uint(hmax[row * ldmax + i]));
   const RowScale r = row_scale(group_max<4>(big));
   if (at == 0) scale[row] = r.s;
-  if (at < zcols) put_row_codes(codes + row * ldc + at, v, r, cols - at, zcols - at);
+  if (at < zcols) put_row_codes<false>(codes + row * ldc + at, v, r, cols - at, zcols - at);
 }
 
 // ------------------------------------------------------------- launchers
@@ -407,15 +412,17 @@ void gated_unpack(const Launch& L, int type, const int8_t* codes, long long ldc,
 }
 
 namespace {
-// a row a wave, whose lanes hold 16 or 64 numbers of it, or 4 waves (8,192 rows of
-// 4,096, bf16: 39 us with 4 waves and two reads of a row, 24 with one)
+// a row by a wave or by 4, whose lanes hold up to 16 or 64 numbers of it; what no lane
+// can hold, or has cut chunks, is read twice (8,192 rows of 4,096, bf16: 39 us read
+// twice, 24 held)
 template <class E>
 void codes_of(const Launch& L, void (*const (&k)[4])(const E*, long long, int, int, int8_t*,
                                                      long long, int, float*),
               const E* X, long long ldx, int rows, int cols, int8_t* codes, long long ldc,
               int zcols, float* scale) {
-  const int i = zcols <= 1024 ? 1 : zcols <= 4096 ? 2 : zcols <= 16384 ? 3 : 0;
-  HF_LAUNCH("hf_gated_codes", k[i], i == 1 || i == 2 ? (rows + 3) / 4 : rows, 256, X, ldx, rows,
+  const bool even = cols % 8 == 0 && zcols % 8 == 0;
+  const int i = !even ? 0 : zcols <= 1024 ? 1 : zcols <= 4096 ? 2 : zcols <= 16384 ? 3 : 0;
+  HF_LAUNCH("hf_gated_codes", k[i], i == 1 ? (rows + 3) / 4 : rows, 256, X, ldx, rows,
             cols, codes, ldc, zcols, scale);
 }
 }  // namespace

@@ -83,7 +83,7 @@ __device__ __forceinline__ void finish_body(const GGemm& g, const GEpi& e, int d
 }
 
 // ------------------------------------------------------------- checkpoints
-template <class E>
+template <class E, bool STREAM>
 __device__ __forceinline__ void pack_body(const E* X, long long ldx, uint32_t total, int cols,
                                           uint32_t per, int8_t* codes, long long ldc,
                                           uint8_t* scale, long long lds) {
@@ -94,11 +94,11 @@ __device__ __forceinline__ void pack_body(const E* X, long long ldx, uint32_t to
   const int at = 8 * (int)c, have = cols - at;
   float v[8];
   get(X + (size_t)row * ldx + at, v, have);
-  const int byte = put_codes(codes + (size_t)row * ldc + at, v, have);
+  const int byte = put_codes<STREAM>(codes + (size_t)row * ldc + at, v, have);
   if ((c & 3) == 0) scale[(size_t)row * lds + c / 4] = (uint8_t)byte;
 }
 
-template <class E>
+template <class E, bool STREAM>
 __device__ __forceinline__ void unpack_body(const int8_t* codes, long long ldc,
                                             const uint8_t* scale, long long lds, uint32_t rows,
                                             int cols, E* X, long long ldx, uint32_t zrows,
@@ -113,7 +113,7 @@ __device__ __forceinline__ void unpack_body(const int8_t* codes, long long ldc,
   for (int j = 0; j < 8; ++j) v[j] = 0.0f;
   if (have > 0)
     get_codes(codes + (size_t)row * ldc + at, code_step(scale[(size_t)row * lds + c / 4]), v, have);
-  put(X + (size_t)to * ldx + at, v, zcols - at);
+  put<STREAM>(X + (size_t)to * ldx + at, v, zcols - at);
 }
 
 // --------------------------------------------------------- codes of rows
@@ -297,17 +297,23 @@ HF_FINISH(codes_bf16, int8_t, bf16_t)
       float* scale) {                                                                            \
     codes_body<E, W, C>(X, ldx, rows, cols, codes, ldc, zcols, scale);                           \
   }
-#define HF_CODES(SUF, E)                                                                         \
+#define HF_PACK(SUF, E, STREAM)                                                                  \
   extern "C" __global__ __launch_bounds__(256) void hf_gated_pack_##SUF(                         \
       const E* X, long long ldx, uint32_t total, int cols, uint32_t per, int8_t* codes,          \
       long long ldc, uint8_t* scale, long long lds) {                                            \
-    pack_body<E>(X, ldx, total, cols, per, codes, ldc, scale, lds);                              \
+    pack_body<E, STREAM>(X, ldx, total, cols, per, codes, ldc, scale, lds);                      \
   }                                                                                              \
   extern "C" __global__ __launch_bounds__(256) void hf_gated_unpack_##SUF(                       \
       const int8_t* codes, long long ldc, const uint8_t* scale, long long lds, uint32_t rows,    \
       int cols, E* X, long long ldx, uint32_t zrows, int zcols, uint32_t per, uint32_t total) {  \
-    unpack_body<E>(codes, ldc, scale, lds, rows, cols, X, ldx, zrows, zcols, per, total);        \
-  }                                                                                              \
+    unpack_body<E, STREAM>(codes, ldc, scale, lds, rows, cols, X, ldx, zrows, zcols, per,        \
+                           total);                                                               \
+  }
+HF_PACK(f32, float, false)
+HF_PACK(bf16, bf16_t, false)
+HF_PACK(f32_s, float, true)
+HF_PACK(bf16_s, bf16_t, true)
+#define HF_CODES(SUF, E)                                                                         \
   HF_ROW_CODES(hf_gated_codes_##SUF, E, 4, 0)                                                    \
   HF_ROW_CODES(hf_gated_codes_##SUF##_c1, E, 1, 2)                                               \
   HF_ROW_CODES(hf_gated_codes_##SUF##_c4, E, 4, 2)                                               \
@@ -389,11 +395,12 @@ void gated_pack(const Launch& L, int type, const void* X, long long ldx, long lo
   const uint32_t per = (uint32_t)((cols + CODE_BLOCK - 1) / CODE_BLOCK * (CODE_BLOCK / 8));
   const uint32_t total = (uint32_t)rows * per;      // below 2^31: 262,144 rows of 65,536
   if (!total) return;
+  const bool much = rows * cols > L3_BYTES / 4;
   if (type == VT_F32)
-    HF_LAUNCH("hf_gated_pack", hf_gated_pack_f32, (total + 255) / 256, 256, (const float*)X, ldx,
+    HF_LAUNCH("hf_gated_pack", (much ? hf_gated_pack_f32_s : hf_gated_pack_f32), (total + 255) / 256, 256, (const float*)X, ldx,
               total, cols, per, codes, ldc, scale, lds);
   else
-    HF_LAUNCH("hf_gated_pack", hf_gated_pack_bf16, (total + 255) / 256, 256, (const bf16_t*)X, ldx,
+    HF_LAUNCH("hf_gated_pack", (much ? hf_gated_pack_bf16_s : hf_gated_pack_bf16), (total + 255) / 256, 256, (const bf16_t*)X, ldx,
               total, cols, per, codes, ldc, scale, lds);
 }
 
@@ -403,11 +410,12 @@ void gated_unpack(const Launch& L, int type, const int8_t* codes, long long ldc,
   const uint32_t per = (uint32_t)((zcols + 7) / 8);
   const uint32_t total = (uint32_t)zrows * times * per;
   if (!total) return;
+  const bool much = rows * cols * (type == VT_F32 ? 4 : 2) > L3_BYTES / 2;
   if (type == VT_F32)
-    HF_LAUNCH("hf_gated_unpack", hf_gated_unpack_f32, (total + 255) / 256, 256, codes, ldc, scale,
+    HF_LAUNCH("hf_gated_unpack", (much ? hf_gated_unpack_f32_s : hf_gated_unpack_f32), (total + 255) / 256, 256, codes, ldc, scale,
               lds, (uint32_t)rows, cols, (float*)X, ldx, (uint32_t)zrows, zcols, per, total);
   else
-    HF_LAUNCH("hf_gated_unpack", hf_gated_unpack_bf16, (total + 255) / 256, 256, codes, ldc, scale,
+    HF_LAUNCH("hf_gated_unpack", (much ? hf_gated_unpack_bf16_s : hf_gated_unpack_bf16), (total + 255) / 256, 256, codes, ldc, scale,
               lds, (uint32_t)rows, cols, (bf16_t*)X, ldx, (uint32_t)zrows, zcols, per, total);
 }
 

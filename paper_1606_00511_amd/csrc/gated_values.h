@@ -9,19 +9,22 @@ namespace hfk {
 namespace {
 
 // 8 values to p, of any alignment, the first `have` of them, and from it
+// (STREAM: past the caches)
+template <bool STREAM = false>
 __device__ __forceinline__ void put(float* p, const float (&v)[8], int have) {
   if (have >= 8) {
-    put16<false>(p, __builtin_bit_cast(u32x4, f32x4{v[0], v[1], v[2], v[3]}));
-    put16<false>(p + 4, __builtin_bit_cast(u32x4, f32x4{v[4], v[5], v[6], v[7]}));
+    put16<STREAM>(p, __builtin_bit_cast(u32x4, f32x4{v[0], v[1], v[2], v[3]}));
+    put16<STREAM>(p + 4, __builtin_bit_cast(u32x4, f32x4{v[4], v[5], v[6], v[7]}));
   } else {
 #pragma unroll
     for (int j = 0; j < 8; ++j)
       if (j < have) p[j] = v[j];
   }
 }
+template <bool STREAM = false>
 __device__ __forceinline__ void put(bf16_t* p, const float (&v)[8], int have) {
   if (have >= 8) {
-    store_chunk<false>(p, v);
+    store_chunk<STREAM>(p, v);
   } else {
 #pragma unroll
     for (int j = 0; j < 8; ++j)
@@ -71,6 +74,7 @@ __device__ __forceinline__ void get_codes(const int8_t* p, float step, float (&v
 }
 // 8 values of a block of 32, which 4 neighbouring lanes share, to codes: their
 // scale byte; values past `have` count 0
+template <bool STREAM = false>
 __device__ __forceinline__ int put_codes(int8_t* p, const float (&v)[8], int have) {
   // (of magnitudes as whole numbers the largest: NaN is above all, where fmaxf
   // would lose it)
@@ -92,7 +96,10 @@ __device__ __forceinline__ int put_codes(int8_t* p, const float (&v)[8], int hav
   w[0] ^= 0x80808080u;
   w[1] ^= 0x80808080u;
   if (have >= 8) {
-    __builtin_memcpy(p, w, 8);
+    typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+    typedef u32x2 __attribute__((aligned(1))) loose;
+    if (STREAM) __builtin_nontemporal_store(u32x2{w[0], w[1]}, (loose*)p);
+    else *(loose*)p = u32x2{w[0], w[1]};
   } else {
 #pragma unroll
     for (int j = 0; j < 8; ++j)

@@ -509,6 +509,10 @@ class _RowContext:
     work on rows, its workspace, and the checks of tensors.  _prefix: of the C
     calls' names."""
 
+    # torch's current device and stream as plain numbers, where it gives them: a
+    # stream object takes 1.5 us to make, a small call 10
+    _device = _raw_stream = None
+
     def _open(self, h, ws_rows, device):
         """The context h's workspace for calls of ws_rows rows (None: max_rows)."""
         torch, L = self._torch, lib()
@@ -526,6 +530,8 @@ class _RowContext:
         with torch.cuda.device(self.device):
             self._check(getattr(L, self._prefix + "_set_workspace")(
                 h, self.workspace.data_ptr(), nbytes))
+        self._device = getattr(torch._C, "_cuda_getDevice", None)
+        self._raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
     # ------------------------------------------------------------- plumbing
     def _check(self, rc):
@@ -534,14 +540,17 @@ class _RowContext:
         return rc
 
     def _call(self, fn, *args):
-        cuda, L = self._torch.cuda, lib()
-        if cuda.current_device() != self.device.index:
+        cuda, L = self._torch.cuda, _lib or lib()
+        if self._device() != self.device.index if self._device else \
+                cuda.current_device() != self.device.index:
             with cuda.device(self.device):
                 return self._call(fn, *args)
-        current = cuda.current_stream(self.device.index)
-        stream = current.cuda_stream
+        if self._raw_stream:
+            stream = self._raw_stream(self.device.index)
+        else:
+            stream = cuda.current_stream(self.device.index).cuda_stream
         if stream != self._stream:
-            self.workspace.record_stream(current)
+            self.workspace.record_stream(cuda.current_stream(self.device.index))
             self._stream = None
             self._check(getattr(L, self._prefix + "_set_stream")(self._h, stream))
             self._stream = stream
@@ -562,7 +571,7 @@ class _RowContext:
         """(pointer, elements between rows) of a rows x cols tensor."""
         if not isinstance(t, self._torch.Tensor) or t.device != self.device:
             raise TypeError("%s must be a tensor on %s" % (what, self.device))
-        if t.dtype != dtype:
+        if t.dtype is not dtype:
             raise TypeError("%s must be %s, got %s" % (what, dtype, t.dtype))
         if t.shape != (rows, cols):
             raise ValueError("%s is %s, expected %d x %d"

@@ -610,9 +610,10 @@ int hf_gated_product(hf_gated* c, const int8_t* A, int64_t lda, const float* sa,
     gated_few_down(L, VT_I8, c->type, g, e);
     return end(c);
   }
-  // channels at a time: all where they are, or as many as are packed; tiles of
-  // partials go by columns of 64
-  const int64_t step = place ? n : std::max<int64_t>((int64_t)(WPACK_BYTES / (size_t)K) / 256 * 256, 256);
+  // channels at a time: of those where they are as many as a launch takes with the most
+  // rows (fewer than 2^32 work-items), or as many as are packed
+  const int64_t step = place ? (int64_t)1 << 19
+                             : std::max<int64_t>((int64_t)(WPACK_BYTES / (size_t)K) / 256 * 256, 256);
   long long ldaq = 0;
   const void* aq = nullptr;
   for (int64_t n0 = 0; n0 < n; n0 += step) {

@@ -30,7 +30,7 @@ constexpr int LD_GAP = 64, LD_GAP_CODES = 128;
 
 struct Layout {
   size_t part, wg, wu, wd;                    // every call
-  size_t xp, yp, xt, yt, h, dgu;              // forward, gradient
+  size_t xp, yp, xt, yt, h, dgu, gu;          // forward, gradient
   size_t xq, sx, hf, hmax, hq, sh;            // codes
   size_t aq, bq;                              // products of codes
   size_t need;
@@ -46,6 +46,12 @@ struct hf_gated : hfk::CallContext {
 
   template <class T>
   T* at(size_t off) const { return reinterpret_cast<T*>(ws + off); }
+  // of split products: of the three gradients' up to 8 splits
+  size_t part_floats(int64_t R) const {
+    const size_t out = (size_t)up(R, VTILE) * Dp + (size_t)up(Dp, VTILE) * Fp +
+                       (size_t)up(2 * Fp, VTILE) * Dp;
+    return std::max(SPLIT_FLOATS, std::min(8 * out, 2 * SPLIT_FLOATS));
+  }
   size_t ldh() const { return Fp + LD_GAP; }
   size_t ldgu() const { return 2 * Fp + LD_GAP; }
   size_t ldxq() const { return Dc + LD_GAP_CODES; }
@@ -70,7 +76,7 @@ void plan(const hf_gated* c, int64_t R, Layout* l) {
   const size_t Dp = c->Dp, Fp = c->Fp, Dc = c->Dc, Fc = c->Fc, es = c->es, r = (size_t)R;
   // rows of h, dg, du and of packed rows: whole K blocks, and of few rows both terms
   const size_t rk = (size_t)std::max(up(R, 64), 2 * up(std::min<int64_t>(R, TWO_TERM_ROWS), 64));
-  l->part = take(SPLIT_FLOATS * 4);
+  l->part = take(c->part_floats(R) * 4);
   // (as codes: a byte an element, up to 128)
   const size_t wbytes = std::max(Fp * Dp * es, std::max(Fp * Dc, Dp * Fc));
   l->wg = take(wbytes);
@@ -83,6 +89,7 @@ void plan(const hf_gated* c, int64_t R, Layout* l) {
   l->yt = take(64 * Dp * es);
   l->h = take(rk * c->ldh() * es);
   l->dgu = take(rk * c->ldgu() * es);
+  l->gu = take(std::min<size_t>(r, FEW_X) * 2 * Fp * 4);
   off = start;
   l->xq = take(r * c->ldxq());
   l->sx = take(r * 4);
@@ -154,7 +161,7 @@ struct Pads {
       return p;
     }
     *out_ld = pcols;
-    all.p[all.n++] = GPad{p, dst, ld, (int)rows, cols, (int)prows, pcols, times, es};
+    all.p[all.n++] = GPad{p, nullptr, 0, dst, ld, (int)rows, cols, (int)prows, pcols, times, es};
     return dst;
   }
 };
@@ -171,10 +178,12 @@ GGemm product(int M, int N, int K) {
   return g;
 }
 // operands that are read where they are
-void operands(GGemm* g, const void* A, const void* A1, int64_t lda, const void* B, int64_t ldb) {
+void operands(GGemm* g, const void* A, int64_t lda, const void* A1, int64_t lda1, const void* B,
+              int64_t ldb) {
   g->A = A;
   g->A1 = A1;
   g->lda = lda;
+  g->lda1 = lda1;
   g->B = B;
   g->ldb = ldb;
 }
@@ -193,6 +202,47 @@ void set_out(GEpi* e, void* out, int64_t ldo, int64_t rows, int cols) {
   e->nout = (int)rows;
   e->mout = cols;
 }
+// The tile and the splits of K of a product by its estimated time in us:
+//   products  RATE (see gemm_shape.h) a unit, of which two of the smaller tiles share
+//             one, and C_TILE to fill the LDS and store a tile
+//   units     a unit reads UNIT_BYTES a us (measured on 134 MB by 256 workgroups: 5
+//             TB/s, and what one alone reads)
+//   memory    both operands once
+// Partials are written and read again by a launch of its own, few of them in the
+// last-level cache.
+constexpr double UNIT_BYTES = 5.5e4, C_TILE[4] = {4.0, 6.0, 3.0, 3.0};
+inline int es_of(int type) { return type == VT_F32 ? 4 : type == VT_BF16 ? 2 : 1; }
+// one tile's time over k columns, `share` to a unit
+inline double tile_us(int type, int tile, double k, bool shared) {
+  const double rm = tile_m(tile), rn = tile_n(tile);
+  return std::max((shared ? 2.0 : tile == TILE_BIG ? 1.0 : 1.4) * rm * rn * k / RATE[type][tile],
+                  (shared ? 2.0 : 1.0) * (rm + rn) * k * es_of(type) / UNIT_BYTES) + C_TILE[tile];
+}
+inline double parts_us(double bytes) {
+  return bytes > 0.0 ? 4.0 + bytes / (bytes < 64e6 ? 2 * BYTES_US : BYTES_US) : 0.0;
+}
+constexpr int SPLITS[] = {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 48, 64};
+// of K a split takes at least so many columns
+inline int64_t split_k(int type) { return type == VT_F32 ? 64 : type == VT_BF16 ? 128 : 256; }
+Shape shape_of(int type, int64_t M, int64_t N, int64_t K, bool split, int shapes) {
+  Shape best = {0, 1, 1e300};
+  const double mem = (double)(M + N) * K * es_of(type) / BYTES_US + 4.0;
+  for (int tile = 0; tile < (N <= FEW_ROWS ? shapes : std::min(shapes, 2)); ++tile) {
+    const int64_t RM = tile_m(tile), RN = tile_n(tile), slots = tile == TILE_BIG ? 256 : 512;
+    const int64_t tiles = (M + RM - 1) / RM * ((N + RN - 1) / RN);
+    for (int s : SPLITS) {
+      if (s > 1 && (!split || K / s < split_k(type) ||
+                    (size_t)s * up(N, VTILE) * up(M, VPAD) > SPLIT_FLOATS))
+        break;
+      const double t = (double)((tiles * s + slots - 1) / slots) *
+                       tile_us(type, tile, (double)((K + s - 1) / s),
+                               tile != TILE_BIG && tiles * s > 256);
+      const double us = std::max(t, mem) + (s > 1 ? parts_us(8.0 * s * (double)M * N) : 0.0);
+      if (us < best.us) best = {tile, s, us};
+    }
+  }
+  return best;
+}
 // A product in one launch or two, by their estimated time: a last round of few tiles
 // leaves most units idle, and its columns are then a launch of their own, of a shape
 // of their own.  run(g) launches columns [g.m0, g.M); shapes: how many of the tiles
@@ -200,7 +250,7 @@ void set_out(GEpi* e, void* out, int64_t ldo, int64_t rows, int cols) {
 template <class Run>
 void ranged(GGemm g, int type, bool split, int shapes, Run run) {
   const int64_t M = g.M, N = g.N, K = g.K;
-  Shape a = shape_for(type, M, N, K, split, shapes), b = {};
+  Shape a = shape_of(type, M, N, K, split, shapes), b = {};
   int64_t m1 = M;
   double least = a.us;
   for (int tile : {TILE_BIG, TILE_SMALL}) {
@@ -208,8 +258,8 @@ void ranged(GGemm g, int type, bool split, int shapes, Run run) {
     const int64_t slots = tile == TILE_BIG ? 256 : 512;
     const int64_t whole = ((M + rm - 1) / rm * tn) / slots * slots / tn * rm;
     if (whole <= 0 || whole >= M) continue;
-    const Shape x = shape_for(type, whole, N, K, split, shapes);
-    const Shape y = shape_for(type, M - whole, N, K, split, shapes);
+    const Shape x = shape_of(type, whole, N, K, split, shapes);
+    const Shape y = shape_of(type, M - whole, N, K, split, shapes);
     if (x.us + y.us + 4.0 < least) {
       least = x.us + y.us + 4.0;
       a = x;
@@ -239,8 +289,91 @@ void summed(hf_gated* c, const Launch& L, int type, int out_type, const GGemm& a
       e.ldp = all.M;
     }
     kernel(g, e);
-    if (e.part) gated_finish(L, type, out_type, g, e, dup);
+    if (!e.part) return;
+    const GFinish f = {g, e, dup};
+    gated_finish(L, type, out_type, &f, 1);
   });
+}
+
+// The gradients' products: one tile for all of them, and splits of K, of about `per`
+// columns each, so that the units are done together.  A tile is launched when a unit has room for it, the longest first.
+struct Job {
+  int64_t M, N, K;
+  bool on, joined;       // joined: by partials even if there is one split
+};
+double makespan(int type, int tile, const Job (&j)[3], int64_t per, size_t room,
+                int (&splits)[3]) {
+  const int64_t RM = tile_m(tile), RN = tile_n(tile), slots = tile == TILE_BIG ? 256 : 512;
+  int64_t n[3] = {}, all = 0;
+  double t[3] = {}, part = 0.0, bytes = 0.0;
+  size_t floats = 0;
+  const int es = es_of(type);
+  for (int i = 0; i < 3; ++i) {
+    splits[i] = 1;
+    if (!j[i].on) continue;
+    splits[i] = (int)std::min<int64_t>((j[i].K + per - 1) / per, VMAX_SPLITS);
+    n[i] = (j[i].M + RM - 1) / RM * ((j[i].N + RN - 1) / RN) * splits[i];
+    t[i] = (double)((j[i].K + splits[i] - 1) / splits[i]);
+    all += n[i];
+    bytes += (double)es * (j[i].M * j[i].K + j[i].N * j[i].K + j[i].M * j[i].N);
+    if (splits[i] > 1 || j[i].joined) {
+      part += 8.0 * splits[i] * (double)j[i].M * j[i].N;
+      floats += (size_t)splits[i] * up(j[i].N, VTILE) * up(j[i].M, VPAD);
+    }
+  }
+  if (floats > room) return 1e300;
+  // the units' times, as a few groups that are equal
+  struct Group {
+    double at;
+    int64_t units;
+  } g[16] = {{0.0, slots}};
+  int k = 1;
+  double end = 0.0;
+  for (;;) {
+    int i = -1;
+    for (int c = 0; c < 3; ++c)
+      if (n[c] > 0 && (i < 0 || t[c] > t[i])) i = c;
+    if (i < 0) break;
+    int f = 0;
+    for (int c = 1; c < k; ++c)
+      if (g[c].at < g[f].at) f = c;
+    // (whole rounds at once while all units are equal)
+    const double one = tile_us(type, tile, t[i], tile != TILE_BIG && all > 256);
+    const int64_t rounds = k == 1 ? std::max<int64_t>(n[i] / slots, 1) : 1;
+    const int64_t take = std::min(n[i], g[f].units * rounds);
+    n[i] -= take;
+    const int64_t used = std::min(take, g[f].units);
+    const double at = g[f].at + one * (double)rounds;
+    end = std::max(end, at);
+    if (used == g[f].units || k == 16) g[f].at = at;
+    else {
+      g[f].units -= used;
+      g[k++] = {at, used};
+    }
+  }
+  return std::max(end, bytes / BYTES_US + 4.0) + parts_us(part);
+}
+void grads_shapes(int type, int dup, size_t room, GGrads* a) {
+  Job j[3];
+  int64_t K = 0;
+  for (int i = 0; i < 3; ++i) {
+    j[i] = {a->g[i].M, a->g[i].N, a->g[i].K, a->e[i].out != nullptr, i == 0 && dup};
+    if (j[i].on) K = std::max(K, j[i].K);
+  }
+  double best = 1e300;
+  for (int tile : {TILE_SMALL, TILE_BIG})
+    for (int q : {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 24, 32}) {
+      const int64_t per = up((K + q - 1) / q, 64);
+      if (q > 1 && per < split_k(type)) break;
+      int splits[3];
+      const double us = makespan(type, tile, j, per, room, splits);
+      if (us >= best) continue;
+      best = us;
+      for (int i = 0; i < 3; ++i) {
+        a->g[i].tile = tile;
+        a->g[i].splits = splits[i];
+      }
+    }
 }
 
 }  // namespace
@@ -344,23 +477,36 @@ int hf_gated_forward(hf_gated* c, const void* X, int64_t ldx, const void* Wg, in
   const Launch L{c->stream, nullptr};
   const Layout& l = c->lay;
   const int T = (int)rows, D = c->D, F = c->F, Dp = c->Dp, Fp = c->Fp, es = c->es;
-  if (T <= FEW_X && keep == HF_KEEP_NONE && ldg == ldu) {
+  if (T <= FEW_X) {
     GGemm gu = product(F, T, D), gd = product(D, T, F);
     GEpi eu = epilogue(c, T), ed = epilogue(c, T);
-    operands(&gu, Wg, Wu, ldg, X, ldx);
+    operands(&gu, Wg, ldg, Wu, ldu, X, ldx);
     eu.h = c->at<void>(l.h);
     eu.ldh = c->ldh();
     eu.dup = ed.dup = T <= TWO_X ? TWO_X : 0;
+    eu.keep = keep;
+    eu.kept = kept;
+    eu.ldk = ldk;
+    if (keep == HF_KEEP_CODES) {        // (a workgroup may have half a block of codes)
+      eu.kept = c->at<float>(l.gu);
+      eu.ldk = 2 * F;
+    }
     gated_few_up(L, c->type, gu, eu);
+    if (keep == HF_KEEP_CODES) {
+      int8_t* k = (int8_t*)kept;
+      gated_pack(L, VT_F32, eu.kept, 2 * F, T, F, k, ldk, scale, lds);
+      gated_pack(L, VT_F32, (const float*)eu.kept + F, 2 * F, T, F, k + F, ldk,
+                 scale + blocks_of(F), lds);
+    }
     set_out(&ed, Y, ldy, T, D);
     if (T > TWO_X && D == Dp && F == Fp && loads16(Wd, ldd, es)) {
       // (each row of h once for 128 of Wd's: 24 rows, 4,096 x 16,384: 45 -> 33 us)
-      operands(&gd, Wd, nullptr, ldd, eu.h, eu.ldh);
+      operands(&gd, Wd, ldd, nullptr, 0, eu.h, eu.ldh);
       summed(c, L, c->type, c->type, gd, ed, 0, 4, [&](const GGemm& g, const GEpi& e) {
         gated_down(L, c->type, c->type, g, e);
       });
     } else {
-      operands(&gd, Wd, nullptr, ldd, eu.h, eu.ldh);
+      operands(&gd, Wd, ldd, nullptr, 0, eu.h, eu.ldh);
       gated_few_down(L, c->type, c->type, gd, ed);
     }
     return end(c);
@@ -442,28 +588,36 @@ int hf_gated_grad(hf_gated* c, const void* X, int64_t ldx, const uint8_t* xscale
   const int T = (int)rows, D = c->D, F = c->F, Dp = c->Dp, Fp = c->Fp, es = c->es, type = c->type;
   const int dup = two_term(c, T);
   const int Tp = (int)up(T, 64), Kt = dup ? 2 * dup : Tp, T0 = T / 64 * 64;
-  // (no rows: the sum of nothing)
-  GGemm gd = product(Fp, Dp, Kt), gw = product(Dp, 2 * Fp, Kt);
-  GEpi ed = epilogue(c, T), ew = epilogue(c, T);
+  GGrads all = {};
+  GGemm &gx = all.g[0], &gd = all.g[1], &gw = all.g[2];
+  GEpi &ex = all.e[0], &ed = all.e[1], &ew = all.e[2];
+  gx = product(Dp, dup ? 2 * dup : T, 2 * Fp);
+  gd = product(Fp, Dp, Kt);
+  gw = product(Dp, dWg && dWu ? 2 * Fp : Fp, Kt);
+  ex = ed = ew = epilogue(c, T);
   ed.accumulate = ew.accumulate = accumulate;
+  set_out(&ex, dX, lddx, T, D);
   set_out(&ed, dWd, lddd, D, F);
   set_out(&ew, dWg ? dWg : dWu, dWg ? lddg : lddu, F, D);
-  if (!dWg || !dWu) gw.N = Fp;
   ew.n1 = dWg && dWu ? Fp : INT_MAX;
   ew.out1 = dWu;
   ew.ldo1 = lddu;
+  GFinish f[3];
+  int n = 0;
   if (T == 0) {
-    if (accumulate) return HF_OK;
-    gd.splits = gw.splits = 0;
-    if (dWd) gated_finish(L, type, type, gd, ed, 0);
-    if (ew.out) gated_finish(L, type, type, gw, ew, 0);
+    // the sum of nothing
+    for (int i = 1; i < 3 && !accumulate; ++i) {
+      all.g[i].splits = 0;
+      if (all.e[i].out) f[n++] = {all.g[i], all.e[i], 0};
+    }
+    gated_finish(L, type, type, f, n);
     return end(c);
   }
 
   Pads pads;
   const bool weights = D == Dp && F == Fp && ldg == ldu && loads16(Wg, ldg, es) &&
                        loads16(Wu, ldu, es) && loads16(Wd, ldd, es);
-  GGemm gh = product(Fp, Tp, Dp), gx = product(Dp, dup ? 2 * dup : T, 2 * Fp);
+  GGemm gh = product(Fp, Tp, Dp);
   gh.A = pads.operand(weights, Wd, ldd, D, F, es, c->at<void>(l.wd), Dp, Fp, 1, &gh.lda);
   if (dX) {
     gx.A = pads.operand(weights, Wg, ldg, F, D, es, c->at<void>(l.wg), Fp, Dp, 1, &gx.lda);
@@ -471,11 +625,11 @@ int hf_gated_grad(hf_gated* c, const void* X, int64_t ldx, const uint8_t* xscale
   }
   // rows of X and dY: whole K blocks (few bf16 rows: both copies), or where they
   // are, with the last block's in a copy
+  const int prows = dup ? dup : Tp, times = dup ? 2 : 1;
   auto rows_of = [&](const void* p, int64_t ld, size_t copy, size_t tail, bool need_k,
                      const void** at, long long* ldat, long long* out_ld) -> const void* {
     const bool place = D == Dp && loads16(p, ld, es) && !(dup && need_k);
-    const void* q = pads.operand(place, p, ld, T, D, es, c->at<void>(copy), dup ? dup : Tp, Dp,
-                                 dup ? 2 : 1, out_ld);
+    const void* q = pads.operand(place, p, ld, T, D, es, c->at<void>(copy), prows, Dp, times, out_ld);
     if (place && need_k && T % 64)
       *at = pads.operand(false, (const char*)p + (size_t)T0 * ld * es, ld, T - T0, D, es,
                          c->at<void>(tail), 64, Dp, 1, ldat);
@@ -486,20 +640,17 @@ int hf_gated_grad(hf_gated* c, const void* X, int64_t ldx, const uint8_t* xscale
   gd.B = gh.B;
   gd.ldb = gh.ldb;
   gd.ktail = gw.ktail = T0;
-  if (ew.out) {
-    if (xscale) {
-      gw.A = c->at<void>(l.xp);
-      gw.lda = Dp;
-    } else {
-      gw.A = rows_of(X, ldx, l.xp, l.xt, true, &gw.at, &gw.ldat, &gw.lda);
-    }
+  if (ew.out && xscale) {
+    gw.A = pads.operand(false, X, ldx, T, D, es, c->at<void>(l.xp), prows, Dp, times, &gw.lda);
+    GPad& p = pads.all.p[pads.all.n - 1];
+    p.scale = xscale;
+    p.lds = ldxs;
+  } else if (ew.out) {
+    gw.A = rows_of(X, ldx, l.xp, l.xt, true, &gw.at, &gw.ldat, &gw.lda);
   }
   gated_pad(L, pads.all);
-  if (ew.out && xscale)
-    gated_unpack(L, type, (const int8_t*)X, ldx, xscale, ldxs, T, D, c->at<void>(l.xp), Dp,
-                 dup ? dup : Tp, Dp, dup ? 2 : 1);
 
-  GEpi eh = epilogue(c, T), ex = epilogue(c, T);
+  GEpi eh = epilogue(c, T);
   eh.h = c->at<void>(l.h);
   eh.ldh = c->ldh();
   eh.dgu = c->at<void>(l.dgu);
@@ -510,27 +661,29 @@ int hf_gated_grad(hf_gated* c, const void* X, int64_t ldx, const uint8_t* xscale
   eh.ldk = ldk;
   eh.ks = const_cast<uint8_t*>(scale);
   eh.ldks = lds;
-  ranged(gh, type, false, 3, [&](const GGemm& g) { gated_dh(L, type, g, eh); });
+  ranged(gh, type, false, 4, [&](const GGemm& g) { gated_dh(L, type, g, eh); });
 
-  if (dX) {
-    gx.B = eh.dgu;
-    gx.ldb = eh.lddgu;
-    gx.kh = Fp;
-    set_out(&ex, dX, lddx, T, D);
-    summed(c, L, type, type, gx, ex, dup, 4,
-           [&](const GGemm& g, const GEpi& e) { gated_dx(L, type, g, e); });
+  gx.B = eh.dgu;
+  gx.ldb = eh.lddgu;
+  gx.kh = Fp;
+  gd.A = eh.h;
+  gd.lda = c->ldh();
+  gw.B = (const char*)eh.dgu + (dWg ? 0 : (size_t)Fp * es);
+  gw.ldb = eh.lddgu;
+  grads_shapes(type, dup, c->part_floats(c->Rws), &all);
+  float* part = c->at<float>(l.part);
+  for (int i = 0; i < 3; ++i) {
+    GGemm& g = all.g[i];
+    GEpi& e = all.e[i];
+    const int join = i == 0 ? dup : 0;
+    if (!e.out || (g.splits == 1 && !join)) continue;
+    e.part = part;
+    e.ldp = g.M;
+    part += (size_t)g.splits * up(g.N, VTILE) * g.M;
+    f[n++] = {g, e, join};
   }
-  auto dw = [&](const GGemm& g, const GEpi& e) { gated_dw(L, type, g, e); };
-  if (dWd) {
-    gd.A = eh.h;
-    gd.lda = c->ldh();
-    summed(c, L, type, type, gd, ed, 0, 2, dw);
-  }
-  if (ew.out) {
-    gw.B = (const char*)eh.dgu + (dWg ? 0 : (size_t)Fp * es);
-    gw.ldb = eh.lddgu;
-    summed(c, L, type, type, gw, ew, 0, 2, dw);
-  }
+  gated_grads(L, type, all);
+  gated_finish(L, type, type, f, n);
   return end(c);
 }
 
@@ -558,8 +711,7 @@ int hf_gated_unpack(hf_gated* c, const int8_t* codes, int64_t ldc, const uint8_t
       (rc = check_mat(c, X, ldx, cols, c->es, rows, "X")) ||
       (rc = check_apart(c, codes, "codes", X, "X", rows)))
     return rc;
-  gated_unpack(Launch{c->stream, nullptr}, c->type, codes, ldc, scale, lds, rows, (int)cols, X, ldx,
-               rows, (int)cols, 1);
+  gated_unpack(Launch{c->stream, nullptr}, c->type, codes, ldc, scale, lds, rows, (int)cols, X, ldx);
   return end(c);
 }
 
@@ -603,7 +755,7 @@ int hf_gated_product(hf_gated* c, const int8_t* A, int64_t lda, const float* sa,
   if (T <= (place ? TWO_X : FEW_X)) {
     GGemm g = product((int)n, T, (int)k);
     GEpi e = epilogue(c, T);
-    operands(&g, B, nullptr, ldb, A, lda);
+    operands(&g, B, ldb, nullptr, 0, A, lda);
     e.sn = sa;
     e.sm = sb;
     set_out(&e, Y, ldy, T, (int)n);
@@ -661,15 +813,15 @@ int hf_gated_forward_codes(hf_gated* c, const void* X, int64_t ldx, const int8_t
   int8_t* xq = c->at<int8_t>(l.xq);
   int8_t* hq = c->at<int8_t>(l.hq);
   float *sx = c->at<float>(l.sx), *sh = c->at<float>(l.sh);
-  const bool few = T <= FEW_X && ldg == ldu, place = F == Fc && loads16(Wd, ldd, 1);
+  const bool few = T <= FEW_X, place = F == Fc && loads16(Wd, ldd, 1);
   const bool few_down = few && (T <= TWO_X || !place);
   GGemm gu = few ? product(F, T, D) : product(2 * Fp, T, Dc);
   GGemm gd = few_down ? product(D, T, F) : product(c->Dp, T, Fc);
   GEpi eu = epilogue(c, T), ed = epilogue(c, T);
   gd.alim = D;
   if (few) {
-    operands(&gu, Wg, Wu, ldg, xq, c->ldxq());
-    operands(&gd, Wd, nullptr, ldd, hq, c->ldhq());
+    operands(&gu, Wg, ldg, Wu, ldu, xq, c->ldxq());
+    operands(&gd, Wd, ldd, nullptr, 0, hq, c->ldhq());
   } else {
     Pads pads;
     const bool pair = D == Dc && ldg == ldu && loads16(Wg, ldg, 1) && loads16(Wu, ldu, 1);

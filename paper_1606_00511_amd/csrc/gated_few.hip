@@ -80,9 +80,9 @@ __device__ __forceinline__ void few_body(const GGemm& s, const GEpi& e) {
   const E *a[NA], *x[NX];
 #pragma unroll
   for (int i = 0; i < RB; ++i) {
-    const size_t at = (size_t)min(m0 + 16 * i + l, s.alim - 1) * s.lda + EPC * q;
-    a[i] = (const E*)s.A + at;
-    if constexpr (UP) a[RB + i] = (const E*)s.A1 + at;
+    const size_t row = (size_t)min(m0 + 16 * i + l, s.alim - 1);
+    a[i] = (const E*)s.A + row * s.lda + EPC * q;
+    if constexpr (UP) a[RB + i] = (const E*)s.A1 + row * s.lda1 + EPC * q;
   }
 #pragma unroll
   for (int i = 0; i < NX; ++i)
@@ -179,6 +179,7 @@ __device__ __forceinline__ void few_body(const GGemm& s, const GEpi& e) {
     const int n = 16 * j + l, m = m0 + 16 * i + 4 * q;
     if constexpr (UP) {
       float v[4];
+      const bool keep = sizeof(E) != 1 && e.keep != KEEP_NONE && n < e.T;
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         const int mm = min(m + r, e.F - 1);
@@ -190,6 +191,17 @@ __device__ __forceinline__ void few_body(const GGemm& s, const GEpi& e) {
         } else {
           gr = g[r];
           ur = u[r];
+        }
+        if (keep && m + r < e.F) {
+          // (what becomes codes is kept in fp32)
+          const size_t at = (size_t)n * e.ldk + m + r;
+          if (sizeof(E) == 4 || e.keep == KEEP_CODES) {
+            ((float*)e.kept)[at] = gr;
+            ((float*)e.kept)[at + e.F] = ur;
+          } else {
+            store1((bf16_t*)e.kept + at, gr);
+            store1((bf16_t*)e.kept + at + e.F, ur);
+          }
         }
         v[r] = m + r < e.F ? act_of<act.value, sizeof(E) != 2>(gr) * ur : 0.0f;
       }
@@ -235,55 +247,70 @@ __device__ __forceinline__ void few_body(const GGemm& s, const GEpi& e) {
 
 }  // namespace
 
-// up to 16, 32 and 64 rows of X
-#define HF_FEW(NAME, E, O, UP, RB2, U2, TWO)                                                    \
+// up to 16, 32 and 64 rows of X; "up" with 16 rows of both matrices a workgroup, and of
+// more than 16 rows of X with 32 where that leaves no unit without a workgroup (half
+// the reads of X: 24 rows, 4,096 x 16,384: 63 -> 54 us; 28 rows, 2,981 x 3,115, fp32, 98
+// workgroups: 54 us, 195: 38)
+#define HF_FEW(NAME, E, O, UP, RB, U32)                                                         \
+  extern "C" __global__ __launch_bounds__(512) void NAME##_32(GGemm s, GEpi e) {                \
+    few_body<E, O, UP, RB, 2, U32, 8, false>(s, e);                                             \
+  }                                                                                             \
+  extern "C" __global__ __launch_bounds__(512) void NAME##_64(GGemm s, GEpi e) {                \
+    few_body<E, O, UP, RB, 4, 2, 8, false>(s, e);                                               \
+  }
+#define HF_FEW_ALL(NAME, E, O, UP, TWO)                                                         \
   extern "C" __global__ __launch_bounds__(1024) void NAME##_16(GGemm s, GEpi e) {               \
     few_body<E, O, UP, 1, 1, 4, 16, TWO>(s, e);                                                 \
   }                                                                                             \
-  extern "C" __global__ __launch_bounds__(512) void NAME##_32(GGemm s, GEpi e) {                \
-    few_body<E, O, UP, RB2, 2, U2, 8, false>(s, e);                                             \
-  }                                                                                             \
-  extern "C" __global__ __launch_bounds__(512) void NAME##_64(GGemm s, GEpi e) {                \
-    few_body<E, O, UP, RB2, 4, 2, 8, false>(s, e);                                              \
-  }
-HF_FEW(hf_gated_few_up_f32, float, float, true, 2, 2, false)
-HF_FEW(hf_gated_few_up_bf16, bf16_t, bf16_t, true, 2, 2, false)
-HF_FEW(hf_gated_few_up_codes, int8_t, float, true, 2, 2, false)
-HF_FEW(hf_gated_few_down_f32, float, float, false, 1, 4, false)
-HF_FEW(hf_gated_few_down_bf16, bf16_t, bf16_t, false, 1, 4, true)
-HF_FEW(hf_gated_few_down_codes_f32, int8_t, float, false, 1, 4, false)
-HF_FEW(hf_gated_few_down_codes_bf16, int8_t, bf16_t, false, 1, 4, false)
+  HF_FEW(NAME, E, O, UP, 1, 4)
+HF_FEW_ALL(hf_gated_few_up_f32, float, float, true, false)
+HF_FEW_ALL(hf_gated_few_up_bf16, bf16_t, bf16_t, true, false)
+HF_FEW_ALL(hf_gated_few_up_codes, int8_t, float, true, false)
+HF_FEW(hf_gated_few_up2_f32, float, float, true, 2, 2)
+HF_FEW(hf_gated_few_up2_bf16, bf16_t, bf16_t, true, 2, 2)
+HF_FEW(hf_gated_few_up2_codes, int8_t, float, true, 2, 2)
+HF_FEW_ALL(hf_gated_few_down_f32, float, float, false, false)
+HF_FEW_ALL(hf_gated_few_down_bf16, bf16_t, bf16_t, false, true)
+HF_FEW_ALL(hf_gated_few_down_codes_f32, int8_t, float, false, false)
+HF_FEW_ALL(hf_gated_few_down_codes_bf16, int8_t, bf16_t, false, false)
 
 namespace {
-typedef void (*FK)(GGemm, GEpi);
 #define HF_FK(NAME) {NAME##_16, NAME##_32, NAME##_64}
+#define HF_FK2(NAME) {nullptr, NAME##_32, NAME##_64}
 // by type (codes: and the output's) and rows
-const FK few_up[3][3] = {HF_FK(hf_gated_few_up_f32), HF_FK(hf_gated_few_up_bf16),
-                         HF_FK(hf_gated_few_up_codes)};
-const FK few_down[4][3] = {HF_FK(hf_gated_few_down_f32), HF_FK(hf_gated_few_down_bf16),
-                           HF_FK(hf_gated_few_down_codes_f32), HF_FK(hf_gated_few_down_codes_bf16)};
+const GKernel few_up[3][3] = {HF_FK(hf_gated_few_up_f32), HF_FK(hf_gated_few_up_bf16),
+                              HF_FK(hf_gated_few_up_codes)};
+const GKernel few_up2[3][3] = {HF_FK2(hf_gated_few_up2_f32), HF_FK2(hf_gated_few_up2_bf16),
+                               HF_FK2(hf_gated_few_up2_codes)};
+const GKernel few_down[4][3] = {HF_FK(hf_gated_few_down_f32), HF_FK(hf_gated_few_down_bf16),
+                                HF_FK(hf_gated_few_down_codes_f32),
+                                HF_FK(hf_gated_few_down_codes_bf16)};
+inline int size_of(int type) { return type == VT_F32 ? 4 : type == VT_BF16 ? 2 : 1; }
 
-void launch(const Launch& L, const char* name, const FK (&k)[3], int blocks2, int es,
+// two: the kernels with 32 rows a workgroup, or null
+void launch(const Launch& L, const char* name, const GKernel* one, const GKernel* two, int es,
             const GGemm& g, const GEpi& e) {
   const int i = g.N <= 16 ? 0 : g.N <= 32 ? 1 : 2;
-  const int rb = i == 0 ? 1 : blocks2, u = i == 2 || (i == 1 && blocks2 == 2) ? 2 : 4, most = i == 0 ? 16 : 8;
+  const bool rows32 = i > 0 && two && g.M > 255 * 32;
+  const int rb = rows32 ? 2 : 1, u = i == 2 || rows32 ? 2 : 4, most = i == 0 ? 16 : 8;
   const int grid = (g.M + 16 * rb - 1) / (16 * rb);
   // enough waves for 8 a compute unit, each with a group of K at least
   const int groups = (g.K * es + 64 * u - 1) / (64 * u);
   int w = 1;
   while (w < most && 2 * w <= groups && (w < 4 || (long long)grid * w < 2048)) w *= 2;
   prof_begin(L, name);
-  hipExtLaunchKernelGGL(k[i], dim3(grid), dim3(64 * w), 0, L.stream, prof_a(L), prof_b(L), 0, g, e);
+  hipExtLaunchKernelGGL((rows32 ? two : one)[i], dim3(grid), dim3(64 * w), 0, L.stream, prof_a(L),
+                        prof_b(L), 0, g, e);
   prof_end(L, name, 2.0 * g.M * (double)g.N * g.K, 0.0);
 }
 }  // namespace
 
 void gated_few_up(const Launch& L, int type, const GGemm& g, const GEpi& e) {
-  launch(L, "hf_gated_few_up", few_up[type], 2, type == VT_F32 ? 4 : type == VT_BF16 ? 2 : 1, g, e);
+  launch(L, "hf_gated_few_up", few_up[type], few_up2[type], size_of(type), g, e);
 }
 void gated_few_down(const Launch& L, int type, int out_type, const GGemm& g, const GEpi& e) {
-  launch(L, "hf_gated_few_down", few_down[type == VT_I8 ? 2 + out_type : type], 1,
-         type == VT_F32 ? 4 : type == VT_BF16 ? 2 : 1, g, e);
+  launch(L, "hf_gated_few_down", few_down[type == VT_I8 ? 2 + out_type : type], nullptr,
+         size_of(type), g, e);
 }
 
 }  // namespace hfk

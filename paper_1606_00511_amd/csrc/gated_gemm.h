@@ -269,9 +269,17 @@ __device__ __forceinline__ void scaled_part(const float* s, int lane, const GEpi
   }
 }
 
+// The stages of a workgroup, the same ones for every product that a kernel may compute.
+template <class E, int N>
+__device__ __forceinline__ E* stages() {
+  __shared__ __attribute__((aligned(16))) E lds[N];
+  return lds;
+}
+
+// The tile of workgroup L of product s.
 // E: the operands' type, O: the output's, ACT: the activation of "up" and "dh"
 template <class E, class O, int MODE, int ACT, int WM, int WN, int GM, int GN, int S>
-__device__ __forceinline__ void ggemm_body(const GGemm& s, const GEpi& e) {
+__device__ __forceinline__ void ggemm_body(const GGemm& s, const GEpi& e, int L) {
   constexpr bool AKC = MODE == UP || MODE == DOWN, BKC = MODE != DW;
   constexpr int BK = 128 / (int)sizeof(E);
   constexpr int NW = GM * GN;
@@ -280,15 +288,15 @@ __device__ __forceinline__ void ggemm_body(const GGemm& s, const GEpi& e) {
   using TB = Tile<E, BKC, RN, BK, NW>;
   constexpr int EPC = TA::EPC;
   constexpr int STAGE = TA::SIZE + TB::SIZE;
-  __shared__ __attribute__((aligned(16))) E lds[S * STAGE];
+  constexpr int ALL = S * STAGE;
 
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wave / GN, wn = wave % GN;
   const int li = lane & 31, h = lane >> 5;
-  const int gy = gridDim.y;
+  const int gx = (s.M - s.m0 + RM - 1) / RM, gy = (s.N + RN - 1) / RN;
   int tm, tn, tz;
-  if (!tile_of(gy, s.splits, tm, tn, tz)) return;
+  if (!tile_at(L, gx, gy, s.splits, tm, tn, tz)) return;
   const int m0 = s.m0 + tm * RM, n0 = tn * RN;
 
   const int nvb = s.K / BK;
@@ -312,17 +320,18 @@ __device__ __forceinline__ void ggemm_body(const GGemm& s, const GEpi& e) {
   // operand past its width read its last chunk (both feed outputs that are not
   // stored).
   const int fa = MODE == UP ? m0 / 2 : m0;       // A's first row or column
+  const int ra = min(fa, s.alim - 1), rb = min(n0, s.blim - 1);   // (whole tiles may lie past it)
   auto offset_a = [&](int j, long long ld) {
     int row, ch;
     TA::src(wave, lane, j, row, ch);
     if (MODE == UP) row = row / 64 * 32 + row % 32;
-    return AKC ? (uint32_t)((min(fa + row, s.alim - 1) - fa) * ld) + EPC * ch
+    return AKC ? (uint32_t)((min(fa + row, s.alim - 1) - ra) * ld) + EPC * ch
                : (uint32_t)(row * ld) + min(EPC * ch, (s.M - 1 - m0) / EPC * EPC);
   };
   auto offset_b = [&](int j, long long ld) {
     int row, ch;
     TB::src(wave, lane, j, row, ch);
-    return BKC ? (uint32_t)((min(n0 + row, s.blim - 1) - n0) * ld) + EPC * ch
+    return BKC ? (uint32_t)((min(n0 + row, s.blim - 1) - rb) * ld) + EPC * ch
                : (uint32_t)(row * ld) + min(EPC * ch, (s.N - 1 - n0) / EPC * EPC);
   };
   uint32_t offa[TA::INSTR], offb[TB::INSTR];
@@ -330,9 +339,9 @@ __device__ __forceinline__ void ggemm_body(const GGemm& s, const GEpi& e) {
   for (int j = 0; j < TA::INSTR; ++j) offa[j] = offset_a(j, s.lda);
 #pragma unroll
   for (int j = 0; j < TB::INSTR; ++j) offb[j] = offset_b(j, s.ldb);
-  const size_t a0 = AKC ? (size_t)fa * s.lda : (size_t)m0;
-  const size_t b0 = BKC ? (size_t)n0 * s.ldb : (size_t)n0;
-  const uint32_t lds0 = lds_address(lds);
+  const size_t a0 = AKC ? (size_t)ra * s.lda : (size_t)m0;
+  const size_t b0 = BKC ? (size_t)rb * s.ldb : (size_t)n0;
+  const uint32_t lds0 = lds_address(stages<E, ALL>());
   static_assert(TA::CH == 8 || !AKC, "8 rows of 128 bytes a direct load");
   // direct load j of K block vb into stage st (A's, then B's)
   auto issue1 = [&](int vb, int st, int j) {
@@ -360,7 +369,7 @@ __device__ __forceinline__ void ggemm_body(const GGemm& s, const GEpi& e) {
     }
   };
   auto fetch1 = [&](FragsT<E, TA, TB, WM, WN>& f, int st, int q, int i) {
-    const E* la = lds + st * STAGE;
+    const E* la = stages<E, ALL>() + st * STAGE;
     const E* lb = la + TA::SIZE;
     if (i < WN) f.b[i] = TB::frag(lb, wn * 32 * WN + 32 * i, lane, q);
     else f.a[i - WN] = TA::frag(la, wm * 32 * WM + 32 * (i - WN), lane, q);
@@ -372,7 +381,7 @@ __device__ __forceinline__ void ggemm_body(const GGemm& s, const GEpi& e) {
   const int mt = m0 + wm * 32 * WM, nt = n0 + wn * 32 * WN;
   constexpr int RL = 32 * WM;
   static_assert(NW * 32 * RL * 4 <= S * STAGE * (int)sizeof(E), "staging exceeds the stages");
-  float* const mine = (float*)lds + wave * 32 * RL;
+  float* const mine = (float*)stages<E, ALL>() + wave * 32 * RL;
   const bool parts = (MODE == DOWN || MODE == DX || MODE == DW) && e.part;
   float* const part = parts ? e.part + (size_t)tz * gy * RN * e.ldp : nullptr;
   // whether all of the tile's rows and features exist
@@ -457,23 +466,24 @@ __device__ __forceinline__ void ggemm_body(const GGemm& s, const GEpi& e) {
 // Kernels of a product: big: 256 x 256 tiles, 8 waves of 128 x 64; n64: 128 x 64, 4
 // waves of 64 x 32, with three K blocks on their way, for few rows; else 128 x 128, 4
 // waves of 64 x 64
+// (a launch's workgroups are a line: the order of tiles is the kernel's)
 #define HF_GGEMM_WIDE(NAME, E, O, MODE, ACT)                                           \
   extern "C" __global__ __launch_bounds__(512, 1) void NAME##_big(GGemm s, GEpi e) {   \
-    ggemm_body<E, O, MODE, ACT, 4, 2, 2, 4, 2>(s, e);                                  \
+    ggemm_body<E, O, MODE, ACT, 4, 2, 2, 4, 2>(s, e, blockIdx.x);                      \
   }                                                                                    \
   extern "C" __global__ __launch_bounds__(256, 2) void NAME(GGemm s, GEpi e) {         \
-    ggemm_body<E, O, MODE, ACT, 2, 2, 2, 2, 2>(s, e);                                  \
+    ggemm_body<E, O, MODE, ACT, 2, 2, 2, 2, 2>(s, e, blockIdx.x);                      \
   }
 #define HF_GGEMM(NAME, E, O, MODE, ACT)                                                \
   HF_GGEMM_WIDE(NAME, E, O, MODE, ACT)                                                 \
   extern "C" __global__ __launch_bounds__(256, 2) void NAME##_n64(GGemm s, GEpi e) {   \
-    ggemm_body<E, O, MODE, ACT, 2, 1, 2, 2, 3>(s, e);                                  \
+    ggemm_body<E, O, MODE, ACT, 2, 1, 2, 2, 3>(s, e, blockIdx.x);                                  \
   }
 // and n32: 128 x 32, a wave having 32 of the matrix's rows, with four K blocks on their way
 #define HF_GGEMM_FEW(NAME, E, O, MODE, ACT)                                            \
   HF_GGEMM(NAME, E, O, MODE, ACT)                                                      \
   extern "C" __global__ __launch_bounds__(256, 2) void NAME##_n32(GGemm s, GEpi e) {   \
-    ggemm_body<E, O, MODE, ACT, 1, 1, 4, 1, 4>(s, e);                                  \
+    ggemm_body<E, O, MODE, ACT, 1, 1, 4, 1, 4>(s, e, blockIdx.x);                                  \
   }
 #define HF_GK(NAME) {NAME, NAME##_big, NAME##_n64}
 #define HF_GK_FEW(NAME) {NAME, NAME##_big, NAME##_n64, NAME##_n32}
@@ -483,10 +493,10 @@ __device__ __forceinline__ void ggemm_body(const GGemm& s, const GEpi& e) {
   HF_GGEMM(hf_gated_up_f32_##SUF, float, float, UP, ACT)                               \
   HF_GGEMM(hf_gated_up_bf16_##SUF, bf16_t, bf16_t, UP, ACT)                            \
   HF_GGEMM(hf_gated_up_codes_##SUF, int8_t, float, UP, ACT)                            \
-  HF_GGEMM(hf_gated_dh_f32_##SUF, float, float, DH, ACT)                               \
-  HF_GGEMM(hf_gated_dh_bf16_##SUF, bf16_t, bf16_t, DH, ACT)                            \
+  HF_GGEMM_FEW(hf_gated_dh_f32_##SUF, float, float, DH, ACT)                           \
+  HF_GGEMM_FEW(hf_gated_dh_bf16_##SUF, bf16_t, bf16_t, DH, ACT)                        \
   extern const GActKernels gated_##SUF = {                                             \
       {HF_GK(hf_gated_up_f32_##SUF), HF_GK(hf_gated_up_bf16_##SUF),                    \
        HF_GK(hf_gated_up_codes_##SUF)},                                                \
-      {HF_GK(hf_gated_dh_f32_##SUF), HF_GK(hf_gated_dh_bf16_##SUF)}};                  \
+      {HF_GK_FEW(hf_gated_dh_f32_##SUF), HF_GK_FEW(hf_gated_dh_bf16_##SUF)}};                  \
   }  /* namespace hfk */

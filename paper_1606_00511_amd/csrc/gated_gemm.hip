@@ -7,9 +7,30 @@ namespace hfk {
   HF_GGEMM_FEW(NAME##_f32, float, float, MODE, GA_RELU)     \
   HF_GGEMM_FEW(NAME##_bf16, bf16_t, bf16_t, MODE, GA_RELU)
 HF_GGEMM_T(hf_gated_down, DOWN)
-HF_GGEMM_T(hf_gated_dx, DX)
-HF_GGEMM_WIDE(hf_gated_dw_f32, float, float, DW, GA_RELU)
-HF_GGEMM_WIDE(hf_gated_dw_bf16, bf16_t, bf16_t, DW, GA_RELU)
+// dX, dWd and dWg with dWu in one launch, its workgroups in this order: they need
+// nothing of each other, and the last ones of a product leave no unit idle while
+// another's begin
+template <class E, int WM, int WN, int GM, int GN>
+__device__ __forceinline__ void grads_body(const GGrads& a) {
+  const int L = blockIdx.x;
+  if (L < a.first[1]) {
+    ggemm_body<E, E, DX, GA_RELU, WM, WN, GM, GN, 2>(a.g[0], a.e[0], L);
+  } else {
+    const bool last = L >= a.first[2];
+    const GGemm g = last ? a.g[2] : a.g[1];
+    const GEpi e = last ? a.e[2] : a.e[1];
+    ggemm_body<E, E, DW, GA_RELU, WM, WN, GM, GN, 2>(g, e, L - (last ? a.first[2] : a.first[1]));
+  }
+}
+#define HF_GRADS(SUF, E)                                                                        \
+  extern "C" __global__ __launch_bounds__(512, 1) void hf_gated_grads_##SUF##_big(GGrads a) {   \
+    grads_body<E, 4, 2, 2, 4>(a);                                                               \
+  }                                                                                             \
+  extern "C" __global__ __launch_bounds__(256, 2) void hf_gated_grads_##SUF(GGrads a) {         \
+    grads_body<E, 2, 2, 2, 2>(a);                                                               \
+  }
+HF_GRADS(f32, float)
+HF_GRADS(bf16, bf16_t)
 HF_GGEMM_FEW(hf_gated_down_codes_f32, int8_t, float, DOWN, GA_RELU)
 HF_GGEMM_FEW(hf_gated_down_codes_bf16, int8_t, bf16_t, DOWN, GA_RELU)
 
@@ -28,11 +49,10 @@ const GActKernels& act_kernels(int act) {
   }
 }
 void launch(const Launch& L, const char* name, const GKernel* k, const GGemm& g, const GEpi& e) {
-  if (g.M <= g.m0 || g.N < 1) return;
-  const int RM = tile_m(g.tile), RN = tile_n(g.tile);
-  const dim3 grid((g.M - g.m0 + RM - 1) / RM, (g.N + RN - 1) / RN, g.splits);
+  const int grid = gated_tiles(g) * g.splits;
+  if (grid < 1) return;
   prof_begin(L, name);
-  hipExtLaunchKernelGGL(k[g.tile], grid, dim3(g.tile == TILE_BIG ? 512 : 256), 0, L.stream,
+  hipExtLaunchKernelGGL(k[g.tile], dim3(grid), dim3(g.tile == TILE_BIG ? 512 : 256), 0, L.stream,
                         prof_a(L), prof_b(L), 0, g, e);
   prof_end(L, name, 2.0 * (g.M - g.m0) * (double)g.N * g.K, 0.0);
 }
@@ -50,14 +70,18 @@ void gated_down(const Launch& L, int type, int out_type, const GGemm& g, const G
                                   HF_GK_FEW(hf_gated_down_codes_bf16)};
   launch(L, "hf_gated_down", type == VT_I8 ? c[out_type] : k[type], g, e);
 }
-void gated_dx(const Launch& L, int type, const GGemm& g, const GEpi& e) {
-  static const GKernel k[2][4] = {HF_GK_FEW(hf_gated_dx_f32), HF_GK_FEW(hf_gated_dx_bf16)};
-  launch(L, "hf_gated_dx", k[type], g, e);
-}
-void gated_dw(const Launch& L, int type, const GGemm& g, const GEpi& e) {
-  static const GKernel k[2][2] = {{hf_gated_dw_f32, hf_gated_dw_f32_big},
-                                  {hf_gated_dw_bf16, hf_gated_dw_bf16_big}};
-  launch(L, "hf_gated_dw", k[type], g, e);
+void gated_grads(const Launch& L, int type, GGrads a) {
+  a.first[0] = 0;
+  for (int i = 0; i < 3; ++i)
+    a.first[i + 1] = a.first[i] + (a.e[i].out ? gated_tiles(a.g[i]) * a.g[i].splits : 0);
+  if (a.first[3] < 1) return;
+  static void (*const k[2][2])(GGrads) = {{hf_gated_grads_f32, hf_gated_grads_f32_big},
+                                          {hf_gated_grads_bf16, hf_gated_grads_bf16_big}};
+  const int tile = a.g[0].tile;
+  prof_begin(L, "hf_gated_grads");
+  hipExtLaunchKernelGGL(k[type][tile], dim3(a.first[3]), dim3(tile == TILE_BIG ? 512 : 256), 0,
+                        L.stream, prof_a(L), prof_b(L), 0, a);
+  prof_end(L, "hf_gated_grads", 0.0, 0.0);
 }
 
 }  // namespace hfk

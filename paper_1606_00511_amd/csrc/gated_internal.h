@@ -19,7 +19,7 @@ struct GGemm {
   int M, N, K;
   int m0;                // columns of the output before it are another launch's
   const void *A, *A1, *B;
-  long long lda, ldb;
+  long long lda, lda1, ldb;   // lda1: of A1 for few rows (else A's)
   int alim, blim;        // rows m of A and n of B that exist, where these are rows
   int kh;                // row products: A1 has the rows k from kh on
   // operands whose rows are k: those from ktail on are read here, where zeros
@@ -29,6 +29,12 @@ struct GGemm {
   int ktail;
   int splits, tile;
 };
+
+// output tiles of a product's columns from m0 on
+inline int gated_tiles(const GGemm& g) {
+  const int rm = tile_m(g.tile), rn = tile_n(g.tile);
+  return g.M > g.m0 && g.N > 0 ? (g.M - g.m0 + rm - 1) / rm * ((g.N + rn - 1) / rn) : 0;
+}
 
 struct GEpi {
   int act, F, Fp;        // hidden width, and as the workspace has it
@@ -57,32 +63,44 @@ struct GEpi {
 // The kernels with an activation, by type and tile (VT_*, TILE_*).
 typedef void (*GKernel)(GGemm, GEpi);
 struct GActKernels {
-  GKernel up[3][3], dh[2][3];
+  GKernel up[3][3], dh[2][4];
 };
 
 // h = phi(X Wg^T) * (X Wu^T): A = Wg, A1 = Wu (rows alim), B = X; M = 2 Fp
 void gated_up(const Launch& L, int type, const GGemm& g, const GEpi& e);
 // out = B A^T: A = Wd, B = h; codes: out_type, scaled
 void gated_down(const Launch& L, int type, int out_type, const GGemm& g, const GEpi& e);
-// the same of up to FEW_X rows, in place at any alignment; "up" keeps nothing, its
-// M is F, and of codes hmax has an entry for 16 columns; "down" of up to TWO_X
+// the same of up to FEW_X rows, in place at any alignment; "up" keeps codes as
+// fp32, its M is F, and of codes hmax has an entry for 16 columns; "down" of up to TWO_X
 // bf16 rows reads the second terms that "up" wrote, TWO_X rows further down
 constexpr int FEW_X = 64, TWO_X = 16;
 void gated_few_up(const Launch& L, int type, const GGemm& g, const GEpi& e);
 void gated_few_down(const Launch& L, int type, int out_type, const GGemm& g, const GEpi& e);
 // dh = dY Wd in the tile, from it and what is kept h, dg and du
 void gated_dh(const Launch& L, int type, const GGemm& g, const GEpi& e);
-// dX = dg Wg + du Wu
-void gated_dx(const Launch& L, int type, const GGemm& g, const GEpi& e);
-// B^T A over the rows
-void gated_dw(const Launch& L, int type, const GGemm& g, const GEpi& e);
-// out from the partials of g with e; row n + dup joins row n if dup
-void gated_finish(const Launch& L, int type, int out_type, const GGemm& g, const GEpi& e, int dup);
+// The gradients from dg, du and h: dX = dg Wg + du Wu, dWd = dY^T h, and dWg = dg^T X
+// with dWu = du^T X, each if its e.out is there; of one tile
+struct GGrads {
+  GGemm g[3];
+  GEpi e[3];
+  int first[4];          // workgroups of the products before each (set by the launch)
+};
+void gated_grads(const Launch& L, int type, GGrads a);
+// out from the partials of products with their e.part: row n + dup joins row n if dup
+struct GFinish {
+  GGemm g;
+  GEpi e;
+  int dup;
+};
+void gated_finish(const Launch& L, int type, int out_type, const GFinish* f, int n);
 
 // Copies of a call's operands with zeros around: rows x cols elements of es
 // bytes, ld apart, to prows x pcols ones (times > 1: so often, below each other).
+// scale: the source is a checkpoint's codes, with scale bytes lds apart.
 struct GPad {
   const void* src;
+  const uint8_t* scale;
+  long long lds;
   void* dst;
   long long ld;
   int rows, cols, prows, pcols, times;
@@ -98,10 +116,9 @@ void gated_pad(const Launch& L, const GPads& p);
 // checkpoints: rows x cols of the type to codes and scale bytes, and back
 void gated_pack(const Launch& L, int type, const void* X, long long ldx, long long rows, int cols,
                 int8_t* codes, long long ldc, uint8_t* scale, long long lds);
-// zrows (>= rows): rows of zeros up to there, zcols (>= cols) columns
 void gated_unpack(const Launch& L, int type, const int8_t* codes, long long ldc,
                   const uint8_t* scale, long long lds, long long rows, int cols, void* X,
-                  long long ldx, long long zrows, int zcols, int times);
+                  long long ldx);
 
 // codes of rows with a scale each: q = round(x / s), s = max |x| / 127; zeros up
 // to zcols columns

@@ -29,12 +29,40 @@ __device__ __forceinline__ u32x4 padded(const E* src, int c, int cols) {
   return w;
 }
 
+// the same of a checkpoint
+__device__ __forceinline__ u32x4 unpacked(const GPad& p, int row, int c) {
+  const int n = 16 / p.es, at = c * n, have = p.cols - at;
+  float v[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) v[j] = 0.0f;
+  if (have > 0)
+    get_codes((const int8_t*)p.src + (size_t)row * p.ld + at,
+              code_step(p.scale[(size_t)row * p.lds + at / CODE_BLOCK]), v, min(have, n));
+  if (p.es == 4) return __builtin_bit_cast(u32x4, f32x4{v[0], v[1], v[2], v[3]});
+  u32x4 w;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) w[j] = f2bf(v[2 * j]) | f2bf(v[2 * j + 1]) << 16;
+  return w;
+}
+
 // ------------------------------------------------- sums of split products
+struct FinishOne {
+  GFinish f;
+  int rows, chunks, first;     // rows of out (both), 8 columns each; first workgroup
+  long long stride;            // of partials
+};
+struct FinishAll {
+  FinishOne one[3];
+  int n;
+};
+// f's outputs by `groups` workgroups, of which this is the b-th
 template <class E, class O>
-__device__ __forceinline__ void finish_body(const GGemm& g, const GEpi& e, int dup, int rows,
-                                            int chunks, long long stride, long long total) {
-  const int end = min(e.mout, g.M);
-  for (long long i = blockIdx.x * 256ll + threadIdx.x; i < total; i += gridDim.x * 256ll) {
+__device__ __forceinline__ void finish_body(const FinishOne& one, int b, int groups) {
+  const GGemm& g = one.f.g;
+  const GEpi& e = one.f.e;
+  const int dup = one.f.dup, chunks = one.chunks, end = min(e.mout, g.M);
+  const long long stride = one.stride, total = (long long)one.rows * chunks;
+  for (long long i = b * 256ll + threadIdx.x; i < total; i += groups * 256ll) {
     const int row = (int)(i / chunks), m = g.m0 + 8 * (int)(i % chunks);
     const bool second = row >= e.nout;
     const int n = second ? e.n1 + row - e.nout : row, have = end - m;
@@ -100,20 +128,16 @@ __device__ __forceinline__ void pack_body(const E* X, long long ldx, uint32_t to
 
 template <class E, bool STREAM>
 __device__ __forceinline__ void unpack_body(const int8_t* codes, long long ldc,
-                                            const uint8_t* scale, long long lds, uint32_t rows,
-                                            int cols, E* X, long long ldx, uint32_t zrows,
-                                            int zcols, uint32_t per, uint32_t total) {
+                                            const uint8_t* scale, long long lds,
+                                            int cols, E* X, long long ldx, uint32_t per,
+                                            uint32_t total) {
   const uint32_t i = blockIdx.x * 256u + threadIdx.x;
   if (i >= total) return;
-  const uint32_t to = i / per, c = i % per, row = to % zrows;
-  const int at = 8 * (int)c;
-  const int have = row < rows ? cols - at : 0;
+  const uint32_t row = i / per, c = i % per;
+  const int at = 8 * (int)c, have = cols - at;
   float v[8];
-#pragma unroll
-  for (int j = 0; j < 8; ++j) v[j] = 0.0f;
-  if (have > 0)
-    get_codes(codes + (size_t)row * ldc + at, code_step(scale[(size_t)row * lds + c / 4]), v, have);
-  put<STREAM>(X + (size_t)to * ldx + at, v, zcols - at);
+  get_codes(codes + (size_t)row * ldc + at, code_step(scale[(size_t)row * lds + c / 4]), v, have);
+  put<STREAM>(X + (size_t)row * ldx + at, v, have);
 }
 
 // --------------------------------------------------------- codes of rows
@@ -273,7 +297,8 @@ extern "C" __global__ __launch_bounds__(256) void hf_gated_pad(GPads all, int ch
     u32x4 w = u32x4{0u, 0u, 0u, 0u};
     if ((int)row < p.rows) {
       const char* src = (const char*)p.src + (size_t)row * p.ld * p.es;
-      w = p.es == 4 ? padded((const float*)src, (int)c, p.cols)
+      if (p.scale) w = unpacked(p, (int)row, (int)c);
+      else w = p.es == 4 ? padded((const float*)src, (int)c, p.cols)
                     : p.es == 2 ? padded((const uint16_t*)src, (int)c, p.cols)
                                 : padded((const int8_t*)src, (int)c, p.cols);
     }
@@ -282,9 +307,15 @@ extern "C" __global__ __launch_bounds__(256) void hf_gated_pad(GPads all, int ch
 }
 
 #define HF_FINISH(SUF, E, O)                                                                     \
-  extern "C" __global__ __launch_bounds__(256) void hf_gated_finish_##SUF(                       \
-      GGemm g, GEpi e, int dup, int rows, int chunks, long long stride, long long total) {       \
-    finish_body<E, O>(g, e, dup, rows, chunks, stride, total);                                   \
+  extern "C" __global__ __launch_bounds__(256) void hf_gated_finish_##SUF(FinishAll a) {         \
+    const int b = blockIdx.x;                                                                    \
+    if (a.n > 2 && b >= a.one[2].first)                                                          \
+      finish_body<E, O>(a.one[2], b - a.one[2].first, gridDim.x - a.one[2].first);               \
+    else if (a.n > 1 && b >= a.one[1].first)                                                     \
+      finish_body<E, O>(a.one[1], b - a.one[1].first,                                            \
+                        (a.n > 2 ? a.one[2].first : gridDim.x) - a.one[1].first);                \
+    else                                                                                         \
+      finish_body<E, O>(a.one[0], b, a.n > 1 ? a.one[1].first : gridDim.x);                      \
   }
 HF_FINISH(f32, float, float)
 HF_FINISH(bf16, bf16_t, bf16_t)
@@ -304,10 +335,9 @@ HF_FINISH(codes_bf16, int8_t, bf16_t)
     pack_body<E, STREAM>(X, ldx, total, cols, per, codes, ldc, scale, lds);                      \
   }                                                                                              \
   extern "C" __global__ __launch_bounds__(256) void hf_gated_unpack_##SUF(                       \
-      const int8_t* codes, long long ldc, const uint8_t* scale, long long lds, uint32_t rows,    \
-      int cols, E* X, long long ldx, uint32_t zrows, int zcols, uint32_t per, uint32_t total) {  \
-    unpack_body<E, STREAM>(codes, ldc, scale, lds, rows, cols, X, ldx, zrows, zcols, per,        \
-                           total);                                                               \
+      const int8_t* codes, long long ldc, const uint8_t* scale, long long lds, int cols, E* X,   \
+      long long ldx, uint32_t per, uint32_t total) {                                             \
+    unpack_body<E, STREAM>(codes, ldc, scale, lds, cols, X, ldx, per, total);                    \
   }
 HF_PACK(f32, float, false)
 HF_PACK(bf16, bf16_t, false)
@@ -365,28 +395,29 @@ void gated_pad(const Launch& L, const GPads& p) {
   HF_LAUNCH("hf_gated_pad", hf_gated_pad, grid, 256, p, c[0], c[1], c[2], c[3], c[4]);
 }
 
-void gated_finish(const Launch& L, int type, int out_type, const GGemm& g, const GEpi& e, int dup) {
-  const int halves = e.n1 < g.N ? 2 : 1;
-  const int rows = halves * e.nout, chunks = (std::min(e.mout, g.M) - g.m0 + 7) / 8;
-  const int rn = tile_n(g.tile);
-  if (chunks < 1) return;
-  const long long stride = (long long)((g.N + rn - 1) / rn) * rn * e.ldp;
-  const long long total = (long long)rows * chunks;
-  const long long grid = std::min<long long>((total + 255) / 256, 1 << 20);
+void gated_finish(const Launch& L, int type, int out_type, const GFinish* f, int n) {
+  FinishAll a = {};
+  int grid = 0;
+  for (int i = 0; i < n; ++i) {
+    const GGemm& g = f[i].g;
+    const GEpi& e = f[i].e;
+    const int chunks = (std::min(e.mout, g.M) - g.m0 + 7) / 8, rn = tile_n(g.tile);
+    const int rows = (e.n1 < g.N ? 2 : 1) * e.nout;
+    if (chunks < 1 || rows < 1) continue;
+    a.one[a.n++] = FinishOne{f[i], rows, chunks, grid,
+                             (long long)((g.N + rn - 1) / rn) * rn * e.ldp};
+    grid += (int)std::min<long long>(((long long)rows * chunks + 255) / 256, 1 << 20);
+  }
   if (grid < 1) return;
   if (type == VT_I8) {
     if (out_type == VT_F32)
-      HF_LAUNCH("hf_gated_finish", hf_gated_finish_codes_f32, grid, 256, g, e, dup, rows, chunks,
-                stride, total);
+      HF_LAUNCH("hf_gated_finish", hf_gated_finish_codes_f32, grid, 256, a);
     else
-      HF_LAUNCH("hf_gated_finish", hf_gated_finish_codes_bf16, grid, 256, g, e, dup, rows, chunks,
-                stride, total);
+      HF_LAUNCH("hf_gated_finish", hf_gated_finish_codes_bf16, grid, 256, a);
   } else if (type == VT_F32) {
-    HF_LAUNCH("hf_gated_finish", hf_gated_finish_f32, grid, 256, g, e, dup, rows, chunks, stride,
-              total);
+    HF_LAUNCH("hf_gated_finish", hf_gated_finish_f32, grid, 256, a);
   } else {
-    HF_LAUNCH("hf_gated_finish", hf_gated_finish_bf16, grid, 256, g, e, dup, rows, chunks, stride,
-              total);
+    HF_LAUNCH("hf_gated_finish", hf_gated_finish_bf16, grid, 256, a);
   }
 }
 
@@ -406,17 +437,17 @@ void gated_pack(const Launch& L, int type, const void* X, long long ldx, long lo
 
 void gated_unpack(const Launch& L, int type, const int8_t* codes, long long ldc,
                   const uint8_t* scale, long long lds, long long rows, int cols, void* X,
-                  long long ldx, long long zrows, int zcols, int times) {
-  const uint32_t per = (uint32_t)((zcols + 7) / 8);
-  const uint32_t total = (uint32_t)zrows * times * per;
+                  long long ldx) {
+  const uint32_t per = (uint32_t)((cols + 7) / 8);
+  const uint32_t total = (uint32_t)rows * per;
   if (!total) return;
   const bool much = rows * cols * (type == VT_F32 ? 4 : 2) > L3_BYTES / 2;
   if (type == VT_F32)
-    HF_LAUNCH("hf_gated_unpack", (much ? hf_gated_unpack_f32_s : hf_gated_unpack_f32), (total + 255) / 256, 256, codes, ldc, scale,
-              lds, (uint32_t)rows, cols, (float*)X, ldx, (uint32_t)zrows, zcols, per, total);
+    HF_LAUNCH("hf_gated_unpack", (much ? hf_gated_unpack_f32_s : hf_gated_unpack_f32),
+              (total + 255) / 256, 256, codes, ldc, scale, lds, cols, (float*)X, ldx, per, total);
   else
-    HF_LAUNCH("hf_gated_unpack", (much ? hf_gated_unpack_bf16_s : hf_gated_unpack_bf16), (total + 255) / 256, 256, codes, ldc, scale,
-              lds, (uint32_t)rows, cols, (bf16_t*)X, ldx, (uint32_t)zrows, zcols, per, total);
+    HF_LAUNCH("hf_gated_unpack", (much ? hf_gated_unpack_bf16_s : hf_gated_unpack_bf16),
+              (total + 255) / 256, 256, codes, ldc, scale, lds, cols, (bf16_t*)X, ldx, per, total);
 }
 
 namespace {

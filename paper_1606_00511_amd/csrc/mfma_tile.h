@@ -216,10 +216,8 @@ __device__ __forceinline__ void store_part(const float* s, int lane, O* out, lon
 // walks groups of 8 tiles of n, m by m, so that the workgroups resident on an
 // XCD share their operand panels in its L2.  Tiles without rows take no place
 // in the order (2,251 of 3,001 rows counted, 50,257 x 1,024: 301 -> 222 us).
-__device__ __forceinline__ bool tile_of(int gy, int gz, int& tm, int& tn, int& tz) {
-  const int gx = gridDim.x;
+__device__ __forceinline__ bool tile_at(int L, int gx, int gy, int gz, int& tm, int& tn, int& tz) {
   const int T = gx * gy * gz;
-  const int L = blockIdx.x + gx * (blockIdx.y + gridDim.y * blockIdx.z);
   if (L >= T) return false;
   // XCD x's share: T / 8 workgroups, one more for the first T % 8
   const int x = L % 8, q = T / 8, r8 = T % 8;
@@ -234,6 +232,10 @@ __device__ __forceinline__ bool tile_of(int gy, int gz, int& tm, int& tn, int& t
   tn = first + w % rows;
   tm = w / rows;
   return true;
+}
+__device__ __forceinline__ bool tile_of(int gy, int gz, int& tm, int& tn, int& tz) {
+  return tile_at(blockIdx.x + gridDim.x * (blockIdx.y + gridDim.y * blockIdx.z), gridDim.x, gy, gz,
+                 tm, tn, tz);
 }
 
 // The K loop of a workgroup's tile: acc(a, b) += the products of a wave's blocks

@@ -540,7 +540,7 @@ class _RowContext:
         return rc
 
     def _call(self, fn, *args):
-        cuda, L = self._torch.cuda, _lib or lib()
+        cuda, L = self._torch.cuda, lib()
         if self._device() != self.device.index if self._device else \
                 cuda.current_device() != self.device.index:
             with cuda.device(self.device):

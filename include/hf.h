@@ -626,7 +626,7 @@ int hf_gated_set_stream(hf_gated* ctx, void* hip_stream);
  * NULL context or rows > max_rows.  Grows with rows. */
 size_t hf_gated_workspace_bytes(const hf_gated* ctx, int64_t rows);
 /* Hand over a device workspace, 256-byte aligned; calls with more rows than
- * its bytes serve return HF_EWORKSPACE. */
+ * its bytes serve return HF_EWORKSPACE.  Synchronises the device. */
 int hf_gated_set_workspace(hf_gated* ctx, void* dev_ptr, size_t bytes);
 
 /*

@@ -442,6 +442,8 @@ int hf_gated_set_workspace(hf_gated* c, void* p, size_t bytes) {
     if (plan_bytes(c, mid) <= bytes) lo = mid;
     else hi = mid - 1;
   }
+  c->ws = nullptr;
+  HIP_TRY(c, hipDeviceSynchronize());      // (calls so far may be at work in it)
   plan(c, lo, &c->lay);
   c->Rws = lo;
   c->pending = false;

@@ -211,7 +211,7 @@ __device__ __forceinline__ void few_body(const GGemm& s, const GEpi& e) {
         for (int r = 0; r < 4; ++r) big = max(big, __float_as_uint(v[r]) & 0x7fffffffu);
         big = max(big, (uint32_t)__shfl_xor((int)big, 16, 64));
         big = max(big, (uint32_t)__shfl_xor((int)big, 32, 64));
-        if (q == 0 && n < e.T && m < e.Fp) e.hmax[(size_t)n * e.ldmax + m / 16] = __uint_as_float(big);
+        if (q == 0 && n < e.T && m < e.F) e.hmax[(size_t)n * e.ldmax + m / 16] = __uint_as_float(big);
       }
       if (n < e.T && m < e.Fp) {
         if constexpr (sizeof(E) == 2) {

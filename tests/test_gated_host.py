@@ -74,6 +74,19 @@ result = [log(), at, to]
     assert hip_stub.unordered(lines, [("0xb00", at, to)]) == []
 
 
+def test_workspace_of_fewer_rows(stub):
+    """A workspace serves calls of up to the rows that its bytes are for, and is
+    handed over with nothing at work in the one before."""
+    lines = hip_stub.run(stub, GATED + """
+h = gated()
+assert L.hf_gated_set_workspace(h, 1 << 20, L.hf_gated_workspace_bytes(h, 100)) == H.HF_OK
+result = log()
+assert forward(h, 100) == H.HF_OK and forward(h, 200) == H.HF_EWORKSPACE
+assert b"200 rows above" in L.hf_gated_last_error(h)
+""")
+    assert lines == [["syncall"]]
+
+
 def test_no_rows(stub):
     """No rows: nothing runs, but the gradients of the matrices are set to zero
     unless they are added to."""

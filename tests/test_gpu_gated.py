@@ -14,7 +14,7 @@ pytestmark = pytest.mark.gpu
 
 # one row and column; around the 32, 64 and 128 of blocks, tiles and few rows; odd
 # widths; more than one tile of 256; hidden below the width
-SIZES = [(1, 1, 1), (1, 64, 64), (2, 3, 5), (3, 130, 33), (17, 65, 131), (31, 128, 192),
+SIZES = [(1, 1, 1), (1, 64, 64), (20, 66, 8176), (2, 3, 5), (3, 130, 33), (17, 65, 131), (31, 128, 192),
          (33, 64, 256), (64, 192, 96), (127, 100, 260), (128, 256, 128), (129, 192, 320),
          (130, 72, 517), (256, 320, 704), (300, 129, 450), (700, 512, 1365)]
 ACTS = ["silu", "gelu", "gelu_tanh", "sigmoid", "tanh", "relu"]
@@ -385,8 +385,9 @@ def test_product_largest_sum():
 
 
 @pytest.mark.parametrize("type", ["fp32", "bf16"])
+# (8,176: half of the last 32 rows that a workgroup has of the matrices are none)
 @pytest.mark.parametrize("T,D,F", [(1, 64, 64), (4, 33, 75), (24, 128, 512), (200, 256, 384),
-                                   (300, 130, 515)])
+                                   (300, 130, 515), (20, 64, 8176), (40, 70, 8209)])
 def test_forward_codes(type, T, D, F):
     act = ACTS[(T + D) % 6]
     dt = G.TYPES[type]

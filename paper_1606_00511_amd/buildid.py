@@ -15,7 +15,7 @@ HEADER = os.path.join(os.path.dirname(HERE), "include", "hf.h")
 SOURCES = ["hf_api.cpp", "gemm.hip", "gemm_bf16.hip", "rowops.hip", "cgvec.hip",
            "noalloc.hip", "narrow.hip", "vocab_api.cpp", "vocab_gemm.hip",
            "vocab_rows.hip", "vocab_embed.hip", "gated_api.cpp", "gated_gemm.hip",
-           "gated_rows.hip", "gated_few.hip",
+           "gated_rows.hip", "gated_few.hip", "gated_one.hip",
            "gated_sigmoid.hip", "gated_tanh.hip", "gated_relu.hip", "gated_silu.hip",
            "gated_gelu.hip", "gated_gelu_tanh.hip"]
 

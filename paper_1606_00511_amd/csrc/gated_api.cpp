@@ -486,6 +486,10 @@ int hf_gated_forward(hf_gated* c, const void* X, int64_t ldx, const void* Wg, in
     eu.h = c->at<void>(l.h);
     eu.ldh = c->ldh();
     eu.dup = ed.dup = T <= TWO_X ? TWO_X : 0;
+    // (of one row h is fp32, unless its rows of Wd are short)
+    const bool one = T == 1 && F * es > ONE_BYTES;
+    eu.h32 = one;
+    if (one) eu.dup = 0;
     eu.keep = keep;
     eu.kept = kept;
     eu.ldk = ldk;
@@ -493,7 +497,8 @@ int hf_gated_forward(hf_gated* c, const void* X, int64_t ldx, const void* Wg, in
       eu.kept = c->at<float>(l.gu);
       eu.ldk = 2 * F;
     }
-    gated_few_up(L, c->type, gu, eu);
+    if (one && D * es > ONE_BYTES) gated_one_up(L, c->type, gu, eu);
+    else gated_few_up(L, c->type, gu, eu);
     if (keep == HF_KEEP_CODES) {
       int8_t* k = (int8_t*)kept;
       gated_pack(L, VT_F32, eu.kept, 2 * F, T, F, k, ldk, scale, lds);
@@ -509,7 +514,8 @@ int hf_gated_forward(hf_gated* c, const void* X, int64_t ldx, const void* Wg, in
       });
     } else {
       operands(&gd, Wd, ldd, nullptr, 0, eu.h, eu.ldh);
-      gated_few_down(L, c->type, c->type, gd, ed);
+      if (one) gated_one_down(L, c->type, c->type, gd, ed);
+      else gated_few_down(L, c->type, c->type, gd, ed);
     }
     return end(c);
   }
@@ -761,7 +767,8 @@ int hf_gated_product(hf_gated* c, const int8_t* A, int64_t lda, const float* sa,
     e.sn = sa;
     e.sm = sb;
     set_out(&e, Y, ldy, T, (int)n);
-    gated_few_down(L, VT_I8, c->type, g, e);
+    if (T == 1 && k > ONE_BYTES) gated_one_down(L, VT_I8, c->type, g, e);
+    else gated_few_down(L, VT_I8, c->type, g, e);
     return end(c);
   }
   // channels at a time: of those where they are as many as a launch takes with the most
@@ -845,16 +852,22 @@ int hf_gated_forward_codes(hf_gated* c, const void* X, int64_t ldx, const int8_t
   eu.ldh = Fc;
   eu.hmax = c->at<float>(l.hmax);
   eu.ldmax = few ? (F + 15) / 16 : Fp / 32;
-  if (few) {
+  const bool one_up = T == 1 && D > ONE_BYTES;
+  if (one_up) {
+    gated_one_up(L, VT_I8, gu, eu);
+  } else if (few) {
     gated_few_up(L, VT_I8, gu, eu);
   } else {
     ranged(gu, VT_I8, false, 3, [&](const GGemm& g) { gated_up(L, VT_I8, g, eu); });
   }
-  gated_codes_h(L, c->at<float>(l.hf), Fc, eu.hmax, eu.ldmax, T, F, hq, c->ldhq(), Fc, sh);
+  if (one_up) gated_codes_h(L, (float*)eu.h, Fc, (float*)eu.h, Fc, F, T, F, hq, c->ldhq(), Fc, sh);
+  else gated_codes_h(L, (float*)eu.h, Fc, eu.hmax, eu.ldmax, eu.ldmax, T, F, hq, c->ldhq(), Fc, sh);
   ed.sn = sh;
   ed.sm = sd;
   set_out(&ed, Y, ldy, T, D);
-  if (few_down) {
+  if (T == 1 && F > ONE_BYTES) {
+    gated_one_down(L, VT_I8, c->type, gd, ed);
+  } else if (few_down) {
     gated_few_down(L, VT_I8, c->type, gd, ed);
   } else {
     summed(c, L, VT_I8, c->type, gd, ed, 0, 4, [&](const GGemm& g, const GEpi& e) {

@@ -214,7 +214,7 @@ __device__ __forceinline__ void few_body(const GGemm& s, const GEpi& e) {
         if (q == 0 && n < e.T && m < e.F) e.hmax[(size_t)n * e.ldmax + m / 16] = __uint_as_float(big);
       }
       if (n < e.T && m < e.Fp) {
-        if constexpr (sizeof(E) == 2) {
+        if (sizeof(E) == 2 && !e.h32) {
           uint32_t b[4];
 #pragma unroll
           for (int r = 0; r < 4; ++r) b[r] = f2bf(v[r]);

@@ -41,6 +41,7 @@ struct GEpi {
   int T;                 // rows of the call
   void* h;               // phi(g) u: fp32 for codes, else of the type
   long long ldh;
+  int h32;               // few rows: h is fp32 whatever the type
   int dup;               // > 0: the rounding's rest too, dup rows further down
   int keep;
   void* kept;            // g, and F elements further u
@@ -74,6 +75,11 @@ void gated_down(const Launch& L, int type, int out_type, const GGemm& g, const G
 // fp32, its M is F, and of codes hmax has an entry for 16 columns; "down" of up to TWO_X
 // bf16 rows reads the second terms that "up" wrote, TWO_X rows further down
 constexpr int FEW_X = 64, TWO_X = 16;
+// the same of one row, with rows of the matrices longer than ONE_BYTES: h is fp32 (also
+// of gated_few_up where h32), and "up" of codes leaves no hmax
+constexpr int ONE_BYTES = 2048;
+void gated_one_up(const Launch& L, int type, const GGemm& g, const GEpi& e);
+void gated_one_down(const Launch& L, int type, int out_type, const GGemm& g, const GEpi& e);
 void gated_few_up(const Launch& L, int type, const GGemm& g, const GEpi& e);
 void gated_few_down(const Launch& L, int type, int out_type, const GGemm& g, const GEpi& e);
 // dh = dY Wd in the tile, from it and what is kept h, dg and du
@@ -124,8 +130,8 @@ void gated_unpack(const Launch& L, int type, const int8_t* codes, long long ldc,
 // to zcols columns
 void gated_codes(const Launch& L, int type, const void* X, long long ldx, long long rows, int cols,
                  int8_t* codes, long long ldc, int zcols, float* scale);
-// the same of fp32 rows whose largest numbers are in hmax's ldmax parts
-void gated_codes_h(const Launch& L, const float* H, long long ldh, const float* hmax, int ldmax,
-                   int rows, int cols, int8_t* codes, long long ldc, int zcols, float* scale);
+// the same of fp32 rows of whose numbers the largest are among nmax in hmax, ldmax apart
+void gated_codes_h(const Launch& L, const float* H, long long ldh, const float* hmax,
+                   long long ldmax, int nmax, int rows, int cols, int8_t* codes, long long ldc, int zcols, float* scale);
 
 }  // namespace hfk

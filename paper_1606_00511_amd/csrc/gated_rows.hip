@@ -354,7 +354,8 @@ HF_CODES(bf16, bf16_t)
 // 2,048 columns of a row a workgroup, which finds the row's largest among the
 // products' parts of it first
 extern "C" __global__ __launch_bounds__(256) void hf_gated_codes_h(const float* H, long long ldh,
-                                                                   const float* hmax, int ldmax,
+                                                                   const float* hmax,
+                                                                   long long ldmax, int nmax,
                                                                    int cols, int8_t* codes,
                                                                    long long ldc, int zcols,
                                                                    int chunks, float* scale) {
@@ -365,8 +366,8 @@ extern "C" __global__ __launch_bounds__(256) void hf_gated_codes_h(const float* 
   for (int j = 0; j < 8; ++j) v[j] = 0.0f;
   if (at < cols) get(H + row * ldh + at, v, cols - at);
   uint32_t big = 0;
-  for (int i = threadIdx.x; i < ldmax; i += 256)
-    big = max(big, __float_as_uint(hmax[row * ldmax + i]));
+#pragma unroll 8
+  for (int i = threadIdx.x; i < nmax; i += 256) big = max(big, magnitude(hmax[row * ldmax + i]));
   const RowScale r = row_scale(group_max<4>(big));
   if (at == 0) scale[row] = r.s;
   if (at < zcols) put_row_codes<false>(codes + row * ldc + at, v, r, cols - at, zcols - at);
@@ -478,12 +479,12 @@ void gated_codes(const Launch& L, int type, const void* X, long long ldx, long l
                      scale);
 }
 
-void gated_codes_h(const Launch& L, const float* H, long long ldh, const float* hmax, int ldmax,
-                   int rows, int cols, int8_t* codes, long long ldc, int zcols, float* scale) {
+void gated_codes_h(const Launch& L, const float* H, long long ldh, const float* hmax,
+                   long long ldmax, int nmax, int rows, int cols, int8_t* codes, long long ldc, int zcols, float* scale) {
   if (rows < 1) return;
   const int chunks = (zcols + 2047) / 2048;
   HF_LAUNCH("hf_gated_codes_h", hf_gated_codes_h, (long long)rows * chunks, 256, H, ldh, hmax,
-            ldmax, cols, codes, ldc, zcols, chunks, scale);
+            ldmax, nmax, cols, codes, ldc, zcols, chunks, scale);
 }
 
 }  // namespace hfk

@@ -14,7 +14,8 @@ pytestmark = pytest.mark.gpu
 
 # one row and column; around the 32, 64 and 128 of blocks, tiles and few rows; odd
 # widths; more than one tile of 256; hidden below the width
-SIZES = [(1, 1, 1), (1, 64, 64), (20, 66, 8176), (2, 3, 5), (3, 130, 33), (17, 65, 131), (31, 128, 192),
+SIZES = [(1, 1, 1), (3, 2600, 1100), (4, 40, 5000), (5, 1024, 520), (1, 1300, 1100),
+         (1, 1100, 300), (1, 70, 2600), (1, 64, 64), (20, 66, 8176), (2, 3, 5), (3, 130, 33), (17, 65, 131), (31, 128, 192),
          (33, 64, 256), (64, 192, 96), (127, 100, 260), (128, 256, 128), (129, 192, 320),
          (130, 72, 517), (256, 320, 704), (300, 129, 450), (700, 512, 1365)]
 ACTS = ["silu", "gelu", "gelu_tanh", "sigmoid", "tanh", "relu"]
@@ -347,7 +348,7 @@ def test_codes_edges():
 
 
 @pytest.mark.parametrize("type", ["fp32", "bf16"])
-@pytest.mark.parametrize("T,N,K", [(1, 1, 1), (1, 1000, 128), (3, 5, 130), (16, 77, 64),
+@pytest.mark.parametrize("T,N,K", [(1, 1, 1), (1, 1000, 128), (1, 33, 9000), (1, 50, 2049), (4, 50, 1030), (3, 5, 130), (16, 77, 64),
                                    (33, 300, 256), (129, 257, 1000), (260, 640, 512),
                                    (5, 40000, 200)])
 def test_product(type, T, N, K):
@@ -387,7 +388,8 @@ def test_product_largest_sum():
 @pytest.mark.parametrize("type", ["fp32", "bf16"])
 # (8,176: half of the last 32 rows that a workgroup has of the matrices are none)
 @pytest.mark.parametrize("T,D,F", [(1, 64, 64), (4, 33, 75), (24, 128, 512), (200, 256, 384),
-                                   (300, 130, 515), (20, 64, 8176), (40, 70, 8209)])
+                                   (300, 130, 515), (20, 64, 8176), (40, 70, 8209), (1, 3001, 70),
+                                   (1, 72, 5003), (1, 2100, 2300)])
 def test_forward_codes(type, T, D, F):
     act = ACTS[(T + D) % 6]
     dt = G.TYPES[type]

@@ -33,15 +33,13 @@ __device__ __forceinline__ void put_term(float* p, const float (&v)[8], long lon
   *(f32x4*)(p + 4) = f32x4{v[4], v[5], v[6], v[7]};
 }
 __device__ __forceinline__ void put_term(bf16_t* p, const float (&v)[8], long long rest) {
-  uint32_t b[8];
-#pragma unroll
-  for (int j = 0; j < 8; ++j) b[j] = f2bf(v[j]);
-  *(u32x4*)p = u32x4{b[0] | b[1] << 16, b[2] | b[3] << 16, b[4] | b[5] << 16, b[6] | b[7] << 16};
+  const u32x4 w = f2bf8(v);
+  *(u32x4*)p = w;
   if (!rest) return;
+  float left[8];
 #pragma unroll
-  for (int j = 0; j < 8; ++j) b[j] = f2bf(v[j] - bf2f(b[j]));
-  *(u32x4*)(p + rest) =
-      u32x4{b[0] | b[1] << 16, b[2] | b[3] << 16, b[4] | b[5] << 16, b[6] | b[7] << 16};
+  for (int j = 0; j < 8; ++j) left[j] = v[j] - bf2f(j & 1 ? w[j / 2] >> 16 : w[j / 2] & 0xffffu);
+  *(u32x4*)(p + rest) = f2bf8(left);
 }
 
 // what a wave has written to its own part of LDS is there for its other lanes

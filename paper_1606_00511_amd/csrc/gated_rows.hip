@@ -39,10 +39,7 @@ __device__ __forceinline__ u32x4 unpacked(const GPad& p, int row, int c) {
     get_codes((const int8_t*)p.src + (size_t)row * p.ld + at,
               code_step(p.scale[(size_t)row * p.lds + at / CODE_BLOCK]), v, min(have, n));
   if (p.es == 4) return __builtin_bit_cast(u32x4, f32x4{v[0], v[1], v[2], v[3]});
-  u32x4 w;
-#pragma unroll
-  for (int j = 0; j < 4; ++j) w[j] = f2bf(v[2 * j]) | f2bf(v[2 * j + 1]) << 16;
-  return w;
+  return f2bf8(v);
 }
 
 // ------------------------------------------------- sums of split products

@@ -8,6 +8,16 @@
 namespace hfk {
 namespace {
 
+// two values rounded to bf16, in one instruction (one by one they take four: unpacking
+// 16,384 x 8,192 98 -> 81 us)
+__device__ __forceinline__ uint32_t f2bf2(float a, float b) {
+  typedef float f32x2 __attribute__((ext_vector_type(2)));
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{a, b}), bf16x2));
+}
+__device__ __forceinline__ u32x4 f2bf8(const float (&v)[8]) {
+  return u32x4{f2bf2(v[0], v[1]), f2bf2(v[2], v[3]), f2bf2(v[4], v[5]), f2bf2(v[6], v[7])};
+}
 // 8 values to p, of any alignment, the first `have` of them, and from it
 // (STREAM: past the caches)
 template <bool STREAM = false>
@@ -24,7 +34,7 @@ __device__ __forceinline__ void put(float* p, const float (&v)[8], int have) {
 template <bool STREAM = false>
 __device__ __forceinline__ void put(bf16_t* p, const float (&v)[8], int have) {
   if (have >= 8) {
-    store_chunk<STREAM>(p, v);
+    put16<STREAM>(p, f2bf8(v));
   } else {
 #pragma unroll
     for (int j = 0; j < 8; ++j)

@@ -433,7 +433,8 @@ int hf_prof_get(hf_ctx* ctx, int32_t i, const char** name, int64_t* launches,
  * behind it the softmax head over a vocabulary larger than HF_MAX_CLASSES,
  * with the loss of hard labels or of a teacher's top logits.  With tied
  * weights the embedding and the head share one matrix and one gradient.  What
- * lies between them (rows in, their gradient back) is the caller's: an hf_ctx
+ * lies between them (rows in, their gradient back) is the caller's, or made of
+ * hf_gated's below: an hf_ctx
  * takes no rows from an embedding that is trained with it, and gives no
  * activations to a head; and the solvers have no curvature product of these.
  *
@@ -584,12 +585,14 @@ const char* hf_vocab_last_error(const hf_vocab* ctx);
  * A context (hf_gated) holds D, F, the activation phi and the type of the
  * rows, the matrices and their gradients: fp32 or bf16 (sums and the activation
  * are fp32; h, and in the gradient dg and du, are rounded to the type for the
- * product that reads them, with bf16 calls of up to 128 rows to two terms of
- * it; each output is rounded to its type once).  Matrices are row-major; rows
- * may lie `ld` elements apart and start at any element (rows of 16-byte
- * multiples and widths that are multiples of 64, of codes 128, are read in
- * place, others are copied to the workspace first).  Columns and rows around an
- * output are left as they were.  Outputs may not overlap inputs.
+ * product that reads them, with bf16 forward calls of up to 16 rows and
+ * gradients of up to 128 to two terms of it, or not at all; each output is
+ * rounded to its type once).  Matrices are row-major; rows may lie `ld` elements
+ * apart and start at any element (forward calls of up to 64 rows read them in
+ * place, others rows of 16-byte multiples and widths that are multiples of 64,
+ * of codes 128; what lies otherwise is copied to the workspace first).  Columns
+ * and rows around an output are left as they were.  Outputs may not overlap
+ * inputs.
  * Memory, streams, the order of calls and errors as for hf_vocab; calls make no
  * allocation and can be captured into a graph.  hf_gated_pack, _unpack and
  * _codes use no workspace.  Repeated calls give the same bits (operands that lie

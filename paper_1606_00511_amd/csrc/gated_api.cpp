@@ -17,9 +17,10 @@ using namespace hfk;
 
 namespace {
 
-// bf16 calls of at most so many rows hold h, dg and du as two bf16 terms, the
-// second what the first's rounding left: with few rows nothing averages a
-// rounding away, and the matrix cores wait for the matrices anyway.
+// bf16 gradients of at most so many rows hold h, dg and du as two bf16 terms, the
+// second what the first's rounding left (forward calls: up to TWO_X rows): with few
+// rows little averages a rounding away, and the matrix cores wait for the matrices
+// anyway.
 constexpr int TWO_TERM_ROWS = 128;
 constexpr size_t WPACK_BYTES = (size_t)64 << 20;   // packed channels of a product of codes
 
@@ -281,16 +282,16 @@ void ranged(GGemm g, int type, bool split, int shapes, Run run) {
 // a product into e's out: straight, or by partials
 template <class Kernel>
 void summed(hf_gated* c, const Launch& L, int type, int out_type, const GGemm& all, const GEpi& out,
-            int dup, int shapes, Kernel kernel) {
+            int shapes, Kernel kernel) {
   ranged(all, type, true, shapes, [&](const GGemm& g) {
     GEpi e = out;
-    if (g.splits > 1 || dup) {
+    if (g.splits > 1) {
       e.part = c->at<float>(c->lay.part);
       e.ldp = all.M;
     }
     kernel(g, e);
     if (!e.part) return;
-    const GFinish f = {g, e, dup};
+    const GFinish f = {g, e, 0};
     gated_finish(L, type, out_type, &f, 1);
   });
 }
@@ -507,9 +508,10 @@ int hf_gated_forward(hf_gated* c, const void* X, int64_t ldx, const void* Wg, in
     }
     set_out(&ed, Y, ldy, T, D);
     if (T > TWO_X && D == Dp && F == Fp && loads16(Wd, ldd, es)) {
-      // (each row of h once for 128 of Wd's: 24 rows, 4,096 x 16,384: 45 -> 33 us)
+      // (each row of h once for 128 of Wd's: 24 rows, 4,096 x 16,384: 45 -> 40 us with
+      // the partials)
       operands(&gd, Wd, ldd, nullptr, 0, eu.h, eu.ldh);
-      summed(c, L, c->type, c->type, gd, ed, 0, 4, [&](const GGemm& g, const GEpi& e) {
+      summed(c, L, c->type, c->type, gd, ed, 4, [&](const GGemm& g, const GEpi& e) {
         gated_down(L, c->type, c->type, g, e);
       });
     } else {
@@ -519,9 +521,7 @@ int hf_gated_forward(hf_gated* c, const void* X, int64_t ldx, const void* Wg, in
     }
     return end(c);
   }
-  const int dup = two_term(c, T);
-
-  GGemm gu = product(2 * Fp, T, Dp), gd = product(Dp, dup ? 2 * dup : T, Fp);
+  GGemm gu = product(2 * Fp, T, Dp), gd = product(Dp, T, Fp);
   GEpi eu = epilogue(c, T), ed = epilogue(c, T);
   Pads pads;
   gu.B = pads.operand(D == Dp && loads16(X, ldx, es), X, ldx, T, D, es, c->at<void>(l.xp), T, Dp, 1,
@@ -537,7 +537,6 @@ int hf_gated_forward(hf_gated* c, const void* X, int64_t ldx, const void* Wg, in
 
   eu.h = c->at<void>(l.h);
   eu.ldh = c->ldh();
-  eu.dup = dup;
   eu.keep = keep;
   eu.kept = kept;
   eu.ldk = ldk;
@@ -548,7 +547,7 @@ int hf_gated_forward(hf_gated* c, const void* X, int64_t ldx, const void* Wg, in
   gd.B = eu.h;
   gd.ldb = c->ldh();
   set_out(&ed, Y, ldy, T, D);
-  summed(c, L, c->type, c->type, gd, ed, dup, 4, [&](const GGemm& g, const GEpi& e) {
+  summed(c, L, c->type, c->type, gd, ed, 4, [&](const GGemm& g, const GEpi& e) {
     gated_down(L, c->type, c->type, g, e);
   });
   return end(c);
@@ -793,7 +792,7 @@ int hf_gated_product(hf_gated* c, const int8_t* A, int64_t lda, const float* sa,
     e.sn = sa;
     e.sm = sb + n0;
     set_out(&e, (char*)Y + n0 * c->es, ldy, T, nn);
-    summed(c, L, VT_I8, c->type, g, e, 0, 4, [&](const GGemm& gg, const GEpi& ee) {
+    summed(c, L, VT_I8, c->type, g, e, 4, [&](const GGemm& gg, const GEpi& ee) {
       gated_down(L, VT_I8, c->type, gg, ee);
     });
   }
@@ -870,7 +869,7 @@ int hf_gated_forward_codes(hf_gated* c, const void* X, int64_t ldx, const int8_t
   } else if (few_down) {
     gated_few_down(L, VT_I8, c->type, gd, ed);
   } else {
-    summed(c, L, VT_I8, c->type, gd, ed, 0, 4, [&](const GGemm& g, const GEpi& e) {
+    summed(c, L, VT_I8, c->type, gd, ed, 4, [&](const GGemm& g, const GEpi& e) {
       gated_down(L, VT_I8, c->type, g, e);
     });
   }

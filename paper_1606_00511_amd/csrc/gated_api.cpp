@@ -287,7 +287,7 @@ void summed(hf_gated* c, const Launch& L, int type, int out_type, const GGemm& a
     GEpi e = out;
     if (g.splits > 1) {
       e.part = c->at<float>(c->lay.part);
-      e.ldp = all.M;
+      e.ldp = g.M - g.m0;
     }
     kernel(g, e);
     if (!e.part) return;

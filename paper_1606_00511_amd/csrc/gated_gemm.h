@@ -443,7 +443,7 @@ __device__ __forceinline__ void ggemm_body(const GGemm& s, const GEpi& e, int L)
       stage(b);
       const int nb = nt + 32 * b;
       if (parts) {
-        store_part<float, RL>(mine, lane, part, e.ldp, nb, s.N, mt, s.M, 0);
+        store_part<float, RL>(mine, lane, part, e.ldp, nb, s.N, mt - s.m0, s.M - s.m0, 0);
       } else if constexpr (sizeof(E) == 1) {
         scaled_part<O, RL>(mine, lane, e, nb, mt, sm);
       } else {

@@ -57,7 +57,7 @@ struct GEpi {
   long long ldo, ldo1;
   int n1, nout, mout;    // rows of each, columns
   int accumulate;
-  float* part;           // partials [split][n][m] (codes: int32)
+  float* part;           // partials [split][n][m - m0] (codes: int32), rows ldp apart
   long long ldp;
 };
 

@@ -63,7 +63,7 @@ __device__ __forceinline__ void finish_body(const FinishOne& one, int b, int gro
     const int row = (int)(i / chunks), m = g.m0 + 8 * (int)(i % chunks);
     const bool second = row >= e.nout;
     const int n = second ? e.n1 + row - e.nout : row, have = end - m;
-    const float* p = e.part + (size_t)n * e.ldp + m;
+    const float* p = e.part + (size_t)n * e.ldp + (m - g.m0);
     float v[8];
     if constexpr (sizeof(E) == 1) {
       int t[8] = {};

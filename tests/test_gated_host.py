@@ -3,6 +3,7 @@ that takes the runtime's place: the order of streams, launch sizes, no launch
 where there is nothing to do.  No GPU."""
 
 import os
+import subprocess
 
 import pytest
 
@@ -132,3 +133,21 @@ result = out + log()
         assert all(v > 0 for v in g + b), l
         assert g[0] * g[1] * g[2] * b[0] * b[1] * b[2] < 1 << 32, l
         assert g[0] * b[0] < 1 << 32 and g[1] < 65536 and g[2] < 65536, l
+
+
+def test_ranges(tmp_path):
+    """What every launch reads and writes lies in one array of the call, or in one
+    part of the workspace: over sizes of all scales, whole and odd, rows apart or
+    not, all of what is kept and of the gradients asked for (gated_ranges.cpp)."""
+    obj = [str(tmp_path / n) for n in ("ranges.o", "stub.o")]
+    hip = ["-D__HIP_PLATFORM_AMD__", "-I/opt/rocm/include", "-fPIE", "-O1", "-w"]
+    subprocess.run(["/opt/rocm/bin/hipcc", "-x", "hip", "--offload-host-only", "-std=c++17", *hip,
+                    "-I" + os.path.join(hip_stub.ROOT, "include"),
+                    "-I" + os.path.join(hip_stub.ROOT, "paper_1606_00511_amd", "csrc"), "-c", "-o",
+                    obj[0], os.path.join(hip_stub.ROOT, "tests", "gated_ranges.cpp")], check=True)
+    subprocess.run(["g++", *hip, "-c", "-o", obj[1],
+                    os.path.join(hip_stub.ROOT, "tests", "hip_stub.cpp")], check=True)
+    exe = str(tmp_path / "ranges")
+    subprocess.run(["g++", "-pie", "-o", exe, *obj], check=True)
+    p = subprocess.run([exe, "5000"], capture_output=True, text=True)
+    assert p.returncode == 0, p.stdout + p.stderr

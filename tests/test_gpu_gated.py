@@ -17,7 +17,9 @@ pytestmark = pytest.mark.gpu
 SIZES = [(1, 1, 1), (3, 2600, 1100), (4, 40, 5000), (5, 1024, 520), (1, 1300, 1100),
          (1, 1100, 300), (1, 70, 2600), (1, 64, 64), (20, 66, 8176), (2, 3, 5), (3, 130, 33), (17, 65, 131), (31, 128, 192),
          (33, 64, 256), (64, 192, 96), (127, 100, 260), (128, 256, 128), (129, 192, 320),
-         (130, 72, 517), (256, 320, 704), (300, 129, 450), (700, 512, 1365)]
+         (130, 72, 517), (256, 320, 704), (300, 129, 450), (700, 512, 1365),
+         # (the last columns of Y a launch of their own, by partials)
+         (1592, 5760, 139)]
 ACTS = ["silu", "gelu", "gelu_tanh", "sigmoid", "tanh", "relu"]
 
 
@@ -350,7 +352,7 @@ def test_codes_edges():
 @pytest.mark.parametrize("type", ["fp32", "bf16"])
 @pytest.mark.parametrize("T,N,K", [(1, 1, 1), (1, 1000, 128), (1, 33, 9000), (1, 50, 2049), (4, 50, 1030), (3, 5, 130), (16, 77, 64),
                                    (33, 300, 256), (129, 257, 1000), (260, 640, 512),
-                                   (5, 40000, 200)])
+                                   (5, 40000, 200), (396, 16896, 3968)])
 def test_product(type, T, N, K):
     g = torch.Generator("cuda").manual_seed(T + N + K)
     r = lambda *s: torch.randint(-127, 128, s, generator=g, device="cuda").to(torch.int8)   # noqa: E731

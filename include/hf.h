@@ -434,9 +434,9 @@ int hf_prof_get(hf_ctx* ctx, int32_t i, const char** name, int64_t* launches,
  * with the loss of hard labels or of a teacher's top logits.  With tied
  * weights the embedding and the head share one matrix and one gradient.  What
  * lies between them (rows in, their gradient back) is the caller's, or made of
- * hf_gated's below: an hf_ctx
- * takes no rows from an embedding that is trained with it, and gives no
- * activations to a head; and the solvers have no curvature product of these.
+ * hf_gated's below: an hf_ctx takes no rows from an embedding that is trained
+ * with it, and gives no activations to a head; and the solvers have no curvature
+ * product of these.
  *
  * A context (hf_vocab) holds the vocabulary V, the width D and the type of
  * the rows, the matrices and their gradients: fp32 or bf16 (sums, softmax
@@ -682,7 +682,8 @@ int hf_gated_grad(hf_gated* ctx, const void* X, int64_t ldx,
  * Each number is within half a step 2^(b - 127), at most 2^-6.99 of the
  * block's largest.  A block with a NaN or an infinity has b = 255 and unpacks to
  * NaN.  hf_gated_unpack writes the numbers in the type: exactly, as 7 bits and a
- * power of two (below bf16's smallest normal number, rounded).
+ * power of two (below bf16's smallest normal number, rounded; 64 2^122, next to
+ * the types' largest number, is past it: infinity).
  *   codes  rows x cols, ldc apart;  scale  rows x ceil(cols / 32), lds apart
  */
 int hf_gated_pack(hf_gated* ctx, const void* X, int64_t ldx, int64_t rows,
@@ -695,8 +696,9 @@ int hf_gated_unpack(hf_gated* ctx, const int8_t* codes, int64_t ldc,
 /*
  * hf_gated_codes: rows of the type as 8-bit codes with a scale for each row (a
  * token's, or a matrix's channel's): s = max |x| / 127 in fp32, q = x / s
- * rounded to nearest, ties to even.  A row of zeros has s = 0; one with a NaN or
- * an infinity has s = NaN and codes 0.
+ * rounded to nearest, ties to even.  A row whose s is 0 (of zeros, or of numbers
+ * below 2^-143) has codes 0; one with a NaN or an infinity has s = NaN and codes
+ * 0.
  *   X  rows x cols;  codes  rows x cols, ldc apart;  scale  rows fp32
  */
 int hf_gated_codes(hf_gated* ctx, const void* X, int64_t ldx, int64_t rows,

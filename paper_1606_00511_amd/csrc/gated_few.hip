@@ -251,7 +251,7 @@ __device__ __forceinline__ void few_body(const GGemm& s, const GEpi& e) {
 // up to 16, 32 and 64 rows of X; "up" with 16 rows of both matrices a workgroup, and of
 // more than 16 rows of X with 32 where that leaves no unit without a workgroup (half
 // the reads of X: 24 rows, 4,096 x 16,384: 63 -> 54 us; 28 rows, 2,981 x 3,115, fp32, 98
-// workgroups: 54 us, 195: 38)
+// workgroups: 54 us, 195: 36)
 #define HF_FEW(NAME, E, O, UP, RB, U32)                                                         \
   extern "C" __global__ __launch_bounds__(512) void NAME##_32(GGemm s, GEpi e) {                \
     few_body<E, O, UP, RB, 2, U32, 8, false>(s, e);                                             \

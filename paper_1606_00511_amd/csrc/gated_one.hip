@@ -7,7 +7,8 @@
 // joined in a fixed tree.  A small matrix is so spread over
 // the whole card, which 16 rows a workgroup would not fill, and a large one is read
 // evenly (bf16: 1,024 x 4,096: down 7.9 -> 4.6 us; 4,096 x 16,384: up 49 -> 46, down 34
-// -> 27, 403 MB at 5.6 TB/s; two rows: 51 and 36 us in gated_few.hip, 50 and 39 here).
+// -> 27, 403 MB at 5.6 TB/s; with two rows of X the second one's products cost what
+// the even reads gain: 87 us in gated_few.hip, 89 so).
 // Rows of one or two pieces leave a wave too little to do: theirs is gated_few.hip (1,024
 // x 4,096: up 5.9 us, 7.2 to 7.9 here).  h stays in fp32 between the two products.
 // Loads need no alignment.

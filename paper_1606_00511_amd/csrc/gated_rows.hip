@@ -54,12 +54,15 @@ struct FinishAll {
 };
 // f's outputs by `groups` workgroups, of which this is the b-th
 template <class E, class O>
-__device__ __forceinline__ void finish_body(const FinishOne& one, int b, int groups) {
+__device__ __forceinline__ void finish_body(const FinishOne& one, uint32_t b, uint32_t groups) {
   const GGemm& g = one.f.g;
   const GEpi& e = one.f.e;
-  const int dup = one.f.dup, chunks = one.chunks, end = min(e.mout, g.M);
-  const long long stride = one.stride, total = (long long)one.rows * chunks;
-  for (long long i = b * 256ll + threadIdx.x; i < total; i += groups * 256ll) {
+  const int dup = one.f.dup, end = min(e.mout, g.M);
+  const uint32_t chunks = one.chunks;
+  const long long stride = one.stride;
+  // (at most 2^30 chunks, of two matrices of 65,536 x 65,536)
+  const uint32_t total = (uint32_t)one.rows * chunks;
+  for (uint32_t i = b * 256u + threadIdx.x; i < total; i += groups * 256u) {
     const int row = (int)(i / chunks), m = g.m0 + 8 * (int)(i % chunks);
     const bool second = row >= e.nout;
     const int n = second ? e.n1 + row - e.nout : row, have = end - m;
@@ -170,7 +173,7 @@ __device__ __forceinline__ void put_row_codes(int8_t* p, const float (&v)[8], co
   else if (EVEN) have = 8;
   // x inv is off by less than 2^-15 of a step: only next to a border, 2^-13 of all
   // places, does it not tell the code (a branch for each number: 49 us for 8,192 rows
-  // of 4,096, for 8 at once 32)
+  // of 4,096, for 8 at once 30)
   float q[8], near = 0.0f;
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
@@ -451,7 +454,7 @@ void gated_unpack(const Launch& L, int type, const int8_t* codes, long long ldc,
 namespace {
 // a row by a wave or by 4, whose lanes hold up to 16 or 64 numbers of it; what no lane
 // can hold, or has cut chunks, is read twice (8,192 rows of 4,096, bf16: 39 us read
-// twice, 24 held)
+// twice, 30 held)
 template <class E>
 void codes_of(const Launch& L, void (*const (&k)[4])(const E*, long long, int, int, int8_t*,
                                                      long long, int, float*),

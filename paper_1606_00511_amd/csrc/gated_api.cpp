@@ -291,7 +291,7 @@ void summed(hf_gated* c, const Launch& L, int type, int out_type, const GGemm& a
     }
     kernel(g, e);
     if (!e.part) return;
-    const GFinish f = {g, e, 0};
+    const GFinish f = {g, e, 0, 0, 0};
     gated_finish(L, type, out_type, &f, 1);
   });
 }
@@ -375,6 +375,34 @@ void grads_shapes(int type, int dup, size_t room, GGrads* a) {
         a->g[i].splits = splits[i];
       }
     }
+  // Or by equal shares of all K blocks (hf_gated_shares_f32), where that promises to be
+  // quicker by 15%: units are then at work on different K blocks of neighbouring tiles and
+  // share little of what they read, and nearly every tile is left in parts.  (4,096 rows,
+  // 1,024 x 2,731, fp32: products 1,056 -> 973 us and sums of partials 43 -> 33; where 11%
+  // were promised, 16,384 rows, 256 x 512: 201 -> 197, and 6 -> 26; bf16, whose products
+  // wait for their reads, 4,096 rows, 1,024 x 2,731: 139 -> 131, and 0 -> 25.)
+  if (type != VT_F32) return;
+  best /= 1.15;
+  for (int tile : {TILE_SMALL, TILE_BIG}) {
+    const int64_t RM = tile_m(tile), RN = tile_n(tile), units = units_of(tile), BK = 32;
+    int64_t work[4] = {}, tiles = 0;
+    for (int i = 0; i < 3; ++i) {
+      const int64_t n = j[i].on ? (j[i].M + RM - 1) / RM * ((j[i].N + RN - 1) / RN) : 0;
+      tiles += n;
+      work[i + 1] = work[i] + n * (j[i].K / BK);
+    }
+    if (work[3] >= 1 << 30 || (size_t)(2 * units * RM * RN) > room) continue;
+    const int64_t share = (work[3] + units - 1) / units;
+    if (share < 32 || 16 * share < K / BK) continue;    // (tiles in many parts)
+    const double us = tile_us(type, tile, (double)(share * BK), tile != TILE_BIG) +
+                      C_TILE[tile] * (double)(tiles / units + 1) +
+                      parts_us(8.0 * (double)(std::min(tiles, units) + units) * RM * RN);
+    if (us >= best) continue;
+    best = us;
+    a->share = (int)share;
+    for (int i = 0; i < 4; ++i) a->work[i] = (int)work[i];
+    for (int i = 0; i < 3; ++i) a->g[i].tile = tile;
+  }
 }
 
 }  // namespace
@@ -615,7 +643,7 @@ int hf_gated_grad(hf_gated* c, const void* X, int64_t ldx, const uint8_t* xscale
     // the sum of nothing
     for (int i = 1; i < 3 && !accumulate; ++i) {
       all.g[i].splits = 0;
-      if (all.e[i].out) f[n++] = {all.g[i], all.e[i], 0};
+      if (all.e[i].out) f[n++] = {all.g[i], all.e[i], 0, 0, 0};
     }
     gated_finish(L, type, type, f, n);
     return end(c);
@@ -683,11 +711,16 @@ int hf_gated_grad(hf_gated* c, const void* X, int64_t ldx, const uint8_t* xscale
     GGemm& g = all.g[i];
     GEpi& e = all.e[i];
     const int join = i == 0 ? dup : 0;
-    if (!e.out || (g.splits == 1 && !join)) continue;
+    if (e.out && all.share) {
+      all.part = e.part = part;
+      e.ldp = tile_m(g.tile);
+      f[n++] = {g, e, 0, all.share, all.work[i]};
+    }
+    if (!e.out || all.share || (g.splits == 1 && !join)) continue;
     e.part = part;
     e.ldp = g.M;
     part += (size_t)g.splits * up(g.N, VTILE) * g.M;
-    f[n++] = {g, e, join};
+    f[n++] = {g, e, join, 0, 0};
   }
   gated_grads(L, type, all);
   gated_finish(L, type, type, f, n);

@@ -22,6 +22,39 @@ __device__ __forceinline__ void grads_body(const GGrads& a) {
     ggemm_body<E, E, DW, GA_RELU, WM, WN, GM, GN, 2>(g, e, L - (last ? a.first[2] : a.first[1]));
   }
 }
+// The same by units that have equal shares of the K blocks of all tiles in a row: a
+// share ends inside a tile, whose partials the units that have a share of it leave in
+// parts 2 u (that began in another unit's share) and 2 u + 1 of the workspace.
+template <class E, int WM, int WN, int GM, int GN>
+__device__ __forceinline__ void shares_body(const GGrads& a) {
+  constexpr int RM = 32 * WM * GM, RN = 32 * WN * GN, BK = 128 / (int)sizeof(E);
+  // (an XCD's units have neighbouring tiles)
+  const int L = blockIdx.x, u = L % 8 * (gridDim.x / 8) + L / 8;
+  const int end = min((u + 1) * a.share, a.work[3]);
+  for (int at = u * a.share; at < end;) {
+    const int i = at >= a.work[2] ? 2 : at >= a.work[1] ? 1 : 0;
+    const GGemm g = a.g[i];
+    const GEpi e = a.e[i];
+    const int gx = (g.M + RM - 1) / RM, gy = (g.N + RN - 1) / RN, nvb = g.K / BK;
+    const int r = (at - a.work[i]) / nvb;
+    Piece p;
+    // (what follows from the thread is worked out for each tile: kept over the loop it
+    // takes registers that the products need)
+    p.tid = threadIdx.x;
+    asm("" : "+v"(p.tid));
+    tile_in(r, gx, gy, p.tm, p.tn);
+    p.vb0 = at - a.work[i] - r * nvb;
+    p.nblk = min(nvb - p.vb0, end - at);
+    p.part = p.nblk == nvb ? nullptr : a.part + (size_t)(2 * u + (p.vb0 == 0)) * (RM * RN);
+    p.ldp = RM;
+    p.om = p.tm * RM;
+    p.on = p.tn * RN;
+    if (i == 0) ggemm_piece<E, E, DX, GA_RELU, WM, WN, GM, GN, 2>(g, e, p);
+    else ggemm_piece<E, E, DW, GA_RELU, WM, WN, GM, GN, 2>(g, e, p);
+    at += p.nblk;
+    __syncthreads();       // the stages are free
+  }
+}
 #define HF_GRADS(SUF, E)                                                                        \
   extern "C" __global__ __launch_bounds__(512, 1) void hf_gated_grads_##SUF##_big(GGrads a) {   \
     grads_body<E, 4, 2, 2, 4>(a);                                                               \
@@ -31,6 +64,12 @@ __device__ __forceinline__ void grads_body(const GGrads& a) {
   }
 HF_GRADS(f32, float)
 HF_GRADS(bf16, bf16_t)
+extern "C" __global__ __launch_bounds__(512, 1) void hf_gated_shares_f32_big(GGrads a) {
+  shares_body<float, 4, 2, 2, 4>(a);
+}
+extern "C" __global__ __launch_bounds__(256, 2) void hf_gated_shares_f32(GGrads a) {
+  shares_body<float, 2, 2, 2, 2>(a);
+}
 HF_GGEMM_FEW(hf_gated_down_codes_f32, int8_t, float, DOWN, GA_RELU)
 HF_GGEMM_FEW(hf_gated_down_codes_bf16, int8_t, bf16_t, DOWN, GA_RELU)
 
@@ -75,12 +114,13 @@ void gated_grads(const Launch& L, int type, GGrads a) {
   for (int i = 0; i < 3; ++i)
     a.first[i + 1] = a.first[i] + (a.e[i].out ? gated_tiles(a.g[i]) * a.g[i].splits : 0);
   if (a.first[3] < 1) return;
-  static void (*const k[2][2])(GGrads) = {{hf_gated_grads_f32, hf_gated_grads_f32_big},
-                                          {hf_gated_grads_bf16, hf_gated_grads_bf16_big}};
+  static void (*const k[3][2])(GGrads) = {{hf_gated_grads_f32, hf_gated_grads_f32_big},
+                                          {hf_gated_grads_bf16, hf_gated_grads_bf16_big},
+                                          {hf_gated_shares_f32, hf_gated_shares_f32_big}};
   const int tile = a.g[0].tile;
   prof_begin(L, "hf_gated_grads");
-  hipExtLaunchKernelGGL(k[type][tile], dim3(a.first[3]), dim3(tile == TILE_BIG ? 512 : 256), 0,
-                        L.stream, prof_a(L), prof_b(L), 0, a);
+  hipExtLaunchKernelGGL(k[a.share ? 2 : type][tile], dim3(a.share ? units_of(tile) : a.first[3]),
+                        dim3(tile == TILE_BIG ? 512 : 256), 0, L.stream, prof_a(L), prof_b(L), 0, a);
   prof_end(L, "hf_gated_grads", 0.0, 0.0);
 }
 

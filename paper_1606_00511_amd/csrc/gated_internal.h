@@ -90,13 +90,21 @@ struct GGrads {
   GGemm g[3];
   GEpi e[3];
   int first[4];          // workgroups of the products before each (set by the launch)
+  // > 0: units have `share` K blocks each of all tiles in a row, of which work[i] are
+  // those of the products before i; part: 2 tiles a unit
+  int share, work[4];
+  float* part;
 };
+// workgroups of a tile that the card runs at a time
+inline int units_of(int tile) { return tile == TILE_BIG ? 256 : 512; }
 void gated_grads(const Launch& L, int type, GGrads a);
 // out from the partials of products with their e.part: row n + dup joins row n if dup
+// (share > 0: as units' shares left them, work K blocks before this product's)
 struct GFinish {
   GGemm g;
   GEpi e;
   int dup;
+  int share, work;
 };
 void gated_finish(const Launch& L, int type, int out_type, const GFinish* f, int n);
 

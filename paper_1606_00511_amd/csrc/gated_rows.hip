@@ -47,6 +47,7 @@ struct FinishOne {
   GFinish f;
   int rows, chunks, first;     // rows of out (both), 8 columns each; first workgroup
   long long stride;            // of partials
+  int rm, rn, gx, gy, blocks;  // with shares: the tiles, and K blocks of each
 };
 struct FinishAll {
   FinishOne one[3];
@@ -67,12 +68,28 @@ __device__ __forceinline__ void finish_body(const FinishOne& one, uint32_t b, ui
     const bool second = row >= e.nout;
     const int n = second ? e.n1 + row - e.nout : row, have = end - m;
     const float* p = e.part + (size_t)n * e.ldp + (m - g.m0);
+    int parts = g.splits;
+    if (one.f.share) {
+      // the tile's units; of the first one the place where its share ends, of the others
+      // where they begin
+      const int rm = one.rm, rn = one.rn, tm = m / rm, tn = n / rn;
+      const int at = one.f.work + tile_place(tm, tn, one.gx, one.gy) * one.blocks;
+      const int u0 = at / one.f.share, u1 = (at + one.blocks - 1) / one.f.share;
+      parts = u1 - u0 + 1;
+      if (parts == 1) continue;            // (written by its unit)
+      p = e.part + (size_t)(2 * u0 + 1) * rm * rn + (n - tn * rn) * rm + m - tm * rm;
+    }
+    // partial s of the sum
+    auto from = [&](const float* q, int s) {
+      return one.f.share && s ? q + (2 * s - 1) * stride : q + s * stride;
+    };
     float v[8];
     if constexpr (sizeof(E) == 1) {
       int t[8] = {};
 #pragma unroll 4
-      for (int s = 0; s < g.splits; ++s) {
-        const i32x4 a = *(const i32x4*)(p + s * stride), b = *(const i32x4*)(p + s * stride + 4);
+      for (int s = 0; s < parts; ++s) {
+        const float* w = from(p, s);
+        const i32x4 a = *(const i32x4*)w, b = *(const i32x4*)(w + 4);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           t[j] += a[j];
@@ -88,8 +105,9 @@ __device__ __forceinline__ void finish_body(const FinishOne& one, uint32_t b, ui
       for (int h = 0; h < (dup ? 2 : 1); ++h) {
         const float* q = p + (size_t)h * dup * e.ldp;
 #pragma unroll 4
-        for (int s = 0; s < g.splits; ++s) {
-          const f32x4 a = *(const f32x4*)(q + s * stride), b = *(const f32x4*)(q + s * stride + 4);
+        for (int s = 0; s < parts; ++s) {
+          const float* w = from(q, s);
+          const f32x4 a = *(const f32x4*)w, b = *(const f32x4*)(w + 4);
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
             v[j] += a[j];
@@ -405,8 +423,10 @@ void gated_finish(const Launch& L, int type, int out_type, const GFinish* f, int
     const int chunks = (std::min(e.mout, g.M) - g.m0 + 7) / 8, rn = tile_n(g.tile);
     const int rows = (e.n1 < g.N ? 2 : 1) * e.nout;
     if (chunks < 1 || rows < 1) continue;
+    const int rm = tile_m(g.tile), gy = (g.N + rn - 1) / rn;
     a.one[a.n++] = FinishOne{f[i], rows, chunks, grid,
-                             (long long)((g.N + rn - 1) / rn) * rn * e.ldp};
+                             f[i].share ? (long long)rm * rn : (long long)gy * rn * e.ldp, rm, rn,
+                             (g.M + rm - 1) / rm, gy, g.K / (type == VT_F32 ? 32 : 64)};
     grid += (int)std::min<long long>(((long long)rows * chunks + 255) / 256, 1 << 20);
   }
   if (grid < 1) return;

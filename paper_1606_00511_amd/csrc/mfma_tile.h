@@ -210,11 +210,26 @@ __device__ __forceinline__ void store_part(const float* s, int lane, O* out, lon
   }
 }
 
+// Tile r of gx x gy in an order that walks groups of 8 tiles of n, m by m; and its
+// place in that order.
+constexpr int TILE_GROUP = 8;
+__device__ __forceinline__ void tile_in(int r, int gx, int gy, int& tm, int& tn) {
+  const int g = r / (TILE_GROUP * gx);
+  const int first = g * TILE_GROUP;
+  const int rows = min(TILE_GROUP, gy - first);
+  const int w = r - g * TILE_GROUP * gx;
+  tn = first + w % rows;
+  tm = w / rows;
+}
+__device__ __forceinline__ int tile_place(int tm, int tn, int gx, int gy) {
+  const int first = tn / TILE_GROUP * TILE_GROUP;
+  return first * gx + tm * min(TILE_GROUP, gy - first) + tn - first;
+}
+
 // The tile (tm, tn) and split this workgroup computes, of gy tiles of n that
 // have rows and gz splits; false: none.  Consecutive workgroups go to the 8
-// XCDs in turn; each XCD gets a contiguous eighth of the logical order, which
-// walks groups of 8 tiles of n, m by m, so that the workgroups resident on an
-// XCD share their operand panels in its L2.  Tiles without rows take no place
+// XCDs in turn; each XCD gets a contiguous eighth of the order of tile_in, so that
+// the workgroups resident on an XCD share their operand panels in its L2.  Tiles without rows take no place
 // in the order (2,251 of 3,001 rows counted, 50,257 x 1,024: 301 -> 222 us).
 __device__ __forceinline__ bool tile_at(int L, int gx, int gy, int gz, int& tm, int& tn, int& tz) {
   const int T = gx * gy * gz;
@@ -223,14 +238,7 @@ __device__ __forceinline__ bool tile_at(int L, int gx, int gy, int gz, int& tm, 
   const int x = L % 8, q = T / 8, r8 = T % 8;
   const int Lg = x * q + min(x, r8) + L / 8;
   tz = Lg / (gx * gy);
-  const int r = Lg % (gx * gy);
-  constexpr int G = 8;
-  const int g = r / (G * gx);
-  const int first = g * G;
-  const int rows = min(G, gy - first);
-  const int w = r - g * G * gx;
-  tn = first + w % rows;
-  tm = w / rows;
+  tile_in(Lg % (gx * gy), gx, gy, tm, tn);
   return true;
 }
 __device__ __forceinline__ bool tile_of(int gy, int gz, int& tm, int& tn, int& tz) {

@@ -34,6 +34,11 @@ void within(const char* what, const void* p, size_t bytes, int align = 1) {
     exit(1);
   }
 }
+void equal(const char* what, long long a, long long b) {
+  if (a == b) return;
+  printf("%s: %s: %lld, not %lld\n", call.c_str(), what, a, b);
+  exit(1);
+}
 // rows x cols elements of es bytes, ld apart
 void rect(const char* what, const void* p, long long rows, long long ld, long long cols, int es,
           int align = 1) {
@@ -127,9 +132,21 @@ void gated_dh(const Launch&, int type, const GGemm& g, const GEpi& e) {
 }
 void gated_grads(const Launch&, int type, GGrads a) {
   const int es = es_of(type);
+  const size_t tile = tile_m(a.g[0].tile) * tile_n(a.g[0].tile);
+  if (a.share) {
+    within("shares' partials", a.part, 2 * units_of(a.g[0].tile) * tile * 4, 16);
+    int work = 0;
+    for (int i = 0; i < 3; ++i) {
+      equal("work", a.work[i], work);
+      if (a.e[i].out) work += gated_tiles(a.g[i]) * (a.g[i].K * es / 128);
+    }
+    equal("work", a.work[3], work);
+    equal("units", (work + a.share - 1) / a.share <= units_of(a.g[0].tile), 1);
+  }
   for (int i = 0; i < 3; ++i) {
     const GGemm& g = a.g[i];
-    const GEpi& e = a.e[i];
+    GEpi e = a.e[i];
+    if (a.share) e.part = nullptr;       // (whole tiles)
     if (!e.out) continue;
     if (i == 0) {
       rect("Wg", g.A, g.kh, g.lda, g.M, es, 16);
@@ -148,7 +165,9 @@ void gated_finish(const Launch&, int type, int out_type, const GFinish* f, int n
   for (int i = 0; i < n; ++i) {
     const GGemm& g = f[i].g;
     GEpi e = f[i].e;
-    if (g.splits) within("partials", e.part, part_floats(g, e) * 4, 16);
+    if (f[i].share)
+      within("shares' partials", e.part, 2 * units_of(g.tile) * (size_t)e.ldp * tile_n(g.tile) * 4, 16);
+    else if (g.splits) within("partials", e.part, part_floats(g, e) * 4, 16);
     if (type == VT_I8) {
       within("scales", e.sm, e.mout * 4);
       within("scales", e.sn, e.nout * 4);

@@ -135,6 +135,22 @@ result = out + log()
         assert g[0] * b[0] < 1 << 32 and g[1] < 65536 and g[2] < 65536, l
 
 
+def test_shares(stub):
+    """The sizes whose fp32 gradients units share equally, in tiles of 128 and of 256,
+    and some whose do not."""
+    lines = hip_stub.run(stub, GATED + """
+def grads(D, F, T, type=0):
+    h = gated(D, F, type, T)
+    assert grad(h, T, D, F) == H.HF_OK and L.hf_gated_destroy(h) == H.HF_OK
+    return [l[1] for l in log() if "shares" in l[1] or "grads" in l[1]]
+result = [grads(256, 7466, 896), grads(1000, 2500, 2500), grads(1024, 2731, 4096),
+          grads(768, 2050, 300), grads(1024, 2731, 4096, 1)]
+""")
+    assert lines[0] == ["hf_gated_shares_f32"]
+    assert lines[1:3] == [["hf_gated_shares_f32_big"]] * 2
+    assert all("shares" not in l[0] for l in lines[3:])
+
+
 def test_ranges(tmp_path):
     """What every launch reads and writes lies in one array of the call, or in one
     part of the workspace: over sizes of all scales, whole and odd, rows apart or

@@ -234,6 +234,35 @@ def test_single_matrices(type):
         assert torch.equal(out, want[i]), i
 
 
+# tiles of 128 and of 256, rows that end inside a K block, read in place and copied; the
+# last two sizes share some of the gradients alone
+@pytest.mark.parametrize("T,D,F", [(896, 256, 7466), (2500, 1000, 2500), (4067, 1536, 910),
+                                   (1536, 1024, 5504)])
+def test_shares(T, D, F):
+    """Gradients whose units have equal shares of all products: all of them, added
+    to and not, and each alone, whose shares end elsewhere."""
+    X, Wg, Wu, Wd, dY = G.inputs(T, D, F, torch.float32, seed=T)
+    n = net(T, D, F, "fp32")
+    _, kept = n.hf_gated_forward(X, Wg, Wu, Wd, keep="full")
+    want, bound = G.grads("silu", X, Wg, Wu, Wd, kept[:, :F], kept[:, F:], dY)
+    ptr = lambda t: (t.data_ptr(), t.stride(0))     # noqa: E731
+    for need in ((1, 1, 1, 1), (1, 0, 0, 0), (0, 1, 1, 0), (0, 0, 1, 0), (0, 0, 0, 1), (1, 0, 1, 1)):
+        for acc in (0, 1):
+            old = [torch.randn_like(w.float()) if acc and i else torch.full_like(w.float(), math.nan)
+                   for i, w in enumerate(want)]
+            out = [t.clone() for t in old]
+            args = [v for t, on in zip(out, need) for v in (ptr(t) if on else (None, 0))]
+            n._call("hf_gated_grad", *ptr(X), None, 0, *ptr(Wg), *ptr(Wu), *ptr(Wd),
+                    H.HF_KEEP_FULL, *ptr(kept), None, 0, *ptr(dY), T, *args, acc)
+            for i, (o, t, w, b) in enumerate(zip(out, old, want, bound)):
+                if not need[i]:
+                    assert torch.equal(o.view(torch.int32), t.view(torch.int32))
+                    continue
+                w = w + t.double() if acc and i else w
+                # (one more rounding, of the sum, where it is added to)
+                G.close(o, w, b + 2 * G.S * (w.abs() + b) * acc, "%s of %s" % (i, need))
+
+
 def test_no_rows():
     n = net(8, 64, 96)
     X, Wg, Wu, Wd, dY = G.inputs(0, 64, 96, torch.bfloat16)

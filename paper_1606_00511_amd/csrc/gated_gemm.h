@@ -274,17 +274,21 @@ __device__ __forceinline__ E* stages() {
   return lds;
 }
 
-// What a workgroup computes of product s: tile (tm, tn) over nblk K blocks from vb0 on,
-// and where its partial goes, element (n - on, m - om); null: to s's output.
+// A tile's share of K for a workgroup that has several in turn: nblk K blocks from vb0 on
+// of tile (tm, tn), and where their partial goes, rows of the tile's columns; null: to the
+// product's output.
 struct Piece {
   int tid, tm, tn, vb0, nblk;
   float* part;
-  long long ldp;
-  int om, on;
 };
+// The tile of workgroup L of product s, or (PIECE) what p says.  (Both are this function:
+// with the other's tile handed over as a piece too, "up" of 8,192 rows, 4,096 x 16,384,
+// took 1,865 us for 1,818.)
 // E: the operands' type, O: the output's, ACT: the activation of "up" and "dh"
-template <class E, class O, int MODE, int ACT, int WM, int WN, int GM, int GN, int S>
-__device__ __forceinline__ void ggemm_piece(const GGemm& s, const GEpi& e, const Piece& p) {
+template <class E, class O, int MODE, int ACT, int WM, int WN, int GM, int GN, int S,
+          bool PIECE = false>
+__device__ __forceinline__ void ggemm_body(const GGemm& s, const GEpi& e, int L,
+                                           const Piece& p = Piece()) {
   constexpr bool AKC = MODE == UP || MODE == DOWN, BKC = MODE != DW;
   constexpr int BK = 128 / (int)sizeof(E);
   constexpr int NW = GM * GN;
@@ -295,12 +299,25 @@ __device__ __forceinline__ void ggemm_piece(const GGemm& s, const GEpi& e, const
   constexpr int STAGE = TA::SIZE + TB::SIZE;
   constexpr int ALL = S * STAGE;
 
-  const int lane = p.tid & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(p.tid >> 6);
+  const int tid = PIECE ? p.tid : threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wave / GN, wn = wave % GN;
   const int li = lane & 31, h = lane >> 5;
-  const int m0 = s.m0 + p.tm * RM, n0 = p.tn * RN;
-  const int vb0 = p.vb0, nblk = p.nblk;
+  const int gx = (s.M - s.m0 + RM - 1) / RM, gy = (s.N + RN - 1) / RN;
+  int tm = p.tm, tn = p.tn, tz = 0;
+  if (!PIECE && !tile_at(L, gx, gy, s.splits, tm, tn, tz)) return;
+  const int m0 = s.m0 + tm * RM, n0 = tn * RN;
+
+  const int nvb = s.K / BK;
+  int vb0 = 0, nblk = nvb;
+  if (PIECE) {
+    vb0 = p.vb0;
+    nblk = p.nblk;
+  } else if (s.splits > 1) {
+    const int per = (nvb + s.splits - 1) / s.splits;
+    vb0 = min(tz * per, nvb);
+    nblk = min(nvb, vb0 + per) - vb0;
+  }
 
   typename SumT<E>::T acc[WM][WN];
 #pragma unroll
@@ -377,7 +394,9 @@ __device__ __forceinline__ void ggemm_piece(const GGemm& s, const GEpi& e, const
   constexpr int RL = 32 * WM;
   static_assert(NW * 32 * RL * 4 <= S * STAGE * (int)sizeof(E), "staging exceeds the stages");
   float* const mine = (float*)stages<E, ALL>() + wave * 32 * RL;
-  const bool parts = (MODE == DOWN || MODE == DX || MODE == DW) && p.part;
+  const bool parts = (MODE == DOWN || MODE == DX || MODE == DW) && (PIECE ? p.part : e.part);
+  float* const part = PIECE ? p.part : parts ? e.part + (size_t)tz * gy * RN * e.ldp : nullptr;
+  const int on = PIECE ? n0 : 0, om = PIECE ? m0 : s.m0;    // its first row and column
   // whether all of the tile's rows and features exist
   const int fw = MODE == UP ? mt / 2 : mt;
   const bool full = (MODE == UP || MODE == DH) && n0 + RN <= e.T &&
@@ -439,8 +458,8 @@ __device__ __forceinline__ void ggemm_piece(const GGemm& s, const GEpi& e, const
       stage(b);
       const int nb = nt + 32 * b;
       if (parts) {
-        store_part<float, RL>(mine, lane, p.part, p.ldp, nb - p.on, s.N - p.on, mt - p.om,
-                              s.M - p.om, 0);
+        store_part<float, RL>(mine, lane, part, PIECE ? RM : e.ldp, nb - on, s.N - on, mt - om,
+                              s.M - om, 0);
       } else if constexpr (sizeof(E) == 1) {
         scaled_part<O, RL>(mine, lane, e, nb, mt, sm);
       } else {
@@ -452,30 +471,6 @@ __device__ __forceinline__ void ggemm_piece(const GGemm& s, const GEpi& e, const
       staged_fence();
     }
   }
-}
-
-// The tile and split of workgroup L of product s.
-template <class E, class O, int MODE, int ACT, int WM, int WN, int GM, int GN, int S>
-__device__ __forceinline__ void ggemm_body(const GGemm& s, const GEpi& e, int L) {
-  constexpr int RM = 32 * WM * GM, RN = 32 * WN * GN, BK = 128 / (int)sizeof(E);
-  const int gx = (s.M - s.m0 + RM - 1) / RM, gy = (s.N + RN - 1) / RN;
-  Piece p;
-  int tz;
-  if (!tile_at(L, gx, gy, s.splits, p.tm, p.tn, tz)) return;
-  p.tid = threadIdx.x;
-  const int nvb = s.K / BK;
-  p.vb0 = 0;
-  p.nblk = nvb;
-  if (s.splits > 1) {
-    const int per = (nvb + s.splits - 1) / s.splits;
-    p.vb0 = min(tz * per, nvb);
-    p.nblk = min(nvb, p.vb0 + per) - p.vb0;
-  }
-  p.part = e.part ? e.part + (size_t)tz * gy * RN * e.ldp : nullptr;
-  p.ldp = e.ldp;
-  p.om = s.m0;
-  p.on = 0;
-  ggemm_piece<E, O, MODE, ACT, WM, WN, GM, GN, S>(s, e, p);
 }
 
 }  // namespace

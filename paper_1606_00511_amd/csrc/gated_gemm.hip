@@ -46,11 +46,8 @@ __device__ __forceinline__ void shares_body(const GGrads& a) {
     p.vb0 = at - a.work[i] - r * nvb;
     p.nblk = min(nvb - p.vb0, end - at);
     p.part = p.nblk == nvb ? nullptr : a.part + (size_t)(2 * u + (p.vb0 == 0)) * (RM * RN);
-    p.ldp = RM;
-    p.om = p.tm * RM;
-    p.on = p.tn * RN;
-    if (i == 0) ggemm_piece<E, E, DX, GA_RELU, WM, WN, GM, GN, 2>(g, e, p);
-    else ggemm_piece<E, E, DW, GA_RELU, WM, WN, GM, GN, 2>(g, e, p);
+    if (i == 0) ggemm_body<E, E, DX, GA_RELU, WM, WN, GM, GN, 2, true>(g, e, 0, p);
+    else ggemm_body<E, E, DW, GA_RELU, WM, WN, GM, GN, 2, true>(g, e, 0, p);
     at += p.nblk;
     __syncthreads();       // the stages are free
   }

@@ -225,10 +225,14 @@ inline double parts_us(double bytes) {
 constexpr int SPLITS[] = {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 48, 64};
 // of K a split takes at least so many columns
 inline int64_t split_k(int type) { return type == VT_F32 ? 64 : type == VT_BF16 ? 128 : 256; }
-Shape shape_of(int type, int64_t M, int64_t N, int64_t K, bool split, int shapes) {
+// last: the last columns of a product, which tiles of fewer rows spread over more units
+// (3,001 rows, up of 1,021 x 2,731, bf16: 17.2 -> 11.0 us; 5,000 rows, 1,500 x 5,000: 24.9
+// -> 17.7)
+Shape shape_of(int type, int64_t M, int64_t N, int64_t K, bool split, int shapes,
+               bool last = false) {
   Shape best = {0, 1, 1e300};
   const double mem = (double)(M + N) * K * es_of(type) / BYTES_US + 4.0;
-  for (int tile = 0; tile < (N <= FEW_ROWS ? shapes : std::min(shapes, 2)); ++tile) {
+  for (int tile = 0; tile < (last || N <= FEW_ROWS ? shapes : std::min(shapes, 2)); ++tile) {
     const int64_t RM = tile_m(tile), RN = tile_n(tile), slots = tile == TILE_BIG ? 256 : 512;
     const int64_t tiles = (M + RM - 1) / RM * ((N + RN - 1) / RN);
     for (int s : SPLITS) {
@@ -260,7 +264,7 @@ void ranged(GGemm g, int type, bool split, int shapes, Run run) {
     const int64_t whole = ((M + rm - 1) / rm * tn) / slots * slots / tn * rm;
     if (whole <= 0 || whole >= M) continue;
     const Shape x = shape_of(type, whole, N, K, split, shapes);
-    const Shape y = shape_of(type, M - whole, N, K, split, shapes);
+    const Shape y = shape_of(type, M - whole, N, K, split, shapes, true);
     if (x.us + y.us + 4.0 < least) {
       least = x.us + y.us + 4.0;
       a = x;

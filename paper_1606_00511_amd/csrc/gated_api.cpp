@@ -534,9 +534,10 @@ int hf_gated_forward(hf_gated* c, const void* X, int64_t ldx, const void* Wg, in
     else gated_few_up(L, c->type, gu, eu);
     if (keep == HF_KEEP_CODES) {
       int8_t* k = (int8_t*)kept;
-      gated_pack(L, VT_F32, eu.kept, 2 * F, T, F, k, ldk, scale, lds);
-      gated_pack(L, VT_F32, (const float*)eu.kept + F, 2 * F, T, F, k + F, ldk,
-                 scale + blocks_of(F), lds);
+      const int once = F % CODE_BLOCK ? F : 2 * F;     // (no block has both g and u)
+      for (int f = 0; f < 2 * F; f += once)
+        gated_pack(L, VT_F32, (const float*)eu.kept + f, 2 * F, T, once, k + f, ldk,
+                   scale + blocks_of(f), lds);
     }
     set_out(&ed, Y, ldy, T, D);
     if (T > TWO_X && D == Dp && F == Fp && loads16(Wd, ldd, es)) {

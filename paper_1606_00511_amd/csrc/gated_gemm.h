@@ -215,6 +215,24 @@ __device__ __forceinline__ void dh_full(const float* s, int lane, const GEpi& e,
     staged_fence();
   }
 }
+// what is kept of row n's features from f on, of which there are `have`
+template <class E>
+__device__ __forceinline__ void get_kept(const GEpi& e, int n, int f, int have, float (&g)[8],
+                                         float (&u)[8]) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) g[j] = u[j] = 0.0f;
+  if (have <= 0) return;
+  if (e.keep == KEEP_FULL) {
+    const E* p = (const E*)e.kept + (size_t)n * e.ldk + f;
+    get(p, g, have);
+    get(p + e.F, u, have);
+  } else {
+    const int8_t* p = (const int8_t*)e.kept + (size_t)n * e.ldk + f;
+    const uint8_t* ks = e.ks + (size_t)n * e.ldks + f / CODE_BLOCK;
+    get_codes(p, code_step(ks[0]), g, have);
+    get_codes(p + e.F, code_step(ks[(e.F + CODE_BLOCK - 1) / CODE_BLOCK]), u, have);
+  }
+}
 // 32 rows from n0 of "dh", any below Np and of any features
 template <class E, int WM, int ACT>
 __device__ __forceinline__ void dh_rows(const float* s, int lane, const GEpi& e, int n0, int f0,
@@ -229,20 +247,7 @@ __device__ __forceinline__ void dh_rows(const float* s, int lane, const GEpi& e,
     const int have = n < e.T ? e.F - f : 0;
     float d[8], g[8], u[8];
     staged8<RL>(s, r, 2 * fc, d);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) g[j] = u[j] = 0.0f;
-    if (have > 0) {
-      if (e.keep == KEEP_FULL) {
-        const E* p = (const E*)e.kept + (size_t)n * e.ldk + f;
-        get(p, g, have);
-        get(p + e.F, u, have);
-      } else {
-        const int8_t* p = (const int8_t*)e.kept + (size_t)n * e.ldk + f;
-        const uint8_t* ks = e.ks + (size_t)n * e.ldks + f / CODE_BLOCK;
-        get_codes(p, code_step(ks[0]), g, have);
-        get_codes(p + e.F, code_step(ks[(e.F + CODE_BLOCK - 1) / CODE_BLOCK]), u, have);
-      }
-    }
+    get_kept<E>(e, n, f, have, g, u);
     dh_chunk<E, ACT, false>(e, n, f, have, d, g, u);
   }
 }

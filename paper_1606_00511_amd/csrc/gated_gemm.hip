@@ -7,6 +7,40 @@ namespace hfk {
   HF_GGEMM_FEW(NAME##_f32, float, float, MODE, GA_RELU)     \
   HF_GGEMM_FEW(NAME##_bf16, bf16_t, bf16_t, MODE, GA_RELU)
 HF_GGEMM_T(hf_gated_down, DOWN)
+// dh = dY Wd of few rows, by partials (a product like dX's of one matrix), and what "dh"
+// makes of their sum: a tile's whole K on one unit is a chain of reads that wait for
+// memory, 0.7 us a block of 128 bytes, and few rows have few tiles
+HF_GGEMM_T(hf_gated_dh_part, DX)
+template <class E>
+__device__ __forceinline__ void dh_sum_body(const GGemm& g, const GEpi& e, long long stride) {
+  const uint32_t chunks = (uint32_t)e.Fp / 8, i = blockIdx.x * 256u + threadIdx.x;
+  const int n = (int)(i / chunks), f = 8 * (int)(i % chunks);
+  if (n >= g.N) return;
+  const int have = n < e.T ? e.F - f : 0;
+  const float* p = e.part + (size_t)n * e.ldp + f;
+  float d[8], gv[8], u[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) d[j] = 0.0f;
+  get_kept<E>(e, n, f, have, gv, u);
+#pragma unroll 4
+  for (int s = 0; s < g.splits; ++s) {
+    const f32x4 a = *(const f32x4*)(p + s * stride), b = *(const f32x4*)(p + s * stride + 4);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      d[j] += a[j];
+      d[4 + j] += b[j];
+    }
+  }
+  with_act(e.act, [&](auto act) { dh_chunk<E, act.value, false>(e, n, f, have, d, gv, u); });
+}
+extern "C" __global__ __launch_bounds__(256) void hf_gated_dh_sum_f32(GGemm g, GEpi e,
+                                                                      long long stride) {
+  dh_sum_body<float>(g, e, stride);
+}
+extern "C" __global__ __launch_bounds__(256) void hf_gated_dh_sum_bf16(GGemm g, GEpi e,
+                                                                       long long stride) {
+  dh_sum_body<bf16_t>(g, e, stride);
+}
 // dX, dWd and dWg with dWu in one launch, its workgroups in this order: they need
 // nothing of each other, and the last ones of a product leave no unit idle while
 // another's begin
@@ -99,6 +133,16 @@ void gated_up(const Launch& L, int type, const GGemm& g, const GEpi& e) {
 }
 void gated_dh(const Launch& L, int type, const GGemm& g, const GEpi& e) {
   launch(L, "hf_gated_dh", act_kernels(e.act).dh[type], g, e);
+}
+void gated_dh_split(const Launch& L, int type, const GGemm& g, const GEpi& e) {
+  static const GKernel k[2][4] = {HF_GK_FEW(hf_gated_dh_part_f32), HF_GK_FEW(hf_gated_dh_part_bf16)};
+  launch(L, "hf_gated_dh_part", k[type], g, e);
+  const int rn = tile_n(g.tile), grid = (int)(((long long)g.N * (e.Fp / 8) + 255) / 256);
+  prof_begin(L, "hf_gated_dh_sum");
+  hipExtLaunchKernelGGL((type == VT_F32 ? hf_gated_dh_sum_f32 : hf_gated_dh_sum_bf16), dim3(grid),
+                        dim3(256), 0, L.stream, prof_a(L), prof_b(L), 0, g, e,
+                        (long long)((g.N + rn - 1) / rn) * rn * e.ldp);
+  prof_end(L, "hf_gated_dh_sum", 0.0, 0.0);
 }
 void gated_down(const Launch& L, int type, int out_type, const GGemm& g, const GEpi& e) {
   static const GKernel k[2][4] = {HF_GK_FEW(hf_gated_down_f32), HF_GK_FEW(hf_gated_down_bf16)};

@@ -84,6 +84,8 @@ void gated_few_up(const Launch& L, int type, const GGemm& g, const GEpi& e);
 void gated_few_down(const Launch& L, int type, int out_type, const GGemm& g, const GEpi& e);
 // dh = dY Wd in the tile, from it and what is kept h, dg and du
 void gated_dh(const Launch& L, int type, const GGemm& g, const GEpi& e);
+// the same by partials of dh (g.splits, e.part)
+void gated_dh_split(const Launch& L, int type, const GGemm& g, const GEpi& e);
 // The gradients from dg, du and h: dX = dg Wg + du Wu, dWd = dY^T h, and dWg = dg^T X
 // with dWu = du^T X, each if its e.out is there; of one tile
 struct GGrads {

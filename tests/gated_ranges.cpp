@@ -130,6 +130,11 @@ void gated_dh(const Launch&, int type, const GGemm& g, const GEpi& e) {
   rect("kept", e.kept, e.T, e.ldk, 2 * e.F, e.keep == KEEP_FULL ? es : 1);
   if (e.keep == KEEP_CODES) rect("kept's scale", e.ks, e.T, e.ldks, 2 * blocks_of(e.F), 1);
 }
+void gated_dh_split(const Launch& L, int type, const GGemm& g, const GEpi& e) {
+  gated_dh(L, type, g, e);
+  within("partials", e.part, part_floats(g, e) * 4, 16);
+  equal("one matrix", g.kh >= g.K, 1);
+}
 void gated_grads(const Launch&, int type, GGrads a) {
   const int es = es_of(type);
   const size_t tile = tile_m(a.g[0].tile) * tile_n(a.g[0].tile);

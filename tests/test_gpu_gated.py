@@ -149,7 +149,7 @@ def test_grad(type, T, D, F):
 
 @pytest.mark.parametrize("type", ["fp32", "bf16"])
 @pytest.mark.parametrize("act", ACTS)
-@pytest.mark.parametrize("T,D,F", [(45, 100, 130), (192, 128, 256)])
+@pytest.mark.parametrize("T,D,F", [(45, 100, 130), (192, 128, 256), (33, 2100, 70), (192, 2048, 256)])
 def test_grad_of_codes(type, act, T, D, F):
     """From 8-bit checkpoints of g, u and X: the gradient of the numbers they
     stand for."""

@@ -478,11 +478,13 @@ def test_streams():
     assert all(torch.equal(y, want[i % 2]) for i, y in enumerate(got))
 
 
-@pytest.mark.parametrize("type,T", [("bf16", 5), ("bf16", 300), ("fp32", 70)])
-def test_graph(type, T):
+# (the last two: dh by partials, shares of K)
+@pytest.mark.parametrize("type,T,D,F", [("bf16", 5, 128, 320), ("bf16", 300, 128, 320),
+                                        ("fp32", 70, 128, 320), ("fp32", 14, 1088, 1152),
+                                        ("fp32", 896, 256, 7466)])
+def test_graph(type, T, D, F):
     """A captured training step (forward, gradients) and a captured serving step,
     replayed with other inputs, eager calls of the same context between."""
-    D, F = 128, 320
     dt = G.TYPES[type]
     n = net(T, D, F, type)
     X, Wg, Wu, Wd, dY = G.inputs(T, D, F, dt)

@@ -585,9 +585,8 @@ const char* hf_vocab_last_error(const hf_vocab* ctx);
  * A context (hf_gated) holds D, F, the activation phi and the type of the
  * rows, the matrices and their gradients: fp32 or bf16 (sums and the activation
  * are fp32; h, and in the gradient dg and du, are rounded to the type for the
- * product that reads them, with bf16 forward calls of up to 16 rows and
- * gradients of up to 128 to two terms of it, or not at all; each output is
- * rounded to its type once).  Matrices are row-major; rows may lie `ld` elements
+ * product that reads them, with bf16 calls of up to 128 rows to two terms of it,
+ * or not at all; each output is rounded to its type once).  Matrices are row-major; rows may lie `ld` elements
  * apart and start at any element (forward calls of up to 64 rows read them in
  * place, others rows of 16-byte multiples and widths that are multiples of 64,
  * of codes 128; what lies otherwise is copied to the workspace first).  Columns

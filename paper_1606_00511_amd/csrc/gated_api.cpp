@@ -17,9 +17,9 @@ using namespace hfk;
 
 namespace {
 
-// bf16 gradients of at most so many rows hold h, dg and du as two bf16 terms, the
-// second what the first's rounding left (forward calls: up to TWO_X rows): with few
-// rows little averages a rounding away, and the matrix cores wait for the matrices
+// bf16 calls of at most so many rows hold h, and in the gradient dg and du, as two bf16
+// terms, the second what the first's rounding left: h's is half of what Y is off by (2-norm
+// 0.0023 with it, 0.0017 without), and up to here the matrix cores wait for the matrices
 // anyway.
 constexpr int TWO_TERM_ROWS = 128;
 constexpr size_t WPACK_BYTES = (size_t)64 << 20;   // packed channels of a product of codes
@@ -61,9 +61,9 @@ struct hf_gated : hfk::CallContext {
 
 namespace {
 
-// rows apart of the second terms, 0 where there are none
-inline int two_term(const hf_gated* c, int64_t T) {
-  return c->type == VT_BF16 && T > 0 && T <= TWO_TERM_ROWS ? (int)up(T, 64) : 0;
+// whether a call of T rows has second terms
+inline bool two_term(const hf_gated* c, int64_t T) {
+  return c->type == VT_BF16 && T > 0 && T <= TWO_TERM_ROWS;
 }
 
 void plan(const hf_gated* c, int64_t R, Layout* l) {
@@ -283,19 +283,20 @@ void ranged(GGemm g, int type, bool split, int shapes, Run run) {
   g.splits = b.splits;
   run(g);
 }
-// a product into e's out: straight, or by partials
+// a product into e's out: straight, or by partials; dup > 0: the rows of second terms
+// are dup rows further down and join the first ones'
 template <class Kernel>
 void summed(hf_gated* c, const Launch& L, int type, int out_type, const GGemm& all, const GEpi& out,
-            int shapes, Kernel kernel) {
+            int dup, int shapes, Kernel kernel) {
   ranged(all, type, true, shapes, [&](const GGemm& g) {
     GEpi e = out;
-    if (g.splits > 1) {
+    if (g.splits > 1 || dup) {
       e.part = c->at<float>(c->lay.part);
       e.ldp = g.M - g.m0;
     }
     kernel(g, e);
     if (!e.part) return;
-    const GFinish f = {g, e, 0, 0, 0};
+    const GFinish f = {g, e, dup, 0, 0};
     gated_finish(L, type, out_type, &f, 1);
   });
 }
@@ -512,13 +513,14 @@ int hf_gated_forward(hf_gated* c, const void* X, int64_t ldx, const void* Wg, in
   const Launch L{c->stream, nullptr};
   const Layout& l = c->lay;
   const int T = (int)rows, D = c->D, F = c->F, Dp = c->Dp, Fp = c->Fp, es = c->es;
+  const int dup = two_term(c, T) ? T : 0;        // (h's second terms: the next T rows)
   if (T <= FEW_X) {
     GGemm gu = product(F, T, D), gd = product(D, T, F);
     GEpi eu = epilogue(c, T), ed = epilogue(c, T);
     operands(&gu, Wg, ldg, Wu, ldu, X, ldx);
     eu.h = c->at<void>(l.h);
     eu.ldh = c->ldh();
-    eu.dup = ed.dup = T <= TWO_X ? TWO_X : 0;
+    eu.dup = ed.dup = dup;
     // (of one row h is fp32, unless its rows of Wd are short)
     const bool one = T == 1 && F * es > ONE_BYTES;
     eu.h32 = one;
@@ -540,11 +542,12 @@ int hf_gated_forward(hf_gated* c, const void* X, int64_t ldx, const void* Wg, in
                    scale + blocks_of(f), lds);
     }
     set_out(&ed, Y, ldy, T, D);
-    if (T > TWO_X && D == Dp && F == Fp && loads16(Wd, ldd, es)) {
+    if (T > FEW_DOWN && D == Dp && F == Fp && loads16(Wd, ldd, es)) {
       // (each row of h once for 128 of Wd's: 24 rows, 4,096 x 16,384: 45 -> 40 us with
       // the partials)
+      gd = product(D, T + dup, F);
       operands(&gd, Wd, ldd, nullptr, 0, eu.h, eu.ldh);
-      summed(c, L, c->type, c->type, gd, ed, 4, [&](const GGemm& g, const GEpi& e) {
+      summed(c, L, c->type, c->type, gd, ed, dup, 4, [&](const GGemm& g, const GEpi& e) {
         gated_down(L, c->type, c->type, g, e);
       });
     } else {
@@ -554,8 +557,9 @@ int hf_gated_forward(hf_gated* c, const void* X, int64_t ldx, const void* Wg, in
     }
     return end(c);
   }
-  GGemm gu = product(2 * Fp, T, Dp), gd = product(Dp, T, Fp);
+  GGemm gu = product(2 * Fp, T, Dp), gd = product(Dp, T + dup, Fp);
   GEpi eu = epilogue(c, T), ed = epilogue(c, T);
+  eu.dup = dup;
   Pads pads;
   gu.B = pads.operand(D == Dp && loads16(X, ldx, es), X, ldx, T, D, es, c->at<void>(l.xp), T, Dp, 1,
                       &gu.ldb);
@@ -580,7 +584,7 @@ int hf_gated_forward(hf_gated* c, const void* X, int64_t ldx, const void* Wg, in
   gd.B = eu.h;
   gd.ldb = c->ldh();
   set_out(&ed, Y, ldy, T, D);
-  summed(c, L, c->type, c->type, gd, ed, 4, [&](const GGemm& g, const GEpi& e) {
+  summed(c, L, c->type, c->type, gd, ed, dup, 4, [&](const GGemm& g, const GEpi& e) {
     gated_down(L, c->type, c->type, g, e);
   });
   return end(c);
@@ -626,7 +630,7 @@ int hf_gated_grad(hf_gated* c, const void* X, int64_t ldx, const uint8_t* xscale
   const Launch L{c->stream, nullptr};
   const Layout& l = c->lay;
   const int T = (int)rows, D = c->D, F = c->F, Dp = c->Dp, Fp = c->Fp, es = c->es, type = c->type;
-  const int dup = two_term(c, T);
+  const int dup = two_term(c, T) ? (int)up(T, 64) : 0;    // (rows are K: whole K blocks)
   const int Tp = (int)up(T, 64), Kt = dup ? 2 * dup : Tp, T0 = T / 64 * 64;
   GGrads all = {};
   GGemm &gx = all.g[0], &gd = all.g[1], &gw = all.g[2];
@@ -810,7 +814,7 @@ int hf_gated_product(hf_gated* c, const int8_t* A, int64_t lda, const float* sa,
   const Layout& l = c->lay;
   const int T = (int)rows, K = (int)up(k, CPAD);
   const bool place = k % CPAD == 0 && loads16(B, ldb, 1);
-  if (T <= (place ? TWO_X : FEW_X)) {
+  if (T <= (place ? FEW_DOWN : FEW_X)) {
     GGemm g = product((int)n, T, (int)k);
     GEpi e = epilogue(c, T);
     operands(&g, B, ldb, nullptr, 0, A, lda);
@@ -843,7 +847,7 @@ int hf_gated_product(hf_gated* c, const int8_t* A, int64_t lda, const float* sa,
     e.sn = sa;
     e.sm = sb + n0;
     set_out(&e, (char*)Y + n0 * c->es, ldy, T, nn);
-    summed(c, L, VT_I8, c->type, g, e, 4, [&](const GGemm& gg, const GEpi& ee) {
+    summed(c, L, VT_I8, c->type, g, e, 0, 4, [&](const GGemm& gg, const GEpi& ee) {
       gated_down(L, VT_I8, c->type, gg, ee);
     });
   }
@@ -873,7 +877,7 @@ int hf_gated_forward_codes(hf_gated* c, const void* X, int64_t ldx, const int8_t
   int8_t* hq = c->at<int8_t>(l.hq);
   float *sx = c->at<float>(l.sx), *sh = c->at<float>(l.sh);
   const bool few = T <= FEW_X, place = F == Fc && loads16(Wd, ldd, 1);
-  const bool few_down = few && (T <= TWO_X || !place);
+  const bool few_down = few && (T <= FEW_DOWN || !place);
   GGemm gu = few ? product(F, T, D) : product(2 * Fp, T, Dc);
   GGemm gd = few_down ? product(D, T, F) : product(c->Dp, T, Fc);
   GEpi eu = epilogue(c, T), ed = epilogue(c, T);
@@ -920,7 +924,7 @@ int hf_gated_forward_codes(hf_gated* c, const void* X, int64_t ldx, const int8_t
   } else if (few_down) {
     gated_few_down(L, VT_I8, c->type, gd, ed);
   } else {
-    summed(c, L, VT_I8, c->type, gd, ed, 4, [&](const GGemm& g, const GEpi& e) {
+    summed(c, L, VT_I8, c->type, gd, ed, 0, 4, [&](const GGemm& g, const GEpi& e) {
       gated_down(L, VT_I8, c->type, g, e);
     });
   }

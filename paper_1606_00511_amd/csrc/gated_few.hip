@@ -252,24 +252,24 @@ __device__ __forceinline__ void few_body(const GGemm& s, const GEpi& e) {
 // more than 16 rows of X with 32 where that leaves no unit without a workgroup (half
 // the reads of X: 24 rows, 4,096 x 16,384: 63 -> 54 us; 28 rows, 2,981 x 3,115, fp32, 98
 // workgroups: 54 us, 195: 36)
-#define HF_FEW(NAME, E, O, UP, RB, U32)                                                         \
+#define HF_FEW(NAME, E, O, UP, RB, U32, TWO)                                                    \
   extern "C" __global__ __launch_bounds__(512) void NAME##_32(GGemm s, GEpi e) {                \
-    few_body<E, O, UP, RB, 2, U32, 8, false>(s, e);                                             \
+    few_body<E, O, UP, RB, 2, U32, 8, TWO>(s, e);                                               \
   }                                                                                             \
   extern "C" __global__ __launch_bounds__(512) void NAME##_64(GGemm s, GEpi e) {                \
-    few_body<E, O, UP, RB, 4, 2, 8, false>(s, e);                                               \
+    few_body<E, O, UP, RB, 4, 2, 8, TWO>(s, e);                                                 \
   }
 #define HF_FEW_ALL(NAME, E, O, UP, TWO)                                                         \
   extern "C" __global__ __launch_bounds__(1024) void NAME##_16(GGemm s, GEpi e) {               \
     few_body<E, O, UP, 1, 1, 4, 16, TWO>(s, e);                                                 \
   }                                                                                             \
-  HF_FEW(NAME, E, O, UP, 1, 4)
+  HF_FEW(NAME, E, O, UP, 1, 4, TWO)
 HF_FEW_ALL(hf_gated_few_up_f32, float, float, true, false)
 HF_FEW_ALL(hf_gated_few_up_bf16, bf16_t, bf16_t, true, false)
 HF_FEW_ALL(hf_gated_few_up_codes, int8_t, float, true, false)
-HF_FEW(hf_gated_few_up2_f32, float, float, true, 2, 2)
-HF_FEW(hf_gated_few_up2_bf16, bf16_t, bf16_t, true, 2, 2)
-HF_FEW(hf_gated_few_up2_codes, int8_t, float, true, 2, 2)
+HF_FEW(hf_gated_few_up2_f32, float, float, true, 2, 2, false)
+HF_FEW(hf_gated_few_up2_bf16, bf16_t, bf16_t, true, 2, 2, false)
+HF_FEW(hf_gated_few_up2_codes, int8_t, float, true, 2, 2, false)
 HF_FEW_ALL(hf_gated_few_down_f32, float, float, false, false)
 HF_FEW_ALL(hf_gated_few_down_bf16, bf16_t, bf16_t, false, true)
 HF_FEW_ALL(hf_gated_few_down_codes_f32, int8_t, float, false, false)

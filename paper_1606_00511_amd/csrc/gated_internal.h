@@ -73,8 +73,9 @@ void gated_up(const Launch& L, int type, const GGemm& g, const GEpi& e);
 void gated_down(const Launch& L, int type, int out_type, const GGemm& g, const GEpi& e);
 // the same of up to FEW_X rows, in place at any alignment; "up" keeps codes as
 // fp32, its M is F, and of codes hmax has an entry for 16 columns; "down" of up to TWO_X
-// bf16 rows reads the second terms that "up" wrote, TWO_X rows further down
-constexpr int FEW_X = 64, TWO_X = 16;
+// bf16 rows reads the second terms that "up" wrote, e.dup rows further down.  (Aligned
+// rows of Wd are read by tiles from more than FEW_DOWN rows on.)
+constexpr int FEW_X = 64, TWO_X = FEW_X, FEW_DOWN = 16;
 // the same of one row, with rows of the matrices longer than ONE_BYTES: h is fp32 (also
 // of gated_few_up where h32), and "up" of codes leaves no hmax
 constexpr int ONE_BYTES = 2048;

@@ -705,7 +705,8 @@ int hf_gated_codes(hf_gated* ctx, const void* X, int64_t ldx, int64_t rows,
 
 /*
  * hf_gated_product: the product of two matrices of codes, y_tn = sa_t sb_n
- * sum_k A_tk B_nk, the sum exact in 32 bits, then rounded to fp32 and scaled.
+ * sum_k A_tk B_nk, the sum exact in 32 bits, then rounded to fp32 and scaled by
+ * one scale after the other, wherever in the type's range y is.
  *   A  rows x k codes, lda apart, with sa: rows fp32 scales
  *   B  n x k codes, ldb apart, with sb: n fp32 scales
  *   n  1 .. HF_GATED_MAX_OUT;  k  1 .. the larger of the context's widths

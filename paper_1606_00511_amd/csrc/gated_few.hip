@@ -186,9 +186,9 @@ __device__ __forceinline__ void few_body(const GGemm& s, const GEpi& e) {
         const int mm = min(m + r, e.F - 1);
         float gr, ur;
         if constexpr (sizeof(E) == 1) {
-          const float sn = e.sn[min(n, e.T - 1)];
-          gr = (float)g[r] * (sn * e.sm[mm]);
-          ur = (float)u[r] * (sn * e.sm1[mm]);
+          const RowFactor sn(e.sn[min(n, e.T - 1)]);
+          gr = sn.scaled(g[r], e.sm[mm]);
+          ur = sn.scaled(u[r], e.sm1[mm]);
         } else {
           gr = g[r];
           ur = u[r];
@@ -235,7 +235,7 @@ __device__ __forceinline__ void few_body(const GGemm& s, const GEpi& e) {
 #pragma unroll
       for (int r = 0; r < 4; ++r)
         if (m + r < e.mout) {
-          if constexpr (sizeof(E) == 1) store1(out + r, (float)g[r] * (e.sn[n] * e.sm[m + r]));
+          if constexpr (sizeof(E) == 1) store1(out + r, RowFactor(e.sn[n]).scaled(g[r], e.sm[m + r]));
           else store1(out + r, g[r]);
         }
     }

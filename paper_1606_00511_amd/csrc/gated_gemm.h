@@ -76,11 +76,11 @@ __device__ __forceinline__ void up_rows(const float* s, int lane, const GEpi& e,
     staged8<RL>(s, r, c, g);
     staged8<RL>(s, r, c + 8, u);
     if constexpr (I8) {
-      const float sn = e.sn[n];
+      const RowFactor sn(e.sn[n]);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        g[j] = (float)__float_as_int(g[j]) * (sn * sg[j]);
-        u[j] = (float)__float_as_int(u[j]) * (sn * su[j]);
+        g[j] = sn.scaled(__float_as_int(g[j]), sg[j]);
+        u[j] = sn.scaled(__float_as_int(u[j]), su[j]);
       }
     }
 #pragma unroll
@@ -265,9 +265,9 @@ __device__ __forceinline__ void scaled_part(const float* s, int lane, const GEpi
     if (n >= e.nout) break;
     float v[8];
     staged8<RL>(s, r, 2 * c, v);
-    const float sn = e.sn[n];
+    const RowFactor sn(e.sn[n]);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = (float)__float_as_int(v[j]) * (sn * sm[j]);
+    for (int j = 0; j < 8; ++j) v[j] = sn.scaled(__float_as_int(v[j]), sm[j]);
     put((O*)e.out + (size_t)n * e.ldo + m, v, have);
   }
 }

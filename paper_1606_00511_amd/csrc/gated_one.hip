@@ -154,8 +154,9 @@ __device__ __forceinline__ void one_body(const GGemm& s, const GEpi& e) {
   if (lane) return;
   float gr = (float)acc[0], ur = (float)acc[NA - 1];
   if constexpr (sizeof(E) == 1) {
-    gr *= e.sn[0] * e.sm[m];
-    if constexpr (UP) ur *= e.sn[0] * e.sm1[m];
+    const RowFactor sn(e.sn[0]);
+    gr = sn.scaled(acc[0], e.sm[m]);
+    if constexpr (UP) ur = sn.scaled(acc[1], e.sm1[m]);
   }
   if constexpr (UP) {
     if (sizeof(E) != 1 && e.keep != KEEP_NONE) {

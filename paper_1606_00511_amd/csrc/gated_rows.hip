@@ -96,9 +96,9 @@ __device__ __forceinline__ void finish_body(const FinishOne& one, uint32_t b, ui
           t[4 + j] += b[j];
         }
       }
-      const float sn = e.sn[n];
+      const RowFactor sn(e.sn[n]);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] = (float)t[j] * (sn * e.sm[min(m + j, e.mout - 1)]);
+      for (int j = 0; j < 8; ++j) v[j] = sn.scaled(t[j], e.sm[min(m + j, e.mout - 1)]);
     } else {
 #pragma unroll
       for (int j = 0; j < 8; ++j) v[j] = 0.0f;

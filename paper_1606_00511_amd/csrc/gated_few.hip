@@ -223,7 +223,7 @@ __device__ __forceinline__ void few_body(const GGemm& s, const GEpi& e) {
           *(uint2*)h = uint2{b[0] | b[1] << 16, b[2] | b[3] << 16};
           if (e.dup) {
 #pragma unroll
-            for (int r = 0; r < 4; ++r) b[r] = f2bf(v[r] - bf2f(b[r]));
+            for (int r = 0; r < 4; ++r) b[r] = f2bf(rest_of(v[r], b[r]));
             *(uint2*)(h + e.dup * e.ldh) = uint2{b[0] | b[1] << 16, b[2] | b[3] << 16};
           }
         } else {

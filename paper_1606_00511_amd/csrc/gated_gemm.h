@@ -38,7 +38,7 @@ __device__ __forceinline__ void put_term(bf16_t* p, const float (&v)[8], long lo
   if (!rest) return;
   float left[8];
 #pragma unroll
-  for (int j = 0; j < 8; ++j) left[j] = v[j] - bf2f(j & 1 ? w[j / 2] >> 16 : w[j / 2] & 0xffffu);
+  for (int j = 0; j < 8; ++j) left[j] = rest_of(v[j], j & 1 ? w[j / 2] >> 16 : w[j / 2] & 0xffffu);
   *(u32x4*)(p + rest) = f2bf8(left);
 }
 

@@ -35,6 +35,11 @@ struct RowFactor {
     return (float)sum * a * sb * c;
   }
 };
+// What v's rounding to the bf16 number b left; 0 where that is not finite (beside an
+// infinity its rest would be one of the other sign, or NaN).
+__device__ __forceinline__ float rest_of(float v, uint32_t b) {
+  return (b & 0x7f80u) == 0x7f80u ? 0.0f : v - bf2f(b);
+}
 // 8 values to p, of any alignment, the first `have` of them, and from it
 // (STREAM: past the caches)
 template <bool STREAM = false>

@@ -594,10 +594,10 @@ const char* hf_vocab_last_error(const hf_vocab* ctx);
  * inputs.
  * Memory, streams, the order of calls and errors as for hf_vocab; calls make no
  * allocation and can be captured into a graph.  hf_gated_pack, _unpack and
- * _codes use no workspace.  Repeated calls give the same bits (operands that lie
- * otherwise may be summed in another order).  Rows do not mix:
- * a row with a number that is not finite spoils its own results and the
- * matrices' gradients.
+ * _codes use no workspace, but keep the order of calls.  Repeated calls give the
+ * same bits (operands that lie otherwise may be summed in another order).  Rows
+ * do not mix: a row with a number that is not finite spoils its own results and
+ * the matrices' gradients.
  */
 typedef struct hf_gated hf_gated;
 

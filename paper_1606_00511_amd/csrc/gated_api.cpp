@@ -757,7 +757,7 @@ int hf_gated_pack(hf_gated* c, const void* X, int64_t ldx, int64_t rows, int64_t
       (rc = check_mat(c, X, ldx, cols, c->es, rows, "X")) ||
       (rc = check_mat(c, codes, ldc, cols, 1, rows, "codes")) ||
       (rc = check_mat(c, scale, lds, blocks_of(cols), 1, rows, "scale")) ||
-      (rc = check_apart(c, X, "X", codes, "codes", rows)))
+      (rc = check_apart(c, X, "X", codes, "codes", rows)) || (rc = follow(c, true)))
     return rc;
   gated_pack(Launch{c->stream, nullptr}, c->type, X, ldx, rows, (int)cols, codes, ldc, scale, lds);
   return end(c);
@@ -771,7 +771,7 @@ int hf_gated_unpack(hf_gated* c, const int8_t* codes, int64_t ldc, const uint8_t
       (rc = check_mat(c, codes, ldc, cols, 1, rows, "codes")) ||
       (rc = check_mat(c, scale, lds, blocks_of(cols), 1, rows, "scale")) ||
       (rc = check_mat(c, X, ldx, cols, c->es, rows, "X")) ||
-      (rc = check_apart(c, codes, "codes", X, "X", rows)))
+      (rc = check_apart(c, codes, "codes", X, "X", rows)) || (rc = follow(c, true)))
     return rc;
   gated_unpack(Launch{c->stream, nullptr}, c->type, codes, ldc, scale, lds, rows, (int)cols, X, ldx);
   return end(c);
@@ -785,7 +785,7 @@ int hf_gated_codes(hf_gated* c, const void* X, int64_t ldx, int64_t rows, int64_
       (rc = check_mat(c, X, ldx, cols, c->es, rows, "X")) ||
       (rc = check_mat(c, codes, ldc, cols, 1, rows, "codes")) ||
       (rc = check_mat(c, scale, 1, 1, 4, rows, "scale")) ||
-      (rc = check_apart(c, X, "X", codes, "codes", rows)))
+      (rc = check_apart(c, X, "X", codes, "codes", rows)) || (rc = follow(c, true)))
     return rc;
   gated_codes(Launch{c->stream, nullptr}, c->type, X, ldx, rows, (int)cols, codes, ldc, (int)cols,
               scale);

@@ -1,6 +1,9 @@
 // Activations of the gated block and their derivatives, of the product z itself.
 // Written without cancellation: gelu's and gelu_tanh's 1 + erf and 1 + tanh are
-// erfc and a sigmoid, so that values far below 0 keep their digits.
+// erfc and a sigmoid, so that values below 0 are off by about as many units of the
+// last place as their exponent is large (silu's, of z itself, by a few).  This ends
+// where the factor of z leaves fp32's normal numbers: values are within 2^-119 of 0
+// there (silu from -87 on, gelu from -12.9, gelu_tanh from -10), and soon are 0.
 #pragma once
 
 #include <type_traits>

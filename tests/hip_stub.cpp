@@ -36,6 +36,13 @@ extern "C" {
 
 const char* stub_log() { return text.c_str(); }
 void stub_clear() { text.clear(); }
+// the kernels of the library
+const char* stub_names() {
+  static std::string all;
+  all.clear();
+  for (const auto& n : names) all += n.second + "\n";
+  return all.c_str();
+}
 void stub_capture(void* stream, int on) {
   if (on) capturing.insert(stream);
   else capturing.erase(stream);

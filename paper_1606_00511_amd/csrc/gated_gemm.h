@@ -14,7 +14,7 @@
 // of its accumulators, and neither goes through memory.
 // Sums are fp32 (codes: int32, exact), the activation and its slope fp32; h, dg
 // and du are rounded to the type for the products that read them (few bf16
-// rows: to two terms of it, as few rows average no rounding away).
+// rows: to two terms of it, which cost little where the matrices bound a product).
 #pragma once
 
 #include "gated_act.h"

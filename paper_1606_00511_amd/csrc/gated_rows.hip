@@ -61,7 +61,7 @@ __device__ __forceinline__ void finish_body(const FinishOne& one, uint32_t b, ui
   const int dup = one.f.dup, end = min(e.mout, g.M);
   const uint32_t chunks = one.chunks;
   const long long stride = one.stride;
-  // (at most 2^30 chunks, of two matrices of 65,536 x 65,536)
+  // (at most 2^31 chunks, of 262,144 rows of 65,536, and 2^28 a step: below 2^32)
   const uint32_t total = (uint32_t)one.rows * chunks;
   for (uint32_t i = b * 256u + threadIdx.x; i < total; i += groups * 256u) {
     const int row = (int)(i / chunks), m = g.m0 + 8 * (int)(i % chunks);
@@ -445,7 +445,7 @@ void gated_finish(const Launch& L, int type, int out_type, const GFinish* f, int
 void gated_pack(const Launch& L, int type, const void* X, long long ldx, long long rows, int cols,
                 int8_t* codes, long long ldc, uint8_t* scale, long long lds) {
   const uint32_t per = (uint32_t)((cols + CODE_BLOCK - 1) / CODE_BLOCK * (CODE_BLOCK / 8));
-  const uint32_t total = (uint32_t)rows * per;      // below 2^31: 262,144 rows of 65,536
+  const uint32_t total = (uint32_t)rows * per;      // at most 2^31: 262,144 rows of 65,536
   if (!total) return;
   const bool much = rows * cols > L3_BYTES / 4;
   if (type == VT_F32)

@@ -19,8 +19,10 @@ constexpr size_t SPLIT_FLOATS = (size_t)32 << 20;   // partials of a split-K pro
 // longest of three and then some:
 //   products  a 256 x 256 tile has a compute unit to itself, two of the others
 //             share one; RATE: multiply-adds a us of a unit with them, measured
-//             at 8,192 x 8,192 x 2,048 (bf16) and 8,192 x 2,048 x 2,048 (fp32);
-//             filling the LDS and storing a tile take about 6 and 4 us more
+//             at 8,192 x 8,192 x 2,048 (bf16) and 8,192 x 2,048 x 2,048 (fp32), of
+//             codes taken as twice bf16's, as the matrix cores have it (4.3e6 is
+//             reached: 8,192 x 16,384 x 4,096 in 504 us); filling the LDS and
+//             storing a tile take about 6 and 4 us more
 //   memory    A once at 4.7 TB/s, which takes 5.5 MB on their way: AHEAD bytes
 //             of A per workgroup (32,000 x 1,024 of bf16 for 5 rows: 18.6 us
 //             with 250 tiles of 128 x 128, 13.6 with 250 of 128 x 64), and

@@ -695,7 +695,8 @@ int hf_gated_unpack(hf_gated* ctx, const int8_t* codes, int64_t ldc,
 /*
  * hf_gated_codes: rows of the type as 8-bit codes with a scale for each row (a
  * token's, or a matrix's channel's): s = max |x| / 127 in fp32, q = x / s
- * rounded to nearest, ties to even.  A row whose s is 0 (of zeros, or of numbers
+ * rounded to nearest, ties to even, in [-127, 127] (past which x / s may lie where
+ * s is below fp32's normal numbers).  A row whose s is 0 (of zeros, or of numbers
  * below 2^-143) has codes 0; one with a NaN or an infinity has s = NaN and codes
  * 0.
  *   X  rows x cols;  codes  rows x cols, ldc apart;  scale  rows fp32

@@ -87,3 +87,18 @@ def test_block_scales(T, D, F):
     sh = (h.abs().amax(1) / 127).float().double()
     want = times((h / sh[:, None]).round(), sh, q[2])
     assert float((Y.double() - want).norm()) <= 0.01 * float(want.norm())
+
+
+@pytest.mark.parametrize("cols", [100, 1024])
+def test_codes_of_the_smallest_numbers(cols):
+    """Rows whose scale is below fp32's normal numbers, rounded to few digits: codes of the
+    quotient by it, within 127."""
+    g = torch.Generator("cuda").manual_seed(cols)
+    X = torch.randn(40, cols, generator=g, device="cuda", dtype=torch.float64)
+    X = (X * torch.exp2(-115.0 - torch.arange(40, device="cuda").double())[:, None]).float()
+    codes, s = H.HFGated(64, 64, 1, dtype="fp32").hf_gated_codes(X)
+    want = (X.abs().amax(1).double() / 127).float()
+    assert torch.equal(s, want)
+    q = (X.double() / torch.where(want > 0, want, 1.0).double()[:, None]).round()
+    q = torch.where(want[:, None] > 0, q, 0.0).clamp(-127, 127)
+    assert torch.equal(codes.double(), q) and (s == 0).any() and (q.abs().amax(1) == 127).any()

@@ -588,10 +588,10 @@ const char* hf_vocab_last_error(const hf_vocab* ctx);
  * product that reads them, with bf16 calls of up to 128 rows to two terms of it,
  * or not at all; each output is rounded to its type once).  Matrices are row-major; rows may lie `ld` elements
  * apart and start at any element (forward calls of up to 64 rows read them in
- * place, others rows of 16-byte multiples and widths that are multiples of 64,
- * of codes 128; what lies otherwise is copied to the workspace first).  Columns
- * and rows around an output are left as they were.  Outputs may not overlap
- * inputs.
+ * place, but for bf16 ones of more than 32 with long rows of Wd; others rows of
+ * 16-byte multiples and widths that are multiples of 64, of codes 128; what lies
+ * otherwise is copied to the workspace first).  Columns and rows around an
+ * output are left as they were.  Outputs may not overlap inputs.
  * Memory, streams, the order of calls and errors as for hf_vocab; calls make no
  * allocation and can be captured into a graph.  hf_gated_pack, _unpack and
  * _codes use no workspace, but keep the order of calls.  Repeated calls give the

@@ -514,7 +514,11 @@ int hf_gated_forward(hf_gated* c, const void* X, int64_t ldx, const void* Wg, in
   const Layout& l = c->lay;
   const int T = (int)rows, D = c->D, F = c->F, Dp = c->Dp, Fp = c->Fp, es = c->es;
   const int dup = two_term(c, T) ? T : 0;        // (h's second terms: the next T rows)
-  if (T <= FEW_X) {
+  // Rows of Wd that tiles cannot read where they are: reading both terms of more than 32
+  // rows of h for every 16 of Wd's costs more than copies for tiles where rows are long (48
+  // rows, 1,021 x 2,731: 37 us, by copies 30; 2,001 x 5,003: 96, 52; 300 x 900: 16, 20).
+  const bool whole = D == Dp && F == Fp && loads16(Wd, ldd, es);
+  if (T <= FEW_X && (whole || !dup || T <= 32 || F <= 2048)) {
     GGemm gu = product(F, T, D), gd = product(D, T, F);
     GEpi eu = epilogue(c, T), ed = epilogue(c, T);
     operands(&gu, Wg, ldg, Wu, ldu, X, ldx);
@@ -542,7 +546,7 @@ int hf_gated_forward(hf_gated* c, const void* X, int64_t ldx, const void* Wg, in
                    scale + blocks_of(f), lds);
     }
     set_out(&ed, Y, ldy, T, D);
-    if (T > FEW_DOWN && D == Dp && F == Fp && loads16(Wd, ldd, es)) {
+    if (T > FEW_DOWN && whole) {
       // (each row of h once for 128 of Wd's: 24 rows, 4,096 x 16,384: 45 -> 40 us with
       // the partials)
       gd = product(D, T + dup, F);

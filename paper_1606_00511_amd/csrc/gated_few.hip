@@ -251,29 +251,31 @@ __device__ __forceinline__ void few_body(const GGemm& s, const GEpi& e) {
 // up to 16, 32 and 64 rows of X; "up" with 16 rows of both matrices a workgroup, and of
 // more than 16 rows of X with 32 where that leaves no unit without a workgroup (half
 // the reads of X: 24 rows, 4,096 x 16,384: 63 -> 54 us; 28 rows, 2,981 x 3,115, fp32, 98
-// workgroups: 54 us, 195: 36)
-#define HF_FEW(NAME, E, O, UP, RB, U32, TWO)                                                    \
-  extern "C" __global__ __launch_bounds__(512) void NAME##_32(GGemm s, GEpi e) {                \
-    few_body<E, O, UP, RB, 2, U32, 8, TWO>(s, e);                                               \
+// workgroups: 54 us, 195: 36).  With second terms a wave has half as much on its way and
+// up to twice as many share K (24 rows, 300 x 900: 14.5 -> 13.0 us; 869 x 3,110: 23.7 ->
+// 22.0).
+#define HF_FEW(NAME, E, O, UP, RB, U32, U64, W, TWO)                                            \
+  extern "C" __global__ __launch_bounds__(64 * W) void NAME##_32(GGemm s, GEpi e) {             \
+    few_body<E, O, UP, RB, 2, U32, W, TWO>(s, e);                                               \
   }                                                                                             \
-  extern "C" __global__ __launch_bounds__(512) void NAME##_64(GGemm s, GEpi e) {                \
-    few_body<E, O, UP, RB, 4, 2, 8, TWO>(s, e);                                                 \
+  extern "C" __global__ __launch_bounds__(64 * W) void NAME##_64(GGemm s, GEpi e) {             \
+    few_body<E, O, UP, RB, 4, U64, W, TWO>(s, e);                                               \
   }
-#define HF_FEW_ALL(NAME, E, O, UP, TWO)                                                         \
+#define HF_FEW_ALL(NAME, E, O, UP, U32, U64, W, TWO)                                            \
   extern "C" __global__ __launch_bounds__(1024) void NAME##_16(GGemm s, GEpi e) {               \
     few_body<E, O, UP, 1, 1, 4, 16, TWO>(s, e);                                                 \
   }                                                                                             \
-  HF_FEW(NAME, E, O, UP, 1, 4, TWO)
-HF_FEW_ALL(hf_gated_few_up_f32, float, float, true, false)
-HF_FEW_ALL(hf_gated_few_up_bf16, bf16_t, bf16_t, true, false)
-HF_FEW_ALL(hf_gated_few_up_codes, int8_t, float, true, false)
-HF_FEW(hf_gated_few_up2_f32, float, float, true, 2, 2, false)
-HF_FEW(hf_gated_few_up2_bf16, bf16_t, bf16_t, true, 2, 2, false)
-HF_FEW(hf_gated_few_up2_codes, int8_t, float, true, 2, 2, false)
-HF_FEW_ALL(hf_gated_few_down_f32, float, float, false, false)
-HF_FEW_ALL(hf_gated_few_down_bf16, bf16_t, bf16_t, false, true)
-HF_FEW_ALL(hf_gated_few_down_codes_f32, int8_t, float, false, false)
-HF_FEW_ALL(hf_gated_few_down_codes_bf16, int8_t, bf16_t, false, false)
+  HF_FEW(NAME, E, O, UP, 1, U32, U64, W, TWO)
+HF_FEW_ALL(hf_gated_few_up_f32, float, float, true, 4, 2, 8, false)
+HF_FEW_ALL(hf_gated_few_up_bf16, bf16_t, bf16_t, true, 4, 2, 8, false)
+HF_FEW_ALL(hf_gated_few_up_codes, int8_t, float, true, 4, 2, 8, false)
+HF_FEW(hf_gated_few_up2_f32, float, float, true, 2, 2, 2, 8, false)
+HF_FEW(hf_gated_few_up2_bf16, bf16_t, bf16_t, true, 2, 2, 2, 8, false)
+HF_FEW(hf_gated_few_up2_codes, int8_t, float, true, 2, 2, 2, 8, false)
+HF_FEW_ALL(hf_gated_few_down_f32, float, float, false, 4, 2, 8, false)
+HF_FEW_ALL(hf_gated_few_down_bf16, bf16_t, bf16_t, false, 2, 1, 16, true)
+HF_FEW_ALL(hf_gated_few_down_codes_f32, int8_t, float, false, 4, 2, 8, false)
+HF_FEW_ALL(hf_gated_few_down_codes_bf16, int8_t, bf16_t, false, 4, 2, 8, false)
 
 namespace {
 #define HF_FK(NAME) {NAME##_16, NAME##_32, NAME##_64}
@@ -288,12 +290,13 @@ const GKernel few_down[4][3] = {HF_FK(hf_gated_few_down_f32), HF_FK(hf_gated_few
                                 HF_FK(hf_gated_few_down_codes_bf16)};
 inline int size_of(int type) { return type == VT_F32 ? 4 : type == VT_BF16 ? 2 : 1; }
 
-// two: the kernels with 32 rows a workgroup, or null
+// two: the kernels with 32 rows a workgroup, or null; rest: X's rows have second terms
 void launch(const Launch& L, const char* name, const GKernel* one, const GKernel* two, int es,
-            const GGemm& g, const GEpi& e) {
+            bool rest, const GGemm& g, const GEpi& e) {
   const int i = g.N <= 16 ? 0 : g.N <= 32 ? 1 : 2;
   const bool rows32 = i > 0 && two && g.M > 255 * 32;
-  const int rb = rows32 ? 2 : 1, u = i == 2 || rows32 ? 2 : 4, most = i == 0 ? 16 : 8;
+  const int rb = rows32 ? 2 : 1, most = i == 0 || rest ? 16 : 8;
+  const int u = (i == 2 || rows32 ? 2 : 4) / (i > 0 && rest ? 2 : 1);
   const int grid = (g.M + 16 * rb - 1) / (16 * rb);
   // enough waves for 8 a compute unit, each with a group of K at least
   const int groups = (g.K * es + 64 * u - 1) / (64 * u);
@@ -307,11 +310,11 @@ void launch(const Launch& L, const char* name, const GKernel* one, const GKernel
 }  // namespace
 
 void gated_few_up(const Launch& L, int type, const GGemm& g, const GEpi& e) {
-  launch(L, "hf_gated_few_up", few_up[type], few_up2[type], size_of(type), g, e);
+  launch(L, "hf_gated_few_up", few_up[type], few_up2[type], size_of(type), false, g, e);
 }
 void gated_few_down(const Launch& L, int type, int out_type, const GGemm& g, const GEpi& e) {
   launch(L, "hf_gated_few_down", few_down[type == VT_I8 ? 2 + out_type : type], nullptr,
-         size_of(type), g, e);
+         size_of(type), type == VT_BF16, g, e);
 }
 
 }  // namespace hfk
